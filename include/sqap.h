@@ -340,6 +340,46 @@ sqap_status sqap_w4a4_linear(const uint8_t *Xq, const sqap_f16 *sx, int32_t M,
                              void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * The same linears in microscaled 4-bit floating point, the format that the matrix cores multiply as it is: 32
+ * consecutive channels share a scale 2^e, an element is one of 0, 1/2, 1, 3/2, 2, 3, 4, 6 with a sign.
+ * Codes: canonical packing (above), bit 3 the sign, bits 0-2 the element's place in that list.  A scale is the byte
+ * e + 127; 255 stands for a scale that is not a number.
+ *
+ * sqap_mx4_quantize: for output row i and each block of 32 channels, v taken from X[rows[i], :] (or X[i, :] when
+ * rows is NULL),
+ *   e    = floor(log2 max|v|) - 2  (0 when all are zero)
+ *   code = v / 2^e to the nearest element, halfway cases to the even code, at most 6; the sign is v's
+ * A block with an infinity or a NaN gets the scale 255 and codes of zero: everything computed from it is NaN.
+ * Serves activations and weights alike.  Xq: [M, K/2], Xs: [M, K/32].  ldx: row pitch of X in elements.  Row
+ * numbers are not range-checked.
+ * EINVAL: null pointer, M < 0, K <= 0, ldx < K.  EUNSUPPORTED: K not a multiple of 32, K > 1048576, X not 16-byte
+ * aligned or ldx not a multiple of 8, Xq not 4-byte aligned, more than 2^31 - 1 rows of 2048 channels.
+ *
+ * sqap_mx4_weight_pack: re-lays codes [N, K/2] (16-byte aligned) and scales [N, K/32], as the quantizer writes them
+ * or a checkpoint holds them, into the library's streaming layout and returns a handle that owns a device copy on
+ * the current device.  The inputs may be freed once the stream has run past this call.  EINVAL: null pointer,
+ * N, K <= 0.  EUNSUPPORTED: K not a multiple of 32 or above 1048576, N above 2^24.  ENOMEM / EDEVICE.
+ *
+ * sqap_mx4_linear: Y[m,n] = binary16(sum_k x[m,k] w[n,k]), x and w the values that codes and scales stand for.
+ * Products are exact, sums are binary32; their order depends on the shape, not on the call, so that a call gives the
+ * same bits every time.  A row whose blocks are finite is not touched by another that is not.  Xq: 16-byte aligned; Y: [M, N] half with pitch ldy >= N elements, of any
+ * alignment; what lies behind a row's N elements is left as it was.  Needs no workspace; may be captured.
+ * EINVAL: null pointer, not a handle, M < 0, ldy < N, a handle of another device than the current one.
+ * EUNSUPPORTED: Xq not 16-byte aligned, M above 2^24, or more than 2^30 tiles of 16 x 64 outputs.
+ */
+typedef struct sqap_mx4_weight sqap_mx4_weight;
+sqap_status sqap_mx4_quantize(const sqap_f16 *X, int64_t ldx, const int32_t *rows, int32_t M, int32_t K,
+                              uint8_t *Xq, uint8_t *Xs, void *stream);
+sqap_status sqap_mx4_weight_pack(const uint8_t *Wq, const uint8_t *Ws, int32_t N, int32_t K,
+                                 sqap_mx4_weight **out, void *stream);
+/* Frees a handle (NULL is allowed).  The caller makes sure no kernel still uses it. */
+sqap_status sqap_mx4_weight_free(sqap_mx4_weight *w);
+/* Shape and device footprint of a handle; any out pointer may be NULL. */
+sqap_status sqap_mx4_weight_info(const sqap_mx4_weight *w, int32_t *N, int32_t *K, size_t *device_bytes);
+sqap_status sqap_mx4_linear(const uint8_t *Xq, const uint8_t *Xs, int32_t M, const sqap_mx4_weight *W,
+                            sqap_f16 *Y, int64_t ldy, void *stream);
+
+/*
  * Decoder glue between the linears.  The paper runs its W4A4 linears inside a
  * Llama-2-7B decoder (Implementation Details; Section 3.3 takes Q and K from
  * it) and does not restate that architecture; the calls below follow the

@@ -28,6 +28,7 @@ EXPORTS = (
     "sqap_attention", "sqap_residual_add", "sqap_rope_append", "sqap_plan_linear_shares", "sqap_decode_attention", "sqap_group_info", "sqap_init",
     "sqap_set_persistent_kernels", "sqap_attn_scores_workspace_bytes", "sqap_attn_scores_noalloc", "sqap_set_mid_m_kernel", "sqap_decoder_create", "sqap_decoder_step", "sqap_decoder_status",
     "sqap_decoder_set_wait_limit", "sqap_decoder_free",
+    "sqap_mx4_quantize", "sqap_mx4_weight_pack", "sqap_mx4_weight_free", "sqap_mx4_weight_info", "sqap_mx4_linear",
 )
 
 
@@ -115,6 +116,11 @@ def lib():
                                                                       ctypes.POINTER(ctypes.c_double),
                                                                       ctypes.POINTER(ctypes.c_int32),
                                                                       ctypes.POINTER(ctypes.c_int32)]
+        L.sqap_mx4_quantize.argtypes = [vp, i64, vp, i32, i32, vp, vp, vp]
+        L.sqap_mx4_weight_pack.argtypes = [vp, vp, i32, i32, ctypes.POINTER(vp), vp]
+        L.sqap_mx4_weight_free.argtypes = [vp]
+        L.sqap_mx4_weight_info.argtypes = [vp, ctypes.POINTER(i32), ctypes.POINTER(i32), ctypes.POINTER(sz)]
+        L.sqap_mx4_linear.argtypes = [vp, vp, i32, vp, vp, i64, vp]
         for name in EXPORTS:
             if name not in ("sqap_last_error", "sqap_version", "sqap_workspace_bytes", "sqap_attn_scores_workspace_bytes"):
                 getattr(L, name).restype = ctypes.c_int32
@@ -392,6 +398,48 @@ def sqap_workspace_bytes(M, N, K):
 def sqap_w4a4_linear(Xq, sx, W, Y, acc_out=None, workspace=None, stream=None):
     """Xq [M,K/2] u8, sx [M] fp16, W: Weight -> Y [M,N] fp16 (+ acc_out [M,N] int32)."""
     _native.w4a4_linear(Xq, sx, W.handle, Y, acc_out, workspace, stream)
+
+
+class Mx4Weight:
+    """Owns a sqap_mx4_weight handle."""
+
+    def __init__(self, handle, N, K):
+        self.handle, self.N, self.K = handle, N, K
+
+    def free(self):
+        if self.handle:
+            _check(lib().sqap_mx4_weight_free(self.handle))
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+    @property
+    def device_bytes(self):
+        b = ctypes.c_size_t()
+        _check(lib().sqap_mx4_weight_info(self.handle, None, None, ctypes.byref(b)))
+        return b.value
+
+
+def sqap_mx4_quantize(X, rows, Xq, Xs, stream=None):
+    """X [S,K] fp16, rows int32 [M] or None -> Xq [M,K/2] u8, Xs [M,K/32] u8 (activations and weights alike)."""
+    _native.mx4_quantize(X, rows, Xq, Xs, stream)
+
+
+def sqap_mx4_weight_pack(Wq, Ws, stream=None):
+    """Wq [N,K/2] u8, Ws [N,K/32] u8 -> Mx4Weight."""
+    N, half = Wq.shape
+    h = ctypes.c_void_p()
+    _check(lib().sqap_mx4_weight_pack(_ptr(Wq), _ptr(Ws), N, 2 * half, ctypes.byref(h), _stream(stream)))
+    return Mx4Weight(h, N, 2 * half)
+
+
+def sqap_mx4_linear(Xq, Xs, W, Y, stream=None):
+    """Xq [M,K/2] u8, Xs [M,K/32] u8, W: Mx4Weight -> Y [M,N] fp16."""
+    _native.mx4_linear(Xq, Xs, W.handle, Y, stream)
 
 
 class Group:

@@ -632,6 +632,103 @@ sqap_status sqap_w4a4_linear(const uint8_t *Xq, const sqap_f16 *sx, int32_t M,
                               as_stream(stream));
 }
 
+// ---- microscaled 4-bit floating point
+
+static const Mx4Weight *check_mx4(const sqap_mx4_weight *w)
+{
+    const Mx4Weight *ww = reinterpret_cast<const Mx4Weight *>(w);
+    return ww && ww->magic == kMx4Magic ? ww : nullptr;
+}
+
+sqap_status sqap_mx4_quantize(const sqap_f16 *X, int64_t ldx, const int32_t *rows, int32_t M, int32_t K, uint8_t *Xq, uint8_t *Xs, void *stream)
+{
+    const char *who = "sqap_mx4_quantize";
+    if (M < 0 || K <= 0) return fail(SQAP_EINVAL, "%s: M %d, K %d", who, M, K);
+    if (ldx < K) return fail(SQAP_EINVAL, "%s: pitch %lld below K %d", who, (long long)ldx, K);
+    if (M == 0) return SQAP_OK;
+    if (!X || !Xq || !Xs) return fail(SQAP_EINVAL, "%s: null pointer", who);
+    if (K % 32 != 0 || K > kMx4MaxK) return fail(SQAP_EUNSUPPORTED, "%s: K = %d (a multiple of 32, <= %d)", who, K, kMx4MaxK);
+    if (!aligned16(X) || (ldx & 7)) return fail(SQAP_EUNSUPPORTED, "%s: X and its pitch must be 16-byte aligned", who);
+    if (reinterpret_cast<uintptr_t>(Xq) & 3u) return fail(SQAP_EUNSUPPORTED, "%s: Xq must be 4-byte aligned", who);
+    if ((int64_t)M * ((K / 8 + 255) / 256) > INT32_MAX) return fail(SQAP_EUNSUPPORTED, "%s: M = %d rows of K = %d", who, M, K);
+    return launch_mx4_quantize(reinterpret_cast<const __half *>(X), ldx, rows, M, K, Xq, Xs, as_stream(stream));
+}
+
+sqap_status sqap_mx4_weight_pack(const uint8_t *Wq, const uint8_t *Ws, int32_t N, int32_t K, sqap_mx4_weight **out, void *stream)
+{
+    const char *who = "sqap_mx4_weight_pack";
+    if (out) *out = nullptr;
+    if (N <= 0 || K <= 0) return fail(SQAP_EINVAL, "%s: N %d, K %d", who, N, K);
+    if (!Wq || !Ws || !out) return fail(SQAP_EINVAL, "%s: null pointer", who);
+    if (K % 32 != 0 || K > kMx4MaxK) return fail(SQAP_EUNSUPPORTED, "%s: K = %d (a multiple of 32, <= %d)", who, K, kMx4MaxK);
+    if (N > kMx4MaxRows) return fail(SQAP_EUNSUPPORTED, "%s: N = %d above %d", who, N, kMx4MaxRows);
+    if (!aligned16(Wq)) return fail(SQAP_EUNSUPPORTED, "%s: Wq must be 16-byte aligned", who);
+    Mx4Weight *w = new (std::nothrow) Mx4Weight();
+    if (!w) return fail(SQAP_ENOMEM, "%s: host allocation failed", who);
+    w->magic = kMx4Magic;
+    w->N = N;
+    w->K = K;
+    w->n_groups = (N + 255) / 256 * 16;
+    w->ksteps = (K + 255) / 256 * 2;
+    w->kquads = (w->ksteps + 3) / 4;
+    const size_t data_bytes = (size_t)w->n_groups * w->ksteps * 1024, scale_bytes = (size_t)w->n_groups * w->kquads * 256;
+    w->bytes = data_bytes + scale_bytes;
+    hipError_t e = hipGetDevice(&w->device);
+    if (e == hipSuccess) e = hipMalloc(reinterpret_cast<void **>(&w->data), data_bytes);
+    if (e == hipSuccess) e = hipMalloc(reinterpret_cast<void **>(&w->scales), scale_bytes);
+    sqap_status st = SQAP_OK;
+    if (e != hipSuccess) st = fail(e == hipErrorOutOfMemory ? SQAP_ENOMEM : SQAP_EDEVICE, "%s: %s", who, hipGetErrorString(e));
+    if (st == SQAP_OK) st = launch_mx4_pack(Wq, Ws, *w, as_stream(stream));
+    if (st != SQAP_OK) {
+        if (w->data) (void)hipFree(w->data);
+        if (w->scales) (void)hipFree(w->scales);
+        delete w;
+        return st;
+    }
+    *out = reinterpret_cast<sqap_mx4_weight *>(w);
+    return SQAP_OK;
+}
+
+sqap_status sqap_mx4_weight_free(sqap_mx4_weight *w)
+{
+    if (!w) return SQAP_OK;
+    Mx4Weight *ww = reinterpret_cast<Mx4Weight *>(w);
+    if (ww->magic != kMx4Magic) return fail(SQAP_EINVAL, "sqap_mx4_weight_free: not a weight handle");
+    ww->magic = 0;
+    const hipError_t e1 = hipFree(ww->data), e2 = hipFree(ww->scales);
+    delete ww;
+    if (e1 != hipSuccess || e2 != hipSuccess)
+        return fail(SQAP_EDEVICE, "sqap_mx4_weight_free: %s", hipGetErrorString(e1 != hipSuccess ? e1 : e2));
+    return SQAP_OK;
+}
+
+sqap_status sqap_mx4_weight_info(const sqap_mx4_weight *w, int32_t *N, int32_t *K, size_t *device_bytes)
+{
+    const Mx4Weight *ww = check_mx4(w);
+    if (!ww) return fail(SQAP_EINVAL, "sqap_mx4_weight_info: not a weight handle");
+    if (N) *N = ww->N;
+    if (K) *K = ww->K;
+    if (device_bytes) *device_bytes = ww->bytes;
+    return SQAP_OK;
+}
+
+sqap_status sqap_mx4_linear(const uint8_t *Xq, const uint8_t *Xs, int32_t M, const sqap_mx4_weight *W, sqap_f16 *Y, int64_t ldy, void *stream)
+{
+    const char *who = "sqap_mx4_linear";
+    const Mx4Weight *w = check_mx4(W);
+    if (!w) return fail(SQAP_EINVAL, "%s: W is not a weight handle", who);
+    if (M < 0) return fail(SQAP_EINVAL, "%s: M = %d", who, M);
+    if (ldy < w->N) return fail(SQAP_EINVAL, "%s: ldy %lld below N %d", who, (long long)ldy, w->N);
+    if (M == 0) return SQAP_OK;
+    if (!Xq || !Xs || !Y) return fail(SQAP_EINVAL, "%s: null pointer", who);
+    if (!aligned16(Xq)) return fail(SQAP_EUNSUPPORTED, "%s: Xq must be 16-byte aligned", who);
+    if (M > kMx4MaxRows || (int64_t)((M + 15) / 16) * ((w->N + 63) / 64) > (1 << 30))
+        return fail(SQAP_EUNSUPPORTED, "%s: M = %d, N = %d", who, M, w->N);
+    const DeviceOfCall device;
+    if (device_ordinal() != w->device) return fail(SQAP_EINVAL, "%s: the weight is on device %d, the current one is %d", who, w->device, device_ordinal());
+    return launch_mx4_linear(Xq, Xs, M, *w, reinterpret_cast<__half *>(Y), ldy, as_stream(stream));
+}
+
 sqap_status sqap_decoder_create(const sqap_decoder_layer *layers, int32_t n_layers, int32_t n_heads, int32_t head_dim,
                                 const sqap_f16 *gamma_final, const sqap_weight *head, float eps, double rope_base,
                                 sqap_decoder **out)

@@ -145,6 +145,8 @@ struct Calls {
     decltype(&sqap_attention) attention;
     decltype(&sqap_decode_attention) decode_attention;
     decltype(&sqap_w4a4_linear) w4a4_linear;
+    decltype(&sqap_mx4_quantize) mx4_quantize;
+    decltype(&sqap_mx4_linear) mx4_linear;
     decltype(&sqap_group_run) group_run;
     decltype(&sqap_decoder_step) decoder_step;
     PyObject *failed;                     // called with a status that is not zero: raises
@@ -240,6 +242,12 @@ SQAP_METHOD(decode_attention, 12,
 SQAP_METHOD(w4a4_linear, 7,
             run(c->w4a4_linear, ptr<uint8_t>(a[0]), ptr<sqap_f16>(a[1]), (int32_t)size(a[0], 0), handle<sqap_weight>(a[2]), ptr<sqap_f16>(a[3]),
                 pitch(a[3]), ptr<int32_t>(a[4]), ptr(a[5]), bytes(a[5]), stream(c, a[6])))
+SQAP_METHOD(mx4_quantize, 5,
+            run(c->mx4_quantize, ptr<sqap_f16>(a[0]), pitch(a[0]), ptr<int32_t>(a[1]), (int32_t)rows_of(a[0], a[1]), (int32_t)size(a[0], 1),
+                ptr<uint8_t>(a[2]), ptr<uint8_t>(a[3]), stream(c, a[4])))
+SQAP_METHOD(mx4_linear, 5,
+            run(c->mx4_linear, ptr<uint8_t>(a[0]), ptr<uint8_t>(a[1]), (int32_t)size(a[0], 0), handle<sqap_mx4_weight>(a[2]),
+                ptr<sqap_f16>(a[3]), pitch(a[3]), stream(c, a[4])))
 SQAP_METHOD(group_run, 2, run(c->group_run, handle<sqap_group>(a[0]), stream(c, a[1])))
 SQAP_METHOD(decoder_step, 7,
             run(c->decoder_step, handle<sqap_decoder>(a[0]), ptr<sqap_f16>(a[1]), ptr<int32_t>(a[2]), as_i32(a[3]), ptr<sqap_f16>(a[4]),
@@ -265,7 +273,7 @@ SQAP_METHOD(attention, 8, attention_call(c, a))
 
 #define SQAP_CALLS(X)                                                                                                                   \
     X(attn_scores_batch) X(prune_topk) X(kept_rows) X(prune_rows) X(prune_select) X(quantize_act) X(rmsnorm_quantize_act)              \
-    X(swiglu_quantize_act) X(rope) X(rope_append) X(attention) X(decode_attention) X(w4a4_linear) X(group_run) X(decoder_step)
+    X(swiglu_quantize_act) X(rope) X(rope_append) X(attention) X(decode_attention) X(w4a4_linear) X(mx4_quantize) X(mx4_linear) X(group_run) X(decoder_step)
 
 PyMethodDef methods[] = {
 #define SQAP_ENTRY(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(m_##NAME)), METH_FASTCALL, nullptr},

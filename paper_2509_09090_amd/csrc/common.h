@@ -94,6 +94,21 @@ struct Group {
 };
 constexpr uint32_t kGroupMagic = 0x53514752u;  // "SQGR"
 
+// Packed weight in microscaled 4-bit floating point (mx4.hip): fragments of 16 channels x 128 codes, 1 KiB each, along K first; a word of
+// scale bytes per lane and four fragments.
+struct Mx4Weight {
+    uint32_t magic;
+    int32_t N, K;
+    int32_t n_groups;          // of 16 channels, a multiple of 16: a tile needs no guard in N
+    int32_t ksteps, kquads;    // fragments along K (an even number: codes of zero behind K), words of scales along K
+    uint8_t *data;             // n_groups * ksteps KiB
+    unsigned *scales;          // n_groups * kquads * 64 words
+    size_t bytes;
+    int device;
+};
+constexpr uint32_t kMx4Magic = 0x53514d34u;  // "SQM4"
+constexpr int kMx4MaxK = 1 << 20, kMx4MaxRows = 1 << 24;
+
 static inline hipStream_t as_stream(void *s) { return reinterpret_cast<hipStream_t>(s); }
 
 // Launcher state that belongs to a device (function attributes set, CU count): one slot per device
@@ -217,6 +232,10 @@ sqap_status launch_few_linear(const uint8_t *Xq, const __half *sx, int M, int K,
                               unsigned long long *error_word, hipStream_t st);
 bool rows_kernel_wanted();
 void set_mid_m_kernel(int which);        // 0: tiles split along K between workgroups, 1: whole outputs per workgroup
+
+sqap_status launch_mx4_quantize(const __half *X, int64_t ldx, const int32_t *rows, int M, int K, uint8_t *Xq, uint8_t *Xs, hipStream_t st);
+sqap_status launch_mx4_pack(const uint8_t *Wq, const uint8_t *Ws, const Mx4Weight &w, hipStream_t st);
+sqap_status launch_mx4_linear(const uint8_t *Xq, const uint8_t *Xs, int M, const Mx4Weight &w, __half *Y, int64_t ldy, hipStream_t st);
 
 sqap_status launch_rope(__half *X, int64_t ld, const int32_t *pos, int S, int H, int d, double base, hipStream_t st);
 sqap_status launch_rope_append(__half *QKV, int64_t ld, const int32_t *pos, int S, int H, int d, double base,
