@@ -471,6 +471,76 @@ sqap_status sqap_residual_add(sqap_f16 *X, int64_t ldx, const sqap_f16 *delta, i
                               int32_t K, void *stream);
 
 /*
+ * A key/value cache held in 8 bits, for a batch of sequences of different lengths, with as many query heads to a key
+ * head as H / kv_heads.  SQAP_CACHE8_BLOCK = 64 consecutive positions of a key head are a block.  When the last row of
+ * a block arrives, its keys get one scale and its values another,
+ *   scale = binary32(amax / 127),  code = 127 v / amax to the nearest, halfway cases to even,
+ * and stand for code * scale from then on; until then its rows stay as they are, in half precision, in the tail.  So
+ * what the cache holds depends on the rows alone, not on how they were split into calls.  A block whose keys (values)
+ * hold an infinity or a NaN gets a scale that is NaN: the outputs of that head that see any of its positions are NaN.  A
+ * block of zeros has the scale 0.
+ *
+ * The caller owns the buffers (device):
+ *   codes   int8    [batch][kv_heads][capacity / 64][2 (keys, values)][64 * head_dim], in the library's order
+ *   scales  float   [batch][kv_heads][capacity / 64][2]
+ *   tail    half    [batch][kv_heads][2][64][head_dim]: row i is position 64 * (length / 64) + i of the sequence
+ * which need no initialisation; a cache is emptied by starting again with past = 0.  The lengths are the caller's:
+ * `past` [batch] int32, device, says how many positions each sequence holds before a call, and is not changed by it.
+ * Rows of the tail, scales and codes past a sequence's length hold nothing and are not read.
+ *
+ * New rows are fused q|k|v rows [H d | kv_heads d | kv_heads d] (pitch ld), rotated on their way as by sqap_rope at
+ * positions pos [rows] int32, device; they are only read.  The rows of sequence b are starts[b] .. starts[b + 1] - 1
+ * (starts: [batch + 1] int32, device), max_new the most that a sequence has.
+ *
+ * sqap_cache8_append: appends them.  Q_out: NULL, or [rows, H d] (pitch ldq) that receives the rotated queries; it may
+ * lie over QKV's query columns (ldq = ld).  Rows before starts[0] and behind starts[batch] are not touched.
+ *
+ * sqap_cache8_attention: causal attention of rotated queries Q [rows, H d] over what the cache holds after the rows have
+ * been appended: query j of sequence b sees positions 0 .. past[b] + j,
+ *   o = sum_t softmax_t((q . k_t) / sqrt(d)) v_t,
+ * scores, maximum and sums in binary32, probabilities rounded to half for the second product, O [rows, H d] (pitch ldo).
+ *
+ * sqap_cache8_decode_attention: one new row per sequence (QKV [batch, ...], pos [batch]): append and attention over
+ * positions 0 .. past[b] in one launch, in binary32 throughout but for the operands' own halves (a probability
+ * enters as the sum of two).  Same cache as by sqap_cache8_append.  longest: the most positions that a sequence
+ * has, the new one included, as far as the host knows; it decides how the work is split, nothing else.  workspace: at least
+ * sqap_cache8_workspace_bytes(batch, H, kv_heads, head_dim, longest) bytes, 16-byte aligned (may be NULL when that is 0); its
+ * first 4 * batch * H bytes (counters) must be ZERO before its first use, every call leaves them zero.
+ * Calls that share a workspace must be ordered on one stream; graphs that are replayed side by side need one each.
+ *
+ * sqap_cache8_read: positions first .. first + count - 1 of every sequence as halves (codes times scale, rounded once),
+ * out [batch * count, 2 kv_heads d] (pitch ld): keys, then values; zeros where lengths[b] (device) does not reach.
+ *
+ * What the device finds wrong it leaves alone: a sequence with past[b] < 0 or no rows is skipped, its outputs
+ * stay as they were (a padded batch); one whose rows do not fit the capacity, or are more than max_new, is not appended
+ * and its outputs are NaN; one whose starts do not lie in order within 0 .. rows is skipped.
+ * All may be captured in a graph and replayed with other past, pos and starts.
+ * EINVAL: null pointer, negative size, sizes of the cache that are not positive, H not a multiple of kv_heads, capacity
+ * not a multiple of 64, a pitch too small, base <= 0, first < 0, workspace missing, too small or misaligned.
+ * EUNSUPPORTED: head_dim not 64 or 128, more than 65535 sequences or key heads (times 16 query heads), operands or
+ * pitches not 16-byte aligned (scales: 4).
+ */
+#define SQAP_CACHE8_BLOCK 64
+typedef struct sqap_cache8 {
+    int8_t *codes;
+    float *scales;
+    sqap_f16 *tail;
+    int32_t batch, capacity, kv_heads, head_dim;
+} sqap_cache8;
+sqap_status sqap_cache8_append(const sqap_f16 *QKV, int64_t ld, const int32_t *starts, const int32_t *pos,
+                               const int32_t *past, int32_t rows, int32_t max_new, int32_t H, double base,
+                               const sqap_cache8 *cache, sqap_f16 *Q_out, int64_t ldq, void *stream);
+sqap_status sqap_cache8_attention(const sqap_f16 *Q, int64_t ldq, const int32_t *starts, const int32_t *past,
+                                  int32_t rows, int32_t max_new, int32_t H, const sqap_cache8 *cache, sqap_f16 *O,
+                                  int64_t ldo, void *stream);
+size_t sqap_cache8_workspace_bytes(int32_t batch, int32_t H, int32_t kv_heads, int32_t head_dim, int32_t longest);
+sqap_status sqap_cache8_decode_attention(const sqap_f16 *QKV, int64_t ld, const int32_t *pos, const int32_t *past,
+                                         int32_t H, double base, const sqap_cache8 *cache, int32_t longest, sqap_f16 *O,
+                                         int64_t ldo, void *workspace, size_t workspace_bytes, void *stream);
+sqap_status sqap_cache8_read(const sqap_cache8 *cache, const int32_t *lengths, int32_t first, int32_t count,
+                             sqap_f16 *out, int64_t ld, void *stream);
+
+/*
  * Self-test of the quantizer's arithmetic.  The quantizer divides every element
  * of a row by the same scale; it does so with the reciprocal in two parts and
  * one fused multiply-add, which gives the correctly rounded binary32 quotient.

@@ -29,6 +29,7 @@ EXPORTS = (
     "sqap_set_persistent_kernels", "sqap_attn_scores_workspace_bytes", "sqap_attn_scores_noalloc", "sqap_set_mid_m_kernel", "sqap_decoder_create", "sqap_decoder_step", "sqap_decoder_status",
     "sqap_decoder_set_wait_limit", "sqap_decoder_free",
     "sqap_mx4_quantize", "sqap_mx4_weight_pack", "sqap_mx4_weight_free", "sqap_mx4_weight_info", "sqap_mx4_linear",
+    "sqap_cache8_append", "sqap_cache8_attention", "sqap_cache8_workspace_bytes", "sqap_cache8_decode_attention", "sqap_cache8_read",
 )
 
 
@@ -44,6 +45,12 @@ class DecoderLayer(ctypes.Structure):
     _fields_ = [("qkv", ctypes.c_void_p), ("o", ctypes.c_void_p), ("gate_up", ctypes.c_void_p), ("down", ctypes.c_void_p),
                 ("gamma_attn", ctypes.c_void_p), ("gamma_mlp", ctypes.c_void_p), ("kv", ctypes.c_void_p),
                 ("ldkv", ctypes.c_int64)]
+
+
+class Cache8Desc(ctypes.Structure):
+    """Mirror of sqap_cache8."""
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("tail", ctypes.c_void_p), ("batch", ctypes.c_int32),
+                ("capacity", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
 
 
 class SqapError(RuntimeError):
@@ -121,8 +128,15 @@ def lib():
         L.sqap_mx4_weight_free.argtypes = [vp]
         L.sqap_mx4_weight_info.argtypes = [vp, ctypes.POINTER(i32), ctypes.POINTER(i32), ctypes.POINTER(sz)]
         L.sqap_mx4_linear.argtypes = [vp, vp, i32, vp, vp, i64, vp]
+        cache = ctypes.POINTER(Cache8Desc)
+        L.sqap_cache8_append.argtypes = [vp, i64, vp, vp, vp, i32, i32, i32, ctypes.c_double, cache, vp, i64, vp]
+        L.sqap_cache8_attention.argtypes = [vp, i64, vp, vp, i32, i32, i32, cache, vp, i64, vp]
+        L.sqap_cache8_workspace_bytes.restype = sz
+        L.sqap_cache8_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+        L.sqap_cache8_decode_attention.argtypes = [vp, i64, vp, vp, i32, ctypes.c_double, cache, i32, vp, i64, vp, sz, vp]
+        L.sqap_cache8_read.argtypes = [cache, vp, i32, i32, vp, i64, vp]
         for name in EXPORTS:
-            if name not in ("sqap_last_error", "sqap_version", "sqap_workspace_bytes", "sqap_attn_scores_workspace_bytes"):
+            if name not in ("sqap_last_error", "sqap_version", "sqap_workspace_bytes", "sqap_attn_scores_workspace_bytes", "sqap_cache8_workspace_bytes"):
                 getattr(L, name).restype = ctypes.c_int32
         _lib = L
     return _lib
@@ -440,6 +454,49 @@ def sqap_mx4_weight_pack(Wq, Ws, stream=None):
 def sqap_mx4_linear(Xq, Xs, W, Y, stream=None):
     """Xq [M,K/2] u8, Xs [M,K/32] u8, W: Mx4Weight -> Y [M,N] fp16."""
     _native.mx4_linear(Xq, Xs, W.handle, Y, stream)
+
+
+CACHE8_BLOCK = 64
+
+
+class Cache8:
+    """A key/value cache in 8 bits for `batch` sequences of up to `capacity` positions (rounded up to whole blocks): holds the
+    buffers that sqap_cache8 describes.  How many positions each sequence has is the caller's `past`."""
+
+    def __init__(self, batch, capacity, kv_heads, head_dim, device="cuda"):
+        blocks = -(-int(capacity) // CACHE8_BLOCK)
+        self.batch, self.capacity, self.kv_heads, self.head_dim = batch, blocks * CACHE8_BLOCK, kv_heads, head_dim
+        self.codes = torch.zeros((batch, kv_heads, blocks, 2, CACHE8_BLOCK * head_dim), dtype=torch.int8, device=device)
+        self.scales = torch.zeros((batch, kv_heads, blocks, 2), dtype=torch.float32, device=device)
+        self.tail = torch.zeros((batch, kv_heads, 2, CACHE8_BLOCK, head_dim), dtype=torch.float16, device=device)
+        self._desc = Cache8Desc(self.codes.data_ptr(), self.scales.data_ptr(), self.tail.data_ptr(), batch, self.capacity, kv_heads, head_dim)
+        self.handle = ctypes.c_void_p(ctypes.addressof(self._desc))
+
+
+def sqap_cache8_append(QKV, starts, pos, past, cache, H, max_new, Q_out=None, base=10000.0, stream=None):
+    """Fused rows QKV [rows, (H + 2 kv_heads) d] of sequences starts [batch+1] int32, at positions pos [rows] int32, appended to a
+    Cache8 that holds past [batch] int32 positions; Q_out [rows, H d] receives the rotated queries."""
+    _native.cache8_append(QKV, starts, pos, past, cache.handle, H, max_new, Q_out, base, stream)
+
+
+def sqap_cache8_attention(Q, starts, past, cache, H, max_new, O, stream=None):
+    """Causal attention of rotated queries Q [rows, H d], appended behind past [batch] int32 positions, over a Cache8."""
+    _native.cache8_attention(Q, starts, past, cache.handle, H, max_new, O, stream)
+
+
+def sqap_cache8_workspace_bytes(batch, H, kv_heads, head_dim, longest):
+    return int(lib().sqap_cache8_workspace_bytes(batch, H, kv_heads, head_dim, longest))
+
+
+def sqap_cache8_decode_attention(QKV, pos, past, cache, H, O, workspace, longest, base=10000.0, stream=None):
+    """One new row per sequence, QKV [batch, (H + 2 kv_heads) d] at pos [batch] int32: append behind past [batch] int32 positions and
+    attention in one launch into O [batch, H d].  workspace: device bytes, zeroed once (see sqap_cache8_workspace_bytes)."""
+    _native.cache8_decode_attention(QKV, pos, past, cache.handle, H, O, workspace, longest, base, stream)
+
+
+def sqap_cache8_read(cache, lengths, first, count, out, stream=None):
+    """Positions first .. first + count - 1 of every sequence as halves: out [batch * count, 2 kv_heads d], keys then values."""
+    _check(lib().sqap_cache8_read(ctypes.byref(cache._desc), _ptr(lengths), first, count, _ptr(out), out.stride(0), _stream(stream)))
 
 
 class Group:

@@ -729,6 +729,120 @@ sqap_status sqap_mx4_linear(const uint8_t *Xq, const uint8_t *Xs, int32_t M, con
     return launch_mx4_linear(Xq, Xs, M, *w, reinterpret_cast<__half *>(Y), ldy, as_stream(stream));
 }
 
+// ---- key/value cache in 8 bits
+
+static sqap_status check_cache8(const char *who, const sqap_cache8 *c, int32_t H, Cache8View *out)
+{
+    if (!c) return fail(SQAP_EINVAL, "%s: null cache", who);
+    if (c->batch < 0 || c->capacity <= 0 || c->kv_heads <= 0 || c->head_dim <= 0)
+        return fail(SQAP_EINVAL, "%s: cache of batch %d, capacity %d, %d key heads of %d", who, c->batch, c->capacity, c->kv_heads, c->head_dim);
+    if (c->capacity % kCache8Block != 0) return fail(SQAP_EINVAL, "%s: capacity %d is not a multiple of %d", who, c->capacity, kCache8Block);
+    if (H <= 0 || H % c->kv_heads != 0) return fail(SQAP_EINVAL, "%s: %d heads, %d key heads", who, H, c->kv_heads);
+    if (c->head_dim != 64 && c->head_dim != 128) return fail(SQAP_EUNSUPPORTED, "%s: head size %d (64 or 128)", who, c->head_dim);
+    if (c->batch > 65535 || (int64_t)c->kv_heads * ((H / c->kv_heads + 15) / 16) > 65535)
+        return fail(SQAP_EUNSUPPORTED, "%s: batch %d, %d heads, %d key heads", who, c->batch, H, c->kv_heads);
+    if (c->batch == 0) return SQAP_OK;
+    if (!c->codes || !c->scales || !c->tail) return fail(SQAP_EINVAL, "%s: a cache buffer is null", who);
+    if (!aligned16(c->codes) || !aligned16(c->tail) || (reinterpret_cast<uintptr_t>(c->scales) & 3u))
+        return fail(SQAP_EUNSUPPORTED, "%s: codes and tail must be 16-byte aligned, scales 4-byte", who);
+    out->codes = c->codes;
+    out->scales = c->scales;
+    out->tail = reinterpret_cast<__half *>(c->tail);
+    out->batch = c->batch;
+    out->blocks = c->capacity / kCache8Block;
+    out->kv_heads = c->kv_heads;
+    return SQAP_OK;
+}
+
+static sqap_status check_rows16(const char *who, const char *what, const void *p, int64_t ld, int64_t columns)
+{
+    if (ld < columns) return fail(SQAP_EINVAL, "%s: pitch of %s %lld below %lld", who, what, (long long)ld, (long long)columns);
+    if (!p) return fail(SQAP_EINVAL, "%s: null %s", who, what);
+    if (!aligned16(p) || (ld & 7)) return fail(SQAP_EUNSUPPORTED, "%s: %s and its pitch must be 16-byte aligned", who, what);
+    return SQAP_OK;
+}
+
+sqap_status sqap_cache8_append(const sqap_f16 *QKV, int64_t ld, const int32_t *starts, const int32_t *pos, const int32_t *past, int32_t rows,
+                               int32_t max_new, int32_t H, double base, const sqap_cache8 *cache, sqap_f16 *Q_out, int64_t ldq, void *stream)
+{
+    const char *who = "sqap_cache8_append";
+    Cache8View v = {};
+    if (rows < 0 || max_new < 0) return fail(SQAP_EINVAL, "%s: rows %d, max_new %d", who, rows, max_new);
+    if (!(base > 0.0)) return fail(SQAP_EINVAL, "%s: base must be positive", who);
+    sqap_status s = check_cache8(who, cache, H, &v);
+    if (s != SQAP_OK || rows == 0 || max_new == 0 || cache->batch == 0) return s;
+    if (!starts || !pos || !past) return fail(SQAP_EINVAL, "%s: null pointer", who);
+    const int64_t width = (int64_t)H * cache->head_dim;
+    s = check_rows16(who, "QKV", QKV, ld, width + 2 * (int64_t)cache->kv_heads * cache->head_dim);
+    if (s == SQAP_OK && Q_out) s = check_rows16(who, "Q_out", Q_out, ldq, width);
+    if (s != SQAP_OK) return s;
+    return launch_cache8_append(reinterpret_cast<const __half *>(QKV), ld, starts, pos, past, rows, max_new < rows ? max_new : rows, H, base, v,
+                                cache->head_dim, reinterpret_cast<__half *>(Q_out), ldq, as_stream(stream));
+}
+
+sqap_status sqap_cache8_attention(const sqap_f16 *Q, int64_t ldq, const int32_t *starts, const int32_t *past, int32_t rows, int32_t max_new,
+                                  int32_t H, const sqap_cache8 *cache, sqap_f16 *O, int64_t ldo, void *stream)
+{
+    const char *who = "sqap_cache8_attention";
+    Cache8View v = {};
+    if (rows < 0 || max_new < 0) return fail(SQAP_EINVAL, "%s: rows %d, max_new %d", who, rows, max_new);
+    sqap_status s = check_cache8(who, cache, H, &v);
+    if (s != SQAP_OK || rows == 0 || max_new == 0 || cache->batch == 0) return s;
+    if (!starts || !past) return fail(SQAP_EINVAL, "%s: null pointer", who);
+    const int64_t width = (int64_t)H * cache->head_dim;
+    s = check_rows16(who, "Q", Q, ldq, width);
+    if (s == SQAP_OK) s = check_rows16(who, "O", O, ldo, width);
+    if (s != SQAP_OK) return s;
+    const DeviceOfCall device;
+    return launch_cache8_attention(reinterpret_cast<const __half *>(Q), ldq, starts, past, rows, max_new < rows ? max_new : rows, H, v,
+                                   cache->head_dim, reinterpret_cast<__half *>(O), ldo, as_stream(stream));
+}
+
+size_t sqap_cache8_workspace_bytes(int32_t batch, int32_t H, int32_t kv_heads, int32_t head_dim, int32_t longest)
+{
+    if (batch <= 0 || H <= 0 || kv_heads <= 0 || H % kv_heads != 0 || head_dim <= 0 || longest <= 0) return 0;
+    return cache8_workspace_bytes(batch, H, kv_heads, head_dim, longest);
+}
+
+sqap_status sqap_cache8_decode_attention(const sqap_f16 *QKV, int64_t ld, const int32_t *pos, const int32_t *past, int32_t H, double base,
+                                         const sqap_cache8 *cache, int32_t longest, sqap_f16 *O, int64_t ldo, void *workspace,
+                                         size_t workspace_bytes, void *stream)
+{
+    const char *who = "sqap_cache8_decode_attention";
+    Cache8View v = {};
+    if (!(base > 0.0)) return fail(SQAP_EINVAL, "%s: base must be positive", who);
+    sqap_status s = check_cache8(who, cache, H, &v);
+    if (s != SQAP_OK) return s;
+    if (longest <= 0) return fail(SQAP_EINVAL, "%s: longest = %d", who, longest);
+    if (cache->batch == 0) return SQAP_OK;
+    if (!pos || !past) return fail(SQAP_EINVAL, "%s: null pointer", who);
+    const int64_t width = (int64_t)H * cache->head_dim;
+    s = check_rows16(who, "QKV", QKV, ld, width + 2 * (int64_t)cache->kv_heads * cache->head_dim);
+    if (s == SQAP_OK) s = check_rows16(who, "O", O, ldo, width);
+    if (s != SQAP_OK) return s;
+    const size_t need = cache8_workspace_bytes(cache->batch, H, cache->kv_heads, cache->head_dim, longest);
+    if (need > 0) {
+        if (!workspace || workspace_bytes < need)
+            return fail(SQAP_EINVAL, "%s: workspace of %zu bytes needed, %zu given", who, need, workspace ? workspace_bytes : (size_t)0);
+        if (!aligned16(workspace)) return fail(SQAP_EINVAL, "%s: workspace must be 16-byte aligned", who);
+    }
+    return launch_cache8_decode(reinterpret_cast<const __half *>(QKV), ld, pos, past, H, base, v, cache->head_dim, longest,
+                                reinterpret_cast<__half *>(O), ldo, need > 0 ? workspace : nullptr, as_stream(stream));
+}
+
+sqap_status sqap_cache8_read(const sqap_cache8 *cache, const int32_t *lengths, int32_t first, int32_t count, sqap_f16 *out, int64_t ld, void *stream)
+{
+    const char *who = "sqap_cache8_read";
+    Cache8View v = {};
+    if (first < 0 || count < 0 || (int64_t)first + count > INT32_MAX) return fail(SQAP_EINVAL, "%s: positions %d, %d of them", who, first, count);
+    sqap_status s = check_cache8(who, cache, cache ? cache->kv_heads : 1, &v);
+    if (s != SQAP_OK || count == 0 || cache->batch == 0) return s;
+    if (!lengths) return fail(SQAP_EINVAL, "%s: null lengths", who);
+    s = check_rows16(who, "out", out, ld, 2 * (int64_t)cache->kv_heads * cache->head_dim);
+    if (s != SQAP_OK) return s;
+    return launch_cache8_read(v, cache->head_dim, lengths, first, count, reinterpret_cast<__half *>(out), ld, as_stream(stream));
+}
+
 sqap_status sqap_decoder_create(const sqap_decoder_layer *layers, int32_t n_layers, int32_t n_heads, int32_t head_dim,
                                 const sqap_f16 *gamma_final, const sqap_weight *head, float eps, double rope_base,
                                 sqap_decoder **out)

@@ -1,0 +1,894 @@
+// A key/value cache held in 8 bits, and attention over it.
+//
+// 64 positions of a key head are a block: codes in -127 .. 127 with one binary32 scale for its keys and one for its values.  A block gets
+// its codes once, when its last row arrives; until then its rows stay as they are, in half precision (`tail`), so that what the cache
+// holds does not depend on how many rows came with a call, and no code is rounded twice.
+// Codes are exact as halves (integers below 2^11), and so are their products with halves in binary32: attention runs on the half
+// precision matrix instructions with the scales outside (the keys' on the scores, the values' on the probabilities).
+//
+// Codes lie in the order in which the lanes of a 16x16x32 matrix instruction hold them (lane l: row r = l % 16, group g = l / 16):
+//   keys    [4 tiles of 16 positions][d / 64][lane][16]   position 16 T + r, columns 64 c + 16 g + 0 .. 15
+//   values  [d / 16][lane][16]                            column 16 t + r; byte 8 s + 4 q + i: position 32 s + 16 q + 4 g + i
+// The values' order of positions is that of the lanes' scores, so that probabilities enter the second product where they were computed.
+#include <algorithm>
+
+#include "common.h"
+#include "decode_attn.h"
+
+namespace sqap {
+
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef _Float16 v4h __attribute__((ext_vector_type(4)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef unsigned v2u __attribute__((ext_vector_type(2)));
+
+constexpr int kBlock = kCache8Block;
+constexpr float kLog2e = 1.4426950408889634f;
+
+// ---------------------------------------------------------------- pieces
+
+template <int D>
+__device__ __forceinline__ int8_t *block_codes(const Cache8View &c, int64_t head, int block, int values)
+{
+    return c.codes + ((head * c.blocks + block) * 2 + values) * (kBlock * D);
+}
+
+// Four codes as halves: the byte with its sign flipped behind 0x64 is 1024 + (code + 128), from which 1152 is taken.
+__device__ __forceinline__ v4h halves_of(int w)
+{
+    const unsigned u = (unsigned)w ^ 0x80808080u;
+    union { unsigned u[2]; v2h h[2]; } x;
+    x.u[0] = __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u);
+    x.u[1] = __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u);
+    const v2h bias = {(_Float16)1152.f, (_Float16)1152.f};
+    const v2h a = x.h[0] - bias, b = x.h[1] - bias;
+    return v4h{a[0], a[1], b[0], b[1]};
+}
+__device__ __forceinline__ v8h halves_of(int lo, int hi)
+{
+    const v4h a = halves_of(lo), b = halves_of(hi);
+    return v8h{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+}
+
+// The code of x: 127 x / amax to the nearest, halfway cases to even.  127 x is exact; the quotient with its remainder put right is exact
+// wherever it is representable, as every halfway case is, and a quotient that is not halfway is 2^-12 or more away from that.
+struct Steps {
+    float amax, reciprocal;
+};
+__device__ __forceinline__ Steps steps_of(float amax) { return {amax, amax > 0.f ? 1.0f / amax : 0.f}; }
+__device__ __forceinline__ int code_of(float x, const Steps &s)
+{
+    const float n = 127.0f * x, q = n * s.reciprocal;
+    return (int)rintf(fmaf(fmaf(-q, s.amax, n), s.reciprocal, q));
+}
+// largest magnitude of a half, as its bits: infinities and NaN are above all numbers
+__device__ __forceinline__ unsigned magnitude(__half h) { return __half_as_ushort(h) & 0x7fffu; }
+__device__ __forceinline__ bool finite_bits(unsigned m) { return m < 0x7c00u; }
+__device__ __forceinline__ float scale_of(unsigned m) { return finite_bits(m) ? __half2float(__ushort_as_half((unsigned short)m)) / 127.0f : NAN; }
+
+__device__ __forceinline__ unsigned wavefront_umax(unsigned v)
+{
+    v = max(v, dpp_move<kDppXor1>(v));
+    v = max(v, dpp_move<kDppXor2>(v));
+    v = max(v, dpp_move<kDppHalfMirror>(v));
+    v = max(v, dpp_move<kDppMirror>(v));
+    return max(max((unsigned)__builtin_amdgcn_readlane((int)v, 0), (unsigned)__builtin_amdgcn_readlane((int)v, 16)),
+               max((unsigned)__builtin_amdgcn_readlane((int)v, 32), (unsigned)__builtin_amdgcn_readlane((int)v, 48)));
+}
+
+// half-split rotation of one pair, as rope_kernel does it
+__device__ __forceinline__ void rotate_pair(__half lo, __half hi, double cs, double sn, __half &out_lo, __half &out_hi)
+{
+    const double a = (double)__half2float(lo), b = (double)__half2float(hi);
+    out_lo = __float2half_rn((float)(a * cs - b * sn));
+    out_hi = __float2half_rn((float)(b * cs + a * sn));
+}
+
+// Where a sequence's new rows lie: [row, row + n) of the fused rows, or nothing (n = 0) where the arrays do not describe one.
+struct Span {
+    int row, n, past;
+    bool fits;                  // in the cache
+};
+__device__ __forceinline__ Span span_of(const int32_t *starts, const int32_t *past, int b, int rows, int max_new, int capacity)
+{
+    Span s = {starts[b], 0, past[b], false};
+    const int end = starts[b + 1];
+    if (s.past >= 0 && s.row >= 0 && end >= s.row && end <= rows) s.n = end - s.row;
+    s.fits = s.n > 0 && s.n <= max_new && s.past <= capacity - s.n;
+    return s;
+}
+
+// ---------------------------------------------------------------- append
+
+// One workgroup per sequence, key head and block that the new rows touch (the first and the last of them together: the one reads the
+// tail that the other writes).  Keys: four threads per position, each with D / 8 pairs of columns (i, i + D / 2); the same threads turn
+// the query heads that share the key head.  Values: a column per thread and as many positions as the workgroup leaves it.
+template <int D>
+__global__ __launch_bounds__(256) void cache8_append_kernel(const __half *__restrict__ QKV, int64_t ld, const int32_t *__restrict__ starts,
+                                                            const int32_t *__restrict__ pos, const int32_t *__restrict__ past, int rows, int max_new, int H,
+                                                            const Cache8View cache, __half *__restrict__ Q_out, int64_t ldq, const RopeFreq freq)
+{
+    constexpr int P = D / 8, HALF = D / 2, PARTS = 256 / D, TOKENS = kBlock / PARTS;
+    __shared__ unsigned tops[2][2][4];
+    const int b = blockIdx.z, h = blockIdx.y, t = threadIdx.x, wave = t >> 6;
+    const Span sp = span_of(starts, past, b, rows, max_new, cache.blocks * kBlock);
+    if (!sp.fits) return;
+    const int end = sp.past + sp.n, first = sp.past / kBlock, last = (end - 1) / kBlock, G = H / cache.kv_heads;
+    const int64_t head = (int64_t)b * cache.kv_heads + h;
+    __half *tail_k = cache.tail + head * 2 * kBlock * D, *tail_v = tail_k + kBlock * D;
+    int block = first + (int)blockIdx.x;
+    if (blockIdx.x > 0 && block >= last) return;
+    for (int turn = 0;; ++turn) {
+        const bool full = (block + 1) * kBlock <= end;
+        // ---- keys
+        const int slot = t >> 2, sub = t & 3, p = block * kBlock + slot;
+        const bool is_new = p >= sp.past && p < end;
+        const __half *row = QKV + (int64_t)(sp.row + (is_new ? p - sp.past : 0)) * ld;
+        __half lo[P], hi[P];
+        unsigned top_k = 0;
+        if (is_new) {
+            double cs[P], sn[P];
+            const int at = pos[sp.row + p - sp.past];
+#pragma unroll
+            for (int i = 0; i < P; ++i) sincos((double)at * freq.f[sub * P + i], &sn[i], &cs[i]);
+            auto turned = [&](const __half *from) {
+                union Piece { v4i v[P / 8]; __half h[P]; } a, c;
+#pragma unroll
+                for (int i = 0; i < P / 8; ++i) {
+                    a.v[i] = *reinterpret_cast<const v4i *>(from + sub * P + 8 * i);
+                    c.v[i] = *reinterpret_cast<const v4i *>(from + HALF + sub * P + 8 * i);
+                }
+#pragma unroll
+                for (int i = 0; i < P; ++i) rotate_pair(a.h[i], c.h[i], cs[i], sn[i], lo[i], hi[i]);
+            };
+            if (Q_out) {
+                for (int j = 0; j < G; ++j) {
+                    turned(row + (int64_t)(h * G + j) * D);
+                    __half *to = Q_out + (int64_t)(sp.row + p - sp.past) * ldq + (int64_t)(h * G + j) * D + sub * P;
+                    union Piece { v4i v[P / 8]; __half h[P]; } a, c;
+#pragma unroll
+                    for (int i = 0; i < P; ++i) a.h[i] = lo[i], c.h[i] = hi[i];
+#pragma unroll
+                    for (int i = 0; i < P / 8; ++i) {
+                        *reinterpret_cast<v4i *>(to + 8 * i) = a.v[i];
+                        *reinterpret_cast<v4i *>(to + HALF + 8 * i) = c.v[i];
+                    }
+                }
+            }
+            turned(row + (int64_t)(H + h) * D);
+        } else {
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                lo[i] = p < sp.past ? tail_k[slot * D + sub * P + i] : __half(0.f);
+                hi[i] = p < sp.past ? tail_k[slot * D + HALF + sub * P + i] : __half(0.f);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < P; ++i) top_k = max(top_k, max(magnitude(lo[i]), magnitude(hi[i])));
+        // ---- values: this thread's column, positions 64 / PARTS of them
+        const int col = t % D, part = t / D;
+        __half v[TOKENS];
+        unsigned top_v = 0;
+        const __half *vbase = QKV + (int64_t)(H + cache.kv_heads + h) * D + col;
+#pragma unroll
+        for (int i = 0; i < TOKENS; ++i) {
+            const int s = part * TOKENS + i, q = block * kBlock + s;
+            v[i] = q < sp.past ? tail_v[s * D + col] : q < end ? vbase[(int64_t)(sp.row + q - sp.past) * ld] : __half(0.f);
+            top_v = max(top_v, magnitude(v[i]));
+        }
+        // ---- what becomes of them
+        if (full) {
+            top_k = wavefront_umax(top_k);
+            top_v = wavefront_umax(top_v);
+            if ((t & 63) == 0) {
+                tops[turn][0][wave] = top_k;
+                tops[turn][1][wave] = top_v;
+            }
+        }
+        __syncthreads();                                              // (and nobody reads the tail any more)
+        if (full) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                top_k = max(top_k, tops[turn][0][w]);
+                top_v = max(top_v, tops[turn][1][w]);
+            }
+            const bool ok_k = finite_bits(top_k), ok_v = finite_bits(top_v);
+            const Steps sk = steps_of(__half2float(__ushort_as_half((unsigned short)top_k))), sv = steps_of(__half2float(__ushort_as_half((unsigned short)top_v)));
+            int8_t *kc = block_codes<D>(cache, head, block, 0), *vc = block_codes<D>(cache, head, block, 1);
+            // columns sub P .. and HALF + sub P ..: whole or half pieces of 16
+            auto store = [&](int column, const __half (&x)[P]) {
+                int w[P / 4];
+#pragma unroll
+                for (int i = 0; i < P / 4; ++i) {
+                    w[i] = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[i] |= (ok_k ? code_of(__half2float(x[4 * i + e]), sk) & 255 : 0) << (8 * e);
+                }
+                int8_t *to = kc + ((((slot >> 4) * (D / 64) + (column >> 6)) * 64 + ((column >> 4) & 3) * 16 + (slot & 15)) * 16 + (column & 15));
+                if constexpr (P == 16) *reinterpret_cast<v4i *>(to) = v4i{w[0], w[1], w[2], w[3]};
+                else *reinterpret_cast<v2u *>(to) = v2u{(unsigned)w[0], (unsigned)w[1]};
+            };
+            store(sub * P, lo);
+            store(HALF + sub * P, hi);
+#pragma unroll
+            for (int i = 0; i < TOKENS; i += 4) {
+                const int s = part * TOKENS + i;                      // four positions of one lane group
+                int w = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w |= (ok_v ? code_of(__half2float(v[i + e]), sv) & 255 : 0) << (8 * e);
+                *reinterpret_cast<int *>(vc + ((col >> 4) * 64 + ((s >> 2) & 3) * 16 + (col & 15)) * 16 + (s >> 5) * 8 + ((s >> 4) & 1) * 4) = w;
+            }
+            if (t == 0) {
+                float *to = cache.scales + (head * cache.blocks + block) * 2;
+                to[0] = scale_of(top_k);
+                to[1] = scale_of(top_v);
+            }
+        } else {
+            if (is_new) {
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    tail_k[slot * D + sub * P + i] = lo[i];
+                    tail_k[slot * D + HALF + sub * P + i] = hi[i];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < TOKENS; ++i) {
+                const int s = part * TOKENS + i, q = block * kBlock + s;
+                if (q >= sp.past && q < end) tail_v[s * D + col] = v[i];
+            }
+        }
+        if (blockIdx.x > 0 || block == last) return;
+        block = last;
+    }
+}
+
+// ---------------------------------------------------------------- reading back
+
+template <int D>
+__global__ __launch_bounds__(256) void cache8_read_kernel(const Cache8View cache, const int32_t *__restrict__ lengths, int first, int count,
+                                                          __half *__restrict__ out, int64_t ld)
+{
+    // one workgroup per position; a thread per two columns of a head
+    const int j = blockIdx.x, b = blockIdx.y, p = first + j, n = lengths[b];
+    __half *row = out + ((int64_t)b * count + j) * ld;
+    for (int u = threadIdx.x; u < cache.kv_heads * D; u += 256) {
+        const int which = u >= cache.kv_heads * D / 2, w = (u - which * (cache.kv_heads * D / 2)) * 2, h = w / D, c = w % D;
+        const int64_t head = (int64_t)b * cache.kv_heads + h;
+        __half v[2] = {__half(0.f), __half(0.f)};
+        if (p < n && n <= cache.blocks * kBlock) {
+            const int s = p % kBlock, block = p / kBlock;
+            if (block == n / kBlock) {
+                const __half *from = cache.tail + ((head * 2 + which) * kBlock + s) * D + c;
+                v[0] = from[0];
+                v[1] = from[1];
+            } else {
+                const float scale = cache.scales[(head * cache.blocks + block) * 2 + which];
+                const int8_t *codes = block_codes<D>(cache, head, block, which);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int x = c + e;
+                    const int at = which ? ((x >> 4) * 64 + ((s >> 2) & 3) * 16 + (x & 15)) * 16 + (s >> 5) * 8 + ((s >> 4) & 1) * 4 + (s & 3)
+                                         : (((s >> 4) * (D / 64) + (x >> 6)) * 64 + ((x >> 4) & 3) * 16 + (s & 15)) * 16 + (x & 15);
+                    v[e] = __float2half_rn((float)codes[at] * scale);
+                }
+            }
+        }
+        __half *to = row + (int64_t)which * cache.kv_heads * D + w;
+        to[0] = v[0];
+        to[1] = v[1];
+    }
+}
+
+// ---------------------------------------------------------------- attention of many rows
+
+// What both attentions keep of the values' scales: sums of values are held in units of `unit`, the scale of the block that last changed
+// it.  A block whose scale is above it or below 2^-8 of it makes the sums change units; others enter through their probabilities,
+// which then stay in the range that a half resolves.
+struct Unit {
+    float unit = 0.f;
+    // factor for the block's probabilities; `change` is what the sums so far have to be multiplied with (1: nothing)
+    __device__ __forceinline__ float enter(float scale, float &change)
+    {
+        change = 1.f;
+        if (!(scale > 0.f)) return scale;                             // no values but zeros, or NaN: the sums stay as they are
+        if (scale > unit || scale < unit * 0.00390625f) {
+            change = unit / scale;
+            unit = scale;
+        }
+        return scale / unit;
+    }
+};
+
+// Rows are (query, head) pairs of the heads that share a key head, query first, 128 to a workgroup and 32 to a wavefront, so that a
+// block of keys and values is taken from memory and made halves once for all of them.  Everything is transposed (scores: positions x
+// rows), as in attention.hip: probabilities are the second product's operand where they were computed.
+constexpr int kRowsOfTile = 128;
+
+template <int D>
+__global__ __launch_bounds__(256) void cache8_attention_kernel(const __half *__restrict__ Q, int64_t ldq, const int32_t *__restrict__ starts,
+                                                               const int32_t *__restrict__ past, int rows, int max_new, int H, const Cache8View cache,
+                                                               __half *__restrict__ O, int64_t ldo)
+{
+    constexpr int NP = D / 16, CT = D / 32, BUF = 2 * kBlock * D * 2, PIECES = kBlock * D / 16 / 256;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];     // two buffers: keys [2][NP] KiB, values [CT][4] KiB
+    __shared__ int not_finite;
+    const int b = blockIdx.z, kh = blockIdx.y, t = threadIdx.x, l = t & 63, wave = t >> 6, c = l & 31, h = l >> 5;
+    const Span sp = span_of(starts, past, b, rows, max_new, cache.blocks * kBlock);
+    const int G = H / cache.kv_heads;
+    const int64_t n_rows = (int64_t)sp.n * G, tile = (int64_t)(gridDim.x - 1 - blockIdx.x) * kRowsOfTile;     // (the longest first)
+    if (tile >= n_rows) return;
+    const int64_t mine = tile + wave * 32 + c;
+    const int64_t mine_in = min(mine, n_rows - 1);
+    const int query = (int)(mine_in / G), head = kh * G + (int)(mine_in % G);
+    if (!sp.fits) {
+        if (mine < n_rows && h == 0)
+            for (int i = 0; i < D; ++i) O[(int64_t)(sp.row + query) * ldo + (int64_t)head * D + i] = __ushort_as_half(0x7e00);
+        return;
+    }
+    if (t == 0) not_finite = 0;
+    const int end = sp.past + sp.n, sees = sp.past + query;           // last position that this lane's row sees
+    const int tile_last = sp.past + (int)((min(tile + kRowsOfTile, n_rows) - 1) / G), n_blocks = tile_last / kBlock + 1;
+    const int64_t kv_head = (int64_t)b * cache.kv_heads + kh;
+    const __half *tail_k = cache.tail + kv_head * 2 * kBlock * D, *tail_v = tail_k + kBlock * D;
+    const float *scales = cache.scales + kv_head * cache.blocks * 2;
+    const int tail_block = end / kBlock, tail_rows = end % kBlock;
+
+    v8h qf[NP];
+#pragma unroll
+    for (int m = 0; m < NP; ++m)
+        qf[m] = *reinterpret_cast<const v8h *>(Q + (int64_t)(sp.row + query) * ldq + (int64_t)head * D + 16 * m + 8 * h);
+
+    v4i kraw[PIECES], vraw[PIECES];
+    auto fetch = [&](int j) {
+        if (j >= n_blocks || j == tail_block) return;
+        const v4i *k = reinterpret_cast<const v4i *>(block_codes<D>(cache, kv_head, j, 0)), *v = reinterpret_cast<const v4i *>(block_codes<D>(cache, kv_head, j, 1));
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            kraw[i] = k[t + 256 * i];
+            vraw[i] = v[t + 256 * i];
+        }
+    };
+    auto keep = [&](int j) {
+        if (j >= n_blocks) return;
+        uint8_t *kt = lds + (j & 1) * BUF, *vt = kt + kBlock * D * 2;
+        if (j != tail_block) {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const int u = t + 256 * i, r = u & 15, g = (u >> 4) & 3, x = u >> 6;
+                // keys: piece x = (T, c): position 16 T + r, columns 64 c + 16 g ..
+                const int T = x / (D / 64), m = (x % (D / 64)) * 4 + g, row = 16 * (T & 1) + r;
+                uint8_t *to = kt + (((T >> 1) * NP + m) * 64 + row) * 16;
+                *reinterpret_cast<v8h *>(to) = halves_of(kraw[i][0], kraw[i][1]);
+                *reinterpret_cast<v8h *>(to + 512) = halves_of(kraw[i][2], kraw[i][3]);
+                // values: piece x: column 16 x + r, four positions per word
+                const int col = 16 * x + r;
+                uint8_t *vo = vt + ((col >> 5) * 4 * 64 + (g & 1) * 32 + (col & 31)) * 16 + (g >> 1) * 8;
+#pragma unroll
+                for (int n = 0; n < 4; ++n) *reinterpret_cast<v4h *>(vo + n * 1024) = halves_of(vraw[i][n]);
+            }
+            return;
+        }
+        bool odd = false;
+        for (int u = t; u < kBlock * D / 8; u += 256) {
+            const int s = u / (D / 8), x = (u % (D / 8)) * 8;
+            v8h k = {}, v = {};
+            if (s < tail_rows) {
+                k = *reinterpret_cast<const v8h *>(tail_k + s * D + x);
+                v = *reinterpret_cast<const v8h *>(tail_v + s * D + x);
+            }
+            *reinterpret_cast<v8h *>(kt + (((s >> 5) * NP + (x >> 4)) * 64 + ((x >> 3) & 1) * 32 + (s & 31)) * 16) = k;
+            const int n = s >> 4, o = s & 15;                         // 8 q + 4 h + i of its sixteen positions
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int col = x + e;
+                _Float16 w = v[e];
+                if (!(__builtin_fabsf((float)w) <= 65504.f)) {        // comes back at the end, to the rows that see it
+                    w = (_Float16)0.f;
+                    odd = true;
+                }
+                *reinterpret_cast<_Float16 *>(vt + (((col >> 5) * 4 + n) * 64 + ((o >> 2) & 1) * 32 + (col & 31)) * 16 + (o >> 3) * 8 + (o & 3) * 2) = w;
+            }
+        }
+        if (odd) not_finite = 1;
+    };
+
+    v16f ot[CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) ot[ct][i] = 0.f;
+    float mrun = -INFINITY, lrun = 0.f;
+    Unit unit;
+    const float per_d = kLog2e / sqrtf((float)D);
+    const int wave_last = sp.past + (int)(min(tile + wave * 32 + 31, n_rows - 1) / G), wave_first = sp.past + (int)(min(tile + wave * 32, n_rows - 1) / G);
+    __syncthreads();
+    fetch(0);
+    keep(0);
+    for (int j = 0; j < n_blocks; ++j) {
+        fetch(j + 1);
+        __syncthreads();
+        if (j * kBlock <= wave_last) {
+            const uint8_t *kt = lds + (j & 1) * BUF, *vt = kt + kBlock * D * 2;
+            const float sk = j == tail_block ? per_d : scales[2 * j] * per_d, sv = j == tail_block ? 1.f : scales[2 * j + 1];
+            v16f s[2];
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[tt][i] = 0.f;
+#pragma unroll
+                for (int m = 0; m < NP; ++m)
+                    s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const v8h *>(kt + ((tt * NP + m) * 64 + l) * 16), qf[m], s[tt], 0, 0, 0);
+            }
+            float top = -INFINITY;
+            const bool whole = (j + 1) * kBlock - 1 <= wave_first;    // every row sees every position
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    s[tt][i] *= sk;
+                    if (!whole && j * kBlock + 32 * tt + 8 * (i >> 2) + 4 * h + (i & 3) > sees) s[tt][i] = -INFINITY;
+                    top = fmaxf(top, s[tt][i]);
+                }
+            top = fmaxf(top, __shfl_xor(top, 32));
+            float change;
+            const float factor = unit.enter(sv, change);
+            if (top > mrun) {                                         // (a row that sees nothing of the block keeps its maximum)
+                const float raise = exp2f(mrun - top);
+                change *= raise;
+                lrun *= raise;
+                mrun = top;
+            }
+            if (__any(change != 1.f)) {
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) ot[ct][i] *= change;
+            }
+            v8h p[4];
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float e = exp2f(s[tt][i] - mrun);
+                    lrun += e;
+                    p[2 * tt + (i >> 3)][i & 7] = (_Float16)(e == 0.f ? 0.f : e * factor);
+                }
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+                    ot[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const v8h *>(vt + ((ct * 4 + n) * 64 + l) * 16), p[n], ot[ct], 0, 0, 0);
+        }
+        keep(j + 1);
+    }
+    lrun += __shfl_xor(lrun, 32);
+    const float norm = unit.unit / lrun;
+    const bool odd = tile_last / kBlock == tail_block && not_finite;
+    if (mine >= n_rows) return;
+    __half *to = O + (int64_t)(sp.row + query) * ldo + (int64_t)head * D;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            const int col = 32 * ct + 8 * a + 4 * h;
+            union { __half h[4]; v2u v; } u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float o = ot[ct][4 * a + i] * norm;
+                if (odd) {                                            // infinities and NaN among the tail's values that this row sees
+                    for (int s = 0; s <= sees - tail_block * kBlock; ++s) {
+                        const float x = __half2float(tail_v[s * D + col + i]);
+                        if (!(fabsf(x) <= 65504.f)) o += x;
+                    }
+                }
+                u.h[i] = __float2half_rn(o);
+            }
+            *reinterpret_cast<v2u *>(to + col) = u.v;
+        }
+}
+
+// ---------------------------------------------------------------- attention of one row per sequence
+
+// One workgroup per sequence, key head, up to 16 of the query heads that share it, and share of the sequence's blocks; a block is one
+// wavefront's.  The workgroup whose share ends with the last block appends the new row there.  Where there are several shares, each leaves
+// its sums in the workspace and the workgroup that arrives last adds them in their order.
+constexpr int kDecodeWaves = 4;
+struct DecodeArgs {
+    const __half *QKV;
+    int64_t ld;
+    const int32_t *pos, *past;
+    int H, G, chunks, shares;
+    Cache8View cache;
+    __half *O;
+    int64_t ldo;
+    unsigned *counters;
+    float *partials;
+    RopeFreq freq;
+};
+
+template <int D>
+struct DecodeLds {
+    __attribute__((aligned(16))) _Float16 q[16][D];
+    __attribute__((aligned(16))) union {
+        struct {
+            _Float16 k[kBlock][D + 8];           // rows of the last block
+            _Float16 v[D][kBlock + 8];           // its values, transposed, positions in the order of the codes
+        } tail;
+        float o[kDecodeWaves][16][D + 4];        // the wavefronts' sums
+    } u;
+    double cs[D / 2], sn[D / 2];
+    __half knew[D], vnew[D];
+    float m[kDecodeWaves][16], l[kDecodeWaves][16];
+    unsigned top[2][kDecodeWaves];
+    int odd[D];                                  // what is not finite among a column's values in the tail: 1 infinity, 2 minus infinity, 4 NaN
+    int arrived;
+};
+
+// slot of position s in the values' order: 8 of each 32 per lane group
+__device__ __forceinline__ int value_slot(int s) { return (s & 32) | ((s >> 2) & 3) << 3 | ((s >> 4) & 1) << 2 | (s & 3); }
+
+template <int D>
+__global__ __launch_bounds__(64 * kDecodeWaves) void cache8_decode_kernel(const DecodeArgs a)
+{
+    constexpr int HALF = D / 2, C = D / 64, T = 64 * kDecodeWaves, DT = D / 16;
+    __shared__ DecodeLds<D> lds;
+    const Cache8View &cache = a.cache;
+    const int share = blockIdx.x, kh = blockIdx.y / a.chunks, chunk = blockIdx.y % a.chunks, b = blockIdx.z;
+    const int t = threadIdx.x, l = t & 63, wave = t >> 6, r = l & 15, g = l >> 4;
+    const int first_head = kh * a.G + chunk * 16, heads = min(16, a.G - chunk * 16);
+    const int past = a.past[b];
+    if (past < 0) return;
+    const __half *row = a.QKV + (int64_t)b * a.ld;
+    __half *out = a.O + (int64_t)b * a.ldo + (int64_t)first_head * D;
+    if (past >= cache.blocks * kBlock) {                              // no room: nothing is appended, and the outputs say so
+        if (share == 0)
+            for (int i = t; i < heads * D; i += T) out[i] = __ushort_as_half(0x7e00);
+        return;
+    }
+    const int last = past / kBlock, slot = past % kBlock;
+    const int per_share = (last + 1 + a.shares - 1) / a.shares, active = (last + per_share) / per_share;
+    const int begin = share * per_share, stop = min(begin + per_share, last + 1);
+    if (begin > last) return;
+    const bool has_last = stop == last + 1;
+    const int64_t head = (int64_t)b * cache.kv_heads + kh;
+    __half *tail_k = cache.tail + head * 2 * kBlock * D, *tail_v = tail_k + kBlock * D;
+
+    if (t < HALF) sincos((double)a.pos[b] * a.freq.f[t], &lds.sn[t], &lds.cs[t]);
+    __syncthreads();
+    for (int u = t; u < heads * HALF; u += T) {
+        const int j = u / HALF, i = u % HALF;
+        const __half *q = row + (int64_t)(first_head + j) * D;
+        __half x, y;
+        rotate_pair(q[i], q[i + HALF], lds.cs[i], lds.sn[i], x, y);
+        lds.q[j][i] = (_Float16)__half2float(x);
+        lds.q[j][i + HALF] = (_Float16)__half2float(y);
+    }
+    if (t < D) lds.odd[t] = 0;
+    if (has_last && t < HALF) {
+        const __half *k = row + (int64_t)(a.H + kh) * D, *v = row + (int64_t)(a.H + cache.kv_heads + kh) * D;
+        rotate_pair(k[t], k[t + HALF], lds.cs[t], lds.sn[t], lds.knew[t], lds.knew[t + HALF]);
+        lds.vnew[t] = v[t];
+        lds.vnew[t + HALF] = v[t + HALF];
+    }
+    __syncthreads();
+    float tail_sk = 1.f, tail_sv = 1.f;
+    if (has_last) {
+        const bool full = slot == kBlock - 1;
+        unsigned top_k = 0, top_v = 0;
+        for (int u = t; u < kBlock * D / 8; u += T) {
+            const int s = u / (D / 8), x = (u % (D / 8)) * 8;
+            union { v4i i; __half h[8]; } k = {v4i{0, 0, 0, 0}}, v = {v4i{0, 0, 0, 0}};
+            if (s < slot) {
+                k.i = *reinterpret_cast<const v4i *>(tail_k + s * D + x);
+                v.i = *reinterpret_cast<const v4i *>(tail_v + s * D + x);
+            } else if (s == slot) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) k.h[e] = lds.knew[x + e], v.h[e] = lds.vnew[x + e];
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                top_k = max(top_k, magnitude(k.h[e]));
+                top_v = max(top_v, magnitude(v.h[e]));
+                const float w = __half2float(v.h[e]);
+                // (times the low half of a probability, zero or negative as often as not, an infinity would be NaN: it is added at the end)
+                const bool odd = !full && !finite_bits(magnitude(v.h[e]));
+                if (odd) atomicOr(&lds.odd[x + e], w > 0.f ? 1 : w < 0.f ? 2 : 4);
+                lds.u.tail.v[x + e][value_slot(s)] = odd ? (_Float16)0.f : (_Float16)w;
+            }
+            *reinterpret_cast<v4i *>(&lds.u.tail.k[s][x]) = k.i;
+        }
+        if (full) {
+            top_k = wavefront_umax(top_k);
+            top_v = wavefront_umax(top_v);
+            if (l == 0) lds.top[0][wave] = top_k, lds.top[1][wave] = top_v;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < kDecodeWaves; ++w) top_k = max(top_k, lds.top[0][w]), top_v = max(top_v, lds.top[1][w]);
+            tail_sk = scale_of(top_k);
+            tail_sv = scale_of(top_v);
+            const bool ok_k = finite_bits(top_k), ok_v = finite_bits(top_v);
+            const Steps sk = steps_of(__half2float(__ushort_as_half((unsigned short)top_k))), sv = steps_of(__half2float(__ushort_as_half((unsigned short)top_v)));
+            int *kc = reinterpret_cast<int *>(block_codes<D>(cache, head, last, 0)), *vc = reinterpret_cast<int *>(block_codes<D>(cache, head, last, 1));
+            // words of four codes, in the order of the cache; the rows in LDS become their codes
+            for (int u = t; u < kBlock * D / 4; u += T) {
+                const int e4 = u & 3, lane = (u >> 2) & 63, x = u >> 8, lr = lane & 15, lg = lane >> 4;
+                _Float16 *k = &lds.u.tail.k[(x / C) * 16 + lr][(x % C) * 64 + lg * 16 + e4 * 4];
+                _Float16 *v = &lds.u.tail.v[x * 16 + lr][(e4 >> 1) * 32 + lg * 8 + (e4 & 1) * 4];
+                int wk = 0, wv = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int ck = ok_k ? code_of((float)k[e], sk) : 0, cv = ok_v ? code_of((float)v[e], sv) : 0;
+                    k[e] = (_Float16)(float)ck;
+                    v[e] = (_Float16)(float)cv;
+                    wk |= (ck & 255) << (8 * e);
+                    wv |= (cv & 255) << (8 * e);
+                }
+                if (chunk == 0) {
+                    kc[u] = wk;
+                    vc[u] = wv;
+                }
+            }
+            if (chunk == 0 && t == 0) {
+                float *to = cache.scales + (head * cache.blocks + last) * 2;
+                to[0] = tail_sk;
+                to[1] = tail_sv;
+            }
+        } else if (chunk == 0 && t < D) {
+            tail_k[slot * D + t] = lds.knew[t];
+            tail_v[slot * D + t] = lds.vnew[t];
+        }
+        __syncthreads();
+    }
+
+    // queries: column r of the products; columns past the heads repeat the last head
+    v8h qf[2 * C];
+#pragma unroll
+    for (int m = 0; m < 2 * C; ++m) qf[m] = *reinterpret_cast<const v8h *>(&lds.q[min(r, heads - 1)][64 * (m >> 1) + 16 * g + 8 * (m & 1)]);
+    v4f ot[DT];
+#pragma unroll
+    for (int i = 0; i < DT; ++i) ot[i] = v4f{0.f, 0.f, 0.f, 0.f};
+    float mrun = -INFINITY, lrun = 0.f;
+    Unit unit;
+    const float per_d = kLog2e / sqrtf((float)D);
+    const float *scales = cache.scales + head * cache.blocks * 2;
+    for (int j = begin + wave; j < stop; j += kDecodeWaves) {
+        const bool is_last = j == last;
+        v4f s[4];
+        v4i vraw[DT];
+        float sk, sv;
+#pragma unroll
+        for (int T4 = 0; T4 < 4; ++T4) s[T4] = v4f{0.f, 0.f, 0.f, 0.f};
+        if (!is_last) {
+            const v4i *k = reinterpret_cast<const v4i *>(block_codes<D>(cache, head, j, 0)) + l, *v = reinterpret_cast<const v4i *>(block_codes<D>(cache, head, j, 1)) + l;
+            v4i kraw[4 * C];
+#pragma unroll
+            for (int i = 0; i < 4 * C; ++i) kraw[i] = k[i * 64];
+#pragma unroll
+            for (int i = 0; i < DT; ++i) vraw[i] = v[i * 64];
+            sk = scales[2 * j] * per_d;
+            sv = scales[2 * j + 1];
+#pragma unroll
+            for (int T4 = 0; T4 < 4; ++T4)
+#pragma unroll
+                for (int m = 0; m < 2 * C; ++m) {
+                    const v4i w = kraw[T4 * C + (m >> 1)];
+                    s[T4] = __builtin_amdgcn_mfma_f32_16x16x32_f16((m & 1) ? halves_of(w[2], w[3]) : halves_of(w[0], w[1]), qf[m], s[T4], 0, 0, 0);
+                }
+        } else {
+            sk = tail_sk * per_d;
+            sv = tail_sv;
+#pragma unroll
+            for (int T4 = 0; T4 < 4; ++T4)
+#pragma unroll
+                for (int m = 0; m < 2 * C; ++m)
+                    s[T4] = __builtin_amdgcn_mfma_f32_16x16x32_f16(*reinterpret_cast<const v8h *>(&lds.u.tail.k[16 * T4 + r][64 * (m >> 1) + 16 * g + 8 * (m & 1)]),
+                                                                   qf[m], s[T4], 0, 0, 0);
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int T4 = 0; T4 < 4; ++T4)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[T4][i] *= sk;
+                if (is_last && 16 * T4 + 4 * g + i > slot) s[T4][i] = -INFINITY;
+                top = fmaxf(top, s[T4][i]);
+            }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        float change;
+        const float factor = unit.enter(sv, change);
+        if (top > mrun) {
+            const float raise = exp2f(mrun - top);
+            change *= raise;
+            lrun *= raise;
+            mrun = top;
+        }
+#pragma unroll
+        for (int i = 0; i < DT; ++i) ot[i] *= change;
+        v8h p[2], rest[2];                                            // a probability as the sum of two halves
+#pragma unroll
+        for (int T4 = 0; T4 < 4; ++T4)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float e = exp2f(s[T4][i] - mrun), w = e == 0.f ? 0.f : e * factor;
+                lrun += e;
+                const _Float16 w0 = (_Float16)w;
+                p[T4 >> 1][(T4 & 1) * 4 + i] = w0;
+                rest[T4 >> 1][(T4 & 1) * 4 + i] = (_Float16)(w - (float)w0);
+            }
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const v8h v = is_last ? *reinterpret_cast<const v8h *>(&lds.u.tail.v[16 * i + r][32 * n + 8 * g]) : halves_of(vraw[i][2 * n], vraw[i][2 * n + 1]);
+                ot[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[n], ot[i], 0, 0, 0);
+                ot[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, rest[n], ot[i], 0, 0, 0);
+            }
+    }
+    lrun += __shfl_xor(lrun, 16);
+    lrun += __shfl_xor(lrun, 32);
+    __syncthreads();                                                  // the last block's rows have been read
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) lds.u.o[wave][r][16 * i + 4 * g + e] = ot[i][e] * unit.unit;
+    if (g == 0) {
+        lds.m[wave][r] = mrun;
+        lds.l[wave][r] = lrun;
+    }
+    __syncthreads();
+    // the wavefronts' sums in one
+    const int64_t item = (int64_t)b * gridDim.y + blockIdx.y;
+    const int per_item = heads_of_partial(a.G) * (D + 2);
+    float *mine = a.partials + (item * a.shares + share) * per_item;
+    auto merged = [&](int j, int i, float &top, float &sum) {
+        top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kDecodeWaves; ++w) top = fmaxf(top, lds.m[w][j]);
+        sum = 0.f;
+        float o = 0.f;
+#pragma unroll
+        for (int w = 0; w < kDecodeWaves; ++w) {
+            if (begin + w >= stop) break;                             // a wavefront without a block
+            const float f = exp2f(lds.m[w][j] - top);
+            sum += f * lds.l[w][j];
+            o += f * lds.u.o[w][j][i];
+        }
+        const int odd = lds.odd[i];
+        if (odd) o = odd == 1 ? o + INFINITY : odd == 2 ? o - INFINITY : NAN;
+        return o;
+    };
+    if (active == 1) {
+        for (int u = t; u < heads * D; u += T) {
+            float top, sum;
+            const float o = merged(u / D, u % D, top, sum);
+            out[u] = __float2half_rn(o / sum);
+        }
+        return;
+    }
+    for (int u = t; u < heads * D; u += T) {
+        float top, sum;
+        const float o = merged(u / D, u % D, top, sum);
+        __hip_atomic_store(mine + u, o, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (u % D == 0) {
+            __hip_atomic_store(mine + heads * D + u / D, top, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(mine + heads * D + heads + u / D, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                  // this wavefront's stores have arrived before the workgroup does
+    __syncthreads();
+    if (t == 0) lds.arrived = (int)__hip_atomic_fetch_add(a.counters + item, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (lds.arrived != active - 1) return;
+    if (t == 0) __hip_atomic_store(a.counters + item, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // the next call starts from zero again
+    const float *all = a.partials + item * a.shares * per_item;
+    for (int u = t; u < heads * D; u += T) {
+        const int j = u / D;
+        float top = -INFINITY, sum = 0.f, o = 0.f;
+        for (int w = 0; w < active; ++w)
+            top = fmaxf(top, __hip_atomic_load(all + (int64_t)w * per_item + heads * D + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+        for (int w = 0; w < active; ++w) {
+            const float *from = all + (int64_t)w * per_item;
+            const float f = exp2f(__hip_atomic_load(from + heads * D + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) - top);
+            sum += f * __hip_atomic_load(from + heads * D + heads + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            o += f * __hip_atomic_load(from + u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        out[u] = __float2half_rn(o / sum);
+    }
+}
+
+// ---------------------------------------------------------------- launches
+
+sqap_status launch_cache8_append(const __half *QKV, int64_t ld, const int32_t *starts, const int32_t *pos, const int32_t *past, int rows, int max_new,
+                                 int H, double base, const Cache8View &cache, int d, __half *Q_out, int64_t ldq, hipStream_t st)
+{
+    const int touched = (max_new + kBlock - 2) / kBlock + 1;          // blocks of the longest sequence, at most
+    const dim3 grid(std::max(1, touched - 1), cache.kv_heads, cache.batch);
+    const RopeFreq freq = rope_frequencies(d, base);
+    if (d == 64) hipLaunchKernelGGL(cache8_append_kernel<64>, grid, dim3(256), 0, st, QKV, ld, starts, pos, past, rows, max_new, H, cache, Q_out, ldq, freq);
+    else hipLaunchKernelGGL(cache8_append_kernel<128>, grid, dim3(256), 0, st, QKV, ld, starts, pos, past, rows, max_new, H, cache, Q_out, ldq, freq);
+    SQAP_HIP_CHECK(hipGetLastError());
+    return SQAP_OK;
+}
+
+sqap_status launch_cache8_read(const Cache8View &cache, int d, const int32_t *lengths, int first, int count, __half *out, int64_t ld, hipStream_t st)
+{
+    const dim3 grid(count, cache.batch);
+    if (d == 64) hipLaunchKernelGGL(cache8_read_kernel<64>, grid, dim3(256), 0, st, cache, lengths, first, count, out, ld);
+    else hipLaunchKernelGGL(cache8_read_kernel<128>, grid, dim3(256), 0, st, cache, lengths, first, count, out, ld);
+    SQAP_HIP_CHECK(hipGetLastError());
+    return SQAP_OK;
+}
+
+template <int D>
+static sqap_status launch_attention_d(const __half *Q, int64_t ldq, const int32_t *starts, const int32_t *past, int rows, int max_new, int H,
+                                      const Cache8View &cache, __half *O, int64_t ldo, hipStream_t st)
+{
+    constexpr int LDS = 2 * 2 * kBlock * D * 2;
+    const int64_t tiles = ((int64_t)max_new * (H / cache.kv_heads) + kRowsOfTile - 1) / kRowsOfTile;
+    static std::atomic<bool> ready[kMaxDeviceSlots];
+    if (LDS > 65536 - 64 && !ready[device_slot()].load(std::memory_order_relaxed)) {
+        SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(cache8_attention_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+        ready[device_slot()].store(true, std::memory_order_relaxed);
+    }
+    hipLaunchKernelGGL(cache8_attention_kernel<D>, dim3((unsigned)tiles, cache.kv_heads, cache.batch), dim3(256), LDS, st, Q, ldq, starts, past, rows, max_new, H,
+                       cache, O, ldo);
+    SQAP_HIP_CHECK(hipGetLastError());
+    return SQAP_OK;
+}
+
+sqap_status launch_cache8_attention(const __half *Q, int64_t ldq, const int32_t *starts, const int32_t *past, int rows, int max_new, int H,
+                                    const Cache8View &cache, int d, __half *O, int64_t ldo, hipStream_t st)
+{
+    return d == 64 ? launch_attention_d<64>(Q, ldq, starts, past, rows, max_new, H, cache, O, ldo, st)
+                   : launch_attention_d<128>(Q, ldq, starts, past, rows, max_new, H, cache, O, ldo, st);
+}
+
+// Shares of a sequence: as many workgroups as fill the device a few times over, four blocks at least to each (one per wavefront).
+static int decode_shares(int batch, int H, int kv_heads, int longest)
+{
+    const int chunks = (H / kv_heads + 15) / 16, blocks = (longest + kBlock - 1) / kBlock;
+    const int64_t items = (int64_t)batch * kv_heads * chunks;
+    return (int)std::max<int64_t>(1, std::min<int64_t>((blocks + kDecodeWaves - 1) / kDecodeWaves, 1024 / items));
+}
+
+// counters in front: room for one per sequence and query head (a workgroup uses one)
+static size_t counter_bytes(int batch, int H) { return ((size_t)batch * H * 4 + 255) / 256 * 256; }
+
+size_t cache8_workspace_bytes(int batch, int H, int kv_heads, int d, int longest)
+{
+    const int shares = decode_shares(batch, H, kv_heads, longest), G = H / kv_heads;
+    if (shares == 1) return 0;
+    const size_t items = (size_t)batch * kv_heads * ((G + 15) / 16);
+    return counter_bytes(batch, H) + items * shares * heads_of_partial(G) * (d + 2) * 4;
+}
+
+sqap_status launch_cache8_decode(const __half *QKV, int64_t ld, const int32_t *pos, const int32_t *past, int H, double base, const Cache8View &cache,
+                                 int d, int longest, __half *O, int64_t ldo, void *workspace, hipStream_t st)
+{
+    DecodeArgs a = {};
+    a.QKV = QKV;
+    a.ld = ld;
+    a.pos = pos;
+    a.past = past;
+    a.H = H;
+    a.G = H / cache.kv_heads;
+    a.chunks = (a.G + 15) / 16;
+    a.shares = decode_shares(cache.batch, H, cache.kv_heads, longest);
+    a.cache = cache;
+    a.O = O;
+    a.ldo = ldo;
+    a.counters = static_cast<unsigned *>(workspace);
+    a.partials = reinterpret_cast<float *>(static_cast<char *>(workspace) + counter_bytes(cache.batch, H));
+    a.freq = rope_frequencies(d, base);
+    const dim3 grid(a.shares, cache.kv_heads * a.chunks, cache.batch);
+    if (d == 64) hipLaunchKernelGGL(cache8_decode_kernel<64>, grid, dim3(64 * kDecodeWaves), 0, st, a);
+    else hipLaunchKernelGGL(cache8_decode_kernel<128>, grid, dim3(64 * kDecodeWaves), 0, st, a);
+    SQAP_HIP_CHECK(hipGetLastError());
+    return SQAP_OK;
+}
+
+}  // namespace sqap

@@ -147,6 +147,9 @@ struct Calls {
     decltype(&sqap_w4a4_linear) w4a4_linear;
     decltype(&sqap_mx4_quantize) mx4_quantize;
     decltype(&sqap_mx4_linear) mx4_linear;
+    decltype(&sqap_cache8_append) cache8_append;
+    decltype(&sqap_cache8_attention) cache8_attention;
+    decltype(&sqap_cache8_decode_attention) cache8_decode_attention;
     decltype(&sqap_group_run) group_run;
     decltype(&sqap_decoder_step) decoder_step;
     PyObject *failed;                     // called with a status that is not zero: raises
@@ -248,6 +251,16 @@ SQAP_METHOD(mx4_quantize, 5,
 SQAP_METHOD(mx4_linear, 5,
             run(c->mx4_linear, ptr<uint8_t>(a[0]), ptr<uint8_t>(a[1]), (int32_t)size(a[0], 0), handle<sqap_mx4_weight>(a[2]),
                 ptr<sqap_f16>(a[3]), pitch(a[3]), stream(c, a[4])))
+SQAP_METHOD(cache8_append, 10,
+            run(c->cache8_append, ptr<sqap_f16>(a[0]), pitch(a[0]), ptr<int32_t>(a[1]), ptr<int32_t>(a[2]), ptr<int32_t>(a[3]), (int32_t)size(a[0], 0),
+                as_i32(a[6]), as_i32(a[5]), as_double(a[8]), handle<sqap_cache8>(a[4]), ptr<sqap_f16>(a[7]), a[7] == Py_None ? 0 : pitch(a[7]),
+                stream(c, a[9])))
+SQAP_METHOD(cache8_attention, 8,
+            run(c->cache8_attention, ptr<sqap_f16>(a[0]), pitch(a[0]), ptr<int32_t>(a[1]), ptr<int32_t>(a[2]), (int32_t)size(a[0], 0), as_i32(a[5]),
+                as_i32(a[4]), handle<sqap_cache8>(a[3]), ptr<sqap_f16>(a[6]), pitch(a[6]), stream(c, a[7])))
+SQAP_METHOD(cache8_decode_attention, 10,
+            run(c->cache8_decode_attention, ptr<sqap_f16>(a[0]), pitch(a[0]), ptr<int32_t>(a[1]), ptr<int32_t>(a[2]), as_i32(a[4]), as_double(a[8]),
+                handle<sqap_cache8>(a[3]), as_i32(a[7]), ptr<sqap_f16>(a[5]), pitch(a[5]), ptr(a[6]), bytes(a[6]), stream(c, a[9])))
 SQAP_METHOD(group_run, 2, run(c->group_run, handle<sqap_group>(a[0]), stream(c, a[1])))
 SQAP_METHOD(decoder_step, 7,
             run(c->decoder_step, handle<sqap_decoder>(a[0]), ptr<sqap_f16>(a[1]), ptr<int32_t>(a[2]), as_i32(a[3]), ptr<sqap_f16>(a[4]),
@@ -273,7 +286,8 @@ SQAP_METHOD(attention, 8, attention_call(c, a))
 
 #define SQAP_CALLS(X)                                                                                                                   \
     X(attn_scores_batch) X(prune_topk) X(kept_rows) X(prune_rows) X(prune_select) X(quantize_act) X(rmsnorm_quantize_act)              \
-    X(swiglu_quantize_act) X(rope) X(rope_append) X(attention) X(decode_attention) X(w4a4_linear) X(mx4_quantize) X(mx4_linear) X(group_run) X(decoder_step)
+    X(swiglu_quantize_act) X(rope) X(rope_append) X(attention) X(decode_attention) X(w4a4_linear) X(mx4_quantize) X(mx4_linear) X(cache8_append) X(cache8_attention)                              \
+    X(cache8_decode_attention) X(group_run) X(decoder_step)
 
 PyMethodDef methods[] = {
 #define SQAP_ENTRY(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(m_##NAME)), METH_FASTCALL, nullptr},

@@ -109,6 +109,17 @@ struct Mx4Weight {
 constexpr uint32_t kMx4Magic = 0x53514d34u;  // "SQM4"
 constexpr int kMx4MaxK = 1 << 20, kMx4MaxRows = 1 << 24;
 
+// A key/value cache in 8 bits (cache8.hip): the caller's buffers as include/sqap.h describes them.
+constexpr int kCache8Block = SQAP_CACHE8_BLOCK;
+struct Cache8View {
+    int8_t *codes;             // [batch][kv_heads][blocks][keys, values][64 d]
+    float *scales;             // [batch][kv_heads][blocks][keys, values]
+    __half *tail;              // [batch][kv_heads][keys, values][64][d]
+    int batch, blocks, kv_heads;
+};
+// query heads that share a key head, at most as many as a workgroup takes
+static __host__ __device__ inline int heads_of_partial(int G) { return G < 16 ? G : 16; }
+
 static inline hipStream_t as_stream(void *s) { return reinterpret_cast<hipStream_t>(s); }
 
 // Launcher state that belongs to a device (function attributes set, CU count): one slot per device
@@ -236,6 +247,15 @@ void set_mid_m_kernel(int which);        // 0: tiles split along K between workg
 sqap_status launch_mx4_quantize(const __half *X, int64_t ldx, const int32_t *rows, int M, int K, uint8_t *Xq, uint8_t *Xs, hipStream_t st);
 sqap_status launch_mx4_pack(const uint8_t *Wq, const uint8_t *Ws, const Mx4Weight &w, hipStream_t st);
 sqap_status launch_mx4_linear(const uint8_t *Xq, const uint8_t *Xs, int M, const Mx4Weight &w, __half *Y, int64_t ldy, hipStream_t st);
+
+sqap_status launch_cache8_append(const __half *QKV, int64_t ld, const int32_t *starts, const int32_t *pos, const int32_t *past, int rows, int max_new,
+                                 int H, double base, const Cache8View &cache, int d, __half *Q_out, int64_t ldq, hipStream_t st);
+sqap_status launch_cache8_attention(const __half *Q, int64_t ldq, const int32_t *starts, const int32_t *past, int rows, int max_new, int H,
+                                    const Cache8View &cache, int d, __half *O, int64_t ldo, hipStream_t st);
+size_t cache8_workspace_bytes(int batch, int H, int kv_heads, int d, int longest);
+sqap_status launch_cache8_decode(const __half *QKV, int64_t ld, const int32_t *pos, const int32_t *past, int H, double base, const Cache8View &cache,
+                                 int d, int longest, __half *O, int64_t ldo, void *workspace, hipStream_t st);
+sqap_status launch_cache8_read(const Cache8View &cache, int d, const int32_t *lengths, int first, int count, __half *out, int64_t ld, hipStream_t st);
 
 sqap_status launch_rope(__half *X, int64_t ld, const int32_t *pos, int S, int H, int d, double base, hipStream_t st);
 sqap_status launch_rope_append(__half *QKV, int64_t ld, const int32_t *pos, int S, int H, int d, double base,

@@ -44,3 +44,63 @@ def mx4_values(code, scale):
     v = np.where(code >= 8, -LEVELS[code & 7], LEVELS[code & 7]).reshape(code.shape[0], -1, 32)
     s = np.where(scale == 255, np.nan, np.exp2(scale.astype(np.float64) - 127.0))
     return (v * s[..., None]).reshape(code.shape)
+
+
+# ---------------------------------------------------------------- the 8-bit cache and attention over it
+
+BLOCK = 64
+
+
+def turn(x, pos, base=10000.0):
+    """x [rows, heads, d] halves at positions pos [rows]: half-split rotation in binary64, rounded to binary32 and that to half."""
+    d = x.shape[-1]
+    a = np.asarray(pos, dtype=np.float64)[:, None, None] * base ** (-2.0 * np.arange(d // 2) / d)
+    lo, hi = x[..., :d // 2].astype(np.float64), x[..., d // 2:].astype(np.float64)
+    return np.concatenate([lo * np.cos(a) - hi * np.sin(a), hi * np.cos(a) + lo * np.sin(a)], -1).astype(np.float32).astype(np.float16)
+
+
+def block_codes(x):
+    """x [64, d] halves -> codes, scale (binary32)."""
+    top = np.abs(x.astype(np.float64)).max() if np.isfinite(x).all() else np.nan
+    if not np.isfinite(top):
+        return np.zeros(x.shape), np.float32(np.nan)
+    scale = np.float32(top) / np.float32(127.0)
+    return (np.rint(127.0 * x.astype(np.float64) / top) if top > 0 else np.zeros(x.shape)), scale
+
+
+def held(x):
+    """x [n, d] halves of one head, as the cache holds them: values in binary64 (a NaN scale makes a block NaN)."""
+    out = x.astype(np.float64)
+    for j in range(x.shape[0] // BLOCK):
+        codes, scale = block_codes(x[j * BLOCK:(j + 1) * BLOCK])
+        out[j * BLOCK:(j + 1) * BLOCK] = codes * np.float64(scale)
+    return out
+
+
+def attend(q, k, v, sees):
+    """q [rows, d], k, v [n, d] values, row i sees positions 0 .. sees[i]: outputs, sum of p |v|, and how far the scores may be off in
+    binary32 (d products and a few operations, each rounded or truncated), relative to a probability."""
+    s = q @ k.T / math.sqrt(q.shape[1])
+    hidden = np.arange(k.shape[0])[None] > np.asarray(sees)[:, None]
+    s = np.where(hidden, -np.inf, s)
+    p = np.exp(s - s.max(-1, keepdims=True))
+    p = np.where(hidden, 0.0, p)
+    p = p / p.sum(-1, keepdims=True)
+    vv = np.where(np.isfinite(v), v, 0.0)
+    o = p @ vv
+    for i in range(q.shape[0]):                                    # infinities and NaN only where they are seen
+        seen = v[:sees[i] + 1]
+        odd = ~np.isfinite(seen)
+        if odd.any():
+            with np.errstate(invalid="ignore"):
+                o[i] = o[i] + np.where(odd, seen, 0.0).sum(0)
+    size = (np.abs(q) @ np.where(np.isfinite(k), np.abs(k), 0.0).T / math.sqrt(q.shape[1])).max(-1, keepdims=True)
+    return o, p @ np.abs(vv), (q.shape[1] + 16) * 2.0 ** -23 * size
+
+
+def attention_bound(o, mass, score_off, n, v_top, single_half):
+    """Largest difference of a half output from `o`.  A probability is off by the scores' error, a few roundings of binary32 and, where it
+    enters as one half, half a step of it; numerator and denominator count.  A probability below the normal halves is off by
+    up to 2^-25 of the largest one; the output is rounded once."""
+    rel = 2.0 * (score_off + (n / 32 + 16) * 2.0 ** -23) + (HALF_STEP if single_half else 2.0 ** -21)
+    return HALF_STEP * np.abs(o) * (1 + rel) + HALF_TINY + rel * mass + n * 2.0 ** -25 * v_top
