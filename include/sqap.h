@@ -541,6 +541,28 @@ sqap_status sqap_cache8_read(const sqap_cache8 *cache, const int32_t *lengths, i
                              sqap_f16 *out, int64_t ld, void *stream);
 
 /*
+ * The next token of each of `batch` rows of logits [batch, vocab] (halves, pitch ld, any alignment), as the vocabulary
+ * head or sqap_decoder_step leaves them.  Tokens are ranked by logit, the lower index first among equals (-0 == +0;
+ * NaN and minus infinity are never drawn).  With w = exp((l - max) / temperature):
+ *   top_k   the top_k first in rank stay (<= 0 or >= vocab: all)
+ *   top_p   of those, a token stays if the mass of those before it in rank is below top_p times their mass (>= 1: all;
+ *           <= 0 or NaN: the first)
+ *   min_p   of those, a token stays if w >= min_p (the first always does; <= 0 or NaN: all; above 1 acts as 1)
+ * and the drawn one is, in index order, the first whose cumulated mass exceeds uniform times the mass of what stayed.
+ * temperature <= 0 or NaN: the first in rank, with probability 1.  A row without a logit above minus infinity gets the token -1
+ * and the probability 0; of several infinite logits each weighs the same.
+ * temperature, top_k, top_p, min_p: device, [batch] each, or NULL (1, all, all, all).  uniform: device, [batch], numbers
+ * in [0, 1) (others are taken to the nearer end, NaN to 0).  token_out: device, [batch] int32.  prob_out: device, [batch]
+ * binary32, or NULL: the probability with which the token was drawn, among those that stayed.
+ * Masses are integers of 2^-40 of the largest (a token below that is never drawn), so sums are exact and every call gives
+ * the same; a mass itself is off by a few units in the 22nd bit.  No workspace; may be captured.
+ * EINVAL: null pointer, negative size, vocab < 1, ld < vocab.  EUNSUPPORTED: vocab > 1048576.
+ */
+sqap_status sqap_sample(const sqap_f16 *logits, int64_t ld, int32_t batch, int32_t vocab, const float *temperature,
+                        const int32_t *top_k, const float *top_p, const float *min_p, const float *uniform,
+                        int32_t *token_out, float *prob_out, void *stream);
+
+/*
  * Self-test of the quantizer's arithmetic.  The quantizer divides every element
  * of a row by the same scale; it does so with the reciprocal in two parts and
  * one fused multiply-add, which gives the correctly rounded binary32 quotient.

@@ -30,6 +30,7 @@ EXPORTS = (
     "sqap_decoder_set_wait_limit", "sqap_decoder_free",
     "sqap_mx4_quantize", "sqap_mx4_weight_pack", "sqap_mx4_weight_free", "sqap_mx4_weight_info", "sqap_mx4_linear",
     "sqap_cache8_append", "sqap_cache8_attention", "sqap_cache8_workspace_bytes", "sqap_cache8_decode_attention", "sqap_cache8_read",
+    "sqap_sample",
 )
 
 
@@ -135,6 +136,7 @@ def lib():
         L.sqap_cache8_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
         L.sqap_cache8_decode_attention.argtypes = [vp, i64, vp, vp, i32, ctypes.c_double, cache, i32, vp, i64, vp, sz, vp]
         L.sqap_cache8_read.argtypes = [cache, vp, i32, i32, vp, i64, vp]
+        L.sqap_sample.argtypes = [vp, i64, i32, i32] + [vp] * 8
         for name in EXPORTS:
             if name not in ("sqap_last_error", "sqap_version", "sqap_workspace_bytes", "sqap_attn_scores_workspace_bytes", "sqap_cache8_workspace_bytes"):
                 getattr(L, name).restype = ctypes.c_int32
@@ -497,6 +499,12 @@ def sqap_cache8_decode_attention(QKV, pos, past, cache, H, O, workspace, longest
 def sqap_cache8_read(cache, lengths, first, count, out, stream=None):
     """Positions first .. first + count - 1 of every sequence as halves: out [batch * count, 2 kv_heads d], keys then values."""
     _check(lib().sqap_cache8_read(ctypes.byref(cache._desc), _ptr(lengths), first, count, _ptr(out), out.stride(0), _stream(stream)))
+
+
+def sqap_sample(logits, temperature, top_k, top_p, min_p, uniform, token_out, prob_out=None, stream=None):
+    """Next tokens of logits [batch, vocab] fp16: temperature, top_p, min_p [batch] fp32 and top_k [batch] int32, each or None;
+    uniform [batch] fp32 in [0, 1) -> token_out [batch] int32, prob_out [batch] fp32 or None."""
+    _native.sample(logits, temperature, top_k, top_p, min_p, uniform, token_out, prob_out, stream)
 
 
 class Group:

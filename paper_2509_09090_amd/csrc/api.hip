@@ -843,6 +843,20 @@ sqap_status sqap_cache8_read(const sqap_cache8 *cache, const int32_t *lengths, i
     return launch_cache8_read(v, cache->head_dim, lengths, first, count, reinterpret_cast<__half *>(out), ld, as_stream(stream));
 }
 
+sqap_status sqap_sample(const sqap_f16 *logits, int64_t ld, int32_t batch, int32_t vocab, const float *temperature, const int32_t *top_k,
+                        const float *top_p, const float *min_p, const float *uniform, int32_t *token_out, float *prob_out, void *stream)
+{
+    const char *who = "sqap_sample";
+    if (batch < 0 || vocab < 1) return fail(SQAP_EINVAL, "%s: batch %d, vocab %d", who, batch, vocab);
+    if (ld < vocab) return fail(SQAP_EINVAL, "%s: pitch %lld below vocab %d", who, (long long)ld, vocab);
+    if (batch == 0) return SQAP_OK;
+    if (!logits || !uniform || !token_out) return fail(SQAP_EINVAL, "%s: null pointer", who);
+    if (vocab > kSampleMaxVocab) return fail(SQAP_EUNSUPPORTED, "%s: vocab = %d > %d", who, vocab, kSampleMaxVocab);
+    const DeviceOfCall device;
+    return launch_sample(reinterpret_cast<const __half *>(logits), ld, batch, vocab, temperature, top_k, top_p, min_p, uniform, token_out, prob_out,
+                         as_stream(stream));
+}
+
 sqap_status sqap_decoder_create(const sqap_decoder_layer *layers, int32_t n_layers, int32_t n_heads, int32_t head_dim,
                                 const sqap_f16 *gamma_final, const sqap_weight *head, float eps, double rope_base,
                                 sqap_decoder **out)

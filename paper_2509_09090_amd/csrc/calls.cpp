@@ -150,6 +150,7 @@ struct Calls {
     decltype(&sqap_cache8_append) cache8_append;
     decltype(&sqap_cache8_attention) cache8_attention;
     decltype(&sqap_cache8_decode_attention) cache8_decode_attention;
+    decltype(&sqap_sample) sample;
     decltype(&sqap_group_run) group_run;
     decltype(&sqap_decoder_step) decoder_step;
     PyObject *failed;                     // called with a status that is not zero: raises
@@ -261,6 +262,9 @@ SQAP_METHOD(cache8_attention, 8,
 SQAP_METHOD(cache8_decode_attention, 10,
             run(c->cache8_decode_attention, ptr<sqap_f16>(a[0]), pitch(a[0]), ptr<int32_t>(a[1]), ptr<int32_t>(a[2]), as_i32(a[4]), as_double(a[8]),
                 handle<sqap_cache8>(a[3]), as_i32(a[7]), ptr<sqap_f16>(a[5]), pitch(a[5]), ptr(a[6]), bytes(a[6]), stream(c, a[9])))
+SQAP_METHOD(sample, 9,
+            run(c->sample, ptr<sqap_f16>(a[0]), pitch(a[0]), (int32_t)size_of(a[0], 2, 0), (int32_t)size_of(a[0], 2, 1), ptr<float>(a[1]),
+                ptr<int32_t>(a[2]), ptr<float>(a[3]), ptr<float>(a[4]), ptr<float>(a[5]), ptr<int32_t>(a[6]), ptr<float>(a[7]), stream(c, a[8])))
 SQAP_METHOD(group_run, 2, run(c->group_run, handle<sqap_group>(a[0]), stream(c, a[1])))
 SQAP_METHOD(decoder_step, 7,
             run(c->decoder_step, handle<sqap_decoder>(a[0]), ptr<sqap_f16>(a[1]), ptr<int32_t>(a[2]), as_i32(a[3]), ptr<sqap_f16>(a[4]),
@@ -287,7 +291,7 @@ SQAP_METHOD(attention, 8, attention_call(c, a))
 #define SQAP_CALLS(X)                                                                                                                   \
     X(attn_scores_batch) X(prune_topk) X(kept_rows) X(prune_rows) X(prune_select) X(quantize_act) X(rmsnorm_quantize_act)              \
     X(swiglu_quantize_act) X(rope) X(rope_append) X(attention) X(decode_attention) X(w4a4_linear) X(mx4_quantize) X(mx4_linear) X(cache8_append) X(cache8_attention)                              \
-    X(cache8_decode_attention) X(group_run) X(decoder_step)
+    X(cache8_decode_attention) X(sample) X(group_run) X(decoder_step)
 
 PyMethodDef methods[] = {
 #define SQAP_ENTRY(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(m_##NAME)), METH_FASTCALL, nullptr},

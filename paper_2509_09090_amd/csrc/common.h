@@ -257,6 +257,10 @@ sqap_status launch_cache8_decode(const __half *QKV, int64_t ld, const int32_t *p
                                  int d, int longest, __half *O, int64_t ldo, void *workspace, hipStream_t st);
 sqap_status launch_cache8_read(const Cache8View &cache, int d, const int32_t *lengths, int first, int count, __half *out, int64_t ld, hipStream_t st);
 
+constexpr int kSampleMaxVocab = 1 << 20;
+sqap_status launch_sample(const __half *logits, int64_t ld, int batch, int vocab, const float *temperature, const int32_t *top_k,
+                          const float *top_p, const float *min_p, const float *uniform, int32_t *token, float *prob, hipStream_t st);
+
 sqap_status launch_rope(__half *X, int64_t ld, const int32_t *pos, int S, int H, int d, double base, hipStream_t st);
 sqap_status launch_rope_append(__half *QKV, int64_t ld, const int32_t *pos, int S, int H, int d, double base,
                                __half *KV, int64_t ldkv, hipStream_t st);

@@ -104,3 +104,41 @@ def attention_bound(o, mass, score_off, n, v_top, single_half):
     up to 2^-25 of the largest one; the output is rounded once."""
     rel = 2.0 * (score_off + (n / 32 + 16) * 2.0 ** -23) + (HALF_STEP if single_half else 2.0 ** -21)
     return HALF_STEP * np.abs(o) * (1 + rel) + HALF_TINY + rel * mass + n * 2.0 ** -25 * v_top
+
+
+# ---------------------------------------------------------------- sampling
+
+def sample(logits, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, u=0.0):
+    """One row of halves -> token, probability, and how near a decision came to its border (relative to the mass it is about)."""
+    x = logits.astype(np.float64)
+    can = ~np.isnan(x) & (x > -np.inf)
+    if not can.any():
+        return -1, 0.0, 1.0
+    order = np.flatnonzero(can)
+    order = order[np.argsort(-x[order], kind="stable")]
+    top = x[order[0]]
+    if not temperature > 0:
+        return int(order[0]), 1.0, 1.0
+    w = np.zeros(x.shape)
+    w[can] = np.where(x[can] == top, 1.0, 0.0) if np.isinf(top) else np.exp((x[can] - top) / temperature)
+    near = 1.0
+    if top_k > 0:
+        order = order[:top_k]
+    if not top_p >= 1.0:
+        mass = w[order]
+        before = np.cumsum(mass) - mass
+        share = (top_p if top_p > 0 else 0.0) * mass.sum()
+        near = min(near, (np.abs(before[1:] - share) / mass.sum()).min(initial=1.0)) if top_p > 0 else near
+        order = order[:max(1, int((before < share).sum()))]
+    if min_p > 0:
+        least = min(min_p, 1.0)
+        near = min(near, np.abs(w[order[1:]] - least).min(initial=1.0)) if least < 1.0 else near
+        order = order[(w[order] >= least)]
+    index = np.sort(order)
+    cum = np.cumsum(w[index])
+    u = min(max(u, 0.0), np.nextafter(1.0, 0.0)) if u == u else 0.0
+    hit = int((cum <= u * cum[-1]).sum())
+    near = min(near, (np.abs(cum[:-1] - u * cum[-1]) / cum[-1]).min(initial=1.0)) if u > 0 else near
+    if (w[w > 0] == 1.0).all():
+        near = 1.0                                                 # whole masses: both sides add them exactly
+    return int(index[hit]), float(w[index[hit]] / cum[-1]), float(near)

@@ -1,0 +1,187 @@
+"""Sampling from logits against the definition in 64 bits.  A mass is off by 2^-21 of itself at most (an exponential and two products in
+binary32, whose argument carries 2^-24 of at most 41 binary places, and the cut at 2^-40): where a decision of the reference lies nearer than that to
+its border the row says nothing about the token; how many such rows there are is bounded too."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from paper_2509_09090_amd import binding as B
+from tests import lowbit_ref as R
+
+MASS_OFF = 2.0 ** -20
+
+
+def test_refusals():
+    L, p = B.lib(), ctypes.c_void_p(4096)
+    good = dict(logits=p, ld=100, batch=2, vocab=100, temperature=p, top_k=p, top_p=p, min_p=p, uniform=p, token=p, prob=p, stream=None)
+    call = lambda **kw: L.sqap_sample(*{**good, **kw}.values())                  # noqa: E731
+    for bad in (dict(batch=-1), dict(vocab=0), dict(vocab=-5), dict(ld=99), dict(logits=None), dict(uniform=None), dict(token=None)):
+        assert call(**bad) == B.EINVAL, bad
+    assert call(vocab=(1 << 20) + 1, ld=1 << 21) == B.EUNSUPPORTED
+    assert call(batch=0, logits=None) == B.OK
+
+
+@pytest.fixture(scope="module")
+def G():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from tests import gpu_util
+    return gpu_util
+
+
+def _run(G, logits, temperature=None, top_k=None, top_p=None, min_p=None, u=None, pitch=0):
+    import torch
+    b, v = logits.shape
+    wide = torch.full((b, v + pitch), float("nan"), dtype=torch.float16, device=G.DEV)
+    wide[:, :v] = G.to_dev(logits)
+    dev = lambda a, t: None if a is None else G.to_dev(np.asarray(a, dtype=t))   # noqa: E731
+    token = torch.full((b + 1,), -7, dtype=torch.int32, device=G.DEV)
+    prob = torch.full((b + 1,), -7.0, dtype=torch.float32, device=G.DEV)
+    B.sqap_sample(wide[:, :v], dev(temperature, np.float32), dev(top_k, np.int32), dev(top_p, np.float32), dev(min_p, np.float32),
+                  dev(np.zeros(b) if u is None else u, np.float32), token[:b], prob[:b])
+    assert int(token[b]) == -7 and float(prob[b]) == -7.0
+    return token[:b].cpu().numpy(), prob[:b].cpu().numpy()
+
+
+def _check(G, logits, temperature=None, top_k=None, top_p=None, min_p=None, u=None, pitch=0, most_open=0):
+    b = logits.shape[0]
+    token, prob = _run(G, logits, temperature, top_k, top_p, min_p, u, pitch)
+    at = lambda a, i, d: d if a is None else float(np.float32(a[i]))             # noqa: E731
+    n_open = 0
+    for i in range(b):
+        want, p, near = R.sample(logits[i], at(temperature, i, 1.0), int(at(top_k, i, 0)), at(top_p, i, 1.0), at(min_p, i, 0.0), at(u, i, 0.0))
+        if near <= MASS_OFF:
+            n_open += 1
+            continue
+        assert token[i] == want, (i, token[i], want, near)
+        # (a mass is a whole number of 2^-40 of the largest, which is one of those that are added up: a quotient of masses is off by 2^-40 more)
+        assert abs(prob[i] - p) <= 4 * MASS_OFF * p + 2.0 ** -40, (i, prob[i], p)
+    assert n_open <= most_open
+    return token, prob
+
+
+def _logits(rng, b, v):
+    x = rng.standard_normal((b, v)) * rng.uniform(0.3, 6, (b, 1))
+    x[:, : max(1, v // 50)] += 4
+    return rng.permuted(x, axis=1).astype(np.float16)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("b,v,pitch", [(1, 1, 0), (3, 2, 1), (5, 7, 0), (4, 8, 3), (7, 100, 1), (6, 1000, 0), (5, 8191, 1), (5, 8193, 0), (9, 32000, 0),
+                                       (4, 32769, 7), (4, 65537, 0), (3, 128001, 1), (2, 1 << 20, 0)])
+def test_filters(G, b, v, pitch):
+    rng = np.random.default_rng(v + b)
+    x = _logits(rng, b, v)
+    u = rng.random(b).astype(np.float32)
+    t = rng.uniform(0.2, 2.0, b).astype(np.float32)
+    k = rng.integers(1, min(v, 300) + 1, b)
+    p = rng.uniform(0.05, 0.999, b).astype(np.float32)
+    m = rng.uniform(0.0, 0.3, b).astype(np.float32)
+    # (of a row of v tokens some 2 v MASS_OFF lie that near to a border: a row in a thousand here, but of the largest vocabulary most)
+    few = b if v > 200000 else 1
+    _check(G, x, u=u, pitch=pitch, most_open=few)
+    _check(G, x, t, u=u, pitch=pitch, most_open=few)
+    _check(G, x, t, top_k=k, u=u, pitch=pitch, most_open=1)
+    _check(G, x, t, top_p=p, u=u, pitch=pitch, most_open=few)
+    _check(G, x, t, min_p=m, u=u, pitch=pitch, most_open=few)
+    _check(G, x, t, k, p, m, u, pitch, most_open=1)
+    _check(G, x, None, k, p, None, u, pitch, most_open=1)
+
+
+@pytest.mark.gpu
+def test_parameters_that_switch_a_filter_off_or_stop_it(G):
+    rng = np.random.default_rng(5)
+    v = 3000
+    row = _logits(rng, 1, v)
+    u = rng.random(12).astype(np.float32)
+    x = np.repeat(row, 12, 0)
+    t = [0.0, -1.0, np.nan, 1e-45, 1e-3, 1.0, 1e30, np.inf, 1.0, 1.0, 1.0, 1.0]
+    k = [0, -4, 1, v, v + 5, 2 ** 31 - 1, -2 ** 31, 0, 1, 2, v - 1, 7]
+    p = [1.0, 2.0, np.nan, 0.5, 0.0, -1.0, 1.0, 1.0, 0.9, 1e-9, 0.999, np.inf]
+    m = [0.0, -1.0, np.nan, 0.0, 0.1, 0.0, 0.0, 0.0, 1.0, 5.0, 1e-30, 0.01]
+    _check(G, x, t, k, p, m, u, most_open=1)
+    _check(G, x, u=[0.0, 1.0, 1.5, -0.5, np.nan, np.inf, -np.inf, 0.5, np.nextafter(np.float32(1), np.float32(0)), 1e-30, 0.25, 0.75], most_open=1)
+
+
+@pytest.mark.gpu
+def test_ties_go_to_the_lowest_index(G):
+    rng = np.random.default_rng(6)
+    for v in (300, 9000, 40000):
+        x = rng.choice(np.array([-1.0, 0.5, 2.0, 2.5], dtype=np.float16), (16, v))
+        x[:, rng.integers(0, v, 5)] = 3.0
+        x[8:] = 1.25                                                  # all equal
+        # cuts inside a run of equal logits, wavefronts and slabs; halfway numbers are avoided: masses are multiples of one
+        k = rng.integers(1, v, 16)
+        u = (rng.integers(0, 2 ** 20, 16) + 0.37) / 2 ** 20
+        _check(G, x, top_k=k, u=u, most_open=16)
+        token, prob = _run(G, x[8:], top_k=k[8:], u=np.full(8, 1.0 - 2.0 ** -24))
+        assert np.array_equal(token, k[8:] - 1)
+        assert np.all(np.abs(prob * k[8:] - 1) < 1e-6)
+        token, _ = _run(G, x[8:], top_p=(k[8:] - 0.5) / v, u=np.full(8, 1.0 - 2.0 ** -24))
+        assert np.array_equal(token, k[8:] - 1)
+    assert list(_run(G, x[:8], temperature=np.zeros(8))[0]) == [int(np.argmax(r)) for r in x[:8]]
+
+
+@pytest.mark.gpu
+def test_masked_rows_and_values_that_are_not_finite(G):
+    v = 500
+    rng = np.random.default_rng(7)
+    x = _logits(rng, 12, v)
+    x[0] = -np.inf                                                    # nothing can be drawn
+    x[1] = np.nan
+    x[2, ::2] = np.nan
+    x[2, 1::2] = -np.inf
+    x[3] = -np.inf
+    x[3, 77] = -65504.0                                               # one can
+    x[4] = -65504.0                                                   # masked by the lowest number, as a whole
+    x[5, 1:] = -65504.0
+    x[6, 10] = x[6, 400] = np.inf
+    x[7, rng.integers(0, v, 200)] = np.nan
+    x[8, rng.integers(0, v, 450)] = -np.inf
+    x[9] = np.float16(-0.0)
+    x[9, 250:] = 0.0                                                  # the two zeros are equal
+    x[10] = np.float16(2.0 ** -24) * rng.integers(-3, 4, v)
+    x[11, 3] = 65504.0
+    u = rng.random(12).astype(np.float32)
+    t = np.full(12, 0.7, dtype=np.float32)
+    for kw in (dict(), dict(top_k=np.full(12, 40)), dict(top_p=np.full(12, 0.8)), dict(min_p=np.full(12, 0.02)),
+               dict(top_k=np.full(12, 300), top_p=np.full(12, 0.95), min_p=np.full(12, 0.001))):
+        token, prob = _check(G, x, t, u=u, most_open=1, **kw)
+        assert token[0] == token[1] == token[2] == -1 and not prob[:3].any()
+        assert token[3] == 77 and prob[3] == 1.0
+    _check(G, x, np.zeros(12), u=u)
+
+
+@pytest.mark.gpu
+def test_frequencies_follow_the_probabilities(G):
+    """Evenly spread numbers draw each token as often as its probability says, to one draw."""
+    v, n = 40, 4096
+    x = np.repeat(_logits(np.random.default_rng(8), 1, v), n, 0)
+    u = (np.arange(n) + 0.5) / n
+    token, _ = _run(G, x, u=u)
+    w = np.exp(x[0].astype(np.float64) - x[0].astype(np.float64).max())
+    assert np.all(np.abs(np.bincount(token, minlength=v) - n * w / w.sum()) <= 1 + 1e-3)
+    assert np.all(np.diff(token) >= 0)
+
+
+@pytest.mark.gpu
+def test_replayed_from_a_graph(G):
+    import torch
+    rng = np.random.default_rng(9)
+    b, v = 8, 32000
+    logits = G.to_dev(_logits(rng, b, v))
+    args = [G.to_dev(np.asarray(a)) for a in (np.full(b, 0.8, np.float32), np.full(b, 50, np.int32), np.full(b, 0.9, np.float32), np.full(b, 0.01, np.float32))]
+    u = G.to_dev(rng.random(b).astype(np.float32))
+    token, again = torch.empty(b, dtype=torch.int32, device=G.DEV), torch.empty(b, dtype=torch.int32, device=G.DEV)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        B.sqap_sample(logits, *args, u, token)                        # (no probabilities asked for)
+    for _ in range(4):
+        u.copy_(G.to_dev(rng.random(b).astype(np.float32)))
+        logits.copy_(G.to_dev(_logits(rng, b, v)))
+        graph.replay()
+        B.sqap_sample(logits, *args, u, again)
+        torch.cuda.synchronize()
+        assert torch.equal(token, again)
