@@ -668,10 +668,9 @@ sqap_status sqap_mx4_weight_pack(const uint8_t *Wq, const uint8_t *Ws, int32_t N
     w->magic = kMx4Magic;
     w->N = N;
     w->K = K;
-    w->n_groups = (N + 255) / 256 * 16;
-    w->ksteps = (K + 255) / 256 * 2;
-    w->kquads = (w->ksteps + 3) / 4;
-    const size_t data_bytes = (size_t)w->n_groups * w->ksteps * 1024, scale_bytes = (size_t)w->n_groups * w->kquads * 256;
+    w->n_groups = (N + 255) / 256 * 8;
+    w->stages = (K + 255) / 256;
+    const size_t data_bytes = (size_t)w->n_groups * w->stages * 4096, scale_bytes = (size_t)w->n_groups * w->stages * 256;
     w->bytes = data_bytes + scale_bytes;
     hipError_t e = hipGetDevice(&w->device);
     if (e == hipSuccess) e = hipMalloc(reinterpret_cast<void **>(&w->data), data_bytes);

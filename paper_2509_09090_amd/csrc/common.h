@@ -94,15 +94,15 @@ struct Group {
 };
 constexpr uint32_t kGroupMagic = 0x53514752u;  // "SQGR"
 
-// Packed weight in microscaled 4-bit floating point (mx4.hip): fragments of 16 channels x 128 codes, 1 KiB each, along K first; a word of
-// scale bytes per lane and four fragments.
+// Packed weight in microscaled 4-bit floating point (mx4.hip): fragments of 32 channels x 64 codes, 1 KiB each, along K first; a word of
+// scale bytes per lane and stage (four fragments along K, 256 codes).
 struct Mx4Weight {
     uint32_t magic;
     int32_t N, K;
-    int32_t n_groups;          // of 16 channels, a multiple of 16: a tile needs no guard in N
-    int32_t ksteps, kquads;    // fragments along K (an even number: codes of zero behind K), words of scales along K
-    uint8_t *data;             // n_groups * ksteps KiB
-    unsigned *scales;          // n_groups * kquads * 64 words
+    int32_t n_groups;          // of 32 channels, a multiple of 8: a tile needs no guard in N
+    int32_t stages;            // along K; codes of zero behind it
+    uint8_t *data;             // n_groups * stages * 4 KiB
+    unsigned *scales;          // n_groups * stages * 64 words
     size_t bytes;
     int device;
 };

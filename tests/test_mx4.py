@@ -143,12 +143,26 @@ def test_product(G, m, n, k):
     assert np.all(got == 7.0), "something beside the outputs was written"
 
 
+# enough outputs for the tiles, with one stage of K to many, odd and even numbers of them, whole and ragged
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n,k", [(100, 20011, 96), (33, 24500, 256), (130, 17000, 1312), (700, 5003, 352), (161, 9000, 768), (90, 26001, 2080),
+                                   (1100, 10001, 544), (2050, 5200, 32), (1290, 8200, 1280), (515, 16500, 1024)])
+def test_product_of_many_outputs(G, m, n, k):
+    test_product(G, m, n, k)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n", [(100, 20011), (700, 5003), (1100, 10001)])
+def test_tiles_keep_values_that_are_not_finite_in_their_row(G, m, n):
+    test_values_that_are_not_finite_stay_in_their_row(G, m, n)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("m", [3, 40, 100, 700])
-def test_values_that_are_not_finite_stay_in_their_row(G, m):
+def test_values_that_are_not_finite_stay_in_their_row(G, m, n=70):
     import torch
     rng = np.random.default_rng(m)
-    n, k = 70, 352
+    k = 352
     (xc, xs), (wc, ws) = _random_operand(rng, m, k), _random_operand(rng, n, k)
     xs[m // 2, k // 32 - 1] = 255
     xs[0, 0] = 255
