@@ -775,6 +775,7 @@ sqap_status sqap_cache8_append(const sqap_f16 *QKV, int64_t ld, const int32_t *s
     s = check_rows16(who, "QKV", QKV, ld, width + 2 * (int64_t)cache->kv_heads * cache->head_dim);
     if (s == SQAP_OK && Q_out) s = check_rows16(who, "Q_out", Q_out, ldq, width);
     if (s != SQAP_OK) return s;
+    const DeviceOfCall device;
     return launch_cache8_append(reinterpret_cast<const __half *>(QKV), ld, starts, pos, past, rows, max_new < rows ? max_new : rows, H, base, v,
                                 cache->head_dim, reinterpret_cast<__half *>(Q_out), ldq, as_stream(stream));
 }

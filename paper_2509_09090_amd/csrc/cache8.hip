@@ -87,6 +87,34 @@ __device__ __forceinline__ void rotate_pair(__half lo, __half hi, double cs, dou
     out_hi = __float2half_rn((float)(b * cs + a * sn));
 }
 
+// Sine and cosine of an angle of at most some 2^31, in binary64: the nearest multiple of pi / 2 is taken off in two parts of 53 bits (each
+// product exact inside its multiply-add), what is left is at most pi / 4, where the Taylor series to the 15th and 16th power are off by
+// less than half a unit of the last place of the larger one.  Without branches, so that a thread's pairs run side by side: a quarter of the
+// instructions of the library's, which also serves angles beyond (148 rows of 32 heads: 20.3 us with that, 6.9 so).
+__constant__ const double kSeries[15] = {-1.0 / 1307674368000.0, 1.0 / 20922789888000.0, 1.0 / 6227020800.0, -1.0 / 87178291200.0, -1.0 / 39916800.0,
+                                         1.0 / 479001600.0, 1.0 / 362880.0, -1.0 / 3628800.0, -1.0 / 5040.0, 1.0 / 40320.0, 1.0 / 120.0,
+                                         -1.0 / 720.0, -1.0 / 6.0, 1.0 / 24.0, -0.5};
+__device__ __forceinline__ void sincos_of(double a, double &sn, double &cs)
+{
+    const double n = rint(a * 0.63661977236758134308);
+    double r = fma(-n, 1.5707963267948965580, a);
+    r = fma(-n, 6.1232339957367658860e-17, r);
+    const double z = r * r;
+    double s = kSeries[0], c = kSeries[1];
+#pragma unroll
+    for (int i = 2; i < 14; i += 2) {
+        s = fma(s, z, kSeries[i]);
+        c = fma(c, z, kSeries[i + 1]);
+    }
+    c = fma(c, z, kSeries[14]);
+    s = fma(s * z, r, r);
+    c = fma(c, z, 1.0);
+    const int q = (int)n;
+    const double x = q & 1 ? c : s, y = q & 1 ? s : c;
+    sn = q & 2 ? -x : x;
+    cs = (q + 1) & 2 ? -y : y;
+}
+
 // Where a sequence's new rows lie: [row, row + n) of the fused rows, or nothing (n = 0) where the arrays do not describe one.
 struct Span {
     int row, n, past;
@@ -103,144 +131,176 @@ __device__ __forceinline__ Span span_of(const int32_t *starts, const int32_t *pa
 
 // ---------------------------------------------------------------- append
 
-// One workgroup per sequence, key head and block that the new rows touch (the first and the last of them together: the one reads the
-// tail that the other writes).  Keys: four threads per position, each with D / 8 pairs of columns (i, i + D / 2); the same threads turn
-// the query heads that share the key head.  Values: a column per thread and as many positions as the workgroup leaves it.
+// Where the code of column x and place `at` (of 64) lies in the values' half of a block; in LDS the four 16-byte pieces of a column are moved
+// round by its column's eights, so that the threads of a row, 8 columns apart, write to different banks.
+__device__ __forceinline__ int value_at(int s) { return ((s >> 2) & 3) << 4 | (s >> 5) << 3 | ((s >> 4) & 1) << 2 | (s & 3); }
+__device__ __forceinline__ int value_byte(int x, int at) { return x * 64 + ((at >> 4) + (x >> 3) & 3) * 16 + (at & 15); }
+__device__ __forceinline__ int value_piece(int u) { const int x = (u >> 6) * 16 + (u & 15); return x * 64 + (((u >> 4) & 3) + (x >> 3) & 3) * 16; }
+
+constexpr int kAppendGroups = 512, kAppendSplit = 256;
+// One workgroup per sequence, `share` key heads and block that the new rows touch (the first and the last of them together: the one reads
+// the tail that the other writes).  The block's angles are evaluated once, into LDS.  Then, head by head: keys, D / 16 threads per position with 8
+// pairs of columns (i, i + D / 2) each; the same threads turn the query heads that share the key head, and take the value row, whose codes
+// pass through LDS to their order.
 template <int D>
-__global__ __launch_bounds__(256) void cache8_append_kernel(const __half *__restrict__ QKV, int64_t ld, const int32_t *__restrict__ starts,
-                                                            const int32_t *__restrict__ pos, const int32_t *__restrict__ past, int rows, int max_new, int H,
-                                                            const Cache8View cache, __half *__restrict__ Q_out, int64_t ldq, const RopeFreq freq)
+__global__ __launch_bounds__(4 * D, 2) void cache8_append_kernel(const __half *__restrict__ QKV, int64_t ld, const int32_t *__restrict__ starts,
+                                                                 const int32_t *__restrict__ pos, const int32_t *__restrict__ past, int rows, int max_new,
+                                                                 int H, int share, int split, const Cache8View cache, __half *__restrict__ Q_out, int64_t ldq,
+                                                                 const RopeFreq freq)
 {
-    constexpr int P = D / 8, HALF = D / 2, PARTS = 256 / D, TOKENS = kBlock / PARTS;
-    __shared__ unsigned tops[2][2][4];
-    const int b = blockIdx.z, h = blockIdx.y, t = threadIdx.x, wave = t >> 6;
+    constexpr int P = 8, HALF = D / 2, SUBS = HALF / P, T = 4 * D, WAVES = T / 64;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    double2 *angles = reinterpret_cast<double2 *>(lds);               // [64][HALF], pair i of a position at i ^ (i / 8) % 8: no two lanes on one bank
+    int8_t *turned = reinterpret_cast<int8_t *>(angles + kBlock * HALF);          // the values' codes, 64 D
+    unsigned *tops = reinterpret_cast<unsigned *>(turned + kBlock * D);           // [2][keys, values][WAVES]
+    const int b = blockIdx.z, t = threadIdx.x, wave = t >> 6;
     const Span sp = span_of(starts, past, b, rows, max_new, cache.blocks * kBlock);
     if (!sp.fits) return;
     const int end = sp.past + sp.n, first = sp.past / kBlock, last = (end - 1) / kBlock, G = H / cache.kv_heads;
-    const int64_t head = (int64_t)b * cache.kv_heads + h;
-    __half *tail_k = cache.tail + head * 2 * kBlock * D, *tail_v = tail_k + kBlock * D;
+    // what this workgroup does of its heads: 1 keys, 2 values, 4 queries
+    const int groups = (cache.kv_heads + share - 1) / share, group = blockIdx.y % groups, does = split ? 1 << (blockIdx.y / groups) : 7;
+    const int head0 = group * share, heads = min(share, cache.kv_heads - head0);
     int block = first + (int)blockIdx.x;
-    if (blockIdx.x > 0 && block >= last) return;
+    const bool joined = sp.past % kBlock != 0 && last > first;        // the tail is read by the first block and written by the last
+    if (block > last || (joined && blockIdx.x > 0 && block == last)) return;
+    const bool keys = does & 1, values = does & 2, queries = Q_out && (does & 4);
+    if (!keys && !values && !queries) return;
+    struct Row {
+        v4i lo, hi;                                                   // eight halves each
+    };
+    const int slot = t / SUBS, sub = t % SUBS;
+    auto load_row = [&](const __half *from, Row &x) {                 // columns 8 sub .. and HALF + 8 sub ..
+        x.lo = *reinterpret_cast<const v4i *>(from + sub * P);
+        x.hi = *reinterpret_cast<const v4i *>(from + HALF + sub * P);
+    };
+    auto store_row = [&](__half *to, const Row &x) {
+        *reinterpret_cast<v4i *>(to + sub * P) = x.lo;
+        *reinterpret_cast<v4i *>(to + HALF + sub * P) = x.hi;
+    };
+    auto half_at = [](const v4i &x, int i) { return __ushort_as_half((unsigned short)((unsigned)x[i >> 1] >> (16 * (i & 1)))); };
+    auto turn_row = [&](Row &x) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            unsigned lo = 0, hi = 0;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const double2 a = angles[slot * HALF + ((sub * P + 2 * w + e) ^ sub)];
+                __half y, z;
+                rotate_pair(half_at(x.lo, 2 * w + e), half_at(x.hi, 2 * w + e), a.x, a.y, y, z);
+                lo |= (unsigned)__half_as_ushort(y) << (16 * e);
+                hi |= (unsigned)__half_as_ushort(z) << (16 * e);
+            }
+            x.lo[w] = (int)lo;
+            x.hi[w] = (int)hi;
+            __builtin_amdgcn_sched_barrier(0);                        // two pairs side by side: eight would need another wavefront's registers
+        }
+    };
     for (int turn = 0;; ++turn) {
         const bool full = (block + 1) * kBlock <= end;
-        // ---- keys
-        const int slot = t >> 2, sub = t & 3, p = block * kBlock + slot;
+        const int p = block * kBlock + slot;
         const bool is_new = p >= sp.past && p < end;
-        const __half *row = QKV + (int64_t)(sp.row + (is_new ? p - sp.past : 0)) * ld;
-        __half lo[P], hi[P];
-        unsigned top_k = 0;
-        if (is_new) {
-            double cs[P], sn[P];
-            const int at = pos[sp.row + p - sp.past];
+        const int at = sp.row + (is_new ? p - sp.past : 0);
+        const __half *row = QKV + (int64_t)at * ld;
+        if (turn > 0) __syncthreads();                                // (the angles of the first block have been read)
+        auto fetch_rows = [&](int h, Row &key, Row &value, Row &query) {
+            const int64_t tail = ((int64_t)b * cache.kv_heads + h) * 2 * kBlock * D + slot * D;
+            if (keys) load_row(is_new ? row + (int64_t)(H + h) * D : cache.tail + tail, key);        // (an absent row is read and dropped)
+            if (values) load_row(is_new ? row + (int64_t)(H + cache.kv_heads + h) * D : cache.tail + tail + kBlock * D, value);
+            if (queries && is_new) load_row(row + (int64_t)h * G * D, query);
+        };
+        Row key = {v4i{0, 0, 0, 0}, v4i{0, 0, 0, 0}}, value = key, query = key;
+        fetch_rows(head0, key, value, query);                         // (before the angles are worked out)
+        if (keys || queries) {
+            constexpr int EACH = kBlock * HALF / T, STEP = T / HALF;  // positions of a thread, STEP apart, all with one frequency
+            const int i = t % HALF, s0 = t / HALF;
+            const double f = freq.f[i];
+            int at_pos[EACH];
 #pragma unroll
-            for (int i = 0; i < P; ++i) sincos((double)at * freq.f[sub * P + i], &sn[i], &cs[i]);
-            auto turned = [&](const __half *from) {
-                union Piece { v4i v[P / 8]; __half h[P]; } a, c;
-#pragma unroll
-                for (int i = 0; i < P / 8; ++i) {
-                    a.v[i] = *reinterpret_cast<const v4i *>(from + sub * P + 8 * i);
-                    c.v[i] = *reinterpret_cast<const v4i *>(from + HALF + sub * P + 8 * i);
-                }
-#pragma unroll
-                for (int i = 0; i < P; ++i) rotate_pair(a.h[i], c.h[i], cs[i], sn[i], lo[i], hi[i]);
-            };
-            if (Q_out) {
-                for (int j = 0; j < G; ++j) {
-                    turned(row + (int64_t)(h * G + j) * D);
-                    __half *to = Q_out + (int64_t)(sp.row + p - sp.past) * ldq + (int64_t)(h * G + j) * D + sub * P;
-                    union Piece { v4i v[P / 8]; __half h[P]; } a, c;
-#pragma unroll
-                    for (int i = 0; i < P; ++i) a.h[i] = lo[i], c.h[i] = hi[i];
-#pragma unroll
-                    for (int i = 0; i < P / 8; ++i) {
-                        *reinterpret_cast<v4i *>(to + 8 * i) = a.v[i];
-                        *reinterpret_cast<v4i *>(to + HALF + 8 * i) = c.v[i];
+            for (int k = 0; k < EACH; ++k) {
+                const int q = block * kBlock + s0 + k * STEP - sp.past;
+                at_pos[k] = pos[sp.row + min(max(q, 0), sp.n - 1)];
+            }
+#pragma unroll 2
+            for (int k = 0; k < EACH; ++k) {
+                const int s = s0 + k * STEP;
+                double2 a;
+                sincos_of((double)at_pos[k] * f, a.y, a.x);
+                angles[s * HALF + (i ^ ((i >> 3) & 7))] = a;
+            }
+        }
+        for (int hh = 0; hh < heads; ++hh) {
+            const int h = head0 + hh;
+            const int64_t head = (int64_t)b * cache.kv_heads + h;
+            __half *tail_k = cache.tail + head * 2 * kBlock * D, *tail_v = tail_k + kBlock * D;
+            if (hh > 0) fetch_rows(h, key, value, query);
+            const bool turns = queries && is_new;
+            if (hh == 0) __syncthreads();                             // the angles are there
+            if (is_new) {
+                if (keys) turn_row(key);
+                if (turns) {
+                    __half *to = Q_out + (int64_t)at * ldq + (int64_t)h * G * D;
+                    for (int j = 0; j < G; ++j) {
+                        Row next = query;
+                        if (j + 1 < G) load_row(row + (int64_t)(h * G + j + 1) * D, next);
+                        turn_row(query);
+                        store_row(to + (int64_t)j * D, query);
+                        query = next;
                     }
                 }
             }
-            turned(row + (int64_t)(H + h) * D);
-        } else {
+            if (!keys && !values) continue;
+            unsigned top_k = 0, top_v = 0;
+            if (full) {
 #pragma unroll
-            for (int i = 0; i < P; ++i) {
-                lo[i] = p < sp.past ? tail_k[slot * D + sub * P + i] : __half(0.f);
-                hi[i] = p < sp.past ? tail_k[slot * D + HALF + sub * P + i] : __half(0.f);
-            }
-        }
+                for (int i = 0; i < P; ++i) top_k = max(top_k, max(magnitude(half_at(key.lo, i)), magnitude(half_at(key.hi, i))));
 #pragma unroll
-        for (int i = 0; i < P; ++i) top_k = max(top_k, max(magnitude(lo[i]), magnitude(hi[i])));
-        // ---- values: this thread's column, positions 64 / PARTS of them
-        const int col = t % D, part = t / D;
-        __half v[TOKENS];
-        unsigned top_v = 0;
-        const __half *vbase = QKV + (int64_t)(H + cache.kv_heads + h) * D + col;
-#pragma unroll
-        for (int i = 0; i < TOKENS; ++i) {
-            const int s = part * TOKENS + i, q = block * kBlock + s;
-            v[i] = q < sp.past ? tail_v[s * D + col] : q < end ? vbase[(int64_t)(sp.row + q - sp.past) * ld] : __half(0.f);
-            top_v = max(top_v, magnitude(v[i]));
-        }
-        // ---- what becomes of them
-        if (full) {
-            top_k = wavefront_umax(top_k);
-            top_v = wavefront_umax(top_v);
-            if ((t & 63) == 0) {
-                tops[turn][0][wave] = top_k;
-                tops[turn][1][wave] = top_v;
-            }
-        }
-        __syncthreads();                                              // (and nobody reads the tail any more)
-        if (full) {
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                top_k = max(top_k, tops[turn][0][w]);
-                top_v = max(top_v, tops[turn][1][w]);
-            }
-            const bool ok_k = finite_bits(top_k), ok_v = finite_bits(top_v);
-            const Steps sk = steps_of(__half2float(__ushort_as_half((unsigned short)top_k))), sv = steps_of(__half2float(__ushort_as_half((unsigned short)top_v)));
-            int8_t *kc = block_codes<D>(cache, head, block, 0), *vc = block_codes<D>(cache, head, block, 1);
-            // columns sub P .. and HALF + sub P ..: whole or half pieces of 16
-            auto store = [&](int column, const __half (&x)[P]) {
-                int w[P / 4];
-#pragma unroll
-                for (int i = 0; i < P / 4; ++i) {
-                    w[i] = 0;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) w[i] |= (ok_k ? code_of(__half2float(x[4 * i + e]), sk) & 255 : 0) << (8 * e);
+                for (int i = 0; i < P; ++i) top_v = max(top_v, max(magnitude(half_at(value.lo, i)), magnitude(half_at(value.hi, i))));
+                top_k = wavefront_umax(top_k);
+                top_v = wavefront_umax(top_v);
+                if ((t & 63) == 0) {
+                    tops[(hh & 1) * 2 * WAVES + wave] = top_k;
+                    tops[(hh & 1) * 2 * WAVES + WAVES + wave] = top_v;
                 }
-                int8_t *to = kc + ((((slot >> 4) * (D / 64) + (column >> 6)) * 64 + ((column >> 4) & 3) * 16 + (slot & 15)) * 16 + (column & 15));
-                if constexpr (P == 16) *reinterpret_cast<v4i *>(to) = v4i{w[0], w[1], w[2], w[3]};
-                else *reinterpret_cast<v2u *>(to) = v2u{(unsigned)w[0], (unsigned)w[1]};
-            };
-            store(sub * P, lo);
-            store(HALF + sub * P, hi);
-#pragma unroll
-            for (int i = 0; i < TOKENS; i += 4) {
-                const int s = part * TOKENS + i;                      // four positions of one lane group
-                int w = 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) w |= (ok_v ? code_of(__half2float(v[i + e]), sv) & 255 : 0) << (8 * e);
-                *reinterpret_cast<int *>(vc + ((col >> 4) * 64 + ((s >> 2) & 3) * 16 + (col & 15)) * 16 + (s >> 5) * 8 + ((s >> 4) & 1) * 4) = w;
             }
-            if (t == 0) {
-                float *to = cache.scales + (head * cache.blocks + block) * 2;
-                to[0] = scale_of(top_k);
-                to[1] = scale_of(top_v);
-            }
-        } else {
-            if (is_new) {
+            __syncthreads();                                          // (and nobody reads this head's tail any more)
+            if (full) {
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) {
+                    top_k = max(top_k, tops[(hh & 1) * 2 * WAVES + w]);
+                    top_v = max(top_v, tops[(hh & 1) * 2 * WAVES + WAVES + w]);
+                }
+                const bool ok_k = finite_bits(top_k), ok_v = finite_bits(top_v);
+                const Steps sk = steps_of(__half2float(__ushort_as_half((unsigned short)top_k))), sv = steps_of(__half2float(__ushort_as_half((unsigned short)top_v)));
+                int8_t *kc = block_codes<D>(cache, head, block, 0), *vc = block_codes<D>(cache, head, block, 1);
+                auto store = [&](int column, const v4i &x) {          // half a piece of 16 columns
+                    unsigned w[2] = {0u, 0u};
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w[i >> 2] |= (unsigned)(ok_k ? code_of(__half2float(half_at(x, i)), sk) & 255 : 0) << (8 * (i & 3));
+                    int8_t *to = kc + ((((slot >> 4) * (D / 64) + (column >> 6)) * 64 + ((column >> 4) & 3) * 16 + (slot & 15)) * 16 + (column & 15));
+                    *reinterpret_cast<v2u *>(to) = v2u{w[0], w[1]};
+                };
+                if (keys) {
+                    store(sub * P, key.lo);
+                    store(HALF + sub * P, key.hi);
+                    if (t == 0) cache.scales[(head * cache.blocks + block) * 2] = scale_of(top_k);
+                }
+                if (!values) continue;
+                // values: a byte for each of this thread's columns to its place in the block, then whole pieces out
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
-                    tail_k[slot * D + sub * P + i] = lo[i];
-                    tail_k[slot * D + HALF + sub * P + i] = hi[i];
+                    const int x = sub * P + i, at_slot = value_at(slot);
+                    turned[value_byte(x, at_slot)] = (int8_t)(ok_v ? code_of(__half2float(half_at(value.lo, i)), sv) : 0);
+                    turned[value_byte(HALF + x, at_slot)] = (int8_t)(ok_v ? code_of(__half2float(half_at(value.hi, i)), sv) : 0);
                 }
-            }
-#pragma unroll
-            for (int i = 0; i < TOKENS; ++i) {
-                const int s = part * TOKENS + i, q = block * kBlock + s;
-                if (q >= sp.past && q < end) tail_v[s * D + col] = v[i];
+                __syncthreads();
+                if (t < kBlock * D / 16) reinterpret_cast<v4i *>(vc)[t] = *reinterpret_cast<const v4i *>(turned + value_piece(t));
+                if (t == 0) cache.scales[(head * cache.blocks + block) * 2 + 1] = scale_of(top_v);
+            } else if (is_new) {
+                if (keys) store_row(tail_k + slot * D, key);
+                if (values) store_row(tail_v + slot * D, value);
             }
         }
-        if (blockIdx.x > 0 || block == last) return;
+        if (!joined || blockIdx.x > 0 || block == last) return;
         block = last;
     }
 }
@@ -293,7 +353,7 @@ struct Unit {
     __device__ __forceinline__ float enter(float scale, float &change)
     {
         change = 1.f;
-        if (!(scale > 0.f)) return scale;                             // no values but zeros, or NaN: the sums stay as they are
+        if (!(scale > 0.f)) return 1.f;                               // no values but zeros, or NaN: the sums stay as they are
         if (scale > unit || scale < unit * 0.00390625f) {
             change = unit / scale;
             unit = scale;
@@ -302,23 +362,42 @@ struct Unit {
     }
 };
 
-// Rows are (query, head) pairs of the heads that share a key head, query first, 128 to a workgroup and 32 to a wavefront, so that a
-// block of keys and values is taken from memory and made halves once for all of them.  Everything is transposed (scores: positions x
-// rows), as in attention.hip: probabilities are the second product's operand where they were computed.
-constexpr int kRowsOfTile = 128;
+// The maximum is the rounded product of a score and the keys' scale, the scores that are taken from it enter by a multiply-add, unrounded:
+// from here on (in units of ln 2) the difference could be more than a few, and the scores are rounded as well.
+constexpr float kLargeScore = 1048576.f;
+// The maximum lags behind by up to this (a half holds probabilities of 2^6 as well): with 32 rows to a wavefront some row has a new one in
+// most blocks, and the sums are 64 registers.
+constexpr float kRaiseBy = 6.f;
 
-template <int D>
-__global__ __launch_bounds__(256) void cache8_attention_kernel(const __half *__restrict__ Q, int64_t ldq, const int32_t *__restrict__ starts,
-                                                               const int32_t *__restrict__ past, int rows, int max_new, int H, const Cache8View cache,
-                                                               __half *__restrict__ O, int64_t ldo)
+// Rows are (query, head) pairs of the heads that share a key head, query first, 32 to a wavefront and WAVES wavefronts to a workgroup, so
+// that a block of keys and values is taken from memory and made halves once for all of them.  Everything is transposed (scores:
+// positions x rows), as in attention.hip: probabilities are the second product's operand where they were computed.
+// A block's p = 2^(s - m) times its factor is one exponential, of s sk + (log2 factor - m); the sum of the probabilities is put right by the
+// factor once per block.
+template <int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const __half *__restrict__ Q, int64_t ldq, const int32_t *__restrict__ starts,
+                                                                         const int32_t *__restrict__ past, int rows, int max_new, int H,
+                                                                         const Cache8View cache, __half *__restrict__ O, int64_t ldo, int tiles)
 {
-    constexpr int NP = D / 16, CT = D / 32, BUF = 2 * kBlock * D * 2, PIECES = kBlock * D / 16 / 256;
+    constexpr int T = 64 * WAVES, TILE = 32 * WAVES, NP = D / 16, CT = D / 32, BUF = 2 * kBlock * D * 2, COUNT = kBlock * D / 16;
+    constexpr int PIECES = (COUNT + T - 1) / T;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];     // two buffers: keys [2][NP] KiB, values [CT][4] KiB
     __shared__ int not_finite;
-    const int b = blockIdx.z, kh = blockIdx.y, t = threadIdx.x, l = t & 63, wave = t >> 6, c = l & 31, h = l >> 5;
+    // a key head's tiles behind one L2 (workgroup b runs on XCD b % 8) where the heads fill all of them; the longest first
+    const int pairs = cache.kv_heads * cache.batch, id = blockIdx.x;
+    int pair, number;
+    if (pairs % 8 == 0) {
+        pair = (id & 7) + 8 * ((id >> 3) % (pairs / 8));
+        number = (id >> 3) / (pairs / 8);
+    } else {
+        pair = id % pairs;
+        number = id / pairs;
+    }
+    const int b = pair / cache.kv_heads, kh = pair % cache.kv_heads;
+    const int t = threadIdx.x, l = t & 63, wave = t >> 6, c = l & 31, h = l >> 5;
     const Span sp = span_of(starts, past, b, rows, max_new, cache.blocks * kBlock);
     const int G = H / cache.kv_heads;
-    const int64_t n_rows = (int64_t)sp.n * G, tile = (int64_t)(gridDim.x - 1 - blockIdx.x) * kRowsOfTile;     // (the longest first)
+    const int64_t n_rows = (int64_t)sp.n * G, tile = (int64_t)(tiles - 1 - number) * TILE;
     if (tile >= n_rows) return;
     const int64_t mine = tile + wave * 32 + c;
     const int64_t mine_in = min(mine, n_rows - 1);
@@ -330,7 +409,7 @@ __global__ __launch_bounds__(256) void cache8_attention_kernel(const __half *__r
     }
     if (t == 0) not_finite = 0;
     const int end = sp.past + sp.n, sees = sp.past + query;           // last position that this lane's row sees
-    const int tile_last = sp.past + (int)((min(tile + kRowsOfTile, n_rows) - 1) / G), n_blocks = tile_last / kBlock + 1;
+    const int tile_last = sp.past + (int)((min(tile + TILE, n_rows) - 1) / G), n_blocks = tile_last / kBlock + 1;
     const int64_t kv_head = (int64_t)b * cache.kv_heads + kh;
     const __half *tail_k = cache.tail + kv_head * 2 * kBlock * D, *tail_v = tail_k + kBlock * D;
     const float *scales = cache.scales + kv_head * cache.blocks * 2;
@@ -347,8 +426,10 @@ __global__ __launch_bounds__(256) void cache8_attention_kernel(const __half *__r
         const v4i *k = reinterpret_cast<const v4i *>(block_codes<D>(cache, kv_head, j, 0)), *v = reinterpret_cast<const v4i *>(block_codes<D>(cache, kv_head, j, 1));
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            kraw[i] = k[t + 256 * i];
-            vraw[i] = v[t + 256 * i];
+            const int u = t + T * i;
+            if (COUNT % T != 0 && u >= COUNT) break;
+            kraw[i] = k[u];
+            vraw[i] = v[u];
         }
     };
     auto keep = [&](int j) {
@@ -357,10 +438,11 @@ __global__ __launch_bounds__(256) void cache8_attention_kernel(const __half *__r
         if (j != tail_block) {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
-                const int u = t + 256 * i, r = u & 15, g = (u >> 4) & 3, x = u >> 6;
+                const int u = t + T * i, r = u & 15, g = (u >> 4) & 3, x = u >> 6;
+                if (COUNT % T != 0 && u >= COUNT) break;
                 // keys: piece x = (T, c): position 16 T + r, columns 64 c + 16 g ..
-                const int T = x / (D / 64), m = (x % (D / 64)) * 4 + g, row = 16 * (T & 1) + r;
-                uint8_t *to = kt + (((T >> 1) * NP + m) * 64 + row) * 16;
+                const int tk = x / (D / 64), m = (x % (D / 64)) * 4 + g, row = 16 * (tk & 1) + r;
+                uint8_t *to = kt + (((tk >> 1) * NP + m) * 64 + row) * 16;
                 *reinterpret_cast<v8h *>(to) = halves_of(kraw[i][0], kraw[i][1]);
                 *reinterpret_cast<v8h *>(to + 512) = halves_of(kraw[i][2], kraw[i][3]);
                 // values: piece x: column 16 x + r, four positions per word
@@ -372,7 +454,7 @@ __global__ __launch_bounds__(256) void cache8_attention_kernel(const __half *__r
             return;
         }
         bool odd = false;
-        for (int u = t; u < kBlock * D / 8; u += 256) {
+        for (int u = t; u < kBlock * D / 8; u += T) {
             const int s = u / (D / 8), x = (u % (D / 8)) * 8;
             v8h k = {}, v = {};
             if (s < tail_rows) {
@@ -407,12 +489,16 @@ __global__ __launch_bounds__(256) void cache8_attention_kernel(const __half *__r
     __syncthreads();
     fetch(0);
     keep(0);
+    float2 sc = {0.f, 0.f};
+    if (tail_block != 0) sc = *reinterpret_cast<const float2 *>(scales);
     for (int j = 0; j < n_blocks; ++j) {
         fetch(j + 1);
-        __syncthreads();
+        // (keys that are all zeros: the scores are, times anything but zero, which would make NaN of a masked one)
+        const float sk = j == tail_block || sc.x == 0.f ? per_d : sc.x * per_d, sv = j == tail_block ? 1.f : sc.y;
+        if (j + 1 < n_blocks && j + 1 != tail_block) sc = *reinterpret_cast<const float2 *>(scales + 2 * (j + 1));
+        lds_barrier();
         if (j * kBlock <= wave_last) {
-            const uint8_t *kt = lds + (j & 1) * BUF, *vt = kt + kBlock * D * 2;
-            const float sk = j == tail_block ? per_d : scales[2 * j] * per_d, sv = j == tail_block ? 1.f : scales[2 * j + 1];
+            const uint8_t *kt = lds + (j & 1) * BUF + l * 16, *vt = kt + kBlock * D * 2;
             v16f s[2];
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt) {
@@ -420,22 +506,38 @@ __global__ __launch_bounds__(256) void cache8_attention_kernel(const __half *__r
                 for (int i = 0; i < 16; ++i) s[tt][i] = 0.f;
 #pragma unroll
                 for (int m = 0; m < NP; ++m)
-                    s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const v8h *>(kt + ((tt * NP + m) * 64 + l) * 16), qf[m], s[tt], 0, 0, 0);
+                    s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const v8h *>(kt + (tt * NP + m) * 1024), qf[m], s[tt], 0, 0, 0);
+            }
+            if ((j + 1) * kBlock - 1 > wave_first) {                  // some row does not see some position
+                const int last = sees - j * kBlock - 4 * h;
+#pragma unroll
+                for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (32 * tt + 8 * (i >> 2) + (i & 3) > last) s[tt][i] = -INFINITY;
             }
             float top = -INFINITY;
-            const bool whole = (j + 1) * kBlock - 1 <= wave_first;    // every row sees every position
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s[tt][i] *= sk;
-                    if (!whole && j * kBlock + 32 * tt + 8 * (i >> 2) + 4 * h + (i & 3) > sees) s[tt][i] = -INFINITY;
-                    top = fmaxf(top, s[tt][i]);
-                }
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[tt][i]);
             top = fmaxf(top, __shfl_xor(top, 32));
+            if (top > -INFINITY) top *= sk;                           // (nothing seen: it stays, whatever the scale)
+            float by = sk;
+            if (__any(fabsf(top) > kLargeScore && top > -INFINITY)) {
+#pragma unroll
+                for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float w = s[tt][i] * sk;
+                        asm volatile("" : "+v"(w));                   // (rounded)
+                        s[tt][i] = s[tt][i] == -INFINITY ? -INFINITY : w;
+                    }
+                by = 1.f;
+            }
             float change;
             const float factor = unit.enter(sv, change);
-            if (top > mrun) {                                         // (a row that sees nothing of the block keeps its maximum)
+            if (top > mrun + kRaiseBy) {                              // (a row that sees nothing of the block keeps its maximum)
                 const float raise = exp2f(mrun - top);
                 change *= raise;
                 lrun *= raise;
@@ -447,20 +549,29 @@ __global__ __launch_bounds__(256) void cache8_attention_kernel(const __half *__r
 #pragma unroll
                     for (int i = 0; i < 16; ++i) ot[ct][i] *= change;
             }
+            const float from = __log2f(factor) - mrun;
+            float sum = 0.f;
             v8h p[4];
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float e = exp2f(s[tt][i] - mrun);
-                    lrun += e;
-                    p[2 * tt + (i >> 3)][i & 7] = (_Float16)(e == 0.f ? 0.f : e * factor);
+                    const float e = __builtin_amdgcn_exp2f(fmaf(s[tt][i], by, from));
+                    sum += e;
+                    p[2 * tt + (i >> 3)][i & 7] = (_Float16)e;
                 }
+            lrun += sum / factor;
+            if (!(sv >= 0.f)) {                                       // values that are NaN as a whole: for the rows that see any of them
+#pragma unroll
+                for (int n = 0; n < 4; ++n)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) p[n][i] = s[n >> 1][(n & 1) * 8 + i] == -INFINITY ? (_Float16)0.f : (_Float16)NAN;
+            }
 #pragma unroll
             for (int n = 0; n < 4; ++n)
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct)
-                    ot[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const v8h *>(vt + ((ct * 4 + n) * 64 + l) * 16), p[n], ot[ct], 0, 0, 0);
+                    ot[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const v8h *>(vt + (ct * 4 + n) * 1024), p[n], ot[ct], 0, 0, 0);
         }
         keep(j + 1);
     }
@@ -476,18 +587,22 @@ __global__ __launch_bounds__(256) void cache8_attention_kernel(const __half *__r
             const int col = 32 * ct + 8 * a + 4 * h;
             union { __half h[4]; v2u v; } u;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float o = ot[ct][4 * a + i] * norm;
-                if (odd) {                                            // infinities and NaN among the tail's values that this row sees
-                    for (int s = 0; s <= sees - tail_block * kBlock; ++s) {
-                        const float x = __half2float(tail_v[s * D + col + i]);
-                        if (!(fabsf(x) <= 65504.f)) o += x;
-                    }
-                }
-                u.h[i] = __float2half_rn(o);
-            }
+            for (int i = 0; i < 4; ++i) u.h[i] = __float2half_rn(ot[ct][4 * a + i] * norm);
             *reinterpret_cast<v2u *>(to + col) = u.v;
         }
+    if (odd) {                                                        // infinities and NaN among the tail's values that this row sees
+#pragma unroll 1
+        for (int x = 0; x < D / 2; ++x) {
+            const int col = (x >> 2) * 8 + 4 * h + (x & 3);
+            float o = __half2float(to[col]);
+#pragma unroll 1
+            for (int s = 0; s <= sees - tail_block * kBlock; ++s) {
+                const float v = __half2float(tail_v[s * D + col]);
+                if (!(fabsf(v) <= 65504.f)) o += v;
+            }
+            to[col] = __float2half_rn(o);
+        }
+    }
 }
 
 // ---------------------------------------------------------------- attention of one row per sequence
@@ -713,7 +828,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void cache8_decode_kernel(const 
         for (int T4 = 0; T4 < 4; ++T4)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float e = exp2f(s[T4][i] - mrun), w = e == 0.f ? 0.f : e * factor;
+                const float e = exp2f(s[T4][i] - mrun), w = sv >= 0.f ? e * factor : s[T4][i] == -INFINITY ? 0.f : NAN;
                 lrun += e;
                 const _Float16 w0 = (_Float16)w;
                 p[T4 >> 1][(T4 & 1) * 4 + i] = w0;
@@ -802,16 +917,33 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void cache8_decode_kernel(const 
 
 // ---------------------------------------------------------------- launches
 
+template <int D>
+static sqap_status launch_append_d(const __half *QKV, int64_t ld, const int32_t *starts, const int32_t *pos, const int32_t *past, int rows, int max_new,
+                                   int H, double base, const Cache8View &cache, __half *Q_out, int64_t ldq, hipStream_t st)
+{
+    constexpr int LDS = kBlock * D / 2 * 16 + kBlock * D + 4 * 4 * D / 64 * 4;
+    static std::atomic<bool> ready[kMaxDeviceSlots];
+    if (LDS > 65536 && !ready[device_slot()].load(std::memory_order_relaxed)) {
+        SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(cache8_append_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+        ready[device_slot()].store(true, std::memory_order_relaxed);
+    }
+    const int columns = (max_new + kBlock - 2) / kBlock + 1;          // blocks that the longest sequence touches, at most
+    // heads that share a workgroup's angles: as many as leave the device its workgroups.  Where there is less than one per compute unit, keys,
+    // values and queries have workgroups of their own: each is a chain of its own (148 rows of 32 heads 10.5 us together, 7.9 apart).
+    const int64_t items = (int64_t)columns * cache.batch * cache.kv_heads;
+    const int share = (int)std::max<int64_t>(1, std::min<int64_t>(cache.kv_heads, items / kAppendGroups));
+    const int split = items <= kAppendSplit ? 1 : 0;
+    hipLaunchKernelGGL(cache8_append_kernel<D>, dim3(columns, (cache.kv_heads + share - 1) / share * (split ? 3 : 1), cache.batch), dim3(4 * D), LDS, st, QKV, ld,
+                       starts, pos, past, rows, max_new, H, share, split, cache, Q_out, ldq, rope_frequencies(D, base));
+    SQAP_HIP_CHECK(hipGetLastError());
+    return SQAP_OK;
+}
+
 sqap_status launch_cache8_append(const __half *QKV, int64_t ld, const int32_t *starts, const int32_t *pos, const int32_t *past, int rows, int max_new,
                                  int H, double base, const Cache8View &cache, int d, __half *Q_out, int64_t ldq, hipStream_t st)
 {
-    const int touched = (max_new + kBlock - 2) / kBlock + 1;          // blocks of the longest sequence, at most
-    const dim3 grid(std::max(1, touched - 1), cache.kv_heads, cache.batch);
-    const RopeFreq freq = rope_frequencies(d, base);
-    if (d == 64) hipLaunchKernelGGL(cache8_append_kernel<64>, grid, dim3(256), 0, st, QKV, ld, starts, pos, past, rows, max_new, H, cache, Q_out, ldq, freq);
-    else hipLaunchKernelGGL(cache8_append_kernel<128>, grid, dim3(256), 0, st, QKV, ld, starts, pos, past, rows, max_new, H, cache, Q_out, ldq, freq);
-    SQAP_HIP_CHECK(hipGetLastError());
-    return SQAP_OK;
+    return d == 64 ? launch_append_d<64>(QKV, ld, starts, pos, past, rows, max_new, H, base, cache, Q_out, ldq, st)
+                   : launch_append_d<128>(QKV, ld, starts, pos, past, rows, max_new, H, base, cache, Q_out, ldq, st);
 }
 
 sqap_status launch_cache8_read(const Cache8View &cache, int d, const int32_t *lengths, int first, int count, __half *out, int64_t ld, hipStream_t st)
@@ -823,21 +955,29 @@ sqap_status launch_cache8_read(const Cache8View &cache, int d, const int32_t *le
     return SQAP_OK;
 }
 
+template <int D, int WAVES>
+static sqap_status launch_attention_of(const __half *Q, int64_t ldq, const int32_t *starts, const int32_t *past, int rows, int max_new, int H,
+                                       const Cache8View &cache, __half *O, int64_t ldo, hipStream_t st)
+{
+    constexpr int LDS = 2 * 2 * kBlock * D * 2;
+    const int64_t tiles = ((int64_t)max_new * (H / cache.kv_heads) + 32 * WAVES - 1) / (32 * WAVES), items = tiles * cache.kv_heads * cache.batch;
+    if (items > INT32_MAX) return fail(SQAP_EUNSUPPORTED, "sqap_cache8_attention: %lld tiles of rows", (long long)items);
+    static std::atomic<bool> ready[kMaxDeviceSlots];
+    if (LDS > 65536 - 64 && !ready[device_slot()].load(std::memory_order_relaxed)) {
+        SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(cache8_attention_kernel<D, WAVES>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+        ready[device_slot()].store(true, std::memory_order_relaxed);
+    }
+    hipLaunchKernelGGL((cache8_attention_kernel<D, WAVES>), dim3((unsigned)items), dim3(64 * WAVES), LDS, st, Q, ldq, starts, past, rows, max_new, H,
+                       cache, O, ldo, (int)tiles);
+    SQAP_HIP_CHECK(hipGetLastError());
+    return SQAP_OK;
+}
+
 template <int D>
 static sqap_status launch_attention_d(const __half *Q, int64_t ldq, const int32_t *starts, const int32_t *past, int rows, int max_new, int H,
                                       const Cache8View &cache, __half *O, int64_t ldo, hipStream_t st)
 {
-    constexpr int LDS = 2 * 2 * kBlock * D * 2;
-    const int64_t tiles = ((int64_t)max_new * (H / cache.kv_heads) + kRowsOfTile - 1) / kRowsOfTile;
-    static std::atomic<bool> ready[kMaxDeviceSlots];
-    if (LDS > 65536 - 64 && !ready[device_slot()].load(std::memory_order_relaxed)) {
-        SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(cache8_attention_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
-        ready[device_slot()].store(true, std::memory_order_relaxed);
-    }
-    hipLaunchKernelGGL(cache8_attention_kernel<D>, dim3((unsigned)tiles, cache.kv_heads, cache.batch), dim3(256), LDS, st, Q, ldq, starts, past, rows, max_new, H,
-                       cache, O, ldo);
-    SQAP_HIP_CHECK(hipGetLastError());
-    return SQAP_OK;
+    return launch_attention_of<D, 4>(Q, ldq, starts, past, rows, max_new, H, cache, O, ldo, st);
 }
 
 sqap_status launch_cache8_attention(const __half *Q, int64_t ldq, const int32_t *starts, const int32_t *past, int rows, int max_new, int H,
