@@ -24,6 +24,7 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef unsigned v2u __attribute__((ext_vector_type(2)));
+typedef unsigned long long u64;
 
 constexpr int kBlock = kCache8Block;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -358,7 +359,7 @@ struct Unit {
             change = unit / scale;
             unit = scale;
         }
-        return scale / unit;
+        return scale * __builtin_amdgcn_rcpf(unit);                   // (a unit of the last place or two: as much as any of the sums' roundings)
     }
 };
 
@@ -560,7 +561,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
                     sum += e;
                     p[2 * tt + (i >> 3)][i & 7] = (_Float16)e;
                 }
-            lrun += sum / factor;
+            lrun += sum * __builtin_amdgcn_rcpf(factor);
             if (!(sv >= 0.f)) {                                       // values that are NaN as a whole: for the rows that see any of them
 #pragma unroll
                 for (int n = 0; n < 4; ++n)
@@ -610,12 +611,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
 // One workgroup per sequence, key head, up to 16 of the query heads that share it, and share of the sequence's blocks; a block is one
 // wavefront's.  The workgroup whose share ends with the last block appends the new row there.  Where there are several shares, each leaves
 // its sums in the workspace and the workgroup that arrives last adds them in their order.
-constexpr int kDecodeWaves = 4;
+constexpr int kDecodeWaves = 4, kMaxShares = 128;
 struct DecodeArgs {
     const __half *QKV;
     int64_t ld;
     const int32_t *pos, *past;
-    int H, G, chunks, shares;
+    int H, G, chunks, shares, per_share;                      // shares of the longest sequence, and its blocks in each
     Cache8View cache;
     __half *O;
     int64_t ldo;
@@ -629,8 +630,8 @@ struct DecodeLds {
     __attribute__((aligned(16))) _Float16 q[16][D];
     __attribute__((aligned(16))) union {
         struct {
-            _Float16 k[kBlock][D + 8];           // rows of the last block
-            _Float16 v[D][kBlock + 8];           // its values, transposed, positions in the order of the codes
+            unsigned short k[kBlock][D + 8];     // rows of the last block
+            unsigned short v[D][kBlock + 8];     // its values, transposed, positions in the order of the codes (value_place)
         } tail;
         float o[kDecodeWaves][16][D + 4];        // the wavefronts' sums
     } u;
@@ -642,17 +643,19 @@ struct DecodeLds {
     int arrived;
 };
 
-// slot of position s in the values' order: 8 of each 32 per lane group
+// slot of position s in the values' order: 8 of each 32 per lane group; and where column x has it: its eights are moved round by the column's,
+// so that the threads of a row, 8 columns apart, write to different banks (2.0 us for a block's rows without)
 __device__ __forceinline__ int value_slot(int s) { return (s & 32) | ((s >> 2) & 3) << 3 | ((s >> 4) & 1) << 2 | (s & 3); }
+__device__ __forceinline__ int value_place(int x, int at) { return ((at + (x & ~7)) & 56) | (at & 7); }
 
 template <int D>
-__global__ __launch_bounds__(64 * kDecodeWaves) void cache8_decode_kernel(const DecodeArgs a)
+__global__ __launch_bounds__(64 * kDecodeWaves, 2) void cache8_decode_kernel(const DecodeArgs a)
 {
     constexpr int HALF = D / 2, C = D / 64, T = 64 * kDecodeWaves, DT = D / 16;
     __shared__ DecodeLds<D> lds;
     const Cache8View &cache = a.cache;
     const int share = blockIdx.x, kh = blockIdx.y / a.chunks, chunk = blockIdx.y % a.chunks, b = blockIdx.z;
-    const int t = threadIdx.x, l = t & 63, wave = t >> 6, r = l & 15, g = l >> 4;
+    const int t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), r = l & 15, g = l >> 4;
     const int first_head = kh * a.G + chunk * 16, heads = min(16, a.G - chunk * 16);
     const int past = a.past[b];
     if (past < 0) return;
@@ -664,56 +667,121 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void cache8_decode_kernel(const 
         return;
     }
     const int last = past / kBlock, slot = past % kBlock;
-    const int per_share = (last + 1 + a.shares - 1) / a.shares, active = (last + per_share) / per_share;
+    const int per_share = max(a.per_share, (last + a.shares) / a.shares), active = (last + per_share) / per_share;
     const int begin = share * per_share, stop = min(begin + per_share, last + 1);
     if (begin > last) return;
     const bool has_last = stop == last + 1;
     const int64_t head = (int64_t)b * cache.kv_heads + kh;
     __half *tail_k = cache.tail + head * 2 * kBlock * D, *tail_v = tail_k + kBlock * D;
 
-    if (t < HALF) sincos((double)a.pos[b] * a.freq.f[t], &lds.sn[t], &lds.cs[t]);
+    // everything that does not wait for the rotation is asked for first: this wavefront's first block, the unfinished block's rows
+    v4i kraw[4 * C], vraw[DT];
+    auto fetch_keys = [&](int j) {
+        if (j >= stop || j == last) return;
+        const v4i *k = reinterpret_cast<const v4i *>(block_codes<D>(cache, head, j, 0)) + l;
+#pragma unroll
+        for (int i = 0; i < 4 * C; ++i) kraw[i] = k[i * 64];
+    };
+    auto fetch_values = [&](int j) {
+        if (j >= stop || j == last) return;
+        const v4i *v = reinterpret_cast<const v4i *>(block_codes<D>(cache, head, j, 1)) + l;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) vraw[i] = v[i * 64];
+    };
+    const float2 *scales = reinterpret_cast<const float2 *>(cache.scales + head * cache.blocks * 2);
+    float2 sc = {0.f, 0.f};
+    auto fetch_scales = [&](int j) {
+        if (j < stop && j != last) sc = scales[j];
+    };
+    __half qnew[16 * HALF / T][2];
+#pragma unroll
+    for (int i = 0; i < 16 * HALF / T; ++i) {
+        const int u = t + i * T;
+        if (u >= heads * HALF) break;
+        const __half *q = row + (int64_t)(first_head + u / HALF) * D + u % HALF;
+        qnew[i][0] = q[0];
+        qnew[i][1] = q[HALF];
+    }
+    const double angle = t < HALF ? (double)a.pos[b] * a.freq.f[t] : 0.0;
+    __half knew[2] = {}, vnew[2] = {};
+    if (has_last && t < HALF) {
+        const __half *k = row + (int64_t)(a.H + kh) * D, *v = row + (int64_t)(a.H + cache.kv_heads + kh) * D;
+        knew[0] = k[t], knew[1] = k[t + HALF];
+        vnew[0] = v[t], vnew[1] = v[t + HALF];
+    }
+    constexpr int UNITS = kBlock * D / 8 / T;                         // 8 columns of a row of the tail each
+    v4i tk[UNITS], tv[UNITS];
+    if (has_last) {
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            const int u = t + i * T, s = u / (D / 8), x = (u % (D / 8)) * 8;
+            tk[i] = tv[i] = v4i{0, 0, 0, 0};
+            if (s < slot) {
+                tk[i] = *reinterpret_cast<const v4i *>(tail_k + s * D + x);
+                tv[i] = *reinterpret_cast<const v4i *>(tail_v + s * D + x);
+            }
+        }
+    }
+    fetch_scales(begin + wave);
+    fetch_keys(begin + wave);
+    fetch_values(begin + wave);
+
+    if (t < HALF) sincos_of(angle, lds.sn[t], lds.cs[t]);
+    if (t < D) lds.odd[t] = 0;
     __syncthreads();
-    for (int u = t; u < heads * HALF; u += T) {
-        const int j = u / HALF, i = u % HALF;
-        const __half *q = row + (int64_t)(first_head + j) * D;
+#pragma unroll
+    for (int k = 0; k < 16 * HALF / T; ++k) {
+        const int u = t + k * T, j = u / HALF, i = u % HALF;
+        if (u >= heads * HALF) break;
         __half x, y;
-        rotate_pair(q[i], q[i + HALF], lds.cs[i], lds.sn[i], x, y);
+        rotate_pair(qnew[k][0], qnew[k][1], lds.cs[i], lds.sn[i], x, y);
         lds.q[j][i] = (_Float16)__half2float(x);
         lds.q[j][i + HALF] = (_Float16)__half2float(y);
     }
-    if (t < D) lds.odd[t] = 0;
     if (has_last && t < HALF) {
-        const __half *k = row + (int64_t)(a.H + kh) * D, *v = row + (int64_t)(a.H + cache.kv_heads + kh) * D;
-        rotate_pair(k[t], k[t + HALF], lds.cs[t], lds.sn[t], lds.knew[t], lds.knew[t + HALF]);
-        lds.vnew[t] = v[t];
-        lds.vnew[t + HALF] = v[t + HALF];
+        rotate_pair(knew[0], knew[1], lds.cs[t], lds.sn[t], lds.knew[t], lds.knew[t + HALF]);
+        lds.vnew[t] = vnew[0];
+        lds.vnew[t + HALF] = vnew[1];
     }
     __syncthreads();
     float tail_sk = 1.f, tail_sv = 1.f;
     if (has_last) {
         const bool full = slot == kBlock - 1;
         unsigned top_k = 0, top_v = 0;
-        for (int u = t; u < kBlock * D / 8; u += T) {
-            const int s = u / (D / 8), x = (u % (D / 8)) * 8;
-            union { v4i i; __half h[8]; } k = {v4i{0, 0, 0, 0}}, v = {v4i{0, 0, 0, 0}};
-            if (s < slot) {
-                k.i = *reinterpret_cast<const v4i *>(tail_k + s * D + x);
-                v.i = *reinterpret_cast<const v4i *>(tail_v + s * D + x);
-            } else if (s == slot) {
+        // (times the low half of a probability, zero or negative as often as not, an infinity would be NaN: it is added at the end)
+        auto set_aside = [&](int x, __half v, int at) {
+            const float w = __half2float(v);
+            const bool odd = !finite_bits(magnitude(v));
+            if (odd) atomicOr(&lds.odd[x], w > 0.f ? 1 : w < 0.f ? 2 : 4);
+            lds.u.tail.v[x][value_place(x, at)] = odd ? 0 : __half_as_ushort(v);
+        };
 #pragma unroll
-                for (int e = 0; e < 8; ++e) k.h[e] = lds.knew[x + e], v.h[e] = lds.vnew[x + e];
-            }
+        for (int i = 0; i < UNITS; ++i) {
+            const int u = t + i * T, s = u / (D / 8), x = (u % (D / 8)) * 8, at = value_slot(s);
+            *reinterpret_cast<v4i *>(&lds.u.tail.k[s][x]) = tk[i];
+            unsigned mk = 0, mv = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                top_k = max(top_k, magnitude(k.h[e]));
-                top_v = max(top_v, magnitude(v.h[e]));
-                const float w = __half2float(v.h[e]);
-                // (times the low half of a probability, zero or negative as often as not, an infinity would be NaN: it is added at the end)
-                const bool odd = !full && !finite_bits(magnitude(v.h[e]));
-                if (odd) atomicOr(&lds.odd[x + e], w > 0.f ? 1 : w < 0.f ? 2 : 4);
-                lds.u.tail.v[x + e][value_slot(s)] = odd ? (_Float16)0.f : (_Float16)w;
+            for (int w = 0; w < 4; ++w) {
+                mk = max(mk, max((unsigned)tk[i][w] & 0x7fffu, (unsigned)tk[i][w] >> 16 & 0x7fffu));
+                mv = max(mv, max((unsigned)tv[i][w] & 0x7fffu, (unsigned)tv[i][w] >> 16 & 0x7fffu));
             }
-            *reinterpret_cast<v4i *>(&lds.u.tail.k[s][x]) = k.i;
+            top_k = max(top_k, mk);
+            top_v = max(top_v, mv);
+            if (!full && !finite_bits(mv)) {
+#pragma unroll 1
+                for (int e = 0; e < 8; ++e) set_aside(x + e, reinterpret_cast<const __half *>(tail_v + s * D + x)[e], at);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) lds.u.tail.v[x + e][value_place(x, at)] = (unsigned short)((unsigned)tv[i][e >> 1] >> (16 * (e & 1)));
+            }
+        }
+        __syncthreads();
+        if (t < D) {                                                  // the new row
+            lds.u.tail.k[slot][t] = __half_as_ushort(lds.knew[t]);
+            if (full) lds.u.tail.v[t][value_place(t, value_slot(slot))] = __half_as_ushort(lds.vnew[t]);
+            else set_aside(t, lds.vnew[t], value_slot(slot));
+            top_k = max(top_k, magnitude(lds.knew[t]));
+            top_v = max(top_v, magnitude(lds.vnew[t]));
         }
         if (full) {
             top_k = wavefront_umax(top_k);
@@ -730,14 +798,14 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void cache8_decode_kernel(const 
             // words of four codes, in the order of the cache; the rows in LDS become their codes
             for (int u = t; u < kBlock * D / 4; u += T) {
                 const int e4 = u & 3, lane = (u >> 2) & 63, x = u >> 8, lr = lane & 15, lg = lane >> 4;
-                _Float16 *k = &lds.u.tail.k[(x / C) * 16 + lr][(x % C) * 64 + lg * 16 + e4 * 4];
-                _Float16 *v = &lds.u.tail.v[x * 16 + lr][(e4 >> 1) * 32 + lg * 8 + (e4 & 1) * 4];
+                unsigned short *k = &lds.u.tail.k[(x / C) * 16 + lr][(x % C) * 64 + lg * 16 + e4 * 4];
+                unsigned short *v = &lds.u.tail.v[x * 16 + lr][value_place(x * 16 + lr, (e4 >> 1) * 32 + lg * 8 + (e4 & 1) * 4)];
                 int wk = 0, wv = 0;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int ck = ok_k ? code_of((float)k[e], sk) : 0, cv = ok_v ? code_of((float)v[e], sv) : 0;
-                    k[e] = (_Float16)(float)ck;
-                    v[e] = (_Float16)(float)cv;
+                    const int ck = ok_k ? code_of(__half2float(__ushort_as_half(k[e])), sk) : 0, cv = ok_v ? code_of(__half2float(__ushort_as_half(v[e])), sv) : 0;
+                    k[e] = __half_as_ushort(__float2half_rn((float)ck));
+                    v[e] = __half_as_ushort(__float2half_rn((float)cv));
                     wk |= (ck & 255) << (8 * e);
                     wv |= (cv & 255) << (8 * e);
                 }
@@ -768,81 +836,100 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void cache8_decode_kernel(const 
     float mrun = -INFINITY, lrun = 0.f;
     Unit unit;
     const float per_d = kLog2e / sqrtf((float)D);
-    const float *scales = cache.scales + head * cache.blocks * 2;
-    for (int j = begin + wave; j < stop; j += kDecodeWaves) {
-        const bool is_last = j == last;
+    auto block = [&](int j, auto last_c) {
+        constexpr bool LAST = decltype(last_c)::value;                // the last block's rows are in LDS
         v4f s[4];
-        v4i vraw[DT];
-        float sk, sv;
 #pragma unroll
         for (int T4 = 0; T4 < 4; ++T4) s[T4] = v4f{0.f, 0.f, 0.f, 0.f};
-        if (!is_last) {
-            const v4i *k = reinterpret_cast<const v4i *>(block_codes<D>(cache, head, j, 0)) + l, *v = reinterpret_cast<const v4i *>(block_codes<D>(cache, head, j, 1)) + l;
-            v4i kraw[4 * C];
 #pragma unroll
-            for (int i = 0; i < 4 * C; ++i) kraw[i] = k[i * 64];
+        for (int T4 = 0; T4 < 4; ++T4)
 #pragma unroll
-            for (int i = 0; i < DT; ++i) vraw[i] = v[i * 64];
-            sk = scales[2 * j] * per_d;
-            sv = scales[2 * j + 1];
-#pragma unroll
-            for (int T4 = 0; T4 < 4; ++T4)
-#pragma unroll
-                for (int m = 0; m < 2 * C; ++m) {
+            for (int m = 0; m < 2 * C; ++m) {
+                v8h k;
+                if constexpr (LAST) {
+                    k = *reinterpret_cast<const v8h *>(&lds.u.tail.k[16 * T4 + r][64 * (m >> 1) + 16 * g + 8 * (m & 1)]);
+                } else {
                     const v4i w = kraw[T4 * C + (m >> 1)];
-                    s[T4] = __builtin_amdgcn_mfma_f32_16x16x32_f16((m & 1) ? halves_of(w[2], w[3]) : halves_of(w[0], w[1]), qf[m], s[T4], 0, 0, 0);
+                    k = (m & 1) ? halves_of(w[2], w[3]) : halves_of(w[0], w[1]);
                 }
-        } else {
-            sk = tail_sk * per_d;
-            sv = tail_sv;
-#pragma unroll
-            for (int T4 = 0; T4 < 4; ++T4)
-#pragma unroll
-                for (int m = 0; m < 2 * C; ++m)
-                    s[T4] = __builtin_amdgcn_mfma_f32_16x16x32_f16(*reinterpret_cast<const v8h *>(&lds.u.tail.k[16 * T4 + r][64 * (m >> 1) + 16 * g + 8 * (m & 1)]),
-                                                                   qf[m], s[T4], 0, 0, 0);
+                s[T4] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qf[m], s[T4], 0, 0, 0);
+            }
+        float sk = LAST ? tail_sk : sc.x, sv = LAST ? tail_sv : sc.y;
+        sk = sk == 0.f ? per_d : sk * per_d;                          // (keys that are all zeros: as in cache8_attention_kernel)
+        if constexpr (!LAST) {
+            fetch_scales(j + kDecodeWaves);
+            fetch_keys(j + kDecodeWaves);                             // (into the registers that have just become free)
         }
         float top = -INFINITY;
 #pragma unroll
         for (int T4 = 0; T4 < 4; ++T4)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                s[T4][i] *= sk;
-                if (is_last && 16 * T4 + 4 * g + i > slot) s[T4][i] = -INFINITY;
+                if (LAST && 16 * T4 + 4 * g + i > slot) s[T4][i] = -INFINITY;
                 top = fmaxf(top, s[T4][i]);
             }
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
+        if (top > -INFINITY) top *= sk;
+        float by = sk;
+        if (__any(fabsf(top) > kLargeScore && top > -INFINITY)) {
+#pragma unroll
+            for (int T4 = 0; T4 < 4; ++T4)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float w = s[T4][i] * sk;
+                    asm volatile("" : "+v"(w));                       // (rounded)
+                    s[T4][i] = s[T4][i] == -INFINITY ? -INFINITY : w;
+                }
+            by = 1.f;
+        }
         float change;
         const float factor = unit.enter(sv, change);
-        if (top > mrun) {
+        if (top > mrun + kRaiseBy) {
             const float raise = exp2f(mrun - top);
             change *= raise;
             lrun *= raise;
             mrun = top;
         }
+        if (__any(change != 1.f)) {
 #pragma unroll
-        for (int i = 0; i < DT; ++i) ot[i] *= change;
+            for (int i = 0; i < DT; ++i) ot[i] *= change;
+        }
+        const float from = __log2f(factor) - mrun;
+        float sum = 0.f;
         v8h p[2], rest[2];                                            // a probability as the sum of two halves
 #pragma unroll
         for (int T4 = 0; T4 < 4; ++T4)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float e = exp2f(s[T4][i] - mrun), w = sv >= 0.f ? e * factor : s[T4][i] == -INFINITY ? 0.f : NAN;
-                lrun += e;
-                const _Float16 w0 = (_Float16)w;
-                p[T4 >> 1][(T4 & 1) * 4 + i] = w0;
-                rest[T4 >> 1][(T4 & 1) * 4 + i] = (_Float16)(w - (float)w0);
+                const float e = __builtin_amdgcn_exp2f(fmaf(s[T4][i], by, from));
+                sum += e;
+                const _Float16 e0 = (_Float16)e;
+                p[T4 >> 1][(T4 & 1) * 4 + i] = e0;
+                rest[T4 >> 1][(T4 & 1) * 4 + i] = (_Float16)(e - (float)e0);
             }
+        lrun += sum * __builtin_amdgcn_rcpf(factor);
+        if (!(sv >= 0.f)) {                                           // values that are NaN as a whole
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p[n][i] = s[2 * n + (i >> 2)][i & 3] == -INFINITY ? (_Float16)0.f : (_Float16)NAN;
+        }
 #pragma unroll
         for (int i = 0; i < DT; ++i)
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
-                const v8h v = is_last ? *reinterpret_cast<const v8h *>(&lds.u.tail.v[16 * i + r][32 * n + 8 * g]) : halves_of(vraw[i][2 * n], vraw[i][2 * n + 1]);
+                v8h v;
+                if constexpr (LAST) v = *reinterpret_cast<const v8h *>(&lds.u.tail.v[16 * i + r][value_place(16 * i + r, 32 * n + 8 * g)]);
+                else v = halves_of(vraw[i][2 * n], vraw[i][2 * n + 1]);
                 ot[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[n], ot[i], 0, 0, 0);
                 ot[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, rest[n], ot[i], 0, 0, 0);
             }
-    }
+        if constexpr (!LAST) fetch_values(j + kDecodeWaves);
+    };
+    int j = begin + wave;
+    for (; j < stop && j < last; j += kDecodeWaves) block(j, std::false_type{});
+    if (j < stop) block(j, std::true_type{});
     lrun += __shfl_xor(lrun, 16);
     lrun += __shfl_xor(lrun, 32);
     __syncthreads();                                                  // the last block's rows have been read
@@ -899,19 +986,58 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void cache8_decode_kernel(const 
     __syncthreads();
     if (lds.arrived != active - 1) return;
     if (t == 0) __hip_atomic_store(a.counters + item, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // the next call starts from zero again
+    // The shares' sums in one: their maxima and sums first, a factor for each share and head, then the outputs, two columns per load, the
+    // shares dealt to as many groups of threads as there are.
     const float *all = a.partials + item * a.shares * per_item;
-    for (int u = t; u < heads * D; u += T) {
-        const int j = u / D;
-        float top = -INFINITY, sum = 0.f, o = 0.f;
-        for (int w = 0; w < active; ++w)
-            top = fmaxf(top, __hip_atomic_load(all + (int64_t)w * per_item + heads * D + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-        for (int w = 0; w < active; ++w) {
-            const float *from = all + (int64_t)w * per_item;
-            const float f = exp2f(__hip_atomic_load(from + heads * D + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) - top);
-            sum += f * __hip_atomic_load(from + heads * D + heads + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            o += f * __hip_atomic_load(from + u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    float *factor = &lds.u.o[0][0][0];                                // [share][head]
+    __syncthreads();
+    for (int u = t; u < active * heads; u += T) factor[u] = __hip_atomic_load(all + (int64_t)(u / heads) * per_item + heads * D + u % heads, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (t < heads) {
+        float top = -INFINITY;
+        for (int w = 0; w < active; ++w) top = fmaxf(top, factor[w * heads + t]);
+        lds.m[0][t] = top;
+    }
+    __syncthreads();
+    for (int u = t; u < active * heads; u += T) factor[u] = exp2f(factor[u] - lds.m[0][u % heads]);
+    float *sums = factor + kMaxShares * 16;                           // [share][head]
+    for (int u = t; u < active * heads; u += T)
+        sums[u] = __hip_atomic_load(all + (int64_t)(u / heads) * per_item + heads * D + heads + u % heads, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (t < heads) {
+        float sum = 0.f;
+        for (int w = 0; w < active; ++w) sum += factor[w * heads + t] * sums[w * heads + t];
+        lds.l[0][t] = 1.f / sum;
+    }
+    const int pairs = heads * (D / 2), groups = max(1, T / pairs);
+    float2 *parts = reinterpret_cast<float2 *>(sums);                 // [group][pair], over the sums that have been added
+    for (int u0 = 0; u0 < pairs; u0 += T) {
+        const int u = u0 + t % (pairs < T ? pairs : T), group = pairs < T ? t / pairs : 0;
+        float2 o = {0.f, 0.f};
+        if (u < pairs && group < groups) {
+            const int j = u / (D / 2);
+#pragma unroll 8
+            for (int w = group; w < active; w += groups) {
+                const u64 raw = __hip_atomic_load(reinterpret_cast<const u64 *>(all + (int64_t)w * per_item) + u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                const float f = factor[w * heads + j];
+                o.x += f * __uint_as_float((unsigned)raw);
+                o.y += f * __uint_as_float((unsigned)(raw >> 32));
+            }
         }
-        out[u] = __float2half_rn(o / sum);
+        if (groups > 1) {
+            __syncthreads();
+            if (u < pairs && group > 0 && group < groups) parts[(group - 1) * pairs + u] = o;
+            __syncthreads();
+            if (u < pairs && group == 0)
+                for (int w = 0; w < groups - 1; ++w) o.x += parts[w * pairs + u].x, o.y += parts[w * pairs + u].y;
+        } else if (u0 == 0) {
+            __syncthreads();
+        }
+        if (u < pairs && group == 0) {
+            const float norm = lds.l[0][u / (D / 2)];
+            out[2 * u] = __float2half_rn(o.x * norm);
+            out[2 * u + 1] = __float2half_rn(o.y * norm);
+        }
     }
 }
 
@@ -987,12 +1113,13 @@ sqap_status launch_cache8_attention(const __half *Q, int64_t ldq, const int32_t 
                    : launch_attention_d<128>(Q, ldq, starts, past, rows, max_new, H, cache, O, ldo, st);
 }
 
+constexpr int kDecodeGroups = 512;
 // Shares of a sequence: as many workgroups as fill the device a few times over, four blocks at least to each (one per wavefront).
 static int decode_shares(int batch, int H, int kv_heads, int longest)
 {
     const int chunks = (H / kv_heads + 15) / 16, blocks = (longest + kBlock - 1) / kBlock;
     const int64_t items = (int64_t)batch * kv_heads * chunks;
-    return (int)std::max<int64_t>(1, std::min<int64_t>((blocks + kDecodeWaves - 1) / kDecodeWaves, 1024 / items));
+    return (int)std::max<int64_t>(1, std::min<int64_t>({(blocks + kDecodeWaves - 1) / kDecodeWaves, kDecodeGroups / items, kMaxShares}));
 }
 
 // counters in front: room for one per sequence and query head (a workgroup uses one)
@@ -1018,6 +1145,7 @@ sqap_status launch_cache8_decode(const __half *QKV, int64_t ld, const int32_t *p
     a.G = H / cache.kv_heads;
     a.chunks = (a.G + 15) / 16;
     a.shares = decode_shares(cache.batch, H, cache.kv_heads, longest);
+    a.per_share = ((longest + kBlock - 1) / kBlock + a.shares - 1) / a.shares;
     a.cache = cache;
     a.O = O;
     a.ldo = ldo;
