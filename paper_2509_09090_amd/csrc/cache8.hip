@@ -1113,13 +1113,17 @@ sqap_status launch_cache8_attention(const __half *Q, int64_t ldq, const int32_t 
                    : launch_attention_d<128>(Q, ldq, starts, past, rows, max_new, H, cache, O, ldo, st);
 }
 
+// Shares of a sequence.  One up to eight blocks: a wavefront's second block costs 1.5 us, joining 2.5.  Beyond, shares of four blocks while
+// there are few (1500 positions of 32 heads: 11.4 us, shares of eight 12.4), of eight at least once there are eight (4000: 14.0, of four
+// 16.6); and no more than two workgroups per compute unit in all, which is what their registers leave room for (100k positions of 8 key
+// heads: 52 us with 512 workgroups, 66 with 768).
 constexpr int kDecodeGroups = 512;
-// Shares of a sequence: as many workgroups as fill the device a few times over, four blocks at least to each (one per wavefront).
 static int decode_shares(int batch, int H, int kv_heads, int longest)
 {
     const int chunks = (H / kv_heads + 15) / 16, blocks = (longest + kBlock - 1) / kBlock;
     const int64_t items = (int64_t)batch * kv_heads * chunks;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({(blocks + kDecodeWaves - 1) / kDecodeWaves, kDecodeGroups / items, kMaxShares}));
+    const int wanted = blocks <= 8 ? 1 : std::max((blocks + 7) / 8, std::min(8, (blocks + 3) / 4));
+    return (int)std::max<int64_t>(1, std::min<int64_t>({wanted, kDecodeGroups / items, kMaxShares}));
 }
 
 // counters in front: room for one per sequence and query head (a workgroup uses one)
