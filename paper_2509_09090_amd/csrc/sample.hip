@@ -12,158 +12,293 @@ namespace sqap {
 
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 typedef unsigned v4u_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 typedef unsigned long long u64;
 
-constexpr int kSampleT = 1024, kSampleWaves = kSampleT / 64, kSampleCopies = 8;
-constexpr int kSampleMaxSlabs = kSampleMaxVocab / (8 * kSampleT);
-constexpr unsigned kKeyMinusInf = 0x03ffu;                            // keys up to here: minus infinity, and 0 for NaN
-constexpr double kMassOne = 1099511627776.0;                          // 2^40
+constexpr int kSampleT = 1024, kSampleWaves = kSampleT / 64, kSlab = 64 * 8;
+constexpr int kSampleCached = 32768;                                  // logits that are kept in LDS
+constexpr int kBins = 4096;                                           // of 16 keys each
+constexpr int kListed = 8192;                                         // candidates that are kept in LDS
+constexpr int kTieShift = 52;                                         // a slab's ties above its mass, which has 50 bits at most
+constexpr unsigned kKeyMinusInf = 0x03ffu;                            // the lowest key there is
 
-__device__ __forceinline__ unsigned key_of(unsigned h)
-{
-    const unsigned m = h & 0x7fffu;
-    if (m == 0) return 0x8000u;                                       // the two zeros are equal
-    if (m > 0x7c00u) return 0u;                                       // NaN is below every number
-    return h & 0x8000u ? ~h & 0xffffu : h | 0x8000u;
-}
+// Keys of halves that are neither NaN nor minus zero (see `clean`): integers that order as the halves do.
+__device__ __forceinline__ unsigned key_of(unsigned h) { return h & 0x8000u ? ~h & 0xffffu : h | 0x8000u; }
+__device__ __forceinline__ unsigned half_of(unsigned key) { return key & 0x8000u ? key & 0x7fffu : ~key & 0xffffu; }
 __device__ __forceinline__ float value_of(unsigned key)
 {
-    return __half2float(__ushort_as_half((unsigned short)(key & 0x8000u ? key & 0x7fffu : ~key & 0xffffu)));
+    return __half2float(__ushort_as_half((unsigned short)half_of(key)));
 }
 
-// The exponent in two parts (x times a binary64 factor as two binary32 ones), so that a mass is off by 2^-22 or so however far the logit is
-// from the largest.
+__device__ __forceinline__ unsigned bin_of(unsigned key) { return kBins - 1 - (key >> 4); }
+
+// exp2((value - top) * per_nat) in units of 2^-40.  The factor is in two parts, and so is the product, so that a mass is off by 2^-22 or so
+// however far the logit is from the largest.  The difference is held between 0 (an infinite logit's) and one whose mass is none (minus infinity's).
 struct Mass {
-    unsigned top;
-    float top_value, hi, lo;
-    __device__ __forceinline__ u64 operator()(unsigned key) const
+    float top, hi, lo, least;
+    __device__ __forceinline__ void set(float top_, double per_nat)
     {
-        if (key == top) return 1ull << 40;
-        const float x = value_of(key) - top_value, p = x * hi;
-        if (key <= kKeyMinusInf || !(p > -41.f)) return 0;
-        const float rest = fmaf(x, lo, fmaf(x, hi, -p));
-        const float w = exp2f(p) * fmaf(rest, 0.6931471805599453f, 1.f);
-        const float a = floorf(w * 1048576.f);
-        return ((u64)(unsigned)a << 20) + (u64)(unsigned)((w * 1048576.f - a) * 1048576.f);
+        top = fminf(top_, 3e38f);
+        per_nat = fmin(fmax(per_nat, 1e-30), 1e30);
+        hi = (float)per_nat;
+        lo = (float)(per_nat - (double)hi);
+        least = -64.f / hi;
     }
+    __device__ __forceinline__ float scaled(float value) const        // in units of 2^-20
+    {
+        const float x = __builtin_amdgcn_fmed3f(value - top, least, 0.f), p = x * hi;
+        const float rest = fmaf(x, lo, fmaf(x, hi, -p));
+        const float e = __builtin_amdgcn_exp2f(p) * 1048576.f;
+        return fmaf(e * rest, 0.6931471805599453f, e);
+    }
+    static __device__ __forceinline__ unsigned whole(float w) { return (unsigned)w; }
+    static __device__ __forceinline__ unsigned part(float w) { return (unsigned)(__builtin_amdgcn_fractf(w) * 1048576.f); }
+    static __device__ __forceinline__ u64 of(float w) { return ((u64)whole(w) << 20) + part(w); }
+    __device__ __forceinline__ u64 operator()(float value) const { return of(scaled(value)); }
 };
 
-__device__ __forceinline__ u64 shfl_up64(u64 v, int by) { return (u64)__shfl_up((long long)v, by); }
-
-// Inclusive sums over the lanes.
+// Inclusive sums over the lanes: inside rows of 16 by shifts, then the rows' last lanes are added to the rows behind.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 dpp_add(u64 v)
+{
+    const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)v, CTRL, ROWS, 0xf, false);
+    const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)(v >> 32), CTRL, ROWS, 0xf, false);
+    return v + ((u64)hi << 32 | lo);
+}
 __device__ __forceinline__ u64 wave_scan(u64 v)
 {
-    const int l = threadIdx.x & 63;
-#pragma unroll
-    for (int by = 1; by < 64; by <<= 1) {
-        const u64 o = shfl_up64(v, by);
-        if (l >= by) v += o;
-    }
-    return v;
+    v = dpp_add<0x111, 0xf>(v);
+    v = dpp_add<0x112, 0xf>(v);
+    v = dpp_add<0x114, 0xf>(v);
+    v = dpp_add<0x118, 0xf>(v);
+    v = dpp_add<0x142, 0xa>(v);
+    return dpp_add<0x143, 0xc>(v);
 }
-
-// By one whole wavefront: the first of n values whose inclusive sum reaches `target` (>= 1; there is one), and the sum before it.
-__device__ __forceinline__ int first_reaching(const u64 *values, int n, u64 target, u64 &before)
+__device__ __forceinline__ u64 row_scan(u64 v)                      // inside rows of 16 only
 {
-    const int l = threadIdx.x & 63, per = (n + 63) / 64;
-    u64 mine = 0;
-    for (int i = 0; i < per; ++i)
-        if (l * per + i < n) mine += values[l * per + i];
-    const u64 sum = wave_scan(mine);
-    const u64 reached = __ballot(sum >= target);
-    const int lane = reached ? __builtin_ctzll(reached) : 63;
-    u64 cum = (u64)__shfl((long long)(sum - mine), lane);
-    int at = lane * per;
-    for (; at < n - 1 && cum + values[at] < target; ++at) cum += values[at];
-    before = cum;
-    return at;
+    v = dpp_add<0x111, 0xf>(v);
+    v = dpp_add<0x112, 0xf>(v);
+    v = dpp_add<0x114, 0xf>(v);
+    return dpp_add<0x118, 0xf>(v);
 }
+__device__ __forceinline__ u64 lane_value(u64 v, int l)
+{
+    return (u64)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)v, l) | (u64)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)(v >> 32), l) << 32;
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned dpp_add(unsigned v)
+{
+    return v + (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ unsigned wave_scan(unsigned v)
+{
+    v = dpp_add<0x111, 0xf>(v);
+    v = dpp_add<0x112, 0xf>(v);
+    v = dpp_add<0x114, 0xf>(v);
+    v = dpp_add<0x118, 0xf>(v);
+    v = dpp_add<0x142, 0xa>(v);
+    return dpp_add<0x143, 0xc>(v);
+}
+__device__ __forceinline__ unsigned wave_total(unsigned v) { return (unsigned)__builtin_amdgcn_readlane((int)wave_scan(v), 63); }
 
 struct SampleArgs {
     const __half *logits;
     int64_t ld;
-    int vocab;
+    int vocab, slabs;                    // slabs of 512 logits
     const float *temperature, *top_p, *min_p, *uniform;
     const int32_t *top_k;
     int32_t *token;
     float *prob;
 };
 
-struct SampleLds {
-    u64 mass[256], bins[256 * kSampleCopies];
-    unsigned count[256 * kSampleCopies];
-    u64 count64[256];
-    u64 table[kSampleMaxSlabs * kSampleWaves];
-    unsigned ties[kSampleMaxSlabs * kSampleWaves];
-    unsigned wave_top[kSampleWaves];
+struct alignas(16) SampleLds {
+    v4u last[64];                        // the last slab, with minus infinity behind its end
+    u64 bins[kBins];                     // masses or counts by key / 16, the largest first
+    u64 keys[16];                        // counts of one bin's
+    u64 wave_sum[kSampleWaves];
+    u64 before;
+    unsigned ties_before;
+    unsigned wave_max[kSampleWaves];
     int found;
-    unsigned cut_key;
-    u64 cut_count, cut_mass, cut_total, before;
+    unsigned listed;
+    unsigned list[kListed];              // key, and above it the slab
 };
 
-// One workgroup per row.  PIECES > 0: the row is kept in registers, 8 neighbouring logits per piece; 0: it is read again for every pass.
-template <int PIECES>
+// One workgroup per row; a wavefront has every 16th slab of 512 logits, eight to a lane.  CACHED: the row is kept in LDS
+// after the first pass; otherwise it is read again where it is needed, four slabs ahead.
+// What bounds it is the instructions of one compute unit: some 27 for each token where all of them count (128001 of them: 24 us, where the
+// largest alone is found in 6), and the 16 wavefronts' share in every step that is not about the row, so that each step stands here once
+// and has few barriers.  First a bound is found below which nothing can stay: for top-k the k-th largest of the threads' maxima, for top-p alone
+// the point where the maxima of the lanes' eight have the mass that is asked for (the total has to be known first), for min-p its
+// own.  One pass collects the logits from there on in LDS in no order (all that follows is sums of integers), and the cut is found
+// among those, for top-k by counts and for top-p by masses: a histogram of 4096 bins, and of the 16 keys of the bin that holds the cut.  The masses
+// that stay are added up by slab, and the drawn token's slab alone is looked at again.  Where more stay than LDS has room for,
+// the passes go over the row.  A row of 32000: the largest 3.7 us, no filter 10.8, top-k 40 11.5, top-p 0.9 16.5, all three 16.4; of 128001:
+// 6.5, 29.7, 19.4, 46.3, 27.0, and 113 where the 97 in 100 that stay are tens of thousands.  (Full passes throughout, with the
+// histogram of every token: 28 and 99 us for all three and for top-p.)
+template <bool CACHED>
 __global__ __launch_bounds__(kSampleT) void sample_kernel(const SampleArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) uint8_t raw_lds[];
     SampleLds &lds = *reinterpret_cast<SampleLds *>(raw_lds);
-    const int b = blockIdx.x, t = threadIdx.x, l = t & 63, wave = t >> 6;
+    v4u *cached = reinterpret_cast<v4u *>(raw_lds + sizeof(SampleLds));
+    u64 *slab_sum = reinterpret_cast<u64 *>(raw_lds + sizeof(SampleLds) + (CACHED ? (size_t)a.slabs * kSlab * 2 : 0));
+    const int b = blockIdx.x, t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const unsigned short *row = reinterpret_cast<const unsigned short *>(a.logits + (int64_t)b * a.ld);
-    const int slabs = PIECES ? PIECES : (a.vocab + 8 * kSampleT - 1) / (8 * kSampleT);
-    auto load = [&](int i) {
-        const int at = (i * kSampleT + t) * 8;
-        v4u v = {0x7e007e00u, 0x7e007e00u, 0x7e007e00u, 0x7e007e00u};  // past the end: NaN
-        if (at + 8 <= a.vocab) {
-            v = *reinterpret_cast<const v4u_any *>(row + at);
-        } else {
-            for (int e = 0; e < 8 && at + e < a.vocab; ++e) {
-                const unsigned shift = 16 * (e & 1);
-                v[e >> 1] = (v[e >> 1] & ~(0xffffu << shift)) | (unsigned)row[at + e] << shift;
-            }
+    const int slabs = a.slabs, last = slabs - 1;
+    const float temperature = a.temperature ? a.temperature[b] : 1.f, p_given = a.top_p ? a.top_p[b] : 1.f, m_given = a.min_p ? a.min_p[b] : 0.f;
+    const float u = a.uniform[b];
+    const int k_given = a.top_k ? a.top_k[b] : 0;
+    // a lane's logits of a slab other than the last (of the last but one where there is none; nothing where there is but one)
+    auto fetch = [&](int s) {
+        v4u v = {0, 0, 0, 0};
+        if (last > 0) v = *reinterpret_cast<const v4u_any *>(row + min(s, last - 1) * kSlab + l * 8);
+        return v;
+    };
+    // minus infinity in the place of NaN, zero in that of minus zero
+    auto clean = [](v4u v) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            union { unsigned u; v2h h; } x = {v[i]};
+            const v2h zero = {(_Float16)0.f, (_Float16)0.f}, least = {(_Float16)-INFINITY, (_Float16)-INFINITY};
+            x.h = __builtin_elementwise_max(x.h + zero, least);
+            v[i] = x.u;
         }
         return v;
     };
-    v4u held[PIECES ? PIECES : 1];
-    if (PIECES)
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) held[i] = load(i);
-    // body(key, slab, element) over this thread's logits, slab by slab
-    auto each = [&](auto body) {
-        if constexpr (PIECES > 0) {
-#pragma unroll
-            for (int i = 0; i < PIECES; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) body(key_of(held[i][e >> 1] >> (16 * (e & 1)) & 0xffffu), i, e);
-        } else {
-            for (int i = 0; i < slabs; ++i) {
-                const v4u v = load(i);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) body(key_of(v[e >> 1] >> (16 * (e & 1)) & 0xffffu), i, e);
-            }
+    auto half_at = [](const v4u &v, int e) {
+        const unsigned lo = e & 2 ? v[1] : v[0], hi = e & 2 ? v[3] : v[2];
+        return (e & 4 ? hi : lo) >> (16 * (e & 1)) & 0xffffu;
+    };
+    auto float_of = [](unsigned h) { return __half2float(__ushort_as_half((unsigned short)h)); };
+    auto largest = [](const v4u &v) {
+        union { unsigned u; v2h h; } x[4] = {{v[0]}, {v[1]}, {v[2]}, {v[3]}};
+        const v2h m = __builtin_elementwise_max(__builtin_elementwise_max(x[0].h, x[1].h), __builtin_elementwise_max(x[2].h, x[3].h));
+        return fmaxf((float)m[0], (float)m[1]);
+    };
+    auto key_of_value = [](float value) { return key_of(__half_as_ushort(__float2half_rn(value))); };
+    // body(slab, logits) over this wavefront's slabs; `ahead` runs after the first loads
+    auto each_loaded = [&](auto ahead, auto body) {
+        v4u v0 = fetch(wave), v1 = fetch(wave + kSampleWaves), v2 = fetch(wave + 2 * kSampleWaves), v3 = fetch(wave + 3 * kSampleWaves);
+        ahead();
+        for (int s = wave; s < slabs; s += kSampleWaves) {
+            v4u now = v0;
+            v0 = v1;
+            v1 = v2;
+            v2 = v3;
+            v3 = fetch(s + 4 * kSampleWaves);
+            if (s == last) now = lds.last[l];
+            body(s, clean(now));
         }
     };
+    auto each_slab = [&](auto body) {
+        if constexpr (CACHED) {
+            for (int s = wave; s < slabs; s += kSampleWaves) body(s, cached[s * 64 + l]);
+        } else {
+            each_loaded([] {}, body);
+        }
+    };
+    // (all three are values of halves)
+    auto any_between = [](const v4u &v, float low, float high) {
+        const v2h l2 = {(_Float16)low, (_Float16)low}, h2 = {(_Float16)high, (_Float16)high};
+        typedef unsigned short v2s __attribute__((ext_vector_type(2)));
+        v2s outside = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            union { unsigned u; v2h h; v2s s; } x = {v[i]}, y;
+            y.h = __builtin_elementwise_min(__builtin_elementwise_max(x.h, l2), h2);
+            x.u ^= y.u;
+            outside += __builtin_elementwise_min(x.s, v2s{1, 1});
+        }
+        return outside[0] + outside[1] < 8;
+    };
+    // which of a lane's eight are `least` or more
+    auto from_bits = [&](const v4u &v, float least) {
+        unsigned bits = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) bits |= float_of(half_at(v, e)) >= least ? 1u << e : 0u;
+        return bits;
+    };
+    bool listed = false;
+    unsigned n_listed = 0;
+    // The sum of the threads in front, and of all.  (A barrier lies between the last reads of wave_sum and this.)
+    auto block_scan = [&](u64 v, u64 &front) {
+        const u64 cum = wave_scan(v);
+        if (l == 63) lds.wave_sum[wave] = cum;
+        __syncthreads();
+        const u64 waves = row_scan(lds.wave_sum[l & (kSampleWaves - 1)]);
+        front = cum - v + (wave ? lane_value(waves, wave - 1) : 0);
+        return lane_value(waves, kSampleWaves - 1);
+    };
+    // From the largest key down, the first bin whose inclusive sum reaches `target` (>= 1), and the sum before it; -1: none.  Bins and keys are
+    // zeroes again.
+    auto first_bin = [&](u64 target) {
+        __syncthreads();
+        u64 of[4], sum = 0, at;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            sum += of[i] = lds.bins[4 * t + i];
+            lds.bins[4 * t + i] = 0;
+        }
+        if (t < 16) lds.keys[t] = 0;
+        const u64 all = block_scan(sum, at);
+        if (at < target && at + sum >= target) {
+            int i = 0;
+#pragma unroll
+            for (int x = 0; x < 3; ++x)
+                if (i == x && at + of[x] < target) at += of[x], ++i;
+            lds.found = kBins - 1 - (4 * t + i);
+            lds.before = at;
+        }
+        __syncthreads();
+        return all >= target ? lds.found : -1;
+    };
 
-    unsigned top = 0;
-    each([&](unsigned key, int, int) { top = max(top, key); });
-    for (int by = 32; by > 0; by >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, by));
-    if (l == 0) lds.wave_top[wave] = top;
-    if (t == 0) lds.found = a.vocab;
+    // ---- the largest logit, and each thread's
+    float mine = -INFINITY;
+    int mine_at = wave;
+    each_loaded(
+        [&] {
+            if (t < kSlab) reinterpret_cast<unsigned short *>(lds.last)[t] = last * kSlab + t < a.vocab ? row[last * kSlab + t] : 0xfc00;
+            if (t == 0) lds.found = a.vocab, lds.listed = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) lds.bins[4 * t + i] = 0;
+            for (int s = t; s < slabs; s += kSampleT) slab_sum[s] = 0;
+            __syncthreads();
+        },
+        [&](int s, const v4u &v) {
+            if constexpr (CACHED) cached[s * 64 + l] = v;
+            const float m = largest(v);
+            mine_at = m > mine ? s : mine_at;
+            mine = fmaxf(mine, m);
+        });
+    unsigned top_key = key_of_value(mine);
+    top_key = max(top_key, dpp_move<kDppXor1>(top_key));
+    top_key = max(top_key, dpp_move<kDppXor2>(top_key));
+    top_key = max(top_key, dpp_move<kDppHalfMirror>(top_key));
+    top_key = max(top_key, dpp_move<kDppMirror>(top_key));
+    top_key = max(max((unsigned)__builtin_amdgcn_readlane((int)top_key, 0), (unsigned)__builtin_amdgcn_readlane((int)top_key, 16)),
+                  max((unsigned)__builtin_amdgcn_readlane((int)top_key, 32), (unsigned)__builtin_amdgcn_readlane((int)top_key, 48)));
+    if (l == 0) lds.wave_max[wave] = top_key;
     __syncthreads();
-    for (int w = 0; w < kSampleWaves; ++w) top = max(top, lds.wave_top[w]);
-    if (top <= kKeyMinusInf) {                                        // nothing can be drawn
+    top_key = lds.wave_max[l & (kSampleWaves - 1)];
+    top_key = max(top_key, dpp_move<kDppXor1>(top_key));
+    top_key = max(top_key, dpp_move<kDppXor2>(top_key));
+    top_key = max(top_key, dpp_move<kDppHalfMirror>(top_key));
+    top_key = (unsigned)__builtin_amdgcn_readfirstlane((int)max(top_key, dpp_move<kDppMirror>(top_key)));
+    if (top_key <= kKeyMinusInf) {                                    // nothing can be drawn
         if (t == 0) {
             a.token[b] = -1;
             if (a.prob) a.prob[b] = 0.f;
         }
         return;
     }
-    const float temperature = a.temperature ? a.temperature[b] : 1.f;
+    const float top = value_of(top_key);
     if (!(temperature > 0.f)) {                                       // the most likely one
-        int first = a.vocab;
-        each([&](unsigned key, int i, int e) {
-            if (key == top) first = min(first, (i * kSampleT + t) * 8 + e);
-        });
-        if (first < a.vocab) atomicMin(&lds.found, first);
+        if (mine == top) {
+            const v4u v = clean(mine_at == last ? lds.last[l] : fetch(mine_at));
+            atomicMin(&lds.found, mine_at * kSlab + l * 8 + (int)__builtin_ctz(from_bits(v, top)));
+        }
         __syncthreads();
         if (t == 0) {
             a.token[b] = lds.found;
@@ -171,270 +306,273 @@ __global__ __launch_bounds__(kSampleT) void sample_kernel(const SampleArgs a)
         }
         return;
     }
-    Mass mass;
-    mass.top = top;
-    mass.top_value = value_of(top);
     const double per_nat = 1.4426950408889634074 / (double)temperature;
-    mass.hi = (float)per_nat;
-    mass.lo = (float)(per_nat - (double)mass.hi);
+    Mass mass;
+    mass.set(top, per_nat);
 
-    const int k_given = a.top_k ? a.top_k[b] : 0;
+    const float lowest = value_of(kKeyMinusInf + 1);                  // (minus infinity never stays)
     const int k = k_given > 0 && k_given < a.vocab ? k_given : 0;     // 0: all
-    const float p_given = a.top_p ? a.top_p[b] : 1.f;
     const bool by_mass = !(p_given >= 1.f);
-    const float m_given = a.min_p ? a.min_p[b] : 0.f;
-    const u64 least = m_given > 0.f ? (u64)ceil(fmin((double)m_given, 1.0) * kMassOne) : 0;
+    // min-p: the lowest value whose mass is enough, the top's at the latest: of 2^16 keys, 64 at a time
+    float min_value = lowest;
+    if (m_given > 0.f) {
+        const float enough = fminf(m_given, 1.f) * 1048576.f;
+        int below = 0;                                                // (the lowest key of all has no mass)
+#pragma unroll 1
+        for (int step = 1024; step; step >>= step == 1 ? 1 : step == 16 ? 4 : 6) {
+            const int key = below + step * (l + 1);
+            const u64 is = __ballot(key >= (int)top_key || (key > (int)kKeyMinusInf && mass.scaled(value_of((unsigned)key)) >= enough));
+            below += is ? step * (int)__builtin_ctzll(is) : step * 64;
+        }
+        min_value = fmaxf(lowest, value_of((unsigned)min(below + 1, (int)top_key)));
+    }
 
-    // the cut: keys above it stay, and `cut_count` of its own key
+    // the cut: keys above it stay, and `cut_count` of its own key, of which there are `cut_has`
     unsigned cut = 0;
-    u64 cut_count = ~0ull;
-    if (k || by_mass) {
-        auto clear = [&] {
-            for (int i = t; i < 256 * kSampleCopies; i += kSampleT) {
-                lds.bins[i] = 0;
-                lds.count[i] = 0;
-            }
-            __syncthreads();
-        };
-        // values from the largest key down; copies added
-        auto gather = [&](bool masses) {
-            __syncthreads();
-            if (t < 256) {
-                u64 m = 0, c = 0;
-                for (int x = 0; x < kSampleCopies; ++x) {
-                    if (masses) m += lds.bins[(255 - t) * kSampleCopies + x];
-                    c += lds.count[(255 - t) * kSampleCopies + x];
+    u64 cut_count = ~0ull, cut_has = 0, total = 0, front;
+    u64 tie_mass = 0;
+    bool some = false;                                                // (only some of the cut's key stay: they have to be told apart)
+    float from = lowest;
+    const bool plain = !k && !by_mass && !(m_given > 0.f);
+    // masses of the row from `from` on, except for those of `tie_half`: by slab in `slab_sum`, with the number of ties; `max_bins`: each eight's
+    // maximum by its key; `all_bins`: each by its key (or each as one).  The lane's sum is returned.
+    auto masses = [&](unsigned tie_half, bool max_bins, bool all_bins, bool counting) {
+        u64 mine = 0;
+        const float above = tie_half < 0x10000u ? value_of(key_of(tie_half) + 1) : from;
+        each_slab([&](int s, const v4u &v) {
+            u64 sum = 0;
+            unsigned ties = 0;
+            const float m = largest(v);
+            if (__any(m >= from)) {
+                unsigned whole = 0, part = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const unsigned h = half_at(v, e);
+                    float w = mass.scaled(float_of(h));
+                    w = float_of(h) >= above ? w : 0.f;
+                    if (all_bins) {
+                        if (counting) w = w > 0.f ? 1048576.f : 0.f;
+                        if (w > 0.f) atomicAdd(&lds.bins[bin_of(key_of(h))], mass.of(w));
+                    }
+                    whole += mass.whole(w);
+                    part += mass.part(w);
                 }
-                if (masses) lds.mass[t] = m;
-                lds.count64[t] = c;
+                if (tie_half < 0x10000u) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) ties += half_at(v, e) == tie_half ? 1 : 0;
+                }
+                mine += ((u64)whole << 20) + part;
+                sum = ((u64)wave_total(whole) << 20) + wave_total(part);
+                if (tie_half < 0x10000u) ties = wave_total(ties);
+                if (max_bins) {
+                    const u64 w = mass(m);
+                    if (w) atomicAdd(&lds.bins[bin_of(key_of_value(m))], w);
+                }
+            }
+            if (l == 0) slab_sum[s] = sum + ((u64)ties << kTieShift);
+        });
+        return mine;
+    };
+    constexpr unsigned kNoHalf = 0x10000u;
+    for (bool final = plain;; final = true) {
+        // ---- what stays, by slab; the first time (top-p alone) all
+        if (final || (by_mass && !k)) {
+            if (listed) {
+                for (unsigned i = t; i < n_listed; i += kSampleT) {
+                    const unsigned key = lds.list[i] & 0xffffu;
+                    const u64 add = some && key == cut ? 1ull << kTieShift : mass(value_of(key));
+                    if (add && value_of(key) >= from) atomicAdd(&slab_sum[lds.list[i] >> 16], add);
+                }
+            } else {
+                masses(some ? half_of(cut) : kNoHalf, !final, false, false);
             }
             __syncthreads();
-        };
-        // counts of the 256 keys of one bin
-        auto keys_of_bin = [&](unsigned bin) {
-            clear();
-            each([&](unsigned key, int, int) {
-                if (key >> 8 == bin) atomicAdd(&lds.count[(key & 255) * kSampleCopies + (t & (kSampleCopies - 1))], 1u);
+        }
+        if (final) break;
+
+        // ---- the bound
+        u64 target = (u64)k;
+        if (k && k <= kSampleT) {
+            if (mine > -INFINITY) atomicAdd(&lds.bins[bin_of(key_of_value(mine))], 1ull);
+        } else if (by_mass && !k) {
+            u64 two = 0;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (2 * t + i < slabs) {
+                    two += slab_sum[2 * t + i];
+                    slab_sum[2 * t + i] = 0;                          // (what is on the list is added to them)
+                }
+            total = block_scan(two, front);
+            target = min(total, max(1ull, p_given > 0.f ? (u64)ceil((double)p_given * (double)total) : 1ull));
+        }
+        if (by_mass || k) {
+            const int bin = first_bin(target);
+            if (bin > (int)(kKeyMinusInf >> 4)) from = value_of((unsigned)bin << 4);
+        } else {
+            from = min_value;
+        }
+        // ---- what is not below it
+        if (k <= kListed) {
+            bool room = true;
+            each_slab([&](int s, const v4u &v) {
+                unsigned bits = room && largest(v) >= from ? from_bits(v, from) : 0;
+                if (__any(bits != 0)) {
+                    const unsigned n = __builtin_popcount(bits), upto = wave_scan(n), of_all = (unsigned)__builtin_amdgcn_readlane((int)upto, 63);
+                    unsigned first = 0;
+                    if (l == 0) first = atomicAdd(&lds.listed, of_all);
+                    first = (unsigned)__builtin_amdgcn_readfirstlane((int)first);
+                    room = first + of_all <= kListed;
+                    unsigned at = first + upto - n;
+                    for (; room && bits; bits &= bits - 1, ++at) lds.list[at] = key_of(half_at(v, __builtin_ctz(bits))) | (unsigned)s << 16;
+                }
             });
-            gather(false);
-        };
-        clear();
-        each([&](unsigned key, int, int) {
-            if (key > kKeyMinusInf) {
-                const int at = (key >> 8) * kSampleCopies + (t & (kSampleCopies - 1));
-                if (k) atomicAdd(&lds.count[at], 1u);
-                if (by_mass) {
-                    const u64 w = mass(key);
-                    if (w) atomicAdd(&lds.bins[at], w);
-                }
-            }
-        });
-        gather(true);
-        int bin_k = -1;                                               // (places from the top, as gather() leaves them)
-        if (k) {
-            if (wave == 0) {
-                u64 all = 0;
-                for (int i = l; i < 256; i += 64) all += lds.count64[i];
-                all = wave_scan(all);
-                all = (u64)__shfl((long long)all, 63);
-                u64 before = 0;
-                const int at = all >= (u64)k ? first_reaching(lds.count64, 256, (u64)k, before) : -1;
-                if (l == 0) {
-                    lds.found = at;
-                    lds.before = before;
-                }
-            }
             __syncthreads();
-            bin_k = lds.found;
-            if (bin_k >= 0) {
-                const u64 rest = (u64)k - lds.before;
-                keys_of_bin(255 - bin_k);
-                if (wave == 0) {
-                    u64 before;
-                    const int at = first_reaching(lds.count64, 256, rest, before);
-                    if (l == 0) {
-                        lds.cut_key = (unsigned)(255 - bin_k) << 8 | (unsigned)(255 - at);
-                        lds.cut_count = rest - before;
-                    }
-                }
-                __syncthreads();
-                cut = lds.cut_key;
-                cut_count = lds.cut_count;
-            }
+            n_listed = lds.listed;
+            listed = n_listed <= kListed;
         }
-        if (by_mass) {
-            __syncthreads();
-            // the bin of the k-th key holds what stays of it
-            if (bin_k >= 0) {
-                if (wave == 0) {
-                    u64 m = 0;
-                    for (int i = l; i < 256; i += 64) {
-                        const unsigned key = (unsigned)(255 - bin_k) << 8 | (unsigned)(255 - i);
-                        if (key >= cut) m += (key == cut ? cut_count : lds.count64[i]) * mass(key);
+        // ---- the cut, for top-k by counts and then for top-p by masses
+#pragma unroll 1
+        for (int round = k ? 0 : 1; round < (by_mass ? 2 : 1); ++round) {
+            const bool counting = round == 0;
+            u64 kept = 0;
+            if (listed) {
+                for (unsigned i = t; i < n_listed; i += kSampleT) {
+                    const unsigned key = lds.list[i] & 0xffffu;
+                    const u64 w = value_of(key) < from || (cut && key == cut) ? 0 : counting ? 1 : mass(value_of(key));
+                    kept += w;
+                    if (w) atomicAdd(&lds.bins[bin_of(key)], w);
+                }
+            } else {
+                kept = masses(cut ? half_of(cut) : kNoHalf, false, true, counting);
+            }
+            if (!counting && k) {
+                const u64 ties = cut ? cut_count * mass(value_of(cut)) : 0;
+                if (t == 0 && ties) atomicAdd(&lds.bins[bin_of(cut)], ties);
+                total = block_scan(kept, front) + ties;
+                target = min(total, max(1ull, p_given > 0.f ? (u64)ceil((double)p_given * (double)total) : 1ull));
+            }
+            if (counting && !listed) target <<= 40;
+            const int bin = first_bin(target);
+            if (bin < 0) continue;                                    // (fewer tokens than k can be drawn: all of them stay)
+            const u64 rest = counting && !listed ? (target - lds.before) >> 40 : target - lds.before;
+            const float low = bin > (int)(kKeyMinusInf >> 4) ? fmaxf(from, value_of((unsigned)bin << 4)) : from;
+            const unsigned key0 = (unsigned)bin << 4;
+            const float high = value_of(min(key0 + 15u, top_key));
+            if (listed) {
+                for (unsigned i = t; i < n_listed; i += kSampleT) {
+                    const unsigned key = lds.list[i] & 0xffffu;
+                    if (key - key0 < 16u && value_of(key) >= low) atomicAdd(&lds.keys[key & 15], 1ull);
+                }
+            } else {
+                each_slab([&](int, const v4u &v) {
+                    unsigned bits = 0;
+                    if (largest(v) >= low && any_between(v, low, high)) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) bits |= key_of(half_at(v, e)) - key0 < 16u ? 1u << e : 0u;
                     }
-                    m = wave_scan(m);
-                    if (l == 63) lds.mass[bin_k] = m;
-                }
-                if (t > bin_k && t < 256) lds.mass[t] = 0;
-                __syncthreads();
-            }
-            if (wave == 0) {
-                u64 all = 0;
-                for (int i = l; i < 256; i += 64) all += lds.mass[i];
-                all = wave_scan(all);
-                all = (u64)__shfl((long long)all, 63);
-                const double share = p_given > 0.f ? ceil((double)p_given * (double)all) : 1.0;
-                const u64 target = min(all, max(1ull, (u64)share));
-                u64 before;
-                const int at = first_reaching(lds.mass, 256, target, before);
-                if (l == 0) {
-                    lds.found = at;
-                    lds.before = before;
-                    lds.cut_total = target;
-                }
+                    for (; bits; bits &= bits - 1) {
+                        const unsigned h = half_at(v, __builtin_ctz(bits));
+                        if (float_of(h) >= low) atomicAdd(&lds.keys[key_of(h) & 15], 1ull);
+                    }
+                });
             }
             __syncthreads();
-            const int bin = lds.found;
-            const u64 rest = lds.cut_total - lds.before;
-            if (bin != bin_k) keys_of_bin(255 - bin);
-            __syncthreads();
-            if (t < 256) {
-                const unsigned key = (unsigned)(255 - bin) << 8 | (unsigned)(255 - t);
-                lds.mass[t] = key < cut ? 0 : (key == cut && bin == bin_k ? cut_count : lds.count64[t]) * (key > kKeyMinusInf ? mass(key) : 0);
-            }
-            __syncthreads();
-            if (wave == 0) {
-                u64 before;
-                const int at = first_reaching(lds.mass, 256, rest, before);
-                if (l == 0) {
-                    const unsigned key = (unsigned)(255 - bin) << 8 | (unsigned)(255 - at);
-                    const u64 w = max(1ull, mass(key));
-                    lds.cut_key = key;
-                    lds.cut_count = (rest - before + w - 1) / w;
-                }
-            }
-            __syncthreads();
-            cut = lds.cut_key;
-            cut_count = lds.cut_count;
+            // (a lane per key, the largest first)
+            const unsigned key = (unsigned)bin << 4 | (15u - (l & 15));
+            const u64 has = l < 16 && key >= cut ? lds.keys[key & 15] : 0, n = cut && key == cut ? min(has, cut_count) : has;
+            const u64 w = counting ? 1 : mass(value_of(key)), cum = wave_scan(n * w);
+            const int at = __builtin_ctzll(__ballot(n * w > 0 && cum >= rest) | 1ull << 63) & 15;
+            const u64 left = rest - lane_value(cum - n * w, at), each = max(1ull, lane_value(w, at));
+            u64 count = (u64)((double)left / (double)each);
+            if (count * each < left) ++count;
+            cut = (unsigned)__builtin_amdgcn_readlane((int)key, at);
+            cut_count = max(1ull, count);
+            cut_has = lane_value(has, at);
+            from = value_of(cut);
         }
-
+        some = cut && cut_count < cut_has;
+        tie_mass = some && from >= min_value ? mass(from) : 0;
+        from = fmaxf(from, min_value);
     }
 
-    // how many tokens of the cut's key lie before each slab of each wavefront
-    const bool count_ties = cut_count != ~0ull;
-    const int entries = slabs * kSampleWaves;
-    if (count_ties) {
-        auto slab_done = [&](int i, unsigned n) {
-            for (int by = 32; by > 0; by >>= 1) n += (unsigned)__shfl_xor((int)n, by);
-            if (l == 0) lds.ties[i * kSampleWaves + wave] = n;
-        };
+    // ---- the slab of the drawn token: each thread has two
+    u64 of[2], ties[2] = {0, 0}, ties_front = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const u64 both = 2 * t + i < slabs ? slab_sum[2 * t + i] : 0;
+        of[i] = both & ((1ull << kTieShift) - 1);
+        ties[i] = both >> kTieShift;
+    }
+    if (some) {
+        block_scan(ties[0] + ties[1], ties_front);
+        __syncthreads();
+        u64 in_front = ties_front;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (in_front < cut_count) of[i] += min(ties[i], cut_count - in_front) * tie_mass;
+            in_front += ties[i];
+        }
+    }
+    const u64 all = block_scan(of[0] + of[1], front);
+    u64 target = u > 0.f ? (u64)((double)fminf(u, 1.f) * (double)all) : 0;
+    target = min(target, all - 1) + 1;
+    if (front < target && front + of[0] + of[1] >= target) {
+        const int i = front + of[0] < target ? 1 : 0;
+        lds.found = 2 * t + i;
+        lds.before = front + (i ? of[0] : 0);
+        lds.ties_before = (unsigned)(ties_front + (i ? ties[0] : 0));
+    }
+    __syncthreads();
+    if (wave) return;
+    const int s = lds.found;
+    const v4u v = CACHED ? cached[s * 64 + l] : clean(s == last ? lds.last[l] : fetch(s));
+    u64 rank = 0;
+    if (some) {
         unsigned n = 0;
-        each([&](unsigned key, int i, int e) {
-            n = (e == 0 ? 0 : n) + (key == cut ? 1 : 0);
-            if (e == 7) slab_done(i, n);
-        });
-        __syncthreads();
-        if (wave == 0) {
-            const int per = (entries + 63) / 64;
-            u64 mine = 0;
-            for (int i = 0; i < per; ++i)
-                if (l * per + i < entries) mine += lds.ties[l * per + i];
-            u64 cum = wave_scan(mine) - mine;
-            for (int i = 0; i < per; ++i)
-                if (l * per + i < entries) {
-                    const unsigned n_here = lds.ties[l * per + i];
-                    lds.ties[l * per + i] = (unsigned)cum;
-                    cum += n_here;
-                }
-        }
-        __syncthreads();
-    }
-    // masses of what stays, by slab and wavefront
-    unsigned before_ties = 0;
-    auto kept = [&](unsigned key, int i, int e, unsigned own_ties) -> u64 {
-        // own_ties: this lane's tokens of the cut's key in this slab
-        if (e == 0 && count_ties) {
-            u64 n = own_ties;
-            before_ties = lds.ties[i * kSampleWaves + wave] + (unsigned)(wave_scan(n) - n);
-        }
-        if (key < cut || key <= kKeyMinusInf) return 0;
-        if (count_ties && key == cut && (u64)before_ties++ >= cut_count) return 0;
-        const u64 w = mass(key);
-        return w >= least ? w : 0;
-    };
-    auto slab_mass = [&](const v4u &v, int i, u64 (&w)[8]) {
-        unsigned ties = 0;
-        if (count_ties)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) ties += key_of(v[e >> 1] >> (16 * (e & 1)) & 0xffffu) == cut ? 1 : 0;
-        u64 sum = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            w[e] = kept(key_of(v[e >> 1] >> (16 * (e & 1)) & 0xffffu), i, e, ties);
-            sum += w[e];
-        }
-        return sum;
-    };
-    u64 w[8];
-    auto total_of = [&](const v4u &v, int i) {
-        const u64 sum = wave_scan(slab_mass(v, i, w));
-        if (l == 63) lds.table[i * kSampleWaves + wave] = sum;
-    };
-    if constexpr (PIECES > 0) {
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) total_of(held[i], i);
-    } else {
-        for (int i = 0; i < slabs; ++i) total_of(load(i), i);
+        for (int e = 0; e < 8; ++e) n += key_of(half_at(v, e)) == cut ? 1 : 0;
+        rank = lds.ties_before + wave_scan(n) - n;
     }
-    __syncthreads();
-    if (wave == 0) {
-        u64 all = 0;
-        for (int i = l; i < entries; i += 64) all += lds.table[i];
-        all = wave_scan(all);
-        all = (u64)__shfl((long long)all, 63);
-        const float u = a.uniform[b];
-        u64 target = u > 0.f ? (u64)((double)fminf(u, 1.f) * (double)all) : 0;
-        target = min(target, all - 1) + 1;
-        u64 before;
-        const int at = first_reaching(lds.table, entries, target, before);
-        if (l == 0) {
-            lds.found = at;
-            lds.before = target - before;
-            lds.cut_total = all;
-        }
+    u64 w[8], lane_mass = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const unsigned h = half_at(v, e);
+        const bool stays = float_of(h) >= from && !(some && key_of(h) == cut && rank++ >= cut_count);
+        w[e] = stays ? mass(float_of(h)) : 0;
+        lane_mass += w[e];
     }
-    __syncthreads();
-    const int slab = lds.found / kSampleWaves;
-    if (wave != lds.found % kSampleWaves) return;
-    const u64 sum = slab_mass(load(slab), slab, w);
-    const u64 cum = wave_scan(sum), target = lds.before;
-    const u64 reached = __ballot(cum >= target);
-    if (l != __builtin_ctzll(reached)) return;
-    u64 at = cum - sum;
+    const u64 cum = wave_scan(lane_mass), before = lds.before;
+    const u64 reached = __ballot(before + cum >= target);
+    if (reached == 0 || l != __builtin_ctzll(reached)) return;
+    u64 at = before + cum - lane_mass, chosen = 0;
     int e = 0;
-    for (; e < 7 && at + w[e] < target; ++e) at += w[e];
-    u64 chosen = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) chosen = i == e ? w[i] : chosen;
-    a.token[b] = (slab * kSampleT + t) * 8 + e;
-    if (a.prob) a.prob[b] = (float)((double)chosen / (double)lds.cut_total);
+    for (int x = 0; x < 8; ++x)
+        if (e == x) {
+            chosen = w[x];
+            if (x < 7 && at + w[x] < target) at += w[x], ++e;
+        }
+    a.token[b] = s * kSlab + l * 8 + e;
+    if (a.prob) a.prob[b] = (float)((double)chosen / (double)all);
 }
 
 sqap_status launch_sample(const __half *logits, int64_t ld, int batch, int vocab, const float *temperature, const int32_t *top_k,
                           const float *top_p, const float *min_p, const float *uniform, int32_t *token, float *prob, hipStream_t st)
 {
-    const SampleArgs a = {logits, ld, vocab, temperature, top_p, min_p, uniform, top_k, token, prob};
+    const int slabs = (vocab + kSlab - 1) / kSlab;
+    const SampleArgs a = {logits, ld, vocab, slabs, temperature, top_p, min_p, uniform, top_k, token, prob};
+    const bool cached = vocab <= kSampleCached;
+    const size_t lds = sizeof(SampleLds) + (size_t)slabs * sizeof(u64) + (cached ? (size_t)slabs * kSlab * 2 : 0);
     static std::atomic<bool> ready[kMaxDeviceSlots];
-    const int pieces = (vocab + 8 * kSampleT - 1) / (8 * kSampleT);
     if (!ready[device_slot()].load(std::memory_order_relaxed)) {
-        for (const void *f : {reinterpret_cast<const void *>(sample_kernel<1>), reinterpret_cast<const void *>(sample_kernel<4>), reinterpret_cast<const void *>(sample_kernel<0>)})
-            SQAP_HIP_CHECK(hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, sizeof(SampleLds)));
+        const int most = sizeof(SampleLds) + kSampleCached * 2 + kSampleMaxVocab / kSlab * (int)sizeof(u64);
+        SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(sample_kernel<true>), hipFuncAttributeMaxDynamicSharedMemorySize, most));
+        SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(sample_kernel<false>), hipFuncAttributeMaxDynamicSharedMemorySize, most));
         ready[device_slot()].store(true, std::memory_order_relaxed);
     }
     const dim3 grid(batch), block(kSampleT);
-    if (pieces <= 1) hipLaunchKernelGGL(sample_kernel<1>, grid, block, sizeof(SampleLds), st, a);
-    else if (pieces <= 4) hipLaunchKernelGGL(sample_kernel<4>, grid, block, sizeof(SampleLds), st, a);
-    else hipLaunchKernelGGL(sample_kernel<0>, grid, block, sizeof(SampleLds), st, a);
+    if (cached) hipLaunchKernelGGL(sample_kernel<true>, grid, block, lds, st, a);
+    else hipLaunchKernelGGL(sample_kernel<false>, grid, block, lds, st, a);
     SQAP_HIP_CHECK(hipGetLastError());
     return SQAP_OK;
 }
