@@ -16,6 +16,11 @@ published pre-normalisation layer:
     h = silu(g) * u -> int4                  sqap_swiglu_quantize_act
     d = W_down h                             sqap_w4a4_linear
 The last residual add (x + d) is left pending and fused into the next layer's first call.
+
+The same layer in microscaled 4-bit floating point, where its four weights are Mx4Weight: the norms and the product of gate and up
+leave halves, which sqap_mx4_quantize takes, and sqap_mx4_linear multiplies.  With a Cache8 in the place of the fp16 cache
+the call is about a batch of sequences, each with a length of its own: prompts through sqap_cache8_append and sqap_cache8_attention, one new
+row per sequence through sqap_cache8_decode_attention.  Either goes with the other's counterpart.
 """
 import torch
 
@@ -35,29 +40,54 @@ class LayerWeights:
 
 
 class LayerBuffers:
-    """Scratch tensors for up to max_rows token rows of one layer call (reused by every layer)."""
+    """Scratch tensors for up to max_rows token rows of one layer call (reused by every layer).
 
-    def __init__(self, max_rows, hidden, ffn, device="cuda"):
+    kv_width: width of the keys (of the values), where heads of a Cache8 are shared; mx4: for layers of Mx4Weight;
+    cache8_workspace: bytes of sqap_cache8_workspace_bytes for the decode calls over a Cache8."""
+
+    def __init__(self, max_rows, hidden, ffn, device="cuda", kv_width=None, mx4=False, cache8_workspace=0):
         f16, u8 = torch.float16, torch.uint8
+        kv_width = hidden if kv_width is None else kv_width
         self.hidden, self.ffn = hidden, ffn
         self.xq = torch.empty((max_rows, hidden // 2), dtype=u8, device=device)
         self.sx = torch.empty((max_rows,), dtype=f16, device=device)
-        self.qkv = torch.empty((max_rows, 3 * hidden), dtype=f16, device=device)
+        self.qkv = torch.empty((max_rows, hidden + 2 * kv_width), dtype=f16, device=device)
+        self.q = torch.empty((max_rows, hidden), dtype=f16, device=device)      # rotated queries of prompts over a Cache8
         self.attn = torch.empty((max_rows, hidden), dtype=f16, device=device)
         self.o = torch.empty((max_rows, hidden), dtype=f16, device=device)
         self.gu = torch.empty((max_rows, 2 * ffn), dtype=f16, device=device)
         self.hq = torch.empty((max_rows, ffn // 2), dtype=u8, device=device)
         self.sh = torch.empty((max_rows,), dtype=f16, device=device)
+        self.cache8_ws = torch.zeros((cache8_workspace,), dtype=u8, device=device)
+        if mx4:
+            self.y = torch.empty((max_rows, hidden), dtype=f16, device=device)
+            self.h = torch.empty((max_rows, ffn), dtype=f16, device=device)
+            self.xs = torch.empty((max_rows, hidden // 32), dtype=u8, device=device)
+            self.hs = torch.empty((max_rows, ffn // 32), dtype=u8, device=device)
         # the workspace a linear needs is not monotonic in M (the tile shape changes with M): take the largest
-        nbytes = max(B.sqap_workspace_bytes(m, n, k) for m in range(1, max_rows + 1)
-                     for (n, k) in ((3 * hidden, hidden), (hidden, hidden), (2 * ffn, hidden), (hidden, ffn)))
+        nbytes = 0 if mx4 else max(B.sqap_workspace_bytes(m, n, k) for m in range(1, max_rows + 1)
+                                   for (n, k) in ((hidden + 2 * kv_width, hidden), (hidden, hidden), (2 * ffn, hidden), (hidden, ffn)))
         self.ws = torch.zeros((max(nbytes, 256),), dtype=u8, device=device)
         self.iota = torch.arange(max_rows, dtype=torch.int32, device=device)
         self.counter = torch.zeros((1,), dtype=torch.int32, device=device)     # arrival counter of sqap_decode_attention
 
 
+def _cache8_attention(buf, qkv, attn, pos, batch, n_heads, kv, past, starts, max_new, longest, stream):
+    """Append and attention over a Cache8: prompts where `starts` is given, otherwise one new row per sequence."""
+    if kv.batch != batch:
+        raise ValueError("the cache is for %d sequences, not %d" % (kv.batch, batch))
+    if starts is not None:
+        q = buf.q[:pos.numel()]
+        B.sqap_cache8_append(qkv, starts, pos, past, kv, n_heads, max_new, Q_out=q, stream=stream)
+        B.sqap_cache8_attention(q, starts, past, kv, n_heads, max_new, attn, stream=stream)
+    else:
+        if pos.numel() != batch:
+            raise ValueError("one new row per sequence, or `starts`")
+        B.sqap_cache8_decode_attention(qkv, pos, past, kv, n_heads, attn, buf.cache8_ws, longest, stream=stream)
+
+
 def layer_forward(w, buf, x, pending, pos, batch, n_heads, head_dim, x_out, d_out, eps=1e-5, rows=None,
-                  rotate=False, kv=None, past=0, stream=None, fold_quantizer=False):
+                  rotate=False, kv=None, past=0, stream=None, fold_quantizer=False, starts=None, max_new=0, longest=0):
     """Runs one layer on M token rows (batch sequences of M / batch tokens each).
 
     x: residual stream [*, hidden] fp16 (rows picks the M rows when given: the token gather is fused);
@@ -67,17 +97,30 @@ def layer_forward(w, buf, x, pending, pos, batch, n_heads, head_dim, x_out, d_ou
     kv: this layer's key/value cache of ONE sequence, [capacity, 2 * hidden] fp16 (rotated key | value per
     position), holding `past` positions: the M new rows are appended and attention runs over past + M
     keys (prefill fills the cache with past = 0; a decode step has M = 1).  Needs batch == 1.
+    Or kv: a Cache8 of `batch` sequences; past: [batch] int32 on the device; starts: [batch + 1] int32 on the device, the sequences'
+    first rows, of at most max_new rows each, or None for one row per sequence, whose lengths afterwards are at most `longest`.
     """
     M = pos.numel()
     hidden = buf.hidden
+    mx4, cache8 = isinstance(w.qkv, B.Mx4Weight), isinstance(kv, B.Cache8)
+    if (rotate and mx4) or (fold_quantizer and (mx4 or cache8)):
+        raise ValueError("neither rotate nor fold_quantizer goes with weights in microscaled floating point, nor the latter with a Cache8")
     flags = B.ROTATE_HADAMARD if rotate else 0
     xq, sx, qkv, attn, o = buf.xq[:M], buf.sx[:M], buf.qkv[:M], buf.attn[:M], buf.o[:M]
     gu, hq, sh = buf.gu[:M], buf.hq[:M], buf.sh[:M]
-    B.sqap_rmsnorm_quantize_act(x, rows, w.gamma_attn, eps, xq, sx, delta=pending, flags=flags, xsum_out=x_out,
-                                stream=stream)
-    B.sqap_w4a4_linear(xq, sx, w.qkv, qkv, None, buf.ws, stream=stream)
-    one_launch = kv is not None and M == 1 and head_dim % 8 == 0 and head_dim <= 128 and hidden <= 8192
-    if kv is None:
+    if mx4:
+        y, xs, h, hs = buf.y[:M], buf.xs[:M], buf.h[:M], buf.hs[:M]
+        B.sqap_rmsnorm_quantize_act(x, rows, w.gamma_attn, eps, None, None, delta=pending, xsum_out=x_out, y_out=y, stream=stream)
+        B.sqap_mx4_quantize(y, None, xq, xs, stream=stream)
+        B.sqap_mx4_linear(xq, xs, w.qkv, qkv, stream=stream)
+    else:
+        B.sqap_rmsnorm_quantize_act(x, rows, w.gamma_attn, eps, xq, sx, delta=pending, flags=flags, xsum_out=x_out,
+                                    stream=stream)
+        B.sqap_w4a4_linear(xq, sx, w.qkv, qkv, None, buf.ws, stream=stream)
+    one_launch = kv is not None and not cache8 and M == 1 and head_dim % 8 == 0 and head_dim <= 128 and hidden <= 8192
+    if cache8:
+        _cache8_attention(buf, qkv, attn, pos, batch, n_heads, kv, past, starts, max_new, longest, stream)
+    elif kv is None:
         B.sqap_rope(qkv[:, :2 * hidden], pos, 2 * n_heads, head_dim, stream=stream)  # queries and keys in one launch
         B.sqap_attention(qkv[:, :hidden], qkv[:, hidden:2 * hidden], qkv[:, 2 * hidden:], n_heads, head_dim, attn,
                          batch=batch, stream=stream)
@@ -98,6 +141,16 @@ def layer_forward(w, buf, x, pending, pos, batch, n_heads, head_dim, x_out, d_ou
             B.sqap_rope_append(qkv, pos, n_heads, head_dim, kv[past:past + M], stream=stream)
             B.sqap_attention(qkv[:, :hidden], kv[:past + M, :hidden], kv[:past + M, hidden:], n_heads, head_dim, attn,
                              stream=stream)
+    if mx4:
+        B.sqap_mx4_quantize(attn, None, xq, xs, stream=stream)
+        B.sqap_mx4_linear(xq, xs, w.o, o, stream=stream)
+        B.sqap_rmsnorm_quantize_act(x_out, None, w.gamma_mlp, eps, None, None, delta=o, xsum_out=x_out, y_out=y, stream=stream)
+        B.sqap_mx4_quantize(y, None, xq, xs, stream=stream)
+        B.sqap_mx4_linear(xq, xs, w.gate_up, gu, stream=stream)
+        B.sqap_swiglu_quantize_act(gu[:, :buf.ffn], gu[:, buf.ffn:], None, None, h_out=h, stream=stream)
+        B.sqap_mx4_quantize(h, None, hq, hs, stream=stream)
+        B.sqap_mx4_linear(hq, hs, w.down, d_out, stream=stream)
+        return
     if not (one_launch and fold_quantizer):
         B.sqap_quantize_act(attn, None, xq, sx, stream=stream)
     B.sqap_w4a4_linear(xq, sx, w.o, o, None, buf.ws, stream=stream)
