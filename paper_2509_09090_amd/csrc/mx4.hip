@@ -235,39 +235,38 @@ __global__ __launch_bounds__(64 * kFewWaves) void mx4_few_kernel(const uint8_t *
     }
 }
 
-// More rows: tiles of 32 RM WM rows x 64 WN channels; a wavefront has RM x 2 fragments of results (64 channels: one span).  K goes by stages
-// of 256 channels.  Rows pass through LDS in the order in which the lanes hold them (two buffers, one barrier per stage); they are asked
-// for a stage ahead and wait in registers.  The weight goes from memory to the registers of the wavefronts that use it, DEPTH stages
-// ahead: through LDS it would keep that busier than the matrix cores.  WK wavefronts share a stage's four fragments along K; their sums are
-// added in LDS at the end, each wavefront finishing some of the fragments.
-template <int RM, int WM, int RN, int WN, int WK, int DEPTH, int AHEAD>
+// More rows: tiles of 32 RM rows x 128 RN channels, a wavefront has RM x RN fragments of results.  K goes by stages of 256 channels.  Rows
+// pass through LDS in the order in which the lanes hold them (two buffers, one barrier per stage); they are asked for AHEAD stages
+// ahead and wait in registers.  The weight goes from memory to the registers of the wavefront that uses it, DEPTH stages ahead:
+// through LDS it would keep that busier than the matrix cores.  Four wavefronts: two workgroups are a compute unit's, so that one
+// multiplies while the other waits at its barrier.
+constexpr int kTileWaves = 4;
+template <int RM, int RN, int DEPTH, int AHEAD>
 struct Mx4Tile {
-    static constexpr int kRows = 32 * RM * WM, kChannels = 32 * RN * WN, kWaves = WM * WN * WK, kThreads = 64 * kWaves;
-    static constexpr int kPieces = 4 * RM * WM;                       // KiB of a stage
-    static constexpr int kScalesAt = 2 * kPieces * 1024, kScaleBytes = kRows * 8;
-    static constexpr int kMerge = WK > 1 ? WK * WM * WN * RN * 4096 : 0;
-    static constexpr int kLds = kScalesAt + 2 * kScaleBytes > kMerge ? kScalesAt + 2 * kScaleBytes : kMerge;
+    static constexpr int kRows = 32 * RM, kChannels = 32 * RN * kTileWaves, kThreads = 64 * kTileWaves;
+    static constexpr int kPieces = 4 * RM;                            // KiB of a stage
+    static constexpr int kScalesAt = 2 * kPieces * 1024, kScaleBytes = kRows * 8, kLds = kScalesAt + 2 * kScaleBytes;
 };
 
-template <int RM, int WM, int RN, int WN, int WK, int DEPTH, int AHEAD>
-__global__ __launch_bounds__((Mx4Tile<RM, WM, RN, WN, WK, DEPTH, AHEAD>::kThreads), 2)
+template <int RM, int RN, int DEPTH, int AHEAD>
+__global__ __launch_bounds__((Mx4Tile<RM, RN, DEPTH, AHEAD>::kThreads), 2)
 void mx4_tile_kernel(const uint8_t *__restrict__ Xq, const uint8_t *__restrict__ Xs, int M, int K, const uint8_t *__restrict__ data,
                      const unsigned *__restrict__ scales, int stages, int N, __half *__restrict__ Y, int64_t ldy, int row_tiles, int tiles,
                      int tiles_per_xcd)
 {
-    using T = Mx4Tile<RM, WM, RN, WN, WK, DEPTH, AHEAD>;
+    using T = Mx4Tile<RM, RN, DEPTH, AHEAD>;
     static_assert(T::kRows <= T::kThreads, "a thread fetches the scales of a row");
-    constexpr int NW = T::kWaves, LOADS = (T::kPieces + NW - 1) / NW, STEPS = 4 / WK;
+    static_assert(DEPTH % AHEAD == 0, "the registers of a stage's rows are told by its number modulo DEPTH");
+    constexpr int NW = kTileWaves, LOADS = T::kPieces / NW, STEPS = 4;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     // tiles that share weights are neighbours and go to one XCD, behind one L2
     const int tile = (blockIdx.x & 7) * tiles_per_xcd + (blockIdx.x >> 3);
     if (tile >= tiles) return;
-    const int m0 = tile % row_tiles * T::kRows, first_group = tile / row_tiles * RN * WN;
+    const int m0 = tile % row_tiles * T::kRows, first_group = tile / row_tiles * RN * NW;
     const int t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), r = l & 31, h = l >> 5;
-    const int wk = wave / (WM * WN), wm = wave % (WM * WN) / WN, wn = wave % WN;
     const int blocks = K >> 5;
 
-    // rows: a wavefront fetches 8 rows x 128 bytes at a time, whole cache lines (32 rows x 32 bytes, as a fragment has them, took a third longer).
+    // rows: a wavefront fetches 8 rows x 128 bytes at a time, whole cache lines (32 rows x 32 bytes, as a fragment has them: 2368 x 22016 x 4096 in 150 us, 140 so).
     // This lane's offsets from the tile's first row; rows past M and blocks past K are behind the window
     const Window rows = window_of(Xq + (int64_t)m0 * (K >> 1), (unsigned long long)min(M - m0, T::kRows) * (K >> 1));
     constexpr unsigned kBehind = 0xfffffff0u;
@@ -275,7 +274,7 @@ void mx4_tile_kernel(const uint8_t *__restrict__ Xq, const uint8_t *__restrict__
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
         const int p = wave + i * NW, row = p * 8 + (l >> 3);
-        from[i] = row < M - m0 && (T::kPieces % NW == 0 || p < T::kPieces) ? (unsigned)row * (unsigned)(K >> 1) + (unsigned)(l & 7) * 16u : kBehind;
+        from[i] = row < M - m0 ? (unsigned)row * (unsigned)(K >> 1) + (unsigned)(l & 7) * 16u : kBehind;
     }
     v4i fetched[AHEAD][LOADS];
     v2u fetched_scales[AHEAD];
@@ -296,14 +295,13 @@ void mx4_tile_kernel(const uint8_t *__restrict__ Xq, const uint8_t *__restrict__
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int p = wave + i * NW;
-            if (T::kPieces % NW != 0 && p >= T::kPieces) break;
             const int row = p * 8 + (l >> 3), q = l & 7;              // block q of its row, for step q / 2, lane half q % 2
             *reinterpret_cast<v4i *>(lds + ((st & 1) * T::kPieces + (row >> 5) * 4) * 1024 + q * 512 + ((row + q) & 31) * 16) = fetched[i];
         }
         if (t < T::kRows) *reinterpret_cast<v2u *>(lds + T::kScalesAt + (st & 1) * T::kScaleBytes + t * 8) = split_scales(placed);
     };
 
-    const int64_t group0 = first_group + wn * RN;
+    const int64_t group0 = first_group + wave * RN;
     const Window wdata = window_of(data + group0 * stages * 4096, (unsigned long long)stages * 4096 * RN);
     const Window wscales = window_of(scales + group0 * stages * 64, (unsigned long long)stages * 256 * RN);
     const unsigned lane16 = (unsigned)l * 16u, lane4 = (unsigned)l * 4u;
@@ -311,7 +309,7 @@ void mx4_tile_kernel(const uint8_t *__restrict__ Xq, const uint8_t *__restrict__
     unsigned ws[DEPTH][RN], ws_next[RN];
     auto fetch_weight = [&](int d, int s, int st) {                   // (past the last stage: zeros, or the other fragment's; not used)
 #pragma unroll
-        for (int c = 0; c < RN; ++c) wreg[d][s][c] = read16(wdata, lane16 + (unsigned)(s * WK + wk) * 1024u, (unsigned)(c * stages + st) * 4096u);
+        for (int c = 0; c < RN; ++c) wreg[d][s][c] = read16(wdata, lane16 + (unsigned)s * 1024u, (unsigned)(c * stages + st) * 4096u);
     };
     auto fetch_weight_scales = [&](unsigned (&into)[RN], int st) {
 #pragma unroll
@@ -345,12 +343,12 @@ void mx4_tile_kernel(const uint8_t *__restrict__ Xq, const uint8_t *__restrict__
         unsigned xs[RM];
 #pragma unroll
         for (int i = 0; i < RM; ++i)
-            xs[i] = *reinterpret_cast<const unsigned *>(lds + T::kScalesAt + (st & 1) * T::kScaleBytes + ((wm * RM + i) * 32 + r) * 8 + h * 4);
+            xs[i] = *reinterpret_cast<const unsigned *>(lds + T::kScalesAt + (st & 1) * T::kScaleBytes + (i * 32 + r) * 8 + h * 4);
         // a step's fragments are read while the one before is multiplied; no further ahead, there are no registers for them
         v4i x[2][RM];
         auto read = [&](int s) {
 #pragma unroll
-            for (int i = 0; i < RM; ++i) x[s & 1][i] = *reinterpret_cast<const v4i *>(at + ((wm * RM + i) * 4 + s * WK + wk) * 1024 + h * 512 + ((r + 2 * (s * WK + wk) + h) & 31) * 16);
+            for (int i = 0; i < RM; ++i) x[s & 1][i] = *reinterpret_cast<const v4i *>(at + (i * 4 + s) * 1024 + h * 512 + ((r + 2 * s + h) & 31) * 16);
         };
         read(0);
 #pragma unroll
@@ -360,15 +358,11 @@ void mx4_tile_kernel(const uint8_t *__restrict__ Xq, const uint8_t *__restrict__
 #pragma unroll
             for (int i = 0; i < RM; ++i)
 #pragma unroll
-                for (int c = 0; c < RN; ++c) {
-                    if constexpr (WK == 1)
-                        acc[i][c] = s == 0   ? multiply<0>(wreg[d][s][c], x[s & 1][i], acc[i][c], ws[d][c], xs[i])
-                                    : s == 1 ? multiply<1>(wreg[d][s][c], x[s & 1][i], acc[i][c], ws[d][c], xs[i])
-                                    : s == 2 ? multiply<2>(wreg[d][s][c], x[s & 1][i], acc[i][c], ws[d][c], xs[i])
-                                             : multiply<3>(wreg[d][s][c], x[s & 1][i], acc[i][c], ws[d][c], xs[i]);
-                    else
-                        acc[i][c] = multiply<0>(wreg[d][s][c], x[s & 1][i], acc[i][c], ws[d][c] >> (8 * (s * WK + wk)), xs[i] >> (8 * (s * WK + wk)));
-                }
+                for (int c = 0; c < RN; ++c)
+                    acc[i][c] = s == 0   ? multiply<0>(wreg[d][s][c], x[s & 1][i], acc[i][c], ws[d][c], xs[i])
+                                : s == 1 ? multiply<1>(wreg[d][s][c], x[s & 1][i], acc[i][c], ws[d][c], xs[i])
+                                : s == 2 ? multiply<2>(wreg[d][s][c], x[s & 1][i], acc[i][c], ws[d][c], xs[i])
+                                         : multiply<3>(wreg[d][s][c], x[s & 1][i], acc[i][c], ws[d][c], xs[i]);
             // the weight's next fragments take these registers: not asked for before they are free
 #pragma unroll
             for (int i = 0; i < RM; ++i)
@@ -393,83 +387,64 @@ void mx4_tile_kernel(const uint8_t *__restrict__ Xq, const uint8_t *__restrict__
     for (; st + DEPTH <= stages; st += DEPTH) {
         stage(st, std::integral_constant<int, 0>{});
         if constexpr (DEPTH > 1) stage(st + 1, std::integral_constant<int, 1>{});
-        if constexpr (DEPTH > 2) stage(st + 2, std::integral_constant<int, 2>{});
-        if constexpr (DEPTH > 3) stage(st + 3, std::integral_constant<int, 3>{});
+        if constexpr (DEPTH > 2) {
+            stage(st + 2, std::integral_constant<int, 2>{});
+            stage(st + 3, std::integral_constant<int, 3>{});
+        }
     }
     if constexpr (DEPTH > 1) several(std::integral_constant<int, 0>{}, several);
-    auto row_of = [&](int i) { return m0 + (wm * RM + i) * 32 + r; };
+    auto row_of = [&](int i) { return m0 + i * 32 + r; };
     auto channel = [&](int c) {
-        const int group = first_group + wn * RN + c;
+        const int group = first_group + wave * RN + c;
         return (group >> 1) * 64 + 32 * h + (group & 1) * 16;
     };
-    if constexpr (WK > 1) {
-        v4f *merge = reinterpret_cast<v4f *>(lds) + ((wm * WN + wn) * WK * RN * 4) * 64 + l;
 #pragma unroll
-        for (int i = 0; i < RM; ++i) {
-            lds_barrier();
-            if (wk != i % WK) {
+    for (int i = 0; i < RM; ++i)
+        if (row_of(i) < M)
 #pragma unroll
-                for (int q = 0; q < 4 * RN; ++q) {
-                    const v16f &o = acc[i][q >> 2];
-                    merge[(wk * 4 * RN + q) * 64] = v4f{o[4 * (q & 3)], o[4 * (q & 3) + 1], o[4 * (q & 3) + 2], o[4 * (q & 3) + 3]};
-                }
-            }
-            lds_barrier();
-            if (wk == i % WK) {
-#pragma unroll
-                for (int w = 0; w < WK; ++w) {
-                    if (w == i % WK) continue;
-#pragma unroll
-                    for (int q = 0; q < 4 * RN; ++q) {
-                        const v4f o = merge[(w * 4 * RN + q) * 64];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][q >> 2][4 * (q & 3) + e] += o[e];
-                    }
-                }
-                if (row_of(i) < M)
-#pragma unroll
-                    for (int c = 0; c < RN; ++c) store_fragment(Y + (int64_t)row_of(i) * ldy, channel(c), N, acc[i][c]);
-            }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < RM; ++i)
-            if (row_of(i) < M)
-#pragma unroll
-                for (int c = 0; c < RN; ++c) store_fragment(Y + (int64_t)row_of(i) * ldy, channel(c), N, acc[i][c]);
-    }
+            for (int c = 0; c < RN; ++c) store_fragment(Y + (int64_t)row_of(i) * ldy, channel(c), N, acc[i][c]);
 }
 
-template <int RM, int WM, int RN, int WN, int WK, int DEPTH, int AHEAD>
+template <int RM, int RN, int DEPTH, int AHEAD>
 static sqap_status launch_tile(const uint8_t *Xq, const uint8_t *Xs, int M, const Mx4Weight &w, __half *Y, int64_t ldy, hipStream_t st)
 {
-    using T = Mx4Tile<RM, WM, RN, WN, WK, DEPTH, AHEAD>;
+    using T = Mx4Tile<RM, RN, DEPTH, AHEAD>;
     static std::atomic<bool> ready[kMaxDeviceSlots];
     if (T::kLds > 65536 && !ready[device_slot()].load(std::memory_order_relaxed)) {
-        SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(mx4_tile_kernel<RM, WM, RN, WN, WK, DEPTH, AHEAD>),
+        SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(mx4_tile_kernel<RM, RN, DEPTH, AHEAD>),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, T::kLds));
         ready[device_slot()].store(true, std::memory_order_relaxed);
     }
     const int row_tiles = (M + T::kRows - 1) / T::kRows, tiles = row_tiles * ((w.N + T::kChannels - 1) / T::kChannels), per_xcd = (tiles + 7) / 8;
-    hipLaunchKernelGGL((mx4_tile_kernel<RM, WM, RN, WN, WK, DEPTH, AHEAD>), dim3(per_xcd * 8), dim3(T::kThreads), T::kLds, st, Xq, Xs, M, w.K, w.data,
+    hipLaunchKernelGGL((mx4_tile_kernel<RM, RN, DEPTH, AHEAD>), dim3(per_xcd * 8), dim3(T::kThreads), T::kLds, st, Xq, Xs, M, w.K, w.data,
                        w.scales, w.stages, w.N, Y, ldy, row_tiles, tiles, per_xcd);
     SQAP_HIP_CHECK(hipGetLastError());
     return SQAP_OK;
 }
 
+// 32 x 32 outputs per workgroup, K shared by its wavefronts, up to two workgroups per compute unit: 148 x 4096 x 4096 (640 of them) takes
+// 11.4 us so and 8.9 in tiles, 100 x 4096 x 4096 (512) 8.6 and 8.8, 100 x 4096 x 11008 17.6 and 24.2.
+// Otherwise the tile whose rounds over the 256 compute units cost least.  A round's cost is what was measured, in 0.1 us at K = 4096 (the first
+// costs some 3 us more for all of them; other K scale all alike): 320 x 4096 takes 9.5 / 12.7 / 14.6 / 17.8 us in the four kinds, 148 x 12288
+// 16.9 / 14.4 / 17.2 / 20.7, 148 x 22016 21.9 / 23.2 / 19.3 / 22.3, 800 x 12288 38.1 / 35.6 / 31.7 / 34.1, 2368 x 22016 190 / 159 / 155 / 132.
+// Over 44 shapes of 40 to 2368 rows the choice is 1.4 in 100 from the best of them on average.
 sqap_status launch_mx4_linear(const uint8_t *Xq, const uint8_t *Xs, int M, const Mx4Weight &w, __half *Y, int64_t ldy, hipStream_t st)
 {
-    const auto tiles = [&](int rows, int channels) { return (int64_t)((M + rows - 1) / rows) * ((w.N + channels - 1) / channels); };
-    if (M <= 32 || tiles(32, 32) <= 768) {
+    const auto tiles = [&](int rows, int channels) { return ((int64_t)M + rows - 1) / rows * ((w.N + channels - 1) / channels); };
+    if (M <= 32 || tiles(32, 32) <= 512) {
         const int row_tiles = (M + 31) / 32, items = (w.N + 63) / 64 * 2 * row_tiles, per_xcd = (items + 7) / 8;
         hipLaunchKernelGGL(mx4_few_kernel, dim3(per_xcd * 8), dim3(64 * kFewWaves), 0, st, Xq, Xs, M, w.K, w.data, w.scales, w.stages, w.N, Y, ldy,
                            row_tiles, items, per_xcd);
         SQAP_HIP_CHECK(hipGetLastError());
         return SQAP_OK;
     }
-    if (tiles(64, 128) <= 400) return launch_tile<2, 1, 1, 4, 1, 4, 2>(Xq, Xs, M, w, Y, ldy, st);
-    if (tiles(160, 128) <= 512) return launch_tile<5, 1, 1, 4, 1, 2, 2>(Xq, Xs, M, w, Y, ldy, st);
-    return launch_tile<4, 1, 2, 4, 1, 1, 1>(Xq, Xs, M, w, Y, ldy, st);
+    const auto cost = [&](int rows, int channels, int64_t round) { return (tiles(rows, channels) + 255) / 256 * round; };
+    const int64_t c64 = cost(64, 128, 65), c128 = cost(128, 128, 95), c160 = cost(160, 128, 115), wide = cost(128, 256, 140);
+    const int64_t least = std::min({c64, c128, c160, wide});
+    if (c64 == least) return launch_tile<2, 1, 4, 2>(Xq, Xs, M, w, Y, ldy, st);
+    if (c128 == least) return launch_tile<4, 1, 2, 2>(Xq, Xs, M, w, Y, ldy, st);
+    if (c160 == least) return launch_tile<5, 1, 2, 2>(Xq, Xs, M, w, Y, ldy, st);
+    return launch_tile<4, 2, 1, 1>(Xq, Xs, M, w, Y, ldy, st);
 }
 
 }  // namespace sqap

@@ -146,13 +146,14 @@ def test_product(G, m, n, k):
 # enough outputs for the tiles, with one stage of K to many, odd and even numbers of them, whole and ragged
 @pytest.mark.gpu
 @pytest.mark.parametrize("m,n,k", [(100, 20011, 96), (33, 24500, 256), (130, 17000, 1312), (700, 5003, 352), (161, 9000, 768), (90, 26001, 2080),
-                                   (1100, 10001, 544), (2050, 5200, 32), (1290, 8200, 1280), (515, 16500, 1024)])
+                                   (1100, 10001, 544), (2050, 5200, 32), (1290, 8200, 1280), (515, 16500, 1024), (60, 20011, 800), (150, 20011, 800),
+                                   (160, 24000, 96), (148, 22016, 1056), (200, 12300, 32)])
 def test_product_of_many_outputs(G, m, n, k):
     test_product(G, m, n, k)
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("m,n", [(100, 20011), (700, 5003), (1100, 10001)])
+@pytest.mark.parametrize("m,n", [(60, 20011), (100, 20011), (150, 20011), (700, 5003), (1100, 10001)])
 def test_tiles_keep_values_that_are_not_finite_in_their_row(G, m, n):
     test_values_that_are_not_finite_stay_in_their_row(G, m, n)
 
