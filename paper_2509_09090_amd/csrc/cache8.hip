@@ -91,7 +91,7 @@ __device__ __forceinline__ void rotate_pair(__half lo, __half hi, double cs, dou
 // Sine and cosine of an angle of at most some 2^31, in binary64: the nearest multiple of pi / 2 is taken off in two parts of 53 bits (each
 // product exact inside its multiply-add), what is left is at most pi / 4, where the Taylor series to the 15th and 16th power are off by
 // less than half a unit of the last place of the larger one.  Without branches, so that a thread's pairs run side by side: a quarter of the
-// instructions of the library's, which also serves angles beyond (148 rows of 32 heads: 20.3 us with that, 6.9 so).
+// instructions of the library's, which also serves angles beyond.
 __constant__ const double kSeries[15] = {-1.0 / 1307674368000.0, 1.0 / 20922789888000.0, 1.0 / 6227020800.0, -1.0 / 87178291200.0, -1.0 / 39916800.0,
                                          1.0 / 479001600.0, 1.0 / 362880.0, -1.0 / 3628800.0, -1.0 / 5040.0, 1.0 / 40320.0, 1.0 / 120.0,
                                          -1.0 / 720.0, -1.0 / 6.0, 1.0 / 24.0, -0.5};
@@ -138,7 +138,7 @@ __device__ __forceinline__ int value_at(int s) { return ((s >> 2) & 3) << 4 | (s
 __device__ __forceinline__ int value_byte(int x, int at) { return x * 64 + ((at >> 4) + (x >> 3) & 3) * 16 + (at & 15); }
 __device__ __forceinline__ int value_piece(int u) { const int x = (u >> 6) * 16 + (u & 15); return x * 64 + (((u >> 4) & 3) + (x >> 3) & 3) * 16; }
 
-constexpr int kAppendGroups = 512, kAppendSplit = 256;
+constexpr int kAppendGroups = 512, kAppendSplit = 96;
 // One workgroup per sequence, `share` key heads and block that the new rows touch (the first and the last of them together: the one reads
 // the tail that the other writes).  The block's angles are evaluated once, into LDS.  Then, head by head: keys, D / 16 threads per position with 8
 // pairs of columns (i, i + D / 2) each; the same threads turn the query heads that share the key head, and take the value row, whose codes
@@ -162,9 +162,9 @@ __global__ __launch_bounds__(4 * D, 2) void cache8_append_kernel(const __half *_
     const int groups = (cache.kv_heads + share - 1) / share, group = blockIdx.y % groups, does = split ? 1 << (blockIdx.y / groups) : 7;
     const int head0 = group * share, heads = min(share, cache.kv_heads - head0);
     int block = first + (int)blockIdx.x;
-    const bool joined = sp.past % kBlock != 0 && last > first;        // the tail is read by the first block and written by the last
-    if (block > last || (joined && blockIdx.x > 0 && block == last)) return;
     const bool keys = does & 1, values = does & 2, queries = Q_out && (does & 4);
+    const bool joined = (keys || values) && sp.past % kBlock != 0 && last > first;       // the tail is read by the first block and written by the last
+    if (block > last || (joined && blockIdx.x > 0 && block == last)) return;
     if (!keys && !values && !queries) return;
     struct Row {
         v4i lo, hi;                                                   // eight halves each
@@ -644,7 +644,7 @@ struct DecodeLds {
 };
 
 // slot of position s in the values' order: 8 of each 32 per lane group; and where column x has it: its eights are moved round by the column's,
-// so that the threads of a row, 8 columns apart, write to different banks (2.0 us for a block's rows without)
+// so that the threads of a row, 8 columns apart, write to different banks
 __device__ __forceinline__ int value_slot(int s) { return (s & 32) | ((s >> 2) & 3) << 3 | ((s >> 4) & 1) << 2 | (s & 3); }
 __device__ __forceinline__ int value_place(int x, int at) { return ((at + (x & ~7)) & 56) | (at & 7); }
 
@@ -1054,8 +1054,10 @@ static sqap_status launch_append_d(const __half *QKV, int64_t ld, const int32_t 
         ready[device_slot()].store(true, std::memory_order_relaxed);
     }
     const int columns = (max_new + kBlock - 2) / kBlock + 1;          // blocks that the longest sequence touches, at most
-    // heads that share a workgroup's angles: as many as leave the device its workgroups.  Where there is less than one per compute unit, keys,
-    // values and queries have workgroups of their own: each is a chain of its own (148 rows of 32 heads 10.5 us together, 7.9 apart).
+    // heads that share a workgroup's angles: as many as leave the device its workgroups.  Where there are
+    // few, keys, values and queries have workgroups of their own: each is a chain of its own, but keys and queries work out the same
+    // angles (148 rows of 8 key and 32 query heads, 32 of them: 15.3 us together, 10.3 apart; 512 of 8, 72: 8.7 and 7.2; 148 of 32, 128: 8.9 and 9.5).
+    // Angles for more than one head: 2000 rows of 32 heads 25.0 us with 512 workgroups, 35.5 with 256, 27.8 with 1024.
     const int64_t items = (int64_t)columns * cache.batch * cache.kv_heads;
     const int share = (int)std::max<int64_t>(1, std::min<int64_t>(cache.kv_heads, items / kAppendGroups));
     const int split = items <= kAppendSplit ? 1 : 0;
