@@ -370,6 +370,17 @@ constexpr float kLargeScore = 1048576.f;
 // most blocks, and the sums are 64 registers.
 constexpr float kRaiseBy = 6.f;
 
+// NaN for workgroup `number`'s rows of a sequence that does not fit: of as many tiles as there are of its longest
+template <int D>
+__device__ __forceinline__ void nan_rows(__half *O, int64_t ldo, int first, int64_t n_rows, int G, int kh, int number, int tiles, int per_tile)
+{
+    for (int64_t tile = (int64_t)number * per_tile; tile < n_rows; tile += (int64_t)tiles * per_tile)
+        for (int u = threadIdx.x; u < per_tile * D; u += blockDim.x) {
+            const int64_t row = tile + u / D;
+            if (row < n_rows) O[(first + row / G) * ldo + (kh * G + row % G) * D + u % D] = __ushort_as_half(0x7e00);
+        }
+}
+
 // Rows are (query, head) pairs of the heads that share a key head, query first, 32 to a wavefront and WAVES wavefronts to a workgroup, so
 // that a block of keys and values is taken from memory and made halves once for all of them.  Everything is transposed (scores:
 // positions x rows), as in attention.hip: probabilities are the second product's operand where they were computed.
@@ -399,15 +410,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
     const Span sp = span_of(starts, past, b, rows, max_new, cache.blocks * kBlock);
     const int G = H / cache.kv_heads;
     const int64_t n_rows = (int64_t)sp.n * G, tile = (int64_t)(tiles - 1 - number) * TILE;
+    if (!sp.fits) {                                                   // (of more than max_new rows too: all of them)
+        nan_rows<D>(O, ldo, sp.row, n_rows, G, kh, number, tiles, TILE);
+        return;
+    }
     if (tile >= n_rows) return;
     const int64_t mine = tile + wave * 32 + c;
     const int64_t mine_in = min(mine, n_rows - 1);
     const int query = (int)(mine_in / G), head = kh * G + (int)(mine_in % G);
-    if (!sp.fits) {
-        if (mine < n_rows && h == 0)
-            for (int i = 0; i < D; ++i) O[(int64_t)(sp.row + query) * ldo + (int64_t)head * D + i] = __ushort_as_half(0x7e00);
-        return;
-    }
     if (t == 0) not_finite = 0;
     const int end = sp.past + sp.n, sees = sp.past + query;           // last position that this lane's row sees
     const int tile_last = sp.past + (int)((min(tile + TILE, n_rows) - 1) / G), n_blocks = tile_last / kBlock + 1;
@@ -606,6 +616,267 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
     }
 }
 
+// ---------------------------------------------------------------- 16 rows and a block of their own to a wavefront
+
+// Sums of a wavefront's blocks: row l % 16, columns 16 i + 4 (l / 16) ...
+template <int D>
+struct WaveSums {
+    v4f o[D / 16];
+    float m = -INFINITY, l = 0.f;
+    Unit unit;
+    __device__ __forceinline__ WaveSums()
+    {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) o[i] = v4f{0.f, 0.f, 0.f, 0.f};
+    }
+    // key(T, m), value(i, n): operands of the products; `then` runs when the keys have been used; `ends`: this lane's row sees the first
+    // `sees` + 1 positions of the block only.  TWO: a probability enters as the sum of two halves.
+    template <bool TWO, typename Key, typename Value, typename Then>
+    __device__ __forceinline__ void add(const v8h (&q)[D / 32], float sk, float sv, bool ends, int sees, Key key, Value value, Then then)
+    {
+        const int g = (threadIdx.x & 63) >> 4;
+        v4f s[4];
+#pragma unroll
+        for (int T4 = 0; T4 < 4; ++T4) s[T4] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int T4 = 0; T4 < 4; ++T4)
+#pragma unroll
+            for (int m = 0; m < D / 32; ++m) s[T4] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key(T4, m), q[m], s[T4], 0, 0, 0);
+        const float per_d = kLog2e / sqrtf((float)D);
+        sk = sk == 0.f ? per_d : sk * per_d;                          // (keys that are all zeros: as in cache8_attention_kernel)
+        then();
+        if (ends) {
+#pragma unroll
+            for (int T4 = 0; T4 < 4; ++T4)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (16 * T4 + 4 * g + i > sees) s[T4][i] = -INFINITY;
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int T4 = 0; T4 < 4; ++T4)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, s[T4][i]);
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (top > -INFINITY) top *= sk;
+        float by = sk;
+        if (__any(fabsf(top) > kLargeScore && top > -INFINITY)) {
+#pragma unroll
+            for (int T4 = 0; T4 < 4; ++T4)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float w = s[T4][i] * sk;
+                    asm volatile("" : "+v"(w));                       // (rounded)
+                    s[T4][i] = s[T4][i] == -INFINITY ? -INFINITY : w;
+                }
+            by = 1.f;
+        }
+        float change;
+        const float factor = unit.enter(sv, change);
+        if (top > m + kRaiseBy) {
+            const float raise = exp2f(m - top);
+            change *= raise;
+            l *= raise;
+            m = top;
+        }
+        if (__any(change != 1.f)) {
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) o[i] *= change;
+        }
+        // (no score above minus infinity so far: nothing is added, other wavefronts' blocks may have some)
+        const float from = __log2f(factor) - (m == -INFINITY ? 0.f : m);
+        float sum = 0.f;
+        v8h p[2], rest[2];
+#pragma unroll
+        for (int T4 = 0; T4 < 4; ++T4)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(s[T4][i], by, from));
+                sum += e;
+                const _Float16 e0 = (_Float16)e;
+                p[T4 >> 1][(T4 & 1) * 4 + i] = e0;
+                if constexpr (TWO) rest[T4 >> 1][(T4 & 1) * 4 + i] = (_Float16)(e - (float)e0);
+            }
+        l += sum * __builtin_amdgcn_rcpf(factor);
+        if (!(sv >= 0.f)) {                                           // values that are NaN as a whole
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p[n][i] = s[2 * n + (i >> 2)][i & 3] == -INFINITY ? (_Float16)0.f : (_Float16)NAN;
+        }
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const v8h v = value(i, n);
+                o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[n], o[i], 0, 0, 0);
+                if constexpr (TWO) o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, rest[n], o[i], 0, 0, 0);
+            }
+    }
+};
+
+// slot of position s in the values' order: 8 of each 32 per lane group; and where column x has it: its eights are moved round by the column's,
+// so that the threads of a row, 8 columns apart, write to different banks
+__device__ __forceinline__ int value_slot(int s) { return (s & 32) | ((s >> 2) & 3) << 3 | ((s >> 4) & 1) << 2 | (s & 3); }
+__device__ __forceinline__ int value_place(int x, int at) { return ((at + (x & ~7)) & 56) | (at & 7); }
+
+// Few rows: tiles of 16 (query, head) pairs, and the blocks dealt to the workgroup's wavefronts, each of which takes keys and values to its own
+// registers as the decode call does.
+constexpr int kFewRowsWaves = 8;
+template <int D>
+struct FewRowsLds {
+    __attribute__((aligned(16))) union {
+        struct {
+            unsigned short k[kBlock][D + 8];     // as in DecodeLds
+            unsigned short v[D][kBlock + 8];
+        } tail;
+        float o[kFewRowsWaves][16][D + 4];
+    } u;
+    float m[kFewRowsWaves][16], l[kFewRowsWaves][16];
+    int not_finite;
+};
+template <int D>
+__global__ __launch_bounds__(64 * kFewRowsWaves, 2) void cache8_few_rows_kernel(const __half *__restrict__ Q, int64_t ldq, const int32_t *__restrict__ starts,
+                                                                                const int32_t *__restrict__ past, int rows, int max_new, int H,
+                                                                                const Cache8View cache, __half *__restrict__ O, int64_t ldo, int tiles)
+{
+    constexpr int C = D / 64, DT = D / 16, T = 64 * kFewRowsWaves;
+    extern __shared__ __attribute__((aligned(16))) uint8_t raw_lds[];
+    FewRowsLds<D> &lds = *reinterpret_cast<FewRowsLds<D> *>(raw_lds);
+    const int pairs = cache.kv_heads * cache.batch, id = blockIdx.x;
+    int pair, number;
+    if (pairs % 8 == 0) {                                             // (as in cache8_attention_kernel)
+        pair = (id & 7) + 8 * ((id >> 3) % (pairs / 8));
+        number = (id >> 3) / (pairs / 8);
+    } else {
+        pair = id % pairs;
+        number = id / pairs;
+    }
+    const int b = pair / cache.kv_heads, kh = pair % cache.kv_heads;
+    const int t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), r = l & 15, g = l >> 4;
+    const Span sp = span_of(starts, past, b, rows, max_new, cache.blocks * kBlock);
+    const int G = H / cache.kv_heads;
+    const int64_t n_rows = (int64_t)sp.n * G, tile = (int64_t)(tiles - 1 - number) * 16;
+    if (!sp.fits) {
+        nan_rows<D>(O, ldo, sp.row, n_rows, G, kh, number, tiles, 16);
+        return;
+    }
+    if (tile >= n_rows) return;
+    auto query_of = [&](int64_t row) { return (int)(min(row, n_rows - 1) / G); };
+    auto place = [&](int64_t row) { return kh * G + (int)(min(row, n_rows - 1) % G); };
+    auto out_of = [&](int64_t row) { return O + (int64_t)(sp.row + query_of(row)) * ldo + (int64_t)place(row) * D; };
+    const int end = sp.past + sp.n, sees = sp.past + query_of(tile + r), first_sees = sp.past + query_of(tile);
+    const int n_blocks = (sp.past + query_of(tile + 15)) / kBlock + 1, tail_block = end / kBlock, tail_rows = end % kBlock;
+    const int64_t head = (int64_t)b * cache.kv_heads + kh;
+    const __half *tail_k = cache.tail + head * 2 * kBlock * D, *tail_v = tail_k + kBlock * D;
+    v4i kraw[4 * C], vraw[DT];
+    float2 sc = {0.f, 0.f};
+    auto fetch_keys = [&](int j) {
+        if (j >= n_blocks || j == tail_block) return;
+        sc = reinterpret_cast<const float2 *>(cache.scales)[head * cache.blocks + j];
+        const v4i *k = reinterpret_cast<const v4i *>(block_codes<D>(cache, head, j, 0)) + l;
+#pragma unroll
+        for (int i = 0; i < 4 * C; ++i) kraw[i] = k[i * 64];
+    };
+    auto fetch_values = [&](int j) {
+        if (j >= n_blocks || j == tail_block) return;
+        const v4i *v = reinterpret_cast<const v4i *>(block_codes<D>(cache, head, j, 1)) + l;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) vraw[i] = v[i * 64];
+    };
+    fetch_keys(wave);
+    fetch_values(wave);
+    v8h q[2 * C];
+    const __half *from = Q + (int64_t)(sp.row + query_of(tile + r)) * ldq + (int64_t)place(tile + r) * D;
+#pragma unroll
+    for (int m = 0; m < 2 * C; ++m) q[m] = *reinterpret_cast<const v8h *>(from + 64 * (m >> 1) + 16 * g + 8 * (m & 1));
+    const bool has_tail = n_blocks - 1 == tail_block;
+    if (has_tail) {
+        if (t == 0) lds.not_finite = 0;
+        __syncthreads();
+        bool odd = false;
+        for (int u = t; u < kBlock * D / 8; u += T) {
+            const int s = u / (D / 8), x = (u % (D / 8)) * 8, at = value_slot(s);
+            v4i k = {0, 0, 0, 0}, v = k;
+            if (s < tail_rows) {
+                k = *reinterpret_cast<const v4i *>(tail_k + s * D + x);
+                v = *reinterpret_cast<const v4i *>(tail_v + s * D + x);
+            }
+            *reinterpret_cast<v4i *>(&lds.u.tail.k[s][x]) = k;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                unsigned short w = (unsigned short)((unsigned)v[e >> 1] >> (16 * (e & 1)));
+                if ((w & 0x7fffu) >= 0x7c00u) w = 0, odd = true;      // comes back at the end, to the rows that see it
+                lds.u.tail.v[x + e][value_place(x, at)] = w;
+            }
+        }
+        if (odd) lds.not_finite = 1;
+        __syncthreads();
+    }
+    WaveSums<D> sums;
+    for (int j = wave; j < n_blocks; j += kFewRowsWaves) {
+        const bool ends = (j + 1) * kBlock - 1 > first_sees;
+        const int last = sees - j * kBlock;
+        if (j != tail_block) {
+            const float2 scale = sc;
+            sums.template add<false>(
+                q, scale.x, scale.y, ends, last,
+                [&](int T4, int m) {
+                    const v4i w = kraw[T4 * C + (m >> 1)];
+                    return (m & 1) ? halves_of(w[2], w[3]) : halves_of(w[0], w[1]);
+                },
+                [&](int i, int n) { return halves_of(vraw[i][2 * n], vraw[i][2 * n + 1]); }, [&] { fetch_keys(j + kFewRowsWaves); });
+            fetch_values(j + kFewRowsWaves);
+        } else {
+            sums.template add<false>(
+                q, 1.f, 1.f, true, min(last, tail_rows - 1),
+                [&](int T4, int m) { return *reinterpret_cast<const v8h *>(&lds.u.tail.k[16 * T4 + r][64 * (m >> 1) + 16 * g + 8 * (m & 1)]); },
+                [&](int i, int n) { return *reinterpret_cast<const v8h *>(&lds.u.tail.v[16 * i + r][value_place(16 * i + r, 32 * n + 8 * g)]); }, [] {});
+        }
+    }
+    sums.l += __shfl_xor(sums.l, 16);
+    sums.l += __shfl_xor(sums.l, 32);
+    const bool odd = has_tail && lds.not_finite;
+    __syncthreads();                                                  // the tail's rows have been read
+    const int waves = min(n_blocks, kFewRowsWaves);
+    if (wave < waves) {
+#pragma unroll
+        for (int i = 0; i < DT; ++i) *reinterpret_cast<v4f *>(&lds.u.o[wave][r][16 * i + 4 * g]) = sums.o[i] * sums.unit.unit;
+        if (g == 0) {
+            lds.m[wave][r] = sums.m;
+            lds.l[wave][r] = sums.l;
+        }
+    }
+    __syncthreads();
+    const int row = t / (D / 4), col = t % (D / 4) * 4;               // four columns of a row
+    if (row >= 16 || tile + row >= n_rows) return;
+    float top = -INFINITY, sum = 0.f;
+    for (int w = 0; w < waves; ++w) top = fmaxf(top, lds.m[w][row]);
+    v4f o = {0.f, 0.f, 0.f, 0.f};
+    for (int w = 0; w < waves; ++w) {
+        const float f = exp2f(lds.m[w][row] - top);
+        sum += f * lds.l[w][row];
+        o += f * *reinterpret_cast<const v4f *>(&lds.u.o[w][row][col]);
+    }
+    const float norm = 1.f / sum;
+    union { __half h[4]; v2u v; } out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float x = o[i] * norm;
+        if (odd) {                                                    // infinities and NaN among the tail's values that this row sees
+            x = __half2float(__float2half_rn(x));
+#pragma unroll 1
+            for (int s = 0; s <= sp.past + query_of(tile + row) - tail_block * kBlock; ++s) {
+                const float v = __half2float(tail_v[s * D + col + i]);
+                if (!(fabsf(v) <= 65504.f)) x += v;
+            }
+        }
+        out.h[i] = __float2half_rn(x);
+    }
+    *reinterpret_cast<v2u *>(out_of(tile + row) + col) = out.v;
+}
+
 // ---------------------------------------------------------------- attention of one row per sequence
 
 // One workgroup per sequence, key head, up to 16 of the query heads that share it, and share of the sequence's blocks; a block is one
@@ -642,11 +913,6 @@ struct DecodeLds {
     int odd[D];                                  // what is not finite among a column's values in the tail: 1 infinity, 2 minus infinity, 4 NaN
     int arrived;
 };
-
-// slot of position s in the values' order: 8 of each 32 per lane group; and where column x has it: its eights are moved round by the column's,
-// so that the threads of a row, 8 columns apart, write to different banks
-__device__ __forceinline__ int value_slot(int s) { return (s & 32) | ((s >> 2) & 3) << 3 | ((s >> 4) & 1) << 2 | (s & 3); }
-__device__ __forceinline__ int value_place(int x, int at) { return ((at + (x & ~7)) & 56) | (at & 7); }
 
 template <int D>
 __global__ __launch_bounds__(64 * kDecodeWaves, 2) void cache8_decode_kernel(const DecodeArgs a)
@@ -830,116 +1096,38 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void cache8_decode_kernel(con
     v8h qf[2 * C];
 #pragma unroll
     for (int m = 0; m < 2 * C; ++m) qf[m] = *reinterpret_cast<const v8h *>(&lds.q[min(r, heads - 1)][64 * (m >> 1) + 16 * g + 8 * (m & 1)]);
-    v4f ot[DT];
-#pragma unroll
-    for (int i = 0; i < DT; ++i) ot[i] = v4f{0.f, 0.f, 0.f, 0.f};
-    float mrun = -INFINITY, lrun = 0.f;
-    Unit unit;
-    const float per_d = kLog2e / sqrtf((float)D);
-    auto block = [&](int j, auto last_c) {
-        constexpr bool LAST = decltype(last_c)::value;                // the last block's rows are in LDS
-        v4f s[4];
-#pragma unroll
-        for (int T4 = 0; T4 < 4; ++T4) s[T4] = v4f{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int T4 = 0; T4 < 4; ++T4)
-#pragma unroll
-            for (int m = 0; m < 2 * C; ++m) {
-                v8h k;
-                if constexpr (LAST) {
-                    k = *reinterpret_cast<const v8h *>(&lds.u.tail.k[16 * T4 + r][64 * (m >> 1) + 16 * g + 8 * (m & 1)]);
-                } else {
-                    const v4i w = kraw[T4 * C + (m >> 1)];
-                    k = (m & 1) ? halves_of(w[2], w[3]) : halves_of(w[0], w[1]);
-                }
-                s[T4] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qf[m], s[T4], 0, 0, 0);
-            }
-        float sk = LAST ? tail_sk : sc.x, sv = LAST ? tail_sv : sc.y;
-        sk = sk == 0.f ? per_d : sk * per_d;                          // (keys that are all zeros: as in cache8_attention_kernel)
-        if constexpr (!LAST) {
-            fetch_scales(j + kDecodeWaves);
-            fetch_keys(j + kDecodeWaves);                             // (into the registers that have just become free)
-        }
-        float top = -INFINITY;
-#pragma unroll
-        for (int T4 = 0; T4 < 4; ++T4)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (LAST && 16 * T4 + 4 * g + i > slot) s[T4][i] = -INFINITY;
-                top = fmaxf(top, s[T4][i]);
-            }
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        if (top > -INFINITY) top *= sk;
-        float by = sk;
-        if (__any(fabsf(top) > kLargeScore && top > -INFINITY)) {
-#pragma unroll
-            for (int T4 = 0; T4 < 4; ++T4)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float w = s[T4][i] * sk;
-                    asm volatile("" : "+v"(w));                       // (rounded)
-                    s[T4][i] = s[T4][i] == -INFINITY ? -INFINITY : w;
-                }
-            by = 1.f;
-        }
-        float change;
-        const float factor = unit.enter(sv, change);
-        if (top > mrun + kRaiseBy) {
-            const float raise = exp2f(mrun - top);
-            change *= raise;
-            lrun *= raise;
-            mrun = top;
-        }
-        if (__any(change != 1.f)) {
-#pragma unroll
-            for (int i = 0; i < DT; ++i) ot[i] *= change;
-        }
-        const float from = __log2f(factor) - mrun;
-        float sum = 0.f;
-        v8h p[2], rest[2];                                            // a probability as the sum of two halves
-#pragma unroll
-        for (int T4 = 0; T4 < 4; ++T4)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(s[T4][i], by, from));
-                sum += e;
-                const _Float16 e0 = (_Float16)e;
-                p[T4 >> 1][(T4 & 1) * 4 + i] = e0;
-                rest[T4 >> 1][(T4 & 1) * 4 + i] = (_Float16)(e - (float)e0);
-            }
-        lrun += sum * __builtin_amdgcn_rcpf(factor);
-        if (!(sv >= 0.f)) {                                           // values that are NaN as a whole
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) p[n][i] = s[2 * n + (i >> 2)][i & 3] == -INFINITY ? (_Float16)0.f : (_Float16)NAN;
-        }
-#pragma unroll
-        for (int i = 0; i < DT; ++i)
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                v8h v;
-                if constexpr (LAST) v = *reinterpret_cast<const v8h *>(&lds.u.tail.v[16 * i + r][value_place(16 * i + r, 32 * n + 8 * g)]);
-                else v = halves_of(vraw[i][2 * n], vraw[i][2 * n + 1]);
-                ot[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[n], ot[i], 0, 0, 0);
-                ot[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, rest[n], ot[i], 0, 0, 0);
-            }
-        if constexpr (!LAST) fetch_values(j + kDecodeWaves);
-    };
+    WaveSums<D> own;
     int j = begin + wave;
-    for (; j < stop && j < last; j += kDecodeWaves) block(j, std::false_type{});
-    if (j < stop) block(j, std::true_type{});
-    lrun += __shfl_xor(lrun, 16);
-    lrun += __shfl_xor(lrun, 32);
+    for (; j < stop && j < last; j += kDecodeWaves) {
+        const float2 scale = sc;
+        own.template add<true>(
+            qf, scale.x, scale.y, false, 0,
+            [&](int T4, int m) {
+                const v4i w = kraw[T4 * C + (m >> 1)];
+                return (m & 1) ? halves_of(w[2], w[3]) : halves_of(w[0], w[1]);
+            },
+            [&](int i, int n) { return halves_of(vraw[i][2 * n], vraw[i][2 * n + 1]); },
+            [&] {
+                fetch_scales(j + kDecodeWaves);
+                fetch_keys(j + kDecodeWaves);                         // (into the registers that have just become free)
+            });
+        fetch_values(j + kDecodeWaves);
+    }
+    if (j < stop)
+        own.template add<true>(
+            qf, tail_sk, tail_sv, true, slot,
+            [&](int T4, int m) { return *reinterpret_cast<const v8h *>(&lds.u.tail.k[16 * T4 + r][64 * (m >> 1) + 16 * g + 8 * (m & 1)]); },
+            [&](int i, int n) { return *reinterpret_cast<const v8h *>(&lds.u.tail.v[16 * i + r][value_place(16 * i + r, 32 * n + 8 * g)]); }, [] {});
+    own.l += __shfl_xor(own.l, 16);
+    own.l += __shfl_xor(own.l, 32);
     __syncthreads();                                                  // the last block's rows have been read
 #pragma unroll
     for (int i = 0; i < DT; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) lds.u.o[wave][r][16 * i + 4 * g + e] = ot[i][e] * unit.unit;
+        for (int e = 0; e < 4; ++e) lds.u.o[wave][r][16 * i + 4 * g + e] = own.o[i][e] * own.unit.unit;
     if (g == 0) {
-        lds.m[wave][r] = mrun;
-        lds.l[wave][r] = lrun;
+        lds.m[wave][r] = own.m;
+        lds.l[wave][r] = own.l;
     }
     __syncthreads();
     // the wavefronts' sums in one
@@ -1083,29 +1271,36 @@ sqap_status launch_cache8_read(const Cache8View &cache, int d, const int32_t *le
     return SQAP_OK;
 }
 
-template <int D, int WAVES>
-static sqap_status launch_attention_of(const __half *Q, int64_t ldq, const int32_t *starts, const int32_t *past, int rows, int max_new, int H,
-                                       const Cache8View &cache, __half *O, int64_t ldo, hipStream_t st)
-{
-    constexpr int LDS = 2 * 2 * kBlock * D * 2;
-    const int64_t tiles = ((int64_t)max_new * (H / cache.kv_heads) + 32 * WAVES - 1) / (32 * WAVES), items = tiles * cache.kv_heads * cache.batch;
-    if (items > INT32_MAX) return fail(SQAP_EUNSUPPORTED, "sqap_cache8_attention: %lld tiles of rows", (long long)items);
-    static std::atomic<bool> ready[kMaxDeviceSlots];
-    if (LDS > 65536 - 64 && !ready[device_slot()].load(std::memory_order_relaxed)) {
-        SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(cache8_attention_kernel<D, WAVES>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
-        ready[device_slot()].store(true, std::memory_order_relaxed);
-    }
-    hipLaunchKernelGGL((cache8_attention_kernel<D, WAVES>), dim3((unsigned)items), dim3(64 * WAVES), LDS, st, Q, ldq, starts, past, rows, max_new, H,
-                       cache, O, ldo, (int)tiles);
-    SQAP_HIP_CHECK(hipGetLastError());
-    return SQAP_OK;
-}
+// Tiles of 16 rows, whose blocks are dealt to eight wavefronts, where there would be few tiles of 128: 148 rows of 32 heads (64 of those) take
+// 9.2 us so and 11.1 otherwise, 512 of 8 heads (32) 8.1 and 18.7, 20 of 32 heads over 8 behind 2000 (8) 17 and 61, 1500 of 8 behind 2000
+// (96) 61 and 99, 300 of 32 heads (96) 14.7 and 15.2; but 500 of 32 (128) 25.0 and 21.6, 1000 of 32 over 8 (256) 56 and 36.
+constexpr int kFewTiles = 96;
 
 template <int D>
 static sqap_status launch_attention_d(const __half *Q, int64_t ldq, const int32_t *starts, const int32_t *past, int rows, int max_new, int H,
                                       const Cache8View &cache, __half *O, int64_t ldo, hipStream_t st)
 {
-    return launch_attention_of<D, 4>(Q, ldq, starts, past, rows, max_new, H, cache, O, ldo, st);
+    constexpr int WAVES = 4, LDS = 2 * 2 * kBlock * D * 2;
+    static std::atomic<bool> ready[kMaxDeviceSlots];
+    if (!ready[device_slot()].load(std::memory_order_relaxed)) {
+        SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(cache8_attention_kernel<D, WAVES>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+        SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(cache8_few_rows_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                           (int)sizeof(FewRowsLds<D>)));
+        ready[device_slot()].store(true, std::memory_order_relaxed);
+    }
+    const auto tiles_of = [&](int per_tile) { return ((int64_t)max_new * (H / cache.kv_heads) + per_tile - 1) / per_tile; };
+    const int64_t pairs = (int64_t)cache.kv_heads * cache.batch;
+    const bool few = tiles_of(32 * WAVES) * pairs <= kFewTiles;
+    const int64_t tiles = tiles_of(few ? 16 : 32 * WAVES), items = tiles * pairs;
+    if (items > INT32_MAX) return fail(SQAP_EUNSUPPORTED, "sqap_cache8_attention: %lld tiles of rows", (long long)items);
+    if (few)
+        hipLaunchKernelGGL(cache8_few_rows_kernel<D>, dim3((unsigned)items), dim3(64 * kFewRowsWaves), sizeof(FewRowsLds<D>), st, Q, ldq, starts, past, rows,
+                           max_new, H, cache, O, ldo, (int)tiles);
+    else
+        hipLaunchKernelGGL((cache8_attention_kernel<D, WAVES>), dim3((unsigned)items), dim3(64 * WAVES), LDS, st, Q, ldq, starts, past, rows, max_new, H,
+                           cache, O, ldo, (int)tiles);
+    SQAP_HIP_CHECK(hipGetLastError());
+    return SQAP_OK;
 }
 
 sqap_status launch_cache8_attention(const __half *Q, int64_t ldq, const int32_t *starts, const int32_t *past, int rows, int max_new, int H,

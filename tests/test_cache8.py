@@ -84,6 +84,7 @@ def G():
 
 class Model:
     """A batch of sequences on the host next to the cache on the device.  The rotation's bits are those of sqap_rope."""
+    most = 0                                                              # rows that are announced at least
 
     def __init__(self, G, batch, H, kv, d, capacity, seed=0):
         import torch
@@ -135,7 +136,7 @@ class Model:
         o = t.full((total, self.H * self.d), 9.0, dtype=t.float16, device=G.DEV)
         rows = G.to_dev(x.reshape(total, -1))
         before = rows.clone()
-        most = int(max(counts)) if len(counts) else 0
+        most = max(self.most, int(max(counts)) if len(counts) else 0)
         B.sqap_cache8_append(rows, starts, G.to_dev(np.asarray(pos, dtype=np.int32)), past, self.cache, self.H, most, Q_out=q)
         assert t.equal(rows.view(t.int16), before.view(t.int16))
         assert np.array_equal(q.cpu().numpy().view(np.uint16), y[:, :self.H].reshape(total, -1).view(np.uint16))
@@ -210,6 +211,12 @@ class Model:
         return [p.clone().cpu() for p in parts]
 
 
+@pytest.fixture(params=["few", "many"])
+def announced(request, monkeypatch):
+    """With many rows announced attention goes by tiles of 128 rows, with few by tiles of 16; what comes out is the same."""
+    monkeypatch.setattr(Model, "most", 0 if request.param == "few" else 128 * 97)
+
+
 CASES = [  # H, kv, d, then rows per sequence of one call after the other
     (1, 1, 64, [[1]]),
     (2, 2, 128, [[5], [1], [70]]),
@@ -224,7 +231,7 @@ CASES = [  # H, kv, d, then rows per sequence of one call after the other
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("case", range(len(CASES)))
-def test_prompts(G, case):
+def test_prompts(G, case, announced):
     H, kv, d, calls = CASES[case]
     m = Model(G, len(calls[0]), H, kv, d, 64 * 18, seed=case)
     for counts in calls:
@@ -245,7 +252,7 @@ def test_single_rows(G, H, kv, d, past):
 
 
 @pytest.mark.gpu
-def test_contents_do_not_depend_on_the_calls(G):
+def test_contents_do_not_depend_on_the_calls(G, announced):
     H, kv, d = 4, 2, 128
     x = np.random.default_rng(3).standard_normal((150, H + 2 * kv, d)).astype(np.float16)
     states = []
@@ -269,7 +276,7 @@ def test_contents_do_not_depend_on_the_calls(G):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("d", [64, 128])
-def test_sizes_that_differ_between_blocks(G, d):
+def test_sizes_that_differ_between_blocks(G, d, announced):
     """Values of blocks between 2^-10 and 2^10, zeros, keys so large that one position takes it all, and halfway quotients."""
     m = Model(G, 1, 4, 2, d, 64 * 12, seed=9)
     for k_size, v_size in ((1, 1), (1, 2.0 ** 10), (1, 2.0 ** -10), (20, 2.0 ** -10), (1, 2.0 ** 4), (0, 1), (1, 0), (30, 1)):
@@ -285,7 +292,7 @@ def test_sizes_that_differ_between_blocks(G, d):
 
 
 @pytest.mark.gpu
-def test_zero_values_give_zero(G):
+def test_zero_values_give_zero(G, announced):
     m = Model(G, 1, 2, 1, 64, 256)
     m.append([100], m.rows(100, 1, 0))
     o = m.decode(m.rows(1, 1, 0))
@@ -293,7 +300,7 @@ def test_zero_values_give_zero(G):
 
 
 @pytest.mark.gpu
-def test_values_that_are_not_finite(G):
+def test_values_that_are_not_finite(G, announced):
     """In the tail they reach the rows that see them; in a finished block, that head's rows that see any of it."""
     for d, where in ((64, "k"), (128, "v"), (64, "v"), (128, "k")):
         m = Model(G, 2, 4, 2, d, 64 * 6, seed=d)
@@ -312,12 +319,33 @@ def test_values_that_are_not_finite(G):
 
 
 @pytest.mark.gpu
-def test_queries_that_are_not_finite_stay_alone(G):
+def test_queries_that_are_not_finite_stay_alone(G, announced):
     m = Model(G, 1, 4, 2, 64, 256)
     x = m.rows(90)
     x[40, 1, 7] = np.nan
     x[41, 2, 7] = np.inf
     m.append([90], x)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("max_new", [1, 20, 700])
+def test_more_rows_than_announced(G, max_new):
+    """All outputs of such a sequence are NaN, however many; its neighbour's are what they should be."""
+    import torch
+    H, kv, d = 4, 2, 64
+    m = Model(G, 2, H, kv, d, 1024, seed=3)
+    dev = lambda a: G.to_dev(np.asarray(a, dtype=np.int32))               # noqa: E731
+    n, few = 900, min(max_new, 30)
+    x = m.rows(n + few)
+    starts, past, pos = dev([0, n, n + few]), dev([0, 0]), dev(np.concatenate([np.arange(n), np.arange(few)]))
+    q, o = (torch.full((n + few, H * d), 9.0, dtype=torch.float16, device=G.DEV) for _ in range(2))
+    B.sqap_cache8_append(G.to_dev(x.reshape(n + few, -1)), starts, pos, past, m.cache, H, max_new, Q_out=q)
+    B.sqap_cache8_attention(q, starts, past, m.cache, H, max_new, o)
+    got = o.cpu().numpy()
+    assert np.isnan(got[:n]).all() and np.isfinite(got[n:]).all()
+    y = m.turned(x[n:], np.arange(few))
+    m.note([0, few], y)
+    m.check(got[n:], y, [0, few], True)
 
 
 @pytest.mark.gpu
