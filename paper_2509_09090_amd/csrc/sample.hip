@@ -1,7 +1,7 @@
 // Sampling of the next token from half-precision logits: temperature, the k most likely, the smallest set that holds a share p of the
 // mass, a least share of the most likely one's probability, then the inverse of the cumulated masses in index order at a given number.
 //
-// A token's mass is a function of its logit alone, 2^40 exp((l - max) / T) rounded down to an integer: sums of masses are exact, so that
+// A token's mass is a function of its logit alone, 2^40 exp((l - max) / T) rounded to an integer: sums of masses are exact, so that
 // no order of addition shows, and every cut is a cut between two keys (a half as an integer that orders as the half does) plus a number
 // of tokens of the key at the cut, lowest indices first.
 #include <algorithm>
@@ -32,29 +32,38 @@ __device__ __forceinline__ float value_of(unsigned key)
 
 __device__ __forceinline__ unsigned bin_of(unsigned key) { return kBins - 1 - (key >> 4); }
 
-// exp2((value - top) * per_nat) in units of 2^-40.  The factor is in two parts, and so is the product, so that a mass is off by 2^-22 or so
-// however far the logit is from the largest.  The difference is held between 0 (an infinite logit's) and one whose mass is none (minus infinity's).
+// exp2((value - top) * per_nat) in units of 2^-40, a whole number in binary64 (whose multiply-adds run at binary32's rate, and no instruction
+// of binary32's exponential comes near what a vocabulary of equal shares needs: borders 2^-17 of the mass apart).  The difference is exact; the
+// power of two of its fraction, at most a half, is the Taylor series to the ninth power, off by less than 2^-37.  A top that is infinite
+// is taken for a large number, and everything else to be far below.
 struct Mass {
-    float top, hi, lo, least;
-    __device__ __forceinline__ void set(float top_, double per_nat)
+    static constexpr float kCap = 131072.f;
+    double top, per_nat;
+    __device__ __forceinline__ void set(float top_, double per_nat_)
     {
-        top = fminf(top_, 3e38f);
-        per_nat = fmin(fmax(per_nat, 1e-30), 1e30);
-        hi = (float)per_nat;
-        lo = (float)(per_nat - (double)hi);
-        least = -64.f / hi;
+        top = fminf(top_, kCap);
+        per_nat = top_ > kCap ? 1e30 : per_nat_;
     }
-    __device__ __forceinline__ float scaled(float value) const        // in units of 2^-20
+    __device__ __forceinline__ double units(float value) const
     {
-        const float x = __builtin_amdgcn_fmed3f(value - top, least, 0.f), p = x * hi;
-        const float rest = fmaf(x, lo, fmaf(x, hi, -p));
-        const float e = __builtin_amdgcn_exp2f(p) * 1048576.f;
-        return fmaf(e * rest, 0.6931471805599453f, e);
+        const double p = fmax(((double)fminf(value, kCap) - top) * per_nat, -64.0), n = rint(p), x = p - n;
+        double e = 1.0178086009239696e-07;                            // ln(2)^9 / 9!
+        e = fma(e, x, 1.3215486790144305e-06);
+        e = fma(e, x, 1.5252733804059838e-05);
+        e = fma(e, x, 1.5403530393381606e-04);
+        e = fma(e, x, 1.3333558146428441e-03);
+        e = fma(e, x, 9.618129107628477e-03);
+        e = fma(e, x, 5.5504108664821576e-02);
+        e = fma(e, x, 2.402265069591007e-01);
+        e = fma(e, x, 6.931471805599453e-01);
+        e = fma(e, x, 1.0);
+        return rint(ldexp(e, (int)n + 40));
     }
-    static __device__ __forceinline__ unsigned whole(float w) { return (unsigned)w; }
-    static __device__ __forceinline__ unsigned part(float w) { return (unsigned)(__builtin_amdgcn_fractf(w) * 1048576.f); }
-    static __device__ __forceinline__ u64 of(float w) { return ((u64)whole(w) << 20) + part(w); }
-    __device__ __forceinline__ u64 operator()(float value) const { return of(scaled(value)); }
+    static __device__ __forceinline__ u64 of(double w)                // (whole, below 2^52)
+    {
+        return (u64)__double_as_longlong(w + 4503599627370496.0) & 0xfffffffffffffull;
+    }
+    __device__ __forceinline__ u64 operator()(float value) const { return of(units(value)); }
 };
 
 // Inclusive sums over the lanes: inside rows of 16 by shifts, then the rows' last lanes are added to the rows behind.
@@ -126,16 +135,16 @@ struct alignas(16) SampleLds {
 
 // One workgroup per row; a wavefront has every 16th slab of 512 logits, eight to a lane.  CACHED: the row is kept in LDS
 // after the first pass; otherwise it is read again where it is needed, four slabs ahead.
-// What bounds it is the instructions of one compute unit: some 27 for each token where all of them count (128001 of them: 24 us, where the
-// largest alone is found in 6), and the 16 wavefronts' share in every step that is not about the row, so that each step stands here once
+// What bounds it is the instructions of one compute unit: some 40 for each token where all of them count (128001 of them: 31 us, where
+// the largest alone is found in 6), and the 16 wavefronts' share in every step that is not about the row, so that each step stands here once
 // and has few barriers.  First a bound is found below which nothing can stay: for top-k the k-th largest of the threads' maxima, for top-p alone
 // the point where the maxima of the lanes' eight have the mass that is asked for (the total has to be known first), for min-p its
 // own.  One pass collects the logits from there on in LDS in no order (all that follows is sums of integers), and the cut is found
 // among those, for top-k by counts and for top-p by masses: a histogram of 4096 bins, and of the 16 keys of the bin that holds the cut.  The masses
 // that stay are added up by slab, and the drawn token's slab alone is looked at again.  Where more stay than LDS has room for,
-// the passes go over the row.  A row of 32000: the largest 3.7 us, no filter 10.8, top-k 40 11.5, top-p 0.9 16.5, all three 16.4; of 128001:
-// 6.5, 29.7, 19.4, 46.3, 27.0, and 113 where the 97 in 100 that stay are tens of thousands.  (Full passes throughout, with the
-// histogram of every token: 28 and 99 us for all three and for top-p.)
+// the passes go over the row.  A row of 32000: the largest 3.9 us, no filter 13.4, top-k 40 11.8, top-p 0.9 19.4, all three 17.0; of 128001:
+// 6.3, 37.7, 19.9, 56.2, 28.0, and 146 where the 97 in 100 that stay are tens of thousands.  (Full passes throughout, with the
+// histogram of every token and masses in binary32: 28 and 99 us for all three and for top-p.)
 template <bool CACHED>
 __global__ __launch_bounds__(kSampleT) void sample_kernel(const SampleArgs a)
 {
@@ -316,12 +325,12 @@ __global__ __launch_bounds__(kSampleT) void sample_kernel(const SampleArgs a)
     // min-p: the lowest value whose mass is enough, the top's at the latest: of 2^16 keys, 64 at a time
     float min_value = lowest;
     if (m_given > 0.f) {
-        const float enough = fminf(m_given, 1.f) * 1048576.f;
+        const double enough = (double)fminf(m_given, 1.f) * 1099511627776.0;
         int below = 0;                                                // (the lowest key of all has no mass)
 #pragma unroll 1
         for (int step = 1024; step; step >>= step == 1 ? 1 : step == 16 ? 4 : 6) {
             const int key = below + step * (l + 1);
-            const u64 is = __ballot(key >= (int)top_key || (key > (int)kKeyMinusInf && mass.scaled(value_of((unsigned)key)) >= enough));
+            const u64 is = __ballot(key >= (int)top_key || (key > (int)kKeyMinusInf && mass.units(value_of((unsigned)key)) >= enough));
             below += is ? step * (int)__builtin_ctzll(is) : step * 64;
         }
         min_value = fmaxf(lowest, value_of((unsigned)min(below + 1, (int)top_key)));
@@ -344,25 +353,22 @@ __global__ __launch_bounds__(kSampleT) void sample_kernel(const SampleArgs a)
             unsigned ties = 0;
             const float m = largest(v);
             if (__any(m >= from)) {
-                unsigned whole = 0, part = 0;
+                double eight = 0.0;                                   // (exact)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const unsigned h = half_at(v, e);
-                    float w = mass.scaled(float_of(h));
-                    w = float_of(h) >= above ? w : 0.f;
-                    if (all_bins) {
-                        if (counting) w = w > 0.f ? 1048576.f : 0.f;
-                        if (w > 0.f) atomicAdd(&lds.bins[bin_of(key_of(h))], mass.of(w));
-                    }
-                    whole += mass.whole(w);
-                    part += mass.part(w);
+                    double w = counting ? 1099511627776.0 : mass.units(float_of(h));
+                    w = float_of(h) >= above ? w : 0.0;
+                    if (all_bins && w > 0.0) atomicAdd(&lds.bins[bin_of(key_of(h))], mass.of(w));
+                    eight += w;
                 }
                 if (tie_half < 0x10000u) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) ties += half_at(v, e) == tie_half ? 1 : 0;
                 }
-                mine += ((u64)whole << 20) + part;
-                sum = ((u64)wave_total(whole) << 20) + wave_total(part);
+                sum = mass.of(eight);                                 // 43 bits; 20 of them and the rest on their own
+                mine += sum;
+                sum = ((u64)wave_total((unsigned)(sum >> 20)) << 20) + wave_total((unsigned)sum & 0xfffffu);
                 if (tie_half < 0x10000u) ties = wave_total(ties);
                 if (max_bins) {
                     const u64 w = mass(m);
@@ -490,8 +496,8 @@ __global__ __launch_bounds__(kSampleT) void sample_kernel(const SampleArgs a)
             cut_has = lane_value(has, at);
             from = value_of(cut);
         }
-        some = cut && cut_count < cut_has;
-        tie_mass = some && from >= min_value ? mass(from) : 0;
+        some = cut && cut_count < cut_has && from >= min_value;       // (below min-p's value none of them stays)
+        tie_mass = some ? mass(from) : 0;
         from = fmaxf(from, min_value);
     }
 

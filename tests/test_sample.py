@@ -1,6 +1,7 @@
-"""Sampling from logits against the definition in 64 bits.  A mass is off by 2^-21 of itself at most (an exponential and two products in
-binary32, whose argument carries 2^-24 of at most 41 binary places, and the cut at 2^-40): where a decision of the reference lies nearer than that to
-its border the row says nothing about the token; how many such rows there are is bounded too."""
+"""Sampling from logits against the definition in 64 bits.  A mass is off by 2^-36 of itself at most (the series by 2^-37, the exponent's
+product by 2^-53 of at most 41 binary places) and by 2^-41 of the largest, to which it is rounded; a sum of v of them by v times the latter, and
+it is compared with another such sum, of a total that is one at least.  Where a decision of the reference lies nearer than that to its
+border the row says nothing about the token; how many such rows there are is bounded too."""
 import ctypes
 
 import numpy as np
@@ -9,7 +10,9 @@ import pytest
 from paper_2509_09090_amd import binding as B
 from tests import lowbit_ref as R
 
-MASS_OFF = 2.0 ** -20
+
+def _off(v):
+    return 2.0 ** -35 + v * 2.0 ** -40
 
 
 def test_refusals():
@@ -51,12 +54,12 @@ def _check(G, logits, temperature=None, top_k=None, top_p=None, min_p=None, u=No
     n_open = 0
     for i in range(b):
         want, p, near = R.sample(logits[i], at(temperature, i, 1.0), int(at(top_k, i, 0)), at(top_p, i, 1.0), at(min_p, i, 0.0), at(u, i, 0.0))
-        if near <= MASS_OFF:
+        if near <= _off(logits.shape[1]):
             n_open += 1
             continue
         assert token[i] == want, (i, token[i], want, near)
-        # (a mass is a whole number of 2^-40 of the largest, which is one of those that are added up: a quotient of masses is off by 2^-40 more)
-        assert abs(prob[i] - p) <= 4 * MASS_OFF * p + 2.0 ** -40, (i, prob[i], p)
+        # (the quotient of a mass, off by 2^-41 of the largest more, and of a sum, rounded to binary32)
+        assert abs(prob[i] - p) <= (2 * _off(logits.shape[1]) + 2.0 ** -24) * p + 2.0 ** -40, (i, prob[i], p)
     assert n_open <= most_open
     return token, prob
 
@@ -78,7 +81,7 @@ def test_filters(G, b, v, pitch):
     k = rng.integers(1, min(v, 300) + 1, b)
     p = rng.uniform(0.05, 0.999, b).astype(np.float32)
     m = rng.uniform(0.0, 0.3, b).astype(np.float32)
-    # (of a row of v tokens some 2 v MASS_OFF lie that near to a border: a row in a thousand here, but of the largest vocabulary most)
+    # (of a row of v tokens some 2 v times that lie that near to a border: a row in a thousand here, but of the largest vocabulary most)
     few = b if v > 200000 else 1
     _check(G, x, u=u, pitch=pitch, most_open=few)
     _check(G, x, t, u=u, pitch=pitch, most_open=few)
@@ -87,6 +90,29 @@ def test_filters(G, b, v, pitch):
     _check(G, x, t, min_p=m, u=u, pitch=pitch, most_open=few)
     _check(G, x, t, k, p, m, u, pitch, most_open=1)
     _check(G, x, None, k, p, None, u, pitch, most_open=1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("b,v,size", [(40, 20000, 0.5), (40, 20000, 2.0), (32, 70001, 1.0), (32, 128001, 2.5)])
+def test_filters_that_leave_many(G, b, v, size):
+    """Flat rows, of which tens of thousands of tokens stay: filters alone and on each other, the one's cut above and below the other's."""
+    rng = np.random.default_rng(v + int(10 * size))
+    x = (size * rng.standard_normal((b, v))).astype(np.float16)
+    u = rng.random(b).astype(np.float32)
+    t = rng.uniform(0.7, 1.5, b).astype(np.float32)
+    k = rng.integers(v // 3, v, b)
+    k[::2] = 0
+    p = (1 - 10.0 ** rng.uniform(-3, -0.4, b)).astype(np.float32)
+    m = (10.0 ** rng.uniform(-5, -0.5, b)).astype(np.float32)
+    m[::3] = 0
+    for kw in (dict(), dict(top_p=p), dict(top_k=k), dict(min_p=m), dict(top_p=p, min_p=m), dict(top_k=k, min_p=m), dict(top_k=k, top_p=p, min_p=m)):
+        # What top-p leaves out has a mass of 1 - p at most, of v tokens at most: the masses next to its cut are some (1 - p) / v and less, and the
+        # cut lies within one of them from a border.  Where that is not above what a border may be off by, on both sides, it is open.
+        none_near = int((1 - p <= 2 * v * _off(v)).sum()) if "top_p" in kw else 0
+        # The number that is drawn with lies that near to one of v borders in 2 v off of all rows, the least share for min-p likewise: of b rows
+        # so many on average, and some four times its root more.
+        near = b * 2 * v * _off(v) * (2 if "min_p" in kw else 1)
+        _check(G, x, t, u=u, most_open=2 + none_near + int(near + 4 * near ** 0.5), **kw)
 
 
 @pytest.mark.gpu
