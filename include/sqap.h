@@ -555,7 +555,7 @@ sqap_status sqap_cache8_read(const sqap_cache8 *cache, const int32_t *lengths, i
  * in [0, 1) (others are taken to the nearer end, NaN to 0).  token_out: device, [batch] int32.  prob_out: device, [batch]
  * binary32, or NULL: the probability with which the token was drawn, among those that stayed.
  * Masses are integers of 2^-40 of the largest (a token below that is never drawn), so sums are exact and every call gives
- * the same; a mass itself is off by 2^-36 of itself before it is rounded to such an integer.  No workspace; may be captured.
+ * the same; a mass itself is off by 2^-32 of itself before it is rounded to such an integer.  No workspace; may be captured.
  * EINVAL: null pointer, negative size, vocab < 1, ld < vocab.  EUNSUPPORTED: vocab > 1048576.
  */
 sqap_status sqap_sample(const sqap_f16 *logits, int64_t ld, int32_t batch, int32_t vocab, const float *temperature,

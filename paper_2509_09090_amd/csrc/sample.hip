@@ -34,7 +34,7 @@ __device__ __forceinline__ unsigned bin_of(unsigned key) { return kBins - 1 - (k
 
 // exp2((value - top) * per_nat) in units of 2^-40, a whole number in binary64 (whose multiply-adds run at binary32's rate, and no instruction
 // of binary32's exponential comes near what a vocabulary of equal shares needs: borders 2^-17 of the mass apart).  The difference is exact; the
-// power of two of its fraction, at most a half, is the Taylor series to the ninth power, off by less than 2^-37.  A top that is infinite
+// power of two of its fraction, at most a half, is the Taylor series to the eighth power, off by less than 2^-32.  A top that is infinite
 // is taken for a large number, and everything else to be far below.
 struct Mass {
     static constexpr float kCap = 131072.f;
@@ -46,9 +46,8 @@ struct Mass {
     }
     __device__ __forceinline__ double units(float value) const
     {
-        const double p = fmax(((double)fminf(value, kCap) - top) * per_nat, -64.0), n = rint(p), x = p - n;
-        double e = 1.0178086009239696e-07;                            // ln(2)^9 / 9!
-        e = fma(e, x, 1.3215486790144305e-06);
+        const double p = ((double)__builtin_amdgcn_fmed3f(value, -kCap, kCap) - top) * per_nat, n = rint(p), x = p - n;
+        double e = 1.3215486790144305e-06;                            // ln(2)^8 / 8!
         e = fma(e, x, 1.5252733804059838e-05);
         e = fma(e, x, 1.5403530393381606e-04);
         e = fma(e, x, 1.3333558146428441e-03);
@@ -57,7 +56,7 @@ struct Mass {
         e = fma(e, x, 2.402265069591007e-01);
         e = fma(e, x, 6.931471805599453e-01);
         e = fma(e, x, 1.0);
-        return rint(ldexp(e, (int)n + 40));
+        return rint(ldexp(e, max((int)n, -1000) + 40));               // (the conversion saturates)
     }
     static __device__ __forceinline__ u64 of(double w)                // (whole, below 2^52)
     {
@@ -135,15 +134,15 @@ struct alignas(16) SampleLds {
 
 // One workgroup per row; a wavefront has every 16th slab of 512 logits, eight to a lane.  CACHED: the row is kept in LDS
 // after the first pass; otherwise it is read again where it is needed, four slabs ahead.
-// What bounds it is the instructions of one compute unit: some 40 for each token where all of them count (128001 of them: 31 us, where
+// What bounds it is the instructions of one compute unit: some 28 for each token where all of them count (128001 of them: 30 us, where
 // the largest alone is found in 6), and the 16 wavefronts' share in every step that is not about the row, so that each step stands here once
 // and has few barriers.  First a bound is found below which nothing can stay: for top-k the k-th largest of the threads' maxima, for top-p alone
 // the point where the maxima of the lanes' eight have the mass that is asked for (the total has to be known first), for min-p its
 // own.  One pass collects the logits from there on in LDS in no order (all that follows is sums of integers), and the cut is found
 // among those, for top-k by counts and for top-p by masses: a histogram of 4096 bins, and of the 16 keys of the bin that holds the cut.  The masses
 // that stay are added up by slab, and the drawn token's slab alone is looked at again.  Where more stay than LDS has room for,
-// the passes go over the row.  A row of 32000: the largest 3.9 us, no filter 13.4, top-k 40 11.8, top-p 0.9 19.4, all three 17.0; of 128001:
-// 6.3, 37.7, 19.9, 56.2, 28.0, and 146 where the 97 in 100 that stay are tens of thousands.  (Full passes throughout, with the
+// the passes go over the row.  A row of 32000: the largest 3.6 us, no filter 12.9, top-k 40 11.7, top-p 0.9 19.0, all three 17.0; of 128001:
+// 6.4, 36.7, 19.9, 55.1, 27.9, and 141 where the 97 in 100 that stay are tens of thousands.  (Full passes throughout, with the
 // histogram of every token and masses in binary32: 28 and 99 us for all three and for top-p.)
 template <bool CACHED>
 __global__ __launch_bounds__(kSampleT) void sample_kernel(const SampleArgs a)

@@ -1,4 +1,4 @@
-"""Sampling from logits against the definition in 64 bits.  A mass is off by 2^-36 of itself at most (the series by 2^-37, the exponent's
+"""Sampling from logits against the definition in 64 bits.  A mass is off by 2^-32 of itself at most (the series by 2^-32.2, the exponent's
 product by 2^-53 of at most 41 binary places) and by 2^-41 of the largest, to which it is rounded; a sum of v of them by v times the latter, and
 it is compared with another such sum, of a total that is one at least.  Where a decision of the reference lies nearer than that to its
 border the row says nothing about the token; how many such rows there are is bounded too."""
@@ -12,7 +12,7 @@ from tests import lowbit_ref as R
 
 
 def _off(v):
-    return 2.0 ** -35 + v * 2.0 ** -40
+    return 2.0 ** -31 + v * 2.0 ** -40
 
 
 def test_refusals():
