@@ -517,8 +517,8 @@ sqap_status sqap_residual_add(sqap_f16 *X, int64_t ldx, const sqap_f16 *delta, i
  * All may be captured in a graph and replayed with other past, pos and starts.
  * EINVAL: null pointer, negative size, sizes of the cache that are not positive, H not a multiple of kv_heads, capacity
  * not a multiple of 64, a pitch too small, base <= 0, first < 0, workspace missing, too small or misaligned.
- * EUNSUPPORTED: head_dim not 64 or 128, more than 65535 sequences or key heads (times 16 query heads), operands or
- * pitches not 16-byte aligned (scales: 4).
+ * EUNSUPPORTED: head_dim not 64 or 128, more than 65535 sequences or key heads (times 16 query heads), max_new rows of the
+ * query heads to a key head (or all tiles of 128 of them) beyond 32 bits, operands or pitches not 16-byte aligned (scales: 4).
  */
 #define SQAP_CACHE8_BLOCK 64
 typedef struct sqap_cache8 {

@@ -793,9 +793,13 @@ sqap_status sqap_cache8_attention(const sqap_f16 *Q, int64_t ldq, const int32_t 
     s = check_rows16(who, "Q", Q, ldq, width);
     if (s == SQAP_OK) s = check_rows16(who, "O", O, ldo, width);
     if (s != SQAP_OK) return s;
+    max_new = max_new < rows ? max_new : rows;
+    const int64_t pairs = (int64_t)max_new * (H / cache->kv_heads);
+    if (pairs > INT32_MAX - 128 || (pairs + 127) / 128 * cache->kv_heads * cache->batch > INT32_MAX)
+        return fail(SQAP_EUNSUPPORTED, "%s: %d rows of %d heads", who, max_new, H);
     const DeviceOfCall device;
-    return launch_cache8_attention(reinterpret_cast<const __half *>(Q), ldq, starts, past, rows, max_new < rows ? max_new : rows, H, v,
-                                   cache->head_dim, reinterpret_cast<__half *>(O), ldo, as_stream(stream));
+    return launch_cache8_attention(reinterpret_cast<const __half *>(Q), ldq, starts, past, rows, max_new, H, v, cache->head_dim,
+                                   reinterpret_cast<__half *>(O), ldo, as_stream(stream));
 }
 
 size_t sqap_cache8_workspace_bytes(int32_t batch, int32_t H, int32_t kv_heads, int32_t head_dim, int32_t longest)

@@ -409,18 +409,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
     const int t = threadIdx.x, l = t & 63, wave = t >> 6, c = l & 31, h = l >> 5;
     const Span sp = span_of(starts, past, b, rows, max_new, cache.blocks * kBlock);
     const int G = H / cache.kv_heads;
-    const int64_t n_rows = (int64_t)sp.n * G, tile = (int64_t)(tiles - 1 - number) * TILE;
     if (!sp.fits) {                                                   // (of more than max_new rows too: all of them)
-        nan_rows<D>(O, ldo, sp.row, n_rows, G, kh, number, tiles, TILE);
+        nan_rows<D>(O, ldo, sp.row, (int64_t)sp.n * G, G, kh, number, tiles, TILE);
         return;
     }
+    const int n_rows = sp.n * G, tile = (tiles - 1 - number) * TILE;  // (the launch keeps max_new * G in 32 bits)
     if (tile >= n_rows) return;
-    const int64_t mine = tile + wave * 32 + c;
-    const int64_t mine_in = min(mine, n_rows - 1);
-    const int query = (int)(mine_in / G), head = kh * G + (int)(mine_in % G);
+    const int mine = tile + wave * 32 + c;
+    const int mine_in = min(mine, n_rows - 1);
+    const int query = mine_in / G, head = kh * G + mine_in % G;
     if (t == 0) not_finite = 0;
     const int end = sp.past + sp.n, sees = sp.past + query;           // last position that this lane's row sees
-    const int tile_last = sp.past + (int)((min(tile + TILE, n_rows) - 1) / G), n_blocks = tile_last / kBlock + 1;
+    const int tile_last = sp.past + (min(tile + TILE, n_rows) - 1) / G, n_blocks = tile_last / kBlock + 1;
     const int64_t kv_head = (int64_t)b * cache.kv_heads + kh;
     const __half *tail_k = cache.tail + kv_head * 2 * kBlock * D, *tail_v = tail_k + kBlock * D;
     const float *scales = cache.scales + kv_head * cache.blocks * 2;
@@ -496,7 +496,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
     float mrun = -INFINITY, lrun = 0.f;
     Unit unit;
     const float per_d = kLog2e / sqrtf((float)D);
-    const int wave_last = sp.past + (int)(min(tile + wave * 32 + 31, n_rows - 1) / G), wave_first = sp.past + (int)(min(tile + wave * 32, n_rows - 1) / G);
+    const int wave_last = sp.past + min(tile + wave * 32 + 31, n_rows - 1) / G, wave_first = sp.past + min(tile + wave * 32, n_rows - 1) / G;
     __syncthreads();
     fetch(0);
     keep(0);
@@ -757,17 +757,15 @@ __global__ __launch_bounds__(64 * kFewRowsWaves, 2) void cache8_few_rows_kernel(
     const int t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), r = l & 15, g = l >> 4;
     const Span sp = span_of(starts, past, b, rows, max_new, cache.blocks * kBlock);
     const int G = H / cache.kv_heads;
-    const int64_t n_rows = (int64_t)sp.n * G, tile = (int64_t)(tiles - 1 - number) * 16;
     if (!sp.fits) {
-        nan_rows<D>(O, ldo, sp.row, n_rows, G, kh, number, tiles, 16);
+        nan_rows<D>(O, ldo, sp.row, (int64_t)sp.n * G, G, kh, number, tiles, 16);
         return;
     }
+    const int n_rows = sp.n * G, tile = (tiles - 1 - number) * 16;
     if (tile >= n_rows) return;
-    auto query_of = [&](int64_t row) { return (int)(min(row, n_rows - 1) / G); };
-    auto place = [&](int64_t row) { return kh * G + (int)(min(row, n_rows - 1) % G); };
-    auto out_of = [&](int64_t row) { return O + (int64_t)(sp.row + query_of(row)) * ldo + (int64_t)place(row) * D; };
-    const int end = sp.past + sp.n, sees = sp.past + query_of(tile + r), first_sees = sp.past + query_of(tile);
-    const int n_blocks = (sp.past + query_of(tile + 15)) / kBlock + 1, tail_block = end / kBlock, tail_rows = end % kBlock;
+    const int mine = min(tile + r, n_rows - 1), query = mine / G, first_query = tile / G;
+    const int end = sp.past + sp.n, sees = sp.past + query, first_sees = sp.past + first_query;
+    const int n_blocks = (sp.past + (min(tile + 16, n_rows) - 1) / G) / kBlock + 1, tail_block = end / kBlock, tail_rows = end % kBlock;
     const int64_t head = (int64_t)b * cache.kv_heads + kh;
     const __half *tail_k = cache.tail + head * 2 * kBlock * D, *tail_v = tail_k + kBlock * D;
     v4i kraw[4 * C], vraw[DT];
@@ -788,7 +786,7 @@ __global__ __launch_bounds__(64 * kFewRowsWaves, 2) void cache8_few_rows_kernel(
     fetch_keys(wave);
     fetch_values(wave);
     v8h q[2 * C];
-    const __half *from = Q + (int64_t)(sp.row + query_of(tile + r)) * ldq + (int64_t)place(tile + r) * D;
+    const __half *from = Q + (int64_t)(sp.row + query) * ldq + (int64_t)(kh * G + mine - query * G) * D;
 #pragma unroll
     for (int m = 0; m < 2 * C; ++m) q[m] = *reinterpret_cast<const v8h *>(from + 64 * (m >> 1) + 16 * g + 8 * (m & 1));
     const bool has_tail = n_blocks - 1 == tail_block;
@@ -851,6 +849,7 @@ __global__ __launch_bounds__(64 * kFewRowsWaves, 2) void cache8_few_rows_kernel(
     __syncthreads();
     const int row = t / (D / 4), col = t % (D / 4) * 4;               // four columns of a row
     if (row >= 16 || tile + row >= n_rows) return;
+    const int of = (tile + row) / G;
     float top = -INFINITY, sum = 0.f;
     for (int w = 0; w < waves; ++w) top = fmaxf(top, lds.m[w][row]);
     v4f o = {0.f, 0.f, 0.f, 0.f};
@@ -867,14 +866,14 @@ __global__ __launch_bounds__(64 * kFewRowsWaves, 2) void cache8_few_rows_kernel(
         if (odd) {                                                    // infinities and NaN among the tail's values that this row sees
             x = __half2float(__float2half_rn(x));
 #pragma unroll 1
-            for (int s = 0; s <= sp.past + query_of(tile + row) - tail_block * kBlock; ++s) {
+            for (int s = 0; s <= sp.past + of - tail_block * kBlock; ++s) {
                 const float v = __half2float(tail_v[s * D + col + i]);
                 if (!(fabsf(v) <= 65504.f)) x += v;
             }
         }
         out.h[i] = __float2half_rn(x);
     }
-    *reinterpret_cast<v2u *>(out_of(tile + row) + col) = out.v;
+    *reinterpret_cast<v2u *>(O + (int64_t)(sp.row + of) * ldo + (int64_t)(kh * G + tile + row - of * G) * D + col) = out.v;
 }
 
 // ---------------------------------------------------------------- attention of one row per sequence
@@ -1272,8 +1271,8 @@ sqap_status launch_cache8_read(const Cache8View &cache, int d, const int32_t *le
 }
 
 // Tiles of 16 rows, whose blocks are dealt to eight wavefronts, where there would be few tiles of 128: 148 rows of 32 heads (64 of those) take
-// 9.2 us so and 11.1 otherwise, 512 of 8 heads (32) 8.1 and 18.7, 20 of 32 heads over 8 behind 2000 (8) 17 and 61, 1500 of 8 behind 2000
-// (96) 61 and 99, 300 of 32 heads (96) 14.7 and 15.2; but 500 of 32 (128) 25.0 and 21.6, 1000 of 32 over 8 (256) 56 and 36.
+// 8.7 us so and 11.1 otherwise, 512 of 8 heads (32) 7.6 and 18.7, 20 of 32 heads over 8 behind 2000 (8) 17 and 61, 1500 of 8 behind 2000
+// (96) 61 and 99, 300 of 32 heads (96) 13.7 and 15.2; but 500 of 32 (128) 25.0 and 21.6, 1000 of 32 over 8 (256) 56 and 36.
 constexpr int kFewTiles = 96;
 
 template <int D>
@@ -1292,7 +1291,6 @@ static sqap_status launch_attention_d(const __half *Q, int64_t ldq, const int32_
     const int64_t pairs = (int64_t)cache.kv_heads * cache.batch;
     const bool few = tiles_of(32 * WAVES) * pairs <= kFewTiles;
     const int64_t tiles = tiles_of(few ? 16 : 32 * WAVES), items = tiles * pairs;
-    if (items > INT32_MAX) return fail(SQAP_EUNSUPPORTED, "sqap_cache8_attention: %lld tiles of rows", (long long)items);
     if (few)
         hipLaunchKernelGGL(cache8_few_rows_kernel<D>, dim3((unsigned)items), dim3(64 * kFewRowsWaves), sizeof(FewRowsLds<D>), st, Q, ldq, starts, past, rows,
                            max_new, H, cache, O, ldo, (int)tiles);

@@ -46,7 +46,8 @@ def test_attention_refusals():
     for bad in (dict(rows=-1), dict(max_new=-1), dict(H=-4), dict(H=5), dict(cache=None), dict(Q=None), dict(starts=None), dict(past=None),
                 dict(O=None), dict(ldq=255), dict(ldo=8), dict(cache=_desc(capacity=65))):
         assert call(**bad) == B.EINVAL, bad
-    for bad in (dict(Q=ODD), dict(O=ODD), dict(ldo=260), dict(cache=_desc(head_dim=96))):
+    for bad in (dict(Q=ODD), dict(O=ODD), dict(ldo=260), dict(cache=_desc(head_dim=96)), dict(rows=2 ** 30, max_new=2 ** 30),
+                dict(rows=2 ** 30 - 64, max_new=2 ** 30 - 64, cache=_desc(batch=65535))):
         assert call(**bad) == B.EUNSUPPORTED, bad
     assert call(rows=0) == B.OK
 
@@ -132,18 +133,24 @@ class Model:
         y = self.turned(x, pos)
         starts = G.to_dev(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32))
         past = G.to_dev(self.past)
-        q = t.full((total, self.H * self.d), 9.0, dtype=t.float16, device=G.DEV)
-        o = t.full((total, self.H * self.d), 9.0, dtype=t.float16, device=G.DEV)
-        rows = G.to_dev(x.reshape(total, -1))
-        before = rows.clone()
         most = max(self.most, int(max(counts)) if len(counts) else 0)
-        B.sqap_cache8_append(rows, starts, G.to_dev(np.asarray(pos, dtype=np.int32)), past, self.cache, self.H, most, Q_out=q)
+        padded = max(total, self.most)                                    # (rows behind the last sequence)
+        q = t.full((padded, self.H * self.d), 9.0, dtype=t.float16, device=G.DEV)
+        o = t.full((padded, self.H * self.d), 9.0, dtype=t.float16, device=G.DEV)
+        rows = t.full((padded, (self.H + 2 * self.kv) * self.d), float("nan"), dtype=t.float16, device=G.DEV)
+        rows[:total] = G.to_dev(x.reshape(total, -1))
+        at = t.zeros(padded, dtype=t.int32, device=G.DEV)
+        at[:total] = G.to_dev(np.asarray(pos, dtype=np.int32))
+        before = rows.clone()
+        B.sqap_cache8_append(rows, starts, at, past, self.cache, self.H, most, Q_out=q)
         assert t.equal(rows.view(t.int16), before.view(t.int16))
-        assert np.array_equal(q.cpu().numpy().view(np.uint16), y[:, :self.H].reshape(total, -1).view(np.uint16))
+        assert np.array_equal(q[:total].cpu().numpy().view(np.uint16), y[:, :self.H].reshape(total, -1).view(np.uint16))
         self.note(counts, y)
         if attend:
             B.sqap_cache8_attention(q, starts, past, self.cache, self.H, most, o)
-            self.check(o.cpu().numpy(), y, counts, True)
+            self.check(o[:total].cpu().numpy(), y, counts, True)
+            assert bool((o[total:] == 9).all())
+        assert bool((q[total:] == 9).all())
         self.past = (self.past + np.asarray(counts)).astype(np.int32)
         return y
 
