@@ -385,7 +385,7 @@ __device__ __forceinline__ void nan_rows(__half *O, int64_t ldo, int first, int6
 // that a block of keys and values is taken from memory and made halves once for all of them.  Everything is transposed (scores:
 // positions x rows), as in attention.hip: probabilities are the second product's operand where they were computed.
 // What bounds it is the vector ALU beside the matrix cores, 305 instructions to 32 matrix instructions per wavefront and block, a fifth of them
-// exponentials: 1500, 1115 and 1446 rows of 32 heads over 8 behind 2000, 1994 and 420 positions in 232 us, 0.61 PFLOP/s (a library product of
+// exponentials: 1500, 1115 and 1446 rows of 32 heads over 8 behind 2000, 1994 and 420 positions in 223 us, 0.63 PFLOP/s (a library product of
 // halves reaches 1.24), the matrix cores busy for 29 in 100.  (The next block's scores multiplied between this one's probabilities, in the same
 // wavefront: 335 us, the registers do not suffice.)
 // A block's p = 2^(s - m) times its factor is one exponential, of s sk + (log2 factor - m); the sum of the probabilities is put right by the
@@ -515,6 +515,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
         if (j * kBlock <= wave_last) {
             const uint8_t *kt = lds + (j & 1) * BUF + l * 16, *vt = kt + kBlock * D * 2;
             v16f s[2];
+            __builtin_amdgcn_s_setprio(1);                            // (before the other workgroup's exponentials: 231 -> 223 us)
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt) {
 #pragma unroll
@@ -523,6 +524,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
                 for (int m = 0; m < NP; ++m)
                     s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const v8h *>(kt + (tt * NP + m) * 1024), qf[m], s[tt], 0, 0, 0);
             }
+            __builtin_amdgcn_s_setprio(0);
             if ((j + 1) * kBlock - 1 > wave_first) {                  // some row does not see some position
                 const int last = sees - j * kBlock - 4 * h;
 #pragma unroll
