@@ -88,7 +88,7 @@ __device__ __forceinline__ void rotate_pair(__half lo, __half hi, double cs, dou
     out_hi = __float2half_rn((float)(b * cs + a * sn));
 }
 
-// Sine and cosine of an angle of at most some 2^31, in binary64: the nearest multiple of pi / 2 is taken off in two parts of 53 bits (each
+// Sine and cosine of an angle below some 2^50, in binary64: the nearest multiple of pi / 2 is taken off in two parts of 53 bits (each
 // product exact inside its multiply-add), what is left is at most pi / 4, where the Taylor series to the 15th and 16th power are off by
 // less than half a unit of the last place of the larger one.  Without branches, so that a thread's pairs run side by side: a quarter of the
 // instructions of the library's, which also serves angles beyond.
@@ -110,7 +110,7 @@ __device__ __forceinline__ void sincos_of(double a, double &sn, double &cs)
     c = fma(c, z, kSeries[14]);
     s = fma(s * z, r, r);
     c = fma(c, z, 1.0);
-    const int q = (int)n;
+    const int q = (int)fma(-4.0, floor(0.25 * n), n);                 // (n itself may be beyond an integer)
     const double x = q & 1 ? c : s, y = q & 1 ? s : c;
     sn = q & 2 ? -x : x;
     cs = (q + 1) & 2 ? -y : y;

@@ -43,22 +43,23 @@ class LayerBuffers:
     """Scratch tensors for up to max_rows token rows of one layer call (reused by every layer).
 
     kv_width: width of the keys (of the values), where heads of a Cache8 are shared; mx4: for layers of Mx4Weight;
-    cache8_workspace: bytes of sqap_cache8_workspace_bytes for the decode calls over a Cache8."""
+    cache8_workspace: for calls over a Cache8, the bytes of sqap_cache8_workspace_bytes for its decode calls (0: none)."""
 
-    def __init__(self, max_rows, hidden, ffn, device="cuda", kv_width=None, mx4=False, cache8_workspace=0):
+    def __init__(self, max_rows, hidden, ffn, device="cuda", kv_width=None, mx4=False, cache8_workspace=None):
         f16, u8 = torch.float16, torch.uint8
         kv_width = hidden if kv_width is None else kv_width
         self.hidden, self.ffn = hidden, ffn
         self.xq = torch.empty((max_rows, hidden // 2), dtype=u8, device=device)
         self.sx = torch.empty((max_rows,), dtype=f16, device=device)
         self.qkv = torch.empty((max_rows, hidden + 2 * kv_width), dtype=f16, device=device)
-        self.q = torch.empty((max_rows, hidden), dtype=f16, device=device)      # rotated queries of prompts over a Cache8
         self.attn = torch.empty((max_rows, hidden), dtype=f16, device=device)
         self.o = torch.empty((max_rows, hidden), dtype=f16, device=device)
         self.gu = torch.empty((max_rows, 2 * ffn), dtype=f16, device=device)
         self.hq = torch.empty((max_rows, ffn // 2), dtype=u8, device=device)
         self.sh = torch.empty((max_rows,), dtype=f16, device=device)
-        self.cache8_ws = torch.zeros((cache8_workspace,), dtype=u8, device=device)
+        if cache8_workspace is not None:
+            self.q = torch.empty((max_rows, hidden), dtype=f16, device=device)  # rotated queries of prompts
+            self.cache8_ws = torch.zeros((cache8_workspace,), dtype=u8, device=device)
         if mx4:
             self.y = torch.empty((max_rows, hidden), dtype=f16, device=device)
             self.h = torch.empty((max_rows, ffn), dtype=f16, device=device)

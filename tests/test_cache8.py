@@ -421,6 +421,50 @@ def test_pitches_and_queries_in_place(G):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("H,kv,n,behind", [(4, 2, 75, 0), (8, 8, 300, 100), (32, 32, 500, 0)])
+def test_outputs_over_the_queries(G, H, kv, n, behind):
+    import torch
+    m = Model(G, 1, H, kv, 64, 64 * 9, seed=n)
+    if behind:
+        m.append([behind])
+    x = G.to_dev(m.rows(n).reshape(n, -1))
+    starts, past, pos = (G.to_dev(np.asarray(a, dtype=np.int32)) for a in ([0, n], [behind], behind + np.arange(n)))
+    B.sqap_cache8_append(x, starts, pos, past, m.cache, H, n, Q_out=x[:, :H * 64])
+    apart = torch.empty((n, H * 64), dtype=torch.float16, device=G.DEV)
+    B.sqap_cache8_attention(x[:, :H * 64], starts, past, m.cache, H, n, apart)
+    B.sqap_cache8_attention(x[:, :H * 64], starts, past, m.cache, H, n, x[:, :H * 64])
+    assert torch.equal(x[:, :H * 64], apart) and bool(torch.isfinite(apart).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("base", [1e-3, 0.5, 1.0, 1e6])
+def test_far_positions_and_other_bases(G, base):
+    """Queries and keys turned as by sqap_rope, up to the last position that 32 bits hold and beyond 2^31 turns."""
+    import torch
+    H, kv, d, n = 2, 1, 64, 256
+    rng = np.random.default_rng(int(base * 1000) % 97)
+    x = G.to_dev(rng.standard_normal((n, (H + 2 * kv) * d)).astype(np.float16))
+    pos = rng.integers(0, 2 ** 31, n)
+    pos[:4] = 2 ** 31 - 1, 0, 1, 2 ** 31 - 2
+    pos = G.to_dev(pos.astype(np.int32))
+    want = x.clone()
+    B.sqap_rope(want[:, :(H + kv) * d], pos, H + kv, d, base)
+    cache, q = B.Cache8(1, 320, kv, d, device=G.DEV), torch.empty((n, H * d), dtype=torch.float16, device=G.DEV)
+    one = lambda *a: G.to_dev(np.asarray(a, dtype=np.int32))              # noqa: E731
+    B.sqap_cache8_append(x, one(0, n), pos, one(0), cache, H, n, Q_out=q, base=base)
+    assert torch.equal(q, want[:, :H * d])
+    k = want[:, H * d:(H + 1) * d].cpu().numpy()
+    out = torch.empty((n, 2 * d), dtype=torch.float16, device=G.DEV)
+    B.sqap_cache8_read(cache, one(n), 0, n, out)
+    assert np.array_equal(out[:, :d].cpu().numpy(), np.float32(R.held(k)).astype(np.float16))
+    o, ws = torch.empty((1, H * d), dtype=torch.float16, device=G.DEV), torch.zeros(0, dtype=torch.uint8, device=G.DEV)
+    B.sqap_cache8_decode_attention(x[5:6], pos[:1], one(n), cache, H, o, ws, n + 1, base=base)
+    row = x[5:6].clone()
+    B.sqap_rope(row[:, :(H + kv) * d], pos[:1], H + kv, d, base)
+    assert torch.equal(cache.tail[0, 0, 0, 0], row[0, H * d:(H + 1) * d])
+
+
+@pytest.mark.gpu
 def test_replayed_with_growing_lengths(G):
     """A captured single-row step is replayed with the lengths that the device holds; eager steps of another cache between."""
     import torch
