@@ -18,7 +18,7 @@ typedef unsigned long long u64;
 constexpr int kSampleT = 1024, kSampleWaves = kSampleT / 64, kSlab = 64 * 8;
 constexpr int kSampleCached = 32768;                                  // logits that are kept in LDS
 constexpr int kBins = 4096;                                           // of 16 keys each
-constexpr int kListed = 8192;                                         // candidates that are kept in LDS
+constexpr int kFlat = 4;                                              // (see its use)
 constexpr int kTieShift = 52;                                         // a slab's ties above its mass, which has 50 bits at most
 constexpr unsigned kKeyMinusInf = 0x03ffu;                            // the lowest key there is
 
@@ -119,7 +119,10 @@ struct SampleArgs {
     float *prob;
 };
 
+// kListed: candidates that are kept; the row itself takes the place of two thirds of them where it is kept too
+template <bool CACHED>
 struct alignas(16) SampleLds {
+    static constexpr int kListed = CACHED ? 8192 : 24576;
     v4u last[64];                        // the last slab, with minus infinity behind its end
     u64 bins[kBins];                     // masses or counts by key / 16, the largest first
     u64 keys[16];                        // counts of one bin's
@@ -142,15 +145,17 @@ struct alignas(16) SampleLds {
 // among those, for top-k by counts and for top-p by masses: a histogram of 4096 bins, and of the 16 keys of the bin that holds the cut.  The masses
 // that stay are added up by slab, and the drawn token's slab alone is looked at again.  Where more stay than LDS has room for,
 // the passes go over the row.  A row of 32000: the largest 3.6 us, no filter 12.9, top-k 40 11.7, top-p 0.9 19.0, all three 17.0; of 128001:
-// 6.4, 36.7, 19.9, 55.1, 27.9, and 141 where the 97 in 100 that stay are tens of thousands.  (Full passes throughout, with the
+// 6.4, 36.8, 20.0, 54.6, 28.0, and 114 where the 97 in 100 that stay are tens of thousands.  (Full passes throughout, with the
 // histogram of every token and masses in binary32: 28 and 99 us for all three and for top-p.)
 template <bool CACHED>
 __global__ __launch_bounds__(kSampleT) void sample_kernel(const SampleArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) uint8_t raw_lds[];
-    SampleLds &lds = *reinterpret_cast<SampleLds *>(raw_lds);
-    v4u *cached = reinterpret_cast<v4u *>(raw_lds + sizeof(SampleLds));
-    u64 *slab_sum = reinterpret_cast<u64 *>(raw_lds + sizeof(SampleLds) + (CACHED ? (size_t)a.slabs * kSlab * 2 : 0));
+    using Lds = SampleLds<CACHED>;
+    constexpr int kListed = Lds::kListed;
+    Lds &lds = *reinterpret_cast<Lds *>(raw_lds);
+    v4u *cached = reinterpret_cast<v4u *>(raw_lds + sizeof(Lds));
+    u64 *slab_sum = reinterpret_cast<u64 *>(raw_lds + sizeof(Lds) + (CACHED ? (size_t)a.slabs * kSlab * 2 : 0));
     const int b = blockIdx.x, t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const unsigned short *row = reinterpret_cast<const unsigned short *>(a.logits + (int64_t)b * a.ld);
     const int slabs = a.slabs, last = slabs - 1;
@@ -342,9 +347,14 @@ __global__ __launch_bounds__(kSampleT) void sample_kernel(const SampleArgs a)
     bool some = false;                                                // (only some of the cut's key stay: they have to be told apart)
     float from = lowest;
     const bool plain = !k && !by_mass && !(m_given > 0.f);
-    // masses of the row from `from` on, except for those of `tie_half`: by slab in `slab_sum`, with the number of ties; `max_bins`: each eight's
-    // maximum by its key; `all_bins`: each by its key (or each as one).  The lane's sum is returned.
-    auto masses = [&](unsigned tie_half, bool max_bins, bool all_bins, bool counting) {
+    // masses of the row from `from` on, except for those of `tie_half`: by slab in `slab_sum`, with the number of ties; kMaxima: each eight's
+    // maximum by its key; kAll: each by its key (or each as one).  The lane's sum is returned.
+    enum { kNone, kMaxima, kAll };
+    const std::integral_constant<int, kNone> no_bins;
+    const std::integral_constant<int, kMaxima> maxima;
+    const std::integral_constant<int, kAll> all_bins;
+    auto masses = [&](auto bins_c, unsigned tie_half, bool counting) {
+        constexpr int BINS = decltype(bins_c)::value;
         u64 mine = 0;
         const float above = tie_half < 0x10000u ? value_of(key_of(tie_half) + 1) : from;
         each_slab([&](int s, const v4u &v) {
@@ -352,14 +362,19 @@ __global__ __launch_bounds__(kSampleT) void sample_kernel(const SampleArgs a)
             unsigned ties = 0;
             const float m = largest(v);
             if (__any(m >= from)) {
-                double eight = 0.0;                                   // (exact)
+                double w[8], eight = 0.0;                             // (exact)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const unsigned h = half_at(v, e);
-                    double w = counting ? 1099511627776.0 : mass.units(float_of(h));
-                    w = float_of(h) >= above ? w : 0.0;
-                    if (all_bins && w > 0.0) atomicAdd(&lds.bins[bin_of(key_of(h))], mass.of(w));
-                    eight += w;
+                    const float value = float_of(half_at(v, e));
+                    w[e] = BINS == kAll && counting ? 1099511627776.0 : mass.units(value);
+                    w[e] = value >= above ? w[e] : 0.0;
+                    eight += w[e];
+                }
+                if constexpr (BINS == kAll) {                         // (behind the last of them: a branch in between would part their chains)
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (w[e] > 0.0) atomicAdd(&lds.bins[bin_of(key_of(half_at(v, e)))], mass.of(w[e]));
                 }
                 if (tie_half < 0x10000u) {
 #pragma unroll
@@ -369,7 +384,7 @@ __global__ __launch_bounds__(kSampleT) void sample_kernel(const SampleArgs a)
                 mine += sum;
                 sum = ((u64)wave_total((unsigned)(sum >> 20)) << 20) + wave_total((unsigned)sum & 0xfffffu);
                 if (tie_half < 0x10000u) ties = wave_total(ties);
-                if (max_bins) {
+                if constexpr (BINS == kMaxima) {
                     const u64 w = mass(m);
                     if (w) atomicAdd(&lds.bins[bin_of(key_of_value(m))], w);
                 }
@@ -379,6 +394,11 @@ __global__ __launch_bounds__(kSampleT) void sample_kernel(const SampleArgs a)
         return mine;
     };
     constexpr unsigned kNoHalf = 0x10000u;
+    // Top-p alone, where the threads' maxima are several times the largest: more tokens are likely to stay than LDS has room for, and the first
+    // pass over the masses leaves the histogram of them all, instead of that of the eights' maxima and a second pass (rows of 128001 of which
+    // tens of thousands stay: 107 to 114 us, 141 without; where few stay all the same, 17 us more).
+    const bool flat = by_mass && !k && block_scan(mass(mine), front) > (u64)kFlat << 40;
+    int bin = -1;
     for (bool final = plain;; final = true) {
         // ---- what stays, by slab; the first time (top-p alone) all
         if (final || (by_mass && !k)) {
@@ -388,8 +408,12 @@ __global__ __launch_bounds__(kSampleT) void sample_kernel(const SampleArgs a)
                     const u64 add = some && key == cut ? 1ull << kTieShift : mass(value_of(key));
                     if (add && value_of(key) >= from) atomicAdd(&slab_sum[lds.list[i] >> 16], add);
                 }
+            } else if (final) {
+                masses(no_bins, some ? half_of(cut) : kNoHalf, false);
+            } else if (flat) {
+                masses(all_bins, kNoHalf, false);
             } else {
-                masses(some ? half_of(cut) : kNoHalf, !final, false, false);
+                masses(maxima, kNoHalf, false);
             }
             __syncthreads();
         }
@@ -411,13 +435,13 @@ __global__ __launch_bounds__(kSampleT) void sample_kernel(const SampleArgs a)
             target = min(total, max(1ull, p_given > 0.f ? (u64)ceil((double)p_given * (double)total) : 1ull));
         }
         if (by_mass || k) {
-            const int bin = first_bin(target);
+            bin = first_bin(target);
             if (bin > (int)(kKeyMinusInf >> 4)) from = value_of((unsigned)bin << 4);
         } else {
             from = min_value;
         }
         // ---- what is not below it
-        if (k <= kListed) {
+        if (k <= kListed && (from > lowest || a.vocab <= kListed)) {
             bool room = true;
             each_slab([&](int s, const v4u &v) {
                 unsigned bits = room && largest(v) >= from ? from_bits(v, from) : 0;
@@ -440,7 +464,9 @@ __global__ __launch_bounds__(kSampleT) void sample_kernel(const SampleArgs a)
         for (int round = k ? 0 : 1; round < (by_mass ? 2 : 1); ++round) {
             const bool counting = round == 0;
             u64 kept = 0;
-            if (listed) {
+            if (flat) {
+                // (the bound's bin is the cut's)
+            } else if (listed) {
                 for (unsigned i = t; i < n_listed; i += kSampleT) {
                     const unsigned key = lds.list[i] & 0xffffu;
                     const u64 w = value_of(key) < from || (cut && key == cut) ? 0 : counting ? 1 : mass(value_of(key));
@@ -448,7 +474,7 @@ __global__ __launch_bounds__(kSampleT) void sample_kernel(const SampleArgs a)
                     if (w) atomicAdd(&lds.bins[bin_of(key)], w);
                 }
             } else {
-                kept = masses(cut ? half_of(cut) : kNoHalf, false, true, counting);
+                kept = masses(all_bins, cut ? half_of(cut) : kNoHalf, counting);
             }
             if (!counting && k) {
                 const u64 ties = cut ? cut_count * mass(value_of(cut)) : 0;
@@ -457,7 +483,7 @@ __global__ __launch_bounds__(kSampleT) void sample_kernel(const SampleArgs a)
                 target = min(total, max(1ull, p_given > 0.f ? (u64)ceil((double)p_given * (double)total) : 1ull));
             }
             if (counting && !listed) target <<= 40;
-            const int bin = first_bin(target);
+            if (!flat) bin = first_bin(target);
             if (bin < 0) continue;                                    // (fewer tokens than k can be drawn: all of them stay)
             const u64 rest = counting && !listed ? (target - lds.before) >> 40 : target - lds.before;
             const float low = bin > (int)(kKeyMinusInf >> 4) ? fmaxf(from, value_of((unsigned)bin << 4)) : from;
@@ -567,11 +593,13 @@ sqap_status launch_sample(const __half *logits, int64_t ld, int batch, int vocab
     const int slabs = (vocab + kSlab - 1) / kSlab;
     const SampleArgs a = {logits, ld, vocab, slabs, temperature, top_p, min_p, uniform, top_k, token, prob};
     const bool cached = vocab <= kSampleCached;
-    const size_t lds = sizeof(SampleLds) + (size_t)slabs * sizeof(u64) + (cached ? (size_t)slabs * kSlab * 2 : 0);
+    const size_t lds = (size_t)slabs * sizeof(u64) + (cached ? sizeof(SampleLds<true>) + (size_t)slabs * kSlab * 2 : sizeof(SampleLds<false>));
     static std::atomic<bool> ready[kMaxDeviceSlots];
     if (!ready[device_slot()].load(std::memory_order_relaxed)) {
-        const int most = sizeof(SampleLds) + kSampleCached * 2 + kSampleMaxVocab / kSlab * (int)sizeof(u64);
-        SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(sample_kernel<true>), hipFuncAttributeMaxDynamicSharedMemorySize, most));
+        constexpr int most_cached = sizeof(SampleLds<true>) + kSampleCached * 2 + kSampleCached / kSlab * sizeof(u64);
+        constexpr int most = sizeof(SampleLds<false>) + kSampleMaxVocab / kSlab * sizeof(u64);
+        static_assert(most_cached <= 163840 && most <= 163840, "a compute unit's LDS");
+        SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(sample_kernel<true>), hipFuncAttributeMaxDynamicSharedMemorySize, most_cached));
         SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(sample_kernel<false>), hipFuncAttributeMaxDynamicSharedMemorySize, most));
         ready[device_slot()].store(true, std::memory_order_relaxed);
     }
