@@ -290,8 +290,8 @@ SQAP_METHOD(attention, 8, attention_call(c, a))
 
 #define SQAP_CALLS(X)                                                                                                                   \
     X(attn_scores_batch) X(prune_topk) X(kept_rows) X(prune_rows) X(prune_select) X(quantize_act) X(rmsnorm_quantize_act)              \
-    X(swiglu_quantize_act) X(rope) X(rope_append) X(attention) X(decode_attention) X(w4a4_linear) X(mx4_quantize) X(mx4_linear) X(cache8_append) X(cache8_attention)                              \
-    X(cache8_decode_attention) X(sample) X(group_run) X(decoder_step)
+    X(swiglu_quantize_act) X(rope) X(rope_append) X(attention) X(decode_attention) X(w4a4_linear) X(mx4_quantize) X(mx4_linear)        \
+    X(cache8_append) X(cache8_attention) X(cache8_decode_attention) X(sample) X(group_run) X(decoder_step)
 
 PyMethodDef methods[] = {
 #define SQAP_ENTRY(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(m_##NAME)), METH_FASTCALL, nullptr},
