@@ -506,7 +506,8 @@ sqap_status sqap_residual_add(sqap_f16 *X, int64_t ldx, const sqap_f16 *delta, i
  * enters as the sum of two).  Same cache as by sqap_cache8_append.  longest: the most positions that a sequence
  * has, the new one included, as far as the host knows; it decides how the work is split, nothing else.  workspace: at least
  * sqap_cache8_workspace_bytes(batch, H, kv_heads, head_dim, longest) bytes, 16-byte aligned (may be NULL when that is 0); its
- * first 4 * batch * H bytes (counters) must be ZERO before its first use, every call leaves them zero.
+ * first 16384 bytes (counters) must be ZERO before its first use, every call leaves them zero; calls of any sizes may
+ * follow each other on one that is large enough for each.
  * Calls that share a workspace must be ordered on one stream; graphs that are replayed side by side need one each.
  *
  * sqap_cache8_read: positions first .. first + count - 1 of every sequence as halves (codes times scale, rounded once),

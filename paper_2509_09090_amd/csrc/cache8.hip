@@ -1329,15 +1329,17 @@ static int decode_shares(int batch, int H, int kv_heads, int longest)
     return (int)std::max<int64_t>(1, std::min<int64_t>({wanted, kDecodeGroups / items, kMaxShares}));
 }
 
-// counters in front: room for one per sequence and query head (a workgroup uses one)
-static size_t counter_bytes(int batch, int H) { return ((size_t)batch * H * 4 + 255) / 256 * 256; }
+// Counters in front, one for each sequence, key head and 16 of its query heads; where there is more than one share, that is 256 of them at
+// most.  The room for them is the same whatever the sizes: no call's sums lie where another's counters are.
+constexpr size_t kCounterBytes = 16384;
+static_assert(kCounterBytes >= kDecodeGroups / 2 * sizeof(unsigned), "a counter for each item that is shared");
 
 size_t cache8_workspace_bytes(int batch, int H, int kv_heads, int d, int longest)
 {
     const int shares = decode_shares(batch, H, kv_heads, longest), G = H / kv_heads;
     if (shares == 1) return 0;
     const size_t items = (size_t)batch * kv_heads * ((G + 15) / 16);
-    return counter_bytes(batch, H) + items * shares * heads_of_partial(G) * (d + 2) * 4;
+    return kCounterBytes + items * shares * heads_of_partial(G) * (d + 2) * 4;
 }
 
 sqap_status launch_cache8_decode(const __half *QKV, int64_t ld, const int32_t *pos, const int32_t *past, int H, double base, const Cache8View &cache,
@@ -1357,7 +1359,7 @@ sqap_status launch_cache8_decode(const __half *QKV, int64_t ld, const int32_t *p
     a.O = O;
     a.ldo = ldo;
     a.counters = static_cast<unsigned *>(workspace);
-    a.partials = reinterpret_cast<float *>(static_cast<char *>(workspace) + counter_bytes(cache.batch, H));
+    a.partials = reinterpret_cast<float *>(static_cast<char *>(workspace) + kCounterBytes);
     a.freq = rope_frequencies(d, base);
     const dim3 grid(a.shares, cache.kv_heads * a.chunks, cache.batch);
     if (d == 64) hipLaunchKernelGGL(cache8_decode_kernel<64>, grid, dim3(64 * kDecodeWaves), 0, st, a);

@@ -437,6 +437,23 @@ def test_outputs_over_the_queries(G, H, kv, n, behind):
 
 
 @pytest.mark.gpu
+def test_one_workspace_for_calls_of_all_sizes(G):
+    """Calls of other batches, heads and lengths follow each other on one workspace, zeroed once: the sums of a small batch stay away from the
+    counters of a large one."""
+    import torch
+    models = [Model(G, batch, H, kv, d, 64 * 48, seed=batch) for batch, H, kv, d in ((1, 8, 8, 128), (16, 32, 4, 64), (3, 4, 1, 128), (5, 40, 1, 64))]
+    for m in models:
+        m.append([2000 + 40 * b for b in range(len(m.past))], attend=False)
+    size = max(B.sqap_cache8_workspace_bytes(len(m.past), m.H, m.kv, m.d, 64 * 40) for m in models)
+    ws = torch.full((size,), 0xA5, dtype=torch.uint8, device=G.DEV)
+    ws[:16384] = 0
+    for m in models + models[::-1]:
+        assert B.sqap_cache8_workspace_bytes(len(m.past), m.H, m.kv, m.d, 64 * 40) > 16384
+        m.decode(longest=64 * 40, workspace=ws)
+    assert int(ws[:16384].max()) == 0
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("base", [1e-3, 0.5, 1.0, 1e6])
 def test_far_positions_and_other_bases(G, base):
     """Queries and keys turned as by sqap_rope, up to the last position that 32 bits hold and beyond 2^31 turns."""
