@@ -138,7 +138,7 @@ __device__ __forceinline__ int value_at(int s) { return ((s >> 2) & 3) << 4 | (s
 __device__ __forceinline__ int value_byte(int x, int at) { return x * 64 + ((at >> 4) + (x >> 3) & 3) * 16 + (at & 15); }
 __device__ __forceinline__ int value_piece(int u) { const int x = (u >> 6) * 16 + (u & 15); return x * 64 + (((u >> 4) & 3) + (x >> 3) & 3) * 16; }
 
-constexpr int kAppendGroups = 512, kAppendSplit = 96;
+constexpr int kAppendGroups = 512, kAppendSplit = 96, kAppendValues = 256;
 // One workgroup per sequence, `share` key heads and block that the new rows touch (the first and the last of them together: the one reads
 // the tail that the other writes).  The block's angles are evaluated once, into LDS.  Then, head by head: keys, D / 16 threads per position with 8
 // pairs of columns (i, i + D / 2) each; the same threads turn the query heads that share the key head, and take the value row, whose codes
@@ -158,8 +158,8 @@ __global__ __launch_bounds__(4 * D, 2) void cache8_append_kernel(const __half *_
     const Span sp = span_of(starts, past, b, rows, max_new, cache.blocks * kBlock);
     if (!sp.fits) return;
     const int end = sp.past + sp.n, first = sp.past / kBlock, last = (end - 1) / kBlock, G = H / cache.kv_heads;
-    // what this workgroup does of its heads: 1 keys, 2 values, 4 queries
-    const int groups = (cache.kv_heads + share - 1) / share, group = blockIdx.y % groups, does = split ? 1 << (blockIdx.y / groups) : 7;
+    // what this workgroup does of its heads: 1 keys, 2 values, 4 queries; one of three alone, values or the others, or all
+    const int groups = (cache.kv_heads + share - 1) / share, group = blockIdx.y % groups, role = blockIdx.y / groups, does = split == 3 ? 1 << role : split == 2 ? 5 - 3 * role : 7;
     const int head0 = group * share, heads = min(share, cache.kv_heads - head0);
     int block = first + (int)blockIdx.x;
     const bool keys = does & 1, values = does & 2, queries = Q_out && (does & 4);
@@ -1252,11 +1252,12 @@ static sqap_status launch_append_d(const __half *QKV, int64_t ld, const int32_t 
     // heads that share a workgroup's angles: as many as leave the device its workgroups.  Where there are
     // few, keys, values and queries have workgroups of their own: each is a chain of its own, but keys and queries work out the same
     // angles (148 rows of 8 key and 32 query heads, 32 of them: 15.3 us together, 10.3 apart; 512 of 8, 72: 8.7 and 7.2; 148 of 32, 128: 8.9 and 9.5).
+    // With some more, values alone are apart (148 rows of 32 heads: 8.1 us; 900 of 8, 128: 11.6 together and 10.7; but three prompts, 600: 29.6 and 32.7).
     // Angles for more than one head: 2000 rows of 32 heads 25.0 us with 512 workgroups, 35.5 with 256, 27.8 with 1024.
     const int64_t items = (int64_t)columns * cache.batch * cache.kv_heads;
     const int share = (int)std::max<int64_t>(1, std::min<int64_t>(cache.kv_heads, items / kAppendGroups));
-    const int split = items <= kAppendSplit ? 1 : 0;
-    hipLaunchKernelGGL(cache8_append_kernel<D>, dim3(columns, (cache.kv_heads + share - 1) / share * (split ? 3 : 1), cache.batch), dim3(4 * D), LDS, st, QKV, ld,
+    const int split = items <= kAppendSplit ? 3 : items <= kAppendValues ? 2 : 1;
+    hipLaunchKernelGGL(cache8_append_kernel<D>, dim3(columns, (cache.kv_heads + share - 1) / share * split, cache.batch), dim3(4 * D), LDS, st, QKV, ld,
                        starts, pos, past, rows, max_new, H, share, split, cache, Q_out, ldq, rope_frequencies(D, base));
     SQAP_HIP_CHECK(hipGetLastError());
     return SQAP_OK;
