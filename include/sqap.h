@@ -498,8 +498,8 @@ sqap_status sqap_residual_add(sqap_f16 *X, int64_t ldx, const sqap_f16 *delta, i
  * sqap_cache8_attention: causal attention of rotated queries Q [rows, H d] over what the cache holds after the rows have
  * been appended: query j of sequence b sees positions 0 .. past[b] + j,
  *   o = sum_t softmax_t((q . k_t) / sqrt(d)) v_t,
- * scores, maximum and sums in binary32 (in an order that rows and max_new decide), probabilities rounded to half for the
- * second product, O [rows, H d] (pitch ldo), which may be Q.
+ * scores, maximum and sums in binary32 (in an order that rows and max_new decide); a probability enters the second product as
+ * the sum of two halves.  O [rows, H d] (pitch ldo) may be Q.
  *
  * sqap_cache8_decode_attention: one new row per sequence (QKV [batch, ...], pos [batch]): append and attention over
  * positions 0 .. past[b] in one launch, in binary32 throughout but for the operands' own halves (a probability

@@ -39,16 +39,6 @@ typedef int v4i __attribute__((ext_vector_type(4)));
 
 constexpr float kRaiseBy = 6.0f;
 
-// p - (half I of h), exact: one mixed-precision multiply-add instead of a conversion and a subtraction
-template <int I>
-__device__ __forceinline__ float remainder_of(const v2h h, float p)
-{
-    float r;
-    if (I == 0) asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(r) : "v"(h), "v"(p));
-    else asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(h), "v"(p));
-    return r;
-}
-
 template <int D>
 __device__ __forceinline__ int swizzle(int r)
 {

@@ -366,9 +366,18 @@ struct Unit {
 // The maximum is the rounded product of a score and the keys' scale, the scores that are taken from it enter by a multiply-add, unrounded:
 // from here on (in units of ln 2) the difference could be more than a few, and the scores are rounded as well.
 constexpr float kLargeScore = 1048576.f;
-// The maximum lags behind by up to this (a half holds probabilities of 2^6 as well): with 32 rows to a wavefront some row has a new one in
-// most blocks, and the sums are 64 registers.
+// The maximum lags behind by up to this: with 32 rows to a wavefront some row has a new one in most blocks, and the sums are 64 registers.
 constexpr float kRaiseBy = 6.f;
+// Probabilities (and so all sums of them) are 2^9 times as large: below 2^15 with the lag, and what is below the smallest half is below 2^-33 of
+// the largest, so that many of them together are not missing from the sums of values that they are divided out of.
+constexpr float kLift = 9.f;
+// A probability enters the second product as the sum of two halves, which together hold it to 2^-22 of itself: what one half leaves out (2.0e-4 of
+// the outputs' norm) is as much as the rounding of the outputs.
+__device__ __forceinline__ void two_halves(float a, float b, v2h &high, v2h &low)
+{
+    high = v2h{(_Float16)a, (_Float16)b};
+    low = v2h{(_Float16)remainder_of<0>(high, a), (_Float16)remainder_of<1>(high, b)};
+}
 
 // NaN for workgroup `number`'s rows of a sequence that does not fit: of as many tiles as there are of its longest
 template <int D>
@@ -384,10 +393,10 @@ __device__ __forceinline__ void nan_rows(__half *O, int64_t ldo, int first, int6
 // Rows are (query, head) pairs of the heads that share a key head, query first, 32 to a wavefront and WAVES wavefronts to a workgroup, so
 // that a block of keys and values is taken from memory and made halves once for all of them.  Everything is transposed (scores:
 // positions x rows), as in attention.hip: probabilities are the second product's operand where they were computed.
-// What bounds it is the vector ALU beside the matrix cores, 305 instructions to 32 matrix instructions per wavefront and block, a fifth of them
-// exponentials: 1500, 1115 and 1446 rows of 32 heads over 8 behind 2000, 1994 and 420 positions in 223 us, 0.63 PFLOP/s (a library product of
-// halves reaches 1.24), the matrix cores busy for 29 in 100.  (The next block's scores multiplied between this one's probabilities, in the same
-// wavefront: 335 us, the registers do not suffice.)
+// What bounds it is the vector ALU beside the matrix cores, some 350 instructions to 48 matrix instructions per wavefront and block, a tenth of them
+// exponentials: 1500, 1115 and 1446 rows of 32 heads over 8 behind 2000, 1994 and 420 positions in some 270 us, 0.52 PFLOP/s (a library product of
+// halves reaches 1.24); with probabilities of one half, 32 matrix instructions and 305 others, it was 230, and the outputs 2.0e-4 of their norm
+// further off.  (Then the next block's scores multiplied between this one's probabilities, in the same wavefront: 335 us, the registers do not suffice.)
 // A block's p = 2^(s - m) times its factor is one exponential, of s sk + (log2 factor - m); the sum of the probabilities is put right by the
 // factor once per block.
 template <int D, int WAVES>
@@ -566,29 +575,37 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
 #pragma unroll
                     for (int i = 0; i < 16; ++i) ot[ct][i] *= change;
             }
-            const float from = __log2f(factor) - mrun;
+            const float from = (__log2f(factor) + kLift) - mrun;
             float sum = 0.f;
-            v8h p[4];
+            const bool whole = !(sv >= 0.f);                          // values that are NaN as a whole: for the rows that see any of them
 #pragma unroll
-            for (int tt = 0; tt < 2; ++tt)
+            for (int n = 0; n < 4; ++n) {                             // 16 positions at a time: all at once would not leave the registers
+                v8h p, rest, v[CT];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float e = __builtin_amdgcn_exp2f(fmaf(s[tt][i], by, from));
-                    sum += e;
-                    p[2 * tt + (i >> 3)][i & 7] = (_Float16)e;
+                for (int i = 0; i < 8; i += 2) {
+                    const float s0 = s[n >> 1][(n & 1) * 8 + i], s1 = s[n >> 1][(n & 1) * 8 + i + 1];
+                    const float e0 = __builtin_amdgcn_exp2f(fmaf(s0, by, from)), e1 = __builtin_amdgcn_exp2f(fmaf(s1, by, from));
+                    sum += e0;
+                    sum += e1;
+                    v2h high, low;
+                    two_halves(e0, e1, high, low);
+                    p[i] = high[0];
+                    p[i + 1] = high[1];
+                    rest[i] = low[0];
+                    rest[i + 1] = low[1];
                 }
-            lrun += sum * __builtin_amdgcn_rcpf(factor);
-            if (!(sv >= 0.f)) {                                       // values that are NaN as a whole: for the rows that see any of them
+                if (whole) {
 #pragma unroll
-                for (int n = 0; n < 4; ++n)
+                    for (int i = 0; i < 8; ++i) p[i] = s[n >> 1][(n & 1) * 8 + i] == -INFINITY ? (_Float16)0.f : (_Float16)NAN;
+                }
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) p[n][i] = s[n >> 1][(n & 1) * 8 + i] == -INFINITY ? (_Float16)0.f : (_Float16)NAN;
+                for (int ct = 0; ct < CT; ++ct) v[ct] = *reinterpret_cast<const v8h *>(vt + (ct * 4 + n) * 1024);
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) ot[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[ct], p, ot[ct], 0, 0, 0);
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) ot[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[ct], rest, ot[ct], 0, 0, 0);
             }
-#pragma unroll
-            for (int n = 0; n < 4; ++n)
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct)
-                    ot[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const v8h *>(vt + (ct * 4 + n) * 1024), p[n], ot[ct], 0, 0, 0);
+            lrun += sum * __builtin_amdgcn_rcpf(factor);
         }
         keep(j + 1);
     }
@@ -636,8 +653,8 @@ struct WaveSums {
         for (int i = 0; i < D / 16; ++i) o[i] = v4f{0.f, 0.f, 0.f, 0.f};
     }
     // key(T, m), value(i, n): operands of the products; `then` runs when the keys have been used; `ends`: this lane's row sees the first
-    // `sees` + 1 positions of the block only.  TWO: a probability enters as the sum of two halves.
-    template <bool TWO, typename Key, typename Value, typename Then>
+    // `sees` + 1 positions of the block only.
+    template <typename Key, typename Value, typename Then>
     __device__ __forceinline__ void add(const v8h (&q)[D / 32], float sk, float sv, bool ends, int sees, Key key, Value value, Then then)
     {
         const int g = (threadIdx.x & 63) >> 4;
@@ -691,34 +708,37 @@ struct WaveSums {
             for (int i = 0; i < D / 16; ++i) o[i] *= change;
         }
         // (no score above minus infinity so far: nothing is added, other wavefronts' blocks may have some)
-        const float from = __log2f(factor) - (m == -INFINITY ? 0.f : m);
+        const float from = (__log2f(factor) + kLift) - (m == -INFINITY ? 0.f : m);
         float sum = 0.f;
-        v8h p[2], rest[2];
+        const bool whole = !(sv >= 0.f);                              // values that are NaN as a whole
 #pragma unroll
-        for (int T4 = 0; T4 < 4; ++T4)
+        for (int n = 0; n < 2; ++n) {
+            v8h p, rest;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(s[T4][i], by, from));
-                sum += e;
-                const _Float16 e0 = (_Float16)e;
-                p[T4 >> 1][(T4 & 1) * 4 + i] = e0;
-                if constexpr (TWO) rest[T4 >> 1][(T4 & 1) * 4 + i] = (_Float16)(e - (float)e0);
+            for (int i = 0; i < 8; i += 2) {
+                const float s0 = s[2 * n + (i >> 2)][i & 3], s1 = s[2 * n + (i >> 2)][(i & 3) + 1];
+                const float e0 = __builtin_amdgcn_exp2f(fmaf(s0, by, from)), e1 = __builtin_amdgcn_exp2f(fmaf(s1, by, from));
+                sum += e0;
+                sum += e1;
+                v2h high, low;
+                two_halves(e0, e1, high, low);
+                p[i] = high[0];
+                p[i + 1] = high[1];
+                rest[i] = low[0];
+                rest[i + 1] = low[1];
             }
-        l += sum * __builtin_amdgcn_rcpf(factor);
-        if (!(sv >= 0.f)) {                                           // values that are NaN as a whole
+            if (whole) {
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
+                for (int i = 0; i < 8; ++i) p[i] = s[2 * n + (i >> 2)][i & 3] == -INFINITY ? (_Float16)0.f : (_Float16)NAN;
+            }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) p[n][i] = s[2 * n + (i >> 2)][i & 3] == -INFINITY ? (_Float16)0.f : (_Float16)NAN;
-        }
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {
+            for (int i = 0; i < D / 16; ++i) {
                 const v8h v = value(i, n);
-                o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[n], o[i], 0, 0, 0);
-                if constexpr (TWO) o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, rest[n], o[i], 0, 0, 0);
+                o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p, o[i], 0, 0, 0);
+                o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, rest, o[i], 0, 0, 0);
             }
+        }
+        l += sum * __builtin_amdgcn_rcpf(factor);
     }
 };
 
@@ -824,7 +844,7 @@ __global__ __launch_bounds__(64 * kFewRowsWaves, 2) void cache8_few_rows_kernel(
         const int last = sees - j * kBlock;
         if (j != tail_block) {
             const float2 scale = sc;
-            sums.template add<false>(
+            sums.add(
                 q, scale.x, scale.y, ends, last,
                 [&](int T4, int m) {
                     const v4i w = kraw[T4 * C + (m >> 1)];
@@ -833,7 +853,7 @@ __global__ __launch_bounds__(64 * kFewRowsWaves, 2) void cache8_few_rows_kernel(
                 [&](int i, int n) { return halves_of(vraw[i][2 * n], vraw[i][2 * n + 1]); }, [&] { fetch_keys(j + kFewRowsWaves); });
             fetch_values(j + kFewRowsWaves);
         } else {
-            sums.template add<false>(
+            sums.add(
                 q, 1.f, 1.f, true, min(last, tail_rows - 1),
                 [&](int T4, int m) { return *reinterpret_cast<const v8h *>(&lds.u.tail.k[16 * T4 + r][64 * (m >> 1) + 16 * g + 8 * (m & 1)]); },
                 [&](int i, int n) { return *reinterpret_cast<const v8h *>(&lds.u.tail.v[16 * i + r][value_place(16 * i + r, 32 * n + 8 * g)]); }, [] {});
@@ -1107,7 +1127,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void cache8_decode_kernel(con
     int j = begin + wave;
     for (; j < stop && j < last; j += kDecodeWaves) {
         const float2 scale = sc;
-        own.template add<true>(
+        own.add(
             qf, scale.x, scale.y, false, 0,
             [&](int T4, int m) {
                 const v4i w = kraw[T4 * C + (m >> 1)];
@@ -1121,7 +1141,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void cache8_decode_kernel(con
         fetch_values(j + kDecodeWaves);
     }
     if (j < stop)
-        own.template add<true>(
+        own.add(
             qf, tail_sk, tail_sv, true, slot,
             [&](int T4, int m) { return *reinterpret_cast<const v8h *>(&lds.u.tail.k[16 * T4 + r][64 * (m >> 1) + 16 * g + 8 * (m & 1)]); },
             [&](int i, int n) { return *reinterpret_cast<const v8h *>(&lds.u.tail.v[16 * i + r][value_place(16 * i + r, 32 * n + 8 * g)]); }, [] {});

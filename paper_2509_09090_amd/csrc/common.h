@@ -386,6 +386,17 @@ __device__ __forceinline__ double wave_sum(double v)
     return (row(0) + row(16)) + (row(32) + row(48));
 }
 
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+// p - (half I of h), exact: one mixed-precision multiply-add instead of a conversion and a subtraction
+template <int I>
+__device__ __forceinline__ float remainder_of(const v2h h, float p)
+{
+    float r;
+    if (I == 0) asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(r) : "v"(h), "v"(p));
+    else asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(h), "v"(p));
+    return r;
+}
+
 // The sum of an integer over the four rows of 16 lanes (lanes l, l + 16, l + 32, l + 48), in every lane: the
 // upper 32 lanes are exchanged with the lower (v_permlane32_swap), then the odd rows with the even
 // (v_permlane16_swap); two vector-ALU instructions each, no LDS permute.

@@ -1,0 +1,72 @@
+"""The 8-bit cache where a call's parts meet: probabilities far below the largest, keys that are not finite behind a tile's first rows, shares
+of a single row's positions that have nothing to add, and calls that announce no rows."""
+import numpy as np
+import pytest
+
+from paper_2509_09090_amd import binding as B
+from tests import lowbit_ref as R
+from tests.test_cache8 import G, Model, announced                                            # noqa: F401  (fixtures)
+
+pytestmark = pytest.mark.gpu
+
+
+class Pairs(Model):
+    """Probabilities of prompts enter the second product as two halves, as those of single rows do."""
+
+    def check(self, o, y, counts, single_half):
+        super().check(o, y, counts, False)
+
+
+@pytest.mark.parametrize("H,kv,d,calls", [(1, 1, 64, [[3], [20]]), (4, 1, 128, [[70, 9], [5, 60]]), (6, 3, 64, [[200], [129]]), (8, 8, 128, [[40, 100]])])
+def test_prompts_keep_probabilities_in_binary32(G, announced, H, kv, d, calls):              # noqa: F811
+    """Keys so small that the scores' own error is far below half a step of a half."""
+    m = Pairs(G, len(calls[0]), H, kv, d, 64 * 8, seed=H)
+    for counts in calls:
+        m.append(counts, m.rows(sum(counts), 2.0 ** -6))
+
+
+def _spread(rows):
+    """One head of 64: position 0 has the score 16 * 9.375 / 8 = 18.75 and values of zero, all others the score 0 and ones."""
+    x = np.zeros((rows, 3, 64), np.float16)
+    x[:, 0, 0] = 16
+    x[0, 1, 0] = 9.375
+    x[1:, 2] = 1
+    return x
+
+
+def _check_spread(got, sees):
+    """Outputs are t / (1 + t), t = sees * exp(-18.75) = sees * 2^-27.05.  The exponential's argument is off by its roundings in binary32 (27.05 in
+    units of ln 2: 2^-20 each, a few of them), the scale of the first block's keys and values by two more; what a probability loses below the
+    smallest half that it enters with is 2^-34 of the largest; one rounding to half."""
+    t = sees * np.exp(-18.75)
+    want = t / (1 + t)
+    limit = R.HALF_STEP * want + R.HALF_TINY + 2.0 ** -16 * want + sees * 2.0 ** -34
+    assert np.all(np.abs(got.astype(np.float64) - want[:, None]) <= limit[:, None]), (got[-1, :3], want[-1])
+
+
+def test_many_small_probabilities_add_up_in_prompts(G, announced):                          # noqa: F811
+    import torch
+    n = 4100
+    x, most = _spread(n), max(n, Model.most)
+    dev = lambda a: G.to_dev(np.asarray(a, dtype=np.int32))                                   # noqa: E731
+    cache, starts, past, pos = B.Cache8(1, n, 1, 64, device=G.DEV), dev([0, n]), dev([0]), dev(np.zeros(n))
+    q, o = (torch.zeros((most, 64), dtype=torch.float16, device=G.DEV) for _ in range(2))
+    rows = torch.zeros((most, 192), dtype=torch.float16, device=G.DEV)
+    rows[:n] = G.to_dev(x.reshape(n, -1))
+    B.sqap_cache8_append(rows, starts, torch.zeros(most, dtype=torch.int32, device=G.DEV), past, cache, 1, most, Q_out=q)
+    B.sqap_cache8_attention(q, starts, past, cache, 1, most, o)
+    _check_spread(o[:n].cpu().numpy(), np.arange(n))
+
+
+@pytest.mark.parametrize("longest", [64, 4101, 100000])
+def test_many_small_probabilities_add_up_in_single_rows(G, longest):                        # noqa: F811
+    import torch
+    n = 4100
+    dev = lambda a: G.to_dev(np.asarray(a, dtype=np.int32))                                   # noqa: E731
+    cache = B.Cache8(1, n + 1, 1, 64, device=G.DEV)
+    rows = G.to_dev(_spread(n).reshape(n, -1))
+    B.sqap_cache8_append(rows, dev([0, n]), dev(np.zeros(n)), dev([0]), cache, 1, n)
+    o = torch.zeros((1, 64), dtype=torch.float16, device=G.DEV)
+    ws = torch.zeros((B.sqap_cache8_workspace_bytes(1, 1, 1, 64, longest),), dtype=torch.uint8, device=G.DEV)
+    B.sqap_cache8_decode_attention(rows[n - 1:], dev([0]), dev([n]), cache, 1, o, ws, longest)
+    _check_spread(o.cpu().numpy(), np.array([n]))
