@@ -550,12 +550,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
             top = fmaxf(top, __shfl_xor(top, 32));
             if (top > -INFINITY) top *= sk;                           // (nothing seen: it stays, whatever the scale)
             float by = sk;
-            if (__any(fabsf(top) > kLargeScore && top > -INFINITY)) {
+            const bool bad = !(sk >= 0.f && sv >= 0.f);               // keys or values that are NaN as a whole: for the rows that see any of them
+            if (bad || __any(fabsf(top) > kLargeScore && top > -INFINITY)) {        // (a masked score times NaN would be NaN, too)
 #pragma unroll
                 for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        float w = s[tt][i] * sk;
+                        float w = bad ? NAN : s[tt][i] * sk;
                         asm volatile("" : "+v"(w));                   // (rounded)
                         s[tt][i] = s[tt][i] == -INFINITY ? -INFINITY : w;
                     }
@@ -577,7 +578,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
             }
             const float from = (__log2f(factor) + kLift) - mrun;
             float sum = 0.f;
-            const bool whole = !(sv >= 0.f);                          // values that are NaN as a whole: for the rows that see any of them
 #pragma unroll
             for (int n = 0; n < 4; ++n) {                             // 16 positions at a time: all at once would not leave the registers
                 v8h p, rest, v[CT];
@@ -593,10 +593,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
                     p[i + 1] = high[1];
                     rest[i] = low[0];
                     rest[i + 1] = low[1];
-                }
-                if (whole) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) p[i] = s[n >> 1][(n & 1) * 8 + i] == -INFINITY ? (_Float16)0.f : (_Float16)NAN;
                 }
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) v[ct] = *reinterpret_cast<const v8h *>(vt + (ct * 4 + n) * 1024);
@@ -684,12 +680,13 @@ struct WaveSums {
         top = fmaxf(top, __shfl_xor(top, 32));
         if (top > -INFINITY) top *= sk;
         float by = sk;
-        if (__any(fabsf(top) > kLargeScore && top > -INFINITY)) {
+        const bool bad = !(sk >= 0.f && sv >= 0.f);                   // (NaN as a whole: as in cache8_attention_kernel)
+        if (bad || __any(fabsf(top) > kLargeScore && top > -INFINITY)) {
 #pragma unroll
             for (int T4 = 0; T4 < 4; ++T4)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    float w = s[T4][i] * sk;
+                    float w = bad ? NAN : s[T4][i] * sk;
                     asm volatile("" : "+v"(w));                       // (rounded)
                     s[T4][i] = s[T4][i] == -INFINITY ? -INFINITY : w;
                 }
@@ -710,7 +707,6 @@ struct WaveSums {
         // (no score above minus infinity so far: nothing is added, other wavefronts' blocks may have some)
         const float from = (__log2f(factor) + kLift) - (m == -INFINITY ? 0.f : m);
         float sum = 0.f;
-        const bool whole = !(sv >= 0.f);                              // values that are NaN as a whole
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
             v8h p, rest;
@@ -726,10 +722,6 @@ struct WaveSums {
                 p[i + 1] = high[1];
                 rest[i] = low[0];
                 rest[i + 1] = low[1];
-            }
-            if (whole) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) p[i] = s[2 * n + (i >> 2)][i & 3] == -INFINITY ? (_Float16)0.f : (_Float16)NAN;
             }
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {

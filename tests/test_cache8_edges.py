@@ -70,3 +70,28 @@ def test_many_small_probabilities_add_up_in_single_rows(G, longest):            
     ws = torch.zeros((B.sqap_cache8_workspace_bytes(1, 1, 1, 64, longest),), dtype=torch.uint8, device=G.DEV)
     B.sqap_cache8_decode_attention(rows[n - 1:], dev([0]), dev([n]), cache, 1, o, ws, longest)
     _check_spread(o.cpu().numpy(), np.array([n]))
+
+
+@pytest.mark.parametrize("H,kv,d,past,n,bad", [(1, 1, 64, 10, 118, 100), (1, 1, 128, 50, 80, 70), (4, 2, 64, 40, 160, 150), (3, 1, 128, 77, 200, 255),
+                                               (2, 2, 64, 1, 140, 64), (8, 1, 64, 61, 70, 127)])
+@pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
+def test_keys_that_are_not_finite_leave_the_rows_before_their_block(G, announced, H, kv, d, past, n, bad, value):       # noqa: F811
+    """The history ends where neither a wavefront's rows nor a tile's end with a block, so that rows which see nothing of the block with the bad
+    key stand beside rows that do."""
+    m = Model(G, 2, H, kv, d, 64 * 6, seed=past)
+    m.append([past, 3])
+    x = m.rows(n + 2)
+    x[bad - past, H + kv - 1, 5] = value
+    m.append([n, 2], x)
+    m.check_contents()
+
+
+@pytest.mark.parametrize("value", [np.nan, np.inf])
+def test_bad_key_seen_by_a_bad_query_alone(G, announced, value):                             # noqa: F811
+    """Of 32 (and of 16) rows the last alone sees the block, and its query has no score that is a number."""
+    m = Model(G, 1, 1, 1, 64, 64 * 4, seed=8)
+    m.append([1])
+    x = m.rows(140)
+    x[99, 1, 5] = np.nan
+    x[63, 0] = value
+    m.append([140], x)
