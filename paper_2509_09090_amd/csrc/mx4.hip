@@ -8,6 +8,7 @@
 #include <algorithm>
 
 #include "common.h"
+#include "mx4_stage.h"
 
 namespace sqap {
 
@@ -166,7 +167,8 @@ __device__ __forceinline__ v2u first_scales(const uint8_t *of_row, int blocks)
     return v2u{(unsigned)w, (unsigned)(w >> 32)};
 }
 
-// A window of memory: lane offset + uniform offset, without 64-bit addresses in vector registers; behind its end zeros are read.
+// A window of memory: lane offset + uniform offset, without 64-bit addresses in vector registers; a lane offset behind its end reads zeros, a
+// uniform one stays inside.
 typedef __amdgpu_buffer_rsrc_t Window;
 __device__ __forceinline__ Window window_of(const void *p, unsigned long long bytes)
 {
@@ -310,13 +312,13 @@ void mx4_tile_kernel(const uint8_t *__restrict__ Xq, const uint8_t *__restrict__
     const unsigned lane16 = (unsigned)l * 16u, lane4 = (unsigned)l * 4u;
     v4i wreg[DEPTH][STEPS][RN];
     unsigned ws[DEPTH][RN], ws_next[RN];
-    auto fetch_weight = [&](int d, int s, int st) {                   // (past the last stage: zeros, or the other fragment's; not used)
+    auto fetch_weight = [&](int d, int s, int st) {
 #pragma unroll
-        for (int c = 0; c < RN; ++c) wreg[d][s][c] = read16(wdata, lane16 + (unsigned)s * 1024u, (unsigned)(c * stages + st) * 4096u);
+        for (int c = 0; c < RN; ++c) wreg[d][s][c] = read16(wdata, lane16 + (unsigned)s * 1024u, weight_stage(c, st, stages, 4096u));
     };
     auto fetch_weight_scales = [&](unsigned (&into)[RN], int st) {
 #pragma unroll
-        for (int c = 0; c < RN; ++c) into[c] = __builtin_amdgcn_raw_buffer_load_b32(wscales, lane4, (unsigned)(c * stages + st) * 256u, 0);
+        for (int c = 0; c < RN; ++c) into[c] = __builtin_amdgcn_raw_buffer_load_b32(wscales, lane4, weight_stage(c, st, stages, 256u), 0);
     };
 
     v16f acc[RM][RN];
