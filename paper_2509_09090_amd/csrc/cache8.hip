@@ -1157,12 +1157,14 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void cache8_decode_kernel(con
         top = -INFINITY;
 #pragma unroll
         for (int w = 0; w < kDecodeWaves; ++w) top = fmaxf(top, lds.m[w][j]);
+        // (no score above minus infinity: the share has nothing to add to the others; where there are none the softmax is 0 / 0)
+        const float from = top == -INFINITY && active > 1 ? 0.f : top;
         sum = 0.f;
         float o = 0.f;
 #pragma unroll
         for (int w = 0; w < kDecodeWaves; ++w) {
             if (begin + w >= stop) break;                             // a wavefront without a block
-            const float f = exp2f(lds.m[w][j] - top);
+            const float f = exp2f(lds.m[w][j] - from);
             sum += f * lds.l[w][j];
             o += f * lds.u.o[w][j][i];
         }

@@ -95,3 +95,20 @@ def test_bad_key_seen_by_a_bad_query_alone(G, announced, value):                
     x[99, 1, 5] = np.nan
     x[63, 0] = value
     m.append([140], x)
+
+
+@pytest.mark.parametrize("longest", [64, 1025, 100000])
+@pytest.mark.parametrize("H,kv,d", [(4, 4, 64), (20, 1, 64), (8, 2, 128)])
+def test_last_share_without_a_score(G, H, kv, d, longest):                                   # noqa: F811
+    """The new row opens a block, and its key is infinite: heads whose score is minus infinity see the others as if it were not there, the rest
+    are NaN; how many shares there are makes no difference."""
+    m = Model(G, 1, H, kv, d, 64 * 20, seed=H)
+    m.append([1024], attend=False)
+    x = m.rows(1)
+    i = d // 2 - 1                                                        # a slow pair: turned by less than an eighth
+    x[0, H:H + kv, i] = np.inf
+    x[0, H:H + kv, i + d // 2] = 0
+    x[0, :H, i] = x[0, :H, i + d // 2] = -2
+    x[0, 1, i] = x[0, 1, i + d // 2] = 2
+    o = m.decode(x, longest=longest).cpu().numpy().reshape(H, d)
+    assert np.isnan(o[1]).all() and np.isfinite(np.delete(o, 1, 0)).all()
