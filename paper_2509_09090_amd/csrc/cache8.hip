@@ -1228,9 +1228,9 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void cache8_decode_kernel(con
 #pragma unroll 8
             for (int w = group; w < active; w += groups) {
                 const u64 raw = __hip_atomic_load(reinterpret_cast<const u64 *>(all + (int64_t)w * per_item) + u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                const float f = factor[w * heads + j];
-                o.x += f * __uint_as_float((unsigned)raw);
-                o.y += f * __uint_as_float((unsigned)(raw >> 32));
+                const float f = factor[w * heads + j], x = __uint_as_float((unsigned)raw), y = __uint_as_float((unsigned)(raw >> 32));
+                o.x += fabsf(x) < INFINITY ? f * x : x;               // (an infinite value stays one however small the share's weight)
+                o.y += fabsf(y) < INFINITY ? f * y : y;
             }
         }
         if (groups > 1) {

@@ -112,3 +112,15 @@ def test_last_share_without_a_score(G, H, kv, d, longest):                      
     x[0, 1, i] = x[0, 1, i + d // 2] = 2
     o = m.decode(x, longest=longest).cpu().numpy().reshape(H, d)
     assert np.isnan(o[1]).all() and np.isfinite(np.delete(o, 1, 0)).all()
+
+
+@pytest.mark.parametrize("longest", [64, 1041, 100000])
+def test_infinite_value_in_a_share_without_weight(G, longest):                               # noqa: F811
+    """An infinite value reaches the rows that see it however small its probability, in whichever share it lies."""
+    m = Model(G, 1, 4, 4, 64, 64 * 20, seed=2)
+    m.append([1024], attend=False)
+    x = m.rows(1)
+    x[0, 4:8] = -30 * x[0, :4]                                            # scores around -240
+    x[0, 8, 3], x[0, 9, 4], x[0, 10, 5] = np.inf, -np.inf, np.nan
+    o = m.decode(x, longest=longest).cpu().numpy().reshape(4, 64)
+    assert o[0, 3] == np.inf and o[1, 4] == -np.inf and np.isnan(o[2, 5]) and np.isfinite(o).sum() == 4 * 64 - 3
