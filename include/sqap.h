@@ -365,7 +365,7 @@ sqap_status sqap_w4a4_linear(const uint8_t *Xq, const sqap_f16 *sx, int32_t M,
  * same bits every time.  A row whose blocks are finite is not touched by another that is not.  Xq: 16-byte aligned; Y: [M, N] half with pitch ldy >= N elements, of any
  * alignment; what lies behind a row's N elements is left as it was.  Needs no workspace; may be captured.
  * EINVAL: null pointer, not a handle, M < 0, ldy < N, a handle of another device than the current one.
- * EUNSUPPORTED: Xq not 16-byte aligned, M above 2^24, or more than 2^30 tiles of 16 x 64 outputs.
+ * EUNSUPPORTED: Xq not 16-byte aligned, M above 2^24, or more than 2^24 - 8 tiles of 64 x 128 outputs.
  */
 typedef struct sqap_mx4_weight sqap_mx4_weight;
 sqap_status sqap_mx4_quantize(const sqap_f16 *X, int64_t ldx, const int32_t *rows, int32_t M, int32_t K,
@@ -520,7 +520,8 @@ sqap_status sqap_residual_add(sqap_f16 *X, int64_t ldx, const sqap_f16 *delta, i
  * EINVAL: null pointer, negative size, sizes of the cache that are not positive, H not a multiple of kv_heads, capacity
  * not a multiple of 64, a pitch too small, base <= 0, first < 0, workspace missing, too small or misaligned.
  * EUNSUPPORTED: head_dim not 64 or 128, more than 65535 sequences or key heads (times 16 query heads), max_new rows of the
- * query heads to a key head (or all tiles of 128 of them) beyond 32 bits, operands or pitches not 16-byte aligned (scales: 4).
+ * query heads to a key head beyond 32 bits or, for all key heads and sequences, 2^24 - 1 tiles of 128 of them, operands or pitches
+ * not 16-byte aligned (scales: 4).
  */
 #define SQAP_CACHE8_BLOCK 64
 typedef struct sqap_cache8 {

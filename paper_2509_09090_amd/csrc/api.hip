@@ -721,7 +721,7 @@ sqap_status sqap_mx4_linear(const uint8_t *Xq, const uint8_t *Xs, int32_t M, con
     if (M == 0) return SQAP_OK;
     if (!Xq || !Xs || !Y) return fail(SQAP_EINVAL, "%s: null pointer", who);
     if (!aligned16(Xq)) return fail(SQAP_EUNSUPPORTED, "%s: Xq must be 16-byte aligned", who);
-    if (M > kMx4MaxRows || (int64_t)((M + 15) / 16) * ((w->N + 63) / 64) > (1 << 30))
+    if (M > kMx4MaxRows || (int64_t)((M + 63) / 64) * ((w->N + 127) / 128) > most_workgroups(256) - 7)      // (dealt to eight XCDs alike)
         return fail(SQAP_EUNSUPPORTED, "%s: M = %d, N = %d", who, M, w->N);
     const DeviceOfCall device;
     if (device_ordinal() != w->device) return fail(SQAP_EINVAL, "%s: the weight is on device %d, the current one is %d", who, w->device, device_ordinal());
@@ -795,7 +795,7 @@ sqap_status sqap_cache8_attention(const sqap_f16 *Q, int64_t ldq, const int32_t 
     if (s != SQAP_OK) return s;
     max_new = max_new < rows ? max_new : rows;
     const int64_t pairs = (int64_t)max_new * (H / cache->kv_heads);
-    if (pairs > INT32_MAX - 128 || (pairs + 127) / 128 * cache->kv_heads * cache->batch > INT32_MAX)
+    if (pairs > INT32_MAX - 128 || (pairs + 127) / 128 * cache->kv_heads * cache->batch > most_workgroups(256))
         return fail(SQAP_EUNSUPPORTED, "%s: %d rows of %d heads", who, max_new, H);
     const DeviceOfCall device;
     return launch_cache8_attention(reinterpret_cast<const __half *>(Q), ldq, starts, past, rows, max_new, H, v, cache->head_dim,

@@ -309,11 +309,11 @@ __global__ __launch_bounds__(4 * D, 2) void cache8_append_kernel(const __half *_
 // ---------------------------------------------------------------- reading back
 
 template <int D>
-__global__ __launch_bounds__(256) void cache8_read_kernel(const Cache8View cache, const int32_t *__restrict__ lengths, int first, int count,
+__global__ __launch_bounds__(256) void cache8_read_kernel(const Cache8View cache, const int32_t *__restrict__ lengths, int first, int count, int from,
                                                           __half *__restrict__ out, int64_t ld)
 {
-    // one workgroup per position; a thread per two columns of a head
-    const int j = blockIdx.x, b = blockIdx.y, p = first + j, n = lengths[b];
+    // one workgroup per position (of those from the from-th on); a thread per two columns of a head
+    const int j = from + (int)blockIdx.x, b = blockIdx.y, p = first + j, n = lengths[b];
     __half *row = out + ((int64_t)b * count + j) * ld;
     for (int u = threadIdx.x; u < cache.kv_heads * D; u += 256) {
         const int which = u >= cache.kv_heads * D / 2, w = (u - which * (cache.kv_heads * D / 2)) * 2, h = w / D, c = w % D;
@@ -1286,10 +1286,12 @@ sqap_status launch_cache8_append(const __half *QKV, int64_t ld, const int32_t *s
 
 sqap_status launch_cache8_read(const Cache8View &cache, int d, const int32_t *lengths, int first, int count, __half *out, int64_t ld, hipStream_t st)
 {
-    const dim3 grid(count, cache.batch);
-    if (d == 64) hipLaunchKernelGGL(cache8_read_kernel<64>, grid, dim3(256), 0, st, cache, lengths, first, count, out, ld);
-    else hipLaunchKernelGGL(cache8_read_kernel<128>, grid, dim3(256), 0, st, cache, lengths, first, count, out, ld);
-    SQAP_HIP_CHECK(hipGetLastError());
+    for (int64_t from = 0; from < count; from += most_workgroups(256)) {
+        const dim3 grid((unsigned)std::min(most_workgroups(256), count - from), cache.batch);
+        if (d == 64) hipLaunchKernelGGL(cache8_read_kernel<64>, grid, dim3(256), 0, st, cache, lengths, first, count, (int)from, out, ld);
+        else hipLaunchKernelGGL(cache8_read_kernel<128>, grid, dim3(256), 0, st, cache, lengths, first, count, (int)from, out, ld);
+        SQAP_HIP_CHECK(hipGetLastError());
+    }
     return SQAP_OK;
 }
 

@@ -164,6 +164,9 @@ static inline int device_cu_count()
     return v;
 }
 
+// Workgroups along x that one launch takes: its threads are counted in 32 bits (more of them wrap round without an error).
+constexpr int64_t most_workgroups(int threads) { return (int64_t(1) << 32) / threads - 1; }
+
 #define SQAP_HIP_CHECK(expr)                                                          \
     do {                                                                              \
         hipError_t e_ = (expr);                                                       \

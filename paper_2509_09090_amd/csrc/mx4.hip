@@ -63,9 +63,13 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const __half *__restr
 
 sqap_status launch_mx4_quantize(const __half *X, int64_t ldx, const int32_t *rows, int M, int K, uint8_t *Xq, uint8_t *Xs, hipStream_t st)
 {
-    const int per_row = (K / 8 + 255) / 256;
-    hipLaunchKernelGGL(mx4_quantize_kernel, dim3((unsigned)M * per_row), dim3(256), 0, st, X, ldx, rows, K, per_row, Xq, Xs);
-    SQAP_HIP_CHECK(hipGetLastError());
+    const int per_row = (K / 8 + 255) / 256, most = (int)(most_workgroups(256) / per_row);
+    for (int64_t first = 0; first < M; first += most) {
+        const int n = (int)std::min<int64_t>(most, M - first);
+        hipLaunchKernelGGL(mx4_quantize_kernel, dim3((unsigned)n * per_row), dim3(256), 0, st, rows ? X : X + first * ldx, ldx, rows ? rows + first : rows, K,
+                           per_row, Xq + first * (K >> 1), Xs + first * (K >> 5));
+        SQAP_HIP_CHECK(hipGetLastError());
+    }
     return SQAP_OK;
 }
 

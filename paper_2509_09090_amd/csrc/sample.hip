@@ -591,7 +591,6 @@ sqap_status launch_sample(const __half *logits, int64_t ld, int batch, int vocab
                           const float *top_p, const float *min_p, const float *uniform, int32_t *token, float *prob, hipStream_t st)
 {
     const int slabs = (vocab + kSlab - 1) / kSlab;
-    const SampleArgs a = {logits, ld, vocab, slabs, temperature, top_p, min_p, uniform, top_k, token, prob};
     const bool cached = vocab <= kSampleCached;
     const size_t lds = (size_t)slabs * sizeof(u64) + (cached ? sizeof(SampleLds<true>) + (size_t)slabs * kSlab * 2 : sizeof(SampleLds<false>));
     static std::atomic<bool> ready[kMaxDeviceSlots];
@@ -603,10 +602,14 @@ sqap_status launch_sample(const __half *logits, int64_t ld, int batch, int vocab
         SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(sample_kernel<false>), hipFuncAttributeMaxDynamicSharedMemorySize, most));
         ready[device_slot()].store(true, std::memory_order_relaxed);
     }
-    const dim3 grid(batch), block(kSampleT);
-    if (cached) hipLaunchKernelGGL(sample_kernel<true>, grid, block, lds, st, a);
-    else hipLaunchKernelGGL(sample_kernel<false>, grid, block, lds, st, a);
-    SQAP_HIP_CHECK(hipGetLastError());
+    for (int64_t first = 0; first < batch; first += most_workgroups(kSampleT)) {
+        const auto at = [&](auto *p) { return p ? p + first : p; };
+        const SampleArgs a = {logits + first * ld, ld, vocab, slabs, at(temperature), at(top_p), at(min_p), at(uniform), at(top_k), at(token), at(prob)};
+        const dim3 grid((unsigned)std::min(most_workgroups(kSampleT), batch - first)), block(kSampleT);
+        if (cached) hipLaunchKernelGGL(sample_kernel<true>, grid, block, lds, st, a);
+        else hipLaunchKernelGGL(sample_kernel<false>, grid, block, lds, st, a);
+        SQAP_HIP_CHECK(hipGetLastError());
+    }
     return SQAP_OK;
 }
 
