@@ -514,8 +514,8 @@ sqap_status sqap_residual_add(sqap_f16 *X, int64_t ldx, const sqap_f16 *delta, i
  * out [batch * count, 2 kv_heads d] (pitch ld): keys, then values; zeros where lengths[b] (device) does not reach.
  *
  * What the device finds wrong it leaves alone: a sequence with past[b] < 0 or no rows is skipped, its outputs
- * stay as they were (a padded batch); one whose rows do not fit the capacity, or are more than max_new, is not appended
- * and its outputs are NaN; one whose starts do not lie in order within 0 .. rows is skipped.
+ * stay as they were (a padded batch); one whose rows do not fit the capacity, or are more than max_new (0 too), is not appended,
+ * its rows of Q_out stay as they were, and its outputs O are NaN; one whose starts do not lie in order within 0 .. rows is skipped.
  * All may be captured in a graph and replayed with other past, pos and starts.
  * EINVAL: null pointer, negative size, sizes of the cache that are not positive, H not a multiple of kv_heads, capacity
  * not a multiple of 64, a pitch too small, base <= 0, first < 0, workspace missing, too small or misaligned.

@@ -787,7 +787,7 @@ sqap_status sqap_cache8_attention(const sqap_f16 *Q, int64_t ldq, const int32_t 
     Cache8View v = {};
     if (rows < 0 || max_new < 0) return fail(SQAP_EINVAL, "%s: rows %d, max_new %d", who, rows, max_new);
     sqap_status s = check_cache8(who, cache, H, &v);
-    if (s != SQAP_OK || rows == 0 || max_new == 0 || cache->batch == 0) return s;
+    if (s != SQAP_OK || rows == 0 || cache->batch == 0) return s;      // (no rows announced: all that there are are too many)
     if (!starts || !past) return fail(SQAP_EINVAL, "%s: null pointer", who);
     const int64_t width = (int64_t)H * cache->head_dim;
     s = check_rows16(who, "Q", Q, ldq, width);

@@ -1312,7 +1312,7 @@ static sqap_status launch_attention_d(const __half *Q, int64_t ldq, const int32_
                                            (int)sizeof(FewRowsLds<D>)));
         ready[device_slot()].store(true, std::memory_order_relaxed);
     }
-    const auto tiles_of = [&](int per_tile) { return ((int64_t)max_new * (H / cache.kv_heads) + per_tile - 1) / per_tile; };
+    const auto tiles_of = [&](int per_tile) { return std::max<int64_t>(1, ((int64_t)max_new * (H / cache.kv_heads) + per_tile - 1) / per_tile); };
     const int64_t pairs = (int64_t)cache.kv_heads * cache.batch;
     const bool few = tiles_of(32 * WAVES) * pairs <= kFewTiles;
     const int64_t tiles = tiles_of(few ? 16 : 32 * WAVES), items = tiles * pairs;

@@ -49,7 +49,7 @@ def test_many_small_probabilities_add_up_in_prompts(G, announced):              
     n = 4100
     x, most = _spread(n), max(n, Model.most)
     dev = lambda a: G.to_dev(np.asarray(a, dtype=np.int32))                                   # noqa: E731
-    cache, starts, past, pos = B.Cache8(1, n, 1, 64, device=G.DEV), dev([0, n]), dev([0]), dev(np.zeros(n))
+    cache, starts, past = B.Cache8(1, n, 1, 64, device=G.DEV), dev([0, n]), dev([0])
     q, o = (torch.zeros((most, 64), dtype=torch.float16, device=G.DEV) for _ in range(2))
     rows = torch.zeros((most, 192), dtype=torch.float16, device=G.DEV)
     rows[:n] = G.to_dev(x.reshape(n, -1))
@@ -124,3 +124,19 @@ def test_infinite_value_in_a_share_without_weight(G, longest):                  
     x[0, 8, 3], x[0, 9, 4], x[0, 10, 5] = np.inf, -np.inf, np.nan
     o = m.decode(x, longest=longest).cpu().numpy().reshape(4, 64)
     assert o[0, 3] == np.inf and o[1, 4] == -np.inf and np.isnan(o[2, 5]) and np.isfinite(o).sum() == 4 * 64 - 3
+
+
+def test_no_rows_announced(G):                                                               # noqa: F811
+    """Sequences of more rows than announced have outputs of NaN, also where none are announced."""
+    import torch
+    m = Model(G, 3, 4, 2, 64, 128, seed=1)
+    dev = lambda a: G.to_dev(np.asarray(a, dtype=np.int32))                                   # noqa: E731
+    x = G.to_dev(m.rows(40).reshape(40, -1))
+    o = torch.full((40, 256), 9.0, dtype=torch.float16, device=G.DEV)
+    keep = m.cache.tail.clone()
+    starts, past = dev([2, 33, 33, 38]), dev([0, 0, -1])
+    B.sqap_cache8_append(x, starts, dev(np.arange(40)), past, m.cache, 4, 0)
+    B.sqap_cache8_attention(x[:, :256], starts, past, m.cache, 4, 0, o)
+    got = o.cpu().numpy()
+    assert np.isnan(got[2:33]).all() and np.all(got[:2] == 9) and np.all(got[33:] == 9)
+    assert torch.equal(keep.view(torch.uint8), m.cache.tail.view(torch.uint8))
