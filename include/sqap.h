@@ -362,8 +362,9 @@ sqap_status sqap_w4a4_linear(const uint8_t *Xq, const sqap_f16 *sx, int32_t M,
  *
  * sqap_mx4_linear: Y[m,n] = binary16(sum_k x[m,k] w[n,k]), x and w the values that codes and scales stand for.
  * Products are exact, sums are binary32; their order depends on the shape, not on the call, so that a call gives the
- * same bits every time.  A row whose blocks are finite is not touched by another that is not.  Xq: 16-byte aligned; Y: [M, N] half with pitch ldy >= N elements, of any
- * alignment; what lies behind a row's N elements is left as it was.  Needs no workspace; may be captured.
+ * same bits every time.  A row whose blocks are finite is not touched by another that is not.  Xq: [M, K/2] and Xs:
+ * [M, K/32] of the weight's K (sqap_mx4_weight_info; not checked), Xq 16-byte aligned; Y: [M, N] half with pitch ldy >= N
+ * elements, of any alignment; what lies behind a row's N elements is left as it was.  Needs no workspace; may be captured.
  * EINVAL: null pointer, not a handle, M < 0, ldy < N, a handle of another device than the current one.
  * EUNSUPPORTED: Xq not 16-byte aligned, M above 2^24, or more than 2^24 - 8 tiles of 64 x 128 outputs.
  */

@@ -454,8 +454,8 @@ def sqap_mx4_weight_pack(Wq, Ws, stream=None):
 
 
 def sqap_mx4_linear(Xq, Xs, W, Y, stream=None):
-    """Xq [M,K/2] u8, Xs [M,K/32] u8, W: Mx4Weight -> Y [M,N] fp16."""
-    _native.mx4_linear(Xq, Xs, W.handle, Y, stream)
+    """Xq [M,K/2] u8, Xs [M,K/32] u8, W: Mx4Weight of K channels (ValueError for others) -> Y [M,N] fp16."""
+    _native.mx4_linear(Xq, Xs, W.handle, W.K, Y, stream)
 
 
 CACHE8_BLOCK = 64

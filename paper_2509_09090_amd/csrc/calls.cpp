@@ -128,6 +128,13 @@ T *handle(PyObject *o)
     return v.p == Py_None ? nullptr : reinterpret_cast<T *>(as_i64(v.p));
 }
 
+void of_channels(const char *what, int64_t have, int64_t channels)
+{
+    if (have == channels) return;
+    PyErr_Format(PyExc_ValueError, "%s of %lld channels for a weight of %lld", what, (long long)have, (long long)channels);
+    throw PyFailed{};
+}
+
 int64_t rows_of(PyObject *X, PyObject *rows) { return rows == Py_None ? size(X, 0) : count(rows); }
 
 struct Calls {
@@ -249,9 +256,11 @@ SQAP_METHOD(w4a4_linear, 7,
 SQAP_METHOD(mx4_quantize, 5,
             run(c->mx4_quantize, ptr<sqap_f16>(a[0]), pitch(a[0]), ptr<int32_t>(a[1]), (int32_t)rows_of(a[0], a[1]), (int32_t)size(a[0], 1),
                 ptr<uint8_t>(a[2]), ptr<uint8_t>(a[3]), stream(c, a[4])))
-SQAP_METHOD(mx4_linear, 5,
-            run(c->mx4_linear, ptr<uint8_t>(a[0]), ptr<uint8_t>(a[1]), (int32_t)size(a[0], 0), handle<sqap_mx4_weight>(a[2]),
-                ptr<sqap_f16>(a[3]), pitch(a[3]), stream(c, a[4])))
+// (Xq, Xs, the weight's handle and K, Y, stream: the library takes the weight's K and would read past rows that are shorter)
+SQAP_METHOD(mx4_linear, 6,
+            (of_channels("codes", 2 * size(a[0], 1), as_i64(a[3])), of_channels("scales", 32 * size(a[1], 1), as_i64(a[3])),
+             run(c->mx4_linear, ptr<uint8_t>(a[0]), ptr<uint8_t>(a[1]), (int32_t)size(a[0], 0), handle<sqap_mx4_weight>(a[2]),
+                 ptr<sqap_f16>(a[4]), pitch(a[4]), stream(c, a[5]))))
 SQAP_METHOD(cache8_append, 10,
             run(c->cache8_append, ptr<sqap_f16>(a[0]), pitch(a[0]), ptr<int32_t>(a[1]), ptr<int32_t>(a[2]), ptr<int32_t>(a[3]), (int32_t)size(a[0], 0),
                 as_i32(a[6]), as_i32(a[5]), as_double(a[8]), handle<sqap_cache8>(a[4]), ptr<sqap_f16>(a[7]), a[7] == Py_None ? 0 : pitch(a[7]),

@@ -1,4 +1,4 @@
-"""Calls of the operators in few bits whose rows or positions are more than one launch takes (2^32 threads)."""
+"""Calls of the operators in few bits whose rows or positions are more than one launch takes (2^32 threads), and operands of different sizes."""
 import ctypes
 
 import numpy as np
@@ -6,7 +6,19 @@ import pytest
 
 from paper_2509_09090_amd import binding as B
 from tests import lowbit_ref as R
+from tests.test_calls import recorded                                                        # noqa: F401  (a fixture)
 from tests.test_cache8 import G                                                              # noqa: F401  (a fixture)
+
+
+@pytest.mark.parametrize("codes,scales", [(16, 2), (64, 2), (32, 1), (32, 4), (16, 1)])
+def test_product_of_other_channels_is_refused(recorded, codes, scales):                       # noqa: F811
+    """Codes or scales that are not of the weight's 64 channels do not reach the library, which would read past them."""
+    import torch
+    calls, _ = recorded
+    xq, xs = torch.zeros((3, codes), dtype=torch.uint8), torch.zeros((3, scales), dtype=torch.uint8)
+    with pytest.raises(ValueError, match="channels"):
+        B.sqap_mx4_linear(xq, xs, B.Mx4Weight(None, 5, 64), torch.zeros((3, 5), dtype=torch.float16))
+    assert not calls
 
 
 def test_attention_of_too_many_tiles_is_refused():
