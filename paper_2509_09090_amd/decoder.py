@@ -106,6 +106,9 @@ def layer_forward(w, buf, x, pending, pos, batch, n_heads, head_dim, x_out, d_ou
     mx4, cache8 = isinstance(w.qkv, B.Mx4Weight), isinstance(kv, B.Cache8)
     if (rotate and mx4) or (fold_quantizer and (mx4 or cache8)):
         raise ValueError("neither rotate nor fold_quantizer goes with weights in microscaled floating point, nor the latter with a Cache8")
+    kv_width = kv.kv_heads * kv.head_dim if cache8 else hidden
+    if buf.qkv.shape[1] != hidden + 2 * kv_width or (cache8 and kv.head_dim != head_dim):
+        raise ValueError("buffers for q|k|v rows of %d columns, keys and values of %d each, heads of %d" % (buf.qkv.shape[1], kv_width, head_dim))
     flags = B.ROTATE_HADAMARD if rotate else 0
     xq, sx, qkv, attn, o = buf.xq[:M], buf.sx[:M], buf.qkv[:M], buf.attn[:M], buf.o[:M]
     gu, hq, sh = buf.gu[:M], buf.hq[:M], buf.sh[:M]
