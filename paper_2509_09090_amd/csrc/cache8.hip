@@ -1338,9 +1338,10 @@ sqap_status launch_cache8_attention(const __half *Q, int64_t ldq, const int32_t 
 // 16.6); and no more than two workgroups per compute unit in all, which is what their registers leave room for (100k positions of 8 key
 // heads: 52 us with 512 workgroups, 66 with 768).
 constexpr int kDecodeGroups = 512;
+static int blocks_of(int positions) { return positions / kBlock + (positions % kBlock != 0); }      // (of any number up to 2^31 - 1)
 static int decode_shares(int batch, int H, int kv_heads, int longest)
 {
-    const int chunks = (H / kv_heads + 15) / 16, blocks = (longest + kBlock - 1) / kBlock;
+    const int chunks = (H / kv_heads + 15) / 16, blocks = blocks_of(longest);
     const int64_t items = (int64_t)batch * kv_heads * chunks;
     const int wanted = blocks <= 8 ? 1 : std::max((blocks + 7) / 8, std::min(8, (blocks + 3) / 4));
     return (int)std::max<int64_t>(1, std::min<int64_t>({wanted, kDecodeGroups / items, kMaxShares}));
@@ -1371,7 +1372,7 @@ sqap_status launch_cache8_decode(const __half *QKV, int64_t ld, const int32_t *p
     a.G = H / cache.kv_heads;
     a.chunks = (a.G + 15) / 16;
     a.shares = decode_shares(cache.batch, H, cache.kv_heads, longest);
-    a.per_share = ((longest + kBlock - 1) / kBlock + a.shares - 1) / a.shares;
+    a.per_share = (blocks_of(longest) + a.shares - 1) / a.shares;
     a.cache = cache;
     a.O = O;
     a.ldo = ldo;

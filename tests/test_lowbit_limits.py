@@ -21,6 +21,13 @@ def test_product_of_other_channels_is_refused(recorded, codes, scales):         
     assert not calls
 
 
+def test_longest_of_any_size():
+    """A caller that knows no bound may name the largest number: as many shares, and the same workspace, as for any long cache."""
+    for sizes in ((1, 32, 8, 128), (3, 8, 8, 64), (16, 40, 2, 64)):
+        need = [B.sqap_cache8_workspace_bytes(*sizes, longest) for longest in (1 << 20, 2 ** 31 - 64, 2 ** 31 - 63, 2 ** 31 - 1)]
+        assert need[0] > 0 and need == need[:1] * 4
+
+
 def test_attention_of_too_many_tiles_is_refused():
     """2^24 tiles of 128 pairs, counted as if every sequence had as many rows as announced."""
     p = ctypes.c_void_p(4096)
