@@ -312,7 +312,8 @@ template <int D>
 __global__ __launch_bounds__(256) void cache8_read_kernel(const Cache8View cache, const int32_t *__restrict__ lengths, int first, int count, int from,
                                                           __half *__restrict__ out, int64_t ld)
 {
-    // one workgroup per position (of those from the from-th on); a thread per two columns of a head
+    // One workgroup per position (of those from the from-th on); a thread per two columns of a head, whose codes it gathers byte by byte.  A call to
+    // look at a cache, not one of a step: 1500 positions of 32 heads of 128 24 us, 100003 of 8 heads 323 (1.9 TB/s of codes and halves).
     const int j = from + (int)blockIdx.x, b = blockIdx.y, p = first + j, n = lengths[b];
     __half *row = out + ((int64_t)b * count + j) * ld;
     for (int u = threadIdx.x; u < cache.kv_heads * D; u += 256) {
@@ -393,7 +394,7 @@ __device__ __forceinline__ void nan_rows(__half *O, int64_t ldo, int first, int6
 // Rows are (query, head) pairs of the heads that share a key head, query first, 32 to a wavefront and WAVES wavefronts to a workgroup, so
 // that a block of keys and values is taken from memory and made halves once for all of them.  Everything is transposed (scores:
 // positions x rows), as in attention.hip: probabilities are the second product's operand where they were computed.
-// What bounds it is the vector ALU beside the matrix cores, some 350 instructions to 48 matrix instructions per wavefront and block, a tenth of them
+// What bounds it is the vector ALU beside the matrix cores, 355 instructions to 48 matrix instructions per wavefront and block, a tenth of them
 // exponentials: 1500, 1115 and 1446 rows of 32 heads over 8 behind 2000, 1994 and 420 positions in some 270 us, 0.52 PFLOP/s (a library product of
 // halves reaches 1.24); with probabilities of one half, 32 matrix instructions and 305 others, it was 230, and the outputs 2.0e-4 of their norm
 // further off.  (Then the next block's scores multiplied between this one's probabilities, in the same wavefront: 335 us, the registers do not suffice.)
@@ -524,7 +525,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
         if (j * kBlock <= wave_last) {
             const uint8_t *kt = lds + (j & 1) * BUF + l * 16, *vt = kt + kBlock * D * 2;
             v16f s[2];
-            __builtin_amdgcn_s_setprio(1);                            // (before the other workgroup's exponentials: 231 -> 223 us)
+            __builtin_amdgcn_s_setprio(1);                            // (before the other workgroup's exponentials: 3 in 100; not for the values' products)
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt) {
 #pragma unroll
@@ -740,7 +741,7 @@ __device__ __forceinline__ int value_slot(int s) { return (s & 32) | ((s >> 2) &
 __device__ __forceinline__ int value_place(int x, int at) { return ((at + (x & ~7)) & 56) | (at & 7); }
 
 // Few rows: tiles of 16 (query, head) pairs, and the blocks dealt to the workgroup's wavefronts, each of which takes keys and values to its own
-// registers as the decode call does.
+// registers as the decode call does (heads of 128 take all 256 registers; an address lies in memory and is read once a block).
 constexpr int kFewRowsWaves = 8;
 template <int D>
 struct FewRowsLds {
@@ -1296,8 +1297,8 @@ sqap_status launch_cache8_read(const Cache8View &cache, int d, const int32_t *le
 }
 
 // Tiles of 16 rows, whose blocks are dealt to eight wavefronts, where there would be few tiles of 128: 148 rows of 32 heads (64 of those) take
-// 8.7 us so and 11.1 otherwise, 512 of 8 heads (32) 7.6 and 18.7, 20 of 32 heads over 8 behind 2000 (8) 17 and 61, 1500 of 8 behind 2000
-// (96) 61 and 99, 300 of 32 heads (96) 13.7 and 15.2; but 500 of 32 (128) 25.0 and 21.6, 1000 of 32 over 8 (256) 56 and 36.
+// 9.0 us so and 11.0 otherwise, 512 of 8 heads (32) 8.0 and 19.0, 20 of 32 heads over 8 behind 2000 (8) 18 and 62, 1500 of 8 behind 2000
+// (96) 67 and 103, 300 of 32 heads (96) 13.9 and 15.1; but 500 of 32 (128) 23.7 and 21.3, 1000 of 32 over 8 (256) 56 and 37.
 constexpr int kFewTiles = 96;
 
 template <int D>
