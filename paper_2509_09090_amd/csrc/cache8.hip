@@ -364,8 +364,9 @@ struct Unit {
     }
 };
 
-// The maximum is the rounded product of a score and the keys' scale, the scores that are taken from it enter by a multiply-add, unrounded:
-// from here on (in units of ln 2) the difference could be more than a few, and the scores are rounded as well.
+// The maximum is the rounded product of a score and the keys' scale, the scores that are taken from it enter by a multiply-add, unrounded, which
+// also takes in the maximum and the probabilities' factor as one number.  From here on (in units of ln 2) either rounding could be worth more than a
+// probability has room for: the scores are rounded as well, and the maximum is taken from them before anything else.
 constexpr float kLargeScore = 1048576.f;
 // The maximum lags behind by up to this: with 32 rows to a wavefront some row has a new one in most blocks, and the sums are 64 registers.
 constexpr float kRaiseBy = 6.f;
@@ -550,22 +551,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
                 for (int i = 0; i < 16; ++i) top = fmaxf(top, s[tt][i]);
             top = fmaxf(top, __shfl_xor(top, 32));
             if (top > -INFINITY) top *= sk;                           // (nothing seen: it stays, whatever the scale)
-            float by = sk;
-            const bool bad = !(sk >= 0.f && sv >= 0.f);               // keys or values that are NaN as a whole: for the rows that see any of them
-            if (bad || __any(fabsf(top) > kLargeScore && top > -INFINITY)) {        // (a masked score times NaN would be NaN, too)
-#pragma unroll
-                for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        float w = bad ? NAN : s[tt][i] * sk;
-                        asm volatile("" : "+v"(w));                   // (rounded)
-                        s[tt][i] = s[tt][i] == -INFINITY ? -INFINITY : w;
-                    }
-                by = 1.f;
-            }
             float change;
             const float factor = unit.enter(sv, change);
-            if (top > mrun + kRaiseBy) {                              // (a row that sees nothing of the block keeps its maximum)
+            if (top - mrun > kRaiseBy) {                              // (a row that sees nothing of the block keeps its maximum)
                 const float raise = exp2f(mrun - top);
                 change *= raise;
                 lrun *= raise;
@@ -577,7 +565,21 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
 #pragma unroll
                     for (int i = 0; i < 16; ++i) ot[ct][i] *= change;
             }
-            const float from = (__log2f(factor) + kLift) - mrun;
+            float by = sk, from = __log2f(factor) + kLift;
+            const bool bad = !(sk >= 0.f && sv >= 0.f);               // keys or values that are NaN as a whole: for the rows that see any of them
+            if (bad || __any(fabsf(top) > kLargeScore && top > -INFINITY)) {        // (a masked score times NaN would be NaN, too)
+#pragma unroll
+                for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float w = bad ? NAN : s[tt][i] * sk;
+                        asm volatile("" : "+v"(w));                   // (rounded)
+                        s[tt][i] = s[tt][i] == -INFINITY ? -INFINITY : w - mrun;
+                    }
+                by = 1.f;
+            } else {
+                from -= mrun;
+            }
             float sum = 0.f;
 #pragma unroll
             for (int n = 0; n < 4; ++n) {                             // 16 positions at a time: all at once would not leave the registers
@@ -680,22 +682,9 @@ struct WaveSums {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         if (top > -INFINITY) top *= sk;
-        float by = sk;
-        const bool bad = !(sk >= 0.f && sv >= 0.f);                   // (NaN as a whole: as in cache8_attention_kernel)
-        if (bad || __any(fabsf(top) > kLargeScore && top > -INFINITY)) {
-#pragma unroll
-            for (int T4 = 0; T4 < 4; ++T4)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float w = bad ? NAN : s[T4][i] * sk;
-                    asm volatile("" : "+v"(w));                       // (rounded)
-                    s[T4][i] = s[T4][i] == -INFINITY ? -INFINITY : w;
-                }
-            by = 1.f;
-        }
         float change;
         const float factor = unit.enter(sv, change);
-        if (top > m + kRaiseBy) {
+        if (top - m > kRaiseBy) {
             const float raise = exp2f(m - top);
             change *= raise;
             l *= raise;
@@ -706,7 +695,22 @@ struct WaveSums {
             for (int i = 0; i < D / 16; ++i) o[i] *= change;
         }
         // (no score above minus infinity so far: nothing is added, other wavefronts' blocks may have some)
-        const float from = (__log2f(factor) + kLift) - (m == -INFINITY ? 0.f : m);
+        const float taken = m == -INFINITY ? 0.f : m;
+        float by = sk, from = __log2f(factor) + kLift;
+        const bool bad = !(sk >= 0.f && sv >= 0.f);                   // (NaN as a whole: as in cache8_attention_kernel)
+        if (bad || __any(fabsf(top) > kLargeScore && top > -INFINITY)) {
+#pragma unroll
+            for (int T4 = 0; T4 < 4; ++T4)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float w = bad ? NAN : s[T4][i] * sk;
+                    asm volatile("" : "+v"(w));                       // (rounded)
+                    s[T4][i] = s[T4][i] == -INFINITY ? -INFINITY : w - taken;
+                }
+            by = 1.f;
+        } else {
+            from -= taken;
+        }
         float sum = 0.f;
 #pragma unroll
         for (int n = 0; n < 2; ++n) {

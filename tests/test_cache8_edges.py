@@ -140,3 +140,59 @@ def test_no_rows_announced(G):                                                  
     got = o.cpu().numpy()
     assert np.isnan(got[2:33]).all() and np.all(got[:2] == 9) and np.all(got[33:] == 9)
     assert torch.equal(keep.view(torch.uint8), m.cache.tail.view(torch.uint8))
+
+
+LARGE = [(2.0 ** e, sign) for e in (10, 19, 21, 24.5, 25.5, 26.5, 27.5, 28.5, 29.4) for sign in (1, -1)]
+
+
+def _level(n, score, sign, rng):
+    """One head of 64 whose scores are all the same, near sign * score in units of ln 2, and values that all blocks have the same largest of."""
+    x = np.zeros((n, 3, 64), np.float16)
+    each = np.sqrt(score * np.log(2) * 8)
+    x[:, 0, 0], x[:, 1, 0] = each, sign * each
+    x[:, 2] = rng.uniform(-1, 1, (n, 64))
+    x[:, 2, 0] = 1
+    return x
+
+
+@pytest.mark.parametrize("score,sign", LARGE)
+def test_level_scores_of_any_size_in_prompts(G, announced, score, sign):                     # noqa: F811
+    """Scores so large that a unit of their last place is more than a probability's exponent: where all are alike the outputs are means all the same."""
+    import torch
+    n, rng = 300, np.random.default_rng(int(score) % 1009)
+    x, most = _level(n, score, sign, rng), max(n, Model.most)
+    dev = lambda a: G.to_dev(np.asarray(a, dtype=np.int32))                                   # noqa: E731
+    cache, starts, past = B.Cache8(1, n, 1, 64, device=G.DEV), dev([0, n]), dev([0])
+    q, o = (torch.zeros((most, 64), dtype=torch.float16, device=G.DEV) for _ in range(2))
+    rows = torch.zeros((most, 192), dtype=torch.float16, device=G.DEV)
+    rows[:n] = G.to_dev(x.reshape(n, -1))
+    B.sqap_cache8_append(rows, starts, torch.zeros(most, dtype=torch.int32, device=G.DEV), past, cache, 1, most, Q_out=q)
+    B.sqap_cache8_attention(q, starts, past, cache, 1, most, o)
+    got, v = o[:n].cpu().numpy().astype(np.float64), R.held(x[:, 2])
+    _check_means(got, np.cumsum(v, 0) / np.arange(1, n + 1)[:, None], np.cumsum(np.abs(v), 0) / np.arange(1, n + 1)[:, None], score)
+
+
+def _check_means(got, want, mass, score):
+    """The unfinished block's keys are not what the finished ones' codes stand for to the last place of binary32: that parts their weights by up to 2^-22
+    of the score (codes times scale, the product, its scale).  Where this is no longer small, outputs are some mean of the values, and exact for ones."""
+    off = 2.0 ** -22 * score
+    assert np.isfinite(got).all()
+    if off < 0.01:
+        assert np.all(np.abs(got - want) <= R.HALF_STEP * np.abs(want) + R.HALF_TINY + (2.0 ** -18 + 2 * off) * mass)
+    assert np.all(np.abs(got) <= 1 + R.HALF_STEP) and np.all(np.abs(got[:, 0] - 1) <= R.HALF_STEP)
+
+
+@pytest.mark.parametrize("longest", [64, 1025])
+@pytest.mark.parametrize("score,sign", LARGE)
+def test_level_scores_of_any_size_in_single_rows(G, score, sign, longest):                   # noqa: F811
+    import torch
+    n, rng = 1000, np.random.default_rng(int(score) % 1009)
+    dev = lambda a: G.to_dev(np.asarray(a, dtype=np.int32))                                   # noqa: E731
+    cache, x = B.Cache8(1, n + 1, 1, 64, device=G.DEV), _level(n + 1, score, sign, rng)
+    rows = G.to_dev(x.reshape(n + 1, -1))
+    B.sqap_cache8_append(rows[:n], dev([0, n]), dev(np.zeros(n)), dev([0]), cache, 1, n)
+    o = torch.zeros((1, 64), dtype=torch.float16, device=G.DEV)
+    ws = torch.zeros((B.sqap_cache8_workspace_bytes(1, 1, 1, 64, longest),), dtype=torch.uint8, device=G.DEV)
+    B.sqap_cache8_decode_attention(rows[n:], dev([0]), dev([n]), cache, 1, o, ws, longest)
+    v = R.held(x[:, 2])
+    _check_means(o.cpu().numpy().astype(np.float64), v.mean(0)[None], np.abs(v).mean(0)[None], score)
