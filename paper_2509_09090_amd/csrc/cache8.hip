@@ -400,7 +400,8 @@ __device__ __forceinline__ void nan_rows(__half *O, int64_t ldo, int first, int6
 // halves reaches 1.24); with probabilities of one half, 32 matrix instructions and 305 others, it was 230, and the outputs 2.0e-4 of their norm
 // further off.  (Then the next block's scores multiplied between this one's probabilities, in the same wavefront: 335 us, the registers do not suffice.)
 // A block's p = 2^(s - m) times its factor is one exponential, of s sk + (log2 factor - m); the sum of the probabilities is put right by the
-// factor once per block.
+// factor once per block.  The hardware's exponential, logarithm and reciprocal are off by a unit of the last place of binary32 or so each, which is
+// less than the rounding of the scores and of the sums.
 template <int D, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const __half *__restrict__ Q, int64_t ldq, const int32_t *__restrict__ starts,
                                                                          const int32_t *__restrict__ past, int rows, int max_new, int H,
