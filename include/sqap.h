@@ -545,6 +545,21 @@ sqap_status sqap_cache8_read(const sqap_cache8 *cache, const int32_t *lengths, i
                              sqap_f16 *out, int64_t ld, void *stream);
 
 /*
+ * The sequences of a cache take over what others hold, in place, as a beam search asks for it.  They stand in groups of `width` (which divides
+ * cache->batch); parents [cache->batch] int32, device, says for each which of its group (0 .. width - 1) it continues, as
+ * sqap_beam_select leaves it.  Afterwards sequence i holds the positions that its parent held before the call, lengths[parent] of them
+ * (lengths [cache->batch] int32, device), bit for bit.  One that is its own parent, or whose parent is not one of the group (-1), stays as it is.
+ * lengths_out: NULL, or [cache->batch] int32, device: the lengths afterwards.  longest: the longest sequence's length, as far as the
+ * host knows; it decides how the work is split, nothing else.
+ * Written is what holds those positions: whole blocks, and rows of the tail below the length; everything else is left as it was.  A parent
+ * whose length is not within 1 .. capacity has nothing that could be taken over; its length is handed on all the same.  May be captured.
+ * EINVAL: null pointer, cache sizes as above, width <= 0 or not a divisor of the batch, longest < 0, lengths_out over lengths or
+ * parents.  EUNSUPPORTED: width > 64, and as above.
+ */
+sqap_status sqap_cache8_reorder(const sqap_cache8 *cache, const int32_t *parents, int32_t width, const int32_t *lengths,
+                                int32_t longest, int32_t *lengths_out, void *stream);
+
+/*
  * The next token of each of `batch` rows of logits [batch, vocab] (halves, pitch ld, any alignment), as the vocabulary
  * head or sqap_decoder_step leaves them.  Tokens are ranked by logit, the lower index first among equals (-0 == +0;
  * NaN and minus infinity are never drawn).  With w = exp((l - max) / temperature):
@@ -565,6 +580,30 @@ sqap_status sqap_cache8_read(const sqap_cache8 *cache, const int32_t *lengths, i
 sqap_status sqap_sample(const sqap_f16 *logits, int64_t ld, int32_t batch, int32_t vocab, const float *temperature,
                         const int32_t *top_k, const float *top_p, const float *min_p, const float *uniform,
                         int32_t *token_out, float *prob_out, void *stream);
+
+/*
+ * A step of a beam search: for each of `batch` elements the k best continuations of its `beams` beams.  logits: rows
+ * [batch * beams, vocab] (halves, pitch ld, any alignment), beam by beam; scores [batch, beams] binary32, device: the beams' sums of
+ * logarithms.  A continuation's total is
+ *   scores[beam] + (l[token] - log sum_v exp(l[v])),
+ * and they are ranked by it, in binary64 (the sum of exponentials is off by some 2^-24 of itself); of equal totals the lower beam, then the
+ * higher logit, then the lower token comes first.  -0 == +0; logits that are NaN or minus infinity have no probability; where there are infinite
+ * ones, each of them has the same and the others none.
+ * done: NULL, or [batch, beams] int32, device: a beam that has finished (not 0) has one continuation, the token eos at its own score, and its
+ * logits are not read.  Beams whose score is NaN or minus infinity have none (so that a search may start with one beam).
+ * parent_out, token_out [batch, k] int32, score_out [batch, k] binary32 (the total, rounded once): best first; where there are fewer than k
+ * continuations -1, -1 and minus infinity.  done_out: NULL, or [batch, k] int32: 1 where the parent has finished or the token is eos, else 0.
+ * With k = beams score_out may be scores, done_out done.
+ * workspace: at least sqap_beam_workspace_bytes(batch, beams, vocab, k) bytes, 16-byte aligned, of any contents; calls that share it must be
+ * ordered on one stream, graphs that are replayed side by side need one each.  May be captured.
+ * EINVAL: null pointer, negative batch, beams, vocab or k < 1, ld < vocab, done with an eos outside 0 .. vocab - 1 (without it eos may be any
+ * number, -1 for none), outputs over inputs otherwise, workspace missing, too small or misaligned.  EUNSUPPORTED: more than 64 beams or outputs,
+ * vocab > 1048576, more than 2^24 - 1 rows times 2048 tokens.
+ */
+size_t sqap_beam_workspace_bytes(int32_t batch, int32_t beams, int32_t vocab, int32_t k);
+sqap_status sqap_beam_select(const sqap_f16 *logits, int64_t ld, int32_t batch, int32_t beams, int32_t vocab, const float *scores,
+                             const int32_t *done, int32_t eos, int32_t k, int32_t *parent_out, int32_t *token_out,
+                             float *score_out, int32_t *done_out, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Self-test of the quantizer's arithmetic.  The quantizer divides every element

@@ -30,7 +30,7 @@ EXPORTS = (
     "sqap_decoder_set_wait_limit", "sqap_decoder_free",
     "sqap_mx4_quantize", "sqap_mx4_weight_pack", "sqap_mx4_weight_free", "sqap_mx4_weight_info", "sqap_mx4_linear",
     "sqap_cache8_append", "sqap_cache8_attention", "sqap_cache8_workspace_bytes", "sqap_cache8_decode_attention", "sqap_cache8_read",
-    "sqap_sample",
+    "sqap_sample", "sqap_cache8_reorder", "sqap_beam_workspace_bytes", "sqap_beam_select",
 )
 
 
@@ -137,8 +137,12 @@ def lib():
         L.sqap_cache8_decode_attention.argtypes = [vp, i64, vp, vp, i32, ctypes.c_double, cache, i32, vp, i64, vp, sz, vp]
         L.sqap_cache8_read.argtypes = [cache, vp, i32, i32, vp, i64, vp]
         L.sqap_sample.argtypes = [vp, i64, i32, i32] + [vp] * 8
+        L.sqap_cache8_reorder.argtypes = [cache, vp, i32, vp, i32, vp, vp]
+        L.sqap_beam_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.sqap_beam_workspace_bytes.restype = sz
+        L.sqap_beam_select.argtypes = [vp, i64, i32, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp, sz, vp]
         for name in EXPORTS:
-            if name not in ("sqap_last_error", "sqap_version", "sqap_workspace_bytes", "sqap_attn_scores_workspace_bytes", "sqap_cache8_workspace_bytes"):
+            if name not in ("sqap_last_error", "sqap_version") and not name.endswith("workspace_bytes"):
                 getattr(L, name).restype = ctypes.c_int32
         _lib = L
     return _lib
@@ -505,6 +509,25 @@ def sqap_sample(logits, temperature, top_k, top_p, min_p, uniform, token_out, pr
     """Next tokens of logits [batch, vocab] fp16: temperature, top_p, min_p [batch] fp32 and top_k [batch] int32, each or None;
     uniform [batch] fp32 in [0, 1) -> token_out [batch] int32, prob_out [batch] fp32 or None."""
     _native.sample(logits, temperature, top_k, top_p, min_p, uniform, token_out, prob_out, stream)
+
+
+def sqap_cache8_reorder(cache, parents, lengths, longest, lengths_out=None, stream=None):
+    """The sequences of a Cache8, in groups of `width`, take over what others of their group hold: parents [groups, width] int32
+    (-1: stays), lengths [batch] int32 before, lengths_out [batch] int32 after or None; longest: the longest length, as far as known."""
+    if parents.numel() != cache.batch:
+        raise ValueError("%d parents for %d sequences" % (parents.numel(), cache.batch))
+    _native.cache8_reorder(cache.handle, parents, lengths, longest, lengths_out, stream)
+
+
+def sqap_beam_workspace_bytes(batch, beams, vocab, k):
+    return int(lib().sqap_beam_workspace_bytes(batch, beams, vocab, k))
+
+
+def sqap_beam_select(logits, scores, done, eos, parent_out, token_out, score_out, done_out, workspace, stream=None):
+    """The k best continuations of each batch element: logits [batch * beams, vocab] fp16, scores [batch, beams] fp32, done [batch, beams]
+    int32 or None -> parent_out, token_out [batch, k] int32, score_out [batch, k] fp32, done_out [batch, k] int32 or None.  workspace:
+    device bytes (see sqap_beam_workspace_bytes)."""
+    _native.beam_select(logits, scores, done, eos, parent_out, token_out, score_out, done_out, workspace, stream)
 
 
 class Group:

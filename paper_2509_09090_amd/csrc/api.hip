@@ -847,6 +847,70 @@ sqap_status sqap_cache8_read(const sqap_cache8 *cache, const int32_t *lengths, i
     return launch_cache8_read(v, cache->head_dim, lengths, first, count, reinterpret_cast<__half *>(out), ld, as_stream(stream));
 }
 
+// two ranges of 32-bit words that lie over each other
+static bool overlap(const void *x, int64_t n, const void *y, int64_t m)
+{
+    const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y);
+    return a < b + 4 * (uintptr_t)m && b < a + 4 * (uintptr_t)n;
+}
+
+sqap_status sqap_cache8_reorder(const sqap_cache8 *cache, const int32_t *parents, int32_t width, const int32_t *lengths, int32_t longest,
+                                int32_t *lengths_out, void *stream)
+{
+    const char *who = "sqap_cache8_reorder";
+    Cache8View v = {};
+    sqap_status s = check_cache8(who, cache, cache ? cache->kv_heads : 1, &v);
+    if (s != SQAP_OK) return s;
+    if (width <= 0 || cache->batch % width != 0) return fail(SQAP_EINVAL, "%s: %d sequences in groups of %d", who, cache->batch, width);
+    if (longest < 0) return fail(SQAP_EINVAL, "%s: longest = %d", who, longest);
+    if (width > kBeamMostOutputs) return fail(SQAP_EUNSUPPORTED, "%s: groups of %d > %d", who, width, kBeamMostOutputs);
+    if (cache->batch == 0) return SQAP_OK;
+    if (!parents || !lengths) return fail(SQAP_EINVAL, "%s: null pointer", who);
+    if (lengths_out && (overlap(lengths_out, cache->batch, lengths, cache->batch) || overlap(lengths_out, cache->batch, parents, cache->batch)))
+        return fail(SQAP_EINVAL, "%s: lengths_out lies over lengths or parents", who);
+    const DeviceOfCall device;
+    return launch_cache8_reorder(v, cache->head_dim, parents, width, lengths, longest, lengths_out, as_stream(stream));
+}
+
+static sqap_status check_beam(const char *who, int32_t batch, int32_t beams, int32_t vocab, int32_t k)
+{
+    if (batch < 0 || beams < 1 || vocab < 1 || k < 1) return fail(SQAP_EINVAL, "%s: batch %d, %d beams, vocab %d, %d outputs", who, batch, beams, vocab, k);
+    if (beams > kBeamMostOutputs || k > kBeamMostOutputs || vocab > kSampleMaxVocab || (int64_t)batch * beams * ((vocab + 2047) / 2048) > most_workgroups(256))
+        return fail(SQAP_EUNSUPPORTED, "%s: batch %d, %d beams, vocab %d, %d outputs", who, batch, beams, vocab, k);
+    return SQAP_OK;
+}
+
+size_t sqap_beam_workspace_bytes(int32_t batch, int32_t beams, int32_t vocab, int32_t k)
+{
+    if (batch <= 0 || beams < 1 || vocab < 1 || k < 1) return 0;
+    return beam_workspace_bytes(batch, beams, vocab, k);
+}
+
+sqap_status sqap_beam_select(const sqap_f16 *logits, int64_t ld, int32_t batch, int32_t beams, int32_t vocab, const float *scores, const int32_t *done,
+                             int32_t eos, int32_t k, int32_t *parent_out, int32_t *token_out, float *score_out, int32_t *done_out, void *workspace,
+                             size_t workspace_bytes, void *stream)
+{
+    const char *who = "sqap_beam_select";
+    const sqap_status s = check_beam(who, batch, beams, vocab, k);
+    if (s != SQAP_OK) return s;
+    if (ld < vocab) return fail(SQAP_EINVAL, "%s: pitch %lld below vocab %d", who, (long long)ld, vocab);
+    if (done && (eos < 0 || eos >= vocab)) return fail(SQAP_EINVAL, "%s: finished beams and the token %d of %d", who, eos, vocab);
+    if (batch == 0) return SQAP_OK;
+    if (!logits || !scores || !parent_out || !token_out || !score_out) return fail(SQAP_EINVAL, "%s: null pointer", who);
+    const int64_t in = (int64_t)batch * beams, out = (int64_t)batch * k;
+    const bool in_place = k == beams;
+    if ((overlap(score_out, out, scores, in) && !(in_place && score_out == scores)) ||
+        (done && done_out && overlap(done_out, out, done, in) && !(in_place && done_out == done)))
+        return fail(SQAP_EINVAL, "%s: outputs lie over inputs of another layout", who);
+    const size_t need = beam_workspace_bytes(batch, beams, vocab, k);
+    if (!workspace || workspace_bytes < need)
+        return fail(SQAP_EINVAL, "%s: workspace of %zu bytes needed, %zu given", who, need, workspace ? workspace_bytes : (size_t)0);
+    if (!aligned16(workspace)) return fail(SQAP_EINVAL, "%s: workspace must be 16-byte aligned", who);
+    const DeviceOfCall device;
+    return launch_beam_select(reinterpret_cast<const __half *>(logits), ld, batch, beams, vocab, scores, done, eos, k, parent_out, token_out, score_out,
+                              done_out, workspace, as_stream(stream));
+}
+
 sqap_status sqap_sample(const sqap_f16 *logits, int64_t ld, int32_t batch, int32_t vocab, const float *temperature, const int32_t *top_k,
                         const float *top_p, const float *min_p, const float *uniform, int32_t *token_out, float *prob_out, void *stream)
 {

@@ -135,6 +135,13 @@ void of_channels(const char *what, int64_t have, int64_t channels)
     throw PyFailed{};
 }
 
+void of_rows(int64_t have, int64_t rows)
+{
+    if (have == rows) return;
+    PyErr_Format(PyExc_ValueError, "%lld rows for %lld", (long long)have, (long long)rows);
+    throw PyFailed{};
+}
+
 int64_t rows_of(PyObject *X, PyObject *rows) { return rows == Py_None ? size(X, 0) : count(rows); }
 
 struct Calls {
@@ -157,7 +164,9 @@ struct Calls {
     decltype(&sqap_cache8_append) cache8_append;
     decltype(&sqap_cache8_attention) cache8_attention;
     decltype(&sqap_cache8_decode_attention) cache8_decode_attention;
+    decltype(&sqap_cache8_reorder) cache8_reorder;
     decltype(&sqap_sample) sample;
+    decltype(&sqap_beam_select) beam_select;
     decltype(&sqap_group_run) group_run;
     decltype(&sqap_decoder_step) decoder_step;
     PyObject *failed;                     // called with a status that is not zero: raises
@@ -274,6 +283,16 @@ SQAP_METHOD(cache8_decode_attention, 10,
 SQAP_METHOD(sample, 9,
             run(c->sample, ptr<sqap_f16>(a[0]), pitch(a[0]), (int32_t)size_of(a[0], 2, 0), (int32_t)size_of(a[0], 2, 1), ptr<float>(a[1]),
                 ptr<int32_t>(a[2]), ptr<float>(a[3]), ptr<float>(a[4]), ptr<float>(a[5]), ptr<int32_t>(a[6]), ptr<float>(a[7]), stream(c, a[8])))
+// (cache, parents [groups, width], lengths, longest, lengths_out, stream)
+SQAP_METHOD(cache8_reorder, 6,
+            run(c->cache8_reorder, handle<sqap_cache8>(a[0]), ptr<int32_t>(a[1]), (int32_t)size_of(a[1], 2, 1), ptr<int32_t>(a[2]), as_i32(a[3]),
+                ptr<int32_t>(a[4]), stream(c, a[5])))
+// (logits, scores [batch, beams], done, eos, parents [batch, k], tokens, scores, done, workspace, stream)
+SQAP_METHOD(beam_select, 10,
+            (of_rows(size_of(a[0], 2, 0), size_of(a[1], 2, 0) * size_of(a[1], 2, 1)), of_rows(size_of(a[4], 2, 0), size_of(a[1], 2, 0)),
+             run(c->beam_select, ptr<sqap_f16>(a[0]), pitch(a[0]), (int32_t)size(a[1], 0), (int32_t)size(a[1], 1), (int32_t)size(a[0], 1),
+                 ptr<float>(a[1]), ptr<int32_t>(a[2]), as_i32(a[3]), (int32_t)size(a[4], 1), ptr<int32_t>(a[4]), ptr<int32_t>(a[5]),
+                 ptr<float>(a[6]), ptr<int32_t>(a[7]), ptr(a[8]), bytes(a[8]), stream(c, a[9]))))
 SQAP_METHOD(group_run, 2, run(c->group_run, handle<sqap_group>(a[0]), stream(c, a[1])))
 SQAP_METHOD(decoder_step, 7,
             run(c->decoder_step, handle<sqap_decoder>(a[0]), ptr<sqap_f16>(a[1]), ptr<int32_t>(a[2]), as_i32(a[3]), ptr<sqap_f16>(a[4]),
@@ -300,7 +319,7 @@ SQAP_METHOD(attention, 8, attention_call(c, a))
 #define SQAP_CALLS(X)                                                                                                                   \
     X(attn_scores_batch) X(prune_topk) X(kept_rows) X(prune_rows) X(prune_select) X(quantize_act) X(rmsnorm_quantize_act)              \
     X(swiglu_quantize_act) X(rope) X(rope_append) X(attention) X(decode_attention) X(w4a4_linear) X(mx4_quantize) X(mx4_linear)        \
-    X(cache8_append) X(cache8_attention) X(cache8_decode_attention) X(sample) X(group_run) X(decoder_step)
+    X(cache8_append) X(cache8_attention) X(cache8_decode_attention) X(cache8_reorder) X(sample) X(beam_select) X(group_run) X(decoder_step)
 
 PyMethodDef methods[] = {
 #define SQAP_ENTRY(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(m_##NAME)), METH_FASTCALL, nullptr},
