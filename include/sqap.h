@@ -545,6 +545,42 @@ sqap_status sqap_cache8_read(const sqap_cache8 *cache, const int32_t *lengths, i
                              sqap_f16 *out, int64_t ld, void *stream);
 
 /*
+ * Attention of sequences that share long prefixes, each prefix read once for all of its sequences.  The prefixes are sequences of a cache of
+ * their own, `prefix` (as many key heads, of the same size; any capacity), filled by sqap_cache8_append; prefix_len [prefix->batch] int32,
+ * device, says how many positions each has (0: none).  The sequences of `cache` stand in groups of width = cache->batch / prefix->batch, sequence b
+ * behind prefix b / width, and hold their own positions: past [cache->batch] does not count the prefix.  Row j of sequence b sees
+ * the whole prefix and its own positions 0 .. past[b] + j:
+ *   o = sum_t softmax_t((q . k_t) / sqrt(d)) v_t   over both,
+ * in the precision of sqap_cache8_attention.  Positions of the rotation are the caller's (pos, with the prefix's length in them as a rule).
+ *
+ * sqap_cache8_shared_attention: rotated queries Q of rows that sqap_cache8_append has appended to `cache` (starts, past, rows, max_new as there); O may be Q.
+ * sqap_cache8_shared_decode_attention: one new row per sequence, as sqap_cache8_decode_attention: append and attention.
+ *
+ * longest, longest_prefix: the most own positions (the new one included) and the longest prefix as far as the host knows; they decide how the work
+ * is split, nothing else.  workspace: at least sqap_cache8_shared_workspace_bytes(cache->batch, prefix->batch, H, kv_heads, head_dim, rows, max_new, longest,
+ * longest_prefix) bytes (a decode call: rows = cache->batch, max_new = 1; a prompt: longest = 1 will do), 16-byte aligned, of any contents; its first 16384
+ * bytes are left alone, so that it may be that of the other calls.  Calls that share a workspace must be ordered on one stream; graphs that
+ * are replayed side by side need one each.
+ *
+ * As above a sequence with past[b] < 0 or without rows is skipped; one whose rows do not fit or are more than max_new gets outputs of NaN; so do
+ * the sequences of a group of more than width * max_new rows in all, and of a prefix whose prefix_len is negative or beyond its capacity
+ * (appended to they are all the same).  One whose starts do not lie in order, or outside those of its group's first and last, is skipped.
+ * EINVAL, EUNSUPPORTED: as above; EINVAL also for a cache of prefixes of other heads, a batch that is no multiple of theirs, longest_prefix < 0;
+ * EUNSUPPORTED for more than 13107 sequences, rows of a group times H / kv_heads beyond 32 bits.
+ */
+size_t sqap_cache8_shared_workspace_bytes(int32_t batch, int32_t groups, int32_t H, int32_t kv_heads, int32_t head_dim,
+                                          int32_t rows, int32_t max_new, int32_t longest, int32_t longest_prefix);
+sqap_status sqap_cache8_shared_attention(const sqap_f16 *Q, int64_t ldq, const int32_t *starts, const int32_t *past,
+                                         int32_t rows, int32_t max_new, int32_t H, const sqap_cache8 *cache,
+                                         const sqap_cache8 *prefix, const int32_t *prefix_len, int32_t longest_prefix,
+                                         sqap_f16 *O, int64_t ldo, void *workspace, size_t workspace_bytes, void *stream);
+sqap_status sqap_cache8_shared_decode_attention(const sqap_f16 *QKV, int64_t ld, const int32_t *pos, const int32_t *past,
+                                                int32_t H, double base, const sqap_cache8 *cache, const sqap_cache8 *prefix,
+                                                const int32_t *prefix_len, int32_t longest, int32_t longest_prefix,
+                                                sqap_f16 *O, int64_t ldo, void *workspace, size_t workspace_bytes,
+                                                void *stream);
+
+/*
  * The sequences of a cache take over what others hold, in place, as a beam search asks for it.  They stand in groups of `width` (which divides
  * cache->batch); parents [cache->batch] int32, device, says for each which of its group (0 .. width - 1) it continues, as
  * sqap_beam_select leaves it.  Afterwards sequence i holds the positions that its parent held before the call, lengths[parent] of them

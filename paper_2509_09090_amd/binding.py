@@ -30,7 +30,7 @@ EXPORTS = (
     "sqap_decoder_set_wait_limit", "sqap_decoder_free",
     "sqap_mx4_quantize", "sqap_mx4_weight_pack", "sqap_mx4_weight_free", "sqap_mx4_weight_info", "sqap_mx4_linear",
     "sqap_cache8_append", "sqap_cache8_attention", "sqap_cache8_workspace_bytes", "sqap_cache8_decode_attention", "sqap_cache8_read",
-    "sqap_sample", "sqap_cache8_reorder", "sqap_beam_workspace_bytes", "sqap_beam_select",
+    "sqap_sample", "sqap_cache8_shared_workspace_bytes", "sqap_cache8_shared_attention", "sqap_cache8_shared_decode_attention", "sqap_cache8_reorder", "sqap_beam_workspace_bytes", "sqap_beam_select",
 )
 
 
@@ -137,7 +137,11 @@ def lib():
         L.sqap_cache8_decode_attention.argtypes = [vp, i64, vp, vp, i32, ctypes.c_double, cache, i32, vp, i64, vp, sz, vp]
         L.sqap_cache8_read.argtypes = [cache, vp, i32, i32, vp, i64, vp]
         L.sqap_sample.argtypes = [vp, i64, i32, i32] + [vp] * 8
-        L.sqap_cache8_reorder.argtypes = [cache, vp, i32, vp, i32, vp, vp]
+        L.sqap_cache8_shared_workspace_bytes.argtypes = [i32] * 9
+        L.sqap_cache8_shared_workspace_bytes.restype = sz
+        L.sqap_cache8_shared_attention.argtypes = [vp, i64, vp, vp, i32, i32, i32, vp, vp, vp, i32, vp, i64, vp, sz, vp]
+        L.sqap_cache8_shared_decode_attention.argtypes = [vp, i64, vp, vp, i32, ctypes.c_double, vp, vp, vp, i32, i32, vp, i64, vp, sz, vp]
+        L.sqap_cache8_reorder.argtypes = [vp, vp, i32, vp, i32, vp, vp]
         L.sqap_beam_workspace_bytes.argtypes = [i32, i32, i32, i32]
         L.sqap_beam_workspace_bytes.restype = sz
         L.sqap_beam_select.argtypes = [vp, i64, i32, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp, sz, vp]
@@ -509,6 +513,23 @@ def sqap_sample(logits, temperature, top_k, top_p, min_p, uniform, token_out, pr
     """Next tokens of logits [batch, vocab] fp16: temperature, top_p, min_p [batch] fp32 and top_k [batch] int32, each or None;
     uniform [batch] fp32 in [0, 1) -> token_out [batch] int32, prob_out [batch] fp32 or None."""
     _native.sample(logits, temperature, top_k, top_p, min_p, uniform, token_out, prob_out, stream)
+
+
+def sqap_cache8_shared_workspace_bytes(batch, groups, H, kv_heads, head_dim, rows, max_new, longest, longest_prefix):
+    return int(lib().sqap_cache8_shared_workspace_bytes(batch, groups, H, kv_heads, head_dim, rows, max_new, longest, longest_prefix))
+
+
+def sqap_cache8_shared_attention(Q, starts, past, cache, prefix, prefix_len, H, max_new, O, workspace, longest_prefix, stream=None):
+    """As sqap_cache8_attention, for sequences in groups behind the sequences of another Cache8, `prefix`, which hold prefix_len [groups]
+    int32 positions; past counts a sequence's own ones.  workspace: device bytes (see sqap_cache8_shared_workspace_bytes)."""
+    _native.cache8_shared_attention(Q, starts, past, cache.handle, prefix.handle, prefix_len, H, max_new, O, workspace, longest_prefix, stream)
+
+
+def sqap_cache8_shared_decode_attention(QKV, pos, past, cache, prefix, prefix_len, H, O, workspace, longest, longest_prefix, base=10000.0,
+                                        stream=None):
+    """As sqap_cache8_decode_attention, for sequences in groups behind the sequences of another Cache8, `prefix`."""
+    _native.cache8_shared_decode_attention(QKV, pos, past, cache.handle, prefix.handle, prefix_len, H, O, workspace, longest, longest_prefix, base,
+                                           stream)
 
 
 def sqap_cache8_reorder(cache, parents, lengths, longest, lengths_out=None, stream=None):

@@ -847,6 +847,94 @@ sqap_status sqap_cache8_read(const sqap_cache8 *cache, const int32_t *lengths, i
     return launch_cache8_read(v, cache->head_dim, lengths, first, count, reinterpret_cast<__half *>(out), ld, as_stream(stream));
 }
 
+// a cache of prefixes, and the groups of sequences behind them
+static sqap_status check_prefix(const char *who, const sqap_cache8 *cache, const sqap_cache8 *prefix, const int32_t *prefix_len, int32_t longest_prefix,
+                                int32_t H, Cache8View *out)
+{
+    const sqap_status s = check_cache8(who, prefix, H, out);
+    if (s != SQAP_OK) return s;
+    if (prefix->kv_heads != cache->kv_heads || prefix->head_dim != cache->head_dim)
+        return fail(SQAP_EINVAL, "%s: prefixes of %d key heads of %d, sequences of %d of %d", who, prefix->kv_heads, prefix->head_dim, cache->kv_heads, cache->head_dim);
+    if (cache->batch > 0 && (prefix->batch == 0 || cache->batch % prefix->batch != 0))
+        return fail(SQAP_EINVAL, "%s: %d sequences behind %d prefixes", who, cache->batch, prefix->batch);
+    if (longest_prefix < 0) return fail(SQAP_EINVAL, "%s: longest_prefix = %d", who, longest_prefix);
+    if (cache->batch > 0 && !prefix_len) return fail(SQAP_EINVAL, "%s: null pointer", who);
+    if (cache->batch > 13107) return fail(SQAP_EUNSUPPORTED, "%s: %d sequences", who, cache->batch);
+    return SQAP_OK;
+}
+
+static sqap_status check_workspace(const char *who, const void *workspace, size_t bytes, size_t need)
+{
+    if (!workspace || bytes < need) return fail(SQAP_EINVAL, "%s: workspace of %zu bytes needed, %zu given", who, need, workspace ? bytes : (size_t)0);
+    if (!aligned16(workspace)) return fail(SQAP_EINVAL, "%s: workspace must be 16-byte aligned", who);
+    return SQAP_OK;
+}
+
+size_t sqap_cache8_shared_workspace_bytes(int32_t batch, int32_t groups, int32_t H, int32_t kv_heads, int32_t head_dim, int32_t rows, int32_t max_new,
+                                          int32_t longest, int32_t longest_prefix)
+{
+    if (batch <= 0 || groups <= 0 || batch % groups != 0 || H <= 0 || kv_heads <= 0 || H % kv_heads != 0 || head_dim <= 0 || rows <= 0 || max_new <= 0 ||
+        longest <= 0 || longest_prefix < 0)
+        return 0;
+    return cache8_shared_workspace_bytes(batch, groups, H, kv_heads, head_dim, rows, max_new, longest, longest_prefix);
+}
+
+sqap_status sqap_cache8_shared_attention(const sqap_f16 *Q, int64_t ldq, const int32_t *starts, const int32_t *past, int32_t rows, int32_t max_new,
+                                         int32_t H, const sqap_cache8 *cache, const sqap_cache8 *prefix, const int32_t *prefix_len,
+                                         int32_t longest_prefix, sqap_f16 *O, int64_t ldo, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const char *who = "sqap_cache8_shared_attention";
+    Cache8View v = {}, p = {};
+    if (rows < 0 || max_new < 0) return fail(SQAP_EINVAL, "%s: rows %d, max_new %d", who, rows, max_new);
+    sqap_status s = check_cache8(who, cache, H, &v);
+    if (s == SQAP_OK) s = check_prefix(who, cache, prefix, prefix_len, longest_prefix, H, &p);
+    if (s != SQAP_OK || rows == 0 || cache->batch == 0) return s;
+    if (!starts || !past) return fail(SQAP_EINVAL, "%s: null pointer", who);
+    const int64_t width = (int64_t)H * cache->head_dim;
+    s = check_rows16(who, "Q", Q, ldq, width);
+    if (s == SQAP_OK) s = check_rows16(who, "O", O, ldo, width);
+    if (s != SQAP_OK) return s;
+    max_new = max_new < rows ? max_new : rows;
+    const int G = H / cache->kv_heads;
+    const int64_t pairs = (int64_t)max_new * G, together = (int64_t)(cache->batch / prefix->batch) * max_new;
+    const int64_t of_group = (together < rows ? together : rows) * G;
+    if (of_group > INT32_MAX - 128 || (pairs + 127) / 128 * cache->kv_heads * cache->batch > most_workgroups(256) ||
+        (of_group + 127) / 128 * cache->kv_heads * prefix->batch > most_workgroups(256))
+        return fail(SQAP_EUNSUPPORTED, "%s: %d rows of %d heads", who, max_new, H);
+    const int announced = max_new > 0 ? max_new : 1;                  // (none: any rows there are are too many)
+    s = check_workspace(who, workspace, workspace_bytes,
+                        cache8_shared_workspace_bytes(cache->batch, prefix->batch, H, cache->kv_heads, cache->head_dim, rows, announced, 1, longest_prefix));
+    if (s != SQAP_OK) return s;
+    const DeviceOfCall device;
+    return launch_cache8_shared(reinterpret_cast<const __half *>(Q), ldq, starts, past, rows, max_new, H, v, p, prefix_len, longest_prefix, cache->head_dim,
+                                reinterpret_cast<__half *>(O), ldo, workspace, as_stream(stream));
+}
+
+sqap_status sqap_cache8_shared_decode_attention(const sqap_f16 *QKV, int64_t ld, const int32_t *pos, const int32_t *past, int32_t H, double base,
+                                                const sqap_cache8 *cache, const sqap_cache8 *prefix, const int32_t *prefix_len, int32_t longest,
+                                                int32_t longest_prefix, sqap_f16 *O, int64_t ldo, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const char *who = "sqap_cache8_shared_decode_attention";
+    Cache8View v = {}, p = {};
+    if (!(base > 0.0)) return fail(SQAP_EINVAL, "%s: base must be positive", who);
+    sqap_status s = check_cache8(who, cache, H, &v);
+    if (s == SQAP_OK) s = check_prefix(who, cache, prefix, prefix_len, longest_prefix, H, &p);
+    if (s != SQAP_OK) return s;
+    if (longest <= 0) return fail(SQAP_EINVAL, "%s: longest = %d", who, longest);
+    if (cache->batch == 0) return SQAP_OK;
+    if (!pos || !past) return fail(SQAP_EINVAL, "%s: null pointer", who);
+    const int64_t width = (int64_t)H * cache->head_dim;
+    s = check_rows16(who, "QKV", QKV, ld, width + 2 * (int64_t)cache->kv_heads * cache->head_dim);
+    if (s == SQAP_OK) s = check_rows16(who, "O", O, ldo, width);
+    if (s == SQAP_OK)
+        s = check_workspace(who, workspace, workspace_bytes,
+                            cache8_shared_workspace_bytes(cache->batch, prefix->batch, H, cache->kv_heads, cache->head_dim, cache->batch, 1, longest, longest_prefix));
+    if (s != SQAP_OK) return s;
+    const DeviceOfCall device;
+    return launch_cache8_shared_decode(reinterpret_cast<const __half *>(QKV), ld, pos, past, H, base, v, p, prefix_len, cache->head_dim, longest, longest_prefix,
+                                       reinterpret_cast<__half *>(O), ldo, workspace, as_stream(stream));
+}
+
 // two ranges of 32-bit words that lie over each other
 static bool overlap(const void *x, int64_t n, const void *y, int64_t m)
 {

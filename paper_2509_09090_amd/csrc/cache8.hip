@@ -130,6 +130,45 @@ __device__ __forceinline__ Span span_of(const int32_t *starts, const int32_t *pa
     return s;
 }
 
+// ---------------------------------------------------------------- attention in parts
+
+// Attention behind a shared prefix is worked out in parts: of the rows of a whole group over shares of the prefix, and of each sequence's
+// rows over its own positions.  A part leaves, for each row and head, the sum of the values times p = 2^(s - m + kLift), the maximum m
+// (in units of ln 2) and the sum of the p; cache8_join_kernel puts them together.
+enum class Part { Whole, Own, Prefix };
+struct Parts {
+    float *o;                   // [part][row][head][D]
+    float2 *ml;                 // [part][row][head]
+    int64_t pairs;              // rows times heads
+    int prefix_shares;          // the parts in front; own ones behind them
+    int width;                  // sequences that share a prefix
+    const int32_t *length;      // of the prefixes, [groups]
+};
+
+// The rows of a group: [row, row + n), nothing where they are not within the fused rows or more than have been announced.
+struct GroupRows {
+    int row, n;
+};
+__device__ __forceinline__ GroupRows group_rows(const int32_t *starts, int group, int width, int rows, int max_new)
+{
+    if (!starts) return {group * width, width};
+    GroupRows r = {starts[group * width], 0};
+    const int end = starts[(group + 1) * width];
+    if (r.row >= 0 && end >= r.row && end <= rows && (int64_t)(end - r.row) <= (int64_t)width * max_new) r.n = end - r.row;
+    return r;
+}
+
+// The blocks of a prefix that a share has: [first, end); `active` shares have any.
+struct PrefixShare {
+    int first, end, active;
+};
+__device__ __forceinline__ PrefixShare prefix_share(int length, int capacity, int shares, int share)
+{
+    if (length <= 0 || length > capacity) return {0, 0, 0};
+    const int blocks = (length + kBlock - 1) / kBlock, each = (blocks + shares - 1) / shares;
+    return {min(share * each, blocks), min((share + 1) * each, blocks), (blocks + each - 1) / each};
+}
+
 // ---------------------------------------------------------------- append
 
 // Where the code of column x and place `at` (of 64) lies in the values' half of a block; in LDS the four 16-byte pieces of a column are moved
@@ -402,10 +441,13 @@ __device__ __forceinline__ void nan_rows(__half *O, int64_t ldo, int first, int6
 // A block's p = 2^(s - m) times its factor is one exponential, of s sk + (log2 factor - m); the sum of the probabilities is put right by the
 // factor once per block.  The hardware's exponential, logarithm and reciprocal are off by a unit of the last place of binary32 or so each, which is
 // less than the rounding of the scores and of the sums.
-template <int D, int WAVES>
+// As a part of the attention behind a shared prefix (Part::Prefix) the rows are a group's, all of them see the whole of `cache`, the prefixes,
+// and a workgroup has a share of its blocks.
+template <int D, int WAVES, Part PART>
 __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const __half *__restrict__ Q, int64_t ldq, const int32_t *__restrict__ starts,
                                                                          const int32_t *__restrict__ past, int rows, int max_new, int H,
-                                                                         const Cache8View cache, __half *__restrict__ O, int64_t ldo, int tiles)
+                                                                         const Cache8View cache, __half *__restrict__ O, int64_t ldo, int tiles,
+                                                                         const Parts parts)
 {
     constexpr int T = 64 * WAVES, TILE = 32 * WAVES, NP = D / 16, CT = D / 32, BUF = 2 * kBlock * D * 2, COUNT = kBlock * D / 16;
     constexpr int PIECES = (COUNT + T - 1) / T;
@@ -423,20 +465,35 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
     }
     const int b = pair / cache.kv_heads, kh = pair % cache.kv_heads;
     const int t = threadIdx.x, l = t & 63, wave = t >> 6, c = l & 31, h = l >> 5;
-    const Span sp = span_of(starts, past, b, rows, max_new, cache.blocks * kBlock);
     const int G = H / cache.kv_heads;
-    if (!sp.fits) {                                                   // (of more than max_new rows too: all of them)
-        nan_rows<D>(O, ldo, sp.row, (int64_t)sp.n * G, G, kh, number, tiles, TILE);
-        return;
+    Span sp;
+    int n_rows, tile, part = parts.prefix_shares;
+    PrefixShare share = {0, 0, 0};
+    if constexpr (PART == Part::Prefix) {
+        const GroupRows r = group_rows(starts, b, parts.width, rows, max_new);
+        part = number / tiles;
+        sp = {r.row, r.n, parts.length[b], true};
+        share = prefix_share(sp.past, cache.blocks * kBlock, parts.prefix_shares, part);
+        if (share.first >= share.end) return;
+        tile = number % tiles * TILE;
+    } else {
+        sp = span_of(starts, past, b, rows, max_new, cache.blocks * kBlock);
+        if (!sp.fits) {                                               // (of more than max_new rows too: all of them)
+            if constexpr (PART == Part::Whole) nan_rows<D>(O, ldo, sp.row, (int64_t)sp.n * G, G, kh, number, tiles, TILE);
+            return;
+        }
+        tile = (tiles - 1 - number) * TILE;
     }
-    const int n_rows = sp.n * G, tile = (tiles - 1 - number) * TILE;  // (the launch keeps max_new * G in 32 bits)
+    n_rows = sp.n * G;                                                // (the launch keeps max_new * G in 32 bits)
     if (tile >= n_rows) return;
     const int mine = tile + wave * 32 + c;
     const int mine_in = min(mine, n_rows - 1);
     const int query = mine_in / G, head = kh * G + mine_in % G;
     if (t == 0) not_finite = 0;
-    const int end = sp.past + sp.n, sees = sp.past + query;           // last position that this lane's row sees
-    const int tile_last = sp.past + (min(tile + TILE, n_rows) - 1) / G, n_blocks = tile_last / kBlock + 1;
+    // the positions that the cache holds, the last one that this lane's row sees, and that a row of the tile does
+    const int end = PART == Part::Prefix ? sp.past : sp.past + sp.n, sees = PART == Part::Prefix ? sp.past - 1 : sp.past + query;
+    const int tile_last = PART == Part::Prefix ? sp.past - 1 : sp.past + (min(tile + TILE, n_rows) - 1) / G;
+    const int j_first = PART == Part::Prefix ? share.first : 0, n_blocks = PART == Part::Prefix ? share.end : tile_last / kBlock + 1;
     const int64_t kv_head = (int64_t)b * cache.kv_heads + kh;
     const __half *tail_k = cache.tail + kv_head * 2 * kBlock * D, *tail_v = tail_k + kBlock * D;
     const float *scales = cache.scales + kv_head * cache.blocks * 2;
@@ -512,13 +569,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
     float mrun = -INFINITY, lrun = 0.f;
     Unit unit;
     const float per_d = kLog2e / sqrtf((float)D);
-    const int wave_last = sp.past + min(tile + wave * 32 + 31, n_rows - 1) / G, wave_first = sp.past + min(tile + wave * 32, n_rows - 1) / G;
+    const int wave_last = PART == Part::Prefix ? tile_last : sp.past + min(tile + wave * 32 + 31, n_rows - 1) / G;
+    const int wave_first = PART == Part::Prefix ? tile_last : sp.past + min(tile + wave * 32, n_rows - 1) / G;
     __syncthreads();
-    fetch(0);
-    keep(0);
+    fetch(j_first);
+    keep(j_first);
     float2 sc = {0.f, 0.f};
-    if (tail_block != 0) sc = *reinterpret_cast<const float2 *>(scales);
-    for (int j = 0; j < n_blocks; ++j) {
+    if (tail_block != j_first) sc = *reinterpret_cast<const float2 *>(scales + 2 * j_first);
+    for (int j = j_first; j < n_blocks; ++j) {
         fetch(j + 1);
         // (keys that are all zeros: the scores are, times anything but zero, which would make NaN of a masked one)
         const float sk = j == tail_block || sc.x == 0.f ? per_d : sc.x * per_d, sv = j == tail_block ? 1.f : sc.y;
@@ -566,6 +624,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
 #pragma unroll
                     for (int i = 0; i < 16; ++i) ot[ct][i] *= change;
             }
+            // (a part without a score above minus infinity so far adds nothing; another may have some)
+            const float taken = PART != Part::Whole && mrun == -INFINITY ? 0.f : mrun;
             float by = sk, from = __log2f(factor) + kLift;
             const bool bad = !(sk >= 0.f && sv >= 0.f);               // keys or values that are NaN as a whole: for the rows that see any of them
             if (bad || __any(fabsf(top) > kLargeScore && top > -INFINITY)) {        // (a masked score times NaN would be NaN, too)
@@ -575,11 +635,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
                     for (int i = 0; i < 16; ++i) {
                         float w = bad ? NAN : s[tt][i] * sk;
                         asm volatile("" : "+v"(w));                   // (rounded)
-                        s[tt][i] = s[tt][i] == -INFINITY ? -INFINITY : w - mrun;
+                        s[tt][i] = s[tt][i] == -INFINITY ? -INFINITY : w - taken;
                     }
                 by = 1.f;
             } else {
-                from -= mrun;
+                from -= taken;
             }
             float sum = 0.f;
 #pragma unroll
@@ -610,9 +670,37 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
         keep(j + 1);
     }
     lrun += __shfl_xor(lrun, 32);
-    const float norm = unit.unit / lrun;
-    const bool odd = tile_last / kBlock == tail_block && not_finite;
+    const bool odd = n_blocks - 1 == tail_block && not_finite;
     if (mine >= n_rows) return;
+    if constexpr (PART != Part::Whole) {
+        const int64_t pair = part * parts.pairs + (int64_t)(sp.row + query) * H + head;
+        if (h == 0) parts.ml[pair] = {mrun, lrun};
+        float *sums = parts.o + pair * D;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                v4f x;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = ot[ct][4 * a + i] * unit.unit;
+                *reinterpret_cast<v4f *>(sums + 32 * ct + 8 * a + 4 * h) = x;
+            }
+        if (odd) {                                                    // (as below)
+#pragma unroll 1
+            for (int x = 0; x < D / 2; ++x) {
+                const int col = (x >> 2) * 8 + 4 * h + (x & 3);
+                float o = sums[col];
+#pragma unroll 1
+                for (int s = 0; s <= sees - tail_block * kBlock; ++s) {
+                    const float v = __half2float(tail_v[s * D + col]);
+                    if (!(fabsf(v) <= 65504.f)) o += v;
+                }
+                sums[col] = o;
+            }
+        }
+        return;
+    }
+    const float norm = unit.unit / lrun;
     __half *to = O + (int64_t)(sp.row + query) * ldo + (int64_t)head * D;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
@@ -760,10 +848,11 @@ struct FewRowsLds {
     float m[kFewRowsWaves][16], l[kFewRowsWaves][16];
     int not_finite;
 };
-template <int D>
+template <int D, Part PART>
 __global__ __launch_bounds__(64 * kFewRowsWaves, 2) void cache8_few_rows_kernel(const __half *__restrict__ Q, int64_t ldq, const int32_t *__restrict__ starts,
                                                                                 const int32_t *__restrict__ past, int rows, int max_new, int H,
-                                                                                const Cache8View cache, __half *__restrict__ O, int64_t ldo, int tiles)
+                                                                                const Cache8View cache, __half *__restrict__ O, int64_t ldo, int tiles,
+                                                                                const Parts parts)
 {
     constexpr int C = D / 64, DT = D / 16, T = 64 * kFewRowsWaves;
     extern __shared__ __attribute__((aligned(16))) uint8_t raw_lds[];
@@ -782,7 +871,7 @@ __global__ __launch_bounds__(64 * kFewRowsWaves, 2) void cache8_few_rows_kernel(
     const Span sp = span_of(starts, past, b, rows, max_new, cache.blocks * kBlock);
     const int G = H / cache.kv_heads;
     if (!sp.fits) {
-        nan_rows<D>(O, ldo, sp.row, (int64_t)sp.n * G, G, kh, number, tiles, 16);
+        if constexpr (PART == Part::Whole) nan_rows<D>(O, ldo, sp.row, (int64_t)sp.n * G, G, kh, number, tiles, 16);
         return;
     }
     const int n_rows = sp.n * G, tile = (tiles - 1 - number) * 16;
@@ -876,11 +965,27 @@ __global__ __launch_bounds__(64 * kFewRowsWaves, 2) void cache8_few_rows_kernel(
     const int of = (tile + row) / G;
     float top = -INFINITY, sum = 0.f;
     for (int w = 0; w < waves; ++w) top = fmaxf(top, lds.m[w][row]);
+    const float taken = PART != Part::Whole && top == -INFINITY ? 0.f : top;
     v4f o = {0.f, 0.f, 0.f, 0.f};
     for (int w = 0; w < waves; ++w) {
-        const float f = exp2f(lds.m[w][row] - top);
+        const float f = exp2f(lds.m[w][row] - taken);
         sum += f * lds.l[w][row];
         o += f * *reinterpret_cast<const v4f *>(&lds.u.o[w][row][col]);
+    }
+    if constexpr (PART != Part::Whole) {
+        const int64_t pair = parts.prefix_shares * parts.pairs + (int64_t)(sp.row + of) * H + kh * G + tile + row - of * G;
+        if (odd) {                                                    // (as below)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll 1
+                for (int s = 0; s <= sp.past + of - tail_block * kBlock; ++s) {
+                    const float v = __half2float(tail_v[s * D + col + i]);
+                    if (!(fabsf(v) <= 65504.f)) o[i] += v;
+                }
+        }
+        if (col == 0) parts.ml[pair] = {top, sum};
+        *reinterpret_cast<v4f *>(parts.o + pair * D + col) = o;
+        return;
     }
     const float norm = 1.f / sum;
     union { __half h[4]; v2u v; } out;
@@ -919,6 +1024,11 @@ struct DecodeArgs {
     unsigned *counters;
     float *partials;
     RopeFreq freq;
+    // behind a shared prefix
+    Cache8View prefix;
+    int prefix_tiles;                                         // of a group and key head, 16 rows each
+    Parts parts;
+    __half *q_out;                                            // receives the rotated queries, [batch][H D], where not null
 };
 
 template <int D>
@@ -939,13 +1049,187 @@ struct DecodeLds {
     int arrived;
 };
 
+// 16 (row, head) pairs of a group and key head over a share of the group's prefix, whose blocks are dealt to the wavefronts as in the decode
+// kernel.  ROTATE: Q are the fused rows of the decode call, rotated here.
+struct PrefixTile {
+    const __half *Q;
+    int64_t ld;
+    const int32_t *starts, *pos;
+    int rows, max_new, H;
+};
+template <int D, bool ROTATE>
+__device__ __forceinline__ void prefix_tile(DecodeLds<D> &lds, const PrefixTile &a, const Cache8View &prefix, const Parts &parts, const RopeFreq &freq,
+                                            int group, int kh, int tile, int share)
+{
+    constexpr int HALF = D / 2, C = D / 64, T = 64 * kDecodeWaves, DT = D / 16;
+    const int t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), r = l & 15, g = l >> 4, G = a.H / prefix.kv_heads;
+    const GroupRows rows = group_rows(a.starts, group, parts.width, a.rows, a.max_new);
+    const int length = parts.length[group], pair0 = tile * 16, pairs = min(16, rows.n * G - pair0);
+    const PrefixShare own = prefix_share(length, prefix.blocks * kBlock, parts.prefix_shares, share);
+    if (pairs <= 0 || own.first >= own.end) return;
+    const int64_t head = (int64_t)group * prefix.kv_heads + kh;
+    const int tail_block = length / kBlock, tail_rows = length % kBlock;
+    const bool has_tail = own.end - 1 == tail_block;
+    const __half *tail_k = prefix.tail + head * 2 * kBlock * D, *tail_v = tail_k + kBlock * D;
+    v4i kraw[4 * C], vraw[DT];
+    float2 sc = {0.f, 0.f};
+    auto fetch_keys = [&](int j) {
+        if (j >= own.end || j == tail_block) return;
+        sc = reinterpret_cast<const float2 *>(prefix.scales)[head * prefix.blocks + j];
+        const v4i *k = reinterpret_cast<const v4i *>(block_codes<D>(prefix, head, j, 0)) + l;
+#pragma unroll
+        for (int i = 0; i < 4 * C; ++i) kraw[i] = k[i * 64];
+    };
+    auto fetch_values = [&](int j) {
+        if (j >= own.end || j == tail_block) return;
+        const v4i *v = reinterpret_cast<const v4i *>(block_codes<D>(prefix, head, j, 1)) + l;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) vraw[i] = v[i * 64];
+    };
+    fetch_keys(own.first + wave);
+    fetch_values(own.first + wave);
+    v8h qf[2 * C];
+    auto query = [&](int pair) { return a.Q + (int64_t)(rows.row + (pair0 + pair) / G) * a.ld + (int64_t)(kh * G + (pair0 + pair) % G) * D; };
+    if constexpr (ROTATE) {
+        __half q[16 * HALF / T][2];
+#pragma unroll
+        for (int i = 0; i < 16 * HALF / T; ++i) {
+            const int u = t + i * T;
+            const __half *from = query(min(u / HALF, pairs - 1)) + u % HALF;
+            q[i][0] = from[0];
+            q[i][1] = from[HALF];
+        }
+        // angles of the tile's rows, once for the heads of each
+        double2 *angles = reinterpret_cast<double2 *>(&lds.u);        // [row][HALF]
+        static_assert(sizeof(lds.u) >= 16 * HALF * sizeof(double2), "angles of sixteen rows");
+        const int first = pair0 / G, count = (pair0 + pairs - 1) / G - first + 1;
+        for (int u = t; u < count * HALF; u += T) {
+            double2 x;
+            sincos_of((double)a.pos[rows.row + first + u / HALF] * freq.f[u % HALF], x.y, x.x);
+            angles[u] = x;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 16 * HALF / T; ++i) {
+            const int u = t + i * T, pair = u / HALF, x = u % HALF;
+            const double2 w = angles[((pair0 + min(pair, pairs - 1)) / G - first) * HALF + x];
+            __half lo, hi;
+            rotate_pair(q[i][0], q[i][1], w.x, w.y, lo, hi);
+            lds.q[pair][x] = (_Float16)__half2float(lo);
+            lds.q[pair][x + HALF] = (_Float16)__half2float(hi);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int m = 0; m < 2 * C; ++m) qf[m] = *reinterpret_cast<const v8h *>(&lds.q[r][64 * (m >> 1) + 16 * g + 8 * (m & 1)]);
+    } else {
+        const __half *from = query(min(r, pairs - 1));
+#pragma unroll
+        for (int m = 0; m < 2 * C; ++m) qf[m] = *reinterpret_cast<const v8h *>(from + 64 * (m >> 1) + 16 * g + 8 * (m & 1));
+    }
+    if (has_tail) {
+        if (t == 0) lds.arrived = 0;                                  // values that are not finite: come back at the end
+        __syncthreads();
+        bool odd = false;
+        for (int u = t; u < kBlock * D / 8; u += T) {
+            const int s = u / (D / 8), x = (u % (D / 8)) * 8, at = value_slot(s);
+            v4i k = {0, 0, 0, 0}, v = k;
+            if (s < tail_rows) {
+                k = *reinterpret_cast<const v4i *>(tail_k + s * D + x);
+                v = *reinterpret_cast<const v4i *>(tail_v + s * D + x);
+            }
+            *reinterpret_cast<v4i *>(&lds.u.tail.k[s][x]) = k;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                unsigned short w = (unsigned short)((unsigned)v[e >> 1] >> (16 * (e & 1)));
+                if ((w & 0x7fffu) >= 0x7c00u) w = 0, odd = true;
+                lds.u.tail.v[x + e][value_place(x, at)] = w;
+            }
+        }
+        if (odd) lds.arrived = 1;
+        __syncthreads();
+    }
+    WaveSums<D> sums;
+    for (int j = own.first + wave; j < own.end; j += kDecodeWaves) {
+        if (j != tail_block) {
+            const float2 scale = sc;
+            sums.add(
+                qf, scale.x, scale.y, false, 0,
+                [&](int T4, int m) {
+                    const v4i w = kraw[T4 * C + (m >> 1)];
+                    return (m & 1) ? halves_of(w[2], w[3]) : halves_of(w[0], w[1]);
+                },
+                [&](int i, int n) { return halves_of(vraw[i][2 * n], vraw[i][2 * n + 1]); }, [&] { fetch_keys(j + kDecodeWaves); });
+            fetch_values(j + kDecodeWaves);
+        } else {
+            sums.add(
+                qf, 1.f, 1.f, true, tail_rows - 1,
+                [&](int T4, int m) { return *reinterpret_cast<const v8h *>(&lds.u.tail.k[16 * T4 + r][64 * (m >> 1) + 16 * g + 8 * (m & 1)]); },
+                [&](int i, int n) { return *reinterpret_cast<const v8h *>(&lds.u.tail.v[16 * i + r][value_place(16 * i + r, 32 * n + 8 * g)]); }, [] {});
+        }
+    }
+    sums.l += __shfl_xor(sums.l, 16);
+    sums.l += __shfl_xor(sums.l, 32);
+    const bool odd = has_tail && lds.arrived;
+    __syncthreads();                                                  // the tail's rows have been read
+    const int waves = min(own.end - own.first, kDecodeWaves);
+    if (wave < waves) {
+#pragma unroll
+        for (int i = 0; i < DT; ++i) *reinterpret_cast<v4f *>(&lds.u.o[wave][r][16 * i + 4 * g]) = sums.o[i] * sums.unit.unit;
+        if (g == 0) {
+            lds.m[wave][r] = sums.m;
+            lds.l[wave][r] = sums.l;
+        }
+    }
+    __syncthreads();
+    for (int u = t; u < pairs * (D / 4); u += T) {
+        const int pair = u / (D / 4), col = u % (D / 4) * 4;
+        float top = -INFINITY, sum = 0.f;
+        for (int w = 0; w < waves; ++w) top = fmaxf(top, lds.m[w][pair]);
+        const float taken = top == -INFINITY ? 0.f : top;             // (no score above it: nothing is added to the other parts)
+        v4f o = {0.f, 0.f, 0.f, 0.f};
+        for (int w = 0; w < waves; ++w) {
+            const float f = exp2f(lds.m[w][pair] - taken);
+            sum += f * lds.l[w][pair];
+            o += f * *reinterpret_cast<const v4f *>(&lds.u.o[w][pair][col]);
+        }
+        if (odd) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll 1
+                for (int s = 0; s < tail_rows; ++s) {
+                    const float v = __half2float(tail_v[s * D + col + i]);
+                    if (!(fabsf(v) <= 65504.f)) o[i] += v;
+                }
+        }
+        const int64_t at = share * parts.pairs + (int64_t)(rows.row + (pair0 + pair) / G) * a.H + kh * G + (pair0 + pair) % G;
+        if (col == 0) parts.ml[at] = {top, sum};
+        *reinterpret_cast<v4f *>(parts.o + at * D + col) = o;
+    }
+}
 template <int D>
+__global__ __launch_bounds__(64 * kDecodeWaves, 2) void cache8_prefix_kernel(const PrefixTile a, const Cache8View prefix, const Parts parts, int tiles)
+{
+    __shared__ DecodeLds<D> lds;
+    prefix_tile<D, false>(lds, a, prefix, parts, RopeFreq{}, blockIdx.z / tiles, blockIdx.y, blockIdx.z % tiles, blockIdx.x);
+}
+
+// SHARED: the own positions of sequences that share a prefix, and in the workgroups behind them (where there are any) the prefix; all of them leave parts.
+template <int D, bool SHARED>
 __global__ __launch_bounds__(64 * kDecodeWaves, 2) void cache8_decode_kernel(const DecodeArgs a)
 {
     constexpr int HALF = D / 2, C = D / 64, T = 64 * kDecodeWaves, DT = D / 16;
     __shared__ DecodeLds<D> lds;
     const Cache8View &cache = a.cache;
     const int share = blockIdx.x, kh = blockIdx.y / a.chunks, chunk = blockIdx.y % a.chunks, b = blockIdx.z;
+    if constexpr (SHARED) {
+        if (b >= cache.batch) {
+            if (chunk == 0 && share < a.parts.prefix_shares)
+                prefix_tile<D, true>(lds, PrefixTile{a.QKV, a.ld, nullptr, a.pos, cache.batch, 1, a.H}, a.prefix, a.parts, a.freq,
+                                     (b - cache.batch) / a.prefix_tiles, kh, (b - cache.batch) % a.prefix_tiles, share);
+            return;
+        }
+        if (share >= a.shares) return;
+    }
     const int t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), r = l & 15, g = l >> 4;
     const int first_head = kh * a.G + chunk * 16, heads = min(16, a.G - chunk * 16);
     const int past = a.past[b];
@@ -953,6 +1237,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void cache8_decode_kernel(con
     const __half *row = a.QKV + (int64_t)b * a.ld;
     __half *out = a.O + (int64_t)b * a.ldo + (int64_t)first_head * D;
     if (past >= cache.blocks * kBlock) {                              // no room: nothing is appended, and the outputs say so
+        if (SHARED) return;                                           // (cache8_join_kernel sees to that)
         if (share == 0)
             for (int i = t; i < heads * D; i += T) out[i] = __ushort_as_half(0x7e00);
         return;
@@ -1035,6 +1320,9 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void cache8_decode_kernel(con
         lds.vnew[t + HALF] = vnew[1];
     }
     __syncthreads();
+    if (SHARED && a.q_out && begin == 0)
+        for (int u = t; u < heads * (D / 8); u += T)
+            *reinterpret_cast<v8h *>(a.q_out + ((int64_t)b * a.H + first_head) * D + u * 8) = *reinterpret_cast<const v8h *>(&lds.q[0][0] + u * 8);
     float tail_sk = 1.f, tail_sv = 1.f;
     if (has_last) {
         const bool full = slot == kBlock - 1;
@@ -1164,7 +1452,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void cache8_decode_kernel(con
 #pragma unroll
         for (int w = 0; w < kDecodeWaves; ++w) top = fmaxf(top, lds.m[w][j]);
         // (no score above minus infinity: the share has nothing to add to the others; where there are none the softmax is 0 / 0)
-        const float from = top == -INFINITY && active > 1 ? 0.f : top;
+        const float from = top == -INFINITY && (SHARED || active > 1) ? 0.f : top;
         sum = 0.f;
         float o = 0.f;
 #pragma unroll
@@ -1178,6 +1466,15 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void cache8_decode_kernel(con
         if (odd) o = odd == 1 ? o + INFINITY : odd == 2 ? o - INFINITY : NAN;
         return o;
     };
+    if constexpr (SHARED) {
+        const int64_t pair = (a.parts.prefix_shares + share) * a.parts.pairs + (int64_t)b * a.H + first_head;
+        for (int u = t; u < heads * D; u += T) {
+            float top, sum;
+            a.parts.o[pair * D + u] = merged(u / D, u % D, top, sum);
+            if (u % D == 0) a.parts.ml[pair + u / D] = {top, sum};
+        }
+        return;
+    }
     if (active == 1) {
         for (int u = t; u < heads * D; u += T) {
             float top, sum;
@@ -1256,6 +1553,96 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void cache8_decode_kernel(con
     }
 }
 
+// ---------------------------------------------------------------- the parts in one
+
+// The parts of a (row, head) pair: D / 4 lanes with four columns each; the lanes share out the parts' maxima and sums first.  One workgroup per
+// sequence and 1024 / D of its pairs.
+constexpr int kMostParts = 128;                                       // of a pair
+struct JoinArgs {
+    const int32_t *starts, *past;                             // starts null: one row per sequence
+    int rows, max_new, H, capacity, prefix_capacity;
+    int own_shares, own_each;                                 // as in DecodeArgs; one share where there are prompts
+    Parts parts;
+    __half *O;
+    int64_t ldo;
+};
+template <int D>
+__global__ __launch_bounds__(256) void cache8_join_kernel(const JoinArgs a)
+{
+    constexpr int LANES = D / 4, EACH = 256 / LANES, KEPT = kMostParts / LANES;
+    const int b = blockIdx.y, t = threadIdx.x, lane = t % LANES, group = b / a.parts.width;
+    Span sp;
+    bool fits;
+    if (a.starts) {
+        sp = span_of(a.starts, a.past, b, a.rows, a.max_new, a.capacity);
+        const int first = a.starts[group * a.parts.width], end = a.starts[(group + 1) * a.parts.width];
+        if (sp.row < first || sp.row + sp.n > end) return;            // (starts that are not in order)
+        fits = sp.fits && group_rows(a.starts, group, a.parts.width, a.rows, a.max_new).n > 0;
+    } else {
+        sp = Span{b, 1, a.past[b], true};
+        if (sp.past < 0) return;
+        fits = sp.past < a.capacity;
+    }
+    const int length = a.parts.length[group];
+    const PrefixShare prefix = prefix_share(length, a.prefix_capacity, a.parts.prefix_shares, 0);
+    fits = fits && length >= 0 && length <= a.prefix_capacity;
+    const int last = sp.past / kBlock, own_each = max(a.own_each, (last + a.own_shares) / a.own_shares);
+    const int own = a.starts ? 1 : (last + own_each) / own_each, all = prefix.active + own;
+    auto part_of = [&](int i) { return i < prefix.active ? i : a.parts.prefix_shares + i - prefix.active; };
+    const int64_t pairs = (int64_t)sp.n * a.H;
+    for (int64_t p = (int64_t)blockIdx.x * EACH + t / LANES; p < pairs; p += (int64_t)gridDim.x * EACH) {
+        const int64_t row = sp.row + p / a.H, head = p % a.H, at = row * a.H + head;
+        __half *to = a.O + row * a.ldo + head * D + lane * 4;
+        union { __half h[4]; v2u v; } out;
+        if (!fits) {
+            out.v = v2u{0x7e007e00u, 0x7e007e00u};
+            *reinterpret_cast<v2u *>(to) = out.v;
+            continue;
+        }
+        float2 ml[KEPT];
+        float top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < KEPT; ++k) {
+            const int i = k * LANES + lane;
+            ml[k] = float2{-INFINITY, 0.f};
+            if (i < all) ml[k] = a.parts.ml[part_of(i) * a.parts.pairs + at];
+            top = fmaxf(top, ml[k].x);
+        }
+#pragma unroll
+        for (int i = LANES / 2; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
+#pragma unroll
+        for (int k = 0; k < KEPT; ++k) {
+            ml[k].x = k * LANES + lane < all ? exp2f(ml[k].x - top) : 0.f;             // (no score above minus infinity anywhere: 0 / 0)
+            sum += k * LANES + lane < all ? ml[k].x * ml[k].y : 0.f;
+        }
+#pragma unroll
+        for (int i = LANES / 2; i > 0; i >>= 1) sum += __shfl_xor(sum, i);
+        v4f o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < KEPT; ++k) {
+            const int n = min(all - k * LANES, LANES);
+            for (int i0 = 0; i0 < n; i0 += 4) {                       // four of them asked for at a time (the last one again where there are fewer, for nothing)
+                v4f x[4];
+                float f[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int of = min(i0 + i, n - 1);
+                    f[i] = i0 + i < n ? __shfl(ml[k].x, of, LANES) : 0.f;
+                    x[i] = *reinterpret_cast<const v4f *>(a.parts.o + (part_of(k * LANES + of) * a.parts.pairs + at) * D + lane * 4);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[e] += fabsf(x[i][e]) < INFINITY ? f[i] * x[i][e] : x[i][e];      // (an infinite value stays one however small its weight)
+            }
+        }
+        const float norm = 1.f / sum;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out.h[e] = __float2half_rn(o[e] * norm);
+        *reinterpret_cast<v2u *>(to) = out.v;
+    }
+}
+
 // ---------------------------------------------------------------- launches
 
 template <int D>
@@ -1306,15 +1693,15 @@ sqap_status launch_cache8_read(const Cache8View &cache, int d, const int32_t *le
 // (96) 67 and 103, 300 of 32 heads (96) 13.9 and 15.1; but 500 of 32 (128) 23.7 and 21.3, 1000 of 32 over 8 (256) 56 and 37.
 constexpr int kFewTiles = 96;
 
-template <int D>
+template <int D, Part PART>
 static sqap_status launch_attention_d(const __half *Q, int64_t ldq, const int32_t *starts, const int32_t *past, int rows, int max_new, int H,
-                                      const Cache8View &cache, __half *O, int64_t ldo, hipStream_t st)
+                                      const Cache8View &cache, __half *O, int64_t ldo, const Parts &parts, hipStream_t st)
 {
     constexpr int WAVES = 4, LDS = 2 * 2 * kBlock * D * 2;
     static std::atomic<bool> ready[kMaxDeviceSlots];
     if (!ready[device_slot()].load(std::memory_order_relaxed)) {
-        SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(cache8_attention_kernel<D, WAVES>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
-        SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(cache8_few_rows_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize,
+        SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(cache8_attention_kernel<D, WAVES, PART>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+        SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(cache8_few_rows_kernel<D, PART>), hipFuncAttributeMaxDynamicSharedMemorySize,
                                            (int)sizeof(FewRowsLds<D>)));
         ready[device_slot()].store(true, std::memory_order_relaxed);
     }
@@ -1323,11 +1710,11 @@ static sqap_status launch_attention_d(const __half *Q, int64_t ldq, const int32_
     const bool few = tiles_of(32 * WAVES) * pairs <= kFewTiles;
     const int64_t tiles = tiles_of(few ? 16 : 32 * WAVES), items = tiles * pairs;
     if (few)
-        hipLaunchKernelGGL(cache8_few_rows_kernel<D>, dim3((unsigned)items), dim3(64 * kFewRowsWaves), sizeof(FewRowsLds<D>), st, Q, ldq, starts, past, rows,
-                           max_new, H, cache, O, ldo, (int)tiles);
+        hipLaunchKernelGGL((cache8_few_rows_kernel<D, PART>), dim3((unsigned)items), dim3(64 * kFewRowsWaves), sizeof(FewRowsLds<D>), st, Q, ldq, starts, past, rows,
+                           max_new, H, cache, O, ldo, (int)tiles, parts);
     else
-        hipLaunchKernelGGL((cache8_attention_kernel<D, WAVES>), dim3((unsigned)items), dim3(64 * WAVES), LDS, st, Q, ldq, starts, past, rows, max_new, H,
-                           cache, O, ldo, (int)tiles);
+        hipLaunchKernelGGL((cache8_attention_kernel<D, WAVES, PART>), dim3((unsigned)items), dim3(64 * WAVES), LDS, st, Q, ldq, starts, past, rows, max_new, H,
+                           cache, O, ldo, (int)tiles, parts);
     SQAP_HIP_CHECK(hipGetLastError());
     return SQAP_OK;
 }
@@ -1335,8 +1722,8 @@ static sqap_status launch_attention_d(const __half *Q, int64_t ldq, const int32_
 sqap_status launch_cache8_attention(const __half *Q, int64_t ldq, const int32_t *starts, const int32_t *past, int rows, int max_new, int H,
                                     const Cache8View &cache, int d, __half *O, int64_t ldo, hipStream_t st)
 {
-    return d == 64 ? launch_attention_d<64>(Q, ldq, starts, past, rows, max_new, H, cache, O, ldo, st)
-                   : launch_attention_d<128>(Q, ldq, starts, past, rows, max_new, H, cache, O, ldo, st);
+    return d == 64 ? launch_attention_d<64, Part::Whole>(Q, ldq, starts, past, rows, max_new, H, cache, O, ldo, Parts{}, st)
+                   : launch_attention_d<128, Part::Whole>(Q, ldq, starts, past, rows, max_new, H, cache, O, ldo, Parts{}, st);
 }
 
 // Shares of a sequence.  One up to eight blocks: a wavefront's second block costs 1.5 us, joining 2.5.  Beyond, shares of four blocks while
@@ -1386,10 +1773,145 @@ sqap_status launch_cache8_decode(const __half *QKV, int64_t ld, const int32_t *p
     a.partials = reinterpret_cast<float *>(static_cast<char *>(workspace) + kCounterBytes);
     a.freq = rope_frequencies(d, base);
     const dim3 grid(a.shares, cache.kv_heads * a.chunks, cache.batch);
-    if (d == 64) hipLaunchKernelGGL(cache8_decode_kernel<64>, grid, dim3(64 * kDecodeWaves), 0, st, a);
-    else hipLaunchKernelGGL(cache8_decode_kernel<128>, grid, dim3(64 * kDecodeWaves), 0, st, a);
+    if (d == 64) hipLaunchKernelGGL((cache8_decode_kernel<64, false>), grid, dim3(64 * kDecodeWaves), 0, st, a);
+    else hipLaunchKernelGGL((cache8_decode_kernel<128, false>), grid, dim3(64 * kDecodeWaves), 0, st, a);
     SQAP_HIP_CHECK(hipGetLastError());
     return SQAP_OK;
+}
+
+// ---- behind a shared prefix
+
+// How the prefixes are dealt out.  Few pairs to a group and key head: tiles of 16, blocks dealt to the wavefronts; more: tiles of 128.
+constexpr int kFewPairs = 64, kPrefixGroups = 512, kMostPrefixShares = 64;
+struct SharedPlan {
+    bool few;
+    int64_t tiles;               // of a group and key head
+    int shares, own_shares;
+    int64_t pairs;               // rows times heads
+    size_t q, ml, o, bytes;      // where they are in the workspace
+};
+static SharedPlan shared_plan(int batch, int groups, int H, int kv_heads, int d, int rows, int max_new, int own_shares, int longest_prefix)
+{
+    SharedPlan p = {};
+    const int64_t of_group = std::min<int64_t>((int64_t)(batch / groups) * max_new, rows) * (H / kv_heads);
+    p.few = of_group <= kFewPairs;
+    p.tiles = std::max<int64_t>(1, (of_group + (p.few ? 15 : 127)) / (p.few ? 16 : 128));
+    const int blocks = std::max(1, blocks_of(longest_prefix));
+    const int64_t items = p.tiles * groups * kv_heads;
+    p.shares = (int)std::max<int64_t>(1, std::min<int64_t>({(blocks + 3) / 4, kPrefixGroups / items, kMostPrefixShares}));
+    p.own_shares = own_shares;
+    p.pairs = (int64_t)rows * H;
+    const auto up = [](size_t n) { return (n + 15) / 16 * 16; };
+    p.q = kCounterBytes;                                              // (left alone, for calls that want it zero)
+    p.ml = p.q + (max_new == 1 ? up((size_t)p.pairs * d * 2) : 0);
+    p.o = p.ml + up((size_t)(p.shares + own_shares) * p.pairs * sizeof(float2));
+    p.bytes = p.o + (size_t)(p.shares + own_shares) * p.pairs * d * sizeof(float);
+    return p;
+}
+static int own_shares_of(int batch, int H, int kv_heads, int longest)
+{
+    return std::min(decode_shares(batch, H, kv_heads, longest), kMostParts - kMostPrefixShares);
+}
+
+size_t cache8_shared_workspace_bytes(int batch, int groups, int H, int kv_heads, int d, int rows, int max_new, int longest, int longest_prefix)
+{
+    return shared_plan(batch, groups, H, kv_heads, d, rows, max_new, max_new == 1 ? own_shares_of(batch, H, kv_heads, longest) : 1, longest_prefix).bytes;
+}
+
+template <int D>
+static sqap_status launch_prefix(const SharedPlan &plan, const PrefixTile &a, const Cache8View &prefix, const Parts &parts, hipStream_t st)
+{
+    if (plan.few) {
+        hipLaunchKernelGGL(cache8_prefix_kernel<D>, dim3(plan.shares, prefix.kv_heads, (unsigned)(prefix.batch * plan.tiles)), dim3(64 * kDecodeWaves), 0, st, a, prefix,
+                           parts, (int)plan.tiles);
+    } else {
+        constexpr int WAVES = 4, LDS = 2 * 2 * kBlock * D * 2;
+        static std::atomic<bool> ready[kMaxDeviceSlots];
+        if (!ready[device_slot()].load(std::memory_order_relaxed)) {
+            SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(cache8_attention_kernel<D, WAVES, Part::Prefix>),
+                                               hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+            ready[device_slot()].store(true, std::memory_order_relaxed);
+        }
+        const int64_t items = plan.tiles * plan.shares * prefix.kv_heads * prefix.batch;
+        hipLaunchKernelGGL((cache8_attention_kernel<D, WAVES, Part::Prefix>), dim3((unsigned)items), dim3(64 * WAVES), LDS, st, a.Q, a.ld, a.starts, nullptr, a.rows,
+                           a.max_new, a.H, prefix, nullptr, 0, (int)plan.tiles, parts);
+    }
+    SQAP_HIP_CHECK(hipGetLastError());
+    return SQAP_OK;
+}
+
+template <int D>
+static sqap_status launch_join(const JoinArgs &a, int batch, hipStream_t st)
+{
+    constexpr int EACH = 1024 / D;
+    const int64_t groups = std::max<int64_t>(1, std::min<int64_t>(((int64_t)a.max_new * a.H + EACH - 1) / EACH, 1 << 16));
+    hipLaunchKernelGGL(cache8_join_kernel<D>, dim3((unsigned)groups, batch), dim3(256), 0, st, a);
+    SQAP_HIP_CHECK(hipGetLastError());
+    return SQAP_OK;
+}
+
+template <int D>
+static sqap_status launch_shared_d(const __half *Q, int64_t ldq, const int32_t *starts, const int32_t *past, int rows, int max_new, int H, const Cache8View &cache,
+                                   const Cache8View &prefix, const int32_t *length, int longest_prefix, __half *O, int64_t ldo, char *workspace, hipStream_t st)
+{
+    const SharedPlan plan = shared_plan(cache.batch, prefix.batch, H, cache.kv_heads, D, rows, max_new, 1, longest_prefix);
+    const Parts parts = {reinterpret_cast<float *>(workspace + plan.o), reinterpret_cast<float2 *>(workspace + plan.ml), plan.pairs, plan.shares,
+                         cache.batch / prefix.batch, length};
+    sqap_status s = launch_prefix<D>(plan, PrefixTile{Q, ldq, starts, nullptr, rows, max_new, H}, prefix, parts, st);
+    if (s == SQAP_OK) s = launch_attention_d<D, Part::Own>(Q, ldq, starts, past, rows, max_new, H, cache, nullptr, 0, parts, st);
+    if (s != SQAP_OK) return s;
+    return launch_join<D>(JoinArgs{starts, past, rows, max_new, H, cache.blocks * kBlock, prefix.blocks * kBlock, 1, 1, parts, O, ldo}, cache.batch, st);
+}
+
+sqap_status launch_cache8_shared(const __half *Q, int64_t ldq, const int32_t *starts, const int32_t *past, int rows, int max_new, int H, const Cache8View &cache,
+                                 const Cache8View &prefix, const int32_t *length, int longest_prefix, int d, __half *O, int64_t ldo, void *workspace, hipStream_t st)
+{
+    char *const ws = static_cast<char *>(workspace);
+    return d == 64 ? launch_shared_d<64>(Q, ldq, starts, past, rows, max_new, H, cache, prefix, length, longest_prefix, O, ldo, ws, st)
+                   : launch_shared_d<128>(Q, ldq, starts, past, rows, max_new, H, cache, prefix, length, longest_prefix, O, ldo, ws, st);
+}
+
+template <int D>
+static sqap_status launch_shared_decode_d(DecodeArgs a, const int32_t *length, int longest_prefix, char *workspace, hipStream_t st)
+{
+    const Cache8View &cache = a.cache, &prefix = a.prefix;
+    const SharedPlan plan = shared_plan(cache.batch, prefix.batch, a.H, cache.kv_heads, D, cache.batch, 1, a.shares, longest_prefix);
+    a.parts = {reinterpret_cast<float *>(workspace + plan.o), reinterpret_cast<float2 *>(workspace + plan.ml), plan.pairs, plan.shares, cache.batch / prefix.batch, length};
+    a.prefix_tiles = (int)plan.tiles;
+    a.q_out = plan.few ? nullptr : reinterpret_cast<__half *>(workspace + plan.q);
+    const int behind = plan.few ? (int)(prefix.batch * plan.tiles) : 0;
+    hipLaunchKernelGGL((cache8_decode_kernel<D, true>), dim3(plan.few ? std::max(plan.shares, a.shares) : a.shares, cache.kv_heads * a.chunks, cache.batch + behind),
+                       dim3(64 * kDecodeWaves), 0, st, a);
+    SQAP_HIP_CHECK(hipGetLastError());
+    if (!plan.few) {
+        const sqap_status s = launch_prefix<D>(plan, PrefixTile{a.q_out, (int64_t)a.H * D, nullptr, nullptr, cache.batch, 1, a.H}, prefix, a.parts, st);
+        if (s != SQAP_OK) return s;
+    }
+    return launch_join<D>(JoinArgs{nullptr, a.past, cache.batch, 1, a.H, cache.blocks * kBlock, prefix.blocks * kBlock, a.shares, a.per_share, a.parts, a.O, a.ldo},
+                          cache.batch, st);
+}
+
+sqap_status launch_cache8_shared_decode(const __half *QKV, int64_t ld, const int32_t *pos, const int32_t *past, int H, double base, const Cache8View &cache,
+                                        const Cache8View &prefix, const int32_t *length, int d, int longest, int longest_prefix, __half *O, int64_t ldo,
+                                        void *workspace, hipStream_t st)
+{
+    DecodeArgs a = {};
+    a.QKV = QKV;
+    a.ld = ld;
+    a.pos = pos;
+    a.past = past;
+    a.H = H;
+    a.G = H / cache.kv_heads;
+    a.chunks = (a.G + 15) / 16;
+    a.shares = own_shares_of(cache.batch, H, cache.kv_heads, longest);
+    a.per_share = (blocks_of(longest) + a.shares - 1) / a.shares;
+    a.cache = cache;
+    a.prefix = prefix;
+    a.O = O;
+    a.ldo = ldo;
+    a.freq = rope_frequencies(d, base);
+    char *const ws = static_cast<char *>(workspace);
+    return d == 64 ? launch_shared_decode_d<64>(a, length, longest_prefix, ws, st) : launch_shared_decode_d<128>(a, length, longest_prefix, ws, st);
 }
 
 }  // namespace sqap

@@ -164,6 +164,8 @@ struct Calls {
     decltype(&sqap_cache8_append) cache8_append;
     decltype(&sqap_cache8_attention) cache8_attention;
     decltype(&sqap_cache8_decode_attention) cache8_decode_attention;
+    decltype(&sqap_cache8_shared_attention) cache8_shared_attention;
+    decltype(&sqap_cache8_shared_decode_attention) cache8_shared_decode_attention;
     decltype(&sqap_cache8_reorder) cache8_reorder;
     decltype(&sqap_sample) sample;
     decltype(&sqap_beam_select) beam_select;
@@ -283,6 +285,16 @@ SQAP_METHOD(cache8_decode_attention, 10,
 SQAP_METHOD(sample, 9,
             run(c->sample, ptr<sqap_f16>(a[0]), pitch(a[0]), (int32_t)size_of(a[0], 2, 0), (int32_t)size_of(a[0], 2, 1), ptr<float>(a[1]),
                 ptr<int32_t>(a[2]), ptr<float>(a[3]), ptr<float>(a[4]), ptr<float>(a[5]), ptr<int32_t>(a[6]), ptr<float>(a[7]), stream(c, a[8])))
+// (Q, starts, past, cache, prefix, prefix_len, H, max_new, O, workspace, longest_prefix, stream)
+SQAP_METHOD(cache8_shared_attention, 12,
+            run(c->cache8_shared_attention, ptr<sqap_f16>(a[0]), pitch(a[0]), ptr<int32_t>(a[1]), ptr<int32_t>(a[2]), (int32_t)size(a[0], 0), as_i32(a[7]),
+                as_i32(a[6]), handle<sqap_cache8>(a[3]), handle<sqap_cache8>(a[4]), ptr<int32_t>(a[5]), as_i32(a[10]), ptr<sqap_f16>(a[8]), pitch(a[8]),
+                ptr(a[9]), bytes(a[9]), stream(c, a[11])))
+// (QKV, pos, past, cache, prefix, prefix_len, H, O, workspace, longest, longest_prefix, base, stream)
+SQAP_METHOD(cache8_shared_decode_attention, 13,
+            run(c->cache8_shared_decode_attention, ptr<sqap_f16>(a[0]), pitch(a[0]), ptr<int32_t>(a[1]), ptr<int32_t>(a[2]), as_i32(a[6]), as_double(a[11]),
+                handle<sqap_cache8>(a[3]), handle<sqap_cache8>(a[4]), ptr<int32_t>(a[5]), as_i32(a[9]), as_i32(a[10]), ptr<sqap_f16>(a[7]), pitch(a[7]),
+                ptr(a[8]), bytes(a[8]), stream(c, a[12])))
 // (cache, parents [groups, width], lengths, longest, lengths_out, stream)
 SQAP_METHOD(cache8_reorder, 6,
             run(c->cache8_reorder, handle<sqap_cache8>(a[0]), ptr<int32_t>(a[1]), (int32_t)size_of(a[1], 2, 1), ptr<int32_t>(a[2]), as_i32(a[3]),
@@ -319,7 +331,7 @@ SQAP_METHOD(attention, 8, attention_call(c, a))
 #define SQAP_CALLS(X)                                                                                                                   \
     X(attn_scores_batch) X(prune_topk) X(kept_rows) X(prune_rows) X(prune_select) X(quantize_act) X(rmsnorm_quantize_act)              \
     X(swiglu_quantize_act) X(rope) X(rope_append) X(attention) X(decode_attention) X(w4a4_linear) X(mx4_quantize) X(mx4_linear)        \
-    X(cache8_append) X(cache8_attention) X(cache8_decode_attention) X(cache8_reorder) X(sample) X(beam_select) X(group_run) X(decoder_step)
+    X(cache8_append) X(cache8_attention) X(cache8_decode_attention) X(cache8_shared_attention) X(cache8_shared_decode_attention) X(cache8_reorder) X(sample) X(beam_select) X(group_run) X(decoder_step)
 
 PyMethodDef methods[] = {
 #define SQAP_ENTRY(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(m_##NAME)), METH_FASTCALL, nullptr},
