@@ -16,7 +16,7 @@ typedef unsigned long long u64;
 
 constexpr int kBeamT = 256, kBeamWaves = kBeamT / 64, kBeamMost = kBeamMostOutputs;
 constexpr unsigned kMinusInf = 0x03ffu;                               // key of minus infinity, the lowest there is
-constexpr float kLog2eHigh = 1.44269502f, kLog2eLow = 1.92596299e-8f; // log2(e) as the sum of two
+constexpr float kLog2e = 1.44269502f;
 
 // Keys of halves that are neither NaN nor minus zero: integers that order as the halves do.
 __device__ __forceinline__ unsigned key_of(unsigned h) { return h & 0x8000u ? ~h & 0xffffu : h | 0x8000u; }
@@ -35,23 +35,55 @@ __device__ __forceinline__ v4u clean(v4u v)
     }
     return x.u;
 }
+constexpr unsigned kTwoMinusInf = 0xfc00fc00u;
+// Eight halves without the first n, minus infinity behind them.
+__device__ __forceinline__ v4u without_first(v4u v, int n)
+{
+    if (n >= 8) return v4u{kTwoMinusInf, kTwoMinusInf, kTwoMinusInf, kTwoMinusInf};
+    if (n & 4) v = v4u{v[2], v[3], kTwoMinusInf, kTwoMinusInf};
+    if (n & 2) v = v4u{v[1], v[2], v[3], kTwoMinusInf};
+    if (n & 1) v = v4u{v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16 | kTwoMinusInf << 16};
+    return v;
+}
 __device__ __forceinline__ unsigned half_at(const v4u &v, int e) { return e & 1 ? v[e >> 1] >> 16 : v[e >> 1] & 0xffffu; }
-__device__ __forceinline__ float float_at(const v4u &v, int e) { return __half2float(__ushort_as_half((unsigned short)half_at(v, e))); }
-__device__ __forceinline__ unsigned largest_of(const v4u &v)         // key of the largest of the eight
+__device__ __forceinline__ unsigned largest_of(const v4u &v)         // of the eight: minus infinity where all are NaN, no minus zero
 {
     union { v4u u; v2h h[4]; } x;
     x.u = v;
-    const v2h m = __builtin_elementwise_max(__builtin_elementwise_max(x.h[0], x.h[1]), __builtin_elementwise_max(x.h[2], x.h[3]));
-    union { v2h h; unsigned u; } y;
-    y.h = m;
-    return max(key_of(y.u & 0xffffu), key_of(y.u >> 16));
+    const v2h zero = {(_Float16)0.f, (_Float16)0.f};
+    const v2h m = __builtin_elementwise_max(__builtin_elementwise_max(x.h[0], x.h[1]), __builtin_elementwise_max(x.h[2], x.h[3])) + zero;
+    union { _Float16 h; unsigned short u; } y;
+    y.h = __builtin_elementwise_max(__builtin_elementwise_max(m[0], m[1]), (_Float16)-INFINITY);
+    return y.u;
 }
 
-// exp(value - top), of a difference below zero
-__device__ __forceinline__ float exp_of(float value, float top)
+// Exponentials of logits below a largest one, `top`, are 2^(l log2 e - c) with c = top log2 e rounded: one mixed-precision multiply-add (of half I of
+// h) and the power.  Sums of them are kept below c; what its rounding makes of them is put right once (below_top).
+template <int I>
+__device__ __forceinline__ float power_of(const v2h h, float c)
 {
-    const float d = value - top;
-    return __builtin_amdgcn_exp2f(fmaf(d, kLog2eHigh, d * kLog2eLow));
+    float r;
+    if (I == 0) asm("v_fma_mix_f32 %0, %1, %2, -%3 op_sel_hi:[1,0,0]" : "=v"(r) : "v"(h), "s"(kLog2e), "v"(c));
+    else asm("v_fma_mix_f32 %0, %1, %2, -%3 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(h), "s"(kLog2e), "v"(c));
+    return __builtin_amdgcn_exp2f(r);
+}
+__device__ __forceinline__ float eight_powers(const v4u &v, float c)
+{
+    union { v4u u; v2h h[4]; } x;
+    x.u = v;
+    float e[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        e[2 * i] = power_of<0>(x.h[i], c);
+        e[2 * i + 1] = power_of<1>(x.h[i], c);
+    }
+    return ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+}
+__device__ __forceinline__ bool usual(float top) { return fabsf(top) <= 65504.f; }         // neither infinite nor nothing at all
+__device__ __forceinline__ float below(float from, float to) { return __builtin_amdgcn_exp2f(from * kLog2e - to * kLog2e); }
+__device__ __forceinline__ double below_top(double sum, float top)
+{
+    return usual(top) ? sum + sum * (((double)(top * kLog2e) - (double)top * (double)kLog2e) * 0.69314718055994531) : sum;
 }
 
 // How many of the workgroup's 256 values in LDS are at least `from` (all wavefronts ask the same: four values to a lane).
@@ -80,12 +112,15 @@ struct BeamArgs {
 
 // One workgroup per row and slab of 2048 PIECES logits, which it holds in registers.  The largest of each piece of eight, with the piece's place
 // below it, is a number of its own; at least k pieces are not below the k-th largest of the threads' largest, and the slab's
-// best k lie in those: any other piece has k logits before its own.  Of their logits those that reach the smallest of these maxima are listed and ranked.
+// best k lie in those: any other piece has k logits before its own.  They go to LDS, a thread takes one of their logits each, and those that reach the
+// smallest of these maxima are listed and ranked.
 template <int PIECES>
 __global__ __launch_bounds__(kBeamT) void beam_rows_kernel(const BeamArgs a)
 {
-    constexpr int LISTED = kBeamMost * PIECES * 8;
-    __shared__ unsigned tops[kBeamT], list[LISTED], listed;
+    constexpr int MOST = kBeamMost * PIECES;                          // pieces of the k threads that reach the bound
+    __shared__ unsigned place[MOST], pieces, listed;
+    __shared__ __attribute__((aligned(16))) unsigned tops[kBeamT], list[MOST * 8];
+    __shared__ v4u piece[MOST];
     __shared__ float wave_top[kBeamWaves];
     __shared__ double wave_sum_[kBeamWaves];
     const int t = threadIdx.x, l = t & 63, wave = t >> 6, slab = blockIdx.x % a.slabs;
@@ -93,52 +128,53 @@ __global__ __launch_bounds__(kBeamT) void beam_rows_kernel(const BeamArgs a)
     if (a.done && a.done[row] != 0) return;
     const int first = slab * (kBeamT * 8 * PIECES);
     const __half *from = a.logits + row * a.ld;
+    // (a piece over the end is read as the row's last eight and put right below: nothing waits before all of them have been asked for)
     v4u v[PIECES];
+    if (a.vocab >= 8) {
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) {
-        const int at = first + (p * kBeamT + t) * 8;
-        v[p] = v4u{0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u};
-        if (at + 8 <= a.vocab) v[p] = *reinterpret_cast<const v4u_any *>(from + at);
-        else {
+        for (int p = 0; p < PIECES; ++p) v[p] = *reinterpret_cast<const v4u_any *>(from + min(first + (p * kBeamT + t) * 8, a.vocab - 8));
+    } else {
+        v[0] = v4u{kTwoMinusInf, kTwoMinusInf, kTwoMinusInf, kTwoMinusInf};
+        if (t == 0)
+            for (int e = a.vocab - 1; e >= 0; --e) v[0] = v4u{v[0][0] << 16 | __half_as_ushort(from[e]), v[0][0] >> 16 | v[0][1] << 16,
+                                                             v[0][1] >> 16 | v[0][2] << 16, v[0][2] >> 16 | v[0][3] << 16};
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (at + e < a.vocab) {
-                    const unsigned h = __half_as_ushort(from[at + e]);
-                    v[p][e >> 1] = e & 1 ? (v[p][e >> 1] & 0xffffu) | h << 16 : (v[p][e >> 1] & 0xffff0000u) | h;
-                }
-        }
+        for (int p = 1; p < PIECES; ++p) v[p] = v4u{kTwoMinusInf, kTwoMinusInf, kTwoMinusInf, kTwoMinusInf};
     }
-    if (t == 0) listed = 0;
+    if (t == 0) pieces = 0, listed = 0;
+    // piece by piece as they arrive: the largest, and the sum of exponentials below the thread's largest so far (eight of them in binary32, those
+    // sums in binary64: beside one large term many small ones count)
     unsigned mine = 0, keys[PIECES];
+    float top = -INFINITY;
+    double sum = 0.0;
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
-        v[p] = clean(v[p]);
-        keys[p] = largest_of(v[p]) << 11 | (2047 - (p * kBeamT + t));
+        const int over = first + (p * kBeamT + t) * 8 + 8 - a.vocab;
+        if (over > 0 && a.vocab >= 8) v[p] = without_first(v[p], over);
+        const unsigned largest = largest_of(v[p]);
+        keys[p] = key_of(largest) << 11 | (2047 - (p * kBeamT + t));
         mine = max(mine, keys[p]);
+        const float here = __half2float(__ushort_as_half((unsigned short)largest));
+        if (here > top) {
+            sum = usual(here) ? sum * (double)below(top, here) : 0.0;
+            top = here;
+        }
+        if (usual(top)) sum += (double)eight_powers(v[p], top * kLog2e);
     }
-    tops[t] = mine;
-    // the sum of exponentials, of each thread below its own largest logit
-    const float top = value_of(mine >> 11);
-    // (eight of them in binary32, those sums in binary64: beside one large term many small ones count)
-    double sum = 0.0;
-    if (fabsf(top) <= 65504.f) {
+    if (sum != sum || top > 65504.f) {                                // NaN, or infinite logits: those are counted
+        sum = 0.0;
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
-            float x[8];
+            const v4u x = clean(v[p]);
+            if (usual(top)) sum += (double)eight_powers(x, top * kLog2e);
+            else
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = exp_of(float_at(v[p], e), top);
-            sum += (double)(((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7])));
+                for (int e = 0; e < 8; ++e) sum += half_at(x, e) == 0x7c00u ? 1.0 : 0.0;
         }
-    } else if (top > 0.f) {
-#pragma unroll
-        for (int p = 0; p < PIECES; ++p)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum += half_at(v[p], e) == 0x7c00u ? 1.0 : 0.0;
     }
-    float most = top;
-#pragma unroll
-    for (int i = 32; i > 0; i >>= 1) most = fmaxf(most, __shfl_xor(most, i));
-    const double part = wave_sum(top == most ? sum : fabsf(most) <= 65504.f ? sum * (double)exp_of(top, most) : 0.0);
+    tops[t] = mine;
+    const float most = wavefront_max(top);
+    const double part = wave_sum(top == most ? sum : usual(most) ? sum * (double)below(top, most) : 0.0);
     if (l == 0) wave_top[wave] = most, wave_sum_[wave] = part;
     __syncthreads();
     // a number that k of the threads' largest reach, and no other: bits from the highest on, until the count is right
@@ -151,16 +187,19 @@ __global__ __launch_bounds__(kBeamT) void beam_rows_kernel(const BeamArgs a)
         if (n == a.k) break;
     }
     if (mine >= reach) {
-        const unsigned least = max(reach >> 11, kMinusInf + 1);
 #pragma unroll
         for (int p = 0; p < PIECES; ++p)
             if (keys[p] >= reach) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const unsigned key = key_of(half_at(v[p], e));
-                    if (key >= least) list[atomicAdd(&listed, 1u)] = key << 14 | (16383 - ((p * kBeamT + t) * 8 + e));
-                }
+                const unsigned at = atomicAdd(&pieces, 1u);
+                piece[at] = clean(v[p]);
+                place[at] = p * kBeamT + t;
             }
+    }
+    __syncthreads();
+    const unsigned least = max(reach >> 11, kMinusInf + 1);
+    for (int i = t; i < 8 * (int)pieces; i += kBeamT) {
+        const unsigned key = key_of(reinterpret_cast<const unsigned short *>(&piece[i >> 3])[i & 7]);
+        if (key >= least) list[atomicAdd(&listed, 1u)] = key << 14 | (16383 - (place[i >> 3] * 8 + (i & 7)));
     }
     __syncthreads();
     const int n = (int)listed;
@@ -168,7 +207,11 @@ __global__ __launch_bounds__(kBeamT) void beam_rows_kernel(const BeamArgs a)
     for (int i = t; i < n; i += kBeamT) {
         const unsigned own = list[i];
         int rank = 0;
-        for (int j = 0; j < n; ++j) rank += list[j] > own ? 1 : 0;
+        for (int j = 0; j < n; j += 8) {
+            const v4u x = *reinterpret_cast<const v4u *>(list + j), y = *reinterpret_cast<const v4u *>(list + j + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) rank += (j + e < n && x[e] > own ? 1 : 0) + (j + 4 + e < n && y[e] > own ? 1 : 0);
+        }
         if (rank < a.k) best[rank] = v2u{own >> 14, (unsigned)first + 16383 - (own & 16383)};
     }
     for (int i = n + t; i < a.k; i += kBeamT) best[i] = v2u{0, 0};
@@ -178,8 +221,8 @@ __global__ __launch_bounds__(kBeamT) void beam_rows_kernel(const BeamArgs a)
         double all = 0.0;
         for (int w = 0; w < kBeamWaves; ++w)
             if (wave_top[w] == whole) all += wave_sum_[w];
-            else if (fabsf(whole) <= 65504.f) all += wave_sum_[w] * (double)exp_of(wave_top[w], whole);
-        a.rows[row * a.slabs + slab] = BeamRow{all, whole};
+            else if (usual(whole)) all += wave_sum_[w] * (double)below(wave_top[w], whole);
+        a.rows[row * a.slabs + slab] = BeamRow{below_top(all, whole), whole};
     }
 }
 
@@ -210,47 +253,71 @@ __global__ __launch_bounds__(kBeamT) void beam_select_kernel(const BeamArgs a)
     const int t = threadIdx.x, l = t & 63, wave = t >> 6, each = a.slabs * a.k, all = a.beams * each;
     const int64_t b = blockIdx.x, row0 = b * a.beams;
     if (t == 0) listed = 0;
-    for (int r = wave; r < a.beams; r += kBeamWaves) {
+    constexpr int KEPT = 4;                                           // candidates that a thread keeps; of more, it works out the others again
+    v2u words[KEPT];
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) words[i] = a.best[row0 * each + min(t + i * kBeamT, all - 1)];
+    // rows' sums: eight lanes each
+    for (int r0 = 0; r0 < a.beams; r0 += kBeamT / 8) {
+        const int r = r0 + t / 8, i0 = t % 8;
+        if (r >= a.beams) break;                                      // (all eight lanes)
         const bool done = a.done && a.done[row0 + r] != 0;
+        const double own = (double)a.scores[row0 + r];
+        const BeamRow *rows = a.rows + (row0 + r) * a.slabs;
         float m = -INFINITY;
         double sum = 0.0;
         if (!done) {
-            const BeamRow *rows = a.rows + (row0 + r) * a.slabs;
-            for (int i = l; i < a.slabs; i += 64) m = fmaxf(m, rows[i].top);
-#pragma unroll
-            for (int i = 32; i > 0; i >>= 1) m = fmaxf(m, __shfl_xor(m, i));
-            for (int i = l; i < a.slabs; i += 64) {
+            for (int i = i0; i < a.slabs; i += 8) {                   // (the larger of two: the other's terms below it)
                 const BeamRow x = rows[i];
-                if (x.top == m) sum += x.sum;
-                else if (fabsf(m) <= 65504.f) sum += x.sum * exp((double)x.top - (double)m);
+                const float both = fmaxf(m, x.top);
+                if (usual(both)) sum = x.top == both ? x.sum + sum * exp((double)m - (double)both) : sum + x.sum * exp((double)x.top - (double)both);
+                else if (both > 0.f) sum = (m == both ? sum : 0.0) + (x.top == both ? x.sum : 0.0);
+                m = both;
             }
-            sum = wave_sum(sum);
         }
-        if (l == 0) {
+#pragma unroll
+        for (int d = 4; d > 0; d >>= 1) {
+            const float other = __shfl_xor(m, d), both = fmaxf(m, other);
+            const double more = __shfl_xor(sum, d);
+            const float low = fminf(m, other);
+            if (usual(both)) {
+                const double f = low == both ? 1.0 : exp((double)low - (double)both);
+                sum = (m == both ? sum : sum * f) + (other == both ? more : more * f);
+            } else if (both > 0.f) {
+                sum = (m == both ? sum : 0.0) + (other == both ? more : 0.0);
+            }
+            m = both;
+        }
+        if (i0 == 0) {
             top[r] = m;
             log_sum[r] = done ? 0.0 : log(sum);
-            score[r] = (double)a.scores[row0 + r];
+            score[r] = own;
             ended[r] = done;
         }
     }
     __syncthreads();
-    auto candidate = [&](int c) {
+    auto candidate_of = [&](int c, v2u have) {
         const int r = c / each, i = c - r * each;
         Candidate x = {0, 0};
         if (ended[r]) {
             if (i == 0) x.total = total_key(score[r]), x.tie = (u64)(kBeamMost - 1 - r) << kTieBeam | (unsigned)((1 << kTieKey) - 1 - a.eos);
             return x;
         }
-        const v2u have = a.best[row0 * each + c];
         if (have[0] == 0) return x;
         const float v = value_of(have[0]), m = top[r];
-        if (fabsf(m) > 65504.f && v != m) return x;                   // (beside infinite logits the others have no probability)
+        if (!usual(m) && v != m) return x;                   // (beside infinite logits the others have no probability)
         x.total = total_key(score[r] + ((v == m ? 0.0 : (double)v - (double)m) - log_sum[r]));
         x.tie = (u64)(kBeamMost - 1 - r) << kTieBeam | (u64)have[0] << kTieKey | ((1u << kTieKey) - 1 - have[1]);
         return x;
     };
-    Candidate mine = {0, 0};
-    for (int c = t; c < all; c += kBeamT) {
+    auto candidate = [&](int c) { return candidate_of(c, a.best[row0 * each + c]); };
+    Candidate kept[KEPT], mine = {0, 0};
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) {
+        kept[i] = t + i * kBeamT < all ? candidate_of(t + i * kBeamT, words[i]) : Candidate{0, 0};
+        if (before(kept[i], mine)) mine = kept[i];
+    }
+    for (int c = t + KEPT * kBeamT; c < all; c += kBeamT) {
         const Candidate x = candidate(c);
         if (before(x, mine)) mine = x;
     }
@@ -260,38 +327,50 @@ __global__ __launch_bounds__(kBeamT) void beam_select_kernel(const BeamArgs a)
     Candidate four[4], reach = {0, 0};
 #pragma unroll
     for (int i = 0; i < 4; ++i) four[i] = tops[4 * l + i];
-    auto reached = [&](const Candidate &from) {
-        int n = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) n += __popcll(__ballot(!before(from, four[i])));
-        return n;
-    };
-    // the highest number, bit by bit, that k of them reach, or one that exactly k do
-    auto search = [&](auto count) {
-        for (int bit = 63 + kTieBeam + 6; bit >= 0; --bit) {
-            Candidate next = reach;
-            if (bit >= kTieBeam + 6) next.total |= 1ull << (bit - kTieBeam - 6);
-            else next.tie |= 1ull << bit;
-            const int n = count(next);
+    // the highest number, bit by bit, that k of them reach, or one that exactly k do: of totals, then where those are equal of the ties
+    auto search = [&](auto by_total, auto by_both) {
+        for (int bit = 63; bit >= 0; --bit) {
+            const u64 next = reach.total | 1ull << bit;
+            const int n = by_total(next);
+            if (n >= a.k) reach.total = next;
+            if (n == a.k) return;
+        }
+        for (int bit = kTieBeam + 5; bit >= 0; --bit) {
+            const Candidate next = {reach.total, reach.tie | 1ull << bit};
+            const int n = by_both(next);
             if (n >= a.k) reach = next;
-            if (n == a.k) break;
+            if (n == a.k) return;
         }
     };
-    search(reached);
+    search(
+        [&](u64 from) {
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) n += __popcll(__ballot(four[i].total >= from));
+            return n;
+        },
+        [&](const Candidate &from) {
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) n += __popcll(__ballot(!before(from, four[i])));
+            return n;
+        });
     auto list_them = [&] {
         if (before(reach, mine)) return;
-        for (int c = t; c < all; c += kBeamT) {
-            const Candidate x = candidate(c);
-            if (x.total == 0 || before(reach, x)) continue;
+        auto enter = [&](const Candidate &x) {
+            if (x.total == 0 || before(reach, x)) return;
             const int at = atomicAdd(&listed, 1);
             if (at < kSurvivors) list[at] = x;
-        }
+        };
+#pragma unroll
+        for (int i = 0; i < KEPT; ++i) enter(kept[i]);
+        for (int c = t + KEPT * kBeamT; c < all; c += kBeamT) enter(candidate(c));
     };
     list_them();
     __syncthreads();
     if (listed > kSurvivors) {                                        // many of few threads: count all of them instead
         reach = Candidate{0, 0};
-        search([&](const Candidate &from) {
+        auto count = [&](const Candidate &from) {
             int n = 0;
             if (!before(from, mine))
                 for (int c = t; c < all; c += kBeamT) n += before(from, candidate(c)) ? 0 : 1;
@@ -303,7 +382,8 @@ __global__ __launch_bounds__(kBeamT) void beam_select_kernel(const BeamArgs a)
             n = 0;
             for (int w = 0; w < kBeamWaves; ++w) n += counts[w];
             return n;
-        });
+        };
+        search([&](u64 from) { return count(Candidate{from, 0}); }, count);
         if (t == 0) listed = 0;
         __syncthreads();
         list_them();
@@ -389,58 +469,63 @@ __device__ __forceinline__ Parents parents_of(const int32_t *parents, const int3
     return p;
 }
 
-// Piece `at` of every sequence that moves: all of them are read before the first is written, so that in place is no matter.
-template <int WIDTH, typename V, typename Takes>
-__device__ __forceinline__ void move_piece(V *base, int64_t pitch, const Parents &p, Takes takes)
+// The lane's piece of every sequence that takes over something, from the I-th on: all of them are read (on the way down) before the first is written
+// (on the way back), so that in place is no matter.  base: of the group's first sequence, the others `pitch` bytes apart; `takes` says by a
+// sequence's length whether this lane has anything of it.  (An array of pieces is made one wide register, copied at each of them.)
+template <int I, int WIDTH, typename V, typename Takes>
+__device__ __forceinline__ void move_pieces(char *base, int64_t pitch, unsigned offset, const Parents &p, u64 &moves, Takes takes)
 {
-    V v[WIDTH];
-#pragma unroll
-    for (int i = 0; i < WIDTH; ++i)
-        if (p.moves >> i & 1) {
-            const int n = __builtin_amdgcn_readlane(p.length, i), of = __builtin_amdgcn_readlane(p.parent, i);
-            if (takes(n)) v[i] = base[of * pitch];
-        }
-#pragma unroll
-    for (int i = 0; i < WIDTH; ++i)
-        if (p.moves >> i & 1) {
-            if (takes(__builtin_amdgcn_readlane(p.length, i))) base[i * pitch] = v[i];
-        }
+    V piece;
+    if (moves >> I & 1) {
+        const char *from = base + __builtin_amdgcn_readlane(p.parent, I) * pitch;
+        if (takes(__builtin_amdgcn_readlane(p.length, I))) piece = *reinterpret_cast<const V *>(from + offset);
+    }
+    if constexpr (I + 1 < WIDTH) move_pieces<I + 1, WIDTH, V>(base, pitch, offset, p, moves, takes);
+    else asm volatile("" : "+s"(moves));                              // (no path of its own for each set of sequences)
+    if (moves >> I & 1) {
+        char *to = base + I * pitch;
+        if (takes(__builtin_amdgcn_readlane(p.length, I))) *reinterpret_cast<V *>(to + offset) = piece;
+    }
 }
 
-// One workgroup per group, key head and kibibytes of a block (for all sequences of the group at once), of the unfinished block's rows, or the
-// scales; V: what a thread moves of each.
+// One workgroup per group, key head and 256 pieces of a block (of all sequences of the group at once), of the unfinished block's rows, or of
+// the scales; V: a piece.
 template <int D, int WIDTH, typename V>
 __global__ __launch_bounds__(256) void cache8_reorder_kernel(const Cache8View cache, const int32_t *__restrict__ parents, int width,
                                                              const int32_t *__restrict__ lengths, int32_t *__restrict__ lengths_out, int block_groups)
 {
-    constexpr int BLOCK_V = 2 * kCache8Block * D / (int)sizeof(V), TAIL_V = 2 * BLOCK_V, SPLIT = BLOCK_V / 256, TAIL_SPLIT = TAIL_V / 256;
+    constexpr int BYTES = 2 * kCache8Block * D, SPLIT = BYTES / (256 * (int)sizeof(V)), TAIL_SPLIT = 2 * SPLIT;
     const int t = threadIdx.x, h = blockIdx.y;
-    const int64_t first = (int64_t)blockIdx.z * width, heads = cache.kv_heads;
+    const int64_t first = (int64_t)blockIdx.z * width, heads = cache.kv_heads, head = first * heads + h;
     const Parents p = parents_of(parents, lengths, first, width, cache.blocks * kCache8Block);
     if (lengths_out && h == 0 && blockIdx.x == 0 && t < width) lengths_out[first + t] = p.length;
-    if (p.moves == 0) return;
-    const int64_t head = first * heads + h;                           // of the group's first sequence
     if ((int)blockIdx.x < block_groups) {
-        int most = 0;
-        for (u64 m = p.moves; m; m &= m - 1) most = max(most, __builtin_amdgcn_readlane(p.length, __builtin_ctzll(m)));
-        for (int x = blockIdx.x; x < most / kCache8Block * SPLIT; x += block_groups) {
+#pragma unroll 1
+        for (int x = blockIdx.x;; x += block_groups) {
             const int block = x / SPLIT;
-            V *codes = reinterpret_cast<V *>(cache.codes) + (head * cache.blocks + block) * BLOCK_V + (x % SPLIT) * 256 + t;
-            move_piece<WIDTH>(codes, heads * cache.blocks * BLOCK_V, p, [&](int n) { return block < n / kCache8Block; });
+            u64 moves = __ballot(p.moves >> (t & 63) & 1 && block < p.length / kCache8Block);
+            if (moves == 0) break;                                    // (nor any block behind it)
+            move_pieces<0, WIDTH, V>(reinterpret_cast<char *>(cache.codes) + (head * cache.blocks + block) * BYTES, heads * cache.blocks * BYTES,
+                                     (unsigned)(x % SPLIT * 256 + t) * (unsigned)sizeof(V), p, moves, [](int) { return true; });
         }
         return;
     }
     const int x = (int)blockIdx.x - block_groups;
     if (x < TAIL_SPLIT) {
-        const int piece = x * 256 + t, row = piece / (D * 2 / (int)sizeof(V)) % kCache8Block;
-        V *tail = reinterpret_cast<V *>(cache.tail) + head * TAIL_V + piece;
-        move_piece<WIDTH>(tail, heads * TAIL_V, p, [&](int n) { return row < n % kCache8Block; });
+        const unsigned offset = (unsigned)(x * 256 + t) * (unsigned)sizeof(V);
+        const int row = (int)(offset / (2 * D)) % kCache8Block;
+        u64 moves = __ballot(p.moves >> (t & 63) & 1 && p.length % kCache8Block > 0);
+        move_pieces<0, WIDTH, V>(reinterpret_cast<char *>(cache.tail) + head * 2 * BYTES, heads * 2 * BYTES, offset, p, moves,
+                                 [&](int n) { return row < n % kCache8Block; });
         return;
     }
-    for (int from = 0; from < cache.blocks; from += 256) {
-        const int block = from + t;                                   // (all lanes stay: the lengths are other lanes')
-        v2u *scales = reinterpret_cast<v2u *>(cache.scales) + head * cache.blocks + block;
-        move_piece<WIDTH>(scales, heads * cache.blocks, p, [&](int n) { return block < n / kCache8Block; });
+#pragma unroll 1
+    for (int from = 0;; from += 256) {                                // (a wavefront has 64 scales: the longest decides whether there are any)
+        const int block = from + t;
+        u64 moves = __ballot(p.moves >> (t & 63) & 1 && from + (t & ~63) < p.length / kCache8Block);
+        if (__syncthreads_or(moves != 0) == 0) break;
+        move_pieces<0, WIDTH, v2u>(reinterpret_cast<char *>(cache.scales) + head * cache.blocks * 8, heads * cache.blocks * 8, (unsigned)block * 8u, p, moves,
+                                   [&](int n) { return block < n / kCache8Block; });
     }
 }
 
