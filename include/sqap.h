@@ -566,7 +566,7 @@ sqap_status sqap_cache8_read(const sqap_cache8 *cache, const int32_t *lengths, i
  * the sequences of a group of more than width * max_new rows in all, and of a prefix whose prefix_len is negative or beyond its capacity
  * (appended to they are all the same).  One whose starts do not lie in order, or outside those of its group's first and last, is skipped.
  * EINVAL, EUNSUPPORTED: as above; EINVAL also for a cache of prefixes of other heads, a batch that is no multiple of theirs, longest_prefix < 0;
- * EUNSUPPORTED for more than 13107 sequences, rows of a group times H / kv_heads beyond 32 bits.
+ * EUNSUPPORTED for more than 4095 sequences, rows of a group times H / kv_heads beyond 32 bits.
  */
 size_t sqap_cache8_shared_workspace_bytes(int32_t batch, int32_t groups, int32_t H, int32_t kv_heads, int32_t head_dim,
                                           int32_t rows, int32_t max_new, int32_t longest, int32_t longest_prefix);

@@ -859,7 +859,7 @@ static sqap_status check_prefix(const char *who, const sqap_cache8 *cache, const
         return fail(SQAP_EINVAL, "%s: %d sequences behind %d prefixes", who, cache->batch, prefix->batch);
     if (longest_prefix < 0) return fail(SQAP_EINVAL, "%s: longest_prefix = %d", who, longest_prefix);
     if (cache->batch > 0 && !prefix_len) return fail(SQAP_EINVAL, "%s: null pointer", who);
-    if (cache->batch > 13107) return fail(SQAP_EUNSUPPORTED, "%s: %d sequences", who, cache->batch);
+    if (cache->batch > 4095) return fail(SQAP_EUNSUPPORTED, "%s: %d sequences", who, cache->batch);
     return SQAP_OK;
 }
 

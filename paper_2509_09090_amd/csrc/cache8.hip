@@ -1220,15 +1220,22 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void cache8_decode_kernel(con
     constexpr int HALF = D / 2, C = D / 64, T = 64 * kDecodeWaves, DT = D / 16;
     __shared__ DecodeLds<D> lds;
     const Cache8View &cache = a.cache;
-    const int share = blockIdx.x, kh = blockIdx.y / a.chunks, chunk = blockIdx.y % a.chunks, b = blockIdx.z;
-    if constexpr (SHARED) {
-        if (b >= cache.batch) {
-            if (chunk == 0 && share < a.parts.prefix_shares)
-                prefix_tile<D, true>(lds, PrefixTile{a.QKV, a.ld, nullptr, a.pos, cache.batch, 1, a.H}, a.prefix, a.parts, a.freq,
-                                     (b - cache.batch) / a.prefix_tiles, kh, (b - cache.batch) % a.prefix_tiles, share);
+    int share = blockIdx.x, kh = blockIdx.y / a.chunks, chunk = blockIdx.y % a.chunks, b = blockIdx.z;
+    if constexpr (SHARED) {                                           // (in one dimension: a workgroup without work takes 9 ns to come and go)
+        int id = blockIdx.x;
+        const int items = a.prefix.batch * cache.kv_heads * a.parts.prefix_shares, behind = items * a.prefix_tiles;
+        if (id < behind) {                                            // tiles of one share behind one L2 where the shares fill all of them
+            const int item = id % items;
+            prefix_tile<D, true>(lds, PrefixTile{a.QKV, a.ld, nullptr, a.pos, cache.batch, 1, a.H}, a.prefix, a.parts, a.freq,
+                                 item / a.parts.prefix_shares / cache.kv_heads, item / a.parts.prefix_shares % cache.kv_heads, id / items, item % a.parts.prefix_shares);
             return;
         }
-        if (share >= a.shares) return;
+        id -= behind;
+        share = id % a.shares;
+        id /= a.shares;
+        chunk = id % a.chunks;
+        kh = id / a.chunks % cache.kv_heads;
+        b = id / a.chunks / cache.kv_heads;
     }
     const int t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), r = l & 15, g = l >> 4;
     const int first_head = kh * a.G + chunk * 16, heads = min(16, a.G - chunk * 16);
@@ -1555,8 +1562,8 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void cache8_decode_kernel(con
 
 // ---------------------------------------------------------------- the parts in one
 
-// The parts of a (row, head) pair: D / 4 lanes with four columns each; the lanes share out the parts' maxima and sums first.  One workgroup per
-// sequence and 1024 / D of its pairs.
+// The parts of a (row, head) pair: D / 4 lanes with four columns each; the lanes share out the parts' maxima and sums first.  SPLIT groups of such
+// lanes deal out a pair's parts, where there are many.  One workgroup per sequence and 1024 / D / SPLIT of its pairs.
 constexpr int kMostParts = 128;                                       // of a pair
 struct JoinArgs {
     const int32_t *starts, *past;                             // starts null: one row per sequence
@@ -1566,10 +1573,11 @@ struct JoinArgs {
     __half *O;
     int64_t ldo;
 };
-template <int D>
+template <int D, int SPLIT>
 __global__ __launch_bounds__(256) void cache8_join_kernel(const JoinArgs a)
 {
-    constexpr int LANES = D / 4, EACH = 256 / LANES, KEPT = kMostParts / LANES;
+    constexpr int LANES = D / 4, EACH = 256 / LANES / SPLIT, KEPT = kMostParts / LANES;
+    __shared__ __attribute__((aligned(16))) float sums[SPLIT > 1 ? SPLIT * EACH * D : 4];
     const int b = blockIdx.y, t = threadIdx.x, lane = t % LANES, group = b / a.parts.width;
     Span sp;
     bool fits;
@@ -1590,13 +1598,17 @@ __global__ __launch_bounds__(256) void cache8_join_kernel(const JoinArgs a)
     const int own = a.starts ? 1 : (last + own_each) / own_each, all = prefix.active + own;
     auto part_of = [&](int i) { return i < prefix.active ? i : a.parts.prefix_shares + i - prefix.active; };
     const int64_t pairs = (int64_t)sp.n * a.H;
-    for (int64_t p = (int64_t)blockIdx.x * EACH + t / LANES; p < pairs; p += (int64_t)gridDim.x * EACH) {
+    const int turn = SPLIT > 1 ? t / LANES / EACH : 0;                // the groups of a pair take every SPLIT-th four parts
+    for (int64_t p0 = (int64_t)blockIdx.x * EACH; p0 < pairs; p0 += (int64_t)gridDim.x * EACH) {
+        const int64_t p = p0 + t / LANES % EACH;
+        if (SPLIT == 1 && p >= pairs) break;                          // (otherwise a workgroup has one round, and its last pairs may be none)
+        const bool is_pair = p < pairs;
         const int64_t row = sp.row + p / a.H, head = p % a.H, at = row * a.H + head;
         __half *to = a.O + row * a.ldo + head * D + lane * 4;
         union { __half h[4]; v2u v; } out;
         if (!fits) {
             out.v = v2u{0x7e007e00u, 0x7e007e00u};
-            *reinterpret_cast<v2u *>(to) = out.v;
+            if (is_pair && turn == 0) *reinterpret_cast<v2u *>(to) = out.v;
             continue;
         }
         float2 ml[KEPT];
@@ -1605,7 +1617,7 @@ __global__ __launch_bounds__(256) void cache8_join_kernel(const JoinArgs a)
         for (int k = 0; k < KEPT; ++k) {
             const int i = k * LANES + lane;
             ml[k] = float2{-INFINITY, 0.f};
-            if (i < all) ml[k] = a.parts.ml[part_of(i) * a.parts.pairs + at];
+            if (i < all && is_pair) ml[k] = a.parts.ml[part_of(i) * a.parts.pairs + at];
             top = fmaxf(top, ml[k].x);
         }
 #pragma unroll
@@ -1621,7 +1633,7 @@ __global__ __launch_bounds__(256) void cache8_join_kernel(const JoinArgs a)
 #pragma unroll
         for (int k = 0; k < KEPT; ++k) {
             const int n = min(all - k * LANES, LANES);
-            for (int i0 = 0; i0 < n; i0 += 4) {                       // four of them asked for at a time (the last one again where there are fewer, for nothing)
+            for (int i0 = 4 * turn; i0 < n && is_pair; i0 += 4 * SPLIT) {                       // four of them asked for at a time (the last one again where there are fewer, for nothing)
                 v4f x[4];
                 float f[4];
 #pragma unroll
@@ -1636,10 +1648,17 @@ __global__ __launch_bounds__(256) void cache8_join_kernel(const JoinArgs a)
                     for (int e = 0; e < 4; ++e) o[e] += fabsf(x[i][e]) < INFINITY ? f[i] * x[i][e] : x[i][e];      // (an infinite value stays one however small its weight)
             }
         }
+        if constexpr (SPLIT > 1) {
+            *reinterpret_cast<v4f *>(sums + t * 4) = o;               // [group of a pair][pair][column]
+            __syncthreads();
+            if (turn > 0 || !is_pair) return;
+            for (int x = 1; x < SPLIT; ++x) o += *reinterpret_cast<const v4f *>(sums + t * 4 + x * EACH * D);
+        }
         const float norm = 1.f / sum;
 #pragma unroll
         for (int e = 0; e < 4; ++e) out.h[e] = __float2half_rn(o[e] * norm);
         *reinterpret_cast<v2u *>(to) = out.v;
+        if (SPLIT > 1) return;
     }
 }
 
@@ -1781,8 +1800,10 @@ sqap_status launch_cache8_decode(const __half *QKV, int64_t ld, const int32_t *p
 
 // ---- behind a shared prefix
 
-// How the prefixes are dealt out.  Few pairs to a group and key head: tiles of 16, blocks dealt to the wavefronts; more: tiles of 128.
-constexpr int kFewPairs = 64, kPrefixGroups = 512, kMostPrefixShares = 64;
+// How the prefixes are dealt out.  Up to 64 pairs to a group and key head: tiles of 16, blocks dealt to the wavefronts; up to 256 of them, too, where all
+// tiles together have no more than 20000 blocks: the tiles of 128 want two launches more (32 rows of 32 heads over 8 behind 1000 positions 14 and
+// 27 us, behind 20000 45 and 48, behind 100003 187 and 128; 64 behind 1000 23 and 29).
+constexpr int kFewPairs = 64, kFewPairsAtMost = 256, kFewBlocks = 20000, kPrefixGroups = 512, kMostPrefixShares = 64;
 struct SharedPlan {
     bool few;
     int64_t tiles;               // of a group and key head
@@ -1794,9 +1815,9 @@ static SharedPlan shared_plan(int batch, int groups, int H, int kv_heads, int d,
 {
     SharedPlan p = {};
     const int64_t of_group = std::min<int64_t>((int64_t)(batch / groups) * max_new, rows) * (H / kv_heads);
-    p.few = of_group <= kFewPairs;
-    p.tiles = std::max<int64_t>(1, (of_group + (p.few ? 15 : 127)) / (p.few ? 16 : 128));
     const int blocks = std::max(1, blocks_of(longest_prefix));
+    p.few = of_group <= kFewPairs || (of_group <= kFewPairsAtMost && (of_group + 15) / 16 * groups * kv_heads * blocks <= kFewBlocks);
+    p.tiles = std::max<int64_t>(1, (of_group + (p.few ? 15 : 127)) / (p.few ? 16 : 128));
     const int64_t items = p.tiles * groups * kv_heads;
     p.shares = (int)std::max<int64_t>(1, std::min<int64_t>({(blocks + 3) / 4, kPrefixGroups / items, kMostPrefixShares}));
     p.own_shares = own_shares;
@@ -1840,12 +1861,16 @@ static sqap_status launch_prefix(const SharedPlan &plan, const PrefixTile &a, co
     return SQAP_OK;
 }
 
+// Four groups of lanes to a pair where there are more than eight parts and the pairs alone would leave the device half empty.
 template <int D>
 static sqap_status launch_join(const JoinArgs &a, int batch, hipStream_t st)
 {
-    constexpr int EACH = 1024 / D;
-    const int64_t groups = std::max<int64_t>(1, std::min<int64_t>(((int64_t)a.max_new * a.H + EACH - 1) / EACH, 1 << 16));
-    hipLaunchKernelGGL(cache8_join_kernel<D>, dim3((unsigned)groups, batch), dim3(256), 0, st, a);
+    constexpr int EACH = 1024 / D, SPLIT = 4;
+    const int64_t pairs = (int64_t)std::max(1, a.max_new) * a.H, groups = (pairs + EACH - 1) / EACH;
+    if (a.max_new == 1 && a.parts.prefix_shares > 8 && groups * batch < 1024)
+        hipLaunchKernelGGL((cache8_join_kernel<D, SPLIT>), dim3((unsigned)((pairs + EACH / SPLIT - 1) / (EACH / SPLIT)), batch), dim3(256), 0, st, a);
+    else
+        hipLaunchKernelGGL((cache8_join_kernel<D, 1>), dim3((unsigned)std::min<int64_t>(groups, 1 << 16), batch), dim3(256), 0, st, a);
     SQAP_HIP_CHECK(hipGetLastError());
     return SQAP_OK;
 }
@@ -1877,11 +1902,10 @@ static sqap_status launch_shared_decode_d(DecodeArgs a, const int32_t *length, i
     const Cache8View &cache = a.cache, &prefix = a.prefix;
     const SharedPlan plan = shared_plan(cache.batch, prefix.batch, a.H, cache.kv_heads, D, cache.batch, 1, a.shares, longest_prefix);
     a.parts = {reinterpret_cast<float *>(workspace + plan.o), reinterpret_cast<float2 *>(workspace + plan.ml), plan.pairs, plan.shares, cache.batch / prefix.batch, length};
-    a.prefix_tiles = (int)plan.tiles;
+    a.prefix_tiles = plan.few ? (int)plan.tiles : 0;
     a.q_out = plan.few ? nullptr : reinterpret_cast<__half *>(workspace + plan.q);
-    const int behind = plan.few ? (int)(prefix.batch * plan.tiles) : 0;
-    hipLaunchKernelGGL((cache8_decode_kernel<D, true>), dim3(plan.few ? std::max(plan.shares, a.shares) : a.shares, cache.kv_heads * a.chunks, cache.batch + behind),
-                       dim3(64 * kDecodeWaves), 0, st, a);
+    const int64_t items = (int64_t)prefix.batch * a.prefix_tiles * cache.kv_heads * plan.shares + (int64_t)a.shares * cache.kv_heads * a.chunks * cache.batch;
+    hipLaunchKernelGGL((cache8_decode_kernel<D, true>), dim3((unsigned)items), dim3(64 * kDecodeWaves), 0, st, a);
     SQAP_HIP_CHECK(hipGetLastError());
     if (!plan.few) {
         const sqap_status s = launch_prefix<D>(plan, PrefixTile{a.q_out, (int64_t)a.H * D, nullptr, nullptr, cache.batch, 1, a.H}, prefix, a.parts, st);

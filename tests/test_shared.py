@@ -27,7 +27,7 @@ def test_prompt_refusals():
                 dict(prefix=_desc(batch=0)), dict(prefix=_desc(kv_heads=4)), dict(prefix=_desc(kv_heads=1)), dict(prefix=_desc(head_dim=128)),
                 dict(prefix=_desc(codes=None)), dict(prefix=_desc(capacity=70))):
         assert call(**bad) == B.EINVAL, bad
-    for bad in (dict(Q=ODD), dict(O=ODD), dict(ldo=260), dict(cache=_desc(batch=13108)), dict(prefix=_desc(tail=4104)), dict(cache=_desc(head_dim=96)),
+    for bad in (dict(Q=ODD), dict(O=ODD), dict(ldo=260), dict(cache=_desc(batch=4096)), dict(prefix=_desc(tail=4104)), dict(cache=_desc(head_dim=96)),
                 dict(rows=2 ** 31 - 1, max_new=2 ** 30)):
         assert call(**bad) == B.EUNSUPPORTED, bad
     assert call(rows=0, Q=None) == B.OK and call(cache=_desc(batch=0), starts=None) == B.OK
@@ -43,7 +43,7 @@ def test_decode_refusals():
                 dict(QKV=None), dict(pos=None), dict(past=None), dict(O=None), dict(ld=504), dict(ldo=248), dict(ws=None), dict(bytes=need - 1), dict(ws=ODD),
                 dict(cache=_desc(batch=5)), dict(prefix=_desc(kv_heads=1)), dict(prefix=_desc(head_dim=128))):
         assert call(**bad) == B.EINVAL, bad
-    for bad in (dict(QKV=ODD), dict(O=ODD), dict(cache=_desc(batch=13108)), dict(prefix=_desc(codes=4104))):
+    for bad in (dict(QKV=ODD), dict(O=ODD), dict(cache=_desc(batch=4096)), dict(prefix=_desc(codes=4104))):
         assert call(**bad) == B.EUNSUPPORTED, bad
     assert call(cache=_desc(batch=0), pos=None) == B.OK
 
