@@ -563,8 +563,8 @@ sqap_status sqap_cache8_read(const sqap_cache8 *cache, const int32_t *lengths, i
  * are replayed side by side need one each.
  *
  * As above a sequence with past[b] < 0 or without rows is skipped; one whose rows do not fit or are more than max_new gets outputs of NaN; so do
- * the sequences of a group of more than width * max_new rows in all, and of a prefix whose prefix_len is negative or beyond its capacity
- * (appended to they are all the same).  One whose starts do not lie in order, or outside those of its group's first and last, is skipped.
+ * the sequences of a group whose rows together are not within 0 .. rows or more than width * max_new, and of a prefix whose prefix_len is
+ * negative or beyond its capacity (appended to they are all the same).  One whose starts do not lie in order, or outside those of its group's first and last, is skipped.
  * EINVAL, EUNSUPPORTED: as above; EINVAL also for a cache of prefixes of other heads, a batch that is no multiple of theirs, longest_prefix < 0;
  * EUNSUPPORTED for more than 4095 sequences, rows of a group times H / kv_heads beyond 32 bits.
  */

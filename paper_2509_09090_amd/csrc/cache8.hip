@@ -169,6 +169,29 @@ __device__ __forceinline__ PrefixShare prefix_share(int length, int capacity, in
     return {min(share * each, blocks), min((share + 1) * each, blocks), (blocks + each - 1) / each};
 }
 
+// A sequence behind a prefix: `rows` says whether it has any that count, `fits` whether they are worked out (their outputs are NaN otherwise).
+struct Member {
+    Span sp;
+    bool rows, fits;
+    int length;
+};
+__device__ __forceinline__ Member member_of(const int32_t *starts, const int32_t *past, int b, int rows, int max_new, int capacity, int prefix_capacity, const Parts &parts)
+{
+    const int group = b / parts.width;
+    Member m = {Span{b, 1, past[b], true}, true, true, parts.length[group]};
+    if (starts) {
+        m.sp = span_of(starts, past, b, rows, max_new, capacity);
+        const int first = starts[group * parts.width], end = starts[(group + 1) * parts.width];
+        m.rows = m.sp.n > 0 && m.sp.row >= first && m.sp.row + m.sp.n <= end;        // (starts that are not in order: no rows)
+        m.fits = m.sp.fits && group_rows(starts, group, parts.width, rows, max_new).n > 0;
+    } else {
+        m.rows = m.sp.past >= 0;
+        m.fits = m.sp.past < capacity;
+    }
+    m.fits = m.fits && m.length >= 0 && m.length <= prefix_capacity;
+    return m;
+}
+
 // ---------------------------------------------------------------- append
 
 // Where the code of column x and place `at` (of 64) lies in the values' half of a block; in LDS the four 16-byte pieces of a column are moved
@@ -431,6 +454,222 @@ __device__ __forceinline__ void nan_rows(__half *O, int64_t ldo, int first, int6
         }
 }
 
+// A block of keys and values in LDS, as halves in the order of the products' operands: keys [2][D / 16] KiB, values [D / 32][4] KiB.  kraw, vraw: the
+// pieces of a thread of T, as the cache has them.
+template <int D, int T>
+__device__ __forceinline__ void keep_codes(uint8_t *kt, const v4i *kraw, const v4i *vraw)
+{
+    constexpr int NP = D / 16, COUNT = kBlock * D / 16, PIECES = (COUNT + T - 1) / T;
+    uint8_t *vt = kt + kBlock * D * 2;
+    const int t = threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int u = t + T * i, r = u & 15, g = (u >> 4) & 3, x = u >> 6;
+        if (COUNT % T != 0 && u >= COUNT) break;
+        // keys: piece x = (T, c): position 16 T + r, columns 64 c + 16 g ..
+        const int tk = x / (D / 64), m = (x % (D / 64)) * 4 + g, row = 16 * (tk & 1) + r;
+        uint8_t *to = kt + (((tk >> 1) * NP + m) * 64 + row) * 16;
+        *reinterpret_cast<v8h *>(to) = halves_of(kraw[i][0], kraw[i][1]);
+        *reinterpret_cast<v8h *>(to + 512) = halves_of(kraw[i][2], kraw[i][3]);
+        // values: piece x: column 16 x + r, four positions per word
+        const int col = 16 * x + r;
+        uint8_t *vo = vt + ((col >> 5) * 4 * 64 + (g & 1) * 32 + (col & 31)) * 16 + (g >> 1) * 8;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) *reinterpret_cast<v4h *>(vo + n * 1024) = halves_of(vraw[i][n]);
+    }
+}
+// The same of an unfinished block; says whether there are values among this thread's that are not finite (they come back at the end, to the rows
+// that see them).
+template <int D, int T>
+__device__ __forceinline__ bool keep_tail(uint8_t *kt, const __half *tail_k, const __half *tail_v, int tail_rows)
+{
+    constexpr int NP = D / 16;
+    uint8_t *vt = kt + kBlock * D * 2;
+    bool odd = false;
+    for (int u = threadIdx.x; u < kBlock * D / 8; u += T) {
+        const int s = u / (D / 8), x = (u % (D / 8)) * 8;
+        v8h k = {}, v = {};
+        if (s < tail_rows) {
+            k = *reinterpret_cast<const v8h *>(tail_k + s * D + x);
+            v = *reinterpret_cast<const v8h *>(tail_v + s * D + x);
+        }
+        *reinterpret_cast<v8h *>(kt + (((s >> 5) * NP + (x >> 4)) * 64 + ((x >> 3) & 1) * 32 + (s & 31)) * 16) = k;
+        const int n = s >> 4, o = s & 15;                             // 8 q + 4 h + i of its sixteen positions
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int col = x + e;
+            _Float16 w = v[e];
+            if (!(__builtin_fabsf((float)w) <= 65504.f)) {
+                w = (_Float16)0.f;
+                odd = true;
+            }
+            *reinterpret_cast<_Float16 *>(vt + (((col >> 5) * 4 + n) * 64 + ((o >> 2) & 1) * 32 + (col & 31)) * 16 + (o >> 3) * 8 + (o & 3) * 2) = w;
+        }
+    }
+    return odd;
+}
+
+// Sums of a wavefront's 32 rows: row l % 32, columns 32 ct + 8 a + 4 (l / 32) ...  ALONE: all that the rows see passes through here, so that a row without
+// a score above minus infinity is 0 / 0; otherwise it adds nothing to what others have.
+template <int D, bool ALONE>
+struct TileSums {
+    static constexpr int NP = D / 16, CT = D / 32;
+    v16f ot[CT];
+    float mrun = -INFINITY, lrun = 0.f;
+    Unit unit;
+    __device__ __forceinline__ TileSums()
+    {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) ot[ct][i] = 0.f;
+    }
+    // kt: a block in LDS; sk: the keys' scale times log2(e) / sqrt(d); masked: some row does not see some position, this lane's sees 0 .. last.
+    __device__ __forceinline__ void add(const uint8_t *kt, const v8h (&qf)[NP], float sk, float sv, bool masked, int last)
+    {
+        const int l = threadIdx.x & 63, h = l >> 5;
+        const uint8_t *vt = kt + kBlock * D * 2 + l * 16;
+        kt += l * 16;
+        v16f s[2];
+        __builtin_amdgcn_s_setprio(1);                                // (before the other workgroup's exponentials: 3 in 100; not for the values' products)
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[tt][i] = 0.f;
+#pragma unroll
+            for (int m = 0; m < NP; ++m)
+                s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const v8h *>(kt + (tt * NP + m) * 1024), qf[m], s[tt], 0, 0, 0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+        if (masked) {
+            last -= 4 * h;
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (32 * tt + 8 * (i >> 2) + (i & 3) > last) s[tt][i] = -INFINITY;
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[tt][i]);
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (top > -INFINITY) top *= sk;                               // (nothing seen: it stays, whatever the scale)
+        float change;
+        const float factor = unit.enter(sv, change);
+        if (top - mrun > kRaiseBy) {                                  // (a row that sees nothing of the block keeps its maximum)
+            const float raise = exp2f(mrun - top);
+            change *= raise;
+            lrun *= raise;
+            mrun = top;
+        }
+        if (__any(change != 1.f)) {
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) ot[ct][i] *= change;
+        }
+        const float taken = !ALONE && mrun == -INFINITY ? 0.f : mrun;
+        float by = sk, from = __log2f(factor) + kLift;
+        const bool bad = !(sk >= 0.f && sv >= 0.f);                   // keys or values that are NaN as a whole: for the rows that see any of them
+        if (bad || __any(fabsf(top) > kLargeScore && top > -INFINITY)) {            // (a masked score times NaN would be NaN, too)
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    float w = bad ? NAN : s[tt][i] * sk;
+                    asm volatile("" : "+v"(w));                       // (rounded)
+                    s[tt][i] = s[tt][i] == -INFINITY ? -INFINITY : w - taken;
+                }
+            by = 1.f;
+        } else {
+            from -= taken;
+        }
+        float sum = 0.f;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {                                 // 16 positions at a time: all at once would not leave the registers
+            v8h p, rest, v[CT];
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                const float s0 = s[n >> 1][(n & 1) * 8 + i], s1 = s[n >> 1][(n & 1) * 8 + i + 1];
+                const float e0 = __builtin_amdgcn_exp2f(fmaf(s0, by, from)), e1 = __builtin_amdgcn_exp2f(fmaf(s1, by, from));
+                sum += e0;
+                sum += e1;
+                v2h high, low;
+                two_halves(e0, e1, high, low);
+                p[i] = high[0];
+                p[i + 1] = high[1];
+                rest[i] = low[0];
+                rest[i + 1] = low[1];
+            }
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) v[ct] = *reinterpret_cast<const v8h *>(vt + (ct * 4 + n) * 1024);
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) ot[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[ct], p, ot[ct], 0, 0, 0);
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) ot[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[ct], rest, ot[ct], 0, 0, 0);
+        }
+        lrun += sum * __builtin_amdgcn_rcpf(factor);
+    }
+    // a row's sums in units of one; the row, divided by its sum
+    __device__ __forceinline__ void write_part(float2 *ml, float *o) const
+    {
+        const int h = (threadIdx.x & 63) >> 5;
+        if (h == 0) *ml = {mrun, lrun};
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                v4f x;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = ot[ct][4 * a + i] * unit.unit;
+                *reinterpret_cast<v4f *>(o + 32 * ct + 8 * a + 4 * h) = x;
+            }
+    }
+    __device__ __forceinline__ void write_rows(__half *to) const
+    {
+        const int h = (threadIdx.x & 63) >> 5;
+        const float norm = unit.unit / lrun;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                union { __half h[4]; v2u v; } u;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) u.h[i] = __float2half_rn(ot[ct][4 * a + i] * norm);
+                *reinterpret_cast<v2u *>(to + 32 * ct + 8 * a + 4 * h) = u.v;
+            }
+    }
+};
+// infinities and NaN among the first `seen` rows of an unfinished block's values, to what a lane has written of its row
+template <int D, typename X, typename Get, typename Set>
+__device__ __forceinline__ void add_odd(X *to, const __half *tail_v, int seen, Get get, Set set)
+{
+    const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll 1
+    for (int x = 0; x < D / 2; ++x) {
+        const int col = (x >> 2) * 8 + 4 * h + (x & 3);
+        float o = get(to[col]);
+#pragma unroll 1
+        for (int s = 0; s < seen; ++s) {
+            const float v = __half2float(tail_v[s * D + col]);
+            if (!(fabsf(v) <= 65504.f)) o += v;
+        }
+        to[col] = set(o);
+    }
+}
+template <int D>
+__device__ __forceinline__ void add_odd(float *to, const __half *tail_v, int seen)
+{
+    add_odd<D>(to, tail_v, seen, [](float x) { return x; }, [](float x) { return x; });
+}
+template <int D>
+__device__ __forceinline__ void add_odd(__half *to, const __half *tail_v, int seen)
+{
+    add_odd<D>(to, tail_v, seen, [](__half x) { return __half2float(x); }, [](float x) { return __float2half_rn(x); });
+}
+
 // Rows are (query, head) pairs of the heads that share a key head, query first, 32 to a wavefront and WAVES wavefronts to a workgroup, so
 // that a block of keys and values is taken from memory and made halves once for all of them.  Everything is transposed (scores:
 // positions x rows), as in attention.hip: probabilities are the second product's operand where they were computed.
@@ -449,7 +688,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
                                                                          const Cache8View cache, __half *__restrict__ O, int64_t ldo, int tiles,
                                                                          const Parts parts)
 {
-    constexpr int T = 64 * WAVES, TILE = 32 * WAVES, NP = D / 16, CT = D / 32, BUF = 2 * kBlock * D * 2, COUNT = kBlock * D / 16;
+    constexpr int T = 64 * WAVES, TILE = 32 * WAVES, NP = D / 16, BUF = 2 * kBlock * D * 2, COUNT = kBlock * D / 16;
     constexpr int PIECES = (COUNT + T - 1) / T;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];     // two buffers: keys [2][NP] KiB, values [CT][4] KiB
     __shared__ int not_finite;
@@ -518,56 +757,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
     };
     auto keep = [&](int j) {
         if (j >= n_blocks) return;
-        uint8_t *kt = lds + (j & 1) * BUF, *vt = kt + kBlock * D * 2;
-        if (j != tail_block) {
-#pragma unroll
-            for (int i = 0; i < PIECES; ++i) {
-                const int u = t + T * i, r = u & 15, g = (u >> 4) & 3, x = u >> 6;
-                if (COUNT % T != 0 && u >= COUNT) break;
-                // keys: piece x = (T, c): position 16 T + r, columns 64 c + 16 g ..
-                const int tk = x / (D / 64), m = (x % (D / 64)) * 4 + g, row = 16 * (tk & 1) + r;
-                uint8_t *to = kt + (((tk >> 1) * NP + m) * 64 + row) * 16;
-                *reinterpret_cast<v8h *>(to) = halves_of(kraw[i][0], kraw[i][1]);
-                *reinterpret_cast<v8h *>(to + 512) = halves_of(kraw[i][2], kraw[i][3]);
-                // values: piece x: column 16 x + r, four positions per word
-                const int col = 16 * x + r;
-                uint8_t *vo = vt + ((col >> 5) * 4 * 64 + (g & 1) * 32 + (col & 31)) * 16 + (g >> 1) * 8;
-#pragma unroll
-                for (int n = 0; n < 4; ++n) *reinterpret_cast<v4h *>(vo + n * 1024) = halves_of(vraw[i][n]);
-            }
-            return;
-        }
-        bool odd = false;
-        for (int u = t; u < kBlock * D / 8; u += T) {
-            const int s = u / (D / 8), x = (u % (D / 8)) * 8;
-            v8h k = {}, v = {};
-            if (s < tail_rows) {
-                k = *reinterpret_cast<const v8h *>(tail_k + s * D + x);
-                v = *reinterpret_cast<const v8h *>(tail_v + s * D + x);
-            }
-            *reinterpret_cast<v8h *>(kt + (((s >> 5) * NP + (x >> 4)) * 64 + ((x >> 3) & 1) * 32 + (s & 31)) * 16) = k;
-            const int n = s >> 4, o = s & 15;                         // 8 q + 4 h + i of its sixteen positions
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int col = x + e;
-                _Float16 w = v[e];
-                if (!(__builtin_fabsf((float)w) <= 65504.f)) {        // comes back at the end, to the rows that see it
-                    w = (_Float16)0.f;
-                    odd = true;
-                }
-                *reinterpret_cast<_Float16 *>(vt + (((col >> 5) * 4 + n) * 64 + ((o >> 2) & 1) * 32 + (col & 31)) * 16 + (o >> 3) * 8 + (o & 3) * 2) = w;
-            }
-        }
-        if (odd) not_finite = 1;
+        uint8_t *kt = lds + (j & 1) * BUF;
+        if (j != tail_block) keep_codes<D, T>(kt, kraw, vraw);
+        else if (keep_tail<D, T>(kt, tail_k, tail_v, tail_rows)) not_finite = 1;
     };
 
-    v16f ot[CT];
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) ot[ct][i] = 0.f;
-    float mrun = -INFINITY, lrun = 0.f;
-    Unit unit;
+    TileSums<D, PART == Part::Whole> sums;
     const float per_d = kLog2e / sqrtf((float)D);
     const int wave_last = PART == Part::Prefix ? tile_last : sp.past + min(tile + wave * 32 + 31, n_rows - 1) / G;
     const int wave_first = PART == Part::Prefix ? tile_last : sp.past + min(tile + wave * 32, n_rows - 1) / G;
@@ -582,148 +777,240 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
         const float sk = j == tail_block || sc.x == 0.f ? per_d : sc.x * per_d, sv = j == tail_block ? 1.f : sc.y;
         if (j + 1 < n_blocks && j + 1 != tail_block) sc = *reinterpret_cast<const float2 *>(scales + 2 * (j + 1));
         lds_barrier();
-        if (j * kBlock <= wave_last) {
-            const uint8_t *kt = lds + (j & 1) * BUF + l * 16, *vt = kt + kBlock * D * 2;
-            v16f s[2];
-            __builtin_amdgcn_s_setprio(1);                            // (before the other workgroup's exponentials: 3 in 100; not for the values' products)
-#pragma unroll
-            for (int tt = 0; tt < 2; ++tt) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[tt][i] = 0.f;
-#pragma unroll
-                for (int m = 0; m < NP; ++m)
-                    s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const v8h *>(kt + (tt * NP + m) * 1024), qf[m], s[tt], 0, 0, 0);
-            }
-            __builtin_amdgcn_s_setprio(0);
-            if ((j + 1) * kBlock - 1 > wave_first) {                  // some row does not see some position
-                const int last = sees - j * kBlock - 4 * h;
-#pragma unroll
-                for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (32 * tt + 8 * (i >> 2) + (i & 3) > last) s[tt][i] = -INFINITY;
-            }
-            float top = -INFINITY;
-#pragma unroll
-            for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[tt][i]);
-            top = fmaxf(top, __shfl_xor(top, 32));
-            if (top > -INFINITY) top *= sk;                           // (nothing seen: it stays, whatever the scale)
-            float change;
-            const float factor = unit.enter(sv, change);
-            if (top - mrun > kRaiseBy) {                              // (a row that sees nothing of the block keeps its maximum)
-                const float raise = exp2f(mrun - top);
-                change *= raise;
-                lrun *= raise;
-                mrun = top;
-            }
-            if (__any(change != 1.f)) {
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) ot[ct][i] *= change;
-            }
-            // (a part without a score above minus infinity so far adds nothing; another may have some)
-            const float taken = PART != Part::Whole && mrun == -INFINITY ? 0.f : mrun;
-            float by = sk, from = __log2f(factor) + kLift;
-            const bool bad = !(sk >= 0.f && sv >= 0.f);               // keys or values that are NaN as a whole: for the rows that see any of them
-            if (bad || __any(fabsf(top) > kLargeScore && top > -INFINITY)) {        // (a masked score times NaN would be NaN, too)
-#pragma unroll
-                for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        float w = bad ? NAN : s[tt][i] * sk;
-                        asm volatile("" : "+v"(w));                   // (rounded)
-                        s[tt][i] = s[tt][i] == -INFINITY ? -INFINITY : w - taken;
-                    }
-                by = 1.f;
-            } else {
-                from -= taken;
-            }
-            float sum = 0.f;
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {                             // 16 positions at a time: all at once would not leave the registers
-                v8h p, rest, v[CT];
-#pragma unroll
-                for (int i = 0; i < 8; i += 2) {
-                    const float s0 = s[n >> 1][(n & 1) * 8 + i], s1 = s[n >> 1][(n & 1) * 8 + i + 1];
-                    const float e0 = __builtin_amdgcn_exp2f(fmaf(s0, by, from)), e1 = __builtin_amdgcn_exp2f(fmaf(s1, by, from));
-                    sum += e0;
-                    sum += e1;
-                    v2h high, low;
-                    two_halves(e0, e1, high, low);
-                    p[i] = high[0];
-                    p[i + 1] = high[1];
-                    rest[i] = low[0];
-                    rest[i + 1] = low[1];
-                }
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct) v[ct] = *reinterpret_cast<const v8h *>(vt + (ct * 4 + n) * 1024);
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct) ot[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[ct], p, ot[ct], 0, 0, 0);
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct) ot[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[ct], rest, ot[ct], 0, 0, 0);
-            }
-            lrun += sum * __builtin_amdgcn_rcpf(factor);
-        }
+        if (j * kBlock <= wave_last) sums.add(lds + (j & 1) * BUF, qf, sk, sv, (j + 1) * kBlock - 1 > wave_first, sees - j * kBlock);
         keep(j + 1);
     }
-    lrun += __shfl_xor(lrun, 32);
+    sums.lrun += __shfl_xor(sums.lrun, 32);
     const bool odd = n_blocks - 1 == tail_block && not_finite;
     if (mine >= n_rows) return;
     if constexpr (PART != Part::Whole) {
         const int64_t pair = part * parts.pairs + (int64_t)(sp.row + query) * H + head;
-        if (h == 0) parts.ml[pair] = {mrun, lrun};
-        float *sums = parts.o + pair * D;
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-            for (int a = 0; a < 4; ++a) {
-                v4f x;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = ot[ct][4 * a + i] * unit.unit;
-                *reinterpret_cast<v4f *>(sums + 32 * ct + 8 * a + 4 * h) = x;
-            }
-        if (odd) {                                                    // (as below)
-#pragma unroll 1
-            for (int x = 0; x < D / 2; ++x) {
-                const int col = (x >> 2) * 8 + 4 * h + (x & 3);
-                float o = sums[col];
-#pragma unroll 1
-                for (int s = 0; s <= sees - tail_block * kBlock; ++s) {
-                    const float v = __half2float(tail_v[s * D + col]);
-                    if (!(fabsf(v) <= 65504.f)) o += v;
-                }
-                sums[col] = o;
-            }
-        }
+        sums.write_part(parts.ml + pair, parts.o + pair * D);
+        if (odd) add_odd<D>(parts.o + pair * D, tail_v, sees - tail_block * kBlock + 1);
         return;
     }
-    const float norm = unit.unit / lrun;
     __half *to = O + (int64_t)(sp.row + query) * ldo + (int64_t)head * D;
+    sums.write_rows(to);
+    if (odd) add_odd<D>(to, tail_v, sees - tail_block * kBlock + 1);
+}
+
+// ---------------------------------------------------------------- long prompts behind prefixes
+
+// Many rows to a sequence: tiles of 128 of one sequence pass over its prefix's blocks and then their own, and the blocks of all tiles together are
+// dealt out evenly, so that no compute unit ends early (2675 rows of 32 heads over 8 behind prefixes of 6000 and 2900: 300 us where whole tiles, or
+// equal shares of each, would take 430).  A tile inside a workgroup's range is finished there; of one over its ends, the workgroups leave their sums,
+// one at the beginning and one at the end of each range, and cache8_long_join_kernel adds them.  Ranges are counted in tiles as long as their
+// sequence's longest (a tile's real blocks, fewer where its rows see less, are parted in the same proportion).
+constexpr int kLongBatch = 1024, kLongParts = 32, kLongLeast = 4;
+struct LongSlot {                // what a workgroup's first range belongs to, where it is the rest of a tile
+    int b, kh, tile, first, count;       // the workgroup that begins the tile, how many have a share of it; count 0: none, or not its second
+    int pad[3];
+};
+struct LongArgs {
+    const __half *Q;
+    int64_t ldq;
+    const int32_t *starts, *past;
+    int rows, max_new, H;
+    Cache8View cache, prefix;
+    Parts parts;                 // (width and lengths)
+    __half *O;
+    int64_t ldo;
+    LongSlot *slots;             // [workgroups]
+    float2 *ml;                  // [workgroups][beginning, end][128]
+    float *o;                    // [workgroups][beginning, end][128][D]
+};
+// (read from LDS, but the same in all lanes: into scalar registers)
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x)
+{
+    return (int64_t)((u64)(unsigned)__builtin_amdgcn_readfirstlane((int)x) | (u64)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32);
+}
+__device__ __forceinline__ int blocks_up(int positions) { return (positions + kBlock - 1) / kBlock; }
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void cache8_long_kernel(const LongArgs a)
+{
+    constexpr int T = 256, TILE = 128, NP = D / 16, BUF = 2 * kBlock * D * 2, COUNT = kBlock * D / 16, PIECES = (COUNT + T - 1) / T;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];     // two buffers
+    __shared__ int64_t before[kLongBatch + 1];                        // blocks of the tiles of one key head in front of each sequence
+    __shared__ int64_t wave_sum_[4];
+    __shared__ int wave_most[4], not_finite[2];
+    const Cache8View &cache = a.cache, &prefix = a.prefix;
+    const int t = threadIdx.x, l = t & 63, wave = uniform(t >> 6), c = l & 31, h = l >> 5, G = a.H / cache.kv_heads, batch = cache.batch;
+    const int groups = gridDim.x, w = (int)(blockIdx.x & 7) * (groups / 8) + (int)(blockIdx.x >> 3);      // neighbours behind one L2
+    auto member = [&](int b) { return member_of(a.starts, a.past, b, a.rows, a.max_new, cache.blocks * kBlock, prefix.blocks * kBlock, a.parts); };
+    auto tiles_of = [&](const Member &m) { return (m.sp.n * G + TILE - 1) / TILE; };      // (the launch keeps max_new * G in 32 bits)
+    auto blocks_of_tile = [&](const Member &m) { return blocks_up(m.length) + blocks_up(m.sp.past + m.sp.n); };
+    {
+        constexpr int EACH = kLongBatch / T;
+        int64_t mine[EACH], sum = 0;
+        int most = 0;
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-        for (int a = 0; a < 4; ++a) {
-            const int col = 32 * ct + 8 * a + 4 * h;
-            union { __half h[4]; v2u v; } u;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) u.h[i] = __float2half_rn(ot[ct][4 * a + i] * norm);
-            *reinterpret_cast<v2u *>(to + col) = u.v;
-        }
-    if (odd) {                                                        // infinities and NaN among the tail's values that this row sees
-#pragma unroll 1
-        for (int x = 0; x < D / 2; ++x) {
-            const int col = (x >> 2) * 8 + 4 * h + (x & 3);
-            float o = __half2float(to[col]);
-#pragma unroll 1
-            for (int s = 0; s <= sees - tail_block * kBlock; ++s) {
-                const float v = __half2float(tail_v[s * D + col]);
-                if (!(fabsf(v) <= 65504.f)) o += v;
+        for (int i = 0; i < EACH; ++i) {
+            const int b = t * EACH + i;
+            mine[i] = sum;
+            if (b >= batch) continue;
+            const Member m = member(b);
+            if (m.rows && m.fits) {
+                sum += (int64_t)tiles_of(m) * blocks_of_tile(m);
+                most = max(most, blocks_of_tile(m));
             }
-            to[col] = __float2half_rn(o);
         }
+        int64_t upto = sum;
+#pragma unroll
+        for (int i = 1; i < 64; i <<= 1) {
+            const int64_t x = __shfl_up(upto, i);
+            if (l >= i) upto += x;
+            most = max(most, __shfl_xor(most, i));
+        }
+        if (l == 63) wave_sum_[wave] = upto, wave_most[wave] = most;
+        __syncthreads();
+        upto -= sum;
+        for (int i = 0; i < wave; ++i) upto += wave_sum_[i];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) before[t * EACH + i] = upto + mine[i];
+        if (t == T - 1) before[kLongBatch] = upto + sum;
+        __syncthreads();
+    }
+    const int64_t of_head = uniform(before[kLongBatch]), total = of_head * cache.kv_heads;
+    const int most = uniform(max(max(wave_most[0], wave_most[1]), max(wave_most[2], wave_most[3])));
+    const int64_t range = max(max((total + groups - 1) / groups, (int64_t)(most + kLongParts - 1) / kLongParts), (int64_t)kLongLeast);
+    for (int b = w; b < batch; b += groups) {                         // sequences that do not fit
+        const Member m = member(b);
+        if (!m.rows || m.fits) continue;
+        for (int64_t u = t; u < (int64_t)m.sp.n * a.H * D; u += T) a.O[(m.sp.row + u / (a.H * D)) * a.ldo + u % (a.H * D)] = __ushort_as_half(0x7e00);
+    }
+    LongSlot slot = {0, 0, 0, 0, 0, {0, 0, 0}};
+    const int64_t stop = min((w + 1) * range, total);
+    const float per_d = kLog2e / sqrtf((float)D);
+    for (int64_t u = w * range; u < stop;) {
+        const int kh = (int)(u / of_head);
+        const int64_t at = u % of_head;
+        int b = 0;
+        for (int step = kLongBatch / 2; step > 0; step /= 2)
+            if (before[b + step] <= at) b += step;
+        b = uniform(b);                                               // (the last that begins there: those without tiles lie before it)
+        const Member m = member(b);
+        const Span &sp = m.sp;
+        const int64_t in_sequence = at - uniform(before[b]);
+        const int nominal = blocks_of_tile(m), tile_number = (int)(in_sequence / nominal), from = (int)(in_sequence - (int64_t)tile_number * nominal);
+        const int upto = (int)min((int64_t)nominal, from + (stop - u));
+        const int64_t tile_start = u - from;
+        u += upto - from;
+        const int n_rows = sp.n * G, tile = tile_number * TILE, tile_last = sp.past + (min(tile + TILE, n_rows) - 1) / G;
+        const int of_prefix = blocks_up(m.length), n_blocks = of_prefix + tile_last / kBlock + 1;
+        const int first = (int)((int64_t)from * n_blocks / nominal), end = (int)((int64_t)upto * n_blocks / nominal);
+        const int mine = tile + wave * 32 + c, mine_in = min(mine, n_rows - 1), query = mine_in / G, head = kh * G + mine_in % G;
+        const int sees = sp.past + query, wave_last = sp.past + min(tile + wave * 32 + 31, n_rows - 1) / G, wave_first = sp.past + min(tile + wave * 32, n_rows - 1) / G;
+        const int64_t prefix_head = (int64_t)(b / a.parts.width) * prefix.kv_heads + kh, own_head = (int64_t)b * cache.kv_heads + kh;
+        const __half *prefix_tail = prefix.tail + prefix_head * 2 * kBlock * D, *own_tail = cache.tail + own_head * 2 * kBlock * D;
+        const int prefix_rest = m.length % kBlock, own_unfinished = of_prefix + (sp.past + sp.n) / kBlock, own_rest = (sp.past + sp.n) % kBlock;
+        auto unfinished = [&](int j) { return j == own_unfinished || (j == of_prefix - 1 && prefix_rest > 0); };
+        v8h qf[NP];
+#pragma unroll
+        for (int i = 0; i < NP; ++i) qf[i] = *reinterpret_cast<const v8h *>(a.Q + (int64_t)(sp.row + query) * a.ldq + (int64_t)head * D + 16 * i + 8 * h);
+        v4i kraw[PIECES], vraw[PIECES];
+        float2 sc = {0.f, 0.f};
+        auto fetch = [&](int j) {
+            if (j >= end || unfinished(j)) return;
+            const bool in_prefix = j < of_prefix;
+            const int8_t *codes = in_prefix ? block_codes<D>(prefix, prefix_head, j, 0) : block_codes<D>(cache, own_head, j - of_prefix, 0);
+            const v4i *k = reinterpret_cast<const v4i *>(codes), *v = reinterpret_cast<const v4i *>(codes + kBlock * D);
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const int x = t + T * i;
+                if (COUNT % T != 0 && x >= COUNT) break;
+                kraw[i] = k[x];
+                vraw[i] = v[x];
+            }
+        };
+        auto scale_of_block = [&](int j) {
+            if (j >= end || unfinished(j)) return;
+            sc = *reinterpret_cast<const float2 *>(j < of_prefix ? prefix.scales + (prefix_head * prefix.blocks + j) * 2 : cache.scales + (own_head * cache.blocks + j - of_prefix) * 2);
+        };
+        auto keep = [&](int j) {
+            if (j >= end) return;
+            uint8_t *kt = lds + (j & 1) * BUF;
+            if (!unfinished(j)) {
+                keep_codes<D, T>(kt, kraw, vraw);
+                return;
+            }
+            const bool in_prefix = j < of_prefix;
+            const __half *tail = in_prefix ? prefix_tail : own_tail;
+            if (keep_tail<D, T>(kt, tail, tail + kBlock * D, in_prefix ? prefix_rest : own_rest)) not_finite[in_prefix ? 0 : 1] = 1;
+        };
+        TileSums<D, false> sums;
+        __syncthreads();                                              // (the tile before has been read, and its flags)
+        if (t < 2) not_finite[t] = 0;
+        __syncthreads();
+        fetch(first);
+        keep(first);
+        scale_of_block(first);
+        for (int j = first; j < end; ++j) {
+            fetch(j + 1);
+            const bool as_it_is = unfinished(j);
+            const float sk = as_it_is || sc.x == 0.f ? per_d : sc.x * per_d, sv = as_it_is ? 1.f : sc.y;
+            scale_of_block(j + 1);
+            lds_barrier();
+            const int at_own = (j - of_prefix) * kBlock;              // (the prefix: all of its positions)
+            if (at_own <= wave_last)
+                sums.add(lds + (j & 1) * BUF, qf, sk, sv, at_own < 0 ? as_it_is : at_own + kBlock - 1 > wave_first, at_own < 0 ? prefix_rest - 1 : sees - at_own);
+            keep(j + 1);
+        }
+        sums.lrun += __shfl_xor(sums.lrun, 32);
+        __syncthreads();
+        const bool odd_prefix = not_finite[0], odd_own = not_finite[1];      // (of blocks in this range)
+        const bool whole = from == 0 && upto == nominal;
+        if (from > 0) {
+            const int begun = (int)(tile_start / range), ended = (int)((tile_start + nominal - 1) / range);
+            if (begun == w - 1) slot = {b, kh, tile, begun, ended - begun + 1, {0, 0, 0}};
+        }
+        if (mine >= n_rows) continue;
+        const int odd_rows = odd_own ? sees - (own_unfinished - of_prefix) * kBlock + 1 : 0;
+        if (whole) {
+            __half *to = a.O + (int64_t)(sp.row + query) * a.ldo + (int64_t)head * D;
+            sums.write_rows(to);
+            if (odd_prefix) add_odd<D>(to, prefix_tail + kBlock * D, prefix_rest);
+            if (odd_own) add_odd<D>(to, own_tail + kBlock * D, odd_rows);
+        } else {
+            const int64_t place = ((int64_t)w * 2 + (from > 0 ? 0 : 1)) * TILE + wave * 32 + c;
+            sums.write_part(a.ml + place, a.o + place * D);
+            if (odd_prefix) add_odd<D>(a.o + place * D, prefix_tail + kBlock * D, prefix_rest);
+            if (odd_own) add_odd<D>(a.o + place * D, own_tail + kBlock * D, odd_rows);
+        }
+    }
+    if (t == 0) a.slots[w] = slot;
+}
+
+// The shares of a tile that begins in one workgroup's range and ends in another's: two workgroups for each boundary that is a tile's first.
+template <int D>
+__global__ __launch_bounds__(256) void cache8_long_join_kernel(const LongArgs a)
+{
+    constexpr int LANES = D / 4, EACH = 256 / LANES, ROWS = 64;
+    const int w = blockIdx.y, t = threadIdx.x, lane = t % LANES, G = a.H / a.cache.kv_heads;
+    const LongSlot slot = a.slots[w];
+    if (slot.count == 0) return;
+    const Span sp = span_of(a.starts, a.past, slot.b, a.rows, a.max_new, a.cache.blocks * kBlock);
+    auto place_of = [&](int i, int row) { return ((int64_t)(slot.first + i) * 2 + (i == 0 ? 1 : 0)) * 128 + row; };
+    for (int row = (int)blockIdx.x * ROWS + t / LANES; row < ((int)blockIdx.x + 1) * ROWS; row += EACH) {
+        const int pair = slot.tile + row;
+        if (pair >= sp.n * G) return;
+        float top = -INFINITY, sum = 0.f;
+        for (int i = 0; i < slot.count; ++i) top = fmaxf(top, a.ml[place_of(i, row)].x);
+        v4f o = {0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < slot.count; ++i) {
+            const float2 ml = a.ml[place_of(i, row)];
+            const v4f x = *reinterpret_cast<const v4f *>(a.o + place_of(i, row) * D + lane * 4);
+            const float f = exp2f(ml.x - top);                        // (no score above minus infinity anywhere: 0 / 0)
+            sum += f * ml.y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += fabsf(x[e]) < INFINITY ? f * x[e] : x[e];          // (an infinite value stays one however small its weight)
+        }
+        const float norm = 1.f / sum;
+        union { __half h[4]; v2u v; } out;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out.h[e] = __float2half_rn(o[e] * norm);
+        *reinterpret_cast<v2u *>(a.O + (int64_t)(sp.row + pair / G) * a.ldo + (int64_t)(slot.kh * G + pair % G) * D + lane * 4) = out.v;
     }
 }
 
@@ -1086,6 +1373,19 @@ __device__ __forceinline__ void prefix_tile(DecodeLds<D> &lds, const PrefixTile 
 #pragma unroll
         for (int i = 0; i < DT; ++i) vraw[i] = v[i * 64];
     };
+    constexpr int UNITS = kBlock * D / 8 / T;                         // 8 columns of a row of the tail each
+    v4i tk[UNITS], tv[UNITS];
+    if (has_tail) {
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            const int u = t + i * T, s = u / (D / 8), x = (u % (D / 8)) * 8;
+            tk[i] = tv[i] = v4i{0, 0, 0, 0};
+            if (s < tail_rows) {
+                tk[i] = *reinterpret_cast<const v4i *>(tail_k + s * D + x);
+                tv[i] = *reinterpret_cast<const v4i *>(tail_v + s * D + x);
+            }
+        }
+    }
     fetch_keys(own.first + wave);
     fetch_values(own.first + wave);
     v8h qf[2 * C];
@@ -1130,17 +1430,13 @@ __device__ __forceinline__ void prefix_tile(DecodeLds<D> &lds, const PrefixTile 
         if (t == 0) lds.arrived = 0;                                  // values that are not finite: come back at the end
         __syncthreads();
         bool odd = false;
-        for (int u = t; u < kBlock * D / 8; u += T) {
-            const int s = u / (D / 8), x = (u % (D / 8)) * 8, at = value_slot(s);
-            v4i k = {0, 0, 0, 0}, v = k;
-            if (s < tail_rows) {
-                k = *reinterpret_cast<const v4i *>(tail_k + s * D + x);
-                v = *reinterpret_cast<const v4i *>(tail_v + s * D + x);
-            }
-            *reinterpret_cast<v4i *>(&lds.u.tail.k[s][x]) = k;
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            const int u = t + i * T, s = u / (D / 8), x = (u % (D / 8)) * 8, at = value_slot(s);
+            *reinterpret_cast<v4i *>(&lds.u.tail.k[s][x]) = tk[i];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                unsigned short w = (unsigned short)((unsigned)v[e >> 1] >> (16 * (e & 1)));
+                unsigned short w = (unsigned short)((unsigned)tv[i][e >> 1] >> (16 * (e & 1)));
                 if ((w & 0x7fffu) >= 0x7c00u) w = 0, odd = true;
                 lds.u.tail.v[x + e][value_place(x, at)] = w;
             }
@@ -1149,24 +1445,23 @@ __device__ __forceinline__ void prefix_tile(DecodeLds<D> &lds, const PrefixTile 
         __syncthreads();
     }
     WaveSums<D> sums;
-    for (int j = own.first + wave; j < own.end; j += kDecodeWaves) {
-        if (j != tail_block) {
-            const float2 scale = sc;
-            sums.add(
-                qf, scale.x, scale.y, false, 0,
-                [&](int T4, int m) {
-                    const v4i w = kraw[T4 * C + (m >> 1)];
-                    return (m & 1) ? halves_of(w[2], w[3]) : halves_of(w[0], w[1]);
-                },
-                [&](int i, int n) { return halves_of(vraw[i][2 * n], vraw[i][2 * n + 1]); }, [&] { fetch_keys(j + kDecodeWaves); });
-            fetch_values(j + kDecodeWaves);
-        } else {
-            sums.add(
-                qf, 1.f, 1.f, true, tail_rows - 1,
-                [&](int T4, int m) { return *reinterpret_cast<const v8h *>(&lds.u.tail.k[16 * T4 + r][64 * (m >> 1) + 16 * g + 8 * (m & 1)]); },
-                [&](int i, int n) { return *reinterpret_cast<const v8h *>(&lds.u.tail.v[16 * i + r][value_place(16 * i + r, 32 * n + 8 * g)]); }, [] {});
-        }
+    int j = own.first + wave;
+    for (; j < own.end && j < tail_block; j += kDecodeWaves) {        // (the unfinished block behind the loop: inside it would cost 85 registers)
+        const float2 scale = sc;
+        sums.add(
+            qf, scale.x, scale.y, false, 0,
+            [&](int T4, int m) {
+                const v4i w = kraw[T4 * C + (m >> 1)];
+                return (m & 1) ? halves_of(w[2], w[3]) : halves_of(w[0], w[1]);
+            },
+            [&](int i, int n) { return halves_of(vraw[i][2 * n], vraw[i][2 * n + 1]); }, [&] { fetch_keys(j + kDecodeWaves); });
+        fetch_values(j + kDecodeWaves);
     }
+    if (j < own.end)
+        sums.add(
+            qf, 1.f, 1.f, true, tail_rows - 1,
+            [&](int T4, int m) { return *reinterpret_cast<const v8h *>(&lds.u.tail.k[16 * T4 + r][64 * (m >> 1) + 16 * g + 8 * (m & 1)]); },
+            [&](int i, int n) { return *reinterpret_cast<const v8h *>(&lds.u.tail.v[16 * i + r][value_place(16 * i + r, 32 * n + 8 * g)]); }, [] {});
     sums.l += __shfl_xor(sums.l, 16);
     sums.l += __shfl_xor(sums.l, 32);
     const bool odd = has_tail && lds.arrived;
@@ -1213,9 +1508,10 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void cache8_prefix_kernel(con
     prefix_tile<D, false>(lds, a, prefix, parts, RopeFreq{}, blockIdx.z / tiles, blockIdx.y, blockIdx.z % tiles, blockIdx.x);
 }
 
-// SHARED: the own positions of sequences that share a prefix, and in the workgroups behind them (where there are any) the prefix; all of them leave parts.
+// SHARED: the own positions of sequences that share a prefix, and in the workgroups in front of them (where there are any) the prefix; all of them leave parts.
+// Three workgroups to a compute unit (4 x 32 rows of 32 heads over 8 behind 1000 positions 26 us, with two 32).
 template <int D, bool SHARED>
-__global__ __launch_bounds__(64 * kDecodeWaves, 2) void cache8_decode_kernel(const DecodeArgs a)
+__global__ __launch_bounds__(64 * kDecodeWaves, SHARED ? 3 : 2) void cache8_decode_kernel(const DecodeArgs a)
 {
     constexpr int HALF = D / 2, C = D / 64, T = 64 * kDecodeWaves, DT = D / 16;
     __shared__ DecodeLds<D> lds;
@@ -1578,22 +1874,12 @@ __global__ __launch_bounds__(256) void cache8_join_kernel(const JoinArgs a)
 {
     constexpr int LANES = D / 4, EACH = 256 / LANES / SPLIT, KEPT = kMostParts / LANES;
     __shared__ __attribute__((aligned(16))) float sums[SPLIT > 1 ? SPLIT * EACH * D : 4];
-    const int b = blockIdx.y, t = threadIdx.x, lane = t % LANES, group = b / a.parts.width;
-    Span sp;
-    bool fits;
-    if (a.starts) {
-        sp = span_of(a.starts, a.past, b, a.rows, a.max_new, a.capacity);
-        const int first = a.starts[group * a.parts.width], end = a.starts[(group + 1) * a.parts.width];
-        if (sp.row < first || sp.row + sp.n > end) return;            // (starts that are not in order)
-        fits = sp.fits && group_rows(a.starts, group, a.parts.width, a.rows, a.max_new).n > 0;
-    } else {
-        sp = Span{b, 1, a.past[b], true};
-        if (sp.past < 0) return;
-        fits = sp.past < a.capacity;
-    }
-    const int length = a.parts.length[group];
-    const PrefixShare prefix = prefix_share(length, a.prefix_capacity, a.parts.prefix_shares, 0);
-    fits = fits && length >= 0 && length <= a.prefix_capacity;
+    const int b = blockIdx.y, t = threadIdx.x, lane = t % LANES;
+    const Member member = member_of(a.starts, a.past, b, a.rows, a.max_new, a.capacity, a.prefix_capacity, a.parts);
+    if (!member.rows) return;
+    const Span &sp = member.sp;
+    const bool fits = member.fits;
+    const PrefixShare prefix = prefix_share(member.length, a.prefix_capacity, a.parts.prefix_shares, 0);
     const int last = sp.past / kBlock, own_each = max(a.own_each, (last + a.own_shares) / a.own_shares);
     const int own = a.starts ? 1 : (last + own_each) / own_each, all = prefix.active + own;
     auto part_of = [&](int i) { return i < prefix.active ? i : a.parts.prefix_shares + i - prefix.active; };
@@ -1805,6 +2091,8 @@ sqap_status launch_cache8_decode(const __half *QKV, int64_t ld, const int32_t *p
 // 27 us, behind 20000 45 and 48, behind 100003 187 and 128; 64 behind 1000 23 and 29).
 constexpr int kFewPairs = 64, kFewPairsAtMost = 256, kFewBlocks = 20000, kPrefixGroups = 512, kMostPrefixShares = 64;
 struct SharedPlan {
+    bool together;               // long prompts: cache8_long_kernel
+    int groups;                  // its workgroups
     bool few;
     int64_t tiles;               // of a group and key head
     int shares, own_shares;
@@ -1823,6 +2111,15 @@ static SharedPlan shared_plan(int batch, int groups, int H, int kv_heads, int d,
     p.own_shares = own_shares;
     p.pairs = (int64_t)rows * H;
     const auto up = [](size_t n) { return (n + 15) / 16 * 16; };
+    // rows that fill three quarters of a tile on average
+    p.together = max_new > 1 && batch <= kLongBatch && (int64_t)rows * (H / kv_heads) >= (int64_t)batch * 96;
+    if (p.together) {
+        p.groups = std::max(8, device_cu_count() * 2 / 8 * 8);
+        p.ml = kCounterBytes + (size_t)p.groups * sizeof(LongSlot);
+        p.o = p.ml + (size_t)p.groups * 256 * sizeof(float2);
+        p.bytes = p.o + (size_t)p.groups * 256 * d * sizeof(float);
+        return p;
+    }
     p.q = kCounterBytes;                                              // (left alone, for calls that want it zero)
     p.ml = p.q + (max_new == 1 ? up((size_t)p.pairs * d * 2) : 0);
     p.o = p.ml + up((size_t)(p.shares + own_shares) * p.pairs * sizeof(float2));
@@ -1880,6 +2177,22 @@ static sqap_status launch_shared_d(const __half *Q, int64_t ldq, const int32_t *
                                    const Cache8View &prefix, const int32_t *length, int longest_prefix, __half *O, int64_t ldo, char *workspace, hipStream_t st)
 {
     const SharedPlan plan = shared_plan(cache.batch, prefix.batch, H, cache.kv_heads, D, rows, max_new, 1, longest_prefix);
+    if (plan.together) {
+        constexpr int LDS = 2 * 2 * kBlock * D * 2;
+        static std::atomic<bool> ready[kMaxDeviceSlots];
+        if (!ready[device_slot()].load(std::memory_order_relaxed)) {
+            SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(cache8_long_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+            ready[device_slot()].store(true, std::memory_order_relaxed);
+        }
+        const LongArgs a = {Q, ldq, starts, past, rows, max_new, H, cache, prefix, Parts{nullptr, nullptr, 0, 0, cache.batch / prefix.batch, length}, O, ldo,
+                            reinterpret_cast<LongSlot *>(workspace + kCounterBytes), reinterpret_cast<float2 *>(workspace + plan.ml),
+                            reinterpret_cast<float *>(workspace + plan.o)};
+        hipLaunchKernelGGL(cache8_long_kernel<D>, dim3(plan.groups), dim3(256), LDS, st, a);
+        SQAP_HIP_CHECK(hipGetLastError());
+        hipLaunchKernelGGL(cache8_long_join_kernel<D>, dim3(2, plan.groups), dim3(256), 0, st, a);
+        SQAP_HIP_CHECK(hipGetLastError());
+        return SQAP_OK;
+    }
     const Parts parts = {reinterpret_cast<float *>(workspace + plan.o), reinterpret_cast<float2 *>(workspace + plan.ml), plan.pairs, plan.shares,
                          cache.batch / prefix.batch, length};
     sqap_status s = launch_prefix<D>(plan, PrefixTile{Q, ldq, starts, nullptr, rows, max_new, H}, prefix, parts, st);

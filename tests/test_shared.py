@@ -286,3 +286,116 @@ def test_replayed_with_other_lengths(G, width):
         other, out = B.Cache8(2, 900, kv, d, device=G.DEV), t.zeros((2, H * d), dtype=t.float16, device=G.DEV)
         B.sqap_cache8_decode_attention(rows[:2], pos[:2], t.full((2,), 800, dtype=t.int32, device=G.DEV), other, H, out, ws, 900)
         assert int(ws[:KEPT].max()) == 0
+
+
+# ---- prompts long enough to be worked out together with their prefixes (three quarters of a tile of 128 pairs to a sequence, on average)
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("groups,width,H,kv,d,lengths,calls", [
+    (1, 1, 4, 2, 64, [100], [[300], [2]]),
+    (1, 2, 2, 2, 128, [0], [[96, 200], [130, 64]]),
+    (2, 3, 8, 2, 128, [700, 130], [[200, 33, 0, 129, 64, 301], [64, 0, 31, 127, 1, 64]]),
+    (3, 1, 6, 1, 64, [64, 0, 191], [[65, 100, 16], [1, 63, 128]]),
+    (1, 1, 4, 4, 128, [6000], [[130], [97]]),
+    (1, 3, 32, 1, 64, [3001], [[5, 40, 3], [9, 1, 2]]),
+    (1, 2, 20, 1, 128, [333], [[100, 77]]),
+    (4, 4, 4, 4, 64, [1, 2, 65, 900], [[100 + 10 * b for b in range(16)]]),
+])
+def test_long_prompts(G, groups, width, H, kv, d, lengths, calls):
+    s = Shared(G, groups, width, H, kv, d, lengths, capacity=640, seed=groups + 50)
+    for counts in calls:
+        s.prompt(counts, longest_prefix=0 if counts == calls[-1] else None)
+    s.own.check_contents()
+
+
+@pytest.mark.gpu
+def test_long_prompts_of_many_sequences(G):
+    """A whole thousand sequences in four groups, some without rows; one more than are worked out that way."""
+    for batch in (1024, 1028):
+        s = Shared(G, 4, batch // 4, 8, 1, 64, [70, 5, 0, 128], capacity=64, seed=60)
+        s.prompt([int(n) for n in s.own.rng.integers(8, 20, batch - 3)] + [0, 30, 0])
+
+
+@pytest.mark.gpu
+def test_long_prompts_with_infinite_values(G):
+    """As test_infinite_values_and_keys: in unfinished blocks of a prefix and of own positions, a block of keys without scale, scores of minus
+    infinity over a whole prefix."""
+    H, kv, d, lengths = 4, 2, 64, [70, 130, 1]
+    rows = np.random.default_rng(8).standard_normal((201, H + 2 * kv, d)).astype(np.float16)
+    rows[66, H + kv, 3] = np.inf
+    rows[69, H + kv, 3], rows[69, H + kv + 1, 7] = -np.inf, np.nan
+    rows[80, H + 1, 5] = np.inf
+    s = Shared(G, 3, 1, H, kv, d, lengths, capacity=512, seed=61, prefix_rows=rows)
+    s.prefix.cache.tail[2, :, 0, 0, 5] = -float("inf")
+    s.prefix.k[2][0, :, 5] = -np.inf
+    x = s.own.rows(330)
+    x[100, H + kv, 9] = np.inf                                        # (of 110 rows the last 46 are unfinished)
+    x[150, H + kv + 1, 2] = -np.inf                                   # in a block that is finished
+    x[329, H + kv + 1, 2] = np.nan
+    s.prompt([110, 110, 110], x=x)
+
+
+@pytest.mark.gpu
+def test_long_prompts_that_do_not_fit(G):
+    """NaN where there is no room, more rows than announced, more in a group than announced together or a length that cannot be; padded ones left alone."""
+    t, H, kv, d, width = __import__("torch"), 4, 1, 64, 2
+    s = Shared(G, 5, width, H, kv, d, [70, 20, 64, 9, 30], capacity=192, seed=62)
+    counts = [60, 40, 50, 45, 33, 70, 64, 64, 30, 90]
+    before = s.own.past.copy()
+    y = s.own.append(counts, pos=s.positions(counts), attend=False)
+    s.own.past = before
+    total = sum(counts)
+    q = G.to_dev(np.ascontiguousarray(y[:, :H]).reshape(total, -1))
+    at = np.concatenate([[0], np.cumsum(counts)])
+    starts = at.astype(np.int32)
+    for most, lengths, past, starts_, bad, left in (
+            (100, [70, 20, 64, 9, 30], {1: -1, 3: 160}, None, {3}, {1}),
+            (100, [70, -1, 64, 1000, 30], {}, None, {2, 3, 6, 7}, set()),
+            (69, [70, 20, 64, 9, 30], {}, None, {5, 9}, set()),
+            (59, [70, 20, 64, 9, 30], {}, None, {0, 5, 6, 7, 8, 9}, set()),
+            (100, [70, 20, 64, 9, 30], {}, {3: 700}, set(), {2, 3}),
+            (100, [70, 20, 64, 9, 30], {}, {4: -5}, {5}, {2, 3, 4})):
+        p = before.copy()
+        for b, n in past.items():
+            p[b] = n
+        st = starts.copy()
+        for b, n in (starts_ or {}).items():
+            st[b] = n
+        o = t.full((total, H * d), 9.0, dtype=t.float16, device=G.DEV)
+        B.sqap_cache8_shared_attention(q, G.to_dev(st), G.to_dev(p), s.own.cache, s.prefix.cache, G.to_dev(np.array(lengths, np.int32)), H, most, o,
+                                       s.workspace(total, most, 1, 70), 70)
+        got = o.cpu().numpy()
+        for b in range(10):
+            part = got[at[b]:at[b + 1]]
+            if b in bad:
+                assert np.all(np.isnan(part)), (most, b)
+            elif b in left:
+                assert np.all(part == 9), (most, b)
+        s.check(got, y, counts, skip=bad | left)
+
+
+@pytest.mark.gpu
+def test_long_prompts_replayed(G):
+    """A captured prompt call, replayed with other rows and lengths."""
+    t, H, kv, d, total = __import__("torch"), 4, 2, 128, 300
+    s = Shared(G, 2, 2, H, kv, d, [500, 64], capacity=1024, seed=63)
+    q, o = (t.zeros((total, H * d), dtype=t.float16, device=G.DEV) for _ in range(2))
+    starts, past = t.zeros((5,), dtype=t.int32, device=G.DEV), t.zeros((4,), dtype=t.int32, device=G.DEV)
+    ws = s.workspace(total, 200, 1, 500)
+    graph = t.cuda.CUDAGraph()
+    t.cuda.synchronize()
+    with t.cuda.graph(graph):
+        B.sqap_cache8_shared_attention(q, starts, past, s.own.cache, s.prefix.cache, s.device_lengths, H, 200, o, ws, 500)
+    for counts in ([100, 60, 70, 50], [200, 0, 1, 99], [3, 2, 1, 140]):
+        before, n = s.own.past.copy(), sum(counts)
+        y = s.own.append(counts, pos=s.positions(counts), attend=False)
+        q[:n] = G.to_dev(np.ascontiguousarray(y[:, :H]).reshape(n, -1))
+        starts.copy_(G.to_dev(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)))
+        past.copy_(G.to_dev(before))
+        o.fill_(9.0)
+        graph.replay()
+        t.cuda.synchronize()
+        after, s.own.past = s.own.past, before
+        s.check(o.cpu().numpy(), y, counts)
+        s.own.past = after
+        assert bool((o[n:] == 9).all())
