@@ -533,12 +533,23 @@ struct TileSums {
         v16f s[2];
         __builtin_amdgcn_s_setprio(1);                                // (before the other workgroup's exponentials: 3 in 100; not for the values' products)
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt) {
+        for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[tt][i] = 0.f;
+        // the two halves of the block in turn, keys AHEAD products before they enter (left to itself the compiler reads one and waits for it)
+        constexpr int AHEAD = 4;
+        v8h k[AHEAD];
 #pragma unroll
-            for (int m = 0; m < NP; ++m)
-                s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const v8h *>(kt + (tt * NP + m) * 1024), qf[m], s[tt], 0, 0, 0);
+        for (int i = 0; i < AHEAD; ++i) k[i] = *reinterpret_cast<const v8h *>(kt + ((i & 1) * NP + (i >> 1)) * 1024);
+        __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+        for (int i = 0; i < 2 * NP; ++i) {
+            s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[i % AHEAD], qf[i >> 1], s[i & 1], 0, 0, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if (i + AHEAD < 2 * NP) {
+                k[i % AHEAD] = *reinterpret_cast<const v8h *>(kt + (((i + AHEAD) & 1) * NP + ((i + AHEAD) >> 1)) * 1024);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
         }
         __builtin_amdgcn_s_setprio(0);
         if (masked) {
@@ -587,9 +598,12 @@ struct TileSums {
             from -= taken;
         }
         float sum = 0.f;
+        v8h p[2], rest[2], v[2][CT];
+        auto values = [&](int n) {
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {                                 // 16 positions at a time: all at once would not leave the registers
-            v8h p, rest, v[CT];
+            for (int ct = 0; ct < CT; ++ct) v[n & 1][ct] = *reinterpret_cast<const v8h *>(vt + (ct * 4 + n) * 1024);
+        };
+        auto powers = [&](int n) {
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
                 const float s0 = s[n >> 1][(n & 1) * 8 + i], s1 = s[n >> 1][(n & 1) * 8 + i + 1];
@@ -598,17 +612,25 @@ struct TileSums {
                 sum += e1;
                 v2h high, low;
                 two_halves(e0, e1, high, low);
-                p[i] = high[0];
-                p[i + 1] = high[1];
-                rest[i] = low[0];
-                rest[i + 1] = low[1];
+                p[n & 1][i] = high[0];
+                p[n & 1][i + 1] = high[1];
+                rest[n & 1][i] = low[0];
+                rest[n & 1][i + 1] = low[1];
             }
+        };
+        values(0);
+        __builtin_amdgcn_sched_barrier(0);
+        powers(0);
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) v[ct] = *reinterpret_cast<const v8h *>(vt + (ct * 4 + n) * 1024);
+        for (int n = 0; n < 4; ++n) {
+            if (n < 3) values(n + 1);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) ot[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[ct], p, ot[ct], 0, 0, 0);
+            for (int ct = 0; ct < CT; ++ct) ot[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[n & 1][ct], p[n & 1], ot[ct], 0, 0, 0);
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) ot[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[ct], rest, ot[ct], 0, 0, 0);
+            for (int ct = 0; ct < CT; ++ct) ot[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[n & 1][ct], rest[n & 1], ot[ct], 0, 0, 0);
+            if (n < 3) powers(n + 1);
+            __builtin_amdgcn_sched_barrier(0);
         }
         lrun += sum * __builtin_amdgcn_rcpf(factor);
     }
