@@ -865,6 +865,7 @@ static sqap_status check_prefix(const char *who, const sqap_cache8 *cache, const
 
 static sqap_status check_workspace(const char *who, const void *workspace, size_t bytes, size_t need)
 {
+    if (need == 0) return SQAP_OK;
     if (!workspace || bytes < need) return fail(SQAP_EINVAL, "%s: workspace of %zu bytes needed, %zu given", who, need, workspace ? bytes : (size_t)0);
     if (!aligned16(workspace)) return fail(SQAP_EINVAL, "%s: workspace must be 16-byte aligned", who);
     return SQAP_OK;

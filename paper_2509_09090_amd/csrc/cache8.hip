@@ -1014,24 +1014,43 @@ __global__ __launch_bounds__(256) void cache8_long_join_kernel(const LongArgs a)
     if (slot.count == 0) return;
     const Span sp = span_of(a.starts, a.past, slot.b, a.rows, a.max_new, a.cache.blocks * kBlock);
     auto place_of = [&](int i, int row) { return ((int64_t)(slot.first + i) * 2 + (i == 0 ? 1 : 0)) * 128 + row; };
-    for (int row = (int)blockIdx.x * ROWS + t / LANES; row < ((int)blockIdx.x + 1) * ROWS; row += EACH) {
-        const int pair = slot.tile + row;
-        if (pair >= sp.n * G) return;
-        float top = -INFINITY, sum = 0.f;
-        for (int i = 0; i < slot.count; ++i) top = fmaxf(top, a.ml[place_of(i, row)].x);
-        v4f o = {0.f, 0.f, 0.f, 0.f};
-        for (int i = 0; i < slot.count; ++i) {
-            const float2 ml = a.ml[place_of(i, row)];
-            const v4f x = *reinterpret_cast<const v4f *>(a.o + place_of(i, row) * D + lane * 4);
-            const float f = exp2f(ml.x - top);                        // (no score above minus infinity anywhere: 0 / 0)
-            sum += f * ml.y;
+    // (all of a thread's rows side by side: a share costs one wait for memory)
+    constexpr int ROUNDS = ROWS / EACH;
+    const int row0 = (int)blockIdx.x * ROWS + t / LANES;
+    float top[ROUNDS], sum[ROUNDS];
+    v4f o[ROUNDS];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] += fabsf(x[e]) < INFINITY ? f * x[e] : x[e];          // (an infinite value stays one however small its weight)
+    for (int k = 0; k < ROUNDS; ++k) top[k] = -INFINITY, sum[k] = 0.f, o[k] = v4f{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < slot.count; ++i) {
+        const float2 *ml = a.ml + place_of(i, row0);
+#pragma unroll
+        for (int k = 0; k < ROUNDS; ++k) top[k] = fmaxf(top[k], ml[k * EACH].x);         // (rows behind the last hold what they like)
+    }
+    for (int i = 0; i < slot.count; ++i) {
+        const int64_t place = place_of(i, row0);
+        float2 ml[ROUNDS];
+        v4f x[ROUNDS];
+#pragma unroll
+        for (int k = 0; k < ROUNDS; ++k) {
+            ml[k] = a.ml[place + k * EACH];
+            x[k] = *reinterpret_cast<const v4f *>(a.o + (place + k * EACH) * D + lane * 4);
         }
-        const float norm = 1.f / sum;
+#pragma unroll
+        for (int k = 0; k < ROUNDS; ++k) {
+            const float f = exp2f(ml[k].x - top[k]);                  // (no score above minus infinity anywhere: 0 / 0)
+            sum[k] += f * ml[k].y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[k][e] += fabsf(x[k][e]) < INFINITY ? f * x[k][e] : x[k][e];        // (an infinite value stays one however small its weight)
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < ROUNDS; ++k) {
+        const int pair = slot.tile + row0 + k * EACH;
+        if (pair >= sp.n * G) break;
+        const float norm = 1.f / sum[k];
         union { __half h[4]; v2u v; } out;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) out.h[e] = __float2half_rn(o[e] * norm);
+        for (int e = 0; e < 4; ++e) out.h[e] = __float2half_rn(o[k][e] * norm);
         *reinterpret_cast<v2u *>(a.O + (int64_t)(sp.row + pair / G) * a.ldo + (int64_t)(slot.kh * G + pair % G) * D + lane * 4) = out.v;
     }
 }
@@ -1312,6 +1331,176 @@ __global__ __launch_bounds__(64 * kFewRowsWaves, 2) void cache8_few_rows_kernel(
         out.h[i] = __float2half_rn(x);
     }
     *reinterpret_cast<v2u *>(O + (int64_t)(sp.row + of) * ldo + (int64_t)(kh * G + tile + row - of * G) * D + col) = out.v;
+}
+
+// Few rows behind a prefix that is not long: the same over the prefix's blocks and the sequence's own, which are dealt out together; no parts.
+template <int D>
+struct ShortLds {
+    __attribute__((aligned(16))) union {
+        struct {
+            unsigned short k[kBlock][D + 8];
+            unsigned short v[D][kBlock + 8];
+        } tail[2];                               // of the prefix, of the sequence
+        float o[kFewRowsWaves][16][D + 4];
+    } u;
+    float m[kFewRowsWaves][16], l[kFewRowsWaves][16];
+    int not_finite[2];
+};
+struct ShortArgs {
+    const __half *Q;
+    int64_t ldq;
+    const int32_t *starts, *past;
+    int rows, max_new, H;
+    Cache8View cache, prefix;
+    Parts parts;                 // (width and lengths)
+    __half *O;
+    int64_t ldo;
+    int tiles;
+};
+template <int D>
+__global__ __launch_bounds__(64 * kFewRowsWaves, 2) void cache8_short_kernel(const ShortArgs a)
+{
+    constexpr int C = D / 64, DT = D / 16, T = 64 * kFewRowsWaves, UNITS = kBlock * D / 8 / T;
+    extern __shared__ __attribute__((aligned(16))) uint8_t raw_lds[];
+    ShortLds<D> &lds = *reinterpret_cast<ShortLds<D> *>(raw_lds);
+    const Cache8View &cache = a.cache, &prefix = a.prefix;
+    const int pairs = cache.kv_heads * cache.batch, id = blockIdx.x, pair = id % pairs, number = id / pairs;
+    const int b = pair / cache.kv_heads, kh = pair % cache.kv_heads, group = b / a.parts.width;
+    const int t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), r = l & 15, g = l >> 4, G = a.H / cache.kv_heads;
+    const Member member = member_of(a.starts, a.past, b, a.rows, a.max_new, cache.blocks * kBlock, prefix.blocks * kBlock, a.parts);
+    if (!member.rows) return;
+    const Span &sp = member.sp;
+    if (!member.fits) {
+        nan_rows<D>(a.O, a.ldo, sp.row, (int64_t)sp.n * G, G, kh, number, a.tiles, 16);
+        return;
+    }
+    const int n_rows = sp.n * G, tile = (a.tiles - 1 - number) * 16;
+    if (tile >= n_rows) return;
+    const int mine = min(tile + r, n_rows - 1), query = mine / G, first_sees = sp.past + tile / G, sees = sp.past + query;
+    const int last = sp.past + (min(tile + 16, n_rows) - 1) / G, end = sp.past + sp.n;
+    // finished blocks of the prefix, then own ones that some row sees; then the unfinished ones
+    const int of_prefix = member.length / kBlock, finished = of_prefix + min(last / kBlock + 1, end / kBlock);
+    const int rest[2] = {member.length % kBlock, last / kBlock == end / kBlock ? end % kBlock : 0};
+    const int64_t heads[2] = {(int64_t)group * prefix.kv_heads + kh, (int64_t)b * cache.kv_heads + kh};
+    const __half *tails[2] = {prefix.tail + heads[0] * 2 * kBlock * D, cache.tail + heads[1] * 2 * kBlock * D};
+    v4i kraw[4 * C], vraw[DT];
+    float2 sc = {0.f, 0.f};
+    auto codes_of = [&](int j, int values) {
+        return reinterpret_cast<const v4i *>(j < of_prefix ? block_codes<D>(prefix, heads[0], j, values) : block_codes<D>(cache, heads[1], j - of_prefix, values)) + l;
+    };
+    auto fetch_keys = [&](int j) {
+        if (j >= finished) return;
+        sc = *reinterpret_cast<const float2 *>(j < of_prefix ? prefix.scales + (heads[0] * prefix.blocks + j) * 2 : cache.scales + (heads[1] * cache.blocks + j - of_prefix) * 2);
+        const v4i *k = codes_of(j, 0);
+#pragma unroll
+        for (int i = 0; i < 4 * C; ++i) kraw[i] = k[i * 64];
+    };
+    auto fetch_values = [&](int j) {
+        if (j >= finished) return;
+        const v4i *v = codes_of(j, 1);
+#pragma unroll
+        for (int i = 0; i < DT; ++i) vraw[i] = v[i * 64];
+    };
+    v4i tk[2][UNITS], tv[2][UNITS];
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            const int u = t + i * T, s = u / (D / 8), col = (u % (D / 8)) * 8;
+            tk[x][i] = tv[x][i] = v4i{0, 0, 0, 0};
+            if (s < rest[x]) {
+                tk[x][i] = *reinterpret_cast<const v4i *>(tails[x] + s * D + col);
+                tv[x][i] = *reinterpret_cast<const v4i *>(tails[x] + kBlock * D + s * D + col);
+            }
+        }
+    fetch_keys(wave);
+    fetch_values(wave);
+    v8h q[2 * C];
+    const __half *from = a.Q + (int64_t)(sp.row + query) * a.ldq + (int64_t)(kh * G + mine - query * G) * D;
+#pragma unroll
+    for (int m = 0; m < 2 * C; ++m) q[m] = *reinterpret_cast<const v8h *>(from + 64 * (m >> 1) + 16 * g + 8 * (m & 1));
+    if (t < 2) lds.not_finite[t] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        if (rest[x] == 0) continue;
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            const int u = t + i * T, s = u / (D / 8), col = (u % (D / 8)) * 8, at = value_slot(s);
+            *reinterpret_cast<v4i *>(&lds.u.tail[x].k[s][col]) = tk[x][i];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                unsigned short w = (unsigned short)((unsigned)tv[x][i][e >> 1] >> (16 * (e & 1)));
+                if ((w & 0x7fffu) >= 0x7c00u) w = 0, odd = true;      // comes back at the end, to the rows that see it
+                lds.u.tail[x].v[col + e][value_place(col + e, at)] = w;
+            }
+        }
+        if (odd) lds.not_finite[x] = 1;
+    }
+    __syncthreads();
+    WaveSums<D> sums;
+    int j = wave;
+    for (; j < finished; j += kFewRowsWaves) {
+        const float2 scale = sc;
+        const int at_own = (j - of_prefix) * kBlock;
+        sums.add(
+            q, scale.x, scale.y, at_own >= 0 && at_own + kBlock - 1 > first_sees, sees - at_own,
+            [&](int T4, int m) {
+                const v4i w = kraw[T4 * C + (m >> 1)];
+                return (m & 1) ? halves_of(w[2], w[3]) : halves_of(w[0], w[1]);
+            },
+            [&](int i, int n) { return halves_of(vraw[i][2 * n], vraw[i][2 * n + 1]); }, [&] { fetch_keys(j + kFewRowsWaves); });
+        fetch_values(j + kFewRowsWaves);
+    }
+    j -= finished;                                                    // the unfinished ones go to the wavefronts whose turn it is
+    int which = rest[0] > 0 ? 0 : 1, left = (rest[0] > 0) + (rest[1] > 0);
+    if (j == 1 && left == 2) which = 1;
+    if (j < left)
+        sums.add(
+            q, 1.f, 1.f, true, which == 0 ? rest[0] - 1 : min(sees - end / kBlock * kBlock, rest[1] - 1),
+            [&](int T4, int m) { return *reinterpret_cast<const v8h *>(&lds.u.tail[which].k[16 * T4 + r][64 * (m >> 1) + 16 * g + 8 * (m & 1)]); },
+            [&](int i, int n) { return *reinterpret_cast<const v8h *>(&lds.u.tail[which].v[16 * i + r][value_place(16 * i + r, 32 * n + 8 * g)]); }, [] {});
+    sums.l += __shfl_xor(sums.l, 16);
+    sums.l += __shfl_xor(sums.l, 32);
+    __syncthreads();                                                  // the tails' rows have been read
+#pragma unroll
+    for (int i = 0; i < DT; ++i) *reinterpret_cast<v4f *>(&lds.u.o[wave][r][16 * i + 4 * g]) = sums.o[i] * sums.unit.unit;
+    if (g == 0) {
+        lds.m[wave][r] = sums.m;
+        lds.l[wave][r] = sums.l;
+    }
+    __syncthreads();
+    const int waves = min(finished + left, kFewRowsWaves), row = t / (D / 4), col = t % (D / 4) * 4;          // four columns of a row
+    if (row >= 16 || tile + row >= n_rows) return;
+    const int of = (tile + row) / G;
+    float top = -INFINITY, sum = 0.f;
+    for (int w = 0; w < waves; ++w) top = fmaxf(top, lds.m[w][row]);
+    v4f o = {0.f, 0.f, 0.f, 0.f};
+    for (int w = 0; w < waves; ++w) {
+        const float f = exp2f(lds.m[w][row] - top);
+        sum += f * lds.l[w][row];
+        o += f * *reinterpret_cast<const v4f *>(&lds.u.o[w][row][col]);
+    }
+    const float norm = 1.f / sum;
+    union { __half h[4]; v2u v; } out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float y = o[i] * norm;
+#pragma unroll 1
+        for (int x = 0; x < 2; ++x) {
+            if (!lds.not_finite[x]) continue;                         // infinities and NaN among a tail's values that this row sees
+            y = __half2float(__float2half_rn(y));
+            const int seen = x == 0 ? rest[0] : sp.past + of - end / kBlock * kBlock + 1;
+#pragma unroll 1
+            for (int s = 0; s < seen; ++s) {
+                const float v = __half2float(tails[x][kBlock * D + s * D + col + i]);
+                if (!(fabsf(v) <= 65504.f)) y += v;
+            }
+        }
+        out.h[i] = __float2half_rn(y);
+    }
+    *reinterpret_cast<v2u *>(a.O + (int64_t)(sp.row + of) * a.ldo + (int64_t)(kh * G + tile + row - of * G) * D + col) = out.v;
 }
 
 // ---------------------------------------------------------------- attention of one row per sequence
@@ -2111,9 +2300,13 @@ sqap_status launch_cache8_decode(const __half *QKV, int64_t ld, const int32_t *p
 // How the prefixes are dealt out.  Up to 64 pairs to a group and key head: tiles of 16, blocks dealt to the wavefronts; up to 256 of them, too, where all
 // tiles together have no more than 20000 blocks: the tiles of 128 want two launches more (32 rows of 32 heads over 8 behind 1000 positions 14 and
 // 27 us, behind 20000 45 and 48, behind 100003 187 and 128; 64 behind 1000 23 and 29).
+// Prompts of few rows: tiles of 16 that pass over prefix and own positions by themselves, while they are up to 12000 blocks in all (16 x 10 rows of 32
+// heads over 8 behind 1000 positions, 6144: 25 us, in parts 30; behind 4000 54 and 39; 16 x 20 of 32 heads, 16384: 39 and 36) and prefixes up to 48 blocks
+// long, or 256 tiles (10 rows behind 1000 positions 13 and 20, behind 4000 27 and 24).
+constexpr int kShortBlocks = 12000, kShortPrefix = 48;
 constexpr int kFewPairs = 64, kFewPairsAtMost = 256, kFewBlocks = 20000, kPrefixGroups = 512, kMostPrefixShares = 64;
 struct SharedPlan {
-    bool together;               // long prompts: cache8_long_kernel
+    bool together, direct;       // long prompts: cache8_long_kernel; short ones: cache8_short_kernel
     int groups;                  // its workgroups
     bool few;
     int64_t tiles;               // of a group and key head
@@ -2121,7 +2314,7 @@ struct SharedPlan {
     int64_t pairs;               // rows times heads
     size_t q, ml, o, bytes;      // where they are in the workspace
 };
-static SharedPlan shared_plan(int batch, int groups, int H, int kv_heads, int d, int rows, int max_new, int own_shares, int longest_prefix)
+static SharedPlan shared_plan(bool prompt, int batch, int groups, int H, int kv_heads, int d, int rows, int max_new, int own_shares, int longest_prefix)
 {
     SharedPlan p = {};
     const int64_t of_group = std::min<int64_t>((int64_t)(batch / groups) * max_new, rows) * (H / kv_heads);
@@ -2142,6 +2335,10 @@ static SharedPlan shared_plan(int batch, int groups, int H, int kv_heads, int d,
         p.bytes = p.o + (size_t)p.groups * 256 * d * sizeof(float);
         return p;
     }
+    // few tiles of 16 rows and blocks of prefixes in all, and not many blocks to a wavefront
+    const int64_t tiles = ((int64_t)max_new * (H / kv_heads) + 15) / 16 * kv_heads * batch;
+    p.direct = prompt && tiles * blocks <= kShortBlocks && (blocks <= kShortPrefix || tiles >= 256);
+    if (p.direct) return p;                                           // (no workspace)
     p.q = kCounterBytes;                                              // (left alone, for calls that want it zero)
     p.ml = p.q + (max_new == 1 ? up((size_t)p.pairs * d * 2) : 0);
     p.o = p.ml + up((size_t)(p.shares + own_shares) * p.pairs * sizeof(float2));
@@ -2155,7 +2352,7 @@ static int own_shares_of(int batch, int H, int kv_heads, int longest)
 
 size_t cache8_shared_workspace_bytes(int batch, int groups, int H, int kv_heads, int d, int rows, int max_new, int longest, int longest_prefix)
 {
-    return shared_plan(batch, groups, H, kv_heads, d, rows, max_new, max_new == 1 ? own_shares_of(batch, H, kv_heads, longest) : 1, longest_prefix).bytes;
+    return shared_plan(max_new > 1, batch, groups, H, kv_heads, d, rows, max_new, max_new == 1 ? own_shares_of(batch, H, kv_heads, longest) : 1, longest_prefix).bytes;
 }
 
 template <int D>
@@ -2198,7 +2395,7 @@ template <int D>
 static sqap_status launch_shared_d(const __half *Q, int64_t ldq, const int32_t *starts, const int32_t *past, int rows, int max_new, int H, const Cache8View &cache,
                                    const Cache8View &prefix, const int32_t *length, int longest_prefix, __half *O, int64_t ldo, char *workspace, hipStream_t st)
 {
-    const SharedPlan plan = shared_plan(cache.batch, prefix.batch, H, cache.kv_heads, D, rows, max_new, 1, longest_prefix);
+    const SharedPlan plan = shared_plan(true, cache.batch, prefix.batch, H, cache.kv_heads, D, rows, max_new, 1, longest_prefix);
     if (plan.together) {
         constexpr int LDS = 2 * 2 * kBlock * D * 2;
         static std::atomic<bool> ready[kMaxDeviceSlots];
@@ -2212,6 +2409,18 @@ static sqap_status launch_shared_d(const __half *Q, int64_t ldq, const int32_t *
         hipLaunchKernelGGL(cache8_long_kernel<D>, dim3(plan.groups), dim3(256), LDS, st, a);
         SQAP_HIP_CHECK(hipGetLastError());
         hipLaunchKernelGGL(cache8_long_join_kernel<D>, dim3(2, plan.groups), dim3(256), 0, st, a);
+        SQAP_HIP_CHECK(hipGetLastError());
+        return SQAP_OK;
+    }
+    if (plan.direct) {
+        static std::atomic<bool> ready[kMaxDeviceSlots];
+        if (!ready[device_slot()].load(std::memory_order_relaxed)) {
+            SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(cache8_short_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(ShortLds<D>)));
+            ready[device_slot()].store(true, std::memory_order_relaxed);
+        }
+        const int tiles = std::max(1, (max_new * (H / cache.kv_heads) + 15) / 16);
+        hipLaunchKernelGGL(cache8_short_kernel<D>, dim3((unsigned)tiles * cache.kv_heads * cache.batch), dim3(64 * kFewRowsWaves), sizeof(ShortLds<D>), st,
+                           ShortArgs{Q, ldq, starts, past, rows, max_new, H, cache, prefix, Parts{nullptr, nullptr, 0, 0, cache.batch / prefix.batch, length}, O, ldo, tiles});
         SQAP_HIP_CHECK(hipGetLastError());
         return SQAP_OK;
     }
@@ -2235,7 +2444,7 @@ template <int D>
 static sqap_status launch_shared_decode_d(DecodeArgs a, const int32_t *length, int longest_prefix, char *workspace, hipStream_t st)
 {
     const Cache8View &cache = a.cache, &prefix = a.prefix;
-    const SharedPlan plan = shared_plan(cache.batch, prefix.batch, a.H, cache.kv_heads, D, cache.batch, 1, a.shares, longest_prefix);
+    const SharedPlan plan = shared_plan(false, cache.batch, prefix.batch, a.H, cache.kv_heads, D, cache.batch, 1, a.shares, longest_prefix);
     a.parts = {reinterpret_cast<float *>(workspace + plan.o), reinterpret_cast<float2 *>(workspace + plan.ml), plan.pairs, plan.shares, cache.batch / prefix.batch, length};
     a.prefix_tiles = plan.few ? (int)plan.tiles : 0;
     a.q_out = plan.few ? nullptr : reinterpret_cast<__half *>(workspace + plan.q);

@@ -20,7 +20,10 @@ The last residual add (x + d) is left pending and fused into the next layer's fi
 The same layer in microscaled 4-bit floating point, where its four weights are Mx4Weight: the norms and the product of gate and up
 leave halves, which sqap_mx4_quantize takes, and sqap_mx4_linear multiplies.  With a Cache8 in the place of the fp16 cache
 the call is about a batch of sequences, each with a length of its own: prompts through sqap_cache8_append and sqap_cache8_attention, one new
-row per sequence through sqap_cache8_decode_attention.  Either goes with the other's counterpart.
+row per sequence through sqap_cache8_decode_attention.  Either goes with the other's counterpart.  Sequences that continue a common
+prefix (samples or beams of one observation) share it: the prefixes in a Cache8 of their own, which a call with kv = that cache has filled, then
+calls with `prefix`, through sqap_cache8_shared_attention and sqap_cache8_shared_decode_attention; between the steps of a beam search
+sqap_beam_select chooses, and sqap_cache8_reorder lets every layer's sequences take over their parents'.
 """
 import torch
 
@@ -43,7 +46,8 @@ class LayerBuffers:
     """Scratch tensors for up to max_rows token rows of one layer call (reused by every layer).
 
     kv_width: width of the keys (of the values), where heads of a Cache8 are shared; mx4: for layers of Mx4Weight;
-    cache8_workspace: for calls over a Cache8, the bytes of sqap_cache8_workspace_bytes for its decode calls (0: none)."""
+    cache8_workspace: for calls over a Cache8, the bytes of sqap_cache8_workspace_bytes for its decode calls (0: none), of
+    sqap_cache8_shared_workspace_bytes for calls behind prefixes; the most of them, where a buffer serves several."""
 
     def __init__(self, max_rows, hidden, ffn, device="cuda", kv_width=None, mx4=False, cache8_workspace=None):
         f16, u8 = torch.float16, torch.uint8
@@ -73,22 +77,31 @@ class LayerBuffers:
         self.counter = torch.zeros((1,), dtype=torch.int32, device=device)     # arrival counter of sqap_decode_attention
 
 
-def _cache8_attention(buf, qkv, attn, pos, batch, n_heads, kv, past, starts, max_new, longest, stream):
-    """Append and attention over a Cache8: prompts where `starts` is given, otherwise one new row per sequence."""
+def _cache8_attention(buf, qkv, attn, pos, batch, n_heads, kv, past, starts, max_new, longest, stream, prefix=None, prefix_len=None,
+                      longest_prefix=0):
+    """Append and attention over a Cache8, behind prefixes where they are given: prompts where `starts` is, otherwise one new row per sequence."""
     if kv.batch != batch:
         raise ValueError("the cache is for %d sequences, not %d" % (kv.batch, batch))
     if starts is not None:
         q = buf.q[:pos.numel()]
         B.sqap_cache8_append(qkv, starts, pos, past, kv, n_heads, max_new, Q_out=q, stream=stream)
-        B.sqap_cache8_attention(q, starts, past, kv, n_heads, max_new, attn, stream=stream)
+        if prefix is not None:
+            B.sqap_cache8_shared_attention(q, starts, past, kv, prefix, prefix_len, n_heads, max_new, attn, buf.cache8_ws, longest_prefix, stream=stream)
+        else:
+            B.sqap_cache8_attention(q, starts, past, kv, n_heads, max_new, attn, stream=stream)
     else:
         if pos.numel() != batch:
             raise ValueError("one new row per sequence, or `starts`")
-        B.sqap_cache8_decode_attention(qkv, pos, past, kv, n_heads, attn, buf.cache8_ws, longest, stream=stream)
+        if prefix is not None:
+            B.sqap_cache8_shared_decode_attention(qkv, pos, past, kv, prefix, prefix_len, n_heads, attn, buf.cache8_ws, longest, longest_prefix,
+                                                  stream=stream)
+        else:
+            B.sqap_cache8_decode_attention(qkv, pos, past, kv, n_heads, attn, buf.cache8_ws, longest, stream=stream)
 
 
 def layer_forward(w, buf, x, pending, pos, batch, n_heads, head_dim, x_out, d_out, eps=1e-5, rows=None,
-                  rotate=False, kv=None, past=0, stream=None, fold_quantizer=False, starts=None, max_new=0, longest=0):
+                  rotate=False, kv=None, past=0, stream=None, fold_quantizer=False, starts=None, max_new=0, longest=0, prefix=None,
+                  prefix_len=None, longest_prefix=0):
     """Runs one layer on M token rows (batch sequences of M / batch tokens each).
 
     x: residual stream [*, hidden] fp16 (rows picks the M rows when given: the token gather is fused);
@@ -100,12 +113,16 @@ def layer_forward(w, buf, x, pending, pos, batch, n_heads, head_dim, x_out, d_ou
     keys (prefill fills the cache with past = 0; a decode step has M = 1).  Needs batch == 1.
     Or kv: a Cache8 of `batch` sequences; past: [batch] int32 on the device; starts: [batch + 1] int32 on the device, the sequences'
     first rows, of at most max_new rows each, or None for one row per sequence, whose lengths afterwards are at most `longest`.
+    prefix: this layer's Cache8 of prefixes, one for each batch / prefix.batch sequences of kv, which hold prefix_len [prefix.batch] int32 positions on
+    the device, longest_prefix at most; `past` and `longest` are about a sequence's own positions then, pos about all of them.
     """
     M = pos.numel()
     hidden = buf.hidden
     mx4, cache8 = isinstance(w.qkv, B.Mx4Weight), isinstance(kv, B.Cache8)
     if (rotate and mx4) or (fold_quantizer and (mx4 or cache8)):
         raise ValueError("neither rotate nor fold_quantizer goes with weights in microscaled floating point, nor the latter with a Cache8")
+    if prefix is not None and not cache8:
+        raise ValueError("a prefix goes with a Cache8")
     kv_width = kv.kv_heads * kv.head_dim if cache8 else hidden
     if buf.qkv.shape[1] != hidden + 2 * kv_width or (cache8 and kv.head_dim != head_dim):
         raise ValueError("buffers for q|k|v rows of %d columns, keys and values of %d each, heads of %d" % (buf.qkv.shape[1], kv_width, head_dim))
@@ -123,7 +140,7 @@ def layer_forward(w, buf, x, pending, pos, batch, n_heads, head_dim, x_out, d_ou
         B.sqap_w4a4_linear(xq, sx, w.qkv, qkv, None, buf.ws, stream=stream)
     one_launch = kv is not None and not cache8 and M == 1 and head_dim % 8 == 0 and head_dim <= 128 and hidden <= 8192
     if cache8:
-        _cache8_attention(buf, qkv, attn, pos, batch, n_heads, kv, past, starts, max_new, longest, stream)
+        _cache8_attention(buf, qkv, attn, pos, batch, n_heads, kv, past, starts, max_new, longest, stream, prefix, prefix_len, longest_prefix)
     elif kv is None:
         B.sqap_rope(qkv[:, :2 * hidden], pos, 2 * n_heads, head_dim, stream=stream)  # queries and keys in one launch
         B.sqap_attention(qkv[:, :hidden], qkv[:, hidden:2 * hidden], qkv[:, 2 * hidden:], n_heads, head_dim, attn,

@@ -15,11 +15,12 @@ KEPT = 16384                                                          # bytes of
 
 def test_prompt_refusals():
     L = B.lib()
-    need = B.sqap_cache8_shared_workspace_bytes(4, 2, 4, 2, 64, 3, 2, 1, 500)
+    need = B.sqap_cache8_shared_workspace_bytes(4, 2, 4, 2, 64, 3, 2, 1, 5000)
+    assert B.sqap_cache8_shared_workspace_bytes(4, 2, 4, 2, 64, 3, 2, 1, 500) == 0
     assert need > KEPT and all(B.sqap_cache8_shared_workspace_bytes(*bad) == 0 for bad in (
         (0, 1, 4, 2, 64, 3, 2, 1, 5), (4, 3, 4, 2, 64, 3, 2, 1, 5), (4, 0, 4, 2, 64, 3, 2, 1, 5), (4, 2, 5, 2, 64, 3, 2, 1, 5), (4, 2, 4, 2, 64, 0, 2, 1, 5),
         (4, 2, 4, 2, 64, 3, 0, 1, 5), (4, 2, 4, 2, 64, 3, 2, 0, 5), (4, 2, 4, 2, 64, 3, 2, 1, -1)))
-    good = dict(Q=P, ldq=256, starts=P, past=P, rows=3, max_new=2, H=4, cache=_desc(batch=4), prefix=_desc(capacity=512), length=P, longest_prefix=500,
+    good = dict(Q=P, ldq=256, starts=P, past=P, rows=3, max_new=2, H=4, cache=_desc(batch=4), prefix=_desc(capacity=512), length=P, longest_prefix=5000,
                 O=P, ldo=256, ws=P, bytes=need, stream=None)
     call = lambda **kw: L.sqap_cache8_shared_attention(*{**good, **kw}.values())             # noqa: E731
     for bad in (dict(rows=-1), dict(max_new=-1), dict(H=5), dict(cache=None), dict(prefix=None), dict(Q=None), dict(starts=None), dict(past=None), dict(length=None),
@@ -139,7 +140,7 @@ class Shared:
 # groups, width, heads, key heads, head size, prefixes: pairs of a group and key head below, at and above 16, 64, 128; more than 16 heads to a key head
 SHAPES = [(1, 1, 1, 1, 64, [1]), (1, 4, 4, 4, 128, [276]), (2, 3, 4, 2, 64, [64, 63]), (3, 2, 8, 1, 128, [0, 65, 200]), (2, 8, 8, 4, 128, [700, 130]),
           (1, 17, 4, 4, 64, [128]), (1, 16, 8, 2, 64, [1000]), (1, 13, 10, 2, 128, [333]), (2, 33, 4, 1, 64, [90, 5000]), (1, 5, 32, 1, 128, [191]),
-          (1, 40, 4, 1, 128, [2500]), (1, 1, 20, 1, 64, [4097])]
+          (1, 40, 4, 1, 128, [2500]), (1, 1, 20, 1, 64, [4097]), (2, 64, 4, 2, 64, [300, 70])]
 
 
 @pytest.mark.gpu
@@ -178,8 +179,9 @@ def test_many_own_blocks(G):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("hint", [None, 100000])                  # (in one pass, and in parts)
 @pytest.mark.parametrize("width", [2, 40])
-def test_infinite_values_and_keys(G, width):
+def test_infinite_values_and_keys(G, width, hint):
     """Infinities and NaN among values and keys of the unfinished blocks of a prefix and of own positions, a prefix block without scale, scores that
     are minus infinity over a whole prefix."""
     H, kv, d, lengths = 4, 2, 64, [70, 130, 1]
@@ -197,13 +199,13 @@ def test_infinite_values_and_keys(G, width):
     s.decode()
     x = s.own.rows(6 * width)
     x[1, H + kv, 40] = np.inf                                         # seen by the rows behind it alone
-    s.prompt([2] * (3 * width), x=x)
+    s.prompt([2] * (3 * width), x=x, longest_prefix=hint)
 
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("width", [2, 40])
-@pytest.mark.parametrize("decode", [True, False])
-def test_what_does_not_fit(G, width, decode):
+@pytest.mark.parametrize("decode,hint", [(True, 100), (False, 100), (False, 100000)])
+def test_what_does_not_fit(G, width, decode, hint):
     """Padded sequences keep their outputs; sequences without room, rows or prefix lengths that cannot be give NaN, and nothing reaches the others."""
     t, H, kv, d, groups = __import__("torch"), 4, 2, 64, 4
     s = Shared(G, groups, width, H, kv, d, [100, 5, 64, 70], capacity=128, seed=5)
@@ -217,15 +219,15 @@ def test_what_does_not_fit(G, width, decode):
     x = s.own.rows(n * batch)
     pos = np.concatenate([s.lengths[b // width] + past[b] + np.arange(n) for b in range(batch)]).astype(np.int32)
     o = t.full((n * batch, H * d), 9.0, dtype=t.float16, device=G.DEV)
-    ws = s.workspace(n * batch, n, 128, 100)
+    ws = s.workspace(n * batch, n, 128, hint)
     if decode:
-        B.sqap_cache8_shared_decode_attention(G.to_dev(x.reshape(batch, -1)), G.to_dev(pos), G.to_dev(past), s.own.cache, s.prefix.cache, lengths, H, o, ws, 128, 100)
+        B.sqap_cache8_shared_decode_attention(G.to_dev(x.reshape(batch, -1)), G.to_dev(pos), G.to_dev(past), s.own.cache, s.prefix.cache, lengths, H, o, ws, 128, hint)
         y = s.own.turned(x, pos)
     else:
         starts = G.to_dev(np.arange(batch + 1, dtype=np.int32) * n)
         q = t.full_like(o, 9.0)
         B.sqap_cache8_append(G.to_dev(x.reshape(n * batch, -1)), starts, G.to_dev(pos), G.to_dev(past), s.own.cache, H, n, Q_out=q)
-        B.sqap_cache8_shared_attention(q, starts, G.to_dev(past), s.own.cache, s.prefix.cache, lengths, H, n, o, ws, 100)
+        B.sqap_cache8_shared_attention(q, starts, G.to_dev(past), s.own.cache, s.prefix.cache, lengths, H, n, o, ws, hint)
         y = s.own.turned(x, pos)
     s.own.note(counts, y)
     got = o.cpu().numpy()
@@ -235,7 +237,8 @@ def test_what_does_not_fit(G, width, decode):
 
 
 @pytest.mark.gpu
-def test_rows_that_are_not_announced(G):
+@pytest.mark.parametrize("hint", [70, 100000])
+def test_rows_that_are_not_announced(G, hint):
     """More rows than announced: NaN for that sequence; more than all of a group's together: for the group.  Starts out of order: skipped."""
     t, H, kv, d, width = __import__("torch"), 2, 1, 64, 3
     s = Shared(G, 2, width, H, kv, d, [70, 20], seed=6)
@@ -248,7 +251,7 @@ def test_rows_that_are_not_announced(G):
                                     (5, [0, 1, 6, 7, 9, 40, 13], (), range(9, 13)), (5, [0, 1, -6, 7, 9, 11, 13], (), range(1, 7))):
         o = t.full((13, H * d), 9.0, dtype=t.float16, device=G.DEV)
         B.sqap_cache8_shared_attention(q, G.to_dev(np.array(starts, np.int32)), G.to_dev(before), s.own.cache, s.prefix.cache, s.device_lengths, H, most, o,
-                                       s.workspace(13, max(most, 1), 1, 70), 70)
+                                       s.workspace(13, max(most, 1), 1, hint), hint)
         got = o.cpu().numpy()
         bad, left = list(bad), list(left)
         assert np.all(np.isnan(got[bad])) and np.all(got[left] == 9), (most, starts)
