@@ -546,7 +546,7 @@ sqap_status sqap_cache8_read(const sqap_cache8 *cache, const int32_t *lengths, i
 
 /*
  * Attention of sequences that share long prefixes, each prefix read once for all of its sequences.  The prefixes are sequences of a cache of
- * their own, `prefix` (as many key heads, of the same size; any capacity), filled by sqap_cache8_append; prefix_len [prefix->batch] int32,
+ * their own, `prefix` (as many key heads, of the same size; any capacity; other buffers), filled by sqap_cache8_append; prefix_len [prefix->batch] int32,
  * device, says how many positions each has (0: none).  The sequences of `cache` stand in groups of width = cache->batch / prefix->batch, sequence b
  * behind prefix b / width, and hold their own positions: past [cache->batch] does not count the prefix.  Row j of sequence b sees
  * the whole prefix and its own positions 0 .. past[b] + j:
@@ -565,8 +565,9 @@ sqap_status sqap_cache8_read(const sqap_cache8 *cache, const int32_t *lengths, i
  * As above a sequence with past[b] < 0 or without rows is skipped; one whose rows do not fit or are more than max_new gets outputs of NaN; so do
  * the sequences of a group whose rows together are not within 0 .. rows or more than width * max_new, and of a prefix whose prefix_len is
  * negative or beyond its capacity (appended to they are all the same).  One whose starts do not lie in order, or outside those of its group's first and last, is skipped.
- * EINVAL, EUNSUPPORTED: as above; EINVAL also for a cache of prefixes of other heads, a batch that is no multiple of theirs, longest_prefix < 0;
- * EUNSUPPORTED for more than 4095 sequences, rows of a group times H / kv_heads beyond 32 bits.
+ * EINVAL, EUNSUPPORTED: as above; EINVAL also for a cache of prefixes of other heads or with a buffer of the sequences', a batch that is no multiple of
+ * theirs, longest_prefix < 0; EUNSUPPORTED for more than 4095 sequences, rows of a group times H / kv_heads beyond 32 bits, a decode call of some 2^28 rows
+ * times heads.
  */
 size_t sqap_cache8_shared_workspace_bytes(int32_t batch, int32_t groups, int32_t H, int32_t kv_heads, int32_t head_dim,
                                           int32_t rows, int32_t max_new, int32_t longest, int32_t longest_prefix);

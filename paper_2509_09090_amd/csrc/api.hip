@@ -857,6 +857,8 @@ static sqap_status check_prefix(const char *who, const sqap_cache8 *cache, const
         return fail(SQAP_EINVAL, "%s: prefixes of %d key heads of %d, sequences of %d of %d", who, prefix->kv_heads, prefix->head_dim, cache->kv_heads, cache->head_dim);
     if (cache->batch > 0 && (prefix->batch == 0 || cache->batch % prefix->batch != 0))
         return fail(SQAP_EINVAL, "%s: %d sequences behind %d prefixes", who, cache->batch, prefix->batch);
+    if (cache->batch > 0 && (cache->codes == prefix->codes || cache->scales == prefix->scales || cache->tail == prefix->tail))
+        return fail(SQAP_EINVAL, "%s: the sequences and their prefixes are in one cache", who);
     if (longest_prefix < 0) return fail(SQAP_EINVAL, "%s: longest_prefix = %d", who, longest_prefix);
     if (cache->batch > 0 && !prefix_len) return fail(SQAP_EINVAL, "%s: null pointer", who);
     if (cache->batch > 4095) return fail(SQAP_EUNSUPPORTED, "%s: %d sequences", who, cache->batch);
@@ -927,9 +929,13 @@ sqap_status sqap_cache8_shared_decode_attention(const sqap_f16 *QKV, int64_t ld,
     const int64_t width = (int64_t)H * cache->head_dim;
     s = check_rows16(who, "QKV", QKV, ld, width + 2 * (int64_t)cache->kv_heads * cache->head_dim);
     if (s == SQAP_OK) s = check_rows16(who, "O", O, ldo, width);
-    if (s == SQAP_OK)
-        s = check_workspace(who, workspace, workspace_bytes,
-                            cache8_shared_workspace_bytes(cache->batch, prefix->batch, H, cache->kv_heads, cache->head_dim, cache->batch, 1, longest, longest_prefix));
+    if (s != SQAP_OK) return s;
+    const int G = H / cache->kv_heads;
+    const int64_t own = (int64_t)cache->batch * cache->kv_heads * ((G + 15) / 16), tiles = ((int64_t)(cache->batch / prefix->batch) * G + 15) / 16;
+    if (own + tiles * cache->kv_heads * prefix->batch > most_workgroups(256) - 512)
+        return fail(SQAP_EUNSUPPORTED, "%s: %d sequences of %d heads", who, cache->batch, H);
+    s = check_workspace(who, workspace, workspace_bytes,
+                        cache8_shared_workspace_bytes(cache->batch, prefix->batch, H, cache->kv_heads, cache->head_dim, cache->batch, 1, longest, longest_prefix));
     if (s != SQAP_OK) return s;
     const DeviceOfCall device;
     return launch_cache8_shared_decode(reinterpret_cast<const __half *>(QKV), ld, pos, past, H, base, v, p, prefix_len, cache->head_dim, longest, longest_prefix,

@@ -534,16 +534,8 @@ static void launch_reorder(const Cache8View &cache, const int32_t *parents, int 
 {
     constexpr int SPLIT = 2 * kCache8Block * D / (int)sizeof(V) / 256;
     const int block_groups = (int)std::min<int64_t>(std::max(1, longest / kCache8Block * SPLIT), 65536);
-    for (int group = 0; group < cache.batch / width; group += 65535) {
-        Cache8View part = cache;
-        const int64_t first = (int64_t)group * width, heads = first * cache.kv_heads;
-        part.codes += heads * cache.blocks * 2 * kCache8Block * D;
-        part.scales += heads * cache.blocks * 2;
-        part.tail += heads * 2 * kCache8Block * D;
-        const dim3 grid(block_groups + 2 * SPLIT + 1, cache.kv_heads, std::min(65535, cache.batch / width - group));
-        hipLaunchKernelGGL((cache8_reorder_kernel<D, WIDTH, V>), grid, dim3(256), 0, st, part, parents + first, width, lengths + first,
-                           lengths_out ? lengths_out + first : nullptr, block_groups);
-    }
+    const dim3 grid(block_groups + 2 * SPLIT + 1, cache.kv_heads, cache.batch / width);
+    hipLaunchKernelGGL((cache8_reorder_kernel<D, WIDTH, V>), grid, dim3(256), 0, st, cache, parents, width, lengths, lengths_out, block_groups);
 }
 
 template <int D>

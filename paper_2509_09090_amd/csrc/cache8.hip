@@ -2297,7 +2297,7 @@ sqap_status launch_cache8_decode(const __half *QKV, int64_t ld, const int32_t *p
 
 // ---- behind a shared prefix
 
-// How the prefixes are dealt out.  Up to 64 pairs to a group and key head: tiles of 16, blocks dealt to the wavefronts; up to 256 of them, too, where all
+// How the prefixes are dealt out: shares of two blocks to a wavefront (64 rows of 32 heads over 8 behind 1000 positions 16.3 us, with one 20.4), of one up to 8 blocks.  Up to 64 pairs to a group and key head: tiles of 16, blocks dealt to the wavefronts; up to 256 of them, too, where all
 // tiles together have no more than 20000 blocks: the tiles of 128 want two launches more (32 rows of 32 heads over 8 behind 1000 positions 14 and
 // 27 us, behind 20000 45 and 48, behind 100003 187 and 128; 64 behind 1000 23 and 29).
 // Prompts of few rows: tiles of 16 that pass over prefix and own positions by themselves, while they are up to 12000 blocks in all (16 x 10 rows of 32
@@ -2322,7 +2322,7 @@ static SharedPlan shared_plan(bool prompt, int batch, int groups, int H, int kv_
     p.few = of_group <= kFewPairs || (of_group <= kFewPairsAtMost && (of_group + 15) / 16 * groups * kv_heads * blocks <= kFewBlocks);
     p.tiles = std::max<int64_t>(1, (of_group + (p.few ? 15 : 127)) / (p.few ? 16 : 128));
     const int64_t items = p.tiles * groups * kv_heads;
-    p.shares = (int)std::max<int64_t>(1, std::min<int64_t>({(blocks + 3) / 4, kPrefixGroups / items, kMostPrefixShares}));
+    p.shares = (int)std::max<int64_t>(1, std::min<int64_t>({p.few && blocks > 8 ? (blocks + 7) / 8 : (blocks + 3) / 4, kPrefixGroups / items, kMostPrefixShares}));
     p.own_shares = own_shares;
     p.pairs = (int64_t)rows * H;
     const auto up = [](size_t n) { return (n + 15) / 16 * 16; };

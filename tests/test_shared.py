@@ -11,6 +11,11 @@ from tests.test_cache8 import BASE, ODD, P, Model, _desc
 KEPT = 16384                                                          # bytes of a workspace that are left alone
 
 
+def _front(**kw):
+    """A cache of prefixes."""
+    return _desc(**{**dict(codes=8192, scales=8192, tail=8192), **kw})
+
+
 # ---------------------------------------------------------------- refusals (no GPU)
 
 def test_prompt_refusals():
@@ -20,15 +25,16 @@ def test_prompt_refusals():
     assert need > KEPT and all(B.sqap_cache8_shared_workspace_bytes(*bad) == 0 for bad in (
         (0, 1, 4, 2, 64, 3, 2, 1, 5), (4, 3, 4, 2, 64, 3, 2, 1, 5), (4, 0, 4, 2, 64, 3, 2, 1, 5), (4, 2, 5, 2, 64, 3, 2, 1, 5), (4, 2, 4, 2, 64, 0, 2, 1, 5),
         (4, 2, 4, 2, 64, 3, 0, 1, 5), (4, 2, 4, 2, 64, 3, 2, 0, 5), (4, 2, 4, 2, 64, 3, 2, 1, -1)))
-    good = dict(Q=P, ldq=256, starts=P, past=P, rows=3, max_new=2, H=4, cache=_desc(batch=4), prefix=_desc(capacity=512), length=P, longest_prefix=5000,
+    good = dict(Q=P, ldq=256, starts=P, past=P, rows=3, max_new=2, H=4, cache=_desc(batch=4), prefix=_front(capacity=512), length=P, longest_prefix=5000,
                 O=P, ldo=256, ws=P, bytes=need, stream=None)
     call = lambda **kw: L.sqap_cache8_shared_attention(*{**good, **kw}.values())             # noqa: E731
     for bad in (dict(rows=-1), dict(max_new=-1), dict(H=5), dict(cache=None), dict(prefix=None), dict(Q=None), dict(starts=None), dict(past=None), dict(length=None),
                 dict(O=None), dict(ldq=255), dict(ldo=8), dict(ws=None), dict(bytes=need - 1), dict(ws=ODD), dict(longest_prefix=-1), dict(cache=_desc(batch=3)),
-                dict(prefix=_desc(batch=0)), dict(prefix=_desc(kv_heads=4)), dict(prefix=_desc(kv_heads=1)), dict(prefix=_desc(head_dim=128)),
-                dict(prefix=_desc(codes=None)), dict(prefix=_desc(capacity=70))):
+                dict(prefix=_front(batch=0)), dict(prefix=_front(kv_heads=4)), dict(prefix=_front(kv_heads=1)), dict(prefix=_front(head_dim=128)),
+                dict(prefix=_front(codes=None)), dict(prefix=_front(capacity=70)), dict(prefix=_front(codes=4096)), dict(prefix=_front(scales=4096)),
+                dict(prefix=_front(tail=4096))):
         assert call(**bad) == B.EINVAL, bad
-    for bad in (dict(Q=ODD), dict(O=ODD), dict(ldo=260), dict(cache=_desc(batch=4096)), dict(prefix=_desc(tail=4104)), dict(cache=_desc(head_dim=96)),
+    for bad in (dict(Q=ODD), dict(O=ODD), dict(ldo=260), dict(cache=_desc(batch=4096)), dict(prefix=_front(tail=4104)), dict(cache=_desc(head_dim=96)),
                 dict(rows=2 ** 31 - 1, max_new=2 ** 30)):
         assert call(**bad) == B.EUNSUPPORTED, bad
     assert call(rows=0, Q=None) == B.OK and call(cache=_desc(batch=0), starts=None) == B.OK
@@ -37,14 +43,15 @@ def test_prompt_refusals():
 def test_decode_refusals():
     L = B.lib()
     need = B.sqap_cache8_shared_workspace_bytes(4, 2, 4, 2, 64, 4, 1, 100, 500)
-    good = dict(QKV=P, ld=512, pos=P, past=P, H=4, base=BASE, cache=_desc(batch=4), prefix=_desc(capacity=512), length=P, longest=100, longest_prefix=500, O=P,
+    good = dict(QKV=P, ld=512, pos=P, past=P, H=4, base=BASE, cache=_desc(batch=4), prefix=_front(capacity=512), length=P, longest=100, longest_prefix=500, O=P,
                 ldo=256, ws=P, bytes=need, stream=None)
     call = lambda **kw: L.sqap_cache8_shared_decode_attention(*{**good, **kw}.values())      # noqa: E731
     for bad in (dict(H=3), dict(base=ctypes.c_double(0.0)), dict(cache=None), dict(prefix=None), dict(length=None), dict(longest=0), dict(longest_prefix=-1),
                 dict(QKV=None), dict(pos=None), dict(past=None), dict(O=None), dict(ld=504), dict(ldo=248), dict(ws=None), dict(bytes=need - 1), dict(ws=ODD),
-                dict(cache=_desc(batch=5)), dict(prefix=_desc(kv_heads=1)), dict(prefix=_desc(head_dim=128))):
+                dict(cache=_desc(batch=5)), dict(prefix=_front(kv_heads=1)), dict(prefix=_front(head_dim=128))):
         assert call(**bad) == B.EINVAL, bad
-    for bad in (dict(QKV=ODD), dict(O=ODD), dict(cache=_desc(batch=4096)), dict(prefix=_desc(codes=4104))):
+    for bad in (dict(QKV=ODD), dict(O=ODD), dict(cache=_desc(batch=4096)), dict(prefix=_front(codes=4104)),
+                dict(H=1 << 18, cache=_desc(batch=4000, kv_heads=1 << 14), prefix=_front(kv_heads=1 << 14), ld=1 << 26, ldo=1 << 26)):
         assert call(**bad) == B.EUNSUPPORTED, bad
     assert call(cache=_desc(batch=0), pos=None) == B.OK
 
@@ -100,7 +107,7 @@ class Shared:
                     limit = R.attention_bound(np.where(fine, want, 0.0), mass, np.where(np.isfinite(off), off, 0.0), k.shape[0], v_top, False)
                     assert np.all((far <= limit) | ~fine), (b, head, float(np.nanmax(far / limit)))
 
-    def prompt(self, counts, x=None, most=None, longest_prefix=None, padding=3):
+    def prompt(self, counts, x=None, most=None, longest_prefix=None, padding=3, in_place=False):
         t, G = self.t, self.G
         total = int(sum(counts))
         before = self.own.past.copy()
@@ -109,6 +116,9 @@ class Shared:
         q = t.full((total + padding, self.H * self.d + 8), float("nan"), dtype=t.float16, device=G.DEV)
         q[:total, :-8] = G.to_dev(np.ascontiguousarray(y[:, :self.H]).reshape(total, -1))
         o = t.full((total + padding, self.H * self.d), 9.0, dtype=t.float16, device=G.DEV)
+        if in_place:
+            q[total:] = 9.0
+            o = q[:, :-8]
         most = int(max(counts)) if most is None else most
         longest_prefix = int(self.lengths.max()) if longest_prefix is None else longest_prefix
         ws = self.workspace(total + padding, most, 1, longest_prefix)
@@ -163,9 +173,9 @@ def test_prompts(G, groups, width, H, kv, d, lengths):
     """Rows of many lengths, none at all, behind own positions or at the start; announcements larger than needed."""
     s = Shared(G, groups, width, H, kv, d, lengths, capacity=448, seed=width + 100)
     batch = groups * width
-    s.prompt([1 + (5 * b) % 7 for b in range(batch)])
+    s.prompt([1 + (5 * b) % 7 for b in range(batch)], in_place=True)
     s.prompt([int(n) for n in s.own.rng.integers(0, 80, batch)], most=100, longest_prefix=0)
-    s.prompt([130 if b == batch - 1 else b % 3 for b in range(batch)], longest_prefix=100000, padding=0)
+    s.prompt([130 if b == batch - 1 else b % 3 for b in range(batch)], longest_prefix=100000, padding=0, in_place=True)
     s.own.check_contents()
 
 
@@ -307,7 +317,7 @@ def test_replayed_with_other_lengths(G, width):
 def test_long_prompts(G, groups, width, H, kv, d, lengths, calls):
     s = Shared(G, groups, width, H, kv, d, lengths, capacity=640, seed=groups + 50)
     for counts in calls:
-        s.prompt(counts, longest_prefix=0 if counts == calls[-1] else None)
+        s.prompt(counts, longest_prefix=0 if counts == calls[-1] else None, in_place=counts == calls[-1])
     s.own.check_contents()
 
 
