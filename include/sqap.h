@@ -625,11 +625,12 @@ sqap_status sqap_sample(const sqap_f16 *logits, int64_t ld, int32_t batch, int32
  *   scores[beam] + (l[token] - log sum_v exp(l[v])),
  * and they are ranked by it, in binary64 (the sum of exponentials is off by some 2^-24 of itself); of equal totals the lower beam, then the
  * higher logit, then the lower token comes first.  -0 == +0; logits that are NaN or minus infinity have no probability; where there are infinite
- * ones, each of them has the same and the others none.
+ * ones, each of them has the same and the others none.  Continuations without a probability rank behind all others, at a total of minus infinity, the
+ * lower beam and then the lower token first.
  * done: NULL, or [batch, beams] int32, device: a beam that has finished (not 0) has one continuation, the token eos at its own score, and its
- * logits are not read.  Beams whose score is NaN or minus infinity have none (so that a search may start with one beam).
- * parent_out, token_out [batch, k] int32, score_out [batch, k] binary32 (the total, rounded once): best first; where there are fewer than k
- * continuations -1, -1 and minus infinity.  done_out: NULL, or [batch, k] int32: 1 where the parent has finished or the token is eos, else 0.
+ * logits are not read.  Beams whose score is NaN or minus infinity have none with a probability (so that a search may start with one beam).
+ * parent_out, token_out [batch, k] int32, score_out [batch, k] binary32 (the total, rounded once): best first; where beams * vocab is below k the rest
+ * are -1, -1 and minus infinity.  done_out: NULL, or [batch, k] int32: 1 where the parent has finished or the token is eos, else 0.
  * With k = beams score_out may be scores, done_out done.
  * workspace: at least sqap_beam_workspace_bytes(batch, beams, vocab, k) bytes, 16-byte aligned, of any contents; calls that share it must be
  * ordered on one stream, graphs that are replayed side by side need one each.  May be captured.

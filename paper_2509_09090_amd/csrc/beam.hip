@@ -403,10 +403,28 @@ __global__ __launch_bounds__(kBeamT) void beam_select_kernel(const BeamArgs a)
         out[rank] = (float)total_of(own.total);
         if (done_out) done_out[rank] = ended[r] || of == a.eos ? 1 : 0;
     }
-    for (int i = n + t; i < a.k; i += kBeamT) {
-        parent[i] = token[i] = -1;
-        out[i] = -INFINITY;
-        if (done_out) done_out[i] = 0;
+    if (n >= a.k) return;
+    // Fewer than k with a probability, all of them listed: the others follow in the order of their places, at most k + n of which have to be looked at.
+    static_assert(2 * kBeamMost <= kBeamT, "a place for each thread");
+    const int64_t places = (int64_t)a.beams * a.vocab;
+    bool is_listed = t >= places;
+    int behind = t;                                                   // places in front that are not listed
+    for (int j = 0; j < n; ++j) {
+        const int64_t place = (int64_t)(kBeamMost - 1 - (int)(list[j].tie >> kTieBeam)) * a.vocab + ((1 << kTieKey) - 1 - (int)(list[j].tie & ((1u << kTieKey) - 1)));
+        is_listed = is_listed || place == t;
+        behind -= place < t ? 1 : 0;
+    }
+    if (!is_listed && n + behind < a.k) {
+        const int r = t / a.vocab, of = t % a.vocab;
+        parent[n + behind] = r;
+        token[n + behind] = of;
+        out[n + behind] = -INFINITY;
+        if (done_out) done_out[n + behind] = ended[r] || of == a.eos ? 1 : 0;
+    }
+    if (t < a.k && t >= places) {
+        parent[t] = token[t] = -1;
+        out[t] = -INFINITY;
+        if (done_out) done_out[t] = 0;
     }
 }
 

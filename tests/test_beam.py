@@ -60,7 +60,7 @@ LSE_OFF = 45 * 2.0 ** -24
 
 
 def reference(logits, scores, done, eos, k):
-    """One batch element -> [(total, parent, token)], best first, and totals [beams, vocab]."""
+    """One batch element -> [(total, parent, token)], best first, those without a probability behind them by beam and token, and totals [beams, vocab]."""
     beams, vocab = logits.shape
     x = logits.astype(np.float64)
     x = np.where(np.isnan(x), -np.inf, x) + 0.0
@@ -78,7 +78,8 @@ def reference(logits, scores, done, eos, k):
         d = np.where(x[r] == top, 0.0, -np.inf) if np.isinf(top) else x[r] - top
         total[r] = s + (d - np.log(np.exp(d).sum()))
     order = sorted(((-total[r, t], r, -x[r, t], t) for r in range(beams) for t in np.lexsort((-x[r], -total[r]))[:k] if total[r, t] > -np.inf))[:k]
-    return [(-o[0], o[1], o[3]) for o in order], total
+    rest = [(-np.inf, int(r), int(t)) for r, t in zip(*np.unravel_index(np.flatnonzero(total.ravel() == -np.inf)[:k], total.shape))]
+    return ([(-o[0], o[1], o[3]) for o in order] + rest)[:k], total
 
 
 def select(G, logits, scores, done, eos, k, odd=False, in_place=False):
@@ -108,7 +109,7 @@ def check(G, logits, scores, done=None, eos=-1, k=4, **kw):
     for b in range(batch):
         want, total = reference(logits[b * beams:(b + 1) * beams], scores[b], None if done is None else done[b], eos, k)
         parent, token, score, done_out = (None if x is None else x[b] for x in got)
-        n = len(want)
+        n = len(want)                                                 # (k, or all that there are)
         assert np.all(parent[n:] == -1) and np.all(token[n:] == -1) and np.all(score[n:] == -np.inf)
         assert np.all((parent[:n] >= 0) & (parent[:n] < beams) & (token[:n] >= 0) & (token[:n] < logits.shape[1]))
         assert len(set(zip(parent[:n], token[:n]))) == n
@@ -116,6 +117,8 @@ def check(G, logits, scores, done=None, eos=-1, k=4, **kw):
         if done_out is not None:
             ended = np.array([(done is not None and done[b][p] != 0) or t == eos for p, t in zip(parent[:n], token[:n])], dtype=np.int32)
             assert np.array_equal(done_out[:n], ended) and np.all(done_out[n:] == 0)
+        some = sum(w[0] > -np.inf for w in want)
+        assert [(int(p), int(t)) for p, t in zip(parent[some:n], token[some:n])] == [w[1:] for w in want[some:]]
         with np.errstate(invalid="ignore"):
             near = (score[:n] == mine) | (np.abs(score[:n] - mine) <= LSE_OFF + 2.0 ** -24 * np.abs(mine))
         assert np.all(near), (b, score[:n], mine)
@@ -127,7 +130,7 @@ def check(G, logits, scores, done=None, eos=-1, k=4, **kw):
         # totals of different beams at the places where their order decides: apart, or the same beam's
         rest = sorted(((-total[r, t], r) for r in range(beams) for t in np.argsort(-total[r], kind="stable")[:k + 1]))[:k + 1]
         with np.errstate(invalid="ignore"):
-            apart = all(x[1] == y[1] or not y[0] - x[0] <= 2 * LSE_OFF for x, y in zip(rest, rest[1:]))
+            apart = all(x[1] == y[1] or y[0] == np.inf or not y[0] - x[0] <= 2 * LSE_OFF for x, y in zip(rest, rest[1:]))
         if apart:
             assert [(int(p), int(t)) for p, t in zip(parent[:n], token[:n])] == [w[1:] for w in want], b
             clear += 1
@@ -291,3 +294,20 @@ def test_reorder(G, groups, width, kv, d, capacity, longest):
         assert np.array_equal(cache.tail.view(torch.int16).cpu().numpy().view(np.uint16), want[2])
         if kind != "one":
             assert np.array_equal(out.cpu().numpy(), after)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("beams,vocab,k", [(1, 100, 2), (2, 3, 6), (2, 3, 10), (4, 64, 64), (1, 1, 3), (64, 70, 64)])
+def test_fewer_than_asked_for(G, beams, vocab, k):
+    """Beams that have finished, beams without a score, logits without a probability: what is left follows by beam and token."""
+    rng = np.random.default_rng(beams + k)
+    logits, scores = _logits(rng, 5 * beams, vocab), _scores(rng, 5, beams)
+    done = np.ones((5, beams), np.int32)
+    done[1, ::2] = 0
+    done[2:] = 0
+    scores[1, ::2] = -np.inf
+    scores[2] = -np.inf
+    logits[3 * beams:4 * beams, 1:] = -np.inf
+    logits[4 * beams:] = np.nan
+    check(G, logits, scores, done, eos=vocab - 1, k=k)
+    check(G, logits, scores, done, eos=0, k=k, odd=True)
