@@ -241,24 +241,25 @@ __device__ __forceinline__ u64 total_key(double v)
 __device__ __forceinline__ double total_of(u64 key) { return __longlong_as_double((long long)(key >> 63 ? key & ~(1ull << 63) : ~key)); }
 constexpr int kTieBeam = 36, kTieKey = 20;                            // (tokens have 20 bits, keys 16)
 
-// One workgroup per batch element: the rows' sums from their slabs', then the best k of all their candidates, as in beam_rows_kernel: the threads' best,
-// a number that k of them reach, the few candidates that reach it ranked.
-constexpr int kSurvivors = 2048;
-__global__ __launch_bounds__(kBeamT) void beam_select_kernel(const BeamArgs a)
+// One workgroup per batch element: the rows' sums from their slabs', then the best k of all their candidates, as in beam_rows_kernel: the best of each of 256
+// groups of threads, a number that k of those reach, the few candidates that reach it ranked.
+constexpr int kSurvivors = 2048, kGroups = 256;
+template <int T>
+__global__ __launch_bounds__(T) void beam_select_kernel(const BeamArgs a)
 {
-    __shared__ Candidate tops[kBeamT], list[kSurvivors];
+    constexpr int WAVES = T / 64, KEPT = 8;                           // candidates that a thread keeps; of more, it works out the others again
+    __shared__ Candidate tops[kGroups], list[kSurvivors];
     __shared__ float top[kBeamMost];
     __shared__ double log_sum[kBeamMost], score[kBeamMost];
-    __shared__ int ended[kBeamMost], listed, counts[kBeamWaves];
+    __shared__ int ended[kBeamMost], listed, counts[WAVES];
     const int t = threadIdx.x, l = t & 63, wave = t >> 6, each = a.slabs * a.k, all = a.beams * each;
     const int64_t b = blockIdx.x, row0 = b * a.beams;
     if (t == 0) listed = 0;
-    constexpr int KEPT = 4;                                           // candidates that a thread keeps; of more, it works out the others again
     v2u words[KEPT];
 #pragma unroll
-    for (int i = 0; i < KEPT; ++i) words[i] = a.best[row0 * each + min(t + i * kBeamT, all - 1)];
+    for (int i = 0; i < KEPT; ++i) words[i] = a.best[row0 * each + min(t + i * T, all - 1)];
     // rows' sums: eight lanes each
-    for (int r0 = 0; r0 < a.beams; r0 += kBeamT / 8) {
+    for (int r0 = 0; r0 < a.beams; r0 += T / 8) {
         const int r = r0 + t / 8, i0 = t % 8;
         if (r >= a.beams) break;                                      // (all eight lanes)
         const bool done = a.done && a.done[row0 + r] != 0;
@@ -310,20 +311,33 @@ __global__ __launch_bounds__(kBeamT) void beam_select_kernel(const BeamArgs a)
         x.tie = (u64)(kBeamMost - 1 - r) << kTieBeam | (u64)have[0] << kTieKey | ((1u << kTieKey) - 1 - have[1]);
         return x;
     };
-    auto candidate = [&](int c) { return candidate_of(c, a.best[row0 * each + c]); };
     Candidate kept[KEPT], mine = {0, 0};
 #pragma unroll
     for (int i = 0; i < KEPT; ++i) {
-        kept[i] = t + i * kBeamT < all ? candidate_of(t + i * kBeamT, words[i]) : Candidate{0, 0};
+        kept[i] = t + i * T < all ? candidate_of(t + i * T, words[i]) : Candidate{0, 0};
         if (before(kept[i], mine)) mine = kept[i];
     }
-    for (int c = t + KEPT * kBeamT; c < all; c += kBeamT) {
-        const Candidate x = candidate(c);
+    auto others = [&](auto enter) {                                   // four asked for at a time
+        for (int c0 = t + KEPT * T; c0 < all; c0 += 4 * T) {
+            v2u w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = a.best[row0 * each + min(c0 + i * T, all - 1)];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (c0 + i * T < all) enter(candidate_of(c0 + i * T, w[i]));
+        }
+    };
+    others([&](const Candidate &x) {
+        if (before(x, mine)) mine = x;
+    });
+#pragma unroll
+    for (int d = 1; d < T / kGroups; d <<= 1) {
+        const Candidate x = {(u64)__shfl_xor((unsigned long long)mine.total, d), (u64)__shfl_xor((unsigned long long)mine.tie, d)};
         if (before(x, mine)) mine = x;
     }
-    tops[t] = mine;
+    if (t % (T / kGroups) == 0) tops[t / (T / kGroups)] = mine;
     __syncthreads();
-    // (all wavefronts the same: four of the threads' best to a lane)
+    // (all wavefronts the same: the best of four groups to a lane)
     Candidate four[4], reach = {0, 0};
 #pragma unroll
     for (int i = 0; i < 4; ++i) four[i] = tops[4 * l + i];
@@ -364,7 +378,7 @@ __global__ __launch_bounds__(kBeamT) void beam_select_kernel(const BeamArgs a)
         };
 #pragma unroll
         for (int i = 0; i < KEPT; ++i) enter(kept[i]);
-        for (int c = t + KEPT * kBeamT; c < all; c += kBeamT) enter(candidate(c));
+        others(enter);
     };
     list_them();
     __syncthreads();
@@ -372,15 +386,18 @@ __global__ __launch_bounds__(kBeamT) void beam_select_kernel(const BeamArgs a)
         reach = Candidate{0, 0};
         auto count = [&](const Candidate &from) {
             int n = 0;
-            if (!before(from, mine))
-                for (int c = t; c < all; c += kBeamT) n += before(from, candidate(c)) ? 0 : 1;
+            if (!before(from, mine)) {
+#pragma unroll
+                for (int i = 0; i < KEPT; ++i) n += before(from, kept[i]) ? 0 : 1;
+                others([&](const Candidate &x) { n += before(from, x) ? 0 : 1; });
+            }
 #pragma unroll
             for (int i = 32; i > 0; i >>= 1) n += __shfl_xor(n, i);
             __syncthreads();
             if (l == 0) counts[wave] = n;
             __syncthreads();
             n = 0;
-            for (int w = 0; w < kBeamWaves; ++w) n += counts[w];
+            for (int w = 0; w < WAVES; ++w) n += counts[w];
             return n;
         };
         search([&](u64 from) { return count(Candidate{from, 0}); }, count);
@@ -392,7 +409,7 @@ __global__ __launch_bounds__(kBeamT) void beam_select_kernel(const BeamArgs a)
     const int n = min(listed, kSurvivors);
     int32_t *parent = a.parent + b * a.k, *token = a.token + b * a.k, *done_out = a.done_out ? a.done_out + b * a.k : nullptr;
     float *out = a.score + b * a.k;
-    for (int i = t; i < n; i += kBeamT) {
+    for (int i = t; i < n; i += T) {
         const Candidate own = list[i];
         int rank = 0;
         for (int j = 0; j < n; ++j) rank += before(list[j], own) ? 1 : 0;
@@ -405,7 +422,7 @@ __global__ __launch_bounds__(kBeamT) void beam_select_kernel(const BeamArgs a)
     }
     if (n >= a.k) return;
     // Fewer than k with a probability, all of them listed: the others follow in the order of their places, at most k + n of which have to be looked at.
-    static_assert(2 * kBeamMost <= kBeamT, "a place for each thread");
+    static_assert(2 * kBeamMost <= T, "a place for each thread");
     const int64_t places = (int64_t)a.beams * a.vocab;
     bool is_listed = t >= places;
     int behind = t;                                                   // places in front that are not listed
@@ -428,11 +445,11 @@ __global__ __launch_bounds__(kBeamT) void beam_select_kernel(const BeamArgs a)
     }
 }
 
-// Slabs as large as leave the device its workgroups.
+// Slabs as large as leave the device its workgroups, and no larger than a row.
 static int beam_pieces(int64_t rows, int vocab)
 {
     for (int pieces = 8; pieces > 1; pieces /= 2)
-        if (rows * ((vocab + kBeamT * 8 * pieces - 1) / (kBeamT * 8 * pieces)) >= 256) return pieces;
+        if (vocab > kBeamT * 4 * pieces && rows * ((vocab + kBeamT * 8 * pieces - 1) / (kBeamT * 8 * pieces)) >= 256) return pieces;
     return vocab > 64 * kBeamT * 8 ? 8 : 1;
 }
 static int beam_slabs(int64_t rows, int vocab)
@@ -462,7 +479,9 @@ sqap_status launch_beam_select(const __half *logits, int64_t ld, int batch, int 
     default: hipLaunchKernelGGL(beam_rows_kernel<1>, grid, block, 0, st, a); break;
     }
     SQAP_HIP_CHECK(hipGetLastError());
-    hipLaunchKernelGGL(beam_select_kernel, dim3(batch), block, 0, st, a);
+    // (up to 2048 candidates: 4 beams of 32000 10.4 us, with 1024 threads 11.7; 26908 of them, 31 beams with 62 outputs: 106 us and 35)
+    if (beams * slabs * k <= 2048) hipLaunchKernelGGL(beam_select_kernel<256>, dim3(batch), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(beam_select_kernel<1024>, dim3(batch), dim3(1024), 0, st, a);
     SQAP_HIP_CHECK(hipGetLastError());
     return SQAP_OK;
 }
