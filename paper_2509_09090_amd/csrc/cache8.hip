@@ -823,7 +823,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
 // equal shares of each, would take 430).  A tile inside a workgroup's range is finished there; of one over its ends, the workgroups leave their sums,
 // one at the beginning and one at the end of each range, and cache8_long_join_kernel adds them.  Ranges are counted in tiles as long as their
 // sequence's longest (a tile's real blocks, fewer where its rows see less, are parted in the same proportion).
-constexpr int kLongBatch = 1024, kLongParts = 32, kLongLeast = 4;
+constexpr int kLongBatch = 1024, kLongParts = 32, kLongLeast = 4, kLongTiles = 64;
 struct LongSlot {                // what a workgroup's first range belongs to, where it is the rest of a tile
     int b, kh, tile, first, count;       // the workgroup that begins the tile, how many have a share of it; count 0: none, or not its second
     int pad[3];
@@ -1334,16 +1334,13 @@ __global__ __launch_bounds__(64 * kFewRowsWaves, 2) void cache8_few_rows_kernel(
 }
 
 // Few rows behind a prefix that is not long: the same over the prefix's blocks and the sequence's own, which are dealt out together; no parts.
-template <int D>
+template <int D, int WAVES, int TAILS>
 struct ShortLds {
     __attribute__((aligned(16))) union {
-        struct {
-            unsigned short k[kBlock][D + 8];
-            unsigned short v[D][kBlock + 8];
-        } tail[2];                               // of the prefix, of the sequence
-        float o[kFewRowsWaves][16][D + 4];
+        unsigned short v[TAILS][D][kBlock + 8];  // unfinished values: of the prefix (where it takes part), of the sequence
+        float o[WAVES][16][D + 4];
     } u;
-    float m[kFewRowsWaves][16], l[kFewRowsWaves][16];
+    float m[WAVES][16], l[WAVES][16];
     int not_finite[2];
 };
 struct ShortArgs {
@@ -1357,21 +1354,28 @@ struct ShortArgs {
     int64_t ldo;
     int tiles;
 };
-template <int D>
-__global__ __launch_bounds__(64 * kFewRowsWaves, 2) void cache8_short_kernel(const ShortArgs a)
+template <int D, int WAVES, Part PART>
+__global__ __launch_bounds__(64 * WAVES, 2) void cache8_short_kernel(const ShortArgs a)
 {
-    constexpr int C = D / 64, DT = D / 16, T = 64 * kFewRowsWaves, UNITS = kBlock * D / 8 / T;
+    constexpr int C = D / 64, DT = D / 16, T = 64 * WAVES, OF_TAIL = kBlock / 4 * D / 8, TAILS = PART == Part::Own ? 1 : 2, UNITS = (TAILS * OF_TAIL + T - 1) / T;
     extern __shared__ __attribute__((aligned(16))) uint8_t raw_lds[];
-    ShortLds<D> &lds = *reinterpret_cast<ShortLds<D> *>(raw_lds);
+    using Lds = ShortLds<D, WAVES, TAILS>;
+    Lds &lds = *reinterpret_cast<Lds *>(raw_lds);
     const Cache8View &cache = a.cache, &prefix = a.prefix;
     const int pairs = cache.kv_heads * cache.batch, id = blockIdx.x, pair = id % pairs, number = id / pairs;
-    const int b = pair / cache.kv_heads, kh = pair % cache.kv_heads, group = b / a.parts.width;
+    const int b = pair / cache.kv_heads, kh = pair % cache.kv_heads, group = PART == Part::Own ? 0 : b / a.parts.width;
     const int t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), r = l & 15, g = l >> 4, G = a.H / cache.kv_heads;
-    const Member member = member_of(a.starts, a.past, b, a.rows, a.max_new, cache.blocks * kBlock, prefix.blocks * kBlock, a.parts);
+    Member member;
+    if constexpr (PART == Part::Own) {
+        const Span own = span_of(a.starts, a.past, b, a.rows, a.max_new, cache.blocks * kBlock);
+        member = {own, true, own.fits, 0};
+    } else {
+        member = member_of(a.starts, a.past, b, a.rows, a.max_new, cache.blocks * kBlock, prefix.blocks * kBlock, a.parts);
+    }
     if (!member.rows) return;
     const Span &sp = member.sp;
     if (!member.fits) {
-        nan_rows<D>(a.O, a.ldo, sp.row, (int64_t)sp.n * G, G, kh, number, a.tiles, 16);
+        if constexpr (PART == Part::Whole) nan_rows<D>(a.O, a.ldo, sp.row, (int64_t)sp.n * G, G, kh, number, a.tiles, 16);
         return;
     }
     const int n_rows = sp.n * G, tile = (a.tiles - 1 - number) * 16;
@@ -1380,17 +1384,19 @@ __global__ __launch_bounds__(64 * kFewRowsWaves, 2) void cache8_short_kernel(con
     const int last = sp.past + (min(tile + 16, n_rows) - 1) / G, end = sp.past + sp.n;
     // finished blocks of the prefix, then own ones that some row sees; then the unfinished ones
     const int of_prefix = member.length / kBlock, finished = of_prefix + min(last / kBlock + 1, end / kBlock);
-    const int rest[2] = {member.length % kBlock, last / kBlock == end / kBlock ? end % kBlock : 0};
+    const int prefix_rest = member.length % kBlock, own_rest = last / kBlock == end / kBlock ? end % kBlock : 0;
+    auto rest = [&](int x) { return PART != Part::Own && x == 0 ? prefix_rest : own_rest; };
     const int64_t heads[2] = {(int64_t)group * prefix.kv_heads + kh, (int64_t)b * cache.kv_heads + kh};
-    const __half *tails[2] = {prefix.tail + heads[0] * 2 * kBlock * D, cache.tail + heads[1] * 2 * kBlock * D};
+    const __half *const prefix_tail = prefix.tail + heads[0] * 2 * kBlock * D, *const own_tail = cache.tail + heads[1] * 2 * kBlock * D;
+    auto tail = [&](int x) { return PART != Part::Own && x == 0 ? prefix_tail : own_tail; };
     v4i kraw[4 * C], vraw[DT];
     float2 sc = {0.f, 0.f};
     auto codes_of = [&](int j, int values) {
-        return reinterpret_cast<const v4i *>(j < of_prefix ? block_codes<D>(prefix, heads[0], j, values) : block_codes<D>(cache, heads[1], j - of_prefix, values)) + l;
+        return reinterpret_cast<const v4i *>(PART != Part::Own && j < of_prefix ? block_codes<D>(prefix, heads[0], j, values) : block_codes<D>(cache, heads[1], j - of_prefix, values)) + l;
     };
     auto fetch_keys = [&](int j) {
         if (j >= finished) return;
-        sc = *reinterpret_cast<const float2 *>(j < of_prefix ? prefix.scales + (heads[0] * prefix.blocks + j) * 2 : cache.scales + (heads[1] * cache.blocks + j - of_prefix) * 2);
+        sc = *reinterpret_cast<const float2 *>(PART != Part::Own && j < of_prefix ? prefix.scales + (heads[0] * prefix.blocks + j) * 2 : cache.scales + (heads[1] * cache.blocks + j - of_prefix) * 2);
         const v4i *k = codes_of(j, 0);
 #pragma unroll
         for (int i = 0; i < 4 * C; ++i) kraw[i] = k[i * 64];
@@ -1401,18 +1407,17 @@ __global__ __launch_bounds__(64 * kFewRowsWaves, 2) void cache8_short_kernel(con
 #pragma unroll
         for (int i = 0; i < DT; ++i) vraw[i] = v[i * 64];
     };
-    v4i tk[2][UNITS], tv[2][UNITS];
+    // unfinished values, 4 positions of 8 columns at a time
+    v4i tv[UNITS][4];
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int i = 0; i < UNITS; ++i) {
+        const int u = t + i * T, x = u / OF_TAIL + 2 - TAILS, s = u % OF_TAIL / (D / 8) * 4, col = u % (D / 8) * 8;
 #pragma unroll
-        for (int i = 0; i < UNITS; ++i) {
-            const int u = t + i * T, s = u / (D / 8), col = (u % (D / 8)) * 8;
-            tk[x][i] = tv[x][i] = v4i{0, 0, 0, 0};
-            if (s < rest[x]) {
-                tk[x][i] = *reinterpret_cast<const v4i *>(tails[x] + s * D + col);
-                tv[x][i] = *reinterpret_cast<const v4i *>(tails[x] + kBlock * D + s * D + col);
-            }
+        for (int p = 0; p < 4; ++p) {
+            tv[i][p] = v4i{0, 0, 0, 0};
+            if (x < 2 && s + p < rest(x)) tv[i][p] = *reinterpret_cast<const v4i *>(tail(x) + (kBlock + s + p) * D + col);
         }
+    }
     fetch_keys(wave);
     fetch_values(wave);
     v8h q[2 * C];
@@ -1422,26 +1427,26 @@ __global__ __launch_bounds__(64 * kFewRowsWaves, 2) void cache8_short_kernel(con
     if (t < 2) lds.not_finite[t] = 0;
     __syncthreads();
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        if (rest[x] == 0) continue;
+    for (int i = 0; i < UNITS; ++i) {
+        const int u = t + i * T, x = u / OF_TAIL + 2 - TAILS, s = u % OF_TAIL / (D / 8) * 4, col = u % (D / 8) * 8, at = value_slot(s);
+        if (x >= 2 || rest(x) == 0) continue;
         bool odd = false;
 #pragma unroll
-        for (int i = 0; i < UNITS; ++i) {
-            const int u = t + i * T, s = u / (D / 8), col = (u % (D / 8)) * 8, at = value_slot(s);
-            *reinterpret_cast<v4i *>(&lds.u.tail[x].k[s][col]) = tk[x][i];
+        for (int e = 0; e < 8; ++e) {
+            unsigned w[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                unsigned short w = (unsigned short)((unsigned)tv[x][i][e >> 1] >> (16 * (e & 1)));
-                if ((w & 0x7fffu) >= 0x7c00u) w = 0, odd = true;      // comes back at the end, to the rows that see it
-                lds.u.tail[x].v[col + e][value_place(col + e, at)] = w;
+            for (int p = 0; p < 4; ++p) {
+                w[p] = (unsigned)tv[i][p][e >> 1] >> (16 * (e & 1)) & 0xffffu;
+                if ((w[p] & 0x7fffu) >= 0x7c00u) w[p] = 0, odd = true;      // comes back at the end, to the rows that see it
             }
+            *reinterpret_cast<v2u *>(&lds.u.v[x - 2 + TAILS][col + e][value_place(col + e, at)]) = v2u{w[0] | w[1] << 16, w[2] | w[3] << 16};
         }
         if (odd) lds.not_finite[x] = 1;
     }
     __syncthreads();
     WaveSums<D> sums;
     int j = wave;
-    for (; j < finished; j += kFewRowsWaves) {
+    for (; j < finished; j += WAVES) {
         const float2 scale = sc;
         const int at_own = (j - of_prefix) * kBlock;
         sums.add(
@@ -1450,17 +1455,19 @@ __global__ __launch_bounds__(64 * kFewRowsWaves, 2) void cache8_short_kernel(con
                 const v4i w = kraw[T4 * C + (m >> 1)];
                 return (m & 1) ? halves_of(w[2], w[3]) : halves_of(w[0], w[1]);
             },
-            [&](int i, int n) { return halves_of(vraw[i][2 * n], vraw[i][2 * n + 1]); }, [&] { fetch_keys(j + kFewRowsWaves); });
-        fetch_values(j + kFewRowsWaves);
+            [&](int i, int n) { return halves_of(vraw[i][2 * n], vraw[i][2 * n + 1]); }, [&] { fetch_keys(j + WAVES); });
+        fetch_values(j + WAVES);
     }
     j -= finished;                                                    // the unfinished ones go to the wavefronts whose turn it is
-    int which = rest[0] > 0 ? 0 : 1, left = (rest[0] > 0) + (rest[1] > 0);
+    int which = prefix_rest > 0 ? 0 : 1, left = (prefix_rest > 0) + (own_rest > 0);
     if (j == 1 && left == 2) which = 1;
-    if (j < left)
+    if (j < left) {
+        const __half *keys = tail(which);
         sums.add(
-            q, 1.f, 1.f, true, which == 0 ? rest[0] - 1 : min(sees - end / kBlock * kBlock, rest[1] - 1),
-            [&](int T4, int m) { return *reinterpret_cast<const v8h *>(&lds.u.tail[which].k[16 * T4 + r][64 * (m >> 1) + 16 * g + 8 * (m & 1)]); },
-            [&](int i, int n) { return *reinterpret_cast<const v8h *>(&lds.u.tail[which].v[16 * i + r][value_place(16 * i + r, 32 * n + 8 * g)]); }, [] {});
+            q, 1.f, 1.f, true, which == 0 ? prefix_rest - 1 : min(sees - end / kBlock * kBlock, own_rest - 1),
+            [&](int T4, int m) { return *reinterpret_cast<const v8h *>(keys + min(16 * T4 + r, rest(which) - 1) * D + 64 * (m >> 1) + 16 * g + 8 * (m & 1)); },
+            [&](int i, int n) { return *reinterpret_cast<const v8h *>(&lds.u.v[which - 2 + TAILS][16 * i + r][value_place(16 * i + r, 32 * n + 8 * g)]); }, [] {});
+    }
     sums.l += __shfl_xor(sums.l, 16);
     sums.l += __shfl_xor(sums.l, 32);
     __syncthreads();                                                  // the tails' rows have been read
@@ -1471,36 +1478,53 @@ __global__ __launch_bounds__(64 * kFewRowsWaves, 2) void cache8_short_kernel(con
         lds.l[wave][r] = sums.l;
     }
     __syncthreads();
-    const int waves = min(finished + left, kFewRowsWaves), row = t / (D / 4), col = t % (D / 4) * 4;          // four columns of a row
-    if (row >= 16 || tile + row >= n_rows) return;
-    const int of = (tile + row) / G;
-    float top = -INFINITY, sum = 0.f;
-    for (int w = 0; w < waves; ++w) top = fmaxf(top, lds.m[w][row]);
-    v4f o = {0.f, 0.f, 0.f, 0.f};
-    for (int w = 0; w < waves; ++w) {
-        const float f = exp2f(lds.m[w][row] - top);
-        sum += f * lds.l[w][row];
-        o += f * *reinterpret_cast<const v4f *>(&lds.u.o[w][row][col]);
-    }
-    const float norm = 1.f / sum;
-    union { __half h[4]; v2u v; } out;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float y = o[i] * norm;
-#pragma unroll 1
-        for (int x = 0; x < 2; ++x) {
-            if (!lds.not_finite[x]) continue;                         // infinities and NaN among a tail's values that this row sees
-            y = __half2float(__float2half_rn(y));
-            const int seen = x == 0 ? rest[0] : sp.past + of - end / kBlock * kBlock + 1;
-#pragma unroll 1
-            for (int s = 0; s < seen; ++s) {
-                const float v = __half2float(tails[x][kBlock * D + s * D + col + i]);
-                if (!(fabsf(v) <= 65504.f)) y += v;
-            }
+    const int waves = min(finished + left, WAVES), col = t % (D / 4) * 4;          // four columns of a row
+    for (int row = t / (D / 4); row < 16 && tile + row < n_rows; row += T / (D / 4)) {
+        const int of = (tile + row) / G;
+        float top = -INFINITY, sum = 0.f;
+        for (int w = 0; w < waves; ++w) top = fmaxf(top, lds.m[w][row]);
+        const float taken = PART == Part::Own && top == -INFINITY ? 0.f : top;
+        v4f o = {0.f, 0.f, 0.f, 0.f};
+        for (int w = 0; w < waves; ++w) {
+            const float f = exp2f(lds.m[w][row] - taken);
+            sum += f * lds.l[w][row];
+            o += f * *reinterpret_cast<const v4f *>(&lds.u.o[w][row][col]);
         }
-        out.h[i] = __float2half_rn(y);
+        if constexpr (PART == Part::Own) {
+            const int64_t place = a.parts.prefix_shares * a.parts.pairs + (int64_t)(sp.row + of) * a.H + kh * G + tile + row - of * G;
+            if (lds.not_finite[1]) {                                  // (as below)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll 1
+                    for (int s = 0; s <= sp.past + of - end / kBlock * kBlock; ++s) {
+                        const float v = __half2float(own_tail[kBlock * D + s * D + col + i]);
+                        if (!(fabsf(v) <= 65504.f)) o[i] += v;
+                    }
+            }
+            if (col == 0) a.parts.ml[place] = {top, sum};
+            *reinterpret_cast<v4f *>(a.parts.o + place * D + col) = o;
+            continue;
+        }
+        const float norm = 1.f / sum;
+        union { __half h[4]; v2u v; } out;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float y = o[i] * norm;
+#pragma unroll 1
+            for (int x = 0; x < 2; ++x) {
+                if (!lds.not_finite[x]) continue;                         // infinities and NaN among a tail's values that this row sees
+                y = __half2float(__float2half_rn(y));
+                const int seen = x == 0 ? prefix_rest : sp.past + of - end / kBlock * kBlock + 1;
+#pragma unroll 1
+                for (int s = 0; s < seen; ++s) {
+                    const float v = __half2float(tail(x)[kBlock * D + s * D + col + i]);
+                    if (!(fabsf(v) <= 65504.f)) y += v;
+                }
+            }
+            out.h[i] = __float2half_rn(y);
+        }
+        *reinterpret_cast<v2u *>(a.O + (int64_t)(sp.row + of) * a.ldo + (int64_t)(kh * G + tile + row - of * G) * D + col) = out.v;
     }
-    *reinterpret_cast<v2u *>(a.O + (int64_t)(sp.row + of) * a.ldo + (int64_t)(kh * G + tile + row - of * G) * D + col) = out.v;
 }
 
 // ---------------------------------------------------------------- attention of one row per sequence
@@ -2204,10 +2228,27 @@ sqap_status launch_cache8_read(const Cache8View &cache, int d, const int32_t *le
     return SQAP_OK;
 }
 
+template <int D, int WAVES, Part PART>
+static sqap_status launch_short(const ShortArgs &a, hipStream_t st)
+{
+    constexpr int LDS = sizeof(ShortLds<D, WAVES, PART == Part::Own ? 1 : 2>);
+    static std::atomic<bool> ready[kMaxDeviceSlots];
+    if (!ready[device_slot()].load(std::memory_order_relaxed)) {
+        SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(cache8_short_kernel<D, WAVES, PART>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+        ready[device_slot()].store(true, std::memory_order_relaxed);
+    }
+    hipLaunchKernelGGL((cache8_short_kernel<D, WAVES, PART>), dim3((unsigned)a.tiles * a.cache.kv_heads * a.cache.batch), dim3(64 * WAVES), LDS, st, a);
+    SQAP_HIP_CHECK(hipGetLastError());
+    return SQAP_OK;
+}
+
 // Tiles of 16 rows, whose blocks are dealt to eight wavefronts, where there would be few tiles of 128: 148 rows of 32 heads (64 of those) take
 // 9.0 us so and 11.0 otherwise, 512 of 8 heads (32) 8.0 and 19.0, 20 of 32 heads over 8 behind 2000 (8) 18 and 62, 1500 of 8 behind 2000
 // (96) 67 and 103, 300 of 32 heads (96) 13.9 and 15.1; but 500 of 32 (128) 23.7 and 21.3, 1000 of 32 over 8 (256) 56 and 37.
 constexpr int kFewTiles = 96;
+// Parts of many sequences with up to 32 rows each: cache8_short_kernel, whose two wavefronts and two workgroups' LDS leave four to a CU, in place of tiles of
+// 128 that are almost empty (512 x 2 rows of 32 heads over 8, prefix and join included, 86 us and 119; 700 x 2 of 12 heads 58 and 89).
+constexpr int kShortTiles = 512, kOwnTiles = 2;
 
 template <int D, Part PART>
 static sqap_status launch_attention_d(const __half *Q, int64_t ldq, const int32_t *starts, const int32_t *past, int rows, int max_new, int H,
@@ -2225,6 +2266,10 @@ static sqap_status launch_attention_d(const __half *Q, int64_t ldq, const int32_
     const int64_t pairs = (int64_t)cache.kv_heads * cache.batch;
     const bool few = tiles_of(32 * WAVES) * pairs <= kFewTiles;
     const int64_t tiles = tiles_of(few ? 16 : 32 * WAVES), items = tiles * pairs;
+    if constexpr (PART == Part::Own) {
+        if (tiles_of(16) * pairs > kShortTiles && tiles_of(16) <= kOwnTiles)
+            return launch_short<D, 2, Part::Own>(ShortArgs{Q, ldq, starts, past, rows, max_new, H, cache, cache, parts, nullptr, 0, (int)tiles_of(16)}, st);
+    }
     if (few)
         hipLaunchKernelGGL((cache8_few_rows_kernel<D, PART>), dim3((unsigned)items), dim3(64 * kFewRowsWaves), sizeof(FewRowsLds<D>), st, Q, ldq, starts, past, rows,
                            max_new, H, cache, O, ldo, (int)tiles, parts);
@@ -2300,13 +2345,17 @@ sqap_status launch_cache8_decode(const __half *QKV, int64_t ld, const int32_t *p
 // How the prefixes are dealt out: shares of two blocks to a wavefront (64 rows of 32 heads over 8 behind 1000 positions 16.3 us, with one 20.4), of one up to 8 blocks.  Up to 64 pairs to a group and key head: tiles of 16, blocks dealt to the wavefronts; up to 256 of them, too, where all
 // tiles together have no more than 20000 blocks: the tiles of 128 want two launches more (32 rows of 32 heads over 8 behind 1000 positions 14 and
 // 27 us, behind 20000 45 and 48, behind 100003 187 and 128; 64 behind 1000 23 and 29).
-// Prompts of few rows: tiles of 16 that pass over prefix and own positions by themselves, while they are up to 12000 blocks in all (16 x 10 rows of 32
-// heads over 8 behind 1000 positions, 6144: 25 us, in parts 30; behind 4000 54 and 39; 16 x 20 of 32 heads, 16384: 39 and 36) and prefixes up to 48 blocks
-// long, or 256 tiles (10 rows behind 1000 positions 13 and 20, behind 4000 27 and 24).
-constexpr int kShortBlocks = 12000, kShortPrefix = 48;
+// Prompts of few rows: tiles of 16 that pass over prefix and own positions by themselves.  Up to 512 tiles, which the device holds at once, with eight
+// wavefronts, while they are up to 12000 blocks in all (16 x 10 rows of 32 heads over 8 behind 1000 positions, 6144: 25 us, in parts 30; behind 4000 54
+// and 39) and prefixes up to 48 blocks long, or 256 tiles (10 rows behind 1000 positions 13 and 20, behind 4000 27 and 24).  More tiles with two wavefronts,
+// four to a CU (128 x 4 rows of 32 heads over 8 behind 100 positions 16.5 us, with eight 27), where they repeat the prefixes' blocks no more than 20 times
+// as often as full tiles of 16 over one block would (256 x 4 rows behind 500 positions, 8 times: 42 us, in parts 59; behind 1000, 16: 57 and 63; 243 x 7 of 12
+// heads behind 798, 30: 61 and 52; 512 x 2 behind 600, 20: 92 and 64, behind 2000, 64: 208 and 86).
+constexpr int kShortBlocks = 12000, kShortPrefix = 48, kShortRepeats = 20;
 constexpr int kFewPairs = 64, kFewPairsAtMost = 256, kFewBlocks = 20000, kPrefixGroups = 512, kMostPrefixShares = 64;
 struct SharedPlan {
-    bool together, direct;       // long prompts: cache8_long_kernel; short ones: cache8_short_kernel
+    bool together, direct;       // long prompts: cache8_long_kernel; short ones: cache8_short_kernel,
+    int waves;                   // with so many wavefronts
     int groups;                  // its workgroups
     bool few;
     int64_t tiles;               // of a group and key head
@@ -2326,8 +2375,9 @@ static SharedPlan shared_plan(bool prompt, int batch, int groups, int H, int kv_
     p.own_shares = own_shares;
     p.pairs = (int64_t)rows * H;
     const auto up = [](size_t n) { return (n + 15) / 16 * 16; };
-    // rows that fill three quarters of a tile on average
-    p.together = max_new > 1 && batch <= kLongBatch && (int64_t)rows * (H / kv_heads) >= (int64_t)batch * 96;
+    // rows that fill three quarters of a tile on average, and 64 tiles (128 rows of 32 heads over 8, 32 tiles, behind 2000 positions 47 us and 20 otherwise,
+    // behind 20000 110 and 91; 64 tiles behind 2000 46 and 45; 330 behind 6000 194 and 279)
+    p.together = max_new > 1 && batch <= kLongBatch && (int64_t)rows * (H / kv_heads) >= (int64_t)batch * 96 && (int64_t)rows * H >= 128 * kLongTiles;
     if (p.together) {
         p.groups = std::max(8, device_cu_count() * 2 / 8 * 8);
         p.ml = kCounterBytes + (size_t)p.groups * sizeof(LongSlot);
@@ -2335,9 +2385,9 @@ static SharedPlan shared_plan(bool prompt, int batch, int groups, int H, int kv_
         p.bytes = p.o + (size_t)p.groups * 256 * d * sizeof(float);
         return p;
     }
-    // few tiles of 16 rows and blocks of prefixes in all, and not many blocks to a wavefront
     const int64_t tiles = ((int64_t)max_new * (H / kv_heads) + 15) / 16 * kv_heads * batch;
-    p.direct = prompt && tiles * blocks <= kShortBlocks && (blocks <= kShortPrefix || tiles >= 256);
+    p.waves = tiles <= kShortTiles ? kFewRowsWaves : 2;
+    p.direct = prompt && (tiles <= kShortTiles ? tiles * blocks <= kShortBlocks && (blocks <= kShortPrefix || tiles >= 256) : tiles * 16 * blocks < kShortRepeats * (int64_t)rows * H);
     if (p.direct) return p;                                           // (no workspace)
     p.q = kCounterBytes;                                              // (left alone, for calls that want it zero)
     p.ml = p.q + (max_new == 1 ? up((size_t)p.pairs * d * 2) : 0);
@@ -2413,16 +2463,9 @@ static sqap_status launch_shared_d(const __half *Q, int64_t ldq, const int32_t *
         return SQAP_OK;
     }
     if (plan.direct) {
-        static std::atomic<bool> ready[kMaxDeviceSlots];
-        if (!ready[device_slot()].load(std::memory_order_relaxed)) {
-            SQAP_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(cache8_short_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(ShortLds<D>)));
-            ready[device_slot()].store(true, std::memory_order_relaxed);
-        }
         const int tiles = std::max(1, (max_new * (H / cache.kv_heads) + 15) / 16);
-        hipLaunchKernelGGL(cache8_short_kernel<D>, dim3((unsigned)tiles * cache.kv_heads * cache.batch), dim3(64 * kFewRowsWaves), sizeof(ShortLds<D>), st,
-                           ShortArgs{Q, ldq, starts, past, rows, max_new, H, cache, prefix, Parts{nullptr, nullptr, 0, 0, cache.batch / prefix.batch, length}, O, ldo, tiles});
-        SQAP_HIP_CHECK(hipGetLastError());
-        return SQAP_OK;
+        const ShortArgs a = {Q, ldq, starts, past, rows, max_new, H, cache, prefix, Parts{nullptr, nullptr, 0, 0, cache.batch / prefix.batch, length}, O, ldo, tiles};
+        return plan.waves == 2 ? launch_short<D, 2, Part::Whole>(a, st) : launch_short<D, kFewRowsWaves, Part::Whole>(a, st);
     }
     const Parts parts = {reinterpret_cast<float *>(workspace + plan.o), reinterpret_cast<float2 *>(workspace + plan.ml), plan.pairs, plan.shares,
                          cache.batch / prefix.batch, length};
