@@ -180,6 +180,21 @@ def test_prompts(G, groups, width, H, kv, d, lengths):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("H,kv,d", [(16, 4, 64), (16, 4, 128), (4, 4, 128), (20, 5, 64)])
+def test_prompts_of_many_sequences(G, H, kv, d):
+    """More tiles than the device holds at once: in one pass and in parts; prefixes that end a block, in one or are empty; up to four own blocks."""
+    s = Shared(G, 4, 40, H, kv, d, [70, 0, 128, 191], capacity=256, seed=H + d)
+    counts = lambda: [int(n) for n in s.own.rng.integers(0, 8, 160)]                         # noqa: E731
+    s.prompt(counts(), most=7)
+    s.own.append([int(n) for n in s.own.rng.integers(0, 150, 160)], attend=False)
+    s.prompt(counts(), most=8, in_place=True)
+    s.prompt(counts(), most=8, longest_prefix=100000, padding=0)
+    s.own.append([int(n) for n in 63 - s.own.past % 64], attend=False)
+    s.prompt([2 + b % 3 for b in range(160)], longest_prefix=100000, in_place=True)          # every sequence finishes a block
+    s.own.check_contents()
+
+
+@pytest.mark.gpu
 def test_many_own_blocks(G):
     """Own histories that are split over workgroups, too."""
     s = Shared(G, 1, 2, 8, 2, 64, [300], capacity=4096, seed=3)
@@ -190,7 +205,7 @@ def test_many_own_blocks(G):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("hint", [None, 100000])                  # (in one pass, and in parts)
-@pytest.mark.parametrize("width", [2, 40])
+@pytest.mark.parametrize("width", [2, 40, 140])
 def test_infinite_values_and_keys(G, width, hint):
     """Infinities and NaN among values and keys of the unfinished blocks of a prefix and of own positions, a prefix block without scale, scores that
     are minus infinity over a whole prefix."""
@@ -213,7 +228,7 @@ def test_infinite_values_and_keys(G, width, hint):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("width", [2, 40])
+@pytest.mark.parametrize("width", [2, 40, 80])
 @pytest.mark.parametrize("decode,hint", [(True, 100), (False, 100), (False, 100000)])
 def test_what_does_not_fit(G, width, decode, hint):
     """Padded sequences keep their outputs; sequences without room, rows or prefix lengths that cannot be give NaN, and nothing reaches the others."""
@@ -313,6 +328,14 @@ def test_replayed_with_other_lengths(G, width):
     (1, 3, 32, 1, 64, [3001], [[5, 40, 3], [9, 1, 2]]),
     (1, 2, 20, 1, 128, [333], [[100, 77]]),
     (4, 4, 4, 4, 64, [1, 2, 65, 900], [[100 + 10 * b for b in range(16)]]),
+    # (those above are less than 64 tiles, most of them)
+    (1, 1, 32, 4, 64, [100], [[300], [260]]),
+    (1, 2, 32, 2, 128, [0], [[96, 200], [150, 130]]),
+    (2, 3, 32, 4, 128, [700, 130], [[200, 33, 0, 129, 64, 301], [64, 0, 31, 127, 1, 64]]),
+    (3, 1, 48, 8, 64, [64, 0, 191], [[65, 100, 16], [1, 63, 128]]),
+    (1, 1, 64, 64, 128, [6000], [[130], [128]]),
+    (1, 3, 64, 1, 64, [3001], [[60, 70, 3], [9, 118, 2]]),
+    (1, 2, 40, 2, 128, [333], [[130, 77], [205, 1]]),
 ])
 def test_long_prompts(G, groups, width, H, kv, d, lengths, calls):
     s = Shared(G, groups, width, H, kv, d, lengths, capacity=640, seed=groups + 50)
@@ -330,10 +353,11 @@ def test_long_prompts_of_many_sequences(G):
 
 
 @pytest.mark.gpu
-def test_long_prompts_with_infinite_values(G):
+@pytest.mark.parametrize("H", [4, 32])
+def test_long_prompts_with_infinite_values(G, H):
     """As test_infinite_values_and_keys: in unfinished blocks of a prefix and of own positions, a block of keys without scale, scores of minus
     infinity over a whole prefix."""
-    H, kv, d, lengths = 4, 2, 64, [70, 130, 1]
+    kv, d, lengths = 2, 64, [70, 130, 1]
     rows = np.random.default_rng(8).standard_normal((201, H + 2 * kv, d)).astype(np.float16)
     rows[66, H + kv, 3] = np.inf
     rows[69, H + kv, 3], rows[69, H + kv + 1, 7] = -np.inf, np.nan
@@ -349,9 +373,10 @@ def test_long_prompts_with_infinite_values(G):
 
 
 @pytest.mark.gpu
-def test_long_prompts_that_do_not_fit(G):
+@pytest.mark.parametrize("H", [4, 16])
+def test_long_prompts_that_do_not_fit(G, H):
     """NaN where there is no room, more rows than announced, more in a group than announced together or a length that cannot be; padded ones left alone."""
-    t, H, kv, d, width = __import__("torch"), 4, 1, 64, 2
+    t, kv, d, width = __import__("torch"), 1, 64, 2
     s = Shared(G, 5, width, H, kv, d, [70, 20, 64, 9, 30], capacity=192, seed=62)
     counts = [60, 40, 50, 45, 33, 70, 64, 64, 30, 90]
     before = s.own.past.copy()
@@ -388,9 +413,10 @@ def test_long_prompts_that_do_not_fit(G):
 
 
 @pytest.mark.gpu
-def test_long_prompts_replayed(G):
+@pytest.mark.parametrize("H", [4, 32])
+def test_long_prompts_replayed(G, H):
     """A captured prompt call, replayed with other rows and lengths."""
-    t, H, kv, d, total = __import__("torch"), 4, 2, 128, 300
+    t, kv, d, total = __import__("torch"), 2, 128, 300
     s = Shared(G, 2, 2, H, kv, d, [500, 64], capacity=1024, seed=63)
     q, o = (t.zeros((total, H * d), dtype=t.float16, device=G.DEV) for _ in range(2))
     starts, past = t.zeros((5,), dtype=t.int32, device=G.DEV), t.zeros((4,), dtype=t.int32, device=G.DEV)
