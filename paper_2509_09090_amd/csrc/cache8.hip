@@ -823,7 +823,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
 // equal shares of each, would take 430).  A tile inside a workgroup's range is finished there; of one over its ends, the workgroups leave their sums,
 // one at the beginning and one at the end of each range, and cache8_long_join_kernel adds them.  Ranges are counted in tiles as long as their
 // sequence's longest (a tile's real blocks, fewer where its rows see less, are parted in the same proportion).
-constexpr int kLongBatch = 1024, kLongParts = 32, kLongLeast = 4, kLongTiles = 64;
+constexpr int kLongBatch = 1024, kLongParts = 32, kLongLeast = 4, kLongTiles = 64, kLongWork = 16000;
 struct LongSlot {                // what a workgroup's first range belongs to, where it is the rest of a tile
     int b, kh, tile, first, count;       // the workgroup that begins the tile, how many have a share of it; count 0: none, or not its second
     int pad[3];
@@ -2375,9 +2375,13 @@ static SharedPlan shared_plan(bool prompt, int batch, int groups, int H, int kv_
     p.own_shares = own_shares;
     p.pairs = (int64_t)rows * H;
     const auto up = [](size_t n) { return (n + 15) / 16 * 16; };
-    // rows that fill three quarters of a tile on average, and 64 tiles (128 rows of 32 heads over 8, 32 tiles, behind 2000 positions 47 us and 20 otherwise,
-    // behind 20000 110 and 91; 64 tiles behind 2000 46 and 45; 330 behind 6000 194 and 279)
-    p.together = max_new > 1 && batch <= kLongBatch && (int64_t)rows * (H / kv_heads) >= (int64_t)batch * 96 && (int64_t)rows * H >= 128 * kLongTiles;
+    const int64_t tiles = ((int64_t)max_new * (H / kv_heads) + 15) / 16 * kv_heads * batch;          // of 16
+    // rows that fill three quarters of a tile of 128 on average, 64 of those (128 rows of 32 heads over 8, 32 tiles, behind 2000 positions 47 us and 20
+    // otherwise, behind 20000 110 and 91; 64 tiles behind 2000 46 and 45; 330 behind 6000 194 and 279), and more than a start's worth of work: the kernel
+    // takes 36 us at the least (8 x 148 rows behind 100 positions, 7104 blocks of tiles of 16: 47 us and 33; 300 behind 1000, 11400: 46 and 37; 16 x 100
+    // behind 200, 16000: 49 and 46; 8 x 148 behind 500, 23680: 49 and 49; 8 x 300 behind 100, 24000: 56 and 65)
+    p.together = max_new > 1 && batch <= kLongBatch && (int64_t)rows * (H / kv_heads) >= (int64_t)batch * 96 && (int64_t)rows * H >= 128 * kLongTiles &&
+                 tiles * (blocks + (max_new + 127) / 128) > kLongWork;
     if (p.together) {
         p.groups = std::max(8, device_cu_count() * 2 / 8 * 8);
         p.ml = kCounterBytes + (size_t)p.groups * sizeof(LongSlot);
@@ -2385,7 +2389,6 @@ static SharedPlan shared_plan(bool prompt, int batch, int groups, int H, int kv_
         p.bytes = p.o + (size_t)p.groups * 256 * d * sizeof(float);
         return p;
     }
-    const int64_t tiles = ((int64_t)max_new * (H / kv_heads) + 15) / 16 * kv_heads * batch;
     p.waves = tiles <= kShortTiles ? kFewRowsWaves : 2;
     p.direct = prompt && (tiles <= kShortTiles ? tiles * blocks <= kShortBlocks && (blocks <= kShortPrefix || tiles >= 256) : tiles * 16 * blocks < kShortRepeats * (int64_t)rows * H);
     if (p.direct) return p;                                           // (no workspace)
