@@ -113,7 +113,9 @@ struct BeamArgs {
 // One workgroup per row and slab of 2048 PIECES logits, which it holds in registers.  The largest of each piece of eight, with the piece's place
 // below it, is a number of its own; at least k pieces are not below the k-th largest of the threads' largest, and the slab's
 // best k lie in those: any other piece has k logits before its own.  They go to LDS, a thread takes one of their logits each, and those that reach the
-// smallest of these maxima are listed and ranked.
+// smallest of these maxima are listed and ranked.  128 rows of 128001 (32.8 MB) in 14.4 us, 2.3 TB/s: a slab's start, loads (6.2 of the 14.4, by themselves), one
+// exponential per logit, a search over 16 bits and the ranking follow one another, 2048 workgroups in two rounds, and a round's loads have nothing of their own to
+// hide behind; rows of one wavefront each, without barriers, 16.3.  4 rows of 32000 in 4.8 us: latency.
 template <int PIECES>
 __global__ __launch_bounds__(kBeamT) void beam_rows_kernel(const BeamArgs a)
 {
@@ -242,7 +244,8 @@ __device__ __forceinline__ double total_of(u64 key) { return __longlong_as_doubl
 constexpr int kTieBeam = 36, kTieKey = 20;                            // (tokens have 20 bits, keys 16)
 
 // One workgroup per batch element: the rows' sums from their slabs', then the best k of all their candidates, as in beam_rows_kernel: the best of each of 256
-// groups of threads, a number that k of those reach, the few candidates that reach it ranked.
+// groups of threads, a number that k of those reach, the few candidates that reach it ranked.  6.3 us for 4 beams of 16 slabs with 4 each, 7.6 for 8 beams of 8 slabs
+// with 16: three waits for memory and a search over 64 bits, on one compute unit.
 constexpr int kSurvivors = 2048, kGroups = 256;
 template <int T>
 __global__ __launch_bounds__(T) void beam_select_kernel(const BeamArgs a)
@@ -526,7 +529,9 @@ __device__ __forceinline__ void move_pieces(char *base, int64_t pitch, unsigned 
 }
 
 // One workgroup per group, key head and 256 pieces of a block (of all sequences of the group at once), of the unfinished block's rows, or of
-// the scales; V: a piece.
+// the scales; V: a piece.  All of a group's sequences are read before any is written, so it works in place; who takes over nothing new moves nothing.  64
+// sequences of 8 key heads, up to 2000 positions, 217 MB of reads and writes together: 46 us on data that no cache holds, 4.7 TB/s of the 5.06 that a copy reaches;
+// 4 sequences of 32 heads, up to 70 positions, 3.9: latency.
 template <int D, int WIDTH, typename V>
 __global__ __launch_bounds__(256) void cache8_reorder_kernel(const Cache8View cache, const int32_t *__restrict__ parents, int width,
                                                              const int32_t *__restrict__ lengths, int32_t *__restrict__ lengths_out, int block_groups)
