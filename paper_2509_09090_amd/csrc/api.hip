@@ -879,7 +879,7 @@ size_t sqap_cache8_shared_workspace_bytes(int32_t batch, int32_t groups, int32_t
     if (batch <= 0 || groups <= 0 || batch % groups != 0 || H <= 0 || kv_heads <= 0 || H % kv_heads != 0 || head_dim <= 0 || rows <= 0 || max_new <= 0 ||
         longest <= 0 || longest_prefix < 0)
         return 0;
-    return cache8_shared_workspace_bytes(batch, groups, H, kv_heads, head_dim, rows, max_new, longest, longest_prefix);
+    return cache8_shared_workspace_bytes(batch, groups, H, kv_heads, head_dim, rows, max_new < rows ? max_new : rows, longest, longest_prefix);      // (as the call)
 }
 
 sqap_status sqap_cache8_shared_attention(const sqap_f16 *Q, int64_t ldq, const int32_t *starts, const int32_t *past, int32_t rows, int32_t max_new,

@@ -2346,9 +2346,10 @@ sqap_status launch_cache8_decode(const __half *QKV, int64_t ld, const int32_t *p
 
 // ---- behind a shared prefix
 
-// How the prefixes are dealt out: shares of two blocks to a wavefront (64 rows of 32 heads over 8 behind 1000 positions 16.3 us, with one 20.4), of one up to 8 blocks.  Up to 64 pairs to a group and key head: tiles of 16, blocks dealt to the wavefronts; up to 256 of them, too, where all
-// tiles together have no more than 20000 blocks: the tiles of 128 want two launches more (32 rows of 32 heads over 8 behind 1000 positions 14 and
-// 27 us, behind 20000 45 and 48, behind 100003 187 and 128; 64 behind 1000 23 and 29).
+// How the prefixes are dealt out: shares of two blocks to a wavefront (64 rows of 32 heads over 8 behind 1000 positions 16.3 us, with one 20.4), of one up
+// to 8 blocks.  Up to 64 pairs to a group and key head: tiles of 16, blocks dealt to the wavefronts; up to 256 of them, too, where all tiles together
+// have no more than 20000 blocks: the tiles of 128 want two launches more (32 rows of 32 heads over 8 behind 1000 positions 14 and 27 us,
+// behind 20000 45 and 48, behind 100003 187 and 128; 64 behind 1000 23 and 29).
 // Prompts of few rows: tiles of 16 that pass over prefix and own positions by themselves.  Up to 512 tiles, which the device holds at once, with eight
 // wavefronts, while they are up to 12000 blocks in all (16 x 10 rows of 32 heads over 8 behind 1000 positions, 6144: 25 us, in parts 30; behind 4000 54
 // and 39) and prefixes up to 48 blocks long, or 256 tiles (10 rows behind 1000 positions 13 and 20, behind 4000 27 and 24).  More tiles with two wavefronts,
@@ -2394,7 +2395,8 @@ static SharedPlan shared_plan(bool prompt, int batch, int groups, int H, int kv_
         return p;
     }
     p.waves = tiles <= kShortTiles ? kFewRowsWaves : 2;
-    p.direct = prompt && (tiles <= kShortTiles ? tiles * blocks <= kShortBlocks && (blocks <= kShortPrefix || tiles >= 256) : tiles * 16 * blocks < kShortRepeats * (int64_t)rows * H);
+    p.direct = prompt && (tiles <= kShortTiles ? tiles * blocks <= kShortBlocks && (blocks <= kShortPrefix || tiles >= 256)
+                                               : tiles <= most_workgroups(256) && tiles * 16 * blocks < kShortRepeats * (int64_t)rows * H);
     if (p.direct) return p;                                           // (no workspace)
     p.q = kCounterBytes;                                              // (left alone, for calls that want it zero)
     p.ml = p.q + (max_new == 1 ? up((size_t)p.pairs * d * 2) : 0);

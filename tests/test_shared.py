@@ -40,6 +40,20 @@ def test_prompt_refusals():
     assert call(rows=0, Q=None) == B.OK and call(cache=_desc(batch=0), starts=None) == B.OK
 
 
+@pytest.mark.parametrize("case", [(4, 2, 32, 8, 128, 300, 100000, 1, 100), (4, 4, 32, 8, 64, 700, 20000, 1, 5000), (8, 2, 12, 12, 64, 8, 40, 1, 6000), (1, 1, 64, 64, 128, 1, 9, 1, 20000),
+                                  (4, 1, 4, 2, 64, 30, 2 ** 31 - 1, 1, 500)])
+def test_workspace_of_prompts_that_announce_more_rows_than_there_are(case):
+    """No sequence has more rows than there are: the call asks for no more, and no less."""
+    L = B.lib()
+    need = B.sqap_cache8_shared_workspace_bytes(*case)
+    batch, groups, H, kv, d, rows, max_new, _, longest_prefix = case
+    assert need == B.sqap_cache8_shared_workspace_bytes(batch, groups, H, kv, d, rows, rows, 1, longest_prefix)
+    call = lambda n, most: L.sqap_cache8_shared_attention(P, H * d, P, P, rows, most, H, _desc(batch=batch, kv_heads=kv, head_dim=d),       # noqa: E731
+                                                          _front(batch=groups, kv_heads=kv, head_dim=d), P, longest_prefix, P, H * d, P, n, None)
+    if need:
+        assert call(need - 1, max_new) == B.EINVAL
+
+
 def test_decode_refusals():
     L = B.lib()
     need = B.sqap_cache8_shared_workspace_bytes(4, 2, 4, 2, 64, 4, 1, 100, 500)
@@ -438,3 +452,39 @@ def test_long_prompts_replayed(G, H):
         s.check(o.cpu().numpy(), y, counts)
         s.own.past = after
         assert bool((o[n:] == 9).all())
+
+
+# ---- streams
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [3, 150])
+def test_calls_on_streams_of_their_own(G, rows):
+    """Calls over the same caches on two streams at once, each with a workspace of its own, give what one after the other gives, bit for bit."""
+    t, H, kv, d, batch = __import__("torch"), 32, 4, 64, 6
+    s = Shared(G, 2, 3, H, kv, d, [900, 3333], capacity=256, seed=80)
+    counts = [rows] * batch
+    before = s.own.past.copy()
+    y = s.own.append(counts, pos=s.positions(counts), attend=False)
+    after, s.own.past = s.own.past, before
+    q = G.to_dev(np.ascontiguousarray(y[:, :H]).reshape(rows * batch, -1))
+    starts, past = G.to_dev(np.arange(batch + 1, dtype=np.int32) * rows), G.to_dev(before)
+
+    def call(o, ws, longest_prefix):
+        B.sqap_cache8_shared_attention(q, starts, past, s.own.cache, s.prefix.cache, s.device_lengths, H, rows, o, ws, longest_prefix)
+
+    outputs = []
+    for longest_prefix in (3333, 100000):
+        o, ws = t.full((rows * batch, H * d), 9.0, dtype=t.float16, device=G.DEV), s.workspace(rows * batch, rows, 1, longest_prefix)
+        call(o, ws, longest_prefix)
+        s.check(o.cpu().numpy(), y, counts)
+        outputs.append((longest_prefix, o, t.full_like(o, 9.0), ws))
+    streams = [t.cuda.Stream(), t.cuda.Stream()]
+    t.cuda.synchronize()
+    for _ in range(5):
+        for stream, (longest_prefix, _, o, ws) in zip(streams, outputs):
+            with t.cuda.stream(stream):
+                o.fill_(9.0)
+                call(o, ws, longest_prefix)
+    t.cuda.synchronize()
+    assert all(t.equal(x, o) for _, x, o, _ in outputs)
+    s.own.past = after
