@@ -15,6 +15,7 @@ typedef unsigned v2u __attribute__((ext_vector_type(2)));
 typedef unsigned long long u64;
 
 constexpr int kBeamT = 256, kBeamWaves = kBeamT / 64, kBeamMost = kBeamMostOutputs;
+constexpr int kRankedAtMost = 192;                                     // of a list
 constexpr unsigned kMinusInf = 0x03ffu;                               // key of minus infinity, the lowest there is
 constexpr float kLog2e = 1.44269502f;
 
@@ -204,13 +205,36 @@ __global__ __launch_bounds__(kBeamT) void beam_rows_kernel(const BeamArgs a)
         if (key >= least) list[atomicAdd(&listed, 1u)] = key << 14 | (16383 - (place[i >> 3] * 8 + (i & 7)));
     }
     __syncthreads();
-    const int n = (int)listed;
+    int n = (int)listed;
+    const unsigned *ranked = list;
+    if (n > kRankedAtMost && n <= 8 * 64) {
+        // nearly as many outputs as pieces: the k-th largest of the list first, as above, and only those that reach it are ranked (46 x 31 rows of 427
+        // logits with 62 outputs 48 us, so 17; the ranking of some hundred is shorter)
+        unsigned x[8], bound = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = l + 64 * i < n ? list[l + 64 * i] : 0;
+        for (int bit = 29; bit >= 0; --bit) {
+            const unsigned next = bound | 1u << bit;
+            int count = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) count += __popcll(__ballot(x[i] >= next));
+            if (count >= a.k) bound = next;
+            if (count == a.k) break;
+        }
+        if (t == 0) pieces = 0;
+        __syncthreads();
+        for (int i = t; i < n; i += kBeamT)
+            if (list[i] >= bound) tops[atomicAdd(&pieces, 1u)] = list[i];
+        __syncthreads();
+        n = (int)pieces;
+        ranked = tops;
+    }
     v2u *best = a.best + (row * a.slabs + slab) * a.k;
     for (int i = t; i < n; i += kBeamT) {
-        const unsigned own = list[i];
+        const unsigned own = ranked[i];
         int rank = 0;
         for (int j = 0; j < n; j += 8) {
-            const v4u x = *reinterpret_cast<const v4u *>(list + j), y = *reinterpret_cast<const v4u *>(list + j + 4);
+            const v4u x = *reinterpret_cast<const v4u *>(ranked + j), y = *reinterpret_cast<const v4u *>(ranked + j + 4);
 #pragma unroll
             for (int e = 0; e < 4; ++e) rank += (j + e < n && x[e] > own ? 1 : 0) + (j + 4 + e < n && y[e] > own ? 1 : 0);
         }

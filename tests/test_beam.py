@@ -147,7 +147,7 @@ def _scores(rng, batch, beams):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("batch,beams,vocab,k", [(1, 1, 1, 1), (1, 1, 7, 10), (2, 3, 8, 30), (3, 5, 1003, 10), (1, 4, 32000, 4), (2, 3, 2047, 6), (2, 3, 2048, 6),
-                                                 (2, 3, 2049, 6), (70, 2, 5001, 4), (3, 32, 4099, 64), (1, 64, 300, 64), (2, 8, 128001, 16), (40, 8, 17001, 8),
+                                                 (2, 3, 2049, 6), (70, 2, 5001, 4), (3, 32, 4099, 64), (1, 64, 300, 64), (2, 8, 128001, 16), (40, 8, 17001, 8), (2, 31, 427, 62),
                                                  (1, 2, 1 << 20, 64)])
 def test_against_the_definition(G, batch, beams, vocab, k):
     rng = np.random.default_rng(batch * 1000 + beams)
