@@ -1846,6 +1846,11 @@ __global__ __launch_bounds__(64 * kDecodeWaves, SHARED ? 3 : 2) void cache8_deco
 
     if (t < HALF) sincos_of(angle, lds.sn[t], lds.cs[t]);
     if (t < D) lds.odd[t] = 0;
+    // values of the rows that are missing: zero, sixteen bytes at a time (242 sequences of 32 heads, a first own row behind 17 positions: 63 us, with zeros
+    // taken through the transposition below 73)
+    if (has_last && slot < kBlock - 1)
+#pragma unroll
+        for (int i = 0; i < D * kBlock / 8 / T; ++i) *reinterpret_cast<v4i *>(&lds.u.tail.v[(t + i * T) / 8][(t + i * T) % 8 * 8]) = v4i{0, 0, 0, 0};
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < 16 * HALF / T; ++k) {
@@ -1879,6 +1884,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, SHARED ? 3 : 2) void cache8_deco
 #pragma unroll
         for (int i = 0; i < UNITS; ++i) {
             const int u = t + i * T, s = u / (D / 8), x = (u % (D / 8)) * 8, at = value_slot(s);
+            if (s >= slot) break;                                     // (keys behind the new row: scores that are masked)
             *reinterpret_cast<v4i *>(&lds.u.tail.k[s][x]) = tk[i];
             unsigned mk = 0, mv = 0;
 #pragma unroll
@@ -1976,10 +1982,12 @@ __global__ __launch_bounds__(64 * kDecodeWaves, SHARED ? 3 : 2) void cache8_deco
     own.l += __shfl_xor(own.l, 16);
     own.l += __shfl_xor(own.l, 32);
     __syncthreads();                                                  // the last block's rows have been read
+    if (begin + wave < stop) {
 #pragma unroll
-    for (int i = 0; i < DT; ++i)
+        for (int i = 0; i < DT; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) lds.u.o[wave][r][16 * i + 4 * g + e] = own.o[i][e] * own.unit.unit;
+            for (int e = 0; e < 4; ++e) lds.u.o[wave][r][16 * i + 4 * g + e] = own.o[i][e] * own.unit.unit;
+    }
     if (g == 0) {
         lds.m[wave][r] = own.m;
         lds.l[wave][r] = own.l;
