@@ -1359,7 +1359,7 @@ struct ShortArgs {
     int tiles;
 };
 template <int D, int WAVES, Part PART>
-__global__ __launch_bounds__(64 * WAVES, 2) void cache8_short_kernel(const ShortArgs a)
+__global__ __launch_bounds__(64 * WAVES, D == 64 ? 4 : 2) void cache8_short_kernel(const ShortArgs a)
 {
     constexpr int C = D / 64, DT = D / 16, T = 64 * WAVES, OF_TAIL = kBlock / 4 * D / 8, TAILS = PART == Part::Own ? 1 : 2, UNITS = (TAILS * OF_TAIL + T - 1) / T;
     extern __shared__ __attribute__((aligned(16))) uint8_t raw_lds[];
@@ -1434,6 +1434,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_short_kernel(const Short
     for (int i = 0; i < UNITS; ++i) {
         const int u = t + i * T, x = u / OF_TAIL + 2 - TAILS, s = u % OF_TAIL / (D / 8) * 4, col = u % (D / 8) * 8, at = value_slot(s);
         if (x >= 2 || rest(x) == 0) continue;
+        if (s >= rest(x)) {                                           // (252 sequences of 64 heads, 4 rows behind 30 positions: 66.5 us; with these among the others 71.5)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) *reinterpret_cast<v2u *>(&lds.u.v[x - 2 + TAILS][col + e][value_place(col + e, at)]) = v2u{0, 0};
+            continue;
+        }
         bool odd = false;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -2259,7 +2264,7 @@ static sqap_status launch_short(const ShortArgs &a, hipStream_t st)
 // (96) 67 and 103, 300 of 32 heads (96) 13.9 and 15.1; but 500 of 32 (128) 23.7 and 21.3, 1000 of 32 over 8 (256) 56 and 37.
 constexpr int kFewTiles = 96;
 // Parts of many sequences with up to 32 rows each: cache8_short_kernel, whose two wavefronts and two workgroups' LDS leave four to a CU, in place of tiles of
-// 128 that are almost empty (512 x 2 rows of 32 heads over 8, prefix and join included, 86 us and 119; 700 x 2 of 12 heads 58 and 89).
+// 128 that are almost empty (512 x 2 rows of 32 heads over 8, prefix and join included, 85 us and 119; 700 x 2 of 12 heads of 64 53 and 89).
 constexpr int kShortTiles = 512, kOwnTiles = 2;
 
 template <int D, Part PART>
