@@ -169,6 +169,14 @@ __device__ __forceinline__ PrefixShare prefix_share(int length, int capacity, in
     return {min(share * each, blocks), min((share + 1) * each, blocks), (blocks + each - 1) / each};
 }
 
+// Whether a sequence's rows lie within its group's.  Where starts are not in order they may be another group's, and the sequence is skipped: a part of it
+// would lie where that group's own is.
+__device__ __forceinline__ bool in_its_group(const int32_t *starts, int b, int width, const Span &sp)
+{
+    const int first = b / width * width;
+    return sp.row >= starts[first] && sp.row + sp.n <= starts[first + width];
+}
+
 // A sequence behind a prefix: `rows` says whether it has any that count, `fits` whether they are worked out (their outputs are NaN otherwise).
 struct Member {
     Span sp;
@@ -181,8 +189,7 @@ __device__ __forceinline__ Member member_of(const int32_t *starts, const int32_t
     Member m = {Span{b, 1, past[b], true}, true, true, parts.length[group]};
     if (starts) {
         m.sp = span_of(starts, past, b, rows, max_new, capacity);
-        const int first = starts[group * parts.width], end = starts[(group + 1) * parts.width];
-        m.rows = m.sp.n > 0 && m.sp.row >= first && m.sp.row + m.sp.n <= end;        // (starts that are not in order: no rows)
+        m.rows = m.sp.n > 0 && in_its_group(starts, b, parts.width, m.sp);
         m.fits = m.sp.fits && group_rows(starts, group, parts.width, rows, max_new).n > 0;
     } else {
         m.rows = m.sp.past >= 0;
@@ -743,6 +750,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
             if constexpr (PART == Part::Whole) nan_rows<D>(O, ldo, sp.row, (int64_t)sp.n * G, G, kh, number, tiles, TILE);
             return;
         }
+        if (PART == Part::Own && !in_its_group(starts, b, parts.width, sp)) return;
         tile = (tiles - 1 - number) * TILE;
     }
     n_rows = sp.n * G;                                                // (the launch keeps max_new * G in 32 bits)
@@ -1205,6 +1213,7 @@ __global__ __launch_bounds__(64 * kFewRowsWaves, 2) void cache8_few_rows_kernel(
         if constexpr (PART == Part::Whole) nan_rows<D>(O, ldo, sp.row, (int64_t)sp.n * G, G, kh, number, tiles, 16);
         return;
     }
+    if (PART == Part::Own && !in_its_group(starts, b, parts.width, sp)) return;
     const int n_rows = sp.n * G, tile = (tiles - 1 - number) * 16;
     if (tile >= n_rows) return;
     const int mine = min(tile + r, n_rows - 1), query = mine / G, first_query = tile / G;
@@ -1372,7 +1381,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 64 ? 4 : 2) void cache8_short_kern
     Member member;
     if constexpr (PART == Part::Own) {
         const Span own = span_of(a.starts, a.past, b, a.rows, a.max_new, cache.blocks * kBlock);
-        member = {own, true, own.fits, 0};
+        member = {own, own.n > 0 && in_its_group(a.starts, b, a.parts.width, own), own.fits, 0};
     } else {
         member = member_of(a.starts, a.past, b, a.rows, a.max_new, cache.blocks * kBlock, prefix.blocks * kBlock, a.parts);
     }

@@ -1,0 +1,51 @@
+"""Attention of prompts behind shared prefixes, by the kernels that a call reaches: what a call asks for as workspace tells them apart, and each test says
+which it is about.  longest_prefix is a hint that steers the choice and nothing else."""
+import numpy as np
+import pytest
+
+from paper_2509_09090_amd import binding as B
+from tests.test_shared import Shared
+
+ALONE, TOGETHER, PARTS = "tiles of 16 by themselves", "blocks of all tiles dealt out", "prefix and own positions in parts"
+FAR = 100000                                                          # a hint
+
+
+def kernels(batch, groups, H, kv, d, rows, most, longest_prefix):
+    """Nothing is asked for by the first, a size without rows in it by the second."""
+    need = lambda n: B.sqap_cache8_shared_workspace_bytes(batch, groups, H, kv, d, n, most, 1, longest_prefix)        # noqa: E731
+    return ALONE if need(rows) == 0 else TOGETHER if need(rows) == need(rows + 1) else PARTS
+
+
+@pytest.fixture(scope="module")
+def G():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from tests import gpu_util
+    return gpu_util
+
+
+# groups of three, few of them: own positions by tiles of 16 with eight wavefronts; more: by tiles of 128; many: by tiles of 16 with two
+@pytest.mark.gpu
+@pytest.mark.parametrize("groups,hint,by", [(2, 70, ALONE), (2, FAR, PARTS), (34, FAR, PARTS), (171, FAR, PARTS)])
+def test_rows_of_another_group(G, groups, hint, by):
+    """Starts that lead a sequence to rows of another group: it is skipped, and those rows are their own sequence's."""
+    import torch
+    H, kv, d, width = 2, 1, 64, 3
+    s = Shared(G, groups, width, H, kv, d, [70, 20] + [9] * (groups - 2), seed=6)
+    counts = [1, 5, 1, 2, 2, 2] + [1] * (3 * groups - 6)
+    total, at = sum(counts), np.concatenate([[0], np.cumsum(counts)])
+    assert kernels(3 * groups, groups, H, kv, d, total, 5, hint) == by
+    before = s.own.past.copy()
+    y = s.own.append(counts, pos=s.positions(counts), attend=False)
+    s.own.past = before
+    q = G.to_dev(np.ascontiguousarray(y[:, :H]).reshape(total, -1))
+    # sequence 4 at rows 2 and 3, which are sequence 1's; at 9 .. 13, the last of them the next group's where there is one; sequence 0 beyond its group
+    for starts, skipped in (({4: 2, 5: 4}, {3, 4, 5}), ({5: 14}, {4, 5}), ({1: 9}, {0, 1})):
+        st = at.astype(np.int32)
+        for b, row in starts.items():
+            st[b] = row
+        o = torch.full((total, H * d), 9.0, dtype=torch.float16, device=G.DEV)
+        B.sqap_cache8_shared_attention(q, G.to_dev(st), G.to_dev(before), s.own.cache, s.prefix.cache, s.device_lengths, H, 5, o, s.workspace(total, 5, 1, hint), hint)
+        got = o.cpu().numpy()
+        s.check(got, y, counts, skip=skipped)
+        assert all(np.all(got[at[b]:at[b + 1]] == 9) for b in skipped), starts
