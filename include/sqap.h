@@ -632,11 +632,12 @@ sqap_status sqap_sample(const sqap_f16 *logits, int64_t ld, int32_t batch, int32
  * logits are not read.  Beams whose score is NaN or minus infinity have none with a probability (so that a search may start with one beam).
  * parent_out, token_out [batch, k] int32, score_out [batch, k] binary32 (the total, rounded once): best first; where beams * vocab is below k the rest
  * are -1, -1 and minus infinity.  done_out: NULL, or [batch, k] int32: 1 where the parent has finished or the token is eos, else 0.
- * With k = beams score_out may be scores, done_out done.
+ * With k = beams score_out may be scores, done_out done; otherwise outputs and workspace lie over none of the inputs (of logits: from the first row to
+ * the end of the last) and not over one another.
  * workspace: at least sqap_beam_workspace_bytes(batch, beams, vocab, k) bytes, 16-byte aligned, of any contents; calls that share it must be
  * ordered on one stream, graphs that are replayed side by side need one each.  May be captured.
  * EINVAL: null pointer, negative batch, beams, vocab or k < 1, ld < vocab, done with an eos outside 0 .. vocab - 1 (without it eos may be any
- * number, -1 for none), outputs over inputs otherwise, workspace missing, too small or misaligned.  EUNSUPPORTED: more than 64 beams or outputs,
+ * number, -1 for none), outputs or workspace over what they must not lie over, workspace missing, too small or misaligned.  EUNSUPPORTED: more than 64 beams or outputs,
  * vocab > 1048576, more than 2^24 - 1 rows times 2048 tokens.
  */
 size_t sqap_beam_workspace_bytes(int32_t batch, int32_t beams, int32_t vocab, int32_t k);

@@ -942,11 +942,15 @@ sqap_status sqap_cache8_shared_decode_attention(const sqap_f16 *QKV, int64_t ld,
                                        reinterpret_cast<__half *>(O), ldo, workspace, as_stream(stream));
 }
 
-// two ranges of 32-bit words that lie over each other
-static bool overlap(const void *x, int64_t n, const void *y, int64_t m)
+// a range of memory (null: none), and whether two of them lie over each other
+struct Range {
+    const void *at;
+    size_t bytes;
+};
+static bool overlap(const Range &x, const Range &y)
 {
-    const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y);
-    return a < b + 4 * (uintptr_t)m && b < a + 4 * (uintptr_t)n;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(x.at), b = reinterpret_cast<uintptr_t>(y.at);
+    return x.at && y.at && a < b + y.bytes && b < a + x.bytes;
 }
 
 sqap_status sqap_cache8_reorder(const sqap_cache8 *cache, const int32_t *parents, int32_t width, const int32_t *lengths, int32_t longest,
@@ -961,7 +965,8 @@ sqap_status sqap_cache8_reorder(const sqap_cache8 *cache, const int32_t *parents
     if (width > kBeamMostOutputs) return fail(SQAP_EUNSUPPORTED, "%s: groups of %d > %d", who, width, kBeamMostOutputs);
     if (cache->batch == 0) return SQAP_OK;
     if (!parents || !lengths) return fail(SQAP_EINVAL, "%s: null pointer", who);
-    if (lengths_out && (overlap(lengths_out, cache->batch, lengths, cache->batch) || overlap(lengths_out, cache->batch, parents, cache->batch)))
+    const size_t words = 4 * (size_t)cache->batch;
+    if (overlap({lengths_out, words}, {lengths, words}) || overlap({lengths_out, words}, {parents, words}))
         return fail(SQAP_EINVAL, "%s: lengths_out lies over lengths or parents", who);
     const DeviceOfCall device;
     return launch_cache8_reorder(v, cache->head_dim, parents, width, lengths, longest, lengths_out, as_stream(stream));
@@ -992,15 +997,21 @@ sqap_status sqap_beam_select(const sqap_f16 *logits, int64_t ld, int32_t batch, 
     if (done && (eos < 0 || eos >= vocab)) return fail(SQAP_EINVAL, "%s: finished beams and the token %d of %d", who, eos, vocab);
     if (batch == 0) return SQAP_OK;
     if (!logits || !scores || !parent_out || !token_out || !score_out) return fail(SQAP_EINVAL, "%s: null pointer", who);
-    const int64_t in = (int64_t)batch * beams, out = (int64_t)batch * k;
-    const bool in_place = k == beams;
-    if ((overlap(score_out, out, scores, in) && !(in_place && score_out == scores)) ||
-        (done && done_out && overlap(done_out, out, done, in) && !(in_place && done_out == done)))
-        return fail(SQAP_EINVAL, "%s: outputs lie over inputs of another layout", who);
     const size_t need = beam_workspace_bytes(batch, beams, vocab, k);
     if (!workspace || workspace_bytes < need)
         return fail(SQAP_EINVAL, "%s: workspace of %zu bytes needed, %zu given", who, need, workspace ? workspace_bytes : (size_t)0);
     if (!aligned16(workspace)) return fail(SQAP_EINVAL, "%s: workspace must be 16-byte aligned", who);
+    // An element's outputs are written while others' inputs are still to be read.  Scores and flags in place are read before, by the workgroup that writes them.
+    const size_t rows = (size_t)batch * beams, in = 4 * rows, out = 4 * (size_t)batch * k;
+    const Range read[] = {{logits, 2 * ((rows - 1) * (size_t)ld + vocab)}, {scores, in}, {done, in}};
+    const Range written[] = {{workspace, need}, {parent_out, out}, {token_out, out}, {score_out, out}, {done_out, out}};
+    for (int w = 0; w < 5; ++w) {
+        for (int r = 0; r < 3; ++r)
+            if (overlap(written[w], read[r]) && !(k == beams && written[w].at == read[r].at && ((w == 3 && r == 1) || (w == 4 && r == 2))))
+                return fail(SQAP_EINVAL, "%s: outputs or the workspace lie over inputs", who);
+        for (int v = 0; v < w; ++v)
+            if (overlap(written[w], written[v])) return fail(SQAP_EINVAL, "%s: outputs and the workspace lie over one another", who);
+    }
     const DeviceOfCall device;
     return launch_beam_select(reinterpret_cast<const __half *>(logits), ld, batch, beams, vocab, scores, done, eos, k, parent_out, token_out, score_out,
                               done_out, workspace, as_stream(stream));
