@@ -558,7 +558,8 @@ sqap_status sqap_cache8_read(const sqap_cache8 *cache, const int32_t *lengths, i
  *
  * longest, longest_prefix: the most own positions (the new one included) and the longest prefix as far as the host knows; they decide how the work
  * is split, nothing else.  workspace: at least sqap_cache8_shared_workspace_bytes(cache->batch, prefix->batch, H, kv_heads, head_dim, rows, max_new, longest,
- * longest_prefix) bytes (a decode call: rows = cache->batch, max_new = 1; a prompt: longest = 1 will do), 16-byte aligned, of any contents (may be NULL where
+ * longest_prefix) bytes (a decode call: rows = cache->batch, max_new = 1; a prompt: longest = 1 will do; where those are the same the answer is for
+ * either, and a prompt may ask for less), 16-byte aligned, of any contents (may be NULL where
  * that is 0); its first 16384 bytes are left alone, so that it may be that of the other calls.  Calls that share a workspace must be ordered on one stream; graphs that
  * are replayed side by side need one each.
  *

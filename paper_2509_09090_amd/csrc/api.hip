@@ -879,7 +879,9 @@ size_t sqap_cache8_shared_workspace_bytes(int32_t batch, int32_t groups, int32_t
     if (batch <= 0 || groups <= 0 || batch % groups != 0 || H <= 0 || kv_heads <= 0 || H % kv_heads != 0 || head_dim <= 0 || rows <= 0 || max_new <= 0 ||
         longest <= 0 || longest_prefix < 0)
         return 0;
-    return cache8_shared_workspace_bytes(batch, groups, H, kv_heads, head_dim, rows, max_new < rows ? max_new : rows, longest, longest_prefix);      // (as the call)
+    max_new = max_new < rows ? max_new : rows;                        // (as the call)
+    // (a row for each sequence: single rows, or a prompt, which asks for no more)
+    return cache8_shared_workspace_bytes(max_new > 1 || rows != batch, batch, groups, H, kv_heads, head_dim, rows, max_new, longest, longest_prefix);
 }
 
 sqap_status sqap_cache8_shared_attention(const sqap_f16 *Q, int64_t ldq, const int32_t *starts, const int32_t *past, int32_t rows, int32_t max_new,
@@ -898,15 +900,14 @@ sqap_status sqap_cache8_shared_attention(const sqap_f16 *Q, int64_t ldq, const i
     if (s == SQAP_OK) s = check_rows16(who, "O", O, ldo, width);
     if (s != SQAP_OK) return s;
     max_new = max_new < rows ? max_new : rows;
-    const int G = H / cache->kv_heads;
-    const int64_t pairs = (int64_t)max_new * G, together = (int64_t)(cache->batch / prefix->batch) * max_new;
+    const int G = H / cache->kv_heads, announced = max_new > 0 ? max_new : 1;        // (none: any rows there are are too many)
+    const int64_t pairs = (int64_t)announced * G, together = (int64_t)(cache->batch / prefix->batch) * announced;
     const int64_t of_group = (together < rows ? together : rows) * G;
     if (of_group > INT32_MAX - 128 || (pairs + 127) / 128 * cache->kv_heads * cache->batch > most_workgroups(256) ||
         (of_group + 127) / 128 * cache->kv_heads * prefix->batch > most_workgroups(256))
         return fail(SQAP_EUNSUPPORTED, "%s: %d rows of %d heads", who, max_new, H);
-    const int announced = max_new > 0 ? max_new : 1;                  // (none: any rows there are are too many)
     s = check_workspace(who, workspace, workspace_bytes,
-                        cache8_shared_workspace_bytes(cache->batch, prefix->batch, H, cache->kv_heads, cache->head_dim, rows, announced, 1, longest_prefix));
+                        cache8_shared_workspace_bytes(true, cache->batch, prefix->batch, H, cache->kv_heads, cache->head_dim, rows, max_new, 1, longest_prefix));
     if (s != SQAP_OK) return s;
     const DeviceOfCall device;
     return launch_cache8_shared(reinterpret_cast<const __half *>(Q), ldq, starts, past, rows, max_new, H, v, p, prefix_len, longest_prefix, cache->head_dim,
@@ -935,7 +936,7 @@ sqap_status sqap_cache8_shared_decode_attention(const sqap_f16 *QKV, int64_t ld,
     if (own + tiles * cache->kv_heads * prefix->batch > most_workgroups(256) - 512)
         return fail(SQAP_EUNSUPPORTED, "%s: %d sequences of %d heads", who, cache->batch, H);
     s = check_workspace(who, workspace, workspace_bytes,
-                        cache8_shared_workspace_bytes(cache->batch, prefix->batch, H, cache->kv_heads, cache->head_dim, cache->batch, 1, longest, longest_prefix));
+                        cache8_shared_workspace_bytes(false, cache->batch, prefix->batch, H, cache->kv_heads, cache->head_dim, cache->batch, 1, longest, longest_prefix));
     if (s != SQAP_OK) return s;
     const DeviceOfCall device;
     return launch_cache8_shared_decode(reinterpret_cast<const __half *>(QKV), ld, pos, past, H, base, v, p, prefix_len, cache->head_dim, longest, longest_prefix,

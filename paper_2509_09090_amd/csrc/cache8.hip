@@ -2402,7 +2402,7 @@ static SharedPlan shared_plan(bool prompt, int batch, int groups, int H, int kv_
     p.own_shares = own_shares;
     p.pairs = (int64_t)rows * H;
     const auto up = [](size_t n) { return (n + 15) / 16 * 16; };
-    const int64_t tiles = ((int64_t)max_new * (H / kv_heads) + 15) / 16 * kv_heads * batch;          // of 16
+    const int64_t tiles = ((int64_t)std::max(1, max_new) * (H / kv_heads) + 15) / 16 * kv_heads * batch;          // of 16
     // rows that fill three quarters of a tile of 128 on average, 64 of those (128 rows of 32 heads over 8, 32 tiles, behind 2000 positions 47 us and 20
     // otherwise, behind 20000 110 and 91; 64 tiles behind 2000 46 and 45; 330 behind 6000 194 and 279), and more than a start's worth of work: the kernel
     // takes 36 us at the least (8 x 148 rows behind 100 positions, 7104 blocks of tiles of 16: 47 us and 33; 300 behind 1000, 11400: 46 and 37; 16 x 100
@@ -2417,8 +2417,9 @@ static SharedPlan shared_plan(bool prompt, int batch, int groups, int H, int kv_
         return p;
     }
     p.waves = tiles <= kShortTiles ? kFewRowsWaves : 2;
-    p.direct = prompt && (tiles <= kShortTiles ? tiles * blocks <= kShortBlocks && (blocks <= kShortPrefix || tiles >= 256)
-                                               : tiles <= most_workgroups(256) && tiles * 16 * blocks < kShortRepeats * (int64_t)rows * H);
+    // (no rows announced: NaN for those there are)
+    p.direct = prompt && (max_new == 0 || (tiles <= kShortTiles ? tiles * blocks <= kShortBlocks && (blocks <= kShortPrefix || tiles >= 256)
+                                                                : tiles <= most_workgroups(256) && tiles * 16 * blocks < kShortRepeats * (int64_t)rows * H));
     if (p.direct) return p;                                           // (no workspace)
     p.q = kCounterBytes;                                              // (left alone, for calls that want it zero)
     p.ml = p.q + (max_new == 1 ? up((size_t)p.pairs * d * 2) : 0);
@@ -2431,9 +2432,9 @@ static int own_shares_of(int batch, int H, int kv_heads, int longest)
     return std::min(decode_shares(batch, H, kv_heads, longest), kMostParts - kMostPrefixShares);
 }
 
-size_t cache8_shared_workspace_bytes(int batch, int groups, int H, int kv_heads, int d, int rows, int max_new, int longest, int longest_prefix)
+size_t cache8_shared_workspace_bytes(bool prompt, int batch, int groups, int H, int kv_heads, int d, int rows, int max_new, int longest, int longest_prefix)
 {
-    return shared_plan(max_new > 1, batch, groups, H, kv_heads, d, rows, max_new, max_new == 1 ? own_shares_of(batch, H, kv_heads, longest) : 1, longest_prefix).bytes;
+    return shared_plan(prompt, batch, groups, H, kv_heads, d, rows, max_new, prompt ? 1 : own_shares_of(batch, H, kv_heads, longest), longest_prefix).bytes;
 }
 
 template <int D>

@@ -260,7 +260,7 @@ sqap_status launch_cache8_decode(const __half *QKV, int64_t ld, const int32_t *p
                                  int d, int longest, __half *O, int64_t ldo, void *workspace, hipStream_t st);
 sqap_status launch_cache8_read(const Cache8View &cache, int d, const int32_t *lengths, int first, int count, __half *out, int64_t ld, hipStream_t st);
 
-size_t cache8_shared_workspace_bytes(int batch, int groups, int H, int kv_heads, int d, int rows, int max_new, int longest, int longest_prefix);
+size_t cache8_shared_workspace_bytes(bool prompt, int batch, int groups, int H, int kv_heads, int d, int rows, int max_new, int longest, int longest_prefix);
 sqap_status launch_cache8_shared(const __half *Q, int64_t ldq, const int32_t *starts, const int32_t *past, int rows, int max_new, int H, const Cache8View &cache,
                                  const Cache8View &prefix, const int32_t *length, int longest_prefix, int d, __half *O, int64_t ldo, void *workspace, hipStream_t st);
 sqap_status launch_cache8_shared_decode(const __half *QKV, int64_t ld, const int32_t *pos, const int32_t *past, int H, double base, const Cache8View &cache,

@@ -49,3 +49,35 @@ def test_rows_of_another_group(G, groups, hint, by):
         got = o.cpu().numpy()
         s.check(got, y, counts, skip=skipped)
         assert all(np.all(got[at[b]:at[b + 1]] == 9) for b in skipped), starts
+
+
+@pytest.mark.parametrize("rows,most,longest_prefix,none", [(20, 1, 500, True), (8, 1, 500, False), (8, 2, 500, True), (20, 1, FAR, False), (20, 0, FAR, True)])
+def test_workspace_of_a_row_each(rows, most, longest_prefix, none):
+    """Prompts of one row to a sequence ask for what longer ones of as little work do; a row for each of the eight sequences may be single rows', too."""
+    assert (B.sqap_cache8_shared_workspace_bytes(8, 2, 32, 32, 128, rows, most, 1, longest_prefix) == 0) == none
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("counts", [[1] * 8, [1, 0, 1, 1, 0, 1, 1, 1]])
+@pytest.mark.parametrize("padding", [0, 3])
+def test_prompts_of_a_row_each(G, counts, padding):
+    """Without a workspace; and the same with no rows announced: NaN for those there are."""
+    import torch
+    H, kv, d = 4, 2, 64
+    s = Shared(G, 2, 4, H, kv, d, [130, 70], seed=90)
+    s.own.append([9 * b for b in range(8)], attend=False)
+    before, total = s.own.past.copy(), sum(counts)
+    y = s.own.append(counts, pos=s.positions(counts), attend=False)
+    s.own.past = before
+    starts = G.to_dev(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32))
+    q = torch.zeros((total + padding, H * d), dtype=torch.float16, device=G.DEV)
+    q[:total] = G.to_dev(np.ascontiguousarray(y[:, :H]).reshape(total, -1))
+    for most, hint in ((1, 130), (0, 130), (0, FAR)):
+        o = torch.full_like(q, 9.0)
+        B.sqap_cache8_shared_attention(q, starts, G.to_dev(before), s.own.cache, s.prefix.cache, s.device_lengths, H, most, o, None, hint)
+        got = o.cpu().numpy()
+        assert np.all(got[total:] == 9)
+        if most:
+            s.check(got[:total], y, counts)
+        else:
+            assert np.all(np.isnan(got[:total]))
