@@ -865,6 +865,30 @@ static sqap_status check_prefix(const char *who, const sqap_cache8 *cache, const
     return SQAP_OK;
 }
 
+// a range of memory (null: none), and whether two of them lie over each other
+struct Range {
+    const void *at;
+    size_t bytes;
+};
+static bool overlap(const Range &x, const Range &y)
+{
+    const uintptr_t a = reinterpret_cast<uintptr_t>(x.at), b = reinterpret_cast<uintptr_t>(y.at);
+    return x.at && y.at && a < b + y.bytes && b < a + x.bytes;
+}
+
+// The sequences and their prefixes in memory of their own: positions are appended to the ones while the others are read.
+static sqap_status check_apart(const char *who, const sqap_cache8 *cache, const sqap_cache8 *prefix)
+{
+    auto buffer = [](const sqap_cache8 *c, int i) {
+        const size_t heads = (size_t)c->batch * c->kv_heads, blocks = heads * (c->capacity / kCache8Block);
+        return i == 0 ? Range{c->codes, blocks * 2 * kCache8Block * c->head_dim}
+               : i == 1 ? Range{c->scales, blocks * 2 * sizeof(float)} : Range{c->tail, heads * 2 * kCache8Block * c->head_dim * sizeof(sqap_f16)};
+    };
+    for (int i = 0; i < 9; ++i)
+        if (overlap(buffer(cache, i / 3), buffer(prefix, i % 3))) return fail(SQAP_EINVAL, "%s: buffers of the sequences lie over their prefixes'", who);
+    return SQAP_OK;
+}
+
 static sqap_status check_workspace(const char *who, const void *workspace, size_t bytes, size_t need)
 {
     if (need == 0) return SQAP_OK;
@@ -908,6 +932,7 @@ sqap_status sqap_cache8_shared_attention(const sqap_f16 *Q, int64_t ldq, const i
         return fail(SQAP_EUNSUPPORTED, "%s: %d rows of %d heads", who, max_new, H);
     s = check_workspace(who, workspace, workspace_bytes,
                         cache8_shared_workspace_bytes(true, cache->batch, prefix->batch, H, cache->kv_heads, cache->head_dim, rows, max_new, 1, longest_prefix));
+    if (s == SQAP_OK) s = check_apart(who, cache, prefix);
     if (s != SQAP_OK) return s;
     const DeviceOfCall device;
     return launch_cache8_shared(reinterpret_cast<const __half *>(Q), ldq, starts, past, rows, max_new, H, v, p, prefix_len, longest_prefix, cache->head_dim,
@@ -937,21 +962,11 @@ sqap_status sqap_cache8_shared_decode_attention(const sqap_f16 *QKV, int64_t ld,
         return fail(SQAP_EUNSUPPORTED, "%s: %d sequences of %d heads", who, cache->batch, H);
     s = check_workspace(who, workspace, workspace_bytes,
                         cache8_shared_workspace_bytes(false, cache->batch, prefix->batch, H, cache->kv_heads, cache->head_dim, cache->batch, 1, longest, longest_prefix));
+    if (s == SQAP_OK) s = check_apart(who, cache, prefix);
     if (s != SQAP_OK) return s;
     const DeviceOfCall device;
     return launch_cache8_shared_decode(reinterpret_cast<const __half *>(QKV), ld, pos, past, H, base, v, p, prefix_len, cache->head_dim, longest, longest_prefix,
                                        reinterpret_cast<__half *>(O), ldo, workspace, as_stream(stream));
-}
-
-// a range of memory (null: none), and whether two of them lie over each other
-struct Range {
-    const void *at;
-    size_t bytes;
-};
-static bool overlap(const Range &x, const Range &y)
-{
-    const uintptr_t a = reinterpret_cast<uintptr_t>(x.at), b = reinterpret_cast<uintptr_t>(y.at);
-    return x.at && y.at && a < b + y.bytes && b < a + x.bytes;
 }
 
 sqap_status sqap_cache8_reorder(const sqap_cache8 *cache, const int32_t *parents, int32_t width, const int32_t *lengths, int32_t longest,

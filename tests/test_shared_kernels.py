@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 
 from paper_2509_09090_amd import binding as B
+from tests.test_cache8 import BASE, P, _desc
 from tests.test_shared import Shared
 
 ALONE, TOGETHER, PARTS = "tiles of 16 by themselves", "blocks of all tiles dealt out", "prefix and own positions in parts"
@@ -81,3 +82,45 @@ def test_prompts_of_a_row_each(G, counts, padding):
             s.check(got[:total], y, counts)
         else:
             assert np.all(np.isnan(got[:total]))
+
+
+PREFIX, CACHE = dict(batch=2, capacity=1024, kv_heads=2, head_dim=64), dict(batch=4, capacity=320, kv_heads=2, head_dim=64)
+
+
+def _sizes(batch, capacity, kv_heads, head_dim):
+    blocks = batch * kv_heads * (capacity // 64)
+    return dict(codes=blocks * 128 * head_dim, scales=8 * blocks, tail=batch * kv_heads * 256 * head_dim)
+
+
+@pytest.mark.parametrize("decode", [False, True])
+@pytest.mark.parametrize("mine", ("codes", "scales", "tail"))
+@pytest.mark.parametrize("front", ("codes", "scales", "tail"))
+def test_a_prefix_over_the_sequences(decode, mine, front):
+    """One of the buffers over another's beginning or end (no GPU: all of these are refused)."""
+    L, far = B.lib(), {x: (i + 1) << 24 for i, x in enumerate(("codes", "scales", "tail"))}
+    cache = _desc(**CACHE, **far)
+    size, over = _sizes(**PREFIX)[front], _sizes(**CACHE)[mine]
+    for at in (far[mine], far[mine] + over - 16, far[mine] - size + 16):
+        prefix = _desc(**PREFIX, **{**{x: y << 4 for x, y in far.items()}, front: at})
+        need = B.sqap_cache8_shared_workspace_bytes(4, 2, 4, 2, 64, 4, 1, 320, 1000)
+        if decode:
+            status = L.sqap_cache8_shared_decode_attention(P, 512, P, P, 4, BASE, cache, prefix, P, 320, 1000, P, 256, P, need, None)
+        else:
+            status = L.sqap_cache8_shared_attention(P, 256, P, P, 4, 1, 4, cache, prefix, P, 1000, P, 256, P, need, None)
+        assert status == B.EINVAL, at
+
+
+@pytest.mark.gpu
+def test_a_prefix_beside_the_sequences(G):
+    """Prefixes and sequences in one allocation, end to end."""
+    import torch
+    s = Shared(G, 2, 2, 4, 2, 64, [130, 70], capacity=192, seed=91)
+    for name in ("codes", "scales", "tail"):
+        of = [getattr(x.cache, name) for x in (s.own, s.prefix)]
+        both = torch.cat([x.flatten() for x in of])
+        for model, x, part in zip((s.own, s.prefix), of, both.split([x.numel() for x in of])):
+            setattr(model.cache, name, part.view(x.shape))
+            setattr(model.cache._desc, name, part.data_ptr())
+    s.prompt([5, 0, 70, 1])
+    s.decode()
+    s.own.check_contents()
