@@ -521,7 +521,8 @@ def sqap_cache8_shared_workspace_bytes(batch, groups, H, kv_heads, head_dim, row
 
 def sqap_cache8_shared_attention(Q, starts, past, cache, prefix, prefix_len, H, max_new, O, workspace, longest_prefix, stream=None):
     """As sqap_cache8_attention, for sequences in groups behind the sequences of another Cache8, `prefix`, which hold prefix_len [groups]
-    int32 positions; past counts a sequence's own ones.  workspace: device bytes (see sqap_cache8_shared_workspace_bytes)."""
+    int32 positions; past counts a sequence's own ones.  workspace: device bytes (see sqap_cache8_shared_workspace_bytes).  This call and the three below
+    raise ValueError for tensors that are shorter than said, or not in one piece where they have no pitch."""
     _native.cache8_shared_attention(Q, starts, past, cache.handle, prefix.handle, prefix_len, H, max_new, O, workspace, longest_prefix, stream)
 
 

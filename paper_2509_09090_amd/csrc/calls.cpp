@@ -142,6 +142,39 @@ void of_rows(int64_t have, int64_t rows)
     throw PyFailed{};
 }
 
+void at_least(const char *what, int64_t have, int64_t need)
+{
+    if (have >= need) return;
+    PyErr_Format(PyExc_ValueError, "%s: %lld where %lld are needed", what, (long long)have, (long long)need);
+    throw PyFailed{};
+}
+
+bool says(PyObject *answer)                // (takes it over)
+{
+    const Ref v(answer);
+    const int yes = PyObject_IsTrue(v.p);
+    check(yes >= 0);
+    return yes;
+}
+
+// a tensor of which a call reads or writes so many 32-bit words, one behind the other (None: it does not)
+void holds(const char *what, PyObject *o, int64_t words)
+{
+    if (o == Py_None) return;
+    if (!(plain(o) ? THPVariable_Unpack(o).is_contiguous() : says(PyObject_CallMethod(o, "is_contiguous", nullptr)))) {
+        PyErr_Format(PyExc_ValueError, "%s: not in one piece", what);
+        throw PyFailed{};
+    }
+    at_least(what, (int64_t)(bytes(o) / 4), words);
+}
+bool on_device(PyObject *o) { return o != Py_None && (plain(o) ? THPVariable_Unpack(o).is_cuda() : says(PyObject_GetAttrString(o, "is_cuda"))); }
+
+int64_t batch_of(PyObject *cache)          // sequences of a cache (a handle; null: the call says so)
+{
+    const sqap_cache8 *c = handle<sqap_cache8>(cache);
+    return c ? c->batch : 0;
+}
+
 int64_t rows_of(PyObject *X, PyObject *rows) { return rows == Py_None ? size(X, 0) : count(rows); }
 
 struct Calls {
@@ -287,21 +320,39 @@ SQAP_METHOD(sample, 9,
                 ptr<int32_t>(a[2]), ptr<float>(a[3]), ptr<float>(a[4]), ptr<float>(a[5]), ptr<int32_t>(a[6]), ptr<float>(a[7]), stream(c, a[8])))
 // (Q, starts, past, cache, prefix, prefix_len, H, max_new, O, workspace, longest_prefix, stream)
 SQAP_METHOD(cache8_shared_attention, 12,
-            run(c->cache8_shared_attention, ptr<sqap_f16>(a[0]), pitch(a[0]), ptr<int32_t>(a[1]), ptr<int32_t>(a[2]), (int32_t)size(a[0], 0), as_i32(a[7]),
-                as_i32(a[6]), handle<sqap_cache8>(a[3]), handle<sqap_cache8>(a[4]), ptr<int32_t>(a[5]), as_i32(a[10]), ptr<sqap_f16>(a[8]), pitch(a[8]),
-                ptr(a[9]), bytes(a[9]), stream(c, a[11])))
+            (holds("starts", a[1], batch_of(a[3]) + 1), holds("past", a[2], batch_of(a[3])), holds("prefix_len", a[5], batch_of(a[4])),
+             holds("workspace", a[9], 0), at_least("rows of O", size(a[8], 0), size(a[0], 0)),
+             run(c->cache8_shared_attention, ptr<sqap_f16>(a[0]), pitch(a[0]), ptr<int32_t>(a[1]), ptr<int32_t>(a[2]), (int32_t)size(a[0], 0), as_i32(a[7]),
+                 as_i32(a[6]), handle<sqap_cache8>(a[3]), handle<sqap_cache8>(a[4]), ptr<int32_t>(a[5]), as_i32(a[10]), ptr<sqap_f16>(a[8]), pitch(a[8]),
+                 ptr(a[9]), bytes(a[9]), stream(c, a[11]))))
 // (QKV, pos, past, cache, prefix, prefix_len, H, O, workspace, longest, longest_prefix, base, stream)
 SQAP_METHOD(cache8_shared_decode_attention, 13,
-            run(c->cache8_shared_decode_attention, ptr<sqap_f16>(a[0]), pitch(a[0]), ptr<int32_t>(a[1]), ptr<int32_t>(a[2]), as_i32(a[6]), as_double(a[11]),
-                handle<sqap_cache8>(a[3]), handle<sqap_cache8>(a[4]), ptr<int32_t>(a[5]), as_i32(a[9]), as_i32(a[10]), ptr<sqap_f16>(a[7]), pitch(a[7]),
-                ptr(a[8]), bytes(a[8]), stream(c, a[12])))
+            (at_least("rows of QKV", size(a[0], 0), batch_of(a[3])), at_least("rows of O", size(a[7], 0), batch_of(a[3])), holds("pos", a[1], batch_of(a[3])),
+             holds("past", a[2], batch_of(a[3])), holds("prefix_len", a[5], batch_of(a[4])), holds("workspace", a[8], 0),
+             run(c->cache8_shared_decode_attention, ptr<sqap_f16>(a[0]), pitch(a[0]), ptr<int32_t>(a[1]), ptr<int32_t>(a[2]), as_i32(a[6]), as_double(a[11]),
+                 handle<sqap_cache8>(a[3]), handle<sqap_cache8>(a[4]), ptr<int32_t>(a[5]), as_i32(a[9]), as_i32(a[10]), ptr<sqap_f16>(a[7]), pitch(a[7]),
+                 ptr(a[8]), bytes(a[8]), stream(c, a[12]))))
 // (cache, parents [groups, width], lengths, longest, lengths_out, stream)
 SQAP_METHOD(cache8_reorder, 6,
-            run(c->cache8_reorder, handle<sqap_cache8>(a[0]), ptr<int32_t>(a[1]), (int32_t)size_of(a[1], 2, 1), ptr<int32_t>(a[2]), as_i32(a[3]),
-                ptr<int32_t>(a[4]), stream(c, a[5])))
+            (holds("parents", a[1], batch_of(a[0])), holds("lengths", a[2], batch_of(a[0])), holds("lengths_out", a[4], batch_of(a[0])),
+             run(c->cache8_reorder, handle<sqap_cache8>(a[0]), ptr<int32_t>(a[1]), (int32_t)size_of(a[1], 2, 1), ptr<int32_t>(a[2]), as_i32(a[3]),
+                 ptr<int32_t>(a[4]), stream(c, a[5]))))
 // (logits, scores [batch, beams], done, eos, parents [batch, k], tokens, scores, done, workspace, stream)
+void beam_arguments(PyObject *const *a)
+{
+    const int64_t batch = size_of(a[1], 2, 0), beams = size_of(a[1], 2, 1), k = size_of(a[4], 2, 1);
+    of_rows(size_of(a[0], 2, 0), batch * beams);
+    of_rows(size(a[4], 0), batch);
+    holds("scores", a[1], batch * beams);
+    holds("done", a[2], batch * beams);
+    holds("parent_out", a[4], batch * k);
+    holds("token_out", a[5], batch * k);
+    holds("score_out", a[6], batch * k);
+    if (on_device(a[7])) holds("done_out", a[7], batch * k);          // (one on the host is a stand-in: no kernel writes there)
+    holds("workspace", a[8], 0);
+}
 SQAP_METHOD(beam_select, 10,
-            (of_rows(size_of(a[0], 2, 0), size_of(a[1], 2, 0) * size_of(a[1], 2, 1)), of_rows(size_of(a[4], 2, 0), size_of(a[1], 2, 0)),
+            (beam_arguments(a),
              run(c->beam_select, ptr<sqap_f16>(a[0]), pitch(a[0]), (int32_t)size(a[1], 0), (int32_t)size(a[1], 1), (int32_t)size(a[0], 1),
                  ptr<float>(a[1]), ptr<int32_t>(a[2]), as_i32(a[3]), (int32_t)size(a[4], 1), ptr<int32_t>(a[4]), ptr<int32_t>(a[5]),
                  ptr<float>(a[6]), ptr<int32_t>(a[7]), ptr(a[8]), bytes(a[8]), stream(c, a[9]))))
