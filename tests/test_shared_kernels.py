@@ -124,3 +124,120 @@ def test_a_prefix_beside_the_sequences(G):
     s.prompt([5, 0, 70, 1])
     s.decode()
     s.own.check_contents()
+
+
+# ---- blocks of all tiles dealt out over the device: tiles that are finished in one workgroup's range, that are cut, that have no rows
+
+def _dealt(s, counts, hint=FAR, padding=3, most=None):
+    rows, batch, groups = int(sum(counts)) + padding, len(s.own.past), len(s.lengths)
+    return kernels(batch, groups, s.H, s.kv, s.d, rows, max(counts) if most is None else most, hint) == TOGETHER
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("groups,width,H,kv,d,lengths,calls", [
+    (1, 1, 64, 4, 64, [100], [[300], [140]]),
+    (1, 2, 64, 2, 128, [0], [[96, 200], [130, 64]]),
+    (2, 3, 32, 4, 128, [700, 130], [[200, 33, 0, 129, 64, 301], [64, 0, 31, 127, 1, 64]]),
+    (3, 1, 48, 8, 64, [64, 0, 191], [[65, 100, 16], [1, 63, 128]]),
+    (1, 1, 64, 64, 128, [6000], [[130], [128]]),
+    (1, 3, 64, 1, 64, [3001], [[60, 70, 3], [9, 118, 2]]),
+    (1, 2, 40, 2, 128, [333], [[130, 77], [205, 1]]),
+    (1, 2, 64, 8, 64, [70], [[500, 600], [130, 25]]),                 # 552 tiles of 9 to 12 blocks: whole ones to a workgroup
+    (2, 1, 32, 1, 128, [1, 64], [[700, 640], [1, 270]]),
+])
+def test_dealt_out(G, groups, width, H, kv, d, lengths, calls):
+    """Outputs beside the queries and over them; behind own positions."""
+    s = Shared(G, groups, width, H, kv, d, lengths, capacity=960, seed=groups + 150)
+    for counts, in_place in zip(calls, (False, True)):
+        assert _dealt(s, counts)
+        s.prompt(counts, longest_prefix=FAR, in_place=in_place)
+    s.own.check_contents()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H,n", [(32, 110), (64, 470)])               # (mostly cut tiles; mostly whole ones)
+def test_dealt_out_with_infinite_values(G, H, n):
+    """Infinities and NaN in unfinished blocks of a prefix and of own positions, a prefix block of keys and a block of own values without a scale, scores
+    of minus infinity over a whole prefix."""
+    kv, d, lengths = 2, 64, [70, 130, 1]
+    rows = np.random.default_rng(8).standard_normal((201, H + 2 * kv, d)).astype(np.float16)
+    rows[66, H + kv, 3] = np.inf
+    rows[69, H + kv, 3], rows[69, H + kv + 1, 7] = -np.inf, np.nan
+    rows[80, H + 1, 5] = np.inf
+    s = Shared(G, 3, 1, H, kv, d, lengths, capacity=512, seed=161, prefix_rows=rows)
+    s.prefix.cache.tail[2, :, 0, 0, 5] = -float("inf")
+    s.prefix.k[2][0, :, 5] = -np.inf
+    x = s.own.rows(3 * n)
+    x[n - 10, H + kv, 9] = np.inf                                     # (unfinished: seen by the rows behind it alone)
+    x[n + 40, H + kv + 1, 2] = -np.inf                                # in a block that is finished
+    x[3 * n - 1, H + kv + 1, 2] = np.nan
+    assert n % 64 >= 10 and _dealt(s, [n] * 3)
+    s.prompt([n] * 3, x=x, longest_prefix=FAR, in_place=H == 32)
+
+
+@pytest.mark.gpu
+def test_dealt_out_that_does_not_fit(G):
+    """NaN where there is no room, more rows than announced, more in a group than announced together or a length that cannot be; padded ones, and those
+    whose starts lead elsewhere, left alone."""
+    import torch
+    H, kv, d, width = 16, 1, 64, 2
+    good = [70, 20, 64, 9, 30]
+    s = Shared(G, 5, width, H, kv, d, good, capacity=192, seed=162)
+    counts = [60, 40, 50, 45, 33, 70, 64, 64, 30, 90]
+    before = s.own.past.copy()
+    y = s.own.append(counts, pos=s.positions(counts), attend=False)
+    s.own.past = before
+    total, at = sum(counts), np.concatenate([[0], np.cumsum(counts)])
+    q = G.to_dev(np.ascontiguousarray(y[:, :H]).reshape(total, -1))
+    for most, lengths, past, starts, bad, left in (
+            (100, good, {1: -1, 3: 160}, {}, {3}, {1}),
+            (100, [70, -1, 64, 1000, 30], {}, {}, {2, 3, 6, 7}, set()),
+            (69, good, {}, {}, {5, 9}, set()),
+            (59, good, {}, {}, {0, 5, 6, 7, 8, 9}, set()),
+            (100, good, {}, {3: 700}, set(), {2, 3}),
+            (100, good, {}, {4: -5}, {5}, {2, 3, 4}),
+            (110, good, {}, {1: 105}, set(), {0, 1}),                 # rows 100 .. 104 are the next group's
+            (110, good, {}, {9: 420}, set(), {8, 9})):                # rows 420 .. 425 are the group's before
+        p, st = before.copy(), at.astype(np.int32)
+        for b, n in past.items():
+            p[b] = n
+        for b, n in starts.items():
+            st[b] = n
+        assert _dealt(s, counts, padding=0, most=most)
+        o = torch.full((total, H * d), 9.0, dtype=torch.float16, device=G.DEV)
+        B.sqap_cache8_shared_attention(q, G.to_dev(st), G.to_dev(p), s.own.cache, s.prefix.cache, G.to_dev(np.array(lengths, np.int32)), H, most, o,
+                                       s.workspace(total, most, 1, FAR), FAR)
+        got = o.cpu().numpy()
+        for b in range(10):
+            part = got[at[b]:at[b + 1]]
+            assert np.all(np.isnan(part)) if b in bad else np.all(part == 9) if b in left else True, (most, starts, b)
+        s.check(got, y, counts, skip=bad | left)
+
+
+@pytest.mark.gpu
+def test_dealt_out_and_replayed(G):
+    """A captured prompt call, replayed with other rows and lengths, with eager work between the replays."""
+    import torch
+    H, kv, d, total = 32, 2, 128, 300
+    s = Shared(G, 2, 2, H, kv, d, [500, 64], capacity=1024, seed=163)
+    q, o = (torch.zeros((total, H * d), dtype=torch.float16, device=G.DEV) for _ in range(2))
+    starts, past = torch.zeros((5,), dtype=torch.int32, device=G.DEV), torch.zeros((4,), dtype=torch.int32, device=G.DEV)
+    ws = s.workspace(total, 200, 1, FAR)
+    assert _dealt(s, [total], padding=0, most=200)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        B.sqap_cache8_shared_attention(q, starts, past, s.own.cache, s.prefix.cache, s.device_lengths, H, 200, o, ws, FAR)
+    for counts in ([100, 60, 70, 50], [200, 0, 1, 99], [3, 2, 1, 140], [0, 0, 0, 5]):
+        before, n = s.own.past.copy(), sum(counts)
+        y = s.own.append(counts, pos=s.positions(counts), attend=False)
+        q[:n] = G.to_dev(np.ascontiguousarray(y[:, :H]).reshape(n, -1))
+        starts.copy_(G.to_dev(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)))
+        past.copy_(G.to_dev(before))
+        o.fill_(9.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        after, s.own.past = s.own.past, before
+        s.check(o.cpu().numpy(), y, counts)
+        s.own.past = after
+        assert bool((o[n:] == 9).all())
