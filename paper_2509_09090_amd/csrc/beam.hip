@@ -599,7 +599,8 @@ template <int D, int WIDTH, typename V>
 static void launch_reorder(const Cache8View &cache, const int32_t *parents, int width, const int32_t *lengths, int longest, int32_t *lengths_out, hipStream_t st)
 {
     constexpr int SPLIT = 2 * kCache8Block * D / (int)sizeof(V) / 256;
-    const int block_groups = (int)std::min<int64_t>(std::max(1, longest / kCache8Block * SPLIT), 65536);
+    const int blocks = std::min(longest / kCache8Block, cache.blocks);         // (no cache holds more: groups without a block cost a launch 0.4 ns each)
+    const int block_groups = (int)std::min<int64_t>(std::max<int64_t>(1, (int64_t)blocks * SPLIT), 65536);
     const dim3 grid(block_groups + 2 * SPLIT + 1, cache.kv_heads, cache.batch / width);
     hipLaunchKernelGGL((cache8_reorder_kernel<D, WIDTH, V>), grid, dim3(256), 0, st, cache, parents, width, lengths, lengths_out, block_groups);
 }

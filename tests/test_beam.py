@@ -311,3 +311,33 @@ def test_fewer_than_asked_for(G, beams, vocab, k):
     logits[4 * beams:] = np.nan
     check(G, logits, scores, done, eos=vocab - 1, k=k)
     check(G, logits, scores, done, eos=0, k=k, odd=True)
+
+
+@pytest.mark.gpu
+def test_reorder_with_a_length_that_no_cache_has(G):
+    """`longest` decides how the work is split: one far beyond the capacity costs what the capacity does, not a launch for all those blocks."""
+    import torch
+    groups, width, kv, d, capacity = 16, 2, 32, 64, 192
+    rng = np.random.default_rng(9)
+    cache = B.Cache8(groups * width, capacity, kv, d, device=G.DEV)
+    held = [rng.integers(-128, 128, cache.codes.shape).astype(np.int8), rng.integers(0, 1 << 32, cache.scales.shape, dtype=np.uint32),
+            rng.integers(0, 1 << 16, cache.tail.shape).astype(np.uint16)]
+    views = (cache.codes, cache.scales.view(torch.int32), cache.tail.view(torch.int16))
+    lengths = np.resize(np.array([190, 70, 64], np.int32), groups * width)
+    parents = np.tile(np.array([1, 0], np.int32), (groups, 1))
+    want, _ = _moved(*held, parents, lengths, width, capacity)
+    ms = {}
+    for longest in (capacity, 2 ** 31 - 1, capacity, 2 ** 31 - 1):
+        for x, y in zip(views, held):
+            x.copy_(G.to_dev(y.view(np.int32) if y.dtype == np.uint32 else y.view(np.int16) if y.dtype == np.uint16 else y))
+        p, n = G.to_dev(parents), G.to_dev(lengths)
+        torch.cuda.synchronize()
+        start, stop = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        start.record()
+        B.sqap_cache8_reorder(cache, p, n, longest)
+        stop.record()
+        torch.cuda.synchronize()
+        ms[longest] = start.elapsed_time(stop)
+        for x, y in zip(views, want):
+            assert np.array_equal(x.cpu().numpy().view(y.dtype), y), longest
+    assert ms[2 ** 31 - 1] < 20 * ms[capacity] + 1.0, ms
