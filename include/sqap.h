@@ -625,8 +625,9 @@ sqap_status sqap_sample(const sqap_f16 *logits, int64_t ld, int32_t batch, int32
  * [batch * beams, vocab] (halves, pitch ld, any alignment), beam by beam; scores [batch, beams] binary32, device: the beams' sums of
  * logarithms.  A continuation's total is
  *   scores[beam] + (l[token] - log sum_v exp(l[v])),
- * and they are ranked by it, in binary64 (the sum of exponentials is off by some 2^-24 of itself); of equal totals the lower beam, then the
- * higher logit, then the lower token comes first.  -0 == +0; logits that are NaN or minus infinity have no probability; where there are infinite
+ * and they are ranked by it, in binary64; of equal totals the lower beam, then the higher logit, then the lower token comes first.  The exponentials
+ * are binary32's: the sum of a row is off by up to 45 x 2^-24 of itself (2.7e-6; 9 x 2^-24 where 128000 tokens lie 11 below the largest), all of a beam's totals
+ * by the same.  Within a beam the order is exact; totals of two beams that are nearer than twice that may come in either order.  -0 == +0; logits that are NaN or minus infinity have no probability; where there are infinite
  * ones, each of them has the same and the others none.  Continuations without a probability rank behind all others, at a total of minus infinity, the
  * lower beam and then the lower token first.
  * done: NULL, or [batch, beams] int32, device: a beam that has finished (not 0) has one continuation, the token eos at its own score, and its

@@ -1,8 +1,10 @@
 // Beam search: the best continuations of several beams over the vocabulary, and the reordering of a cache in 8 bits that follows.
 //
 // A token's total is s + (l - log sum exp l), the beam's score and its logarithm of a probability.  Within a beam totals order as the
-// logits do, so the best k of a beam are found on halves, and only they get a total, in binary64: two of them that differ do so by far
-// more than the sums of exponentials are off by.
+// logits do, so the best k of a beam are found on halves, and only they get a total, in binary64.  The order of two beams' totals depends on
+// their sums of exponentials, whose terms are binary32's.  A term 2^x of the largest is off by 0.9 |x| 2^-24 of itself for the roundings of x and of log2 e (in
+// parts, as sums are brought below larger logits: those add up to x), 2 units for its power, 3 for a sum of eight, 2 for each of at most 10 powers that bring it
+// below a larger one: (0.9 |x| + 25) 2^-24.  Terms with |x| > 20 are at most 2^(20 - |x|) of the sum, so the sum is off by no more than 45 x 2^-24 of itself.
 #include <algorithm>
 
 #include "common.h"
@@ -114,9 +116,9 @@ struct BeamArgs {
 // One workgroup per row and slab of 2048 PIECES logits, which it holds in registers.  The largest of each piece of eight, with the piece's place
 // below it, is a number of its own; at least k pieces are not below the k-th largest of the threads' largest, and the slab's
 // best k lie in those: any other piece has k logits before its own.  They go to LDS, a thread takes one of their logits each, and those that reach the
-// smallest of these maxima are listed and ranked.  128 rows of 128001 (32.8 MB) in 14.4 us, 2.3 TB/s: a slab's start, loads (6.2 of the 14.4, by themselves), one
-// exponential per logit, a search over 16 bits and the ranking follow one another, 2048 workgroups in two rounds, and a round's loads have nothing of their own to
-// hide behind; rows of one wavefront each, without barriers, 16.3.  4 rows of 32000 in 4.8 us: latency.
+// smallest of these maxima are listed and ranked.  128 rows of 128001 (32.8 MB) in 14.4 us, 2.3 TB/s: a slab's start and loads (6.2
+// of the 14.4, by themselves), one exponential per logit (3.1), a search over 16 bits, listing and ranking (5) follow one another, and the 1024 workgroups, four to a
+// compute unit, are all there at once (81 registers and 27.7 KB leave five), so that all load, then all compute; rows of one wavefront each, without barriers, 16.3.  4 rows of 32000 in 4.8 us: latency.
 template <int PIECES>
 __global__ __launch_bounds__(kBeamT) void beam_rows_kernel(const BeamArgs a)
 {

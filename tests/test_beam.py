@@ -341,3 +341,24 @@ def test_reorder_with_a_length_that_no_cache_has(G):
         for x, y in zip(views, want):
             assert np.array_equal(x.cpu().numpy().view(y.dtype), y), longest
     assert ms[2 ** 31 - 1] < 20 * ms[capacity] + 1.0, ms
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("vocab", [5000, 128001, 1 << 20])
+@pytest.mark.parametrize("below", [1.0, 3.75, 11.0, 13.875])
+def test_sums_of_flat_tails(G, vocab, below):
+    """All tokens but one as far below the largest: every term's exponent is rounded alike, so that nothing cancels.  Rising tails, too, whose sums are brought
+    below a larger logit again and again."""
+    logits = np.full((3, vocab), -below, np.float16)
+    logits[0, vocab // 3] = 0.0
+    logits[1] = (np.arange(vocab) // 256 % 64 * (below / 64) - below).astype(np.float16)
+    logits[2] += np.float16(1000.0)
+    logits[2, 1] = 1000.0
+    scores = np.array([[-0.25, -20.0, -1.5]], np.float32)
+    parent, token, score, _ = select(G, logits, scores, None, -1, 3)
+    for r in range(3):                                                # (each beam by itself, so that all of them come out)
+        check(G, logits[r:r + 1], scores[:, r:r + 1], k=4)
+    x = logits.astype(np.float64)
+    total = scores[0][:, None] + x - (np.log(np.exp(x - x.max(1, keepdims=True)).sum(1, keepdims=True)) + x.max(1, keepdims=True))
+    mine = total[parent[0], token[0]]
+    assert np.all(np.abs(score[0] - mine) <= LSE_OFF + 2.0 ** -24 * np.abs(mine))
