@@ -626,12 +626,12 @@ sqap_status sqap_sample(const sqap_f16 *logits, int64_t ld, int32_t batch, int32
  * logarithms.  A continuation's total is
  *   scores[beam] + (l[token] - log sum_v exp(l[v])),
  * and they are ranked by it, in binary64; of equal totals the lower beam, then the higher logit, then the lower token comes first.  The exponentials
- * are binary32's: the sum of a row is off by up to 45 x 2^-24 of itself (2.7e-6; 9 x 2^-24 where 128000 tokens lie 11 below the largest), all of a beam's totals
- * by the same.  Within a beam the order is exact; totals of two beams that are nearer than twice that may come in either order.  -0 == +0; logits that are NaN or minus infinity have no probability; where there are infinite
+ * are binary32's: the sum of a row is off by 38 x 2^-24 (2.3e-6) of itself at most (2^20 tokens, nearly all of them 3 to 14 below the largest: by 1.6 x 2^-24), all of a
+ * beam's totals by the same.  Within a beam the order is exact; totals of two beams that are nearer than twice that may come in either order.  -0 == +0; logits that are NaN or minus infinity have no probability; where there are infinite
  * ones, each of them has the same and the others none.  Continuations without a probability rank behind all others, at a total of minus infinity, the
  * lower beam and then the lower token first.
  * done: NULL, or [batch, beams] int32, device: a beam that has finished (not 0) has one continuation, the token eos at its own score, and its
- * logits are not read.  Beams whose score is NaN or minus infinity have none with a probability (so that a search may start with one beam).
+ * logits are not read (its other tokens have no probability).  Beams whose score is NaN or minus infinity have none with a probability (so that a search may start with one beam).
  * parent_out, token_out [batch, k] int32, score_out [batch, k] binary32 (the total, rounded once): best first; where beams * vocab is below k the rest
  * are -1, -1 and minus infinity.  done_out: NULL, or [batch, k] int32: 1 where the parent has finished or the token is eos, else 0.
  * With k = beams score_out may be scores, done_out done; otherwise outputs and workspace lie over none of the inputs (of logits: from the first row to

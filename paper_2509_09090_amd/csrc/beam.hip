@@ -4,7 +4,9 @@
 // logits do, so the best k of a beam are found on halves, and only they get a total, in binary64.  The order of two beams' totals depends on
 // their sums of exponentials, whose terms are binary32's.  A term 2^x of the largest is off by 0.9 |x| 2^-24 of itself for the roundings of x and of log2 e (in
 // parts, as sums are brought below larger logits: those add up to x), 2 units for its power, 3 for a sum of eight, 2 for each of at most 10 powers that bring it
-// below a larger one: (0.9 |x| + 25) 2^-24.  Terms with |x| > 20 are at most 2^(20 - |x|) of the sum, so the sum is off by no more than 45 x 2^-24 of itself.
+// below a larger one: (0.9 |x| + 25) 2^-24.  Terms with |x| > 14 are at most 2^(14 - |x|) of their slab's sum (slabs are joined in binary64),
+// so a sum is off by no more than 38 x 2^-24 of itself.  Most terms are near their own thread's largest, where the rounding is below a unit: flat tails of 2^20
+// logits, 3 to 14 below a largest one in each slab, are off by 1.6 units at most.
 #include <algorithm>
 
 #include "common.h"

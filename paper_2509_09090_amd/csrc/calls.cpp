@@ -318,23 +318,41 @@ SQAP_METHOD(cache8_decode_attention, 10,
 SQAP_METHOD(sample, 9,
             run(c->sample, ptr<sqap_f16>(a[0]), pitch(a[0]), (int32_t)size_of(a[0], 2, 0), (int32_t)size_of(a[0], 2, 1), ptr<float>(a[1]),
                 ptr<int32_t>(a[2]), ptr<float>(a[3]), ptr<float>(a[4]), ptr<float>(a[5]), ptr<int32_t>(a[6]), ptr<float>(a[7]), stream(c, a[8])))
+int64_t shared_arguments(PyObject *first, const char *what, int more, PyObject *past, PyObject *cache, PyObject *prefix, PyObject *length, PyObject *workspace)
+{
+    const int64_t batch = batch_of(cache);
+    holds(what, first, batch + more);
+    holds("past", past, batch);
+    holds("prefix_len", length, batch_of(prefix));
+    holds("workspace", workspace, 0);
+    return batch;
+}
+void single_rows(PyObject *QKV, PyObject *O, int64_t batch)
+{
+    at_least("rows of QKV", size(QKV, 0), batch);
+    at_least("rows of O", size(O, 0), batch);
+}
+void reorder_arguments(PyObject *parents, PyObject *lengths, PyObject *lengths_out, int64_t batch)
+{
+    holds("parents", parents, batch);
+    holds("lengths", lengths, batch);
+    holds("lengths_out", lengths_out, batch);
+}
 // (Q, starts, past, cache, prefix, prefix_len, H, max_new, O, workspace, longest_prefix, stream)
 SQAP_METHOD(cache8_shared_attention, 12,
-            (holds("starts", a[1], batch_of(a[3]) + 1), holds("past", a[2], batch_of(a[3])), holds("prefix_len", a[5], batch_of(a[4])),
-             holds("workspace", a[9], 0), at_least("rows of O", size(a[8], 0), size(a[0], 0)),
+            (shared_arguments(a[1], "starts", 1, a[2], a[3], a[4], a[5], a[9]), at_least("rows of O", size(a[8], 0), size(a[0], 0)),
              run(c->cache8_shared_attention, ptr<sqap_f16>(a[0]), pitch(a[0]), ptr<int32_t>(a[1]), ptr<int32_t>(a[2]), (int32_t)size(a[0], 0), as_i32(a[7]),
                  as_i32(a[6]), handle<sqap_cache8>(a[3]), handle<sqap_cache8>(a[4]), ptr<int32_t>(a[5]), as_i32(a[10]), ptr<sqap_f16>(a[8]), pitch(a[8]),
                  ptr(a[9]), bytes(a[9]), stream(c, a[11]))))
 // (QKV, pos, past, cache, prefix, prefix_len, H, O, workspace, longest, longest_prefix, base, stream)
 SQAP_METHOD(cache8_shared_decode_attention, 13,
-            (at_least("rows of QKV", size(a[0], 0), batch_of(a[3])), at_least("rows of O", size(a[7], 0), batch_of(a[3])), holds("pos", a[1], batch_of(a[3])),
-             holds("past", a[2], batch_of(a[3])), holds("prefix_len", a[5], batch_of(a[4])), holds("workspace", a[8], 0),
+            (single_rows(a[0], a[7], shared_arguments(a[1], "pos", 0, a[2], a[3], a[4], a[5], a[8])),
              run(c->cache8_shared_decode_attention, ptr<sqap_f16>(a[0]), pitch(a[0]), ptr<int32_t>(a[1]), ptr<int32_t>(a[2]), as_i32(a[6]), as_double(a[11]),
                  handle<sqap_cache8>(a[3]), handle<sqap_cache8>(a[4]), ptr<int32_t>(a[5]), as_i32(a[9]), as_i32(a[10]), ptr<sqap_f16>(a[7]), pitch(a[7]),
                  ptr(a[8]), bytes(a[8]), stream(c, a[12]))))
 // (cache, parents [groups, width], lengths, longest, lengths_out, stream)
 SQAP_METHOD(cache8_reorder, 6,
-            (holds("parents", a[1], batch_of(a[0])), holds("lengths", a[2], batch_of(a[0])), holds("lengths_out", a[4], batch_of(a[0])),
+            (reorder_arguments(a[1], a[2], a[4], batch_of(a[0])),
              run(c->cache8_reorder, handle<sqap_cache8>(a[0]), ptr<int32_t>(a[1]), (int32_t)size_of(a[1], 2, 1), ptr<int32_t>(a[2]), as_i32(a[3]),
                  ptr<int32_t>(a[4]), stream(c, a[5]))))
 // (logits, scores [batch, beams], done, eos, parents [batch, k], tokens, scores, done, workspace, stream)
