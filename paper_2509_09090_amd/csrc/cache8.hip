@@ -702,10 +702,10 @@ __device__ __forceinline__ void add_odd(__half *to, const __half *tail_v, int se
 // Rows are (query, head) pairs of the heads that share a key head, query first, 32 to a wavefront and WAVES wavefronts to a workgroup, so
 // that a block of keys and values is taken from memory and made halves once for all of them.  Everything is transposed (scores:
 // positions x rows), as in attention.hip: probabilities are the second product's operand where they were computed.
-// What bounds it is the vector ALU beside the matrix cores, 355 instructions to 48 matrix instructions per wavefront and block, a tenth of them
-// exponentials: 1500, 1115 and 1446 rows of 32 heads over 8 behind 2000, 1994 and 420 positions in some 270 us, 0.52 PFLOP/s (a library product of
-// halves reaches 1.24); with probabilities of one half, 32 matrix instructions and 305 others, it was 230, and the outputs 2.0e-4 of their norm
-// further off.  (Then the next block's scores multiplied between this one's probabilities, in the same wavefront: 335 us, the registers do not suffice.)
+// What bounds it is the vector ALU beside the matrix cores, 357 instructions to 48 matrix instructions per wavefront and block, a tenth of them
+// exponentials: 1500, 1115 and 1446 rows of 32 heads over 8 behind 2000, 1994 and 420 positions in some 285 us, 0.49 PFLOP/s (a library product of
+// halves reaches 1.24; keys read from LDS ahead of their products took 8 us off).  With probabilities of one half, 32 matrix instructions and 305 others, it
+// took 40 us less, and the outputs were 2.0e-4 of their norm further off.  (Then the next block's scores multiplied between this one's probabilities, in the same wavefront: 335 us, the registers do not suffice.)
 // A block's p = 2^(s - m) times its factor is one exponential, of s sk + (log2 factor - m); the sum of the probabilities is put right by the
 // factor once per block.  The hardware's exponential, logarithm and reciprocal are off by a unit of the last place of binary32 or so each, which is
 // less than the rounding of the scores and of the sums.
@@ -827,12 +827,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void cache8_attention_kernel(const _
 // ---------------------------------------------------------------- long prompts behind prefixes
 
 // Many rows to a sequence: tiles of 128 of one sequence pass over its prefix's blocks and then their own, and the blocks of all tiles together are
-// dealt out evenly, so that no compute unit ends early (2675 rows of 32 heads over 8 behind prefixes of 6000 and 2900: 300 us where whole tiles, or
-// equal shares of each, would take 430).  A tile inside a workgroup's range is finished there; of one over its ends, the workgroups leave their sums,
+// dealt out evenly, so that no compute unit ends early (2675 rows of 32 heads over 8 behind prefixes of 6000 and 2900, append and joining
+// included: 449 us, with the prefix and own positions in parts of whole tiles 527; 430 since keys are read ahead).  A tile inside a workgroup's range is finished there; of one over its ends, the workgroups leave their sums,
 // one at the beginning and one at the end of each range, and cache8_long_join_kernel adds them.  Ranges are counted in tiles as long as their
 // sequence's longest (a tile's real blocks, fewer where its rows see less, are parted in the same proportion).
-// 2675 rows of 32 heads over 8 behind 6000 and 2900 take 413 us, 2250 behind 2000 161; matrix cores busy for 43 in 100, 8.3 vector instructions beside each of
-// theirs, and the clock falls as more of both are issued (2.11 to 1.99 GHz: the power limit).
+// Of those 430 append is 20 and joining 15; 2250 rows behind 2000 take 189 with append (26) and joining (15).  Matrix cores are busy for 43 in 100 cycles, 8.3
+// vector instructions stand beside each of theirs, and the clock falls as more of both are issued (2.11 to 1.99 GHz: the power limit).
 constexpr int kLongBatch = 1024, kLongParts = 32, kLongLeast = 4, kLongTiles = 64, kLongWork = 16000;
 struct LongSlot {                // what a workgroup's first range belongs to, where it is the rest of a tile
     int b, kh, tile, first, count;       // the workgroup that begins the tile, how many have a share of it; count 0: none, or not its second
