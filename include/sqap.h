@@ -566,7 +566,8 @@ sqap_status sqap_cache8_read(const sqap_cache8 *cache, const int32_t *lengths, i
  * As above a sequence with past[b] < 0 or without rows is skipped; one whose rows do not fit or are more than max_new gets outputs of NaN; so do
  * the sequences of a group whose rows together are not within 0 .. rows or more than width * max_new, and of a prefix whose prefix_len is
  * negative or beyond its capacity (appended to they are all the same).  One whose starts do not lie in order, or outside those of its group's first and last, is skipped.
- * (Starts out of order can still give the same rows to two that are not skipped: those rows' outputs may then be anything.)
+ * (Starts out of order can make two sequences that are not skipped share rows, or two groups, from the first start to the last: the outputs of rows that they
+ * share may be anything.)
  * EINVAL, EUNSUPPORTED: as above; EINVAL also for a cache of prefixes of other heads or with a buffer over one of the sequences', a batch that is no multiple of
  * theirs, longest_prefix < 0; EUNSUPPORTED for more than 4095 sequences, rows of a group times H / kv_heads beyond 32 bits, a decode call of some 2^28 rows
  * times heads.
